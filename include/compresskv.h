@@ -81,7 +81,8 @@ enum {
   CKV_ERR_CUDA = -6,            /* a CUDA runtime call or kernel launch failed */
   CKV_ERR_DEVICE_TIMEOUT = -7,  /* a kernel's bounded wait ran out (device status only) */
   CKV_ERR_DEVICE_INDEX = -8,    /* an index outside its sequence: given to compresskv_gather, or
-                                   produced by a selection (a device self-check) */
+                                   produced by a selection (a device self-check); a row without
+                                   room in its unit of a 4-bit cache */
   CKV_ERR_STATIC_SCRATCH = -9   /* problem needs more than CKV_STATIC_SCRATCH_BYTES of scratch */
 };
 
@@ -119,7 +120,10 @@ enum {
   CKV_KERNEL_COMBINE = 2,       /* normalised scores summed over queries, then pooled */
   CKV_KERNEL_SELECT = 3,        /* pooling + top-k + window append */
   CKV_KERNEL_GATHER = 4,        /* retained K/V rows -> compressed cache */
-  CKV_KERNEL_FUSED = 5          /* all four steps for every unit of a call (persistent kernels) */
+  CKV_KERNEL_FUSED = 5,         /* all four steps for every unit of a call (persistent kernels) */
+  CKV_KERNEL_Q4_WRITE = 6,      /* rows into a 4-bit cache (append, gather) */
+  CKV_KERNEL_Q4_ATTEND = 7,     /* attention over a 4-bit cache */
+  CKV_KERNEL_Q4_EVICT = 8       /* eviction from a 4-bit cache */
 };
 
 /* Optional launch trace.  When ckv_problem.trace is non-null every kernel
@@ -365,6 +369,151 @@ int compresskv_compress_layer_noalloc(const ckv_problem* p, const void* q_win, c
                                       void* k_out, void* v_out, float* raw_scores,
                                       float* pooled_scores, int32_t* device_status,
                                       void* stream);
+
+/* ------------------------------------------------------------ 4-bit cache
+ * The cache that a model decodes over after the compression, with K and V in
+ * 4 bits (the paper combines its selection with such a cache, Sec. 4.6), and
+ * the steps of a decode loop over it: rows are written by
+ * compresskv_q4_gather (the retained rows of a compression) and
+ * compresskv_q4_append (new tokens), compresskv_q4_attend attends over it and
+ * accumulates how much attention each slot gets, and compresskv_q4_evict
+ * drops the slots that got the least.
+ *
+ * A unit is a (sequence, KV group), u = sequence * num_kv_heads + group, with
+ * `capacity` slots, of which the first lengths[u] are in use.  The order of
+ * the slots means nothing.  The layers of a model may be packed as blocks of
+ * sequences, as in compresskv_compress_layers; a layer's block is then a cache
+ * of its own (every buffer offset by its first sequence).
+ *
+ * A slot's row of K (and of V) is 128 codes of 4 bits, byte b holding channel
+ * 2b in its low and 2b + 1 in its high half, and 8 bf16 numbers: for each
+ * group of 32 channels a scale (first four) and a minimum (last four).  Code n
+ * stands for scale * n + minimum.  Of a group x_c: minimum m = min x rounded
+ * down to bf16, scale s = the smallest bf16 with 15 s >= fl32(max x - m),
+ * n_c = fl32(x_c - m) / s rounded to the nearest integer, ties to even (s = 0
+ * and n = 0 where all are equal).  A group that holds a NaN or an infinity, or
+ * whose spread is beyond fp32, has scale and minimum NaN.
+ *
+ * What is behind a unit's length is free: the calls may write there, and what
+ * it holds is never read as data.  A length outside 0..capacity counts as the
+ * nearer end.  Calls that use one workspace must not overlap on the GPU, and
+ * neither must two calls of which one writes a unit that the other uses. */
+typedef struct ckv_q4_cache {
+  int32_t batch;            /* sequences; at most 65535 units (batch * num_kv_heads) */
+  int32_t num_kv_heads;     /* 1..64 */
+  int32_t head_dim;         /* 128 */
+  int32_t capacity;         /* slots of a unit: a multiple of 32, at most 2^24 (2^31 - 1 in all units) */
+  void* k_codes;            /* uint8 [units][capacity][64]; buffers are 16-byte aligned */
+  void* v_codes;
+  void* k_params;           /* bf16 [units][capacity][8] */
+  void* v_params;
+  int32_t* positions;       /* [units][capacity]: the token's position in its sequence */
+  float* weights;           /* [units][capacity]: accumulated attention; NULL: not kept */
+  int32_t* lengths;         /* [units], device; 4-byte aligned */
+  ckv_trace* trace;         /* optional launch trace, NULL for none */
+} ckv_q4_cache;
+
+/* Rows to append: of K and V, [rows][num_kv_heads][head_dim], head_dim
+ * contiguous, packed by sequence; base 16-byte aligned, strides multiples of
+ * 8 elements.  V may live in page-locked host memory. */
+typedef struct ckv_q4_rows {
+  int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16 */
+  int32_t rows_per_seq;     /* rows of every sequence, where cu_rows is NULL */
+  const int32_t* cu_rows;   /* host [batch+1] (batch <= 512): sequence s has rows cu_rows[s].. */
+  int64_t token_stride;     /* elements between rows */
+  int64_t head_stride;      /* elements between KV heads */
+} ckv_q4_rows;
+
+/* Query tokens: [batch][num_q_heads][num_queries][head_dim], head_dim
+ * contiguous, bases 16-byte aligned, strides multiples of 8 elements (`out`
+ * the same shape; its rows must not overlap). */
+typedef struct ckv_q4_queries {
+  int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads; head h uses group h / (its share) */
+  int32_t num_queries;      /* query tokens of a sequence: 1..16 */
+  int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16, of q and out */
+  int32_t accumulate;       /* non-zero: add the attention to the cache's weights */
+  float scale;              /* softmax scale; 0 selects 1/sqrt(head_dim) */
+  int64_t q_batch_stride, q_head_stride, q_query_stride;
+  int64_t out_batch_stride, out_head_stride, out_query_stride;
+} ckv_q4_queries;
+
+/* Bytes of workspace that compresskv_q4_attend (with these heads and query
+ * tokens, or fewer of either) and compresskv_q4_evict need for the cache;
+ * num_q_heads = num_queries = 0: for the eviction alone.  0 if invalid. */
+size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, int32_t num_queries);
+
+/* Zero the workspace's status word (256 bytes, on `stream`): once after
+ * allocating it and after reading a non-zero status
+ * (compresskv_read_device_status). */
+int compresskv_q4_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
+
+/* Quantise rows of new tokens into the cache, behind what it holds: row i of a
+ * sequence goes to slot start + i of each of its units, with weight 0 (where
+ * weights are kept), and the lengths become start + rows.
+ * positions: device int32 [rows], of each row.  A negative one marks padding:
+ *   that row and those behind it in its sequence are not appended (their
+ *   k_values / v_values are then unspecified).
+ * start: optional device int32 [units]; NULL: the cache's lengths.  Rows of
+ *   rejected speculative tokens are overwritten by starting below the length.
+ * k_values, v_values: optional, [rows][num_kv_heads][head_dim] contiguous in
+ *   the rows' dtype: the values that the codes stand for (what later steps
+ *   will read), for instance for the attention of a prompt's own chunk.
+ * Rows beyond the capacity are not written, and a unit whose start is outside
+ *   0..capacity keeps what it has; either sets *device_status (optional
+ *   device int32) to CKV_ERR_DEVICE_INDEX if it is 0. */
+int compresskv_q4_append(const ckv_q4_cache* c, const ckv_q4_rows* r, const void* k, const void* v,
+                         const int32_t* positions, const int32_t* start, void* k_values, void* v_values,
+                         int32_t* device_status, void* stream);
+
+/* compresskv_gather into the cache: quantise the retained rows of a
+ * compression into slots 0.. of each unit (what it held is replaced), with
+ * their indices as positions.  `p` describes K and V (batch and num_kv_heads
+ * as the cache's).
+ * group_major = 0: indices / cu_out as produced by compresskv_select or
+ *   compresskv_compress_layer(s); non-zero: as by
+ *   compresskv_compress_layer_head_budgets.  No unit may keep more rows than
+ *   the capacity (CKV_ERR_INVALID_ARG).
+ * raw_scores: optional device float, score layout: a prefix row's weight
+ *   starts as its raw score (the window's attention to it), else as 0.
+ * k_values, v_values: optional, the layout of the compression's k_out / v_out:
+ *   the values that the codes stand for.
+ * An index outside [0, L_s) is skipped (its slot keeps what it held) and
+ *   reported as CKV_ERR_DEVICE_INDEX in the status of `workspace` (a
+ *   workspace of either kind, or NULL to skip reporting). */
+int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t group_major,
+                         const int32_t* indices, const int32_t* cu_out, const void* k, const void* v,
+                         const float* raw_scores, void* k_values, void* v_values, void* workspace,
+                         void* stream);
+
+/* Attention of num_queries tokens a sequence over its units:
+ *   z_j = scale * q . K_j,  p = softmax of z over the visible slots,
+ *   out = sum_j p_j V_j (rounded to q's dtype),  lse = log sum_j exp(z_j),
+ * where K_j, V_j are the values that the slot's codes stand for.
+ * q_positions: optional device int32 [batch][num_queries]: a slot is visible
+ *   to a query whose position is at least the slot's; NULL: every slot in use
+ *   is.  A query that sees no slot gives out = 0 and lse = -infinity.
+ * lse: optional device float [batch][num_q_heads][num_queries].
+ * accumulate: p, summed over the queries and the group's heads, is added to
+ *   each visible slot's weight.
+ * Logits, softmax sums and outputs are held in fp32; the results do not
+ * depend on what else runs, and are the same bits on every call. */
+int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const void* q,
+                         const int32_t* q_positions, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Evict, in place, from every unit that holds more slots than its budget:
+ * kept are the `budget` slots with the largest accumulated weight, ties to
+ * the lower slot.  Before all others come slots whose position is below
+ * `sinks` or among the `recent` positions up to the unit's newest one.
+ * (budget = sinks + recent keeps the first tokens and a sliding window.)
+ * A NaN weight counts as the smallest.  The j-th evicted slot below the budget
+ * receives the j-th kept slot behind it, the other kept slots stay where they
+ * are, and the length becomes the budget.
+ * budgets: optional device int32 [units], instead of `budget`; a negative one
+ *   leaves its unit as it is, and one below sinks + recent keeps the lowest of
+ *   the protected slots.  A `budget` below sinks + recent is CKV_ERR_BUDGET. */
+int compresskv_q4_evict(const ckv_q4_cache* c, int32_t budget, const int32_t* budgets, int32_t sinks,
+                        int32_t recent, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Synchronise `stream`, copy the workspace status word to *status and return
  * CKV_OK (or CKV_ERR_CUDA if the copy fails). */

@@ -10,6 +10,7 @@ from .compresskv import (  # noqa: F401
     CompressKVError,
     LayerOutputs,
     Problem,
+    Q4Cache,
     Trace,
     allocate_layer_budgets,
     compress_layer,
@@ -23,6 +24,13 @@ from .compresskv import (  # noqa: F401
     head_budget_layout,
     load,
     output_layout,
+    q4_append,
+    q4_attend,
+    q4_cache,
+    q4_evict,
+    q4_gather,
+    q4_workspace,
+    q4_workspace_size,
     read_device_status,
     score,
     select,

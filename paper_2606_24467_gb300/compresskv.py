@@ -33,7 +33,9 @@ CKV_POOL_AVG = 0
 CKV_POOL_MAX = 1
 CKV_SELECT_PER_GROUP = 0
 CKV_SELECT_PER_LAYER = 1
-KERNEL_KINDS = {1: "score", 2: "combine", 3: "select", 4: "gather", 5: "fused"}
+KERNEL_KINDS = {1: "score", 2: "combine", 3: "select", 4: "gather", 5: "fused", 6: "q4_write",
+                7: "q4_attend", 8: "q4_evict"}
+Q4_TILE = 32  # a 4-bit cache's capacity is a multiple of this
 
 EXPORTED = (
     "compresskv_workspace_size",
@@ -52,6 +54,12 @@ EXPORTED = (
     "compresskv_debug_stall_next_fused_call",
     "compresskv_allocate_layer_budgets",
     "compresskv_status_string",
+    "compresskv_q4_workspace_size",
+    "compresskv_q4_workspace_init",
+    "compresskv_q4_append",
+    "compresskv_q4_gather",
+    "compresskv_q4_attend",
+    "compresskv_q4_evict",
 )
 
 
@@ -68,6 +76,26 @@ class CkvProblem(ctypes.Structure):
                 ("kv_token_stride", c_int64), ("kv_head_stride", c_int64),
                 ("q_batch_stride", c_int64), ("q_head_stride", c_int64),
                 ("q_win_stride", c_int64), ("trace", POINTER(CkvTrace))]
+
+
+class CkvQ4Cache(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32),
+                ("capacity", c_int32), ("k_codes", c_void_p), ("v_codes", c_void_p),
+                ("k_params", c_void_p), ("v_params", c_void_p), ("positions", c_void_p),
+                ("weights", c_void_p), ("lengths", c_void_p), ("trace", POINTER(CkvTrace))]
+
+
+class CkvQ4Rows(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("rows_per_seq", c_int32), ("cu_rows", c_void_p),
+                ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
+class CkvQ4Queries(ctypes.Structure):
+    _fields_ = [("num_q_heads", c_int32), ("num_queries", c_int32), ("dtype", c_int32),
+                ("accumulate", c_int32), ("scale", c_float),
+                ("q_batch_stride", c_int64), ("q_head_stride", c_int64),
+                ("q_query_stride", c_int64), ("out_batch_stride", c_int64),
+                ("out_head_stride", c_int64), ("out_query_stride", c_int64)]
 
 
 class CompressKVError(RuntimeError):
@@ -122,6 +150,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "compresskv_allocate_layer_budgets": (c_int32, [POINTER(ctypes.c_double), c_int32,
                                                         c_int64, c_int32, c_int32, i32p]),
         "compresskv_status_string": (ctypes.c_char_p, [c_int32]),
+        "compresskv_q4_workspace_size": (c_size_t, [vp, c_int32, c_int32]),
+        "compresskv_q4_workspace_init": (c_int32, [vp, c_size_t, vp]),
+        "compresskv_q4_append": (c_int32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "compresskv_q4_gather": (c_int32, [pp, vp, c_int32, vp, i32p, vp, vp, vp, vp, vp, vp, vp]),
+        "compresskv_q4_attend": (c_int32, [vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
+        "compresskv_q4_evict": (c_int32, [vp, c_int32, vp, c_int32, c_int32, vp, c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -504,3 +538,256 @@ class LayerOutputs:
         self.v_out = torch.empty_like(self.k_out)
         self.raw = torch.empty((H, int(cu_prefix[-1])), dtype=torch.float32, device=device) if scores else None
         self.pooled = torch.empty_like(self.raw) if scores else None
+
+
+# ------------------------------------------------------------------ 4-bit cache
+def _invalid(what: str):
+    raise CompressKVError(CKV_ERR_INVALID_ARG, what)
+
+
+def _q4_dtype(t: torch.Tensor) -> int:
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        _invalid("rows and queries must be f16 or bf16")
+    return CKV_DTYPE_BF16 if t.dtype == torch.bfloat16 else CKV_DTYPE_F16
+
+
+class Q4Cache:
+    """A 4-bit KV cache over the caller's tensors (wraps ``ckv_q4_cache``).
+
+    ``k_codes`` / ``v_codes`` are uint8 ``[B, H_kv, capacity, 64]`` (byte b:
+    channel 2b in the low half), ``k_params`` / ``v_params`` bfloat16
+    ``[B, H_kv, capacity, 8]`` (four scales, four minima, each of 32 channels),
+    ``positions`` int32 and ``weights`` float32 ``[B, H_kv, capacity]`` (the
+    latter may be None), ``lengths`` int32 ``[B, H_kv]``; all contiguous, on one
+    device, the capacity a multiple of 32.  The tensors stay the caller's and
+    are kept alive by this object."""
+
+    def __init__(self, k_codes, v_codes, k_params, v_params, positions, lengths, weights=None,
+                 trace: "Trace | None" = None):
+        if k_codes.dim() != 4:
+            _invalid("k_codes must be [B, H_kv, capacity, 64]")
+        lead = tuple(k_codes.shape[:3])
+        want = [("k_codes", k_codes, torch.uint8, lead + (64,)),
+                ("v_codes", v_codes, torch.uint8, lead + (64,)),
+                ("k_params", k_params, torch.bfloat16, lead + (8,)),
+                ("v_params", v_params, torch.bfloat16, lead + (8,)),
+                ("positions", positions, torch.int32, lead),
+                ("lengths", lengths, torch.int32, lead[:2])]
+        if weights is not None:
+            want.append(("weights", weights, torch.float32, lead))
+        for name, t, dtype, shape in want:
+            if (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()
+                    or t.device != k_codes.device):
+                _invalid(f"{name} must be a contiguous {dtype} tensor {shape} on k_codes' device")
+            setattr(self, name, t)
+        self.weights = weights
+        self.trace = trace
+        self.batch, self.num_kv_heads, self.capacity = lead
+        self.device = k_codes.device
+        s = CkvQ4Cache(self.batch, self.num_kv_heads, 128, self.capacity, _addr(k_codes),
+                       _addr(v_codes), _addr(k_params), _addr(v_params), _addr(positions),
+                       _addr(weights), _addr(lengths),
+                       ctypes.pointer(trace.struct) if trace is not None else None)
+        self.struct = s
+        self.addr = ctypes.addressof(s)
+
+    def sequences(self, first: int, count: int) -> "Q4Cache":
+        """Sequences ``first .. first + count - 1`` as a cache of their own (a
+        layer of a cache that packs its layers); the memory is shared."""
+        first, count = int(first), int(count)
+        if first < 0 or count < 1 or first + count > self.batch:
+            _invalid("sequences outside the cache")
+        cut = slice(first, first + count)
+        return Q4Cache(self.k_codes[cut], self.v_codes[cut], self.k_params[cut],
+                       self.v_params[cut], self.positions[cut], self.lengths[cut],
+                       None if self.weights is None else self.weights[cut], self.trace)
+
+
+def q4_cache(batch: int, num_kv_heads: int, capacity: int, device=None, weights: bool = True,
+             trace: "Trace | None" = None) -> Q4Cache:
+    """An empty 4-bit cache; ``capacity`` is rounded up to a multiple of 32."""
+    cap = -(-int(capacity) // Q4_TILE) * Q4_TILE
+    lead = (int(batch), int(num_kv_heads), cap)
+    device = device or "cuda"
+
+    def empty(shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+    return Q4Cache(empty(lead + (64,), torch.uint8), empty(lead + (64,), torch.uint8),
+                   empty(lead + (8,), torch.bfloat16), empty(lead + (8,), torch.bfloat16),
+                   empty(lead, torch.int32),
+                   torch.zeros(lead[:2], dtype=torch.int32, device=device),
+                   empty(lead, torch.float32) if weights else None, trace)
+
+
+def _q4_call(name: str, cache: Q4Cache, stream, *args):
+    """Enqueues on `stream` (default: the current stream of the cache's device)."""
+    dev = cache.device
+    if dev.type != "cuda":
+        _invalid("the cache must be in device memory")
+    fn = _fast(name)
+    if dev.index == torch.cuda.current_device():
+        _check(fn(cache.addr, *args, _raw_stream(stream)), name)
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(cache.addr, *args, _raw_stream(stream)), name)
+
+
+def _q4_on_device(cache: Q4Cache, what: str, *tensors):
+    for t in tensors:
+        if t is not None and t.device != cache.device:
+            _invalid(f"{what} must be on the cache's device")
+
+
+def _q4_rows(cache: Q4Cache, k, v):
+    if k.dim() != 3 or tuple(k.shape[1:]) != (cache.num_kv_heads, 128) or v.shape != k.shape:
+        _invalid("k and v must be [rows, H_kv, 128]")
+    if v.dtype != k.dtype or k.stride(2) != 1 or v.stride() != k.stride():
+        _invalid("k and v must share their dtype and strides, head_dim contiguous")
+    return _q4_dtype(k)
+
+
+def _q4_values(t, like, shape, what):
+    if t is not None and (t.dtype != like.dtype or tuple(t.shape) != tuple(shape)
+                          or not t.is_contiguous()):
+        _invalid(f"{what} must be contiguous {tuple(shape)} in the rows' dtype")
+
+
+def _q4_i32(cache, t, shape, what):
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != tuple(shape)
+                          or not t.is_contiguous()):
+        _invalid(f"{what} must be a contiguous int32 tensor {tuple(shape)}")
+
+
+def q4_workspace_size(cache: Q4Cache, num_q_heads: int = 0, num_queries: int = 0) -> int:
+    n = _fast("compresskv_q4_workspace_size")(cache.addr, int(num_q_heads), int(num_queries))
+    if n == 0:
+        raise CompressKVError(CKV_ERR_INVALID_ARG, "compresskv_q4_workspace_size")
+    return int(n)
+
+
+def q4_workspace(cache: Q4Cache, num_q_heads: int = 0, num_queries: int = 0,
+                 stream=None) -> torch.Tensor:
+    """A zero-status workspace for q4_attend with these heads and query tokens
+    (or fewer) and q4_evict; without them for q4_evict alone."""
+    if cache.device.type != "cuda":
+        _invalid("the cache must be in device memory")
+    n = q4_workspace_size(cache, num_q_heads, num_queries)
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+    assert ws.data_ptr() % 256 == 0
+    with torch.cuda.device(cache.device):
+        _check(_fast("compresskv_q4_workspace_init")(ws.data_ptr(), n, _raw_stream(stream)),
+               "compresskv_q4_workspace_init")
+    return ws
+
+
+def q4_append(cache: Q4Cache, k, v, positions, cu_rows=None, start=None, k_values=None,
+              v_values=None, device_status=None, stream=None) -> None:
+    """Quantises rows of new tokens into the cache.  ``k`` / ``v`` are
+    ``[rows, H_kv, 128]`` packed by sequence (``cu_rows``: host ``[B+1]``; None:
+    the same number for each), ``positions`` int32 ``[rows]`` (negative: padding
+    behind a sequence's rows), ``start`` int32 ``[B, H_kv]`` (default: the
+    cache's lengths); ``k_values`` / ``v_values`` receive what the codes stand
+    for."""
+    dtype = _q4_rows(cache, k, v)
+    rows = k.shape[0]
+    _q4_i32(cache, positions, (rows,), "positions")
+    _q4_i32(cache, start, (cache.batch, cache.num_kv_heads), "start")
+    _q4_i32(cache, device_status, (1,), "device_status")
+    _q4_values(k_values, k, k.shape, "k_values")
+    _q4_values(v_values, k, k.shape, "v_values")
+    r = CkvQ4Rows(dtype, 0, None, k.stride(0) if rows > 1 else cache.num_kv_heads * 128,
+                  k.stride(1) if cache.num_kv_heads > 1 else 128)
+    if cu_rows is None:
+        if rows % cache.batch:
+            _invalid("the rows do not divide by the sequences: give cu_rows")
+        r.rows_per_seq = rows // cache.batch
+    else:
+        cu = _host_i32(cu_rows)
+        if cu.shape != (cache.batch + 1,) or int(cu[-1]) != rows:
+            _invalid("cu_rows must be [B+1] and end at the rows of k")
+        r.cu_rows = _data(cu)
+    _q4_on_device(cache, "k, positions, start, values and status", k, positions, start, k_values,
+                  v_values, device_status)
+    _q4_call("compresskv_q4_append", cache, stream, ctypes.addressof(r), _addr(k), _addr(v),
+             _addr(positions), _addr(start), _addr(k_values), _addr(v_values),
+             _addr(device_status))
+
+
+def q4_gather(problem: Problem, cache: Q4Cache, indices, cu_out, k, v, raw=None, k_values=None,
+              v_values=None, ws=None, stream=None) -> None:
+    """Quantises the retained rows of a compression into the cache, from slot 0
+    of each unit.  ``indices`` / ``cu_out`` as compress_layer(s) or select give
+    them (``[H_kv, rows]``, ``[B+1]``), or as compress_layer_head_budgets does
+    (``[rows]``, ``[H_kv, B+1]``); ``raw``: the raw scores become the rows' first
+    weights; ``k_values`` / ``v_values`` as k_out / v_out of the compression."""
+    dtype = _q4_rows(cache, k, v)
+    s = problem.struct
+    if (s.batch != cache.batch or s.num_kv_heads != cache.num_kv_heads or s.dtype != dtype
+            or s.kv_token_stride != k.stride(0) or s.kv_head_stride != k.stride(1)
+            or k.shape[0] < int(problem._cu[-1])):
+        _invalid("k, v and the cache must be those of the problem")
+    cu = _host_i32(cu_out)
+    H, B = cache.num_kv_heads, cache.batch
+    group_major = cu.ndim == 2
+    if cu.shape != ((H, B + 1) if group_major else (B + 1,)):
+        _invalid("cu_out must be [B+1], or [H_kv, B+1] for budgets per KV group")
+    rows = int(cu.reshape(-1)[-1])
+    _q4_i32(cache, indices, (rows,) if group_major else (H, rows), "indices")
+    shape = (rows, 128) if group_major else (rows, H, 128)
+    _q4_values(k_values, k, shape, "k_values")
+    _q4_values(v_values, k, shape, "v_values")
+    n = int(np.maximum(np.diff(problem._cu) - s.window, 0).sum())
+    if raw is not None and (raw.dtype != torch.float32 or tuple(raw.shape) != (H, n)
+                            or not raw.is_contiguous()):
+        _invalid(f"raw must be a contiguous float32 tensor {(H, n)}")
+    _q4_on_device(cache, "k, indices, raw, values and workspace", k, indices, raw, k_values,
+                  v_values, ws)
+    if cache.device.type != "cuda":
+        _invalid("the cache must be in device memory")
+    fn = _fast("compresskv_q4_gather")
+    with torch.cuda.device(cache.device):
+        _check(fn(problem.addr, cache.addr, int(group_major), _addr(indices), _data(cu), _addr(k),
+                  _addr(v), _addr(raw), _addr(k_values), _addr(v_values), _addr(ws),
+                  _raw_stream(stream)), "compresskv_q4_gather")
+
+
+def q4_attend(cache: Q4Cache, q, out, ws, q_positions=None, scale: float = 0.0, lse=None,
+              accumulate: bool = False, stream=None) -> None:
+    """Attention of ``q`` ``[B, H_q, n, 128]`` (n query tokens a sequence, any
+    strides with head_dim contiguous) over the cache into ``out`` (same shape
+    and dtype).  ``q_positions`` int32 ``[B, n]``: a slot is seen where its
+    position is not above the query's (default: every slot in use is seen);
+    ``lse`` float32 ``[B, H_q, n]``; ``accumulate`` adds each slot's attention to
+    the cache's weights."""
+    if q.dim() != 4 or q.shape[0] != cache.batch or q.shape[3] != 128 or out.shape != q.shape:
+        _invalid("q and out must be [B, H_q, n, 128]")
+    if out.dtype != q.dtype or q.stride(3) != 1 or out.stride(3) != 1:
+        _invalid("q and out must share their dtype, head_dim contiguous")
+    B, hq, n = q.shape[:3]
+    _q4_i32(cache, q_positions, (B, n), "q_positions")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, hq, n)
+                            or not lse.is_contiguous()):
+        _invalid("lse must be a contiguous float32 [B, H_q, n]")
+    qs, os_ = q.stride(), out.stride()
+    # a dimension of one element has a stride that means nothing
+    one = (B == 1, hq == 1, n == 1)
+    a = CkvQ4Queries(hq, n, _q4_dtype(q), int(bool(accumulate)), float(scale),
+                     *(128 if one[i] else qs[i] for i in range(3)),
+                     *(128 if one[i] else os_[i] for i in range(3)))
+    _q4_on_device(cache, "q, out, q_positions, lse and workspace", q, out, q_positions, lse, ws)
+    _q4_call("compresskv_q4_attend", cache, stream, ctypes.addressof(a), _addr(q),
+             _addr(q_positions), _addr(out), _addr(lse), _addr(ws), ws.numel())
+
+
+def q4_evict(cache: Q4Cache, budget, ws, sinks: int = 0, recent: int = 0, stream=None) -> None:
+    """Evicts, in place, every unit's slots beyond ``budget`` (an int, or an
+    int32 device tensor ``[B, H_kv]``) with the least accumulated weight; slots
+    at positions below ``sinks`` and the ``recent`` newest positions stay."""
+    budgets = None
+    if isinstance(budget, torch.Tensor):
+        budgets, budget = budget, 0
+        _q4_i32(cache, budgets, (cache.batch, cache.num_kv_heads), "budget")
+    _q4_on_device(cache, "budget and workspace", budgets, ws)
+    _q4_call("compresskv_q4_evict", cache, stream, int(budget), _addr(budgets), int(sinks),
+             int(recent), _addr(ws), ws.numel())

@@ -5,7 +5,6 @@
 // in compresskv_read_device_status).
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
-#include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
 #include <atomic>
@@ -16,19 +15,29 @@
 
 #include "ckv_params.h"
 #include "compresskv.h"
-
-namespace {
-// A named range around each entry point for profilers (NVTX; nothing happens
-// unless a profiling tool is attached to the process).
-struct NvtxRange {
-  explicit NvtxRange(const char* name) { nvtxRangePushA(name); }
-  ~NvtxRange() { nvtxRangePop(); }
-  NvtxRange(const NvtxRange&) = delete;
-  NvtxRange& operator=(const NvtxRange&) = delete;
-};
-}  // namespace
+#include "host_common.h"
 
 using namespace ckv;
+
+// The address under which the device reads `ptr`: device or managed memory
+// as is, page-locked host memory through its mapped (unified) address.
+// Pageable or unknown memory is refused: a kernel must not touch it.
+int ckv::device_readable(const void* ptr, const void** dev) {
+  cudaPointerAttributes a;
+  if (cudaPointerGetAttributes(&a, ptr) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return CKV_ERR_INVALID_ARG;
+  }
+  if (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged) {
+    *dev = ptr;
+    return CKV_OK;
+  }
+  if (a.type == cudaMemoryTypeHost && a.devicePointer) {
+    *dev = a.devicePointer;
+    return CKV_OK;
+  }
+  return CKV_ERR_INVALID_ARG;
+}
 
 namespace {
 
@@ -160,28 +169,6 @@ struct Info {
   int vgroup(int s, int g) const { return srh_group(s, g, spm, Hkv); }
 };
 
-bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
-
-// The address under which the device reads `ptr`: device or managed memory
-// as is, page-locked host memory through its mapped (unified) address.
-// Pageable or unknown memory is refused: a kernel must not touch it.
-int device_readable(const void* ptr, const void** dev) {
-  cudaPointerAttributes a;
-  if (cudaPointerGetAttributes(&a, ptr) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return CKV_ERR_INVALID_ARG;
-  }
-  if (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged) {
-    *dev = ptr;
-    return CKV_OK;
-  }
-  if (a.type == cudaMemoryTypeHost && a.devicePointer) {
-    *dev = a.devicePointer;
-    return CKV_OK;
-  }
-  return CKV_ERR_INVALID_ARG;
-}
-
 // Device (or managed) memory of the current device: what a kernel may read
 // through a plain pointer.  Host memory of any kind is refused.
 int device_memory(const void* ptr) {
@@ -247,6 +234,15 @@ int validate(const ckv_problem* p, Info& I) {
   if (static_cast<long long>(I.Hkv) * I.p_total > (1LL << 31) - 1) return CKV_ERR_UNSUPPORTED;
   return CKV_OK;
 }
+
+}  // namespace
+
+int ckv::check_problem(const ckv_problem* p) {
+  Info I;
+  return validate(p, I);
+}
+
+namespace {
 
 int output_layout(const Info& I, const int32_t* budgets, std::vector<int>& cu_out) {
   if (!budgets) return CKV_ERR_INVALID_ARG;
@@ -427,58 +423,6 @@ int carve(const Info& I, void* ws, size_t bytes, Workspace& out) {
   out.shared = reinterpret_cast<float*>(b + W.shared);
   out.raw = reinterpret_cast<float*>(b + W.raw);
   return CKV_OK;
-}
-
-// ------------------------------------------------------------------ tracing
-// Records the caller's trace events around each launch.  A failed record
-// (for example a null event handle) is reported as CKV_ERR_INVALID_ARG and
-// the runtime's last-error state is cleared.
-struct Tracer {
-  ckv_trace* t;
-  cudaStream_t s;
-  int slot = -1;
-  int begin(int kind) {
-    slot = -1;
-    if (!t) return CKV_OK;
-    if (t->count < t->capacity && t->events) {
-      slot = t->count++;
-      if (t->kinds) t->kinds[slot] = kind;
-      return record(static_cast<cudaEvent_t>(t->events[2 * slot]));
-    }
-    return CKV_OK;
-  }
-  int end() {
-    if (!t) return CKV_OK;
-    ++t->launches;
-    if (slot >= 0) return record(static_cast<cudaEvent_t>(t->events[2 * slot + 1]));
-    return CKV_OK;
-  }
-  int record(cudaEvent_t e) {
-    if (!e) return CKV_ERR_INVALID_ARG;
-    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-    cudaError_t err = cudaStreamIsCapturing(s, &cs);
-    if (err == cudaSuccess) {
-      err = cs == cudaStreamCaptureStatusActive
-                ? cudaEventRecordWithFlags(e, s, cudaEventRecordExternal)
-                : cudaEventRecord(e, s);
-    }
-    if (err != cudaSuccess) {
-      cudaGetLastError();
-      return CKV_ERR_INVALID_ARG;
-    }
-    return CKV_OK;
-  }
-};
-
-// Launch `fn` bracketed by the trace: trace errors win over a clean launch.
-template <class F>
-int traced(Tracer& tr, int kind, F&& fn) {
-  int rc = tr.begin(kind);
-  if (rc != CKV_OK) return rc;
-  const cudaError_t e = fn();
-  const int rc2 = tr.end();
-  if (e != cudaSuccess) return CKV_ERR_CUDA;
-  return rc2;
 }
 
 // ------------------------------------------------------------------ scoring

@@ -1,0 +1,88 @@
+// Parameter blocks of the 4-bit cache's kernels (append / gather, attention,
+// eviction), shared by their host side and the kernels.  They travel by value
+// like the others (ckv_params.h).
+#pragma once
+
+#include <cstdint>
+#include <vector_types.h>
+
+#include "ckv_params.h"
+
+namespace ckv {
+
+constexpr int kQ4GroupDim = 32;                         // channels that share a scale
+constexpr int kQ4Groups = kHeadDim / kQ4GroupDim;       // 4
+constexpr int kQ4CodeBytes = kHeadDim / 2;              // codes of one K or V row
+constexpr int kQ4ParamBytes = 4 * kQ4Groups;            // 4 bf16 scales, 4 bf16 minima
+constexpr int kQ4TileSlots = 32;                        // capacity is a multiple of this
+constexpr int kQ4MaxUnits = 65535;                      // (sequence, KV group) pairs of a cache
+constexpr int kQ4MaxQueries = 16;                       // query tokens a sequence and call
+constexpr int kQ4HeaderBytes = 256;                     // workspace: the status word
+
+// The cache as the kernels see it; unit u = sequence * num_kv_heads + group,
+// slot row = u * capacity + slot.
+struct Q4Cache {
+  uint8_t* codes[2];     // K, V: [units][capacity][64]
+  uint8_t* params[2];    // K, V: [units][capacity][16]
+  int32_t* positions;    // [units][capacity]
+  float* weights;        // [units][capacity], or null
+  int32_t* lengths;      // [units]
+  int capacity, num_kv_heads, batch;
+};
+
+// Rows into the cache.  Table: per sequence [batch + 1] first rows, or per
+// unit (group-major: [num_kv_heads][batch + 1]) where a unit has its own rows.
+template <int kTable>
+struct Q4WriteParams {
+  Q4Cache c;
+  const uint16_t* src[2];      // K, V rows (f16 / bf16 bits)
+  uint16_t* values[2];         // optional: the values that the codes stand for
+  long long tok_stride, head_stride;          // of src, elements
+  const int32_t* positions;    // append: [rows]
+  const int32_t* start;        // append: first slot of each unit, or null (lengths)
+  const int32_t* indices;      // gather: [num_kv_heads][rows] (or [rows], group-major)
+  const float* raw;            // gather: optional raw scores, score layout
+  int* status;                 // may be null
+  int is_bf16, rows, rows_per_seq;            // append: rows_per_seq < 0: by the table
+  int group_major, window, p_total;
+  int cu_seqlens[kTable ? kMaxBatch + 1 : 1]; // gather: first source row of each sequence
+  int cu_prefix[kTable ? kMaxBatch + 1 : 1];
+  int cu_rows[kTable ? kTable : kMaxBatch + 1];
+};
+constexpr int kQ4SeqTable = kMaxBatch + 1;
+constexpr int kQ4UnitTable = kMaxBudgetUnits + kMaxKvHeads;
+using Q4AppendParams = Q4WriteParams<0>;
+using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
+using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
+
+struct Q4AttendParams {
+  Q4Cache c;
+  const uint16_t* q;           // f16 / bf16 bits
+  uint16_t* out;
+  float* lse;                  // optional, [batch][num_q_heads][num_queries]
+  const int32_t* q_positions;  // optional, [batch][num_queries]
+  long long q_bs, q_hs, q_qs, o_bs, o_hs, o_qs;  // elements
+  float scale;                 // of q.k, natural units
+  int num_q_heads, group, num_queries, is_bf16, accumulate;
+  int* status;
+  float* lse_ws;               // [units][rows]: base-2 log-sum-exp
+  float* z;                    // accumulate: [units][rows][capacity] base-2 logits
+};
+
+struct Q4EvictParams {
+  Q4Cache c;
+  const int32_t* budgets;      // optional, [units]
+  int budget;                  // where `budgets` is null
+  int sinks, recent;
+  int32_t* lists;              // workspace: [units][capacity] pairs of slots
+  int* status;
+};
+
+cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t s);
+cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t s);
+cudaError_t launch_q4_gather(const Q4GatherUnitParams& p, cudaStream_t s);
+cudaError_t launch_q4_attend(const Q4AttendParams& p, cudaStream_t s);
+cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);
+cudaError_t launch_q4_evict(const Q4EvictParams& p, cudaStream_t s);
+
+}  // namespace ckv
