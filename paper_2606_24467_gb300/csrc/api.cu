@@ -16,6 +16,7 @@
 #include "ckv_params.h"
 #include "compresskv.h"
 #include "host_common.h"
+#include "q4_params.h"
 
 using namespace ckv;
 
@@ -110,6 +111,7 @@ int device_facts(DeviceFacts** out) {
     if (score_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
     if (fused_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
     if (resident_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
+    if (q4_attend_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
     if (combine_set_smem_limit(static_cast<size_t>(optin), &f.combine_smem_max) != cudaSuccess)
       return CKV_ERR_CUDA;
     if (select_set_smem_limit(static_cast<size_t>(select_max_smem_floats()) * 4) != cudaSuccess)
@@ -240,6 +242,24 @@ int validate(const ckv_problem* p, Info& I) {
 int ckv::check_problem(const ckv_problem* p) {
   Info I;
   return validate(p, I);
+}
+
+int ckv::usable_sms(cudaStream_t stream, int* sms) {
+  DeviceFacts* F = nullptr;
+  const int rc = device_facts(&F);
+  if (rc == CKV_OK) *sms = stream_sms(*F, stream);
+  return rc;
+}
+
+int ckv::make_row64_map(const void* base, unsigned long long rows, unsigned box_rows,
+                        CUtensorMap* map) {
+  cuuint64_t dims[2] = {64u, rows}, strides[1] = {64u};
+  cuuint32_t box[2] = {64u, box_rows}, estr[2] = {1u, 1u};
+  const CUresult r =
+      g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box,
+               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CKV_OK : CKV_ERR_INVALID_ARG;
 }
 
 namespace {

@@ -1,6 +1,7 @@
 // Host-side helpers shared by the files that implement the C ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
@@ -9,10 +10,14 @@
 #include "compresskv.h"
 
 namespace ckv {
-// The checks that every entry point makes of a problem description, and the
-// address under which the device reads K or V (both in api.cu).
+// In api.cu: the checks that every entry point makes of a problem description;
+// the address under which the device reads K or V; the SMs that kernels on the
+// stream may use (after the current device's one-time set-up); a map over
+// `rows` rows of 64 bytes for boxes of `box_rows`, 64-byte swizzle.
 int check_problem(const ckv_problem* p);
 int device_readable(const void* ptr, const void** dev);
+int usable_sms(cudaStream_t stream, int* sms);
+int make_row64_map(const void* base, unsigned long long rows, unsigned box_rows, CUtensorMap* map);
 }  // namespace ckv
 
 namespace {

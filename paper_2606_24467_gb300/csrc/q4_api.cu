@@ -64,16 +64,22 @@ int check_values(const void* k, const void* v) {
   return aligned16(k) && aligned16(v) ? CKV_OK : CKV_ERR_INVALID_ARG;
 }
 
-// Bytes of the attention's area behind the workspace header.
+// The attention's area behind the workspace header, for up to kMaxSms SMs.
+constexpr int kMaxSms = 160;
 struct AttendArea {
-  size_t lse = 0, z = 0, bytes = 0;
+  size_t first_tile = 0, part_ml = 0, part_o = 0, lse = 0, z = 0, bytes = 0;
 };
 AttendArea attend_area(const ckv_q4_cache* c, int num_q_heads, int num_queries, bool accumulate) {
-  const size_t rows = static_cast<size_t>(c->batch) * num_q_heads * num_queries;
+  const size_t units = units_of(c), rows = static_cast<size_t>(num_q_heads / c->num_kv_heads) * num_queries;
+  const size_t brows = q4_block_rows(static_cast<int>(rows)), blocks = (rows + brows - 1) / brows;
+  const size_t parts = q4_attend_workers(static_cast<int>(rows), kMaxSms) + units * blocks;
   AttendArea a;
-  a.lse = kQ4HeaderBytes;
-  a.z = a.lse + align256(rows * sizeof(float));
-  a.bytes = a.z + (accumulate ? align256(rows * c->capacity * sizeof(float)) : 0);
+  a.first_tile = kQ4HeaderBytes;
+  a.part_ml = a.first_tile + align256((units + 1) * sizeof(long long));
+  a.part_o = a.part_ml + align256(parts * brows * sizeof(float2));
+  a.lse = a.part_o + align256(parts * brows * kHeadDim * sizeof(float));
+  a.z = a.lse + align256(units * rows * sizeof(float));
+  a.bytes = a.z + (accumulate ? align256(units * rows * c->capacity * sizeof(float)) : 0);
   return a;
 }
 size_t evict_bytes(const ckv_q4_cache* c) {
@@ -149,7 +155,10 @@ size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, 
   size_t n = evict_bytes(c);
   if (num_q_heads != 0 || num_queries != 0) {
     if (check_heads(c, num_q_heads, num_queries) != CKV_OK) return 0;
-    n = std::max(n, attend_area(c, num_q_heads, num_queries, c->weights != nullptr).bytes);
+    const bool weights = c->weights != nullptr;
+    n = std::max(n, attend_area(c, num_q_heads, num_queries, weights).bytes);
+    // (fewer rows may take smaller row blocks and then more workers)
+    n = std::max(n, attend_area(c, c->num_kv_heads, 1, weights).bytes);
   }
   return n;
 }
@@ -258,9 +267,15 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   }
   const AttendArea area = attend_area(c, a->num_q_heads, a->num_queries, a->accumulate != 0);
   if ((rc = check_workspace(workspace, workspace_bytes, area.bytes)) != CKV_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int sms = 0;
+  if ((rc = usable_sms(st, &sms)) != CKV_OK) return rc;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Q4AttendParams P;
   std::memset(&P, 0, sizeof(P));
+  const unsigned long long slots = static_cast<unsigned long long>(units_of(c)) * c->capacity;
+  if ((rc = make_row64_map(c->k_codes, slots, kQ4TileSlots, &P.map_k)) != CKV_OK) return rc;
+  if ((rc = make_row64_map(c->v_codes, slots, kQ4TileSlots, &P.map_v)) != CKV_OK) return rc;
   P.c = device_cache(c);
   P.q = static_cast<const uint16_t*>(q);
   P.out = static_cast<uint16_t*>(out);
@@ -272,18 +287,28 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.o_bs = to[0];
   P.o_hs = to[1];
   P.o_qs = to[2];
-  P.scale = a->scale > 0.f ? a->scale : 1.0f / std::sqrt(static_cast<float>(kHeadDim));
+  const double scale = a->scale > 0.f ? a->scale : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
+  P.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
   P.num_q_heads = a->num_q_heads;
   P.group = a->num_q_heads / c->num_kv_heads;
   P.num_queries = a->num_queries;
   P.is_bf16 = a->dtype == CKV_DTYPE_BF16;
   P.accumulate = a->accumulate != 0;
   P.status = static_cast<int*>(workspace);
+  P.rows = P.group * P.num_queries;
+  P.blocks = (P.rows + q4_block_rows(P.rows) - 1) / q4_block_rows(P.rows);
+  // no more CTAs than there can be tiles
+  const long long tiles = static_cast<long long>(slots / kQ4TileSlots) * P.blocks;
+  sms = static_cast<int>(std::min<long long>({sms, kMaxSms, tiles}));
+  P.workers = q4_attend_workers(P.rows, sms);
+  P.first_tile = reinterpret_cast<long long*>(ws + area.first_tile);
+  P.part_ml = reinterpret_cast<float2*>(ws + area.part_ml);
+  P.part_o = reinterpret_cast<float*>(ws + area.part_o);
   P.lse_ws = reinterpret_cast<float*>(ws + area.lse);
   P.z = reinterpret_cast<float*>(ws + area.z);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   Tracer tr{c->trace, st};
-  rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_attend(P, st); });
+  rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_attend(P, sms, st); });
+  if (rc == CKV_OK) rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_combine(P, st); });
   if (rc != CKV_OK || !P.accumulate) return rc;
   return traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_weights(P, st); });
 }

@@ -55,16 +55,28 @@ using Q4AppendParams = Q4WriteParams<0>;
 using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
 using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
+// Attention.  The tiles (32 slots) of all row blocks -- up to 16 query rows of
+// a unit -- form one sequence, of which every worker (a warp) takes `chunk`
+// neighbours, so a worker covers the end of one row block, any number of whole
+// ones and the start of another.  For each it leaves a part; since worker and
+// row block both grow along the sequence, worker + row block numbers the parts.
 struct Q4AttendParams {
+  CUtensorMap map_k, map_v;    // codes: [units * capacity] rows of 64 bytes, boxes of 32 rows
   Q4Cache c;
   const uint16_t* q;           // f16 / bf16 bits
   uint16_t* out;
   float* lse;                  // optional, [batch][num_q_heads][num_queries]
   const int32_t* q_positions;  // optional, [batch][num_queries]
   long long q_bs, q_hs, q_qs, o_bs, o_hs, o_qs;  // elements
-  float scale;                 // of q.k, natural units
+  float scale_log2;            // softmax scale * log2(e)
   int num_q_heads, group, num_queries, is_bf16, accumulate;
+  int rows, blocks;            // query rows of a unit, and row blocks of them
+  int workers;                 // warps of the launch
   int* status;
+  // workspace
+  long long* first_tile;       // [units + 1]: tiles before each unit (one row block)
+  float* part_o;               // [workers + units * blocks][block rows][128]
+  float2* part_ml;             // [workers + units * blocks][block rows]: reference and sum
   float* lse_ws;               // [units][rows]: base-2 log-sum-exp
   float* z;                    // accumulate: [units][rows][capacity] base-2 logits
 };
@@ -81,7 +93,12 @@ struct Q4EvictParams {
 cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherUnitParams& p, cudaStream_t s);
-cudaError_t launch_q4_attend(const Q4AttendParams& p, cudaStream_t s);
+constexpr int q4_block_rows(int rows) { return rows <= 8 ? 8 : 16; }
+// Warps that the attention launches on `sms` SMs.
+int q4_attend_workers(int rows, int sms);
+cudaError_t q4_attend_set_smem_limit();
+cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t s);
+cudaError_t launch_q4_combine(const Q4AttendParams& p, cudaStream_t s);
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);
 cudaError_t launch_q4_evict(const Q4EvictParams& p, cudaStream_t s);
 
