@@ -112,6 +112,7 @@ int device_facts(DeviceFacts** out) {
     if (fused_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
     if (resident_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
     if (q4_attend_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
+    if (q4_evict_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
     if (combine_set_smem_limit(static_cast<size_t>(optin), &f.combine_smem_max) != cudaSuccess)
       return CKV_ERR_CUDA;
     if (select_set_smem_limit(static_cast<size_t>(select_max_smem_floats()) * 4) != cudaSuccess)

@@ -324,6 +324,9 @@ int compresskv_q4_evict(const ckv_q4_cache* c, int32_t budget, const int32_t* bu
     if (budget < static_cast<int64_t>(sinks) + recent) return CKV_ERR_BUDGET;
   }
   if ((rc = check_workspace(workspace, workspace_bytes, evict_bytes(c))) != CKV_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int sms = 0;
+  if ((rc = usable_sms(st, &sms)) != CKV_OK) return rc;
   Q4EvictParams P;
   std::memset(&P, 0, sizeof(P));
   P.c = device_cache(c);
@@ -333,9 +336,8 @@ int compresskv_q4_evict(const ckv_q4_cache* c, int32_t budget, const int32_t* bu
   P.recent = recent;
   P.status = static_cast<int*>(workspace);
   P.lists = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + kQ4HeaderBytes);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   Tracer tr{c->trace, st};
-  return traced(tr, CKV_KERNEL_Q4_EVICT, [&] { return launch_q4_evict(P, st); });
+  return traced(tr, CKV_KERNEL_Q4_EVICT, [&] { return launch_q4_evict(P, sms, st); });
 }
 
 }  // extern "C"

@@ -86,6 +86,7 @@ struct Q4EvictParams {
   const int32_t* budgets;      // optional, [units]
   int budget;                  // where `budgets` is null
   int sinks, recent;
+  int cluster;                 // CTAs a unit (set at the launch)
   int32_t* lists;              // workspace: [units][capacity] pairs of slots
   int* status;
 };
@@ -100,6 +101,7 @@ cudaError_t q4_attend_set_smem_limit();
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t s);
 cudaError_t launch_q4_combine(const Q4AttendParams& p, cudaStream_t s);
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);
-cudaError_t launch_q4_evict(const Q4EvictParams& p, cudaStream_t s);
+cudaError_t q4_evict_set_smem_limit();
+cudaError_t launch_q4_evict(const Q4EvictParams& p, int sms, cudaStream_t s);
 
 }  // namespace ckv

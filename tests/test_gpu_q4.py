@@ -588,6 +588,28 @@ def test_evict_weights(cuda_device, kind):
     check_evict(c0, host(c), np.full((1, 3), 60), 3, 20)
 
 
+@pytest.mark.parametrize("units,n", [(80, 5000), (2, 210001), (80, 26001), (20, 9000), (1, 26000)])
+def test_evict_of_long_units(cuda_device, units, n):
+    """Units that a CTA or a cluster of them holds in shared memory, or does not
+    (the first and the last unit are compared)."""
+    gen = torch.Generator(device=cuda_device).manual_seed(n)
+    c = blank(units, 1, n, cuda_device)
+    for part in ("k", "v"):
+        getattr(c, part + "_codes").random_(0, 256, generator=gen)
+        getattr(c, part + "_params").normal_(generator=gen)
+    order = torch.rand((units, 1, c.capacity), generator=gen, device=cuda_device)
+    order[:, :, n:] = 2
+    c.positions.copy_(order.argsort(-1).int())
+    c.weights.copy_((torch.rand((units, 1, c.capacity), generator=gen, device=cuda_device) * 500).floor())
+    c.lengths.fill_(n)
+    c.lengths[-1] = n - 37
+    pick = [0, units - 1]
+    c0 = {k: v[pick] for k, v in host(c).items()}
+    budget = n // 3
+    ckv.q4_evict(c, budget, ckv.q4_workspace(c), sinks=5, recent=1000)
+    check_evict(c0, {k: v[pick] for k, v in host(c).items()}, np.full((2, 1), budget), 5, 1000)
+
+
 def test_evict_budgets_per_unit(cuda_device):
     gen = torch.Generator().manual_seed(5)
     c = random_cache(3, 4, 500, 500, cuda_device, gen)
