@@ -19,17 +19,20 @@
 // tensor cores' rate, while tcgen05 would want the operands expanded to 16 bits
 // in shared memory, four times the bytes of the codes.
 //
-//   S = Q K^T: A = q rows (16-bit queries as fp16, scaled by a power of two a
-//     row so that the largest is in [2^14, 2^15): exact but for elements below
-//     2^-34 of it), B = codes of 8 slots; the four groups are summed apart and
+//   S^T = K Q^T: A = codes of 16 slots, B = 8 query rows (as fp16, scaled by a
+//     power of two a row so that the largest element is in [2^14, 2^15): exact
+//     but for elements below 2^-34 of it); the four groups are summed apart and
 //     scaled by their s in fp32.  The minima's term sum_J m_J (sum of q over J)
 //     is one more product: the group sums as three bf16 parts (24 bits), m in bf16.
-//   O^T = V^T P^T: the result layout of S is the operand layout of P^T, so no
-//     value changes lanes.  The weights of group J's codes are p s_J, in fp16
-//     (relative error 2^-12, independent for each slot) against a power of two
-//     that follows the largest s seen: 20 binades below the largest p s_J keep
-//     that precision.  The minima's term sum_j p m_J is one more product with
-//     p as two bf16 parts.
+//   O^T = V^T P^T: A = codes of 16 channels, B = P^T, which movmatrix makes of
+//     the result layout of S^T.  With p in fp16 (relative error 2^-12) the weights
+//     of group J's codes are p s_J (rounded once more), those of its minimum p; the
+//     minima's term is a product of its own.  Scales and minima are fp16 too,
+//     exact against a power of two that follows the largest of both: 2^-21 of it
+//     and above for scales, 2^-22 for minima.
+// Eight lanes of a warp need the same slot's scales, so one lane a slot converts
+// them for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
+// leaves them in shared memory.
 // Softmax references are raised only when a logit passes them by 2^8, so the
 // outputs are hardly ever rescaled.
 #include <cuda_runtime.h>
@@ -43,8 +46,9 @@ namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
-constexpr int kTopExp = 14 - 8;        // p s_J <= 2^8 * 2^(k+1) becomes < 2^15
-constexpr int kMinScaleExp = -110;     // smaller scales share this reference
+constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
+constexpr int kTopExp = 7;             // scales become < 2^4, minima < 2^8: p s < 2^15
+constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
 // Shared memory of a worker's stage: codes of K and V (swizzled), then params
 // and positions.
@@ -52,15 +56,23 @@ constexpr int kCodeTile = kQ4TileSlots * kQ4CodeBytes;    // 2048
 constexpr int kParamTile = kQ4TileSlots * kQ4ParamBytes;  // 512
 constexpr int kPosTile = kQ4TileSlots * 4;                // 128
 constexpr int kSideBytes = 2 * kParamTile + kPosTile;     // 1152
+constexpr int kScaleTile = kQ4TileSlots * 16;             // K's scales of the tile at hand, fp32
 
+#ifndef Q4W1
+#define Q4W1 12
+#define Q4S1 2
+#define Q4W2 8
+#define Q4S2 4
+#endif
 template <int NB>
 struct Shape {
-  static constexpr int kWarps = NB == 1 ? 16 : 12;
-  static constexpr int kStages = NB == 1 ? 2 : 3;
+  static constexpr int kWarps = NB == 1 ? Q4W1 : Q4W2;
+  static constexpr int kStages = NB == 1 ? Q4S1 : Q4S2;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
-  static constexpr int kSmem = 1024 + kCodes + kSide + kWarps * kStages * 8;
+  static constexpr int kScales = kWarps * kScaleTile;
+  static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
 };
 
 __device__ __forceinline__ float to_float(uint32_t h, bool bf16) {
@@ -93,6 +105,18 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       "{%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Transpose of an 8x8 matrix of 16-bit numbers: lane (g, t) gives row g,
+// columns 2t and 2t + 1, and receives those of column g.
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+  return r;
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -149,21 +173,23 @@ __device__ __forceinline__ int tiles_of(const Q4Cache& c, int unit) {
   return (length_of(c, unit) + kQ4TileSlots - 1) / kQ4TileSlots;
 }
 
-// A place in the sequence of tiles.
+// A tile's place in the sequence of tiles.
 struct Place {
-  int unit, block, tile, len;  // len: slots in use of the unit
-  __device__ __forceinline__ int tiles() const { return (len + kQ4TileSlots - 1) / kQ4TileSlots; }
+  int unit, block;
+  int row;    // slot row of the cache: unit * capacity + first slot
+  int valid;  // slots in use from there on
   // The next tile; past the end of a row block the next one that has tiles
-  // (or unit = units).
-  __device__ __forceinline__ void next(const Q4AttendParams& p, int units) {
-    if (++tile < tiles()) return;
-    tile = 0;
-    if (++block < p.blocks) return;
-    block = 0;
-    do {
+  // (the caller knows that there is one).
+  __device__ __forceinline__ void next(const Q4AttendParams& p) {
+    row += kQ4TileSlots;
+    valid -= kQ4TileSlots;
+    if (valid > 0) return;
+    if (++block == p.blocks) {
+      block = 0;
       ++unit;
-      len = unit < units ? length_of(p.c, unit) : 0;
-    } while (unit < units && len == 0);
+    }
+    while ((valid = length_of(p.c, unit)) == 0) ++unit;
+    row = unit * p.c.capacity;
   }
 };
 
@@ -189,13 +215,22 @@ __device__ __forceinline__ long long cta_scan(long long v, long long* s_sums, lo
   return before + x - v;
 }
 
-// The query rows of a row block as operands: row lane/4 (and 8 more).
+// The largest of 16 s and |m| of a params row, as the bits of a float (whose
+// order is that of the numbers; NaN above all).
+__device__ __forceinline__ uint32_t top_of(uint4 w) {
+  const uint32_t s = max(max(w.x << 16, w.x & 0xffff0000u), max(w.y << 16, w.y & 0xffff0000u)) + (4u << 23);
+  const uint32_t z = max((w.z << 16) & 0x7fff0000u, w.z & 0x7fff0000u);
+  return max(s, max(z, max((w.w << 16) & 0x7fff0000u, w.w & 0x7fff0000u)));
+}
+
+// The query rows of a row block as operands: row lane/4 of each 8.
 template <int NB>
 struct Queries {
-  uint32_t a[NB][2][8];      // [8 rows][k half][4 groups x 2 steps]
-  uint32_t sum[NB][2];       // group sums * 2^-24 as three bf16 parts
-  float f1, f2[NB];          // z = (products * f1) * f2
-  int limit[NB];             // q_position
+  uint32_t b[NB][8][2];      // [8 rows][4 groups x 2 steps][k half]
+  uint32_t sum[NB][2];       // group sums as three bf16 parts, scaled like the codes' products
+  // of rows 2 (lane % 4) and the next, the columns of a result:
+  float f2[NB][2];           // z = products * f2 (K's scales carry the softmax scale)
+  int limit[NB][2];          // q_position
 };
 
 template <int NB>
@@ -203,17 +238,17 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int b = unit / p.c.num_kv_heads, kv = unit - b * p.c.num_kv_heads;
   const bool bf16 = p.is_bf16 != 0;
-  Q.f1 = p.scale_log2 * 1024.0f;  // codes carry 2^-24, queries 2^14
+  const float f1 = p.scale_log2 * 1024.0f;  // codes carry 2^-24, queries 2^14
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = block * (8 * NB) + nb * 8 + g;
     float x[4][8];
     uint32_t top = 0;
-    Q.limit[nb] = 0x7fffffff;
+    int limit = 0x7fffffff;
     if (r < p.rows) {
       const int h = kv * p.group + r / p.num_queries, qi = r % p.num_queries;
       const uint16_t* src = p.q + b * p.q_bs + h * p.q_hs + qi * p.q_qs + 8 * t;
-      if (p.q_positions) Q.limit[nb] = __ldg(p.q_positions + b * p.num_queries + qi);
+      if (p.q_positions) limit = __ldg(p.q_positions + b * p.num_queries + qi);
 #pragma unroll
       for (int J = 0; J < 4; ++J) {
         const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + 32 * J));
@@ -236,7 +271,11 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
     int e = top >= 0x7f800000u || top == 0 ? 14 : static_cast<int>(top >> 23) - 127;
     e = max(e, -110);  // smaller rows (bf16) scale by no more than 2^124
     const float up = pow2(14 - e);
-    Q.f2[nb] = pow2(max(e, -126));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      Q.f2[nb][j] = __shfl_sync(0xffffffffu, pow2(e), 8 * t + 4 * j);
+      Q.limit[nb][j] = __shfl_sync(0xffffffffu, limit, 8 * t + 4 * j);
+    }
     float part[4];
 #pragma unroll
     for (int J = 0; J < 4; ++J) {
@@ -248,12 +287,12 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
       }
       part[J] += __shfl_xor_sync(0xffffffffu, part[J], 1);
       part[J] += __shfl_xor_sync(0xffffffffu, part[J], 2);
-      part[J] *= 5.9604644775390625e-8f;  // 2^-24
+      part[J] *= 5.9604644775390625e-8f * f1;  // 2^-24
       // nibbles (0, 4), (1, 5), (2, 6), (3, 7) of a word; the odd ones count 16-fold
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        Q.a[nb][0][2 * J + st] = pack_half2(x[J][2 * st], x[J][2 * st + 4]);
-        Q.a[nb][1][2 * J + st] = pack_half2(x[J][2 * st + 1] * 0.0625f, x[J][2 * st + 5] * 0.0625f);
+        Q.b[nb][2 * J + st][0] = pack_half2(x[J][2 * st], x[J][2 * st + 4]);
+        Q.b[nb][2 * J + st][1] = pack_half2(x[J][2 * st + 1] * 0.0625f, x[J][2 * st + 5] * 0.0625f);
       }
     }
     // k index J + 4 * part: this lane's pairs are groups 2 (t & 1), 2 (t & 1) + 1
@@ -279,7 +318,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   const uint32_t codes = base + warp * S::kStages * 2 * kCodeTile;
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
-  const uint32_t bars = base + S::kCodes + S::kSide + warp * S::kStages * 8;
+  const uint32_t scales = base + S::kCodes + S::kSide + warp * kScaleTile;
+  const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
   if (lane == 0)
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
   if (threadIdx.x == 0) s_abort = 0;
@@ -318,7 +358,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   }
   __syncthreads();
   const long long from = worker * chunk;
-  long long left = min(chunk, total - from);  // tiles of this worker
+  int left = static_cast<int>(min(chunk, total - from));  // tiles of this worker
   if (chunk == 0 || left <= 0) return;
   Place c;
   {
@@ -329,29 +369,29 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       at += static_cast<long long>(n) * p.blocks;
       ++u;
     }
-    c.unit = u;
-    c.len = length_of(p.c, u);
     const long long in = from - at;
+    c.unit = u;
     c.block = static_cast<int>(in / n);
-    c.tile = static_cast<int>(in - static_cast<long long>(c.block) * n);
+    const int slot = static_cast<int>(in - static_cast<long long>(c.block) * n) * kQ4TileSlots;
+    c.row = u * p.c.capacity + slot;
+    c.valid = length_of(p.c, u) - slot;
   }
 
   constexpr uint32_t kBytes = 2 * kCodeTile + 2 * kParamTile + (kPos ? kPosTile : 0);
   Place ahead = c;
-  long long to_issue = left;
+  int to_issue = left;
   auto issue = [&](int stage) {
     if (lane == 0) {
       const uint32_t bar = bars + 8 * stage, cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
-      const long long row = static_cast<long long>(ahead.unit) * p.c.capacity + ahead.tile * kQ4TileSlots;
       mbar_arrive_expect_tx(bar, kBytes);
-      tma_rows(cd, &p.map_k, bar, static_cast<int>(row));
-      tma_rows(cd + kCodeTile, &p.map_v, bar, static_cast<int>(row));
+      tma_rows(cd, &p.map_k, bar, ahead.row);
+      tma_rows(cd + kCodeTile, &p.map_v, bar, ahead.row);
+      const size_t row = static_cast<size_t>(ahead.row);
       bulk_copy(sd, p.c.params[0] + row * kQ4ParamBytes, kParamTile, bar);
       bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, kParamTile, bar);
       if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, kPosTile, bar);
     }
-    --to_issue;
-    if (to_issue > 0) ahead.next(p, units);
+    if (--to_issue > 0) ahead.next(p);
   };
   for (int i = 0; i < S::kStages && to_issue > 0; ++i) issue(i);
 
@@ -359,10 +399,11 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   // stored at piece ^ (slot / 2) by the 64-byte swizzle
   const uint32_t mat = (lane & 7) * kQ4CodeBytes + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
 
+  const float f1 = p.scale_log2 * 1024.0f;
   Queries<NB> Q;
   float o[NB][4][2][4];   // [8 rows][group][step][channel, row pair]
   float om[NB][4];        // minima's term (lanes of g >= 4)
-  float ref[NB], l[NB];
+  float ref[NB][2], l[NB][2];  // rows 2t, 2t + 1
   int vexp = kMinScaleExp;
   bool fresh = true;
   uint32_t phase = 0;
@@ -374,8 +415,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       load_queries<NB>(p, c.unit, c.block, Q);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        ref[nb] = -INFINITY;
-        l[nb] = 0.f;
+        ref[nb][0] = ref[nb][1] = -INFINITY;
+        l[nb][0] = l[nb][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) om[nb][i] = 0.f;
 #pragma unroll
@@ -394,204 +435,234 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     }
     __syncwarp();
     const uint32_t cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
-    const int slot0 = c.tile * kQ4TileSlots, valid = c.len - slot0;
+    const int valid = c.valid;
 
-    // ---- scales of V: the largest of the tile; NaN groups and slots behind
-    // the length are taken out (their codes then count nothing)
-    uint32_t nan_groups = 0;  // lane = slot: groups that hold a NaN
-    uint32_t special = 0;
+    // ---- scales: one lane a slot.  Slots behind the length and groups that
+    // hold a NaN count nothing in V's products
+    uint32_t nan_groups = 0;  // of this lane's slot
+    bool special;
     {
+      const uint2 kw = lds64(sd + lane * kQ4ParamBytes);
       uint4 w = lds128(sd + kParamTile + lane * kQ4ParamBytes);
-      uint32_t top = max(max(w.x << 16, w.x & 0xffff0000u), max(w.y << 16, w.y & 0xffff0000u));
-      const uint32_t mz = w.z & 0x7fff7fffu, mw = w.w & 0x7fff7fffu;
-      const uint32_t mtop = max(max(mz << 16, mz & 0xffff0000u), max(mw << 16, mw & 0xffff0000u));
-      uint32_t both = max(top, mtop);
-      if (lane >= valid) both = 0xffffffffu;
-      special = __any_sync(0xffffffffu, both >= 0x7f800000u);
+      if (lane >= valid) w = make_uint4(0u, 0u, 0u, 0u);
+      sts128(scales + lane * 16,
+             make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
+                        __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
+      uint32_t all = __reduce_max_sync(0xffffffffu, top_of(w));
+      special = all >= 0x7f800000u;
       if (special) {
-        uint32_t s[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
-        uint32_t m[4] = {w.z & 0xffffu, w.z >> 16, w.w & 0xffffu, w.w >> 16};
-        top = 0;
+        uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int J = 0; J < 4; ++J) {
-          const bool bad = (s[J] & 0x7fffu) >= 0x7f80u || (m[J] & 0x7fffu) >= 0x7f80u;
-          if (bad && lane < valid) nan_groups |= 1u << J;
-          if (bad || lane >= valid) s[J] = m[J] = 0u;
-          top = max(top, s[J] << 16);
+          const uint32_t half = 0xffffu << (16 * (J & 1)), inf = 0x7f807f80u & half;
+          if ((x[J >> 1] & inf) == inf || (x[2 + (J >> 1)] & inf) == inf) {
+            nan_groups |= 1u << J;
+            x[J >> 1] &= ~half;
+            x[2 + (J >> 1)] &= ~half;
+          }
         }
-        w = make_uint4(s[0] | s[1] << 16, s[2] | s[3] << 16, m[0] | m[1] << 16, m[2] | m[3] << 16);
-        sts128(sd + kParamTile + lane * kQ4ParamBytes, w);
-        __syncwarp();
+        w = make_uint4(x[0], x[1], x[2], x[3]);
+        all = min(__reduce_max_sync(0xffffffffu, top_of(w)), 0x7f000000u);
       }
-      const int k = max(static_cast<int>(__reduce_max_sync(0xffffffffu, top) >> 23) - 127, kMinScaleExp);
-      if (k > vexp) {  // the codes' sums go to the new power of two
+      const int k = max(static_cast<int>(all >> 23) - 127, kMinScaleExp);
+      if (k > vexp) {  // the sums go to the new power of two
         const float f = pow2(max(vexp - k, -126));
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+          om[nb][0] *= f;
+          om[nb][1] *= f;
 #pragma unroll
           for (int J = 0; J < 4; ++J)
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[nb][J][st][i] *= f;
+        }
         vexp = k;
       }
+      const float f = pow2(kTopExp - vexp);
+      const uint32_t s01 = pack_half2(bf_lo(w.x) * f, bf_hi(w.x) * f);
+      const uint32_t s23 = pack_half2(bf_lo(w.y) * f, bf_hi(w.y) * f);
+      // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
+      const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
+      sts128(sd + kParamTile + lane * kQ4ParamBytes,
+             make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632),
+                        pack_half2(bf_lo(w.z) * f, bf_hi(w.z) * f),
+                        pack_half2(bf_lo(w.w) * f, bf_hi(w.w) * f)));
+      __syncwarp();
     }
 
-    // ---- logits: four times 8 slots
-    float z[NB][4][2];
+    // ---- logits: twice 16 slots; slots g and g + 8 of rows 2t and 2t + 1
+    float z[NB][2][4];  // [8 rows][16 slots][slot half, row]
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      uint32_t w[4];
-      ldmatrix4(w, cd + n * 8 * kQ4CodeBytes + mat);
-      const uint32_t mins = lds32(sd + (n * 8 + g) * kQ4ParamBytes + 8 + (t & 1) * 4);
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
-      mma_bf16(acc, Q.sum[0][0], NB > 1 ? Q.sum[NB - 1][0] : 0u, Q.sum[0][1],
-               NB > 1 ? Q.sum[NB - 1][1] : 0u, mins, mins);
-      const uint2 sa = lds64(sd + (n * 8 + 2 * t) * kQ4ParamBytes);
-      const uint2 sb = lds64(sd + (n * 8 + 2 * t + 1) * kQ4ParamBytes);
-#pragma unroll
-      for (int J = 0; J < 4; ++J) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint32_t hi = w[J] >> 8;
-        mma_f16(x, Q.a[0][0][2 * J], NB > 1 ? Q.a[NB - 1][0][2 * J] : 0u, Q.a[0][1][2 * J],
-                NB > 1 ? Q.a[NB - 1][1][2 * J] : 0u, w[J] & 0x000f000fu, w[J] & 0x00f000f0u);
-        mma_f16(x, Q.a[0][0][2 * J + 1], NB > 1 ? Q.a[NB - 1][0][2 * J + 1] : 0u, Q.a[0][1][2 * J + 1],
-                NB > 1 ? Q.a[NB - 1][1][2 * J + 1] : 0u, hi & 0x000f000fu, hi & 0x00f000f0u);
-        const uint32_t wa = J < 2 ? sa.x : sa.y, wb = J < 2 ? sb.x : sb.y;
-        const float s0 = J & 1 ? bf_hi(wa) : bf_lo(wa), s1 = J & 1 ? bf_hi(wb) : bf_lo(wb);
-        acc[0] = fmaf(x[0], s0, acc[0]);
-        acc[1] = fmaf(x[1], s1, acc[1]);
-        if (NB > 1) {
-          acc[2] = fmaf(x[2], s0, acc[2]);
-          acc[3] = fmaf(x[3], s1, acc[3]);
-        }
-      }
+    for (int h = 0; h < 2; ++h) {
+      const int s16 = h * 16;
+      uint32_t wa[4], wb[4];
+      ldmatrix4(wa, cd + s16 * kQ4CodeBytes + mat);
+      ldmatrix4(wb, cd + (s16 + 8) * kQ4CodeBytes + mat);
+      const uint32_t ma = lds32(sd + (s16 + g) * kQ4ParamBytes + 8 + (t & 1) * 4);
+      const uint32_t mb = lds32(sd + (s16 + 8 + g) * kQ4ParamBytes + 8 + (t & 1) * 4);
+      const uint4 sa = lds128(scales + (s16 + g) * 16), sb = lds128(scales + (s16 + 8 + g) * 16);
+      const uint32_t ka[4] = {sa.x, sa.y, sa.z, sa.w}, kb[4] = {sb.x, sb.y, sb.z, sb.w};
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        z[nb][n][0] = acc[2 * nb] * Q.f1 * Q.f2[nb];
-        z[nb][n][1] = acc[2 * nb + 1] * Q.f1 * Q.f2[nb];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[nb][h][i] = 0.f;
+        mma_bf16(z[nb][h], ma, mb, ma, mb, Q.sum[nb][0], Q.sum[nb][1]);
       }
-      if (kPos) {
-        const uint2 at = lds64(sd + 2 * kParamTile + (n * 8 + 2 * t) * 4);
+#pragma unroll
+      for (int J = 0; J < 4; ++J) {
+        const uint32_t ha = wa[J] >> 8, hb = wb[J] >> 8;
+        const uint32_t a0 = wa[J] & 0x000f000fu, a1 = wb[J] & 0x000f000fu;
+        const uint32_t a2 = wa[J] & 0x00f000f0u, a3 = wb[J] & 0x00f000f0u;
+        const uint32_t b0 = ha & 0x000f000fu, b1 = hb & 0x000f000fu;
+        const uint32_t b2 = ha & 0x00f000f0u, b3 = hb & 0x00f000f0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          if (static_cast<int>(at.x) > Q.limit[nb]) z[nb][n][0] = -INFINITY;
-          if (static_cast<int>(at.y) > Q.limit[nb]) z[nb][n][1] = -INFINITY;
+          float x[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_f16(x, a0, a1, a2, a3, Q.b[nb][2 * J][0], Q.b[nb][2 * J][1]);
+          mma_f16(x, b0, b1, b2, b3, Q.b[nb][2 * J + 1][0], Q.b[nb][2 * J + 1][1]);
+          z[nb][h][0] = fmaf(x[0], __uint_as_float(ka[J]), z[nb][h][0]);
+          z[nb][h][1] = fmaf(x[1], __uint_as_float(ka[J]), z[nb][h][1]);
+          z[nb][h][2] = fmaf(x[2], __uint_as_float(kb[J]), z[nb][h][2]);
+          z[nb][h][3] = fmaf(x[3], __uint_as_float(kb[J]), z[nb][h][3]);
         }
+      }
+      if (kPos) {
+        const int at0 = static_cast<int>(lds32(sd + 2 * kParamTile + (s16 + g) * 4));
+        const int at1 = static_cast<int>(lds32(sd + 2 * kParamTile + (s16 + 8 + g) * 4));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (at0 > Q.limit[nb][j]) z[nb][h][j] = -INFINITY;
+            if (at1 > Q.limit[nb][j]) z[nb][h][2 + j] = -INFINITY;
+          }
       }
     }
     if (valid < kQ4TileSlots) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (n * 8 + 2 * t + i >= valid)
+        for (int i = 0; i < 4; ++i)
+          if (h * 16 + (i >> 1) * 8 + g >= valid)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) z[nb][n][i] = -INFINITY;
+            for (int nb = 0; nb < NB; ++nb) z[nb][h][i] = -INFINITY;
     }
     if (p.accumulate) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int r = c.block * (8 * NB) + nb * 8 + g;
-        if (r < p.rows) {
-          float2* zp = reinterpret_cast<float2*>(
-              p.z + (static_cast<long long>(c.unit) * p.rows + r) * p.c.capacity + slot0 + 2 * t);
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int n = 0; n < 4; ++n) zp[n * 4] = make_float2(z[nb][n][0], z[nb][n][1]);
+        for (int j = 0; j < 2; ++j) {
+          const int r = c.block * (8 * NB) + nb * 8 + 2 * t + j;
+          if (r < p.rows) {
+            float* zp = p.z + (static_cast<long long>(c.unit) * (p.rows - 1) + r) * p.c.capacity + c.row + g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              zp[h * 16] = z[nb][h][j] * Q.f2[nb][j];
+              zp[h * 16 + 8] = z[nb][h][2 + j] * Q.f2[nb][j];
+            }
+          }
         }
-      }
     }
 
     // ---- references, probabilities (in place of z)
-    uint32_t seen_nan = 0;
+    uint32_t seen_nan[2] = {0u, 0u};
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      float top = -INFINITY;
+      float top[2];
+      bool raise = false;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(z[nb][n][0], z[nb][n][1]));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const bool raise = top > ref[nb] + kRaise;
+      for (int j = 0; j < 2; ++j) {
+        top[j] = fmaxf(fmaxf(z[nb][0][j], z[nb][0][2 + j]), fmaxf(z[nb][1][j], z[nb][1][2 + j]));
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 4));
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8));
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16)) * Q.f2[nb][j];
+        raise |= top[j] > ref[nb][j] + kRaise;
+      }
       if (__any_sync(0xffffffffu, raise)) {
-        const float f = raise ? (ref[nb] == -INFINITY ? 0.f : ex2_approx(ref[nb] - top)) : 1.0f;
-        if (raise) ref[nb] = top;
-        l[nb] *= f;
-        // rows 2t and 2t + 1 are this lane's columns of the outputs
-        const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
 #pragma unroll
-        for (int J = 0; J < 4; ++J)
+        for (int j = 0; j < 2; ++j) {
+          if (!(top[j] > ref[nb][j] + kRaise)) continue;
+          const float f = ref[nb][j] == -INFINITY ? 0.f : ex2_approx(ref[nb][j] - top[j]);
+          ref[nb][j] = top[j];
+          l[nb][j] *= f;
+          om[nb][j] *= f;
 #pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            o[nb][J][st][0] *= f0;
-            o[nb][J][st][1] *= f1;
-            o[nb][J][st][2] *= f0;
-            o[nb][J][st][3] *= f1;
-          }
-        om[nb][0] *= f0;
-        om[nb][1] *= f1;
+          for (int J = 0; J < 4; ++J)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              o[nb][J][st][j] *= f;
+              o[nb][J][st][2 + j] *= f;
+            }
+        }
       }
       if (special) {
         // rows that see a slot's NaN group
-        uint32_t hit = 0;
+        uint32_t hit[2] = {0u, 0u};
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t m = __shfl_sync(0xffffffffu, nan_groups, n * 8 + 2 * t + i);
-            if (z[nb][n][i] != -INFINITY) hit |= m;
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t m = __shfl_sync(0xffffffffu, nan_groups, h * 16 + (i >> 1) * 8 + g);
+            if (z[nb][h][i] != -INFINITY) hit[i & 1] |= m;
           }
-        hit |= __shfl_xor_sync(0xffffffffu, hit, 1);
-        hit |= __shfl_xor_sync(0xffffffffu, hit, 2);
-        seen_nan |= hit << (4 * nb);
-      }
-      const float r = ref[nb] == -INFINITY ? 0.f : ref[nb];
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          z[nb][n][i] = ex2_approx(z[nb][n][i] - r);
-          l[nb] += z[nb][n][i];
+        for (int j = 0; j < 2; ++j) {
+          hit[j] |= __shfl_xor_sync(0xffffffffu, hit[j], 4);
+          hit[j] |= __shfl_xor_sync(0xffffffffu, hit[j], 8);
+          hit[j] |= __shfl_xor_sync(0xffffffffu, hit[j], 16);
+          seen_nan[j] |= hit[j] << (4 * nb);
         }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float r = ref[nb][j] == -INFINITY ? 0.f : ref[nb][j] - kLift;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = j; i < 4; i += 2) {
+            z[nb][h][i] = ex2_approx(fmaf(z[nb][h][i], Q.f2[nb][j], -r));
+            l[nb][j] += z[nb][h][i];
+          }
+      }
     }
 
     // ---- outputs: twice 16 slots
-    const float inv = pow2(kTopExp - vexp);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int s16 = h * 16;
       uint32_t va[4], vb[4], pm[4];
       ldmatrix4_t(va, cd + kCodeTile + s16 * kQ4CodeBytes + mat);
       ldmatrix4_t(vb, cd + kCodeTile + (s16 + 8) * kQ4CodeBytes + mat);
-      // params as 8x8 matrices of slots x (scales, minima): rows 4-7 of the
-      // transposed operand are the minima (lanes 16-31 repeat the addresses)
-      ldmatrix4_t(pm, sd + kParamTile + (s16 + (lane & 15)) * kQ4ParamBytes);
+      // rows of [2 pairs of scales, 4 minima]: rows 4-7 of the transposed
+      // operand are the minima; rows 8-15 repeat rows 0-7
+      ldmatrix4_t(pm, sd + kParamTile + (s16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
       const uint2 s0 = lds64(sd + kParamTile + (s16 + 2 * t) * kQ4ParamBytes);
       const uint2 s1 = lds64(sd + kParamTile + (s16 + 2 * t + 1) * kQ4ParamBytes);
       const uint2 s2 = lds64(sd + kParamTile + (s16 + 8 + 2 * t) * kQ4ParamBytes);
       const uint2 s3 = lds64(sd + kParamTile + (s16 + 9 + 2 * t) * kQ4ParamBytes);
+      const uint32_t sa[4] = {s0.x, s0.y, s1.x, s1.y}, sb[4] = {s2.x, s2.y, s3.x, s3.y};
+      uint32_t p0[NB], p1[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const float p0 = z[nb][2 * h][0], p1 = z[nb][2 * h][1];
-        const float p2 = z[nb][2 * h + 1][0], p3 = z[nb][2 * h + 1][1];
-        const uint32_t h0 = pack_bf16(p0, p1), h1 = pack_bf16(p2, p3);
-        mma_bf16(om[nb], pm[0], 0u, pm[1], 0u, h0, h1);
-        mma_bf16(om[nb], pm[0], 0u, pm[1], 0u, pack_bf16(p0 - bf_lo(h0), p1 - bf_hi(h0)),
-                 pack_bf16(p2 - bf_lo(h1), p3 - bf_hi(h1)));
-        const float q0 = p0 * inv, q1 = p1 * inv, q2 = p2 * inv, q3 = p3 * inv;
+        p0[nb] = transpose8(pack_half2(z[nb][h][0], z[nb][h][1]));
+        p1[nb] = transpose8(pack_half2(z[nb][h][2], z[nb][h][3]));
+        mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], p0[nb], p1[nb]);
+      }
 #pragma unroll
-        for (int J = 0; J < 4; ++J) {
-          const uint32_t w0 = J < 2 ? s0.x : s0.y, w1 = J < 2 ? s1.x : s1.y;
-          const uint32_t w2 = J < 2 ? s2.x : s2.y, w3 = J < 2 ? s3.x : s3.y;
-          const uint32_t b0 = J & 1 ? pack_half2(q0 * bf_hi(w0), q1 * bf_hi(w1))
-                                    : pack_half2(q0 * bf_lo(w0), q1 * bf_lo(w1));
-          const uint32_t b1 = J & 1 ? pack_half2(q2 * bf_hi(w2), q3 * bf_hi(w3))
-                                    : pack_half2(q2 * bf_lo(w2), q3 * bf_lo(w3));
-          const uint32_t ah = va[J] >> 8, bh = vb[J] >> 8;
-          mma_f16(o[nb][J][0], va[J] & 0x000f000fu, va[J] & 0x00f000f0u, vb[J] & 0x000f000fu,
-                  vb[J] & 0x00f000f0u, b0, b1);
-          mma_f16(o[nb][J][1], ah & 0x000f000fu, ah & 0x00f000f0u, bh & 0x000f000fu, bh & 0x00f000f0u,
-                  b0, b1);
+      for (int J = 0; J < 4; ++J) {
+        const uint32_t ah = va[J] >> 8, bh = vb[J] >> 8;
+        const uint32_t a0 = va[J] & 0x000f000fu, a1 = va[J] & 0x00f000f0u;
+        const uint32_t a2 = vb[J] & 0x000f000fu, a3 = vb[J] & 0x00f000f0u;
+        const uint32_t b0 = ah & 0x000f000fu, b1 = ah & 0x00f000f0u;
+        const uint32_t b2 = bh & 0x000f000fu, b3 = bh & 0x00f000f0u;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const uint32_t q0 = mul_half2(p0[nb], sa[J]), q1 = mul_half2(p1[nb], sb[J]);
+          mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
+          mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
         }
       }
     }
@@ -599,18 +670,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       const float bad = __uint_as_float(0x7fc00000u);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const uint32_t h0 = __shfl_sync(0xffffffffu, seen_nan, 8 * t) >> (4 * nb);
-        const uint32_t h1 = __shfl_sync(0xffffffffu, seen_nan, 8 * t + 4) >> (4 * nb);
 #pragma unroll
         for (int J = 0; J < 4; ++J)
 #pragma unroll
           for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (((i & 1 ? h1 : h0) >> J) & 1u) o[nb][J][st][i] = bad;
+              if ((seen_nan[i & 1] >> (4 * nb + J)) & 1u) o[nb][J][st][i] = bad;
       }
     }
-    if (special) fence_proxy_async_smem();  // (it wrote to the stage)
+    fence_proxy_async_smem();  // (the scales were written into the stage)
     __syncwarp();  // every lane is done with the stage
     if (to_issue > 0) issue(stage);
     if (++stage == S::kStages) {
@@ -620,15 +689,19 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 
     // ---- the row block ends here, or this worker's share of it
     const int unit = c.unit, block = c.block;
-    if (left > 1) c.next(p, units);
+    if (left > 1) c.next(p);
     if (left == 1 || c.unit != unit || c.block != block) {
       const long long part = static_cast<long long>(worker) + static_cast<long long>(unit) * p.blocks + block;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float sum = l[nb];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (t == 0) p.part_ml[part * (8 * NB) + nb * 8 + g] = make_float2(ref[nb], sum);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float sum = l[nb][j];
+          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+          if (g == 0) p.part_ml[part * (8 * NB) + nb * 8 + 2 * t + j] = make_float2(ref[nb][j] - kLift, sum);
+        }
         const float f = pow2(vexp - kTopExp);  // codes' sums: * 2^24, and 1/16 for the odd channels
         float* dst = p.part_o + (part * (8 * NB) + nb * 8) * kHeadDim;
 #pragma unroll
@@ -639,10 +712,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           for (int i = 0; i < 2; ++i) {
             const float m = i ? m1 : m0;
             float4 v;
-            v.x = fmaf(o[nb][J][0][i] * 16777216.0f, f, m);
-            v.y = fmaf(o[nb][J][0][2 + i] * 1048576.0f, f, m);
-            v.z = fmaf(o[nb][J][1][i] * 16777216.0f, f, m);
-            v.w = fmaf(o[nb][J][1][2 + i] * 1048576.0f, f, m);
+            v.x = fmaf(o[nb][J][0][i], 16777216.0f, m) * f;
+            v.y = fmaf(o[nb][J][0][2 + i], 1048576.0f, m) * f;
+            v.z = fmaf(o[nb][J][1][i], 16777216.0f, m) * f;
+            v.w = fmaf(o[nb][J][1][2 + i], 1048576.0f, m) * f;
             if (block * (8 * NB) + nb * 8 + 2 * t + i < p.rows)
               *reinterpret_cast<float4*>(dst + (2 * t + i) * kHeadDim + 32 * J + 4 * g) = v;
           }
