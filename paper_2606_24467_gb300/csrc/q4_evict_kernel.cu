@@ -7,14 +7,17 @@
 // receives the j-th kept slot at or above b.  Sources and destinations are
 // disjoint, so the copies need no order.
 //
-// A CTA, or a cluster of up to eight, takes a unit.  Weights and positions are
-// read once into shared memory as order-preserving 32-bit keys; the b-th
-// largest key comes from at most four passes of a radix selection (8 bits each,
-// most significant first), whose histograms the CTAs of a cluster add up from
-// one another's shared memory.  Then warps count, in slot order, the ties, the
-// holes below b and the kept rows behind it, list the latter two, and copy.
-// Bound by latency: a handful of barriers and two dependent trips to memory
-// against 8 bytes a slot and 344 a moved row.
+// A CTA, or a cluster of up to eight, takes a unit, and every warp a run of
+// its slots, whose weights it holds in registers as order-preserving 32-bit
+// keys (units beyond 131072 slots are read again for every sweep).  A radix
+// selection of 8 bits a pass, whose histograms the CTAs of a cluster add up
+// from one another's shared memory, goes on until at most 64 slots can be the
+// last one kept: those are ranked by (key, slot) directly, which settles ties
+// too.  More equal weights than that are counted in slot order instead.  Then
+// the warps count the holes below b and the kept rows behind it, list both in
+// slot order, and copy.
+// Bound by latency and instructions: a dozen barriers and three dependent trips
+// to memory against 8 bytes a slot and 344 a moved row.
 #include <cuda_runtime.h>
 
 #include "ckv_device.cuh"
@@ -25,6 +28,9 @@ namespace ckv {
 namespace {
 
 constexpr int kBins = 256;
+constexpr int kRanked = 64;  // slots that are ranked directly
+constexpr int kItems = 16;   // keys a lane holds at most
+constexpr int kShortItems = 5;  // ... in a CTA of 256 threads for short units
 
 // Order-preserving key of a weight: larger weight, larger key; -0 and +0 are
 // one, NaN lies below everything.
@@ -58,39 +64,89 @@ __device__ __forceinline__ void unit_sync() {
   }
 }
 
-// kCluster: more CTAs than one a unit; kShared: keys and positions fit shared
-// memory (else they are read again wherever they are needed).
-template <int kThreads, bool kCluster, bool kShared>
-__global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__ Q4EvictParams p) {
+__device__ __forceinline__ int4 remote_words(uint32_t addr, uint32_t rank) {
+  int4 v;
+  asm volatile(
+      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\t"
+      "ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [a];\n\t}"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "r"(addr), "r"(rank)
+      : "memory");
+  return v;
+}
+
+// kHold: keys a lane holds (0: none, they are read again).
+template <int kThreads, int kHold, bool kCluster>
+__global__ void __launch_bounds__(kThreads, kHold == kShortItems ? 6 : 1) evict_kernel(const __grid_constant__ Q4EvictParams p) {
   constexpr int kWarps = kThreads / 32;
-  extern __shared__ uint32_t s_keys[];  // [slice] keys, then [slice] positions (later the lists)
-  __shared__ int s_hist[4][kBins];
-  __shared__ int s_newest, s_pick[3], s_ties[kWarps], s_holes[kWarps], s_rows[kWarps], s_sums[kBins / 32];
+  constexpr int kHists = kCluster ? 4 : 1;  // one a pass where other CTAs read it
+  extern __shared__ int32_t s_lists[];      // a single CTA's holes and rows
+  __shared__ __align__(16) int s_hist[kHists][kBins];
+  __shared__ uint32_t s_key[kRanked], s_all_key[kCluster ? kRanked : 1];
+  __shared__ int s_slot[kRanked], s_all_slot[kCluster ? kRanked : 1], s_ranked, s_newest, s_pick[3];
+  __shared__ uint32_t s_last[2];
+  __shared__ int s_ties[kWarps], s_holes[kWarps], s_rows[kWarps];
   const uint32_t ranks = kCluster ? p.cluster : 1, rank = kCluster ? cluster_rank() : 0;
   const int unit = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int n = min(max(p.c.lengths[unit], 0), p.c.capacity);
-  const int b = p.budgets ? p.budgets[unit] : p.budget;
-  if (b < 0 || b >= n) return;  // (for every CTA of the unit)
   const long long base = static_cast<long long>(unit) * p.c.capacity;
   const int32_t* pos = p.c.positions + base;
   const float* wt = p.c.weights + base;
-  const int slice = ((n + static_cast<int>(ranks) - 1) / static_cast<int>(ranks) + 31) & ~31;
-  const int s0 = min(static_cast<int>(rank) * slice, n), s1 = min(s0 + slice, n);
-  int32_t* s_pos = reinterpret_cast<int32_t*>(s_keys + slice);
-
-  for (int i = tid; i < 4 * kBins; i += kThreads) (&s_hist[0][0])[i] = 0;
-  if (tid == 0) s_newest = -0x7fffffff - 1;
-  __syncthreads();
-  int newest = -0x7fffffff - 1;
-#pragma unroll 4
-  for (int j = s0 + tid; j < s1; j += kThreads) {
-    const int at = pos[j];
-    newest = max(newest, at);
-    if (kShared) {
-      s_pos[j - s0] = at;
-      s_keys[j - s0] = weight_key(wt[j]);
+  // this warp's run of slots.  Short units are cut by their capacity, so that
+  // their loads need not wait for the length.
+  constexpr bool kEarly = kHold == kShortItems;
+  const int parts = static_cast<int>(ranks) * kWarps;
+  const int order = static_cast<int>(rank) * kWarps + warp;
+  int run = ((p.c.capacity + parts - 1) / parts + 31) & ~31;
+  uint32_t held[kHold ? kHold : 1];
+  int at[kHold ? kHold : 1];
+  constexpr int kNone = -0x7fffffff - 1;
+  int newest = kNone;
+  if (kEarly) {
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) {
+      const int j = order * run + 32 * i + lane;
+      at[i] = kNone;
+      held[i] = 0u;
+      if (32 * i < run && j < p.c.capacity) {
+        at[i] = pos[j];
+        held[i] = __float_as_uint(wt[j]);
+      }
     }
   }
+  const int n = min(max(p.c.lengths[unit], 0), p.c.capacity);
+  const int b = p.budgets ? p.budgets[unit] : p.budget;
+  if (b < 0 || b >= n) return;  // (for every CTA of the unit)
+  if (!kEarly) run = ((n + parts - 1) / parts + 31) & ~31;
+  const int w0 = min(order * run, n), w1 = min(w0 + run, n);
+
+  for (int i = tid; i < kHists * kBins; i += kThreads) (&s_hist[0][0])[i] = 0;
+  if (tid == 0) {
+    s_newest = kNone;
+    s_ranked = 0;
+  }
+  if (kHold) {
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) {
+      const int j = w0 + 32 * i + lane;
+      if (!kEarly) {
+        at[i] = kNone;
+        held[i] = 0u;
+        if (j < w1) {
+          at[i] = pos[j];
+          held[i] = __float_as_uint(wt[j]);
+        }
+      } else if (j >= w1) {
+        at[i] = kNone;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) held[i] = weight_key(__uint_as_float(held[i]));
+#pragma unroll
+    for (int i = 0; i < kHold; ++i) newest = max(newest, at[i]);
+  } else {
+    for (int j = w0 + lane; j < w1; j += 32) newest = max(newest, pos[j]);
+  }
+  __syncthreads();
   newest = __reduce_max_sync(0xffffffffu, newest);
   if (lane == 0) atomicMax(&s_newest, newest);
   unit_sync<kCluster>();
@@ -100,72 +156,140 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   auto forced = [&](int at) {
     return at < p.sinks || static_cast<long long>(at) > static_cast<long long>(newest) - p.recent;
   };
-  // (the keys of forced slots are put in place in the first pass)
-  auto key_at = [&](int j) -> uint32_t {
-    if (kShared) return s_keys[j - s0];
-    return forced(pos[j]) ? 0xffffffffu : weight_key(wt[j]);
+  if (kHold) {
+#pragma unroll
+    for (int i = 0; i < kHold; ++i)
+      if (forced(at[i])) held[i] = 0xffffffffu;
+  }
+  // f(slot, key) for every slot of this lane's share of the run (all lanes of
+  // the warp together; slots at or behind w1 are no slots)
+  auto sweep = [&](auto&& f) {
+    if (kHold) {
+#pragma unroll
+      for (int i = 0; i < kHold; ++i)
+        if (w0 + 32 * i < w1) f(w0 + 32 * i + lane, held[i]);
+    } else {
+      for (int j0 = w0; j0 < w1; j0 += 32) {
+        const int j = j0 + lane;
+        f(j, j < w1 ? (forced(pos[j]) ? 0xffffffffu : weight_key(wt[j])) : 0u);
+      }
+    }
   };
 
-  // ---- threshold: the b-th largest key; `need` slots equal to it are kept
-  uint32_t top = 0;
-  int need = b;
+  // ---- the last key kept, and the last slot that is kept with it
+  uint32_t top = b == 0 ? 0xffffffffu : 0u;
+  int need = b;           // slots to keep of those that start with the bits of `top`
+  int last_slot = -1;     // of the slots with key `top`, the last one kept
+  bool count_ties = false;
 #pragma unroll 1
-  for (int pass = 0; pass < 4; ++pass) {
+  for (int pass = 0; pass < 4 && b > 0; ++pass) {
     const int shift = 24 - 8 * pass;
     const uint32_t mask = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
-#pragma unroll 4
-    for (int j = s0 + tid; j < s1; j += kThreads) {
-      uint32_t k;
-      if (kShared && pass == 0) {
-        k = forced(s_pos[j - s0]) ? 0xffffffffu : s_keys[j - s0];
-        s_keys[j - s0] = k;
-      } else {
-        k = key_at(j);
+    int* hist = s_hist[kCluster ? pass : 0];
+    sweep([&](int j, uint32_t k) {
+      const int bin = j < w1 && (k & mask) == top ? static_cast<int>((k >> shift) & 255u) : -1;
+      if (pass == 0) {
+        // signs and exponents: few bins, so a warp adds each once
+        const unsigned same = __match_any_sync(0xffffffffu, bin);
+        if (bin >= 0 && lane == __ffs(same) - 1) atomicAdd(&hist[bin], __popc(same));
+      } else if (bin >= 0) {
+        atomicAdd(&hist[bin], 1);
       }
-      if ((k & mask) == top) atomicAdd(&s_hist[pass][(k >> shift) & 255u], 1);
-    }
+    });
     unit_sync<kCluster>();
-    // threads 0.. take the bins from the largest down
-    int count = 0, incl = 0;
-    if (tid < kBins) {
-      const int bin = kBins - 1 - tid;
+    if (warp == 0) {  // lane l: bins 255 - 8 l and the seven below
+      int4 hi = make_int4(0, 0, 0, 0), lo = hi;
+      int4* mine = reinterpret_cast<int4*>(hist + kBins - 8 - 8 * lane);
       if (kCluster) {
-        for (uint32_t r = 0; r < ranks; ++r) count += remote_word(smem_u32(&s_hist[pass][bin]), r);
+        for (uint32_t r = 0; r < ranks; ++r) {
+          const int4 x = remote_words(smem_u32(mine), r), y = remote_words(smem_u32(mine + 1), r);
+          lo.x += x.x; lo.y += x.y; lo.z += x.z; lo.w += x.w;
+          hi.x += y.x; hi.y += y.y; hi.z += y.z; hi.w += y.w;
+        }
       } else {
-        count = s_hist[pass][bin];
+        lo = mine[0];
+        hi = mine[1];
+        mine[0] = mine[1] = make_int4(0, 0, 0, 0);  // for the next pass
       }
-      incl = count;
+      const int count[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += count[i];
+      int incl = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += y;
       }
-      if (lane == 31) s_sums[warp] = incl;
-    }
-    __syncthreads();
-    if (tid < kBins) {
-      for (int w = 0; w < warp; ++w) incl += s_sums[w];
-      // need = 0 takes the first bin
-      if ((incl - count < need && need <= incl) || (need == 0 && tid == 0)) {
-        s_pick[0] = kBins - 1 - tid;
-        s_pick[1] = need - (incl - count);
-        s_pick[2] = count;
+      int before = incl - sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (before < need && need <= before + count[i]) {
+          s_pick[0] = kBins - 1 - (8 * lane + i);
+          s_pick[1] = need - before;
+          s_pick[2] = count[i];
+        }
+        before += count[i];
       }
     }
     __syncthreads();
+    const int count = s_pick[2];
     top |= static_cast<uint32_t>(s_pick[0]) << shift;
     need = s_pick[1];
-    if (need == s_pick[2] && top != 0) {  // the whole bin is kept
+    if (need == count && top != 0) {  // the whole bin is kept
       top -= 1;
-      need = 0;
+      last_slot = -1;
       break;
     }
+    if (count <= kRanked) {
+      // rank the candidates by (key, slot); a cluster's lists are read by all
+      const uint32_t prefix = 0xffffffffu << shift;
+      sweep([&](int j, uint32_t k) {
+        if (j < w1 && (k & prefix) == top) {
+          const int i = atomicAdd(&s_ranked, 1);
+          s_key[i] = k;
+          s_slot[i] = j;
+        }
+      });
+      unit_sync<kCluster>();
+      if (kCluster) {  // every candidate of the unit
+        int x = tid, r = 0;
+        for (; r < static_cast<int>(ranks); ++r) {
+          const int m = remote_word(smem_u32(&s_ranked), r);
+          if (x < m) break;
+          x -= m;
+        }
+        if (tid < count) {
+          s_all_key[tid] = static_cast<uint32_t>(remote_word(smem_u32(&s_key[x]), r));
+          s_all_slot[tid] = remote_word(smem_u32(&s_slot[x]), r);
+        }
+        __syncthreads();
+      }
+      if (tid < count) {
+        const uint32_t* keys = kCluster ? s_all_key : s_key;
+        const int* slots = kCluster ? s_all_slot : s_slot;
+        const uint32_t key = keys[tid];
+        const int slot = slots[tid];
+        int larger = 0;
+#pragma unroll 8
+        for (int c = 0; c < count; ++c) {
+          const uint32_t k = keys[c];
+          larger += k > key || (k == key && slots[c] < slot);
+        }
+        if (larger == need - 1) {
+          s_last[0] = key;
+          s_last[1] = static_cast<uint32_t>(slot);
+        }
+      }
+      __syncthreads();
+      top = s_last[0];
+      last_slot = static_cast<int>(s_last[1]);
+      break;
+    }
+    count_ties = pass == 3;  // (equal keys, more than are ranked)
     __syncthreads();
   }
 
-  // ---- ranks in slot order: warps take neighbouring runs of slots
-  const int run = ((s1 - s0 + kWarps - 1) / kWarps + 31) & ~31;
-  const int w0 = min(s0 + warp * run, s1), w1 = min(w0 + run, s1);
   // counts of the warps before this one, in this CTA and the ones before it
   auto before = [&](const int (&counts)[kWarps]) {
     int sum = lane < warp ? counts[lane] : 0;
@@ -173,52 +297,51 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
       for (uint32_t r = 0; r + 1 <= rank; ++r) sum += remote_word(smem_u32(&counts[lane]), r);
     return static_cast<int>(__reduce_add_sync(0xffffffffu, sum));
   };
-  int ties = 0;
-  if (need > 0) {
-    for (int j = w0; j < w1; j += 32)
-      ties += __popc(__ballot_sync(0xffffffffu, j + lane < w1 && key_at(j + lane) == top));
+  if (count_ties) {
+    int ties = 0;
+    sweep([&](int j, uint32_t k) { ties += __popc(__ballot_sync(0xffffffffu, j < w1 && k == top)); });
     if (lane == 0) s_ties[warp] = ties;
     unit_sync<kCluster>();
     ties = before(s_ties);
+    // the last tie that is kept is in one warp's run: all before it are kept
+    last_slot = 0x7fffffff;
+    if (ties >= need) last_slot = -1;
+    else
+      sweep([&](int j, uint32_t k) {
+        const unsigned t = __ballot_sync(0xffffffffu, j < w1 && k == top);
+        if (ties < need && ties + __popc(t) >= need)
+          last_slot = (j & ~31) + static_cast<int>(__fns(t, 0, need - ties));
+        ties += __popc(t);
+      });
   }
-  const int first_tie = ties;
-  auto kept = [&](int j) {  // of the 32 slots from j, ties counted on
-    const uint32_t k = j + lane < w1 ? key_at(j + lane) : 0u;
-    bool keep = j + lane < w1 && k > top;
-    if (need > 0) {
-      const unsigned t = __ballot_sync(0xffffffffu, j + lane < w1 && k == top);
-      if (j + lane < w1 && k == top) keep = ties + __popc(t & ((1u << lane) - 1u)) < need;
-      ties += __popc(t);
-    }
-    return keep;
-  };
+  auto kept = [&](int j, uint32_t k) { return j < w1 && (k > top || (k == top && j <= last_slot)); };
+
+  // ---- holes and rows in slot order
   int holes = 0, rows = 0;
-  for (int j = w0; j < w1; j += 32) {
-    const bool keep = kept(j);
-    holes += __popc(__ballot_sync(0xffffffffu, j + lane < w1 && j + lane < b && !keep));
-    rows += __popc(__ballot_sync(0xffffffffu, j + lane >= b && keep));
-  }
+  sweep([&](int j, uint32_t k) {
+    const bool keep = kept(j, k);
+    holes += __popc(__ballot_sync(0xffffffffu, j < w1 && j < b && !keep));
+    rows += __popc(__ballot_sync(0xffffffffu, j >= b && keep));
+  });
   if (lane == 0) {
     s_holes[warp] = holes;
     s_rows[warp] = rows;
   }
-  unit_sync<kCluster>();  // (and the positions in shared memory are done with)
+  unit_sync<kCluster>();
   holes = before(s_holes);
   rows = before(s_rows);
-  ties = first_tie;
-  const bool local = kShared && !kCluster;  // the lists have room in place of the positions
-  int32_t* to = local ? s_pos : p.lists + base;
-  int32_t* from = to + (local ? slice : p.c.capacity) / 2;
-  for (int j = w0; j < w1; j += 32) {
-    const bool keep = kept(j);
+  int32_t* to = kCluster || !kHold ? p.lists + base : s_lists;
+  int32_t* from = to + (kCluster || !kHold ? p.c.capacity / 2 : kThreads * kHold / 2);
+  sweep([&](int j, uint32_t k) {
+    const bool keep = kept(j, k);
     const unsigned below = (1u << lane) - 1u;
-    const bool hole = j + lane < w1 && j + lane < b && !keep, row = j + lane >= b && keep;
+    const bool hole = j < w1 && j < b && !keep, row = j >= b && keep;
     const unsigned hb = __ballot_sync(0xffffffffu, hole), rb = __ballot_sync(0xffffffffu, row);
-    if (hole) to[holes + __popc(hb & below)] = j + lane;
-    if (row) from[rows + __popc(rb & below)] = j + lane;
+    if (hole) to[holes + __popc(hb & below)] = j;
+    if (row) from[rows + __popc(rb & below)] = j;
     holes += __popc(hb);
     rows += __popc(rb);
-  }
+  });
   // every hole of the unit: what its last warp has counted
   if (warp == kWarps - 1 && lane == 0) s_pick[0] = holes;
   unit_sync<kCluster>();
@@ -234,58 +357,66 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const __grid_constant__
   uint32_t* word = reinterpret_cast<uint32_t*>(p.c.positions) + base;
   if (l == 11) word = reinterpret_cast<uint32_t*>(p.c.weights) + base;
   const int step = static_cast<int>(ranks) * kWarps * 2;
-#pragma unroll 2
-  for (int i = (static_cast<int>(rank) * kWarps + warp) * 2 + (lane >> 4); i < moves; i += step) {
-    const long long dst = to[i], src = from[i];
-    if (l < 10) *reinterpret_cast<uint4*>(a + dst * bytes) = *reinterpret_cast<const uint4*>(a + src * bytes);
-    else if (l < 12) word[dst] = word[src];
+  for (int i0 = (static_cast<int>(rank) * kWarps + warp) * 2 + (lane >> 4); i0 < moves; i0 += 4 * step) {
+    uint4 v[4];
+    uint32_t x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + k * step < moves) {
+        const long long src = from[i0 + k * step];
+        if (l < 10) v[k] = *reinterpret_cast<const uint4*>(a + src * bytes);
+        else if (l < 12) x[k] = word[src];
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + k * step < moves) {
+        const long long dst = to[i0 + k * step];
+        if (l < 10) *reinterpret_cast<uint4*>(a + dst * bytes) = v[k];
+        else if (l < 12) word[dst] = x[k];
+      }
   }
   if (rank == 0 && tid == 0) p.c.lengths[unit] = b;
   if (kCluster) unit_sync<true>();  // no CTA leaves while another reads its words
 }
 
-template <int kThreads, bool kCluster, bool kShared>
-cudaError_t launch(const Q4EvictParams& p, size_t smem, cudaStream_t stream) {
+template <int kThreads, int kHold, bool kCluster>
+cudaError_t launch(const Q4EvictParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.c.batch * p.c.num_kv_heads) * p.cluster);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kCluster ? 0 : kThreads * kHold * sizeof(int32_t);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {static_cast<unsigned>(p.cluster), 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = kCluster ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<kThreads, kCluster, kShared>, p);
+  return cudaLaunchKernelEx(&cfg, evict_kernel<kThreads, kHold, kCluster>, p);
 }
-
-constexpr size_t kSharedMost = 200 * 1024;  // 25600 slots a CTA
 
 }  // namespace
 
 cudaError_t q4_evict_set_smem_limit() {
-  cudaError_t e = cudaSuccess;
-  auto set = [&](auto* f) {
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost);
-  };
-  set(evict_kernel<256, false, true>);
-  set(evict_kernel<1024, false, true>);
-  set(evict_kernel<1024, true, true>);
-  return e;
+  return cudaFuncSetAttribute(evict_kernel<1024, kItems, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              1024 * kItems * static_cast<int>(sizeof(int32_t)));
 }
 
 cudaError_t launch_q4_evict(const Q4EvictParams& params, int sms, cudaStream_t stream) {
   Q4EvictParams p = params;
   const long long units = static_cast<long long>(p.c.batch) * p.c.num_kv_heads;
-  // long units share the SMs that there are no other units for
+  const int cap = p.c.capacity;
+  // long units share the SMs that there are no other units for, and those that
+  // no CTA holds
   p.cluster = 1;
-  while (p.cluster < 8 && units * p.cluster * 2 <= sms && p.c.capacity / p.cluster >= 4096) p.cluster *= 2;
-  const int slice = ((p.c.capacity + p.cluster - 1) / p.cluster + 31) & ~31;
-  const size_t smem = static_cast<size_t>(slice) * 8;
-  if (smem > kSharedMost)
-    return p.cluster > 1 ? launch<1024, true, false>(p, 0, stream) : launch<1024, false, false>(p, 0, stream);
-  if (p.cluster > 1) return launch<1024, true, true>(p, smem, stream);
-  return slice <= 4096 ? launch<256, false, true>(p, smem, stream) : launch<1024, false, true>(p, smem, stream);
+  while (p.cluster < 8 && (cap > 1024 * kItems * p.cluster ||
+                           (units * p.cluster * 2 <= sms && cap >= 4096 * p.cluster)))
+    p.cluster *= 2;
+  if (cap > 1024 * kItems * p.cluster) return launch<1024, 0, true>(p, stream);
+  if (p.cluster > 1)
+    return cap <= 8192 * p.cluster ? launch<1024, 8, true>(p, stream) : launch<1024, kItems, true>(p, stream);
+  if (cap <= 256 * kShortItems) return launch<256, kShortItems, false>(p, stream);
+  if (cap <= 256 * kItems) return launch<256, kItems, false>(p, stream);
+  return launch<1024, kItems, false>(p, stream);
 }
 
 }  // namespace ckv

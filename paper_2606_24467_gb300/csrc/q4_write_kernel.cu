@@ -61,12 +61,31 @@ __device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
   return r;
 }
 
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 both2(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
 constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer
 
 // Quantises this half-warp's row (8 channels a lane) into the cache row `dst`
 // and, where asked for, writes the values it stands for.
 template <bool kBf16>
-__device__ __forceinline__ void quantise(const Q4Cache& c, int part, long long dst, uint4 raw,
+__device__ __forceinline__ void quantise(const Q4Cache& c, int part, int dst, uint4 raw,
                                          uint16_t* values) {
   const int l = threadIdx.x & 15;
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -91,54 +110,69 @@ __device__ __forceinline__ void quantise(const Q4Cache& c, int part, long long d
     if (15.0f * s < spread) s = __uint_as_float(__float_as_uint(s) + 0x10000u);
   const bool bad = !(spread <= 3.4028235e38f);  // NaN, infinite
   if (bad) s = m = __uint_as_float(0x7fc00000u);
-  // the smallest scales are lifted by 2^64 (exact), so that 1 / s is finite
-  const float lift = s < 8.67e-19f ? 18446744073709551616.0f : 1.0f;
-  const float sl = s * lift, half = 0.5f * sl;
+  const float half = 0.5f * s;
   float inv;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sl));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   inv *= 1.0f - 0x1p-22f;  // (rcp is within 2^-23: now below 1 / s)
-  float t[8], r[8], most = 0.f;
+  float2 t[4], r[4], val[4];
+  float most = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 x = word_floats<kBf16>(w[i >> 1]);
-    const float d = ((i & 1 ? x.y : x.x) - m) * lift;
-    t[i] = fmaf(d, inv, kMagic);
-    r[i] = fmaf(kMagic - t[i], sl, d);
-    most = fmaxf(most, r[i]);
+  for (int i = 0; i < 4; ++i) {
+    const float2 d = add2(word_floats<kBf16>(w[i]), both2(-m));
+    t[i] = fma2(d, both2(inv), both2(kMagic));
+    const float2 minus_n = fma2(t[i], both2(-1.0f), both2(kMagic));
+    r[i] = fma2(minus_n, both2(s), d);
+    val[i] = fma2(minus_n, both2(-s), both2(m));
+    most = fmaxf(most, fmaxf(r[i].x, r[i].y));
+  }
+  if (s < 8.67e-19f && s > 0.f) {  // 1 / s may not be finite: all times 2^64 (exact)
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s * 0x1p64f));
+    inv *= 1.0f - 0x1p-22f;
+    most = half;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 d = add2(word_floats<kBf16>(w[i]), both2(-m));
+      t[i] = make_float2(fmaf(d.x * 0x1p64f, inv, kMagic), fmaf(d.y * 0x1p64f, inv, kMagic));
+      r[i] = make_float2(fmaf(kMagic - t[i].x, s, d.x), fmaf(kMagic - t[i].y, s, d.y));
+    }
   }
   if (most >= half) {
-    const float above = __uint_as_float(__float_as_uint(half) + 1u);
+    // above a tie, or a tie of an odd code (numbers >= 0 compare like their bits)
+    auto put = [&](float& t, float r) {
+      const int n = __float_as_int(t);
+      if (__float_as_int(r) + (n & 1) > __float_as_int(half)) t = __int_as_float(n + 1);
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t n = __float_as_uint(t[i]);
-      if (r[i] >= (n & 1u ? half : above)) t[i] = __uint_as_float(n + 1u);
+    for (int i = 0; i < 4; ++i) {
+      put(t[i].x, r[i].x);
+      put(t[i].y, r[i].y);
+      val[i] = fma2(add2(t[i], both2(-kMagic)), both2(s), both2(m));
     }
   }
   uint32_t code = 0;
-  float val[8];
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    code = (code << 4) + __float_as_uint(t[i]);
-    val[i] = fmaf(t[i] - kMagic, s, m);
+  for (int i = 3; i >= 0; --i) {
+    code = (code << 4) + __float_as_uint(t[i].y);
+    code = (code << 4) + __float_as_uint(t[i].x);
   }
   code -= 0x4b400000u * 0x11111111u;  // each t has the bits of kMagic above its code
   if (!(s > 0.f)) {  // one value, or NaN
     code = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) val[i] = m;
+    for (int i = 0; i < 4; ++i) val[i] = both2(m);
   }
-  reinterpret_cast<uint32_t*>(c.codes[part] + dst * kQ4CodeBytes)[l] = code;
+  reinterpret_cast<uint32_t*>(c.codes[part] + static_cast<size_t>(dst) * kQ4CodeBytes)[l] = code;
   if ((l & 3) == 0) {
-    uint16_t* pr = reinterpret_cast<uint16_t*>(c.params[part] + dst * kQ4ParamBytes);
+    uint16_t* pr = reinterpret_cast<uint16_t*>(c.params[part] + static_cast<size_t>(dst) * kQ4ParamBytes);
     pr[l >> 2] = static_cast<uint16_t>(__float_as_uint(s) >> 16);
     pr[kQ4Groups + (l >> 2)] = static_cast<uint16_t>(__float_as_uint(m) >> 16);
   }
   if (values) {
     uint4 o;
-    o.x = pack_pair<kBf16>(val[0], val[1]);
-    o.y = pack_pair<kBf16>(val[2], val[3]);
-    o.z = pack_pair<kBf16>(val[4], val[5]);
-    o.w = pack_pair<kBf16>(val[6], val[7]);
+    o.x = pack_pair<kBf16>(val[0].x, val[0].y);
+    o.y = pack_pair<kBf16>(val[1].x, val[1].y);
+    o.z = pack_pair<kBf16>(val[2].x, val[2].y);
+    o.w = pack_pair<kBf16>(val[3].x, val[3].y);
     reinterpret_cast<uint4*>(values)[l] = o;
   }
 }
@@ -151,15 +185,15 @@ __device__ __forceinline__ int2 rows_of(const Q4AppendParams& p, int s) {
 
 // This lane's 16 bytes of a source row, and the row into the cache.
 template <int kTable>
-__device__ __forceinline__ uint4 load_row(const Q4WriteParams<kTable>& p, long long row, int g) {
-  const uint16_t* src = p.src[(threadIdx.x >> 4) & 1] + row * p.tok_stride + static_cast<long long>(g) * p.head_stride;
+__device__ __forceinline__ uint4 load_row(const Q4WriteParams<kTable>& p, int row, int g) {
+  const uint16_t* src = p.src[(threadIdx.x >> 4) & 1] + row * p.tok_stride + g * p.head_stride;
   return __ldg(reinterpret_cast<const uint4*>(src) + (threadIdx.x & 15));
 }
 template <bool kBf16, int kTable>
-__device__ __forceinline__ void store_row(const Q4WriteParams<kTable>& p, uint4 raw, long long dst,
-                                          long long value_row, int position, float weight) {
+__device__ __forceinline__ void store_row(const Q4WriteParams<kTable>& p, uint4 raw, int dst, int value_row,
+                                          int position, float weight) {
   const int lane = threadIdx.x & 31, part = lane >> 4;
-  quantise<kBf16>(p.c, part, dst, raw, p.values[part] ? p.values[part] + value_row * kHeadDim : nullptr);
+  quantise<kBf16>(p.c, part, dst, raw, p.values[part] ? p.values[part] + static_cast<size_t>(value_row) * kHeadDim : nullptr);
   if (lane == 0) p.c.positions[dst] = position;
   if (lane == 16 && p.c.weights) p.c.weights[dst] = weight;
 }
@@ -200,62 +234,85 @@ __global__ void __launch_bounds__(kWriteThreads) append_unit_kernel(const __grid
       break;
     }
   }
-  const long long base = static_cast<long long>(unit) * p.c.capacity;
+  const int base = unit * p.c.capacity;
   if (at >= 0)
     for (int i = warp; i < used && i < p.c.capacity - at; i += warps) {
       if (i != warp) raw = load_row(p, r.x + i, g);
-      store_row<kBf16>(p, raw, base + at + i, static_cast<long long>(r.x + i) * p.c.num_kv_heads + g,
+      store_row<kBf16>(p, raw, base + at + i, (r.x + i) * p.c.num_kv_heads + g,
                        p.positions[r.x + i], 0.f);
     }
   __syncthreads();
   if (threadIdx.x == 0) set_length(p, unit, at, used);
 }
 
-// Many rows: a warp takes kRows neighbouring (row, group) pairs, all their
-// loads first; the lengths follow in a launch of their own.
-template <bool kBf16, int kRows>
-__global__ void __launch_bounds__(kWriteThreads) append_rows_kernel(const __grid_constant__ Q4AppendParams p) {
+// Where a lane's row and group come from and go to.
+struct Move {
+  int row = 0, head = 0;  // of K, V
+  int dst = -1;           // slot row of the cache; -1: nothing to do
+  int position = 0;
+  float weight = 0.f;
+};
+
+// The warp's tasks task0 .. task0 + count - 1 (count <= kTasks), whose moves
+// its first lanes hold: four rows in flight at a time.
+template <bool kBf16, int kTasks, int kTable>
+__device__ __forceinline__ void move_rows(const Q4WriteParams<kTable>& p, const Move& mine, int task0) {
+  constexpr int kBatch = kTasks < 4 ? kTasks : 4;
+  const int lane = threadIdx.x & 31, part = lane >> 4;
+  if (lane < kTasks && mine.dst >= 0) {
+    p.c.positions[mine.dst] = mine.position;
+    if (p.c.weights) p.c.weights[mine.dst] = mine.weight;
+  }
+#pragma unroll 1
+  for (int t = 0; t < kTasks; t += kBatch) {
+    uint4 raw[kBatch];
+    int dst[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      dst[k] = __shfl_sync(0xffffffffu, mine.dst, t + k);
+      const int row = __shfl_sync(0xffffffffu, mine.row, t + k);
+      const int head = __shfl_sync(0xffffffffu, mine.head, t + k);
+      if (dst[k] >= 0) raw[k] = load_row(p, row, head);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (dst[k] >= 0)
+        quantise<kBf16>(p.c, part, dst[k], raw[k],
+                        p.values[part] ? p.values[part] + static_cast<size_t>(task0 + t + k) * kHeadDim : nullptr);
+  }
+}
+
+// Many rows: a warp takes kTasks neighbouring (row, group) pairs; the lengths
+// follow in a launch of their own.
+template <bool kBf16, int kTasks>
+__global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __grid_constant__ Q4AppendParams p) {
   pdl_launch_dependents();
   const int H = p.c.num_kv_heads;
-  const long long tasks = static_cast<long long>(p.rows) * H;
-  const long long task0 = (static_cast<long long>(blockIdx.x) * (kWriteThreads / 32) + (threadIdx.x >> 5)) * kRows;
+  // (the host bounds the tasks by 2^31 - 1, and the slots)
+  const unsigned tasks = static_cast<unsigned>(p.rows) * H;
+  const unsigned task0 = (blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5)) * kTasks;
   if (task0 >= tasks) return;
-  int row = static_cast<int>(task0 / H), g = static_cast<int>(task0 - static_cast<long long>(row) * H);
-  int s;
-  if (p.rows_per_seq >= 0) {
-    s = row / p.rows_per_seq;
-  } else {
-    int lo = 0, hi = p.c.batch;  // cu_rows[s] <= row < cu_rows[s + 1]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.cu_rows[mid] <= row) lo = mid; else hi = mid;
-    }
-    s = lo;
-  }
-  int2 r = rows_of(p, s);
-  uint4 raw[kRows];
-  long long dst[kRows];
-  int at[kRows], position[kRows];
-#pragma unroll
-  for (int k = 0; k < kRows; ++k) {
-    dst[k] = -1;
-    if (task0 + k < tasks) {
-      raw[k] = load_row(p, row, g);
-      at[k] = first_slot(p, s * H + g);
-      position[k] = p.positions[row];
-      const int i = row - r.x;
-      if (at[k] >= 0 && i < p.c.capacity - at[k] && position[k] >= 0)
-        dst[k] = static_cast<long long>(s * H + g) * p.c.capacity + at[k] + i;
-      if (++g == H) {
-        g = 0;
-        ++row;
-        while (row >= r.x + r.y && s + 1 < p.c.batch) r = rows_of(p, ++s);
+  const unsigned task = task0 + (threadIdx.x & 31);
+  Move m;
+  if ((threadIdx.x & 31) < kTasks && task < tasks) {
+    m.row = static_cast<int>(task / H);
+    m.head = static_cast<int>(task) - m.row * H;
+    int s;
+    if (p.rows_per_seq >= 0) {
+      s = m.row / p.rows_per_seq;
+    } else {
+      int lo = 0, hi = p.c.batch;  // cu_rows[s] <= row < cu_rows[s + 1]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.cu_rows[mid] <= m.row) lo = mid; else hi = mid;
       }
+      s = lo;
     }
+    const int at = first_slot(p, s * H + m.head), i = m.row - rows_of(p, s).x;
+    m.position = p.positions[m.row];
+    if (at >= 0 && i < p.c.capacity - at && m.position >= 0) m.dst = (s * H + m.head) * p.c.capacity + at + i;
   }
-#pragma unroll
-  for (int k = 0; k < kRows; ++k)
-    if (dst[k] >= 0) store_row<kBf16>(p, raw[k], dst[k], task0 + k, position[k], 0.f);
+  move_rows<kBf16, kTasks>(p, m, static_cast<int>(task0));
 }
 
 // A CTA a sequence: the first of its rows with a negative position.
@@ -276,103 +333,64 @@ __global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __g
     set_length(p, s * H + g, first_slot(p, s * H + g), s_used);
 }
 
-// A warp takes kRows neighbouring retained rows and groups; further warps
+// A warp takes kTasks neighbouring retained rows and groups; further warps
 // write the units' lengths.
-template <bool kBf16, int kRows, class P>
-__global__ void __launch_bounds__(kWriteThreads) gather_q4_kernel(const __grid_constant__ P p) {
+template <bool kBf16, int kTasks, class P>
+__global__ void __launch_bounds__(kWriteThreads, 4) gather_q4_kernel(const __grid_constant__ P p) {
   const int H = p.c.num_kv_heads, B = p.c.batch, lane = threadIdx.x & 31;
-  const long long tasks = p.group_major ? p.rows : static_cast<long long>(p.rows) * H;
-  const long long warps = (tasks + kRows - 1) / kRows;
-  const long long warp = static_cast<long long>(blockIdx.x) * (kWriteThreads / 32) + (threadIdx.x >> 5);
+  const unsigned tasks = p.group_major ? p.rows : static_cast<unsigned>(p.rows) * H;
+  const unsigned warps = (tasks + kTasks - 1) / kTasks;
+  const unsigned warp = blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5);
   if (warp >= warps) {
-    const long long unit = (warp - warps) * 32 + lane;
-    if (unit < static_cast<long long>(B) * H) {
-      const int s = static_cast<int>(unit / H), g = static_cast<int>(unit - static_cast<long long>(s) * H);
+    const int unit = static_cast<int>(warp - warps) * 32 + lane;
+    if (unit < B * H) {
+      const int s = unit / H, g = unit - s * H;
       const int* cu = p.cu_rows + (p.group_major ? g * (B + 1) : 0);
       p.c.lengths[unit] = cu[s + 1] - cu[s];
     }
     return;
   }
-  const long long task0 = warp * kRows;
-  int row, g;
-  if (p.group_major) {
-    row = static_cast<int>(task0);
-    g = 0;
-    while (g + 1 < H && p.cu_rows[(g + 1) * (B + 1)] <= row) ++g;
-  } else {
-    row = static_cast<int>(task0 / H);
-    g = static_cast<int>(task0 - static_cast<long long>(row) * H);
-  }
-  const int* cu = p.cu_rows + (p.group_major ? g * (B + 1) : 0);
-  int lo = 0, hi = B;  // cu[s] <= row < cu[s + 1]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= row) lo = mid; else hi = mid;
-  }
-  int s = lo;
-  int idx[kRows];
-  long long at[kRows];  // of the row in K, V; -1: an index outside
-  long long dst[kRows];
-  int head[kRows], seq[kRows];
-#pragma unroll
-  for (int k = 0; k < kRows; ++k) {
-    at[k] = -1;
-    if (task0 + k < tasks) {
-      idx[k] = p.indices[p.group_major ? row : static_cast<long long>(g) * p.rows + row];
-      dst[k] = static_cast<long long>(s * H + g) * p.c.capacity + (row - cu[s]);
-      head[k] = g;
-      seq[k] = s;
-      at[k] = p.cu_seqlens[s];
-      // the next pair
-      if (p.group_major || ++g == H) {
-        ++row;
-        if (!p.group_major) g = 0;
-        while (row >= cu[s + 1]) {
-          if (s + 1 < B) {
-            ++s;
-          } else if (p.group_major && g + 1 < H) {
-            ++g;
-            cu += B + 1;
-            s = 0;
-          } else {
-            break;
-          }
-        }
-      }
+  const unsigned task = warp * kTasks + lane;
+  Move m;
+  if (lane < kTasks && task < tasks) {
+    int row = static_cast<int>(task);
+    if (p.group_major) {
+      while (m.head + 1 < H && p.cu_rows[(m.head + 1) * (B + 1)] <= row) ++m.head;
+    } else {
+      row = static_cast<int>(task / H);
+      m.head = static_cast<int>(task) - row * H;
+    }
+    const int* cu = p.cu_rows + (p.group_major ? m.head * (B + 1) : 0);
+    int s = 0, hi = B;  // cu[s] <= row < cu[s + 1]
+    while (hi - s > 1) {
+      const int mid = (s + hi) >> 1;
+      if (cu[mid] <= row) s = mid; else hi = mid;
+    }
+    const int idx = p.indices[p.group_major ? row : static_cast<long long>(m.head) * p.rows + row];
+    const int first = p.cu_seqlens[s], L = p.cu_seqlens[s + 1] - first;
+    if (idx < 0 || idx >= L) {
+      if (p.status) atomicCAS(p.status, 0, CKV_DEV_ERR_INDEX);
+    } else {
+      m.row = first + idx;
+      m.dst = (s * H + m.head) * p.c.capacity + (row - cu[s]);
+      m.position = idx;
+      if (p.raw && idx < L - p.window)
+        m.weight = p.raw[static_cast<long long>(m.head) * p.p_total + p.cu_prefix[s] + idx];
     }
   }
-  uint4 raw[kRows];
-#pragma unroll
-  for (int k = 0; k < kRows; ++k)
-    if (at[k] >= 0) {
-      const int L = p.cu_seqlens[seq[k] + 1] - p.cu_seqlens[seq[k]];
-      if (idx[k] < 0 || idx[k] >= L) {
-        if (lane == 0 && p.status) atomicCAS(p.status, 0, CKV_DEV_ERR_INDEX);
-        at[k] = -1;
-      } else {
-        raw[k] = load_row(p, at[k] + idx[k], head[k]);
-      }
-    }
-#pragma unroll
-  for (int k = 0; k < kRows; ++k)
-    if (at[k] >= 0) {
-      const int L = p.cu_seqlens[seq[k] + 1] - p.cu_seqlens[seq[k]];
-      float weight = 0.f;
-      if (p.raw && idx[k] < L - p.window)
-        weight = p.raw[static_cast<long long>(head[k]) * p.p_total + p.cu_prefix[seq[k]] + idx[k]];
-      store_row<kBf16>(p, raw[k], dst[k], task0 + k, idx[k], weight);
-    }
+  move_rows<kBf16, kTasks>(p, m, static_cast<int>(warp * kTasks));
 }
 
-// Rows a warp takes: four once every SM has more warps than it holds at once.
+// Tasks a warp takes: many once every SM has more warps than it holds.
 constexpr long long kManyTasks = 152 * 64;
+constexpr int kMostTasks = 4;
 
-template <bool kBf16, int kRows, class P>
+template <bool kBf16, int kTasks, class P>
 cudaError_t launch_gather_rows(const P& p, long long tasks, cudaStream_t stream) {
   const long long units = static_cast<long long>(p.c.batch) * p.c.num_kv_heads;
-  const long long warps = (tasks + kRows - 1) / kRows + (units + 31) / 32;
+  const long long warps = (tasks + kTasks - 1) / kTasks + (units + 31) / 32;
   constexpr int kPer = kWriteThreads / 32;
-  gather_q4_kernel<kBf16, kRows, P><<<static_cast<unsigned>((warps + kPer - 1) / kPer), kWriteThreads, 0, stream>>>(p);
+  gather_q4_kernel<kBf16, kTasks, P><<<static_cast<unsigned>((warps + kPer - 1) / kPer), kWriteThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 template <class P>
@@ -380,13 +398,14 @@ cudaError_t launch_gather_any(const P& p, cudaStream_t stream) {
   const long long tasks = p.group_major ? p.rows : static_cast<long long>(p.rows) * p.c.num_kv_heads;
   if (tasks <= kManyTasks)
     return p.is_bf16 ? launch_gather_rows<true, 1>(p, tasks, stream) : launch_gather_rows<false, 1>(p, tasks, stream);
-  return p.is_bf16 ? launch_gather_rows<true, 4>(p, tasks, stream) : launch_gather_rows<false, 4>(p, tasks, stream);
+  return p.is_bf16 ? launch_gather_rows<true, kMostTasks>(p, tasks, stream)
+                   : launch_gather_rows<false, kMostTasks>(p, tasks, stream);
 }
 
-template <bool kBf16, int kRows>
+template <bool kBf16, int kTasks>
 cudaError_t launch_append_rows(const Q4AppendParams& p, long long tasks, cudaStream_t stream) {
-  constexpr long long kPer = static_cast<long long>(kWriteThreads / 32) * kRows;
-  append_rows_kernel<kBf16, kRows>
+  constexpr long long kPer = static_cast<long long>(kWriteThreads / 32) * kTasks;
+  append_rows_kernel<kBf16, kTasks>
       <<<static_cast<unsigned>((tasks + kPer - 1) / kPer), kWriteThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
@@ -407,7 +426,7 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t
   if (tasks <= kManyTasks)
     e = p.is_bf16 ? launch_append_rows<true, 1>(p, tasks, stream) : launch_append_rows<false, 1>(p, tasks, stream);
   else
-    e = p.is_bf16 ? launch_append_rows<true, 4>(p, tasks, stream) : launch_append_rows<false, 4>(p, tasks, stream);
+    e = p.is_bf16 ? launch_append_rows<true, kMostTasks>(p, tasks, stream) : launch_append_rows<false, kMostTasks>(p, tasks, stream);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.c.batch);

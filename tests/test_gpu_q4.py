@@ -573,22 +573,25 @@ def test_evict(cuda_device, n, budget, sinks, recent):
     check_evict(w0, host(c), np.full((2, 2), budget), sinks, recent)
 
 
+@pytest.mark.parametrize("n", [2000, 5000])
 @pytest.mark.parametrize("kind", ["ties", "equal", "zeros", "nan", "inf", "negative", "close"])
-def test_evict_weights(cuda_device, kind):
+def test_evict_weights(cuda_device, kind, n):
     gen = torch.Generator().manual_seed(3)
-    c = random_cache(1, 3, 2000, [[2000, 1999, 77]], cuda_device, gen)
-    w = torch.rand((1, 3, 2016), generator=gen)
+    c = random_cache(1, 3, n, [[n, n - 1, 77]], cuda_device, gen)
+    w = torch.rand((1, 3, c.capacity), generator=gen)
     w = {"ties": (w * 4).floor(), "equal": torch.full_like(w, 0.25),
          "zeros": torch.where(w < 0.5, 0.0, -0.0), "nan": torch.where(w < 0.3, float("nan"), w),
          "inf": torch.where(w < 0.1, float("inf"), torch.where(w < 0.2, float("-inf"), w)),
          "negative": w - 0.5, "close": 1 + (w * 8).floor() * 2.0 ** -23}[kind]
     c.weights.copy_(w)
-    c0 = host(c)
-    ckv.q4_evict(c, 60, ckv.q4_workspace(c), sinks=3, recent=20)
-    check_evict(c0, host(c), np.full((1, 3), 60), 3, 20)
+    for budget in (n * 3 // 4, 60):
+        c0 = host(c)
+        ckv.q4_evict(c, budget, ckv.q4_workspace(c), sinks=3, recent=20)
+        check_evict(c0, host(c), np.full((1, 3), budget), 3, 20)
 
 
-@pytest.mark.parametrize("units,n", [(80, 5000), (2, 210001), (80, 26001), (20, 9000), (1, 26000)])
+@pytest.mark.parametrize("units,n", [(80, 5000), (2, 210001), (80, 26001), (20, 9000), (1, 26000),
+                                     (80, 1250), (3, 70000)])
 def test_evict_of_long_units(cuda_device, units, n):
     """Units that a CTA or a cluster of them holds in shared memory, or does not
     (the first and the last unit are compared)."""
@@ -605,9 +608,9 @@ def test_evict_of_long_units(cuda_device, units, n):
     c.lengths[-1] = n - 37
     pick = [0, units - 1]
     c0 = {k: v[pick] for k, v in host(c).items()}
-    budget = n // 3
-    ckv.q4_evict(c, budget, ckv.q4_workspace(c), sinks=5, recent=1000)
-    check_evict(c0, {k: v[pick] for k, v in host(c).items()}, np.full((2, 1), budget), 5, 1000)
+    budget, recent = n // 3, n // 25
+    ckv.q4_evict(c, budget, ckv.q4_workspace(c), sinks=5, recent=recent)
+    check_evict(c0, {k: v[pick] for k, v in host(c).items()}, np.full((2, 1), budget), 5, recent)
 
 
 def test_evict_budgets_per_unit(cuda_device):
