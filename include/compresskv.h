@@ -442,9 +442,9 @@ typedef struct ckv_q4_queries {
  * num_q_heads = num_queries = 0: for the eviction alone.  0 if invalid. */
 size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, int32_t num_queries);
 
-/* Zero the workspace's status word (256 bytes, on `stream`): once after
- * allocating it and after reading a non-zero status
- * (compresskv_read_device_status). */
+/* Zero the workspace's header (1 KB, on `stream`): once after allocating it
+ * and after reading a non-zero status (compresskv_read_device_status); every
+ * call that completes leaves it ready for the next. */
 int compresskv_q4_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
 
 /* Quantise rows of new tokens into the cache, behind what it holds: row i of a

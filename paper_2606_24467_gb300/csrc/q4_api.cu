@@ -23,7 +23,7 @@ size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // The cache's shape (and, with `pointers`, its buffers).
 int check_cache(const ckv_q4_cache* c, bool pointers = true) {
   if (!c || c->batch < 1 || c->num_kv_heads < 1 || c->capacity < 1) return CKV_ERR_INVALID_ARG;
-  if (c->capacity % kQ4TileSlots) return CKV_ERR_INVALID_ARG;
+  if (c->capacity % kQ4SlotStep) return CKV_ERR_INVALID_ARG;
   if (c->head_dim != kHeadDim || c->num_kv_heads > kMaxKvHeads || c->capacity > kMaxCapacity)
     return CKV_ERR_UNSUPPORTED;
   const long long units = static_cast<long long>(c->batch) * c->num_kv_heads;
@@ -64,22 +64,26 @@ int check_values(const void* k, const void* v) {
   return aligned16(k) && aligned16(v) ? CKV_OK : CKV_ERR_INVALID_ARG;
 }
 
-// The attention's area behind the workspace header, for up to kMaxSms SMs.
-constexpr int kMaxSms = 160;
+// The attention's area behind the workspace header (status word at its start,
+// the tickets from kTicketBytes on).
+constexpr size_t kTicketBytes = 256;
+static_assert(kTicketBytes + kQ4MaxCtas * sizeof(int) <= kQ4HeaderBytes, "tickets");
 struct AttendArea {
-  size_t first_tile = 0, part_ml = 0, part_o = 0, lse = 0, z = 0, bytes = 0;
+  size_t head_ml = 0, head_o = 0, cta_ml = 0, cta_o = 0, lse = 0, z = 0, bytes = 0;
 };
 AttendArea attend_area(const ckv_q4_cache* c, int num_q_heads, int num_queries, bool accumulate) {
-  const size_t units = units_of(c), rows = static_cast<size_t>(num_q_heads / c->num_kv_heads) * num_queries;
-  const size_t brows = q4_block_rows(static_cast<int>(rows)), blocks = (rows + brows - 1) / brows;
-  const size_t parts = q4_attend_workers(static_cast<int>(rows), kMaxSms) + units * blocks;
+  const size_t rows = static_cast<size_t>(num_q_heads / c->num_kv_heads) * num_queries;
+  const size_t brows = q4_block_rows(static_cast<int>(rows));
+  const size_t heads = kQ4MaxCtas * static_cast<size_t>(q4_attend_warps(static_cast<int>(rows))) * brows;
+  const size_t ctas = kQ4MaxCtas * 2 * brows;
   AttendArea a;
-  a.first_tile = kQ4HeaderBytes;
-  a.part_ml = a.first_tile + align256((units + 1) * sizeof(long long));
-  a.part_o = a.part_ml + align256(parts * brows * sizeof(float2));
-  a.lse = a.part_o + align256(parts * brows * kHeadDim * sizeof(float));
-  a.z = a.lse + align256(units * rows * sizeof(float));
-  a.bytes = a.z + (accumulate ? align256(units * rows * c->capacity * sizeof(float)) : 0);
+  a.head_ml = kQ4HeaderBytes;
+  a.head_o = a.head_ml + align256(heads * sizeof(float2));
+  a.cta_ml = a.head_o + align256(heads * kHeadDim * sizeof(float));
+  a.cta_o = a.cta_ml + align256(ctas * sizeof(float2));
+  a.lse = a.cta_o + align256(ctas * kHeadDim * sizeof(float));
+  a.z = a.lse + align256(units_of(c) * rows * sizeof(float));
+  a.bytes = a.z + (accumulate ? align256(units_of(c) * rows * c->capacity * sizeof(float)) : 0);
   return a;
 }
 size_t evict_bytes(const ckv_q4_cache* c) {
@@ -157,7 +161,7 @@ size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, 
     if (check_heads(c, num_q_heads, num_queries) != CKV_OK) return 0;
     const bool weights = c->weights != nullptr;
     n = std::max(n, attend_area(c, num_q_heads, num_queries, weights).bytes);
-    // (fewer rows may take smaller row blocks and then more workers)
+    // (fewer rows may take smaller row blocks and then more warps)
     n = std::max(n, attend_area(c, c->num_kv_heads, 1, weights).bytes);
   }
   return n;
@@ -298,17 +302,17 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.rows = P.group * P.num_queries;
   P.blocks = (P.rows + q4_block_rows(P.rows) - 1) / q4_block_rows(P.rows);
   // no more CTAs than there can be tiles
-  const long long tiles = static_cast<long long>(slots / kQ4TileSlots) * P.blocks;
-  sms = static_cast<int>(std::min<long long>({sms, kMaxSms, tiles}));
-  P.workers = q4_attend_workers(P.rows, sms);
-  P.first_tile = reinterpret_cast<long long*>(ws + area.first_tile);
-  P.part_ml = reinterpret_cast<float2*>(ws + area.part_ml);
-  P.part_o = reinterpret_cast<float*>(ws + area.part_o);
+  const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + kQ4TileSlots - 1) / kQ4TileSlots) * P.blocks;
+  sms = static_cast<int>(std::min<long long>({sms, kQ4MaxCtas, tiles}));
+  P.tickets = reinterpret_cast<int*>(ws + kTicketBytes);
+  P.head_ml = reinterpret_cast<float2*>(ws + area.head_ml);
+  P.head_o = reinterpret_cast<float*>(ws + area.head_o);
+  P.cta_ml = reinterpret_cast<float2*>(ws + area.cta_ml);
+  P.cta_o = reinterpret_cast<float*>(ws + area.cta_o);
   P.lse_ws = reinterpret_cast<float*>(ws + area.lse);
   P.z = reinterpret_cast<float*>(ws + area.z);
   Tracer tr{c->trace, st};
   rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_attend(P, sms, st); });
-  if (rc == CKV_OK) rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_combine(P, st); });
   if (rc != CKV_OK || !P.accumulate) return rc;
   return traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_weights(P, st); });
 }

@@ -6,15 +6,16 @@
 //
 // Bound by memory: 160 bytes a slot against at most a few thousand operations,
 // so the kernel is built around a steady stream of slots and few instructions
-// a code.  Warps are independent workers: each takes a run of tiles of 32
-// slots (see Q4AttendParams), keeps two or three in flight with TMA into its
-// own part of shared memory, and leaves the softmax reference, sum and outputs
-// of each row block it touched; a second kernel joins them.
+// a code.  Every warp takes a run of tiles of 64 slots (see Q4AttendParams) and
+// keeps two to four in flight with TMA into its own part of shared memory.  A
+// row block that lies in its run it finishes itself; of others it leaves the
+// softmax reference, sum and outputs, which its CTA joins, and for row blocks
+// that several CTAs share the last of them to come, always in slot order.
 //
 // Codes enter the tensor cores as they are.  A nibble n masked out of a word is
 // the fp16 subnormal n * 2^-24 (one in bits 4-7 is 16 n * 2^-24), exact in a
-// product with fp32 sums, so five instructions make eight operands and neither
-// scale, minimum nor an offset is applied to a code.  mma.sync takes operands
+// product with fp32 sums, so five instructions make eight operands (V: four, see
+// below) and neither scale, minimum nor an offset is applied to a code.  mma.sync takes operands
 // from registers: with 8 or 16 query rows a unit's products are far below the
 // tensor cores' rate, while tcgen05 would want the operands expanded to 16 bits
 // in shared memory, four times the bytes of the codes.
@@ -27,7 +28,10 @@
 //   O^T = V^T P^T: A = codes of 16 channels, B = P^T, which movmatrix makes of
 //     the result layout of S^T.  With p in fp16 (relative error 2^-12) the weights
 //     of group J's codes are p s_J (rounded once more), those of its minimum p; the
-//     minima's term is a product of its own.  Scales and minima are fp16 too,
+//     minima's term is a product of its own.  A byte holds two channels n and n':
+//     the operands are n + 16 n' and 16 n' (both exact), whose sums give the
+//     channels' by one subtraction at the end, an instruction less a word than
+//     n and 16 n'.  Scales and minima are fp16 too,
 //     exact against a power of two that follows the largest of both: 2^-21 of it
 //     and above for scales, 2^-22 for minima.
 // Eight lanes of a warp need the same slot's scales, so one lane a slot converts
@@ -44,6 +48,16 @@ namespace ckv {
 
 namespace {
 
+#ifndef Q4W1
+#define Q4W1 8
+#define Q4S1 2
+#define Q4W2 8
+#define Q4S2 2
+#endif
+#ifndef Q4MIN
+#define Q4MIN 8
+#define Q4SOLO 4
+#endif
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
@@ -52,18 +66,16 @@ constexpr int kMinScaleExp = -110;     // smaller scales and minima share this r
 
 // Shared memory of a worker's stage: codes of K and V (swizzled), then params
 // and positions.
-constexpr int kCodeTile = kQ4TileSlots * kQ4CodeBytes;    // 2048
-constexpr int kParamTile = kQ4TileSlots * kQ4ParamBytes;  // 512
-constexpr int kPosTile = kQ4TileSlots * 4;                // 128
-constexpr int kSideBytes = 2 * kParamTile + kPosTile;     // 1152
-constexpr int kScaleTile = kQ4TileSlots * 16;             // K's scales of the tile at hand, fp32
+constexpr int kTile = kQ4TileSlots;  // 64
+constexpr int kSteps = kTile / 16;
+constexpr int kCodeTile = kTile * kQ4CodeBytes;    // 4096
+constexpr int kParamTile = kTile * kQ4ParamBytes;  // 1024
+constexpr int kPosTile = kTile * 4;                // 256
+constexpr int kSideBytes = 2 * kParamTile + kPosTile;
+constexpr int kMinTiles = Q4MIN;    // least tiles of a CTA that shares row blocks
+constexpr int kSoloTiles = Q4SOLO;  // most tiles a warp of a row block in one CTA
+constexpr int kScaleTile = kTile * 16;             // K's scales of the tile at hand, fp32
 
-#ifndef Q4W1
-#define Q4W1 12
-#define Q4S1 2
-#define Q4W2 8
-#define Q4S2 4
-#endif
 template <int NB>
 struct Shape {
   static constexpr int kWarps = NB == 1 ? Q4W1 : Q4W2;
@@ -170,7 +182,7 @@ __device__ __forceinline__ int length_of(const Q4Cache& c, int unit) {
   return min(max(__ldg(c.lengths + unit), 0), c.capacity);
 }
 __device__ __forceinline__ int tiles_of(const Q4Cache& c, int unit) {
-  return (length_of(c, unit) + kQ4TileSlots - 1) / kQ4TileSlots;
+  return (length_of(c, unit) + kTile - 1) / kTile;
 }
 
 // A tile's place in the sequence of tiles.
@@ -181,8 +193,8 @@ struct Place {
   // The next tile; past the end of a row block the next one that has tiles
   // (the caller knows that there is one).
   __device__ __forceinline__ void next(const Q4AttendParams& p) {
-    row += kQ4TileSlots;
-    valid -= kQ4TileSlots;
+    row += kTile;
+    valid -= kTile;
     if (valid > 0) return;
     if (++block == p.blocks) {
       block = 0;
@@ -222,6 +234,17 @@ __device__ __forceinline__ uint32_t top_of(uint4 w) {
   const uint32_t z = max((w.z << 16) & 0x7fff0000u, w.z & 0x7fff0000u);
   return max(s, max(z, max((w.w << 16) & 0x7fff0000u, w.w & 0x7fff0000u)));
 }
+
+// What a warp leaves of a row block that it shares with others.
+struct Part {
+  int block;        // unit * blocks + row block, or -1
+  int count;        // tiles of the row block
+  long long first;  // its first tile
+  bool starts, ends;
+};
+
+__device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int row, int lane, float4 v,
+                                          float ref, float sum);
 
 // The query rows of a row block as operands: row lane/4 of each 8.
 template <int NB>
@@ -310,9 +333,13 @@ template <int NB, bool kPos>
 __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     attend_kernel(const __grid_constant__ Q4AttendParams p) {
   using S = Shape<NB>;
+  constexpr int kRows = 8 * NB;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ long long s_sums[S::kWarps], s_before[S::kWarps];
-  __shared__ int s_unit[S::kWarps], s_abort;
+  __shared__ long long s_sums[S::kWarps], s_from;
+  __shared__ int s_most[S::kWarps], s_count, s_unit, s_abort;
+  __shared__ long long s_unit_from;
+  __shared__ float2 s_ml[S::kWarps][kRows];
+  __shared__ Part s_tail[S::kWarps], s_head[S::kWarps];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
@@ -320,80 +347,99 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
   const uint32_t scales = base + S::kCodes + S::kSide + warp * kScaleTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
-  if (lane == 0)
+  if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
-  if (threadIdx.x == 0) s_abort = 0;
+    s_tail[warp].block = s_head[warp].block = -1;
+  }
   if (threadIdx.x == 0) {
+    s_abort = 0;
     tma_prefetch_map(&p.map_k);
     tma_prefetch_map(&p.map_v);
   }
   fence_mbar_init();
 
-  // ---- this worker's tiles
+  // ---- this CTA's tiles, and this warp's share of them
   const int units = p.c.batch * p.c.num_kv_heads;
   const int span = (units + S::kThreads - 1) / S::kThreads;  // units a thread adds up
   const int u0 = min(static_cast<int>(threadIdx.x) * span, units), u1 = min(u0 + span, units);
   long long mine = 0, total = 0;
-  for (int u = u0; u < u1; ++u) mine += tiles_of(p.c, u);
-  const long long before = cta_scan<S::kThreads>(mine, s_sums, &total);
-  if (blockIdx.x == 0) {
-    long long at = before;
-    for (int u = u0; u < u1; ++u) {
-      p.first_tile[u] = at;
-      at += tiles_of(p.c, u);
-    }
-    if (threadIdx.x == 0) p.first_tile[units] = total;
+  int most = 0;
+  for (int u = u0; u < u1; ++u) {
+    const int n = tiles_of(p.c, u);
+    mine += n;
+    most = max(most, n);
   }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) s_most[warp] = most;
+  const long long before = cta_scan<S::kThreads>(mine, s_sums, &total) * p.blocks;
+  for (int w = 0; w < S::kWarps; ++w) most = max(most, s_most[w]);
   total *= p.blocks;
-  const long long chunk = (total + p.workers - 1) / p.workers;
-  // neighbouring workers sit on different SMs
-  const int worker = warp * gridDim.x + blockIdx.x;
-  // the worker's first unit: the thread whose units hold it, then that unit
-  for (int w = 0; w < S::kWarps; ++w) {
-    const long long at = (static_cast<long long>(w) * gridDim.x + blockIdx.x) * chunk;
-    if (at >= before * p.blocks && at < (before + mine) * p.blocks) {
-      s_unit[w] = u0;
-      s_before[w] = before * p.blocks;
+  // Few short row blocks: a CTA takes one whole, and nothing is joined across
+  // CTAs.  Else all CTAs take equal runs of tiles, at least kMinTiles.
+  const bool solo = units * p.blocks <= static_cast<int>(gridDim.x) && most <= kSoloTiles * S::kWarps;
+  const long long even = (total + gridDim.x - 1) / gridDim.x;
+  const int chunk = static_cast<int>(even > kMinTiles ? even : kMinTiles);
+  if (solo) {
+    if (threadIdx.x == 0) s_count = 0;
+    __syncthreads();
+    const int u = blockIdx.x / p.blocks;  // (one unit a thread at most)
+    if (static_cast<int>(threadIdx.x) == u && u < units) {
+      s_count = static_cast<int>(mine);
+      s_from = before + (blockIdx.x - u * p.blocks) * mine;
+      s_unit = u;
+      s_unit_from = before;
+    }
+  } else {
+    const long long from = static_cast<long long>(blockIdx.x) * chunk;
+    if (threadIdx.x == 0) s_count = static_cast<int>(max(0ll, min(static_cast<long long>(chunk), total - from)));
+    // the thread whose units hold the first tile
+    if (from >= before && from < before + mine * p.blocks) {
+      s_from = from;
+      s_unit = u0;
+      s_unit_from = before;
     }
   }
   __syncthreads();
-  const long long from = worker * chunk;
-  int left = static_cast<int>(min(chunk, total - from));  // tiles of this worker
-  if (chunk == 0 || left <= 0) return;
-  Place c;
-  {
-    int u = s_unit[warp];
-    long long at = s_before[warp];
-    int n;
-    while (at + static_cast<long long>(n = tiles_of(p.c, u)) * p.blocks <= from) {
+  const int share = ((solo ? s_count : chunk) + S::kWarps - 1) / S::kWarps;
+  int left = min(share, s_count - warp * share);  // tiles of this warp
+  if (left < 0) left = 0;
+  long long tile = s_from + warp * share;         // the one at hand
+  Place c = {};
+  if (left > 0) {
+    int u = s_unit, n;
+    long long at = s_unit_from;
+    while (at + static_cast<long long>(n = tiles_of(p.c, u)) * p.blocks <= tile) {
       at += static_cast<long long>(n) * p.blocks;
       ++u;
     }
-    const long long in = from - at;
+    const long long in = tile - at;
     c.unit = u;
     c.block = static_cast<int>(in / n);
-    const int slot = static_cast<int>(in - static_cast<long long>(c.block) * n) * kQ4TileSlots;
+    const int slot = static_cast<int>(in - static_cast<long long>(c.block) * n) * kTile;
     c.row = u * p.c.capacity + slot;
     c.valid = length_of(p.c, u) - slot;
   }
 
-  constexpr uint32_t kBytes = 2 * kCodeTile + 2 * kParamTile + (kPos ? kPosTile : 0);
   Place ahead = c;
   int to_issue = left;
   auto issue = [&](int stage) {
     if (lane == 0) {
       const uint32_t bar = bars + 8 * stage, cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
-      mbar_arrive_expect_tx(bar, kBytes);
+      // the capacity may end in the middle of the tile; codes of the next unit
+      // (or zeros, behind the last one) then come along and count nothing
+      const int slots = min(kTile, (ahead.unit + 1) * p.c.capacity - ahead.row);
+      mbar_arrive_expect_tx(bar, 2 * kCodeTile + slots * (2 * kQ4ParamBytes + (kPos ? 4 : 0)));
       tma_rows(cd, &p.map_k, bar, ahead.row);
       tma_rows(cd + kCodeTile, &p.map_v, bar, ahead.row);
       const size_t row = static_cast<size_t>(ahead.row);
-      bulk_copy(sd, p.c.params[0] + row * kQ4ParamBytes, kParamTile, bar);
-      bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, kParamTile, bar);
-      if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, kPosTile, bar);
+      bulk_copy(sd, p.c.params[0] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar);
+      bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar);
+      if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, slots * 4, bar);
     }
     if (--to_issue > 0) ahead.next(p);
   };
   for (int i = 0; i < S::kStages && to_issue > 0; ++i) issue(i);
+
 
   // ldmatrix row of this lane: slot lane & 7, piece lane >> 3 of its 64 bytes,
   // stored at piece ^ (slot / 2) by the 64-byte swizzle
@@ -406,12 +452,14 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   float ref[NB][2], l[NB][2];  // rows 2t, 2t + 1
   int vexp = kMinScaleExp;
   bool fresh = true;
+  int seg_tiles = 0;  // tiles of the row block so far
   uint32_t phase = 0;
   int stage = 0;
   bool failed = false;
 
   for (; left > 0; --left) {
     if (fresh) {
+      seg_tiles = 0;
       load_queries<NB>(p, c.unit, c.block, Q);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -434,35 +482,44 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       break;
     }
     __syncwarp();
+    ++seg_tiles;
     const uint32_t cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
     const int valid = c.valid;
 
-    // ---- scales: one lane a slot.  Slots behind the length and groups that
+    // ---- scales: two slots a lane.  Slots behind the length and groups that
     // hold a NaN count nothing in V's products
-    uint32_t nan_groups = 0;  // of this lane's slot
+    uint32_t nan_groups[2] = {0u, 0u};  // of this lane's slots
     bool special;
     {
-      const uint2 kw = lds64(sd + lane * kQ4ParamBytes);
-      uint4 w = lds128(sd + kParamTile + lane * kQ4ParamBytes);
-      if (lane >= valid) w = make_uint4(0u, 0u, 0u, 0u);
-      sts128(scales + lane * 16,
-             make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
-                        __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
-      uint32_t all = __reduce_max_sync(0xffffffffu, top_of(w));
+      uint4 w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int slot = lane + 32 * i;
+        const uint2 kw = lds64(sd + slot * kQ4ParamBytes);
+        w[i] = lds128(sd + kParamTile + slot * kQ4ParamBytes);
+        if (slot >= valid) w[i] = make_uint4(0u, 0u, 0u, 0u);
+        sts128(scales + slot * 16,
+               make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
+                          __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
+      }
+      uint32_t all = __reduce_max_sync(0xffffffffu, max(top_of(w[0]), top_of(w[1])));
       special = all >= 0x7f800000u;
       if (special) {
-        uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int J = 0; J < 4; ++J) {
-          const uint32_t half = 0xffffu << (16 * (J & 1)), inf = 0x7f807f80u & half;
-          if ((x[J >> 1] & inf) == inf || (x[2 + (J >> 1)] & inf) == inf) {
-            nan_groups |= 1u << J;
-            x[J >> 1] &= ~half;
-            x[2 + (J >> 1)] &= ~half;
+        for (int i = 0; i < 2; ++i) {
+          uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+          for (int J = 0; J < 4; ++J) {
+            const uint32_t half = 0xffffu << (16 * (J & 1)), inf = 0x7f807f80u & half;
+            if ((x[J >> 1] & inf) == inf || (x[2 + (J >> 1)] & inf) == inf) {
+              nan_groups[i] |= 1u << J;
+              x[J >> 1] &= ~half;
+              x[2 + (J >> 1)] &= ~half;
+            }
           }
+          w[i] = make_uint4(x[0], x[1], x[2], x[3]);
         }
-        w = make_uint4(x[0], x[1], x[2], x[3]);
-        all = min(__reduce_max_sync(0xffffffffu, top_of(w)), 0x7f000000u);
+        all = min(__reduce_max_sync(0xffffffffu, max(top_of(w[0]), top_of(w[1]))), 0x7f000000u);
       }
       const int k = max(static_cast<int>(all >> 23) - 127, kMinScaleExp);
       if (k > vexp) {  // the sums go to the new power of two
@@ -481,22 +538,25 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         vexp = k;
       }
       const float f = pow2(kTopExp - vexp);
-      const uint32_t s01 = pack_half2(bf_lo(w.x) * f, bf_hi(w.x) * f);
-      const uint32_t s23 = pack_half2(bf_lo(w.y) * f, bf_hi(w.y) * f);
-      // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
-      const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
-      const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
-      sts128(sd + kParamTile + lane * kQ4ParamBytes,
-             make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632),
-                        pack_half2(bf_lo(w.z) * f, bf_hi(w.z) * f),
-                        pack_half2(bf_lo(w.w) * f, bf_hi(w.w) * f)));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t s01 = pack_half2(bf_lo(w[i].x) * f, bf_hi(w[i].x) * f);
+        const uint32_t s23 = pack_half2(bf_lo(w[i].y) * f, bf_hi(w[i].y) * f);
+        // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
+        const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
+        sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
+               make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632),
+                          pack_half2(bf_lo(w[i].z) * f, bf_hi(w[i].z) * f),
+                          pack_half2(bf_lo(w[i].w) * f, bf_hi(w[i].w) * f)));
+      }
       __syncwarp();
     }
 
-    // ---- logits: twice 16 slots; slots g and g + 8 of rows 2t and 2t + 1
-    float z[NB][2][4];  // [8 rows][16 slots][slot half, row]
+    // ---- logits: 16 slots a step; slots g and g + 8 of rows 2t and 2t + 1
+    float z[NB][kSteps][4];  // [8 rows][16 slots][slot half, row]
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kSteps; ++h) {
       const int s16 = h * 16;
       uint32_t wa[4], wb[4];
       ldmatrix4(wa, cd + s16 * kQ4CodeBytes + mat);
@@ -541,9 +601,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           }
       }
     }
-    if (valid < kQ4TileSlots) {
+    if (valid < kTile) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < kSteps; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (h * 16 + (i >> 1) * 8 + g >= valid)
@@ -559,9 +619,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           if (r < p.rows) {
             float* zp = p.z + (static_cast<long long>(c.unit) * (p.rows - 1) + r) * p.c.capacity + c.row + g;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              zp[h * 16] = z[nb][h][j] * Q.f2[nb][j];
-              zp[h * 16 + 8] = z[nb][h][2 + j] * Q.f2[nb][j];
+            for (int h = 0; h < kSteps; ++h) {
+              // (behind the length there may be the next row)
+              if (h * 16 + g < valid) zp[h * 16] = z[nb][h][j] * Q.f2[nb][j];
+              if (h * 16 + 8 + g < valid) zp[h * 16 + 8] = z[nb][h][2 + j] * Q.f2[nb][j];
             }
           }
         }
@@ -575,7 +636,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       bool raise = false;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        top[j] = fmaxf(fmaxf(z[nb][0][j], z[nb][0][2 + j]), fmaxf(z[nb][1][j], z[nb][1][2 + j]));
+        top[j] = fmaxf(z[nb][0][j], z[nb][0][2 + j]);
+#pragma unroll
+        for (int h = 1; h < kSteps; ++h) top[j] = fmaxf(top[j], fmaxf(z[nb][h][j], z[nb][h][2 + j]));
         top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 4));
         top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8));
         top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16)) * Q.f2[nb][j];
@@ -602,10 +665,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         // rows that see a slot's NaN group
         uint32_t hit[2] = {0u, 0u};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kSteps; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t m = __shfl_sync(0xffffffffu, nan_groups, h * 16 + (i >> 1) * 8 + g);
+            const uint32_t m = __shfl_sync(0xffffffffu, nan_groups[h >> 1], (h & 1) * 16 + (i >> 1) * 8 + g);
             if (z[nb][h][i] != -INFINITY) hit[i & 1] |= m;
           }
 #pragma unroll
@@ -620,7 +683,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       for (int j = 0; j < 2; ++j) {
         const float r = ref[nb][j] == -INFINITY ? 0.f : ref[nb][j] - kLift;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kSteps; ++h)
 #pragma unroll
           for (int i = j; i < 4; i += 2) {
             z[nb][h][i] = ex2_approx(fmaf(z[nb][h][i], Q.f2[nb][j], -r));
@@ -629,9 +692,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
     }
 
-    // ---- outputs: twice 16 slots
+    // ---- outputs
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kSteps; ++h) {
       const int s16 = h * 16;
       uint32_t va[4], vb[4], pm[4];
       ldmatrix4_t(va, cd + kCodeTile + s16 * kQ4CodeBytes + mat);
@@ -653,16 +716,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
 #pragma unroll
       for (int J = 0; J < 4; ++J) {
-        const uint32_t ah = va[J] >> 8, bh = vb[J] >> 8;
-        const uint32_t a0 = va[J] & 0x000f000fu, a1 = va[J] & 0x00f000f0u;
-        const uint32_t a2 = vb[J] & 0x000f000fu, a3 = vb[J] & 0x00f000f0u;
-        const uint32_t b0 = ah & 0x000f000fu, b1 = ah & 0x00f000f0u;
-        const uint32_t b2 = bh & 0x000f000fu, b3 = bh & 0x00f000f0u;
+        // bytes 1 and 3 of a word in the place of 0 and 2
+        const uint32_t ah = __byte_perm(va[J], 0u, 0x4341), bh = __byte_perm(vb[J], 0u, 0x4341);
+        const uint32_t a0 = va[J] & 0x00ff00ffu, a1 = va[J] & 0x00f000f0u;
+        const uint32_t a2 = vb[J] & 0x00ff00ffu, a3 = vb[J] & 0x00f000f0u;
+        const uint32_t b1 = ah & 0x00f000f0u, b3 = bh & 0x00f000f0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const uint32_t q0 = mul_half2(p0[nb], sa[J]), q1 = mul_half2(p1[nb], sb[J]);
           mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
-          mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
+          mma_f16(o[nb][J][1], ah, b1, bh, b3, q0, q1);
         }
       }
     }
@@ -687,23 +750,43 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       phase ^= 1u;
     }
 
-    // ---- the row block ends here, or this worker's share of it
-    const int unit = c.unit, block = c.block;
+    // ---- the row block ends here, or this warp's share of it
+    const int unit = c.unit, block = c.block, done = c.row - c.unit * p.c.capacity;
+    const int len = done + c.valid;
+    ++tile;
+    const bool ends = c.valid <= kTile;
     if (left > 1) c.next(p);
-    if (left == 1 || c.unit != unit || c.block != block) {
-      const long long part = static_cast<long long>(worker) + static_cast<long long>(unit) * p.blocks + block;
+    if (left == 1 || ends) {
+      const int count = (len + kTile - 1) / kTile;
+      const bool starts = seg_tiles > done / kTile;
+      const bool whole = starts && ends, tail = left == 1;
+      if (!whole && lane == 0) {
+        Part& part = tail ? s_tail[warp] : s_head[warp];
+        part.block = unit * p.blocks + block;
+        part.count = count;
+        part.first = tile - 1 - done / kTile;
+        part.starts = starts;
+        part.ends = ends;
+      }
+      // sums of the codes' products: * 2^24 for the pair's sum, 2^20 for its second channel
+      const float f = pow2(vexp - kTopExp);
+      float* head = p.head_o + static_cast<size_t>(blockIdx.x * S::kWarps + warp) * kRows * kHeadDim;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
+        float sum[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          float sum = l[nb][j];
-          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-          if (g == 0) p.part_ml[part * (8 * NB) + nb * 8 + 2 * t + j] = make_float2(ref[nb][j] - kLift, sum);
+          sum[j] = l[nb][j];
+          sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 4);
+          sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
+          sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+          if (!whole && g == 0) {
+            const float2 ml = make_float2(ref[nb][j] - kLift, sum[j]);
+            const int r = nb * 8 + 2 * t + j;
+            if (tail) s_ml[warp][r] = ml;
+            else p.head_ml[(blockIdx.x * S::kWarps + warp) * kRows + r] = ml;
+          }
         }
-        const float f = pow2(vexp - kTopExp);  // codes' sums: * 2^24, and 1/16 for the odd channels
-        float* dst = p.part_o + (part * (8 * NB) + nb * 8) * kHeadDim;
 #pragma unroll
         for (int J = 0; J < 4; ++J) {
           const float m0 = __shfl_sync(0xffffffffu, om[nb][0], (4 + J) * 4 + t);
@@ -711,13 +794,18 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float m = i ? m1 : m0;
+            const int r = nb * 8 + 2 * t + i, row = block * kRows + r;
             float4 v;
-            v.x = fmaf(o[nb][J][0][i], 16777216.0f, m) * f;
+            v.x = fmaf(o[nb][J][0][i] - o[nb][J][0][2 + i], 16777216.0f, m) * f;
             v.y = fmaf(o[nb][J][0][2 + i], 1048576.0f, m) * f;
-            v.z = fmaf(o[nb][J][1][i], 16777216.0f, m) * f;
+            v.z = fmaf(o[nb][J][1][i] - o[nb][J][1][2 + i], 16777216.0f, m) * f;
             v.w = fmaf(o[nb][J][1][2 + i], 1048576.0f, m) * f;
-            if (block * (8 * NB) + nb * 8 + 2 * t + i < p.rows)
-              *reinterpret_cast<float4*>(dst + (2 * t + i) * kHeadDim + 32 * J + 4 * g) = v;
+            if (row >= p.rows) continue;
+            if (whole) write_row(p, unit, row, 8 * J + g, v, ref[nb][i] - kLift, sum[i]);
+            else if (tail) sts128(codes + r * (kHeadDim * 4) + (8 * J + g) * 16,
+                                  make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z),
+                                             __float_as_uint(v.w)));
+            else reinterpret_cast<float4*>(head + r * kHeadDim)[8 * J + g] = v;
           }
         }
       }
@@ -732,84 +820,156 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
     }
   }
+  // ---- units that hold nothing
+  for (int u = blockIdx.x + gridDim.x * warp; u < units; u += gridDim.x * S::kWarps)
+    if (length_of(p.c, u) == 0)
+      for (int r = 0; r < p.rows; ++r)
+        write_row(p, u, r, lane, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
+
+  // ---- row blocks that this CTA's warps share: joined in slot order
+  __syncthreads();
+  if (s_abort) return;
+  __shared__ Part s_shared[2];  // row blocks shared with the CTAs before, behind
+  if (threadIdx.x < 2) s_shared[threadIdx.x].block = -1;
+  __syncthreads();
+  for (int w = -1; w < S::kWarps; ++w) {
+    // a row block's first part here: the first warp's head, or a warp's tail
+    // that is not the one before it
+    const Part& first = w < 0 ? s_head[0] : s_tail[w];
+    const int vu = first.block;
+    if (vu < 0 || (w > 0 && s_tail[w - 1].block == vu)) continue;
+    int end = max(w, 0) + 1;  // tails of warps w .. end - 1, then perhaps a head
+    if (w >= 0)
+      while (end < S::kWarps && s_tail[end].block == vu) ++end;
+    const bool plus = w < 0 || (end < S::kWarps && s_head[end].block == vu);
+    const int tails = w < 0 ? 0 : end - w, head_of = w < 0 ? 0 : end;
+    const bool ends = plus ? s_head[head_of].ends : s_tail[end - 1].ends;
+    const int unit = vu / p.blocks, row0 = (vu - unit * p.blocks) * kRows;
+    const int which = first.starts ? 1 : 0;
+    const bool whole = first.starts && ends;
+    for (int r = warp; r < kRows && row0 + r < p.rows; r += S::kWarps) {
+      float2 hml = make_float2(-INFINITY, 0.f);
+      if (plus) hml = p.head_ml[(blockIdx.x * S::kWarps + head_of) * kRows + r];
+      float top = hml.x;
+      for (int k = 0; k < tails; ++k) top = fmaxf(top, s_ml[w + k][r].x);
+      const float ref0 = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      auto add = [&](float2 ml, float4 v) {
+        const float f = ex2_approx(ml.x - ref0);
+        sum = fmaf(ml.y, f, sum);
+        acc.x = fmaf(v.x, f, acc.x);
+        acc.y = fmaf(v.y, f, acc.y);
+        acc.z = fmaf(v.z, f, acc.z);
+        acc.w = fmaf(v.w, f, acc.w);
+      };
+      for (int k = 0; k < tails; ++k) {
+        const uint4 v = lds128(base + (w + k) * S::kStages * 2 * kCodeTile + r * (kHeadDim * 4) + lane * 16);
+        add(s_ml[w + k][r], make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z),
+                                        __uint_as_float(v.w)));
+      }
+      if (plus)
+        add(hml, reinterpret_cast<const float4*>(
+                     p.head_o + (static_cast<size_t>(blockIdx.x * S::kWarps + head_of) * kRows + r) * kHeadDim)[lane]);
+      if (whole) {
+        write_row(p, unit, row0 + r, lane, acc, top, sum);
+      } else {
+        const size_t at = static_cast<size_t>(blockIdx.x * 2 + which) * kRows + r;
+        reinterpret_cast<float4*>(p.cta_o + at * kHeadDim)[lane] = acc;
+        if (lane == 0) p.cta_ml[at] = make_float2(top, sum);
+      }
+    }
+    if (!whole && threadIdx.x == 0) s_shared[which] = first;
+  }
+
+  // ---- row blocks that CTAs share: the last one to come joins them, in order
+  __threadfence();
+  __syncthreads();
+  if (s_shared[0].block < 0 && s_shared[1].block < 0) return;
+  __shared__ int s_last[2];
+  if (threadIdx.x < 2) {
+    s_last[threadIdx.x] = 0;
+    const Part part = s_shared[threadIdx.x];
+    if (part.block >= 0) {
+      const int c0 = static_cast<int>(part.first / chunk), c1 = static_cast<int>((part.first + part.count - 1) / chunk);
+      if (atomicAdd(p.tickets + c0, 1) == c1 - c0) {
+        p.tickets[c0] = 0;  // for the next call
+        s_last[threadIdx.x] = 1;
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+  float4* s_acc = reinterpret_cast<float4*>(smem_raw + (base - smem_u32(smem_raw)));
+  for (int which = 0; which < 2; ++which) {
+    if (!s_last[which]) continue;
+    const Part part = s_shared[which];
+    const int c0 = static_cast<int>(part.first / chunk), c1 = static_cast<int>((part.first + part.count - 1) / chunk);
+    const int unit = part.block / p.blocks, row0 = (part.block - unit * p.blocks) * kRows;
+    const int rows = min(kRows, p.rows - row0);
+    for (int r0 = 0; r0 < rows; r0 += S::kWarps) {
+      // several warps a row where there are fewer rows
+      const int rn = min(rows - r0, S::kWarps), split = S::kWarps / rn;
+      const int r = r0 + warp % rn, k = warp / rn;
+      float top = -INFINITY, sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k < split) {
+        auto at = [&](int c) { return static_cast<size_t>(c * 2 + (c == c0)) * kRows + r; };
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(&p.cta_ml[at(c)].x));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref0 = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+        for (int c = c0 + k; c <= c1; c += split) {
+          const float2 ml = __ldcg(&p.cta_ml[at(c)]);
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(p.cta_o + at(c) * kHeadDim) + lane);
+          const float f = ex2_approx(ml.x - ref0);
+          sum = fmaf(ml.y, f, sum);
+          acc.x = fmaf(v.x, f, acc.x);
+          acc.y = fmaf(v.y, f, acc.y);
+          acc.z = fmaf(v.z, f, acc.z);
+          acc.w = fmaf(v.w, f, acc.w);
+        }
+      }
+      __syncthreads();
+      s_acc[warp * 32 + lane] = acc;
+      if (lane == 0) s_ml[warp][0] = make_float2(top, sum);
+      __syncthreads();
+      if (k == 0) {
+        for (int i = 1; i < split; ++i) {
+          const float4 v = s_acc[(warp + i * rn) * 32 + lane];
+          sum += s_ml[warp + i * rn][0].y;
+          acc.x += v.x;
+          acc.y += v.y;
+          acc.z += v.z;
+          acc.w += v.w;
+        }
+        write_row(p, unit, row0 + r, lane, acc, top, sum);
+      }
+    }
+  }
 }
 
-// ---------------------------------------------------------------- joining
-// A CTA takes one query row of a unit: its parts' references and sums, then
-// their outputs, a warp a part.
-constexpr int kCombineThreads = 256;
-
-__global__ void __launch_bounds__(kCombineThreads) combine_kernel(const __grid_constant__ Q4AttendParams p) {
-  __shared__ float s_red[kCombineThreads / 32];
-  __shared__ float4 s_o[kCombineThreads / 32][32];
-  const int unit = blockIdx.x, r = blockIdx.y;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int units = p.c.batch * p.c.num_kv_heads;
-  const int brows = p.rows <= 8 ? 8 : 16;
-  const int block = r / brows, rb = r - block * brows;
-  const long long total = p.first_tile[units] * p.blocks;
-  const long long chunk = (total + p.workers - 1) / p.workers;
-  const long long before = p.first_tile[unit], n = p.first_tile[unit + 1] - before;
-  const long long from = before * p.blocks + block * n;
-  const int b = unit / p.c.num_kv_heads, h = (unit - b * p.c.num_kv_heads) * p.group + r / p.num_queries;
-  const int qi = r % p.num_queries;
-  int first = 0, count = 0;
-  if (n > 0) {
-    first = static_cast<int>(from / chunk);
-    count = static_cast<int>((from + n - 1) / chunk) - first + 1;
-  }
-  const long long part0 = static_cast<long long>(first) + static_cast<long long>(unit) * p.blocks + block;
-  const float2* ml = p.part_ml + part0 * brows + rb;
-  float top = -INFINITY;
-  for (int i = threadIdx.x; i < count; i += kCombineThreads) top = fmaxf(top, ml[static_cast<long long>(i) * brows].x);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) s_red[warp] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kCombineThreads / 32; ++w) top = fmaxf(top, s_red[w]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
-  for (int i = warp; i < count; i += kCombineThreads / 32) {
-    const float2 x = ml[static_cast<long long>(i) * brows];
-    const float f = ex2_approx(x.x - ref);
-    const float4 v = reinterpret_cast<const float4*>(p.part_o + ((part0 + i) * brows + rb) * kHeadDim)[lane];
-    sum = fmaf(x.y, f, sum);
-    acc.x = fmaf(v.x, f, acc.x);
-    acc.y = fmaf(v.y, f, acc.y);
-    acc.z = fmaf(v.z, f, acc.z);
-    acc.w = fmaf(v.w, f, acc.w);
-  }
-  s_o[warp][lane] = acc;
-  __syncthreads();
-  if (lane == 0) s_red[warp] = sum;
-  __syncthreads();
-  if (warp != 0) return;
-  sum = 0.f;
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int w = 0; w < kCombineThreads / 32; ++w) {
-    sum += s_red[w];
-    const float4 v = s_o[w][lane];
-    acc.x += v.x;
-    acc.y += v.y;
-    acc.z += v.z;
-    acc.w += v.w;
-  }
+// Four channels (4 * lane ..) of a query row's output: v / sum, where `sum` is
+// that of 2^(logit - ref); the first lane writes the log-sum-exp.
+__device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int row, int lane, float4 v,
+                                          float ref, float sum) {
+  const int b = unit / p.c.num_kv_heads;
+  const int hg = row / p.num_queries, qi = row - hg * p.num_queries;
+  const int h = (unit - b * p.c.num_kv_heads) * p.group + hg;
   const float f = sum == 0.f ? 0.f : 1.0f / sum;
   uint2 y;
   if (p.is_bf16) {
-    y.x = pack_bf16(acc.x * f, acc.y * f);
-    y.y = pack_bf16(acc.z * f, acc.w * f);
+    y.x = pack_bf16(v.x * f, v.y * f);
+    y.y = pack_bf16(v.z * f, v.w * f);
   } else {
-    y.x = pack_half2(acc.x * f, acc.y * f);
-    y.y = pack_half2(acc.z * f, acc.w * f);
+    y.x = pack_half2(v.x * f, v.y * f);
+    y.y = pack_half2(v.z * f, v.w * f);
   }
   *reinterpret_cast<uint2*>(p.out + b * p.o_bs + h * p.o_hs + qi * p.o_qs + 4 * lane) = y;
   if (lane == 0) {
     const float l2 = ref + log2f(sum);
-    p.lse_ws[static_cast<long long>(unit) * p.rows + r] = l2;
+    p.lse_ws[static_cast<long long>(unit) * p.rows + row] = l2;
     if (p.lse) p.lse[(static_cast<long long>(b) * p.num_q_heads + h) * p.num_queries + qi] = l2 * kLn2;
   }
 }
@@ -840,7 +1000,7 @@ cudaError_t launch(const Q4AttendParams& p, int sms, cudaStream_t stream) {
 
 }  // namespace
 
-int q4_attend_workers(int rows, int sms) { return sms * (rows <= 8 ? Shape<1>::kWarps : Shape<2>::kWarps); }
+int q4_attend_warps(int rows) { return rows <= 8 ? Shape<1>::kWarps : Shape<2>::kWarps; }
 
 cudaError_t q4_attend_set_smem_limit() {
   cudaError_t e = cudaSuccess;
@@ -856,12 +1016,6 @@ cudaError_t q4_attend_set_smem_limit() {
 
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t stream) {
   return p.rows <= 8 ? launch<1>(p, sms, stream) : launch<2>(p, sms, stream);
-}
-
-cudaError_t launch_q4_combine(const Q4AttendParams& p, cudaStream_t stream) {
-  const dim3 grid(p.c.batch * p.c.num_kv_heads, p.rows);
-  combine_kernel<<<grid, kCombineThreads, 0, stream>>>(p);
-  return cudaGetLastError();
 }
 
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t stream) {

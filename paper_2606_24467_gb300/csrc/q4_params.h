@@ -14,10 +14,12 @@ constexpr int kQ4GroupDim = 32;                         // channels that share a
 constexpr int kQ4Groups = kHeadDim / kQ4GroupDim;       // 4
 constexpr int kQ4CodeBytes = kHeadDim / 2;              // codes of one K or V row
 constexpr int kQ4ParamBytes = 4 * kQ4Groups;            // 4 bf16 scales, 4 bf16 minima
-constexpr int kQ4TileSlots = 32;                        // capacity is a multiple of this
+constexpr int kQ4SlotStep = 32;                         // capacity is a multiple of this
+constexpr int kQ4TileSlots = 64;                        // slots of a tile of the attention
 constexpr int kQ4MaxUnits = 65535;                      // (sequence, KV group) pairs of a cache
 constexpr int kQ4MaxQueries = 16;                       // query tokens a sequence and call
-constexpr int kQ4HeaderBytes = 256;                     // workspace: the status word
+constexpr int kQ4MaxCtas = 160;                         // of the attention
+constexpr int kQ4HeaderBytes = 1024;                    // workspace: status word, tickets
 
 // The cache as the kernels see it; unit u = sequence * num_kv_heads + group,
 // slot row = u * capacity + slot.
@@ -55,11 +57,10 @@ using Q4AppendParams = Q4WriteParams<0>;
 using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
 using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
-// Attention.  The tiles (32 slots) of all row blocks -- up to 16 query rows of
-// a unit -- form one sequence, of which every worker (a warp) takes `chunk`
-// neighbours, so a worker covers the end of one row block, any number of whole
-// ones and the start of another.  For each it leaves a part; since worker and
-// row block both grow along the sequence, worker + row block numbers the parts.
+// Attention.  The tiles (64 slots) of all row blocks -- up to 16 query rows of
+// a unit -- form one sequence, of which every CTA takes an equal run, and every
+// warp of it a run of that.  Where there are few short row blocks, a CTA takes
+// one each instead.
 struct Q4AttendParams {
   CUtensorMap map_k, map_v;    // codes: [units * capacity] rows of 64 bytes, boxes of 32 rows
   Q4Cache c;
@@ -71,12 +72,13 @@ struct Q4AttendParams {
   float scale_log2;            // softmax scale * log2(e)
   int num_q_heads, group, num_queries, is_bf16, accumulate;
   int rows, blocks;            // query rows of a unit, and row blocks of them
-  int workers;                 // warps of the launch
   int* status;
   // workspace
-  long long* first_tile;       // [units + 1]: tiles before each unit (one row block)
-  float* part_o;               // [workers + units * blocks][block rows][128]
-  float2* part_ml;             // [workers + units * blocks][block rows]: reference and sum
+  int* tickets;                // [CTAs]: CTAs done with the row block that starts in one and goes on
+  float* head_o;               // [warps]: the end of a row block that another warp began,
+  float2* head_ml;             //   [block rows][128], and its softmax reference and sum
+  float* cta_o;                // [CTAs][2]: likewise of row blocks from before, and going on
+  float2* cta_ml;
   float* lse_ws;               // [units][rows]: base-2 log-sum-exp
   float* z;                    // accumulate: [units][rows][capacity] base-2 logits
 };
@@ -95,11 +97,9 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherUnitParams& p, cudaStream_t s);
 constexpr int q4_block_rows(int rows) { return rows <= 8 ? 8 : 16; }
-// Warps that the attention launches on `sms` SMs.
-int q4_attend_workers(int rows, int sms);
+int q4_attend_warps(int rows);  // of a CTA; there is one an SM
 cudaError_t q4_attend_set_smem_limit();
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t s);
-cudaError_t launch_q4_combine(const Q4AttendParams& p, cudaStream_t s);
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);
 cudaError_t q4_evict_set_smem_limit();
 cudaError_t launch_q4_evict(const Q4EvictParams& p, int sms, cudaStream_t s);
