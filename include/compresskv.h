@@ -429,7 +429,7 @@ typedef struct ckv_q4_rows {
  * the same shape; its rows must not overlap). */
 typedef struct ckv_q4_queries {
   int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads; head h uses group h / (its share) */
-  int32_t num_queries;      /* query tokens of a sequence: 1..16 */
+  int32_t num_queries;      /* query tokens of a sequence: 1..16; at most 256 with all heads of a group */
   int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16, of q and out */
   int32_t accumulate;       /* non-zero: add the attention to the cache's weights */
   float scale;              /* softmax scale; 0 selects 1/sqrt(head_dim) */

@@ -98,6 +98,7 @@ int check_workspace(const void* ws, size_t have, size_t need) {
 int check_heads(const ckv_q4_cache* c, int num_q_heads, int num_queries) {
   if (num_q_heads < 1 || num_queries < 1 || num_q_heads % c->num_kv_heads) return CKV_ERR_INVALID_ARG;
   if (num_q_heads > kMaxQHeads || num_queries > kQ4MaxQueries) return CKV_ERR_UNSUPPORTED;
+  if (num_q_heads / c->num_kv_heads * num_queries > kMaxQRows) return CKV_ERR_UNSUPPORTED;
   return CKV_OK;
 }
 
@@ -277,9 +278,14 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   Q4AttendParams P;
   std::memset(&P, 0, sizeof(P));
+  P.group = a->num_q_heads / c->num_kv_heads;
+  P.num_queries = a->num_queries;
+  P.rows = P.group * P.num_queries;
+  P.blocks = (P.rows + q4_block_rows(P.rows) - 1) / q4_block_rows(P.rows);
+  const int tile = q4_attend_tile(P.rows);
   const unsigned long long slots = static_cast<unsigned long long>(units_of(c)) * c->capacity;
-  if ((rc = make_row64_map(c->k_codes, slots, kQ4TileSlots, &P.map_k)) != CKV_OK) return rc;
-  if ((rc = make_row64_map(c->v_codes, slots, kQ4TileSlots, &P.map_v)) != CKV_OK) return rc;
+  if ((rc = make_row64_map(c->k_codes, slots, tile, &P.map_k)) != CKV_OK) return rc;
+  if ((rc = make_row64_map(c->v_codes, slots, tile, &P.map_v)) != CKV_OK) return rc;
   P.c = device_cache(c);
   P.q = static_cast<const uint16_t*>(q);
   P.out = static_cast<uint16_t*>(out);
@@ -294,15 +300,11 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   const double scale = a->scale > 0.f ? a->scale : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
   P.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
   P.num_q_heads = a->num_q_heads;
-  P.group = a->num_q_heads / c->num_kv_heads;
-  P.num_queries = a->num_queries;
   P.is_bf16 = a->dtype == CKV_DTYPE_BF16;
   P.accumulate = a->accumulate != 0;
   P.status = static_cast<int*>(workspace);
-  P.rows = P.group * P.num_queries;
-  P.blocks = (P.rows + q4_block_rows(P.rows) - 1) / q4_block_rows(P.rows);
   // no more CTAs than there can be tiles
-  const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + kQ4TileSlots - 1) / kQ4TileSlots) * P.blocks;
+  const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + tile - 1) / tile) * P.blocks;
   sms = static_cast<int>(std::min<long long>({sms, kQ4MaxCtas, tiles}));
   P.tickets = reinterpret_cast<int*>(ws + kTicketBytes);
   P.head_ml = reinterpret_cast<float2*>(ws + area.head_ml);

@@ -6,7 +6,7 @@
 //
 // Bound by memory: 160 bytes a slot against at most a few thousand operations,
 // so the kernel is built around a steady stream of slots and few instructions
-// a code.  Every warp takes a run of tiles of 64 slots (see Q4AttendParams) and
+// a code.  Every warp takes a run of tiles of 48 or 64 slots (see Q4AttendParams) and
 // keeps two to four in flight with TMA into its own part of shared memory.  A
 // row block that lies in its run it finishes itself; of others it leaves the
 // softmax reference, sum and outputs, which its CTA joins, and for row blocks
@@ -49,8 +49,10 @@ namespace ckv {
 namespace {
 
 #ifndef Q4W1
-#define Q4W1 8
+#define Q4T1 48
+#define Q4W1 12
 #define Q4S1 2
+#define Q4T2 64
 #define Q4W2 8
 #define Q4S2 2
 #endif
@@ -66,25 +68,27 @@ constexpr int kMinScaleExp = -110;     // smaller scales and minima share this r
 
 // Shared memory of a worker's stage: codes of K and V (swizzled), then params
 // and positions.
-constexpr int kTile = kQ4TileSlots;  // 64
-constexpr int kSteps = kTile / 16;
-constexpr int kCodeTile = kTile * kQ4CodeBytes;    // 4096
-constexpr int kParamTile = kTile * kQ4ParamBytes;  // 1024
-constexpr int kPosTile = kTile * 4;                // 256
-constexpr int kSideBytes = 2 * kParamTile + kPosTile;
 constexpr int kMinTiles = Q4MIN;    // least tiles of a CTA that shares row blocks
 constexpr int kSoloTiles = Q4SOLO;  // most tiles a warp of a row block in one CTA
-constexpr int kScaleTile = kTile * 16;             // K's scales of the tile at hand, fp32
 
 template <int NB>
 struct Shape {
+  static constexpr int kTile = NB == 1 ? Q4T1 : Q4T2;  // slots
   static constexpr int kWarps = NB == 1 ? Q4W1 : Q4W2;
   static constexpr int kStages = NB == 1 ? Q4S1 : Q4S2;
   static constexpr int kThreads = kWarps * 32;
+  static constexpr int kSteps = kTile / 16;
+  static constexpr int kCodeTile = kTile * kQ4CodeBytes;
+  static constexpr int kParamTile = kTile * kQ4ParamBytes;
+  static constexpr int kSideBytes = 2 * kParamTile + kTile * 4;
+  static constexpr int kScaleTile = kTile * 16;  // K's scales of the tile at hand, fp32
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
   static constexpr int kScales = kWarps * kScaleTile;
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
+  static_assert(kTile % 16 == 0 && kTile > 32 && kTile <= 64, "two slots a lane");
+  static_assert(kCodeTile % 512 == 0, "swizzle");
+  static_assert(kStages * 2 * kCodeTile >= 8 * NB * kHeadDim * 4, "a warp's outputs fit its stages");
 };
 
 __device__ __forceinline__ float to_float(uint32_t h, bool bf16) {
@@ -181,6 +185,7 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
 __device__ __forceinline__ int length_of(const Q4Cache& c, int unit) {
   return min(max(__ldg(c.lengths + unit), 0), c.capacity);
 }
+template <int kTile>
 __device__ __forceinline__ int tiles_of(const Q4Cache& c, int unit) {
   return (length_of(c, unit) + kTile - 1) / kTile;
 }
@@ -192,6 +197,7 @@ struct Place {
   int valid;  // slots in use from there on
   // The next tile; past the end of a row block the next one that has tiles
   // (the caller knows that there is one).
+  template <int kTile>
   __device__ __forceinline__ void next(const Q4AttendParams& p) {
     row += kTile;
     valid -= kTile;
@@ -205,26 +211,14 @@ struct Place {
   }
 };
 
-// Sum over the CTA of one number a thread: the exclusive prefix, and the total.
-template <int kThreads>
-__device__ __forceinline__ long long cta_scan(long long v, long long* s_sums, long long* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
+// Inclusive prefix over a warp.
+__device__ __forceinline__ int warp_prefix(int x, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 31) s_sums[warp] = x;
-  __syncthreads();
-  long long before = 0, all = 0;
-  for (int w = 0; w < kThreads / 32; ++w) {
-    const long long t = s_sums[w];
-    if (w < warp) before += t;
-    all += t;
-  }
-  *total = all;
-  return before + x - v;
+  return x;
 }
 
 // The largest of 16 s and |m| of a params row, as the bits of a float (whose
@@ -239,7 +233,7 @@ __device__ __forceinline__ uint32_t top_of(uint4 w) {
 struct Part {
   int block;        // unit * blocks + row block, or -1
   int count;        // tiles of the row block
-  long long first;  // its first tile
+  int first;        // its first tile
   bool starts, ends;
 };
 
@@ -334,10 +328,11 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     attend_kernel(const __grid_constant__ Q4AttendParams p) {
   using S = Shape<NB>;
   constexpr int kRows = 8 * NB;
+  constexpr int kTile = S::kTile, kSteps = S::kSteps;
+  constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
+  constexpr int kScaleTile = S::kScaleTile;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ long long s_sums[S::kWarps], s_from;
-  __shared__ int s_most[S::kWarps], s_count, s_unit, s_abort;
-  __shared__ long long s_unit_from;
+  __shared__ int s_sums[S::kWarps], s_most[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
   __shared__ float2 s_ml[S::kWarps][kRows];
   __shared__ Part s_tail[S::kWarps], s_head[S::kWarps];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -357,67 +352,131 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     tma_prefetch_map(&p.map_v);
   }
   fence_mbar_init();
+  __syncthreads();  // (the others' parts and the abort flag)
+  pdl_wait();  // everything before is of this launch alone
+  pdl_launch_dependents();
 
-  // ---- this CTA's tiles, and this warp's share of them
-  const int units = p.c.batch * p.c.num_kv_heads;
-  const int span = (units + S::kThreads - 1) / S::kThreads;  // units a thread adds up
-  const int u0 = min(static_cast<int>(threadIdx.x) * span, units), u1 = min(u0 + span, units);
-  long long mine = 0, total = 0;
-  int most = 0;
-  for (int u = u0; u < u1; ++u) {
-    const int n = tiles_of(p.c, u);
-    mine += n;
-    most = max(most, n);
-  }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if (lane == 0) s_most[warp] = most;
-  const long long before = cta_scan<S::kThreads>(mine, s_sums, &total) * p.blocks;
-  for (int w = 0; w < S::kWarps; ++w) most = max(most, s_most[w]);
-  total *= p.blocks;
+  // ---- this CTA's tiles, and this warp's share of them.  (The host bounds the
+  // tiles by 2^30.)
   // Few short row blocks: a CTA takes one whole, and nothing is joined across
   // CTAs.  Else all CTAs take equal runs of tiles, at least kMinTiles.
-  const bool solo = units * p.blocks <= static_cast<int>(gridDim.x) && most <= kSoloTiles * S::kWarps;
-  const long long even = (total + gridDim.x - 1) / gridDim.x;
-  const int chunk = static_cast<int>(even > kMinTiles ? even : kMinTiles);
-  if (solo) {
-    if (threadIdx.x == 0) s_count = 0;
-    __syncthreads();
-    const int u = blockIdx.x / p.blocks;  // (one unit a thread at most)
-    if (static_cast<int>(threadIdx.x) == u && u < units) {
-      s_count = static_cast<int>(mine);
-      s_from = before + (blockIdx.x - u * p.blocks) * mine;
-      s_unit = u;
-      s_unit_from = before;
+  const int units = p.c.batch * p.c.num_kv_heads, ctas = gridDim.x;
+  int chunk = 0, tile = 0, left = 0;  // tiles of a CTA; this warp's first tile, and how many
+  int unit0 = 0, at = 0;              // the unit that holds it, and that unit's first tile
+  auto divide = [&](int total, int most, int solo_first, int solo_count) {
+    const bool solo = units * p.blocks <= ctas && most <= kSoloTiles * S::kWarps;
+    chunk = solo ? solo_count : max((total + ctas - 1) / ctas, kMinTiles);
+    const int share = (chunk + S::kWarps - 1) / S::kWarps;
+    const int from = solo ? solo_first : static_cast<int>(blockIdx.x) * chunk;
+    const int count = solo ? solo_count : min(chunk, total - from);
+    tile = from + warp * share;
+    left = max(0, min(share, count - warp * share));
+  };
+  constexpr int kPer = 4;
+  if (units <= 32 * kPer) {
+    // every warp for itself: kPer units a lane
+    int n[kPer], mine = 0, most = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int u = lane * kPer + k;
+      n[k] = u < units ? tiles_of<kTile>(p.c, u) : 0;
+      mine += n[k];
+      most = max(most, n[k]);
     }
+    const int incl = warp_prefix(mine, lane);
+    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    most = __reduce_max_sync(0xffffffffu, most);
+    // (first tile and tiles of unit u)
+    auto unit_at = [&](int u, int* count) {
+      int before = incl - mine, c = 0;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        if (k < u % kPer) before += n[k];
+        if (k == u % kPer) c = n[k];
+      }
+      *count = __shfl_sync(0xffffffffu, c, u / kPer);
+      return __shfl_sync(0xffffffffu, before, u / kPer);
+    };
+    const int solo_unit = min(static_cast<int>(blockIdx.x) / p.blocks, units);
+    int solo_count = 0, solo_first = 0;
+    if (solo_unit < units) {
+      solo_first = unit_at(solo_unit, &solo_count) * p.blocks +
+                   (static_cast<int>(blockIdx.x) - solo_unit * p.blocks) * solo_count;
+    }
+    divide(total * p.blocks, most, solo_first, solo_count);
+    // the lane that holds the first tile, then the unit of that lane
+    const unsigned holds = __ballot_sync(0xffffffffu, incl * p.blocks > tile);
+    int before = incl - mine, u = lane * kPer;
+#pragma unroll
+    for (int k = 0; k < kPer - 1; ++k)
+      if (u == lane * kPer + k && (before + n[k]) * p.blocks <= tile) {
+        before += n[k];
+        ++u;
+      }
+    const int src = holds ? __ffs(holds) - 1 : 0;
+    unit0 = __shfl_sync(0xffffffffu, u, src);
+    at = __shfl_sync(0xffffffffu, before, src) * p.blocks;
   } else {
-    const long long from = static_cast<long long>(blockIdx.x) * chunk;
-    if (threadIdx.x == 0) s_count = static_cast<int>(max(0ll, min(static_cast<long long>(chunk), total - from)));
-    // the thread whose units hold the first tile
-    if (from >= before && from < before + mine * p.blocks) {
-      s_from = from;
-      s_unit = u0;
-      s_unit_from = before;
+    const int span = (units + S::kThreads - 1) / S::kThreads;  // units a thread adds up
+    const int u0 = min(static_cast<int>(threadIdx.x) * span, units), u1 = min(u0 + span, units);
+    int mine = 0, most = 0;
+    for (int u = u0; u < u1; ++u) {
+      const int n = tiles_of<kTile>(p.c, u);
+      mine += n;
+      most = max(most, n);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    int incl = warp_prefix(mine, lane);
+    if (lane == 31) {
+      s_sums[warp] = incl;
+      s_most[warp] = most;
+    }
+    if (threadIdx.x == 0) s_at[0] = 0;
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < S::kWarps; ++w) {
+      if (w < warp) incl += s_sums[w];
+      total += s_sums[w];
+      most = max(most, s_most[w]);
+    }
+    const int before = (incl - mine) * p.blocks;
+    // (no more than one unit a thread where a CTA takes a row block)
+    const int u = static_cast<int>(blockIdx.x) / p.blocks;
+    const bool one = units * p.blocks <= ctas;
+    if (one && static_cast<int>(threadIdx.x) == u && u < units) {
+      s_unit[0] = before + (static_cast<int>(blockIdx.x) - u * p.blocks) * mine;
+      s_at[0] = mine;
+    }
+    __syncthreads();
+    divide(total * p.blocks, most, s_unit[0], one ? s_at[0] : 0);
+    __syncthreads();
+    // the thread that holds a warp's first tile
+    const int share = (chunk + S::kWarps - 1) / S::kWarps;
+    const int first = tile - warp * share;
+    for (int w = 0; w < S::kWarps; ++w)
+      if (first + w * share >= before && first + w * share < before + mine * p.blocks) {
+        s_unit[w] = u0;
+        s_at[w] = before;
+      }
+    __syncthreads();
+    if (left > 0) {
+      unit0 = s_unit[warp];
+      at = s_at[warp];
+      int n;
+      while (at + (n = tiles_of<kTile>(p.c, unit0)) * p.blocks <= tile) {
+        at += n * p.blocks;
+        ++unit0;
+      }
     }
   }
-  __syncthreads();
-  const int share = ((solo ? s_count : chunk) + S::kWarps - 1) / S::kWarps;
-  int left = min(share, s_count - warp * share);  // tiles of this warp
-  if (left < 0) left = 0;
-  long long tile = s_from + warp * share;         // the one at hand
   Place c = {};
   if (left > 0) {
-    int u = s_unit, n;
-    long long at = s_unit_from;
-    while (at + static_cast<long long>(n = tiles_of(p.c, u)) * p.blocks <= tile) {
-      at += static_cast<long long>(n) * p.blocks;
-      ++u;
-    }
-    const long long in = tile - at;
-    c.unit = u;
-    c.block = static_cast<int>(in / n);
-    const int slot = static_cast<int>(in - static_cast<long long>(c.block) * n) * kTile;
-    c.row = u * p.c.capacity + slot;
-    c.valid = length_of(p.c, u) - slot;
+    const int len = length_of(p.c, unit0), n = (len + kTile - 1) / kTile;
+    c.unit = unit0;
+    c.block = (tile - at) / n;
+    const int slot = (tile - at - c.block * n) * kTile;
+    c.row = unit0 * p.c.capacity + slot;
+    c.valid = len - slot;
   }
 
   Place ahead = c;
@@ -436,7 +495,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar);
       if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, slots * 4, bar);
     }
-    if (--to_issue > 0) ahead.next(p);
+    if (--to_issue > 0) ahead.template next<S::kTile>(p);
   };
   for (int i = 0; i < S::kStages && to_issue > 0; ++i) issue(i);
 
@@ -495,9 +554,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int slot = lane + 32 * i;
+        w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (slot >= kTile) continue;
         const uint2 kw = lds64(sd + slot * kQ4ParamBytes);
-        w[i] = lds128(sd + kParamTile + slot * kQ4ParamBytes);
-        if (slot >= valid) w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (slot < valid) w[i] = lds128(sd + kParamTile + slot * kQ4ParamBytes);
         sts128(scales + slot * 16,
                make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
                           __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
@@ -545,7 +605,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
         const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
         const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
-        sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
+        if (lane + 32 * i < kTile) sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
                make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632),
                           pack_half2(bf_lo(w[i].z) * f, bf_hi(w[i].z) * f),
                           pack_half2(bf_lo(w[i].w) * f, bf_hi(w[i].w) * f)));
@@ -755,7 +815,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     const int len = done + c.valid;
     ++tile;
     const bool ends = c.valid <= kTile;
-    if (left > 1) c.next(p);
+    if (left > 1) c.template next<S::kTile>(p);
     if (left == 1 || ends) {
       const int count = (len + kTile - 1) / kTile;
       const bool starts = seg_tiles > done / kTile;
@@ -821,7 +881,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     }
   }
   // ---- units that hold nothing
-  for (int u = blockIdx.x + gridDim.x * warp; u < units; u += gridDim.x * S::kWarps)
+  for (int u = blockIdx.x + ctas * warp; u < units; u += ctas * S::kWarps)
     if (length_of(p.c, u) == 0)
       for (int r = 0; r < p.rows; ++r)
         write_row(p, u, r, lane, make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f);
@@ -829,82 +889,103 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   // ---- row blocks that this CTA's warps share: joined in slot order
   __syncthreads();
   if (s_abort) return;
-  __shared__ Part s_shared[2];  // row blocks shared with the CTAs before, behind
-  if (threadIdx.x < 2) s_shared[threadIdx.x].block = -1;
-  __syncthreads();
-  for (int w = -1; w < S::kWarps; ++w) {
-    // a row block's first part here: the first warp's head, or a warp's tail
-    // that is not the one before it
-    const Part& first = w < 0 ? s_head[0] : s_tail[w];
-    const int vu = first.block;
-    if (vu < 0 || (w > 0 && s_tail[w - 1].block == vu)) continue;
-    int end = max(w, 0) + 1;  // tails of warps w .. end - 1, then perhaps a head
-    if (w >= 0)
-      while (end < S::kWarps && s_tail[end].block == vu) ++end;
-    const bool plus = w < 0 || (end < S::kWarps && s_head[end].block == vu);
-    const int tails = w < 0 ? 0 : end - w, head_of = w < 0 ? 0 : end;
-    const bool ends = plus ? s_head[head_of].ends : s_tail[end - 1].ends;
-    const int unit = vu / p.blocks, row0 = (vu - unit * p.blocks) * kRows;
-    const int which = first.starts ? 1 : 0;
-    const bool whole = first.starts && ends;
-    for (int r = warp; r < kRows && row0 + r < p.rows; r += S::kWarps) {
-      float2 hml = make_float2(-INFINITY, 0.f);
-      if (plus) hml = p.head_ml[(blockIdx.x * S::kWarps + head_of) * kRows + r];
-      float top = hml.x;
-      for (int k = 0; k < tails; ++k) top = fmaxf(top, s_ml[w + k][r].x);
-      const float ref0 = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto add = [&](float2 ml, float4 v) {
-        const float f = ex2_approx(ml.x - ref0);
-        sum = fmaf(ml.y, f, sum);
-        acc.x = fmaf(v.x, f, acc.x);
-        acc.y = fmaf(v.y, f, acc.y);
-        acc.z = fmaf(v.z, f, acc.z);
-        acc.w = fmaf(v.w, f, acc.w);
-      };
-      for (int k = 0; k < tails; ++k) {
-        const uint4 v = lds128(base + (w + k) * S::kStages * 2 * kCodeTile + r * (kHeadDim * 4) + lane * 16);
-        add(s_ml[w + k][r], make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z),
-                                        __uint_as_float(v.w)));
-      }
-      if (plus)
-        add(hml, reinterpret_cast<const float4*>(
-                     p.head_o + (static_cast<size_t>(blockIdx.x * S::kWarps + head_of) * kRows + r) * kHeadDim)[lane]);
-      if (whole) {
-        write_row(p, unit, row0 + r, lane, acc, top, sum);
-      } else {
-        const size_t at = static_cast<size_t>(blockIdx.x * 2 + which) * kRows + r;
-        reinterpret_cast<float4*>(p.cta_o + at * kHeadDim)[lane] = acc;
-        if (lane == 0) p.cta_ml[at] = make_float2(top, sum);
+  // Sums weights f of parts 0 .. n - 1 (lane i has the reference and sum of part
+  // i) and returns their common reference.
+  auto weigh = [&](float2 ml, float* f, float* sum) {
+    float top = ml.x;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    *f = ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
+    float x = ml.y * *f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    *sum = x;
+    return top;
+  };
+  auto add = [](float4& acc, float4 v, float f) {
+    acc.x = fmaf(v.x, f, acc.x);
+    acc.y = fmaf(v.y, f, acc.y);
+    acc.z = fmaf(v.z, f, acc.z);
+    acc.w = fmaf(v.w, f, acc.w);
+  };
+  int shared[2] = {-2, -2};  // (-1: the head of the first) warp whose part begins the row block shared with CTAs before, behind
+  {
+    const int tb = lane < S::kWarps ? s_tail[lane].block : -1;
+    const int hb = lane < S::kWarps ? s_head[lane].block : -1;
+    const int prev = __shfl_up_sync(0xffffffffu, tb, 1);
+    // a row block's first part here: the first warp's head, or a tail unlike
+    // the one before it
+    unsigned todo = __ballot_sync(0xffffffffu, tb >= 0 && (lane == 0 || tb != prev)) << 1;
+    if (__shfl_sync(0xffffffffu, hb, 0) >= 0) todo |= 1u;
+    while (todo) {
+      const int w = __ffs(todo) - 2;  // -1: the head
+      todo &= todo - 1;
+      const int vu = __shfl_sync(0xffffffffu, w < 0 ? hb : tb, max(w, 0));
+      const int tails = w < 0 ? 0 : __popc(__ballot_sync(0xffffffffu, tb == vu));
+      const unsigned heads = __ballot_sync(0xffffffffu, hb == vu);
+      const int first = max(w, 0), head = heads ? __ffs(heads) - 1 : -1;
+      const bool starts = w < 0 ? s_head[0].starts : s_tail[first].starts;
+      const bool ends = heads ? s_head[head].ends : s_tail[first + tails - 1].ends;
+      const bool whole = starts && ends;
+      if (!whole) shared[starts] = w;
+      const int unit = vu / p.blocks, row0 = (vu - unit * p.blocks) * kRows;
+      for (int r = warp; r < kRows && row0 + r < p.rows; r += S::kWarps) {
+        const size_t hr = static_cast<size_t>(blockIdx.x * S::kWarps + head) * kRows + r;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        float4 hv = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (lane < tails) ml = s_ml[first + lane][r];
+        if (heads) {
+          if (lane == tails) ml = p.head_ml[hr];
+          hv = reinterpret_cast<const float4*>(p.head_o + hr * kHeadDim)[lane];
+        }
+        float f, sum;
+        const float top = weigh(ml, &f, &sum);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < tails; ++k) {
+          const uint4 v = lds128(base + (first + k) * S::kStages * 2 * kCodeTile + r * (kHeadDim * 4) + lane * 16);
+          add(acc, make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z),
+                               __uint_as_float(v.w)),
+              __shfl_sync(0xffffffffu, f, k));
+        }
+        if (heads) add(acc, hv, __shfl_sync(0xffffffffu, f, tails));
+        if (whole) {
+          write_row(p, unit, row0 + r, lane, acc, top, sum);
+        } else {
+          const size_t to = static_cast<size_t>(blockIdx.x * 2 + starts) * kRows + r;
+          reinterpret_cast<float4*>(p.cta_o + to * kHeadDim)[lane] = acc;
+          if (lane == 0) p.cta_ml[to] = make_float2(top, sum);
+        }
       }
     }
-    if (!whole && threadIdx.x == 0) s_shared[which] = first;
   }
+  if (shared[0] < -1 && shared[1] < -1) return;
 
   // ---- row blocks that CTAs share: the last one to come joins them, in order
-  __threadfence();
+  fence_acq_rel_gpu();
   __syncthreads();
-  if (s_shared[0].block < 0 && s_shared[1].block < 0) return;
   __shared__ int s_last[2];
   if (threadIdx.x < 2) {
-    s_last[threadIdx.x] = 0;
-    const Part part = s_shared[threadIdx.x];
-    if (part.block >= 0) {
-      const int c0 = static_cast<int>(part.first / chunk), c1 = static_cast<int>((part.first + part.count - 1) / chunk);
+    const int w = shared[threadIdx.x];
+    int last = 0;
+    if (w >= -1) {
+      const Part& part = w < 0 ? s_head[0] : s_tail[w];
+      const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
       if (atomicAdd(p.tickets + c0, 1) == c1 - c0) {
         p.tickets[c0] = 0;  // for the next call
-        s_last[threadIdx.x] = 1;
+        last = 1;
       }
+      fence_acq_rel_gpu();
     }
-    __threadfence();
+    s_last[threadIdx.x] = last;
   }
   __syncthreads();
   float4* s_acc = reinterpret_cast<float4*>(smem_raw + (base - smem_u32(smem_raw)));
+#pragma unroll
   for (int which = 0; which < 2; ++which) {
     if (!s_last[which]) continue;
-    const Part part = s_shared[which];
-    const int c0 = static_cast<int>(part.first / chunk), c1 = static_cast<int>((part.first + part.count - 1) / chunk);
+    const Part part = shared[which] < 0 ? s_head[0] : s_tail[shared[which]];
+    const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
     const int unit = part.block / p.blocks, row0 = (part.block - unit * p.blocks) * kRows;
     const int rows = min(kRows, p.rows - row0);
     for (int r0 = 0; r0 < rows; r0 += S::kWarps) {
@@ -914,21 +995,26 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       float top = -INFINITY, sum = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       if (k < split) {
-        auto at = [&](int c) { return static_cast<size_t>(c * 2 + (c == c0)) * kRows + r; };
-        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(&p.cta_ml[at(c)].x));
-#pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ref0 = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
-        for (int c = c0 + k; c <= c1; c += split) {
-          const float2 ml = __ldcg(&p.cta_ml[at(c)]);
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(p.cta_o + at(c) * kHeadDim) + lane);
-          const float f = ex2_approx(ml.x - ref0);
-          sum = fmaf(ml.y, f, sum);
-          acc.x = fmaf(v.x, f, acc.x);
-          acc.y = fmaf(v.y, f, acc.y);
-          acc.z = fmaf(v.z, f, acc.z);
-          acc.w = fmaf(v.w, f, acc.w);
+        // 32 parts at a time
+        for (int c = c0 + k; c <= c1; c += 32 * split) {
+          auto slot = [&](int i) {  // of the warp's i-th part
+            const int x = c + i * split;
+            return static_cast<size_t>(x * 2 + (x == c0)) * kRows + r;
+          };
+          const int n = min(32, (c1 - c) / split + 1);
+          float2 ml = make_float2(-INFINITY, 0.f);
+          if (lane < n) ml = __ldcg(&p.cta_ml[slot(lane)]);
+          float f, s;
+          const float t = weigh(ml, &f, &s);
+          const float both = fmaxf(top, t), ref0 = both == -INFINITY ? 0.f : both;
+          const float old = ex2_approx(top - ref0), now = ex2_approx(t - ref0);
+          sum = fmaf(sum, old, s * now);
+          acc = make_float4(acc.x * old, acc.y * old, acc.z * old, acc.w * old);
+          top = both;
+#pragma unroll 8
+          for (int i = 0; i < n; ++i)
+            add(acc, __ldcg(reinterpret_cast<const float4*>(p.cta_o + slot(i) * kHeadDim) + lane),
+                __shfl_sync(0xffffffffu, f, i) * now);
         }
       }
       __syncthreads();
@@ -936,14 +1022,12 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       if (lane == 0) s_ml[warp][0] = make_float2(top, sum);
       __syncthreads();
       if (k == 0) {
-        for (int i = 1; i < split; ++i) {
-          const float4 v = s_acc[(warp + i * rn) * 32 + lane];
-          sum += s_ml[warp + i * rn][0].y;
-          acc.x += v.x;
-          acc.y += v.y;
-          acc.z += v.z;
-          acc.w += v.w;
-        }
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < split) ml = s_ml[warp + lane * rn][0];
+        float f;
+        top = weigh(ml, &f, &sum);
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < split; ++i) add(acc, s_acc[(warp + i * rn) * 32 + lane], __shfl_sync(0xffffffffu, f, i));
         write_row(p, unit, row0 + r, lane, acc, top, sum);
       }
     }
@@ -978,6 +1062,8 @@ __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int
 constexpr int kWeightThreads = 256;
 
 __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ Q4AttendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
   const int unit = blockIdx.y;
   const int j = blockIdx.x * kWeightThreads + threadIdx.x;
   if (j >= length_of(p.c, unit)) return;
@@ -990,16 +1076,14 @@ __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_co
   p.c.weights[static_cast<long long>(unit) * p.c.capacity + j] += add;
 }
 
-template <int NB>
+template <int NB, bool kPos>
 cudaError_t launch(const Q4AttendParams& p, int sms, cudaStream_t stream) {
-  using S = Shape<NB>;
-  if (p.q_positions) attend_kernel<NB, true><<<sms, S::kThreads, S::kSmem, stream>>>(p);
-  else attend_kernel<NB, false><<<sms, S::kThreads, S::kSmem, stream>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(attend_kernel<NB, kPos>, dim3(sms), Shape<NB>::kThreads, Shape<NB>::kSmem, stream, p);
 }
 
 }  // namespace
 
+int q4_attend_tile(int rows) { return rows <= 8 ? Shape<1>::kTile : Shape<2>::kTile; }
 int q4_attend_warps(int rows) { return rows <= 8 ? Shape<1>::kWarps : Shape<2>::kWarps; }
 
 cudaError_t q4_attend_set_smem_limit() {
@@ -1015,13 +1099,13 @@ cudaError_t q4_attend_set_smem_limit() {
 }
 
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t stream) {
-  return p.rows <= 8 ? launch<1>(p, sms, stream) : launch<2>(p, sms, stream);
+  if (p.rows <= 8) return p.q_positions ? launch<1, true>(p, sms, stream) : launch<1, false>(p, sms, stream);
+  return p.q_positions ? launch<2, true>(p, sms, stream) : launch<2, false>(p, sms, stream);
 }
 
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t stream) {
   const dim3 grid((p.c.capacity + kWeightThreads - 1) / kWeightThreads, p.c.batch * p.c.num_kv_heads);
-  weights_kernel<<<grid, kWeightThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(weights_kernel, grid, kWeightThreads, 0, stream, p);
 }
 
 }  // namespace ckv

@@ -88,6 +88,8 @@ __global__ void __launch_bounds__(kThreads, kHold == kShortItems ? 6 : 1) evict_
   __shared__ int s_ties[kWarps], s_holes[kWarps], s_rows[kWarps];
   const uint32_t ranks = kCluster ? p.cluster : 1, rank = kCluster ? cluster_rank() : 0;
   const int unit = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_launch_dependents();
   const long long base = static_cast<long long>(unit) * p.c.capacity;
   const int32_t* pos = p.c.positions + base;
   const float* wt = p.c.weights + base;
@@ -386,11 +388,13 @@ cudaError_t launch(const Q4EvictParams& p, cudaStream_t stream) {
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kCluster ? 0 : kThreads * kHold * sizeof(int32_t);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {static_cast<unsigned>(p.cluster), 1, 1};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {static_cast<unsigned>(p.cluster), 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = kCluster ? 1 : 0;
+  cfg.numAttrs = kCluster ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, evict_kernel<kThreads, kHold, kCluster>, p);
 }
 

@@ -4,7 +4,7 @@
 #pragma once
 
 #include <cstdint>
-#include <vector_types.h>
+#include <cuda_runtime.h>
 
 #include "ckv_params.h"
 
@@ -15,7 +15,6 @@ constexpr int kQ4Groups = kHeadDim / kQ4GroupDim;       // 4
 constexpr int kQ4CodeBytes = kHeadDim / 2;              // codes of one K or V row
 constexpr int kQ4ParamBytes = 4 * kQ4Groups;            // 4 bf16 scales, 4 bf16 minima
 constexpr int kQ4SlotStep = 32;                         // capacity is a multiple of this
-constexpr int kQ4TileSlots = 64;                        // slots of a tile of the attention
 constexpr int kQ4MaxUnits = 65535;                      // (sequence, KV group) pairs of a cache
 constexpr int kQ4MaxQueries = 16;                       // query tokens a sequence and call
 constexpr int kQ4MaxCtas = 160;                         // of the attention
@@ -57,7 +56,7 @@ using Q4AppendParams = Q4WriteParams<0>;
 using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
 using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
-// Attention.  The tiles (64 slots) of all row blocks -- up to 16 query rows of
+// Attention.  The tiles (48 or 64 slots) of all row blocks -- up to 16 query rows of
 // a unit -- form one sequence, of which every CTA takes an equal run, and every
 // warp of it a run of that.  Where there are few short row blocks, a CTA takes
 // one each instead.
@@ -93,11 +92,30 @@ struct Q4EvictParams {
   int* status;
 };
 
+// Launches a kernel that may be brought up while the one before it in the
+// stream ends (its first act is then to wait for that one's results).
+template <class... A>
+cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t stream,
+                             const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherUnitParams& p, cudaStream_t s);
 constexpr int q4_block_rows(int rows) { return rows <= 8 ? 8 : 16; }
-int q4_attend_warps(int rows);  // of a CTA; there is one an SM
+int q4_attend_tile(int rows);   // slots of a tile, for so many query rows a unit
+int q4_attend_warps(int rows);  // warps of a CTA; there is one an SM
 cudaError_t q4_attend_set_smem_limit();
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t s);
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);

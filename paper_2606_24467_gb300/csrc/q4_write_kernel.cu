@@ -219,6 +219,8 @@ __device__ __forceinline__ void set_length(const Q4AppendParams& p, int unit, in
 // known where it goes.
 template <bool kBf16>
 __global__ void __launch_bounds__(kWriteThreads) append_unit_kernel(const __grid_constant__ Q4AppendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
   const int unit = blockIdx.x;
   const int s = unit / p.c.num_kv_heads, g = unit - s * p.c.num_kv_heads;
   const int2 r = rows_of(p, s);
@@ -286,6 +288,7 @@ __device__ __forceinline__ void move_rows(const Q4WriteParams<kTable>& p, const 
 // follow in a launch of their own.
 template <bool kBf16, int kTasks>
 __global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __grid_constant__ Q4AppendParams p) {
+  pdl_wait();
   pdl_launch_dependents();
   const int H = p.c.num_kv_heads;
   // (the host bounds the tasks by 2^31 - 1, and the slots)
@@ -317,6 +320,8 @@ __global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __g
 
 // A CTA a sequence: the first of its rows with a negative position.
 __global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __grid_constant__ Q4AppendParams p) {
+  pdl_wait();  // the rows' kernel has read the lengths
+  pdl_launch_dependents();
   __shared__ int s_used;
   const int s = blockIdx.x, H = p.c.num_kv_heads;
   const int2 r = rows_of(p, s);
@@ -328,7 +333,6 @@ __global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __g
     if (p.positions[r.x + i] < 0) used = min(used, i);
   if (used < r.y) atomicMin(&s_used, used);
   __syncthreads();
-  pdl_wait();  // the rows' kernel has read the lengths
   for (int g = threadIdx.x; g < H; g += kWriteThreads)
     set_length(p, s * H + g, first_slot(p, s * H + g), s_used);
 }
@@ -337,6 +341,8 @@ __global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __g
 // write the units' lengths.
 template <bool kBf16, int kTasks, class P>
 __global__ void __launch_bounds__(kWriteThreads, 4) gather_q4_kernel(const __grid_constant__ P p) {
+  pdl_wait();
+  pdl_launch_dependents();
   const int H = p.c.num_kv_heads, B = p.c.batch, lane = threadIdx.x & 31;
   const unsigned tasks = p.group_major ? p.rows : static_cast<unsigned>(p.rows) * H;
   const unsigned warps = (tasks + kTasks - 1) / kTasks;
@@ -390,8 +396,8 @@ cudaError_t launch_gather_rows(const P& p, long long tasks, cudaStream_t stream)
   const long long units = static_cast<long long>(p.c.batch) * p.c.num_kv_heads;
   const long long warps = (tasks + kTasks - 1) / kTasks + (units + 31) / 32;
   constexpr int kPer = kWriteThreads / 32;
-  gather_q4_kernel<kBf16, kTasks, P><<<static_cast<unsigned>((warps + kPer - 1) / kPer), kWriteThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(gather_q4_kernel<kBf16, kTasks, P>, dim3(static_cast<unsigned>((warps + kPer - 1) / kPer)),
+                          kWriteThreads, 0, stream, p);
 }
 template <class P>
 cudaError_t launch_gather_any(const P& p, cudaStream_t stream) {
@@ -405,9 +411,8 @@ cudaError_t launch_gather_any(const P& p, cudaStream_t stream) {
 template <bool kBf16, int kTasks>
 cudaError_t launch_append_rows(const Q4AppendParams& p, long long tasks, cudaStream_t stream) {
   constexpr long long kPer = static_cast<long long>(kWriteThreads / 32) * kTasks;
-  append_rows_kernel<kBf16, kTasks>
-      <<<static_cast<unsigned>((tasks + kPer - 1) / kPer), kWriteThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(append_rows_kernel<kBf16, kTasks>, dim3(static_cast<unsigned>((tasks + kPer - 1) / kPer)),
+                          kWriteThreads, 0, stream, p);
 }
 
 }  // namespace
@@ -417,9 +422,8 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t
   if (max_rows <= kSmallRows) {
     constexpr int kMost = kWriteThreads / 32;
     const int warps = max_rows < 1 ? 1 : max_rows < kMost ? max_rows : kMost;
-    if (p.is_bf16) append_unit_kernel<true><<<units, warps * 32, 0, stream>>>(p);
-    else append_unit_kernel<false><<<units, warps * 32, 0, stream>>>(p);
-    return cudaGetLastError();
+    return launch_dependent(p.is_bf16 ? append_unit_kernel<true> : append_unit_kernel<false>, dim3(units), warps * 32,
+                            0, stream, p);
   }
   const long long tasks = static_cast<long long>(p.rows) * p.c.num_kv_heads;
   cudaError_t e;
@@ -428,16 +432,7 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t
   else
     e = p.is_bf16 ? launch_append_rows<true, kMostTasks>(p, tasks, stream) : launch_append_rows<false, kMostTasks>(p, tasks, stream);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.c.batch);
-  cfg.blockDim = dim3(kWriteThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, append_lengths_kernel, p);
+  return launch_dependent(append_lengths_kernel, dim3(p.c.batch), kWriteThreads, 0, stream, p);
 }
 
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t stream) {
