@@ -627,10 +627,10 @@ def _q4_call(name: str, cache: Q4Cache, stream, *args):
         _invalid("the cache must be in device memory")
     fn = _fast(name)
     if dev.index == torch.cuda.current_device():
-        _check(fn(cache.addr, *args, _raw_stream(stream)), name)
+        _check(fn(*args, _raw_stream(stream)), name)
     else:
         with torch.cuda.device(dev):
-            _check(fn(cache.addr, *args, _raw_stream(stream)), name)
+            _check(fn(*args, _raw_stream(stream)), name)
 
 
 def _q4_on_device(cache: Q4Cache, what: str, *tensors):
@@ -640,22 +640,22 @@ def _q4_on_device(cache: Q4Cache, what: str, *tensors):
 
 
 def _q4_rows(cache: Q4Cache, k, v):
-    if k.dim() != 3 or tuple(k.shape[1:]) != (cache.num_kv_heads, 128) or v.shape != k.shape:
+    """(dtype, shape, strides) of the rows."""
+    shape, strides = k.shape, k.stride()
+    if len(shape) != 3 or shape[1] != cache.num_kv_heads or shape[2] != 128 or v.shape != shape:
         _invalid("k and v must be [rows, H_kv, 128]")
-    if v.dtype != k.dtype or k.stride(2) != 1 or v.stride() != k.stride():
+    if v.dtype != k.dtype or strides[2] != 1 or v.stride() != strides:
         _invalid("k and v must share their dtype and strides, head_dim contiguous")
-    return _q4_dtype(k)
+    return _q4_dtype(k), shape, strides
 
 
 def _q4_values(t, like, shape, what):
-    if t is not None and (t.dtype != like.dtype or tuple(t.shape) != tuple(shape)
-                          or not t.is_contiguous()):
+    if t is not None and (t.dtype != like.dtype or t.shape != shape or not t.is_contiguous()):
         _invalid(f"{what} must be contiguous {tuple(shape)} in the rows' dtype")
 
 
 def _q4_i32(cache, t, shape, what):
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != tuple(shape)
-                          or not t.is_contiguous()):
+    if t is not None and (t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous()):
         _invalid(f"{what} must be a contiguous int32 tensor {tuple(shape)}")
 
 
@@ -689,15 +689,15 @@ def q4_append(cache: Q4Cache, k, v, positions, cu_rows=None, start=None, k_value
     behind a sequence's rows), ``start`` int32 ``[B, H_kv]`` (default: the
     cache's lengths); ``k_values`` / ``v_values`` receive what the codes stand
     for."""
-    dtype = _q4_rows(cache, k, v)
-    rows = k.shape[0]
+    dtype, shape, strides = _q4_rows(cache, k, v)
+    rows = shape[0]
     _q4_i32(cache, positions, (rows,), "positions")
     _q4_i32(cache, start, (cache.batch, cache.num_kv_heads), "start")
     _q4_i32(cache, device_status, (1,), "device_status")
-    _q4_values(k_values, k, k.shape, "k_values")
-    _q4_values(v_values, k, k.shape, "v_values")
-    r = CkvQ4Rows(dtype, 0, None, k.stride(0) if rows > 1 else cache.num_kv_heads * 128,
-                  k.stride(1) if cache.num_kv_heads > 1 else 128)
+    _q4_values(k_values, k, shape, "k_values")
+    _q4_values(v_values, k, shape, "v_values")
+    r = CkvQ4Rows(dtype, 0, None, strides[0] if rows > 1 else cache.num_kv_heads * 128,
+                  strides[1] if cache.num_kv_heads > 1 else 128)
     if cu_rows is None:
         if rows % cache.batch:
             _invalid("the rows do not divide by the sequences: give cu_rows")
@@ -709,7 +709,7 @@ def q4_append(cache: Q4Cache, k, v, positions, cu_rows=None, start=None, k_value
         r.cu_rows = _data(cu)
     _q4_on_device(cache, "k, positions, start, values and status", k, positions, start, k_values,
                   v_values, device_status)
-    _q4_call("compresskv_q4_append", cache, stream, ctypes.addressof(r), _addr(k), _addr(v),
+    _q4_call("compresskv_q4_append", cache, stream, cache.addr, ctypes.addressof(r), _addr(k), _addr(v),
              _addr(positions), _addr(start), _addr(k_values), _addr(v_values),
              _addr(device_status))
 
@@ -721,11 +721,11 @@ def q4_gather(problem: Problem, cache: Q4Cache, indices, cu_out, k, v, raw=None,
     them (``[H_kv, rows]``, ``[B+1]``), or as compress_layer_head_budgets does
     (``[rows]``, ``[H_kv, B+1]``); ``raw``: the raw scores become the rows' first
     weights; ``k_values`` / ``v_values`` as k_out / v_out of the compression."""
-    dtype = _q4_rows(cache, k, v)
+    dtype, shape, strides = _q4_rows(cache, k, v)
     s = problem.struct
     if (s.batch != cache.batch or s.num_kv_heads != cache.num_kv_heads or s.dtype != dtype
-            or s.kv_token_stride != k.stride(0) or s.kv_head_stride != k.stride(1)
-            or k.shape[0] < int(problem._cu[-1])):
+            or s.kv_token_stride != strides[0] or s.kv_head_stride != strides[1]
+            or shape[0] < int(problem._cu[-1])):
         _invalid("k, v and the cache must be those of the problem")
     cu = _host_i32(cu_out)
     H, B = cache.num_kv_heads, cache.batch
@@ -737,19 +737,15 @@ def q4_gather(problem: Problem, cache: Q4Cache, indices, cu_out, k, v, raw=None,
     shape = (rows, 128) if group_major else (rows, H, 128)
     _q4_values(k_values, k, shape, "k_values")
     _q4_values(v_values, k, shape, "v_values")
-    n = int(np.maximum(np.diff(problem._cu) - s.window, 0).sum())
-    if raw is not None and (raw.dtype != torch.float32 or tuple(raw.shape) != (H, n)
-                            or not raw.is_contiguous()):
-        _invalid(f"raw must be a contiguous float32 tensor {(H, n)}")
+    if raw is not None:
+        n = int(np.maximum(np.diff(problem._cu) - s.window, 0).sum())
+        if raw.dtype != torch.float32 or tuple(raw.shape) != (H, n) or not raw.is_contiguous():
+            _invalid(f"raw must be a contiguous float32 tensor {(H, n)}")
     _q4_on_device(cache, "k, indices, raw, values and workspace", k, indices, raw, k_values,
                   v_values, ws)
-    if cache.device.type != "cuda":
-        _invalid("the cache must be in device memory")
-    fn = _fast("compresskv_q4_gather")
-    with torch.cuda.device(cache.device):
-        _check(fn(problem.addr, cache.addr, int(group_major), _addr(indices), _data(cu), _addr(k),
-                  _addr(v), _addr(raw), _addr(k_values), _addr(v_values), _addr(ws),
-                  _raw_stream(stream)), "compresskv_q4_gather")
+    _q4_call("compresskv_q4_gather", cache, stream, problem.addr, cache.addr, int(group_major),
+             _addr(indices), _data(cu), _addr(k), _addr(v), _addr(raw), _addr(k_values),
+             _addr(v_values), _addr(ws))
 
 
 def q4_attend(cache: Q4Cache, q, out, ws, q_positions=None, scale: float = 0.0, lse=None,
@@ -776,7 +772,7 @@ def q4_attend(cache: Q4Cache, q, out, ws, q_positions=None, scale: float = 0.0, 
                      *(128 if one[i] else qs[i] for i in range(3)),
                      *(128 if one[i] else os_[i] for i in range(3)))
     _q4_on_device(cache, "q, out, q_positions, lse and workspace", q, out, q_positions, lse, ws)
-    _q4_call("compresskv_q4_attend", cache, stream, ctypes.addressof(a), _addr(q),
+    _q4_call("compresskv_q4_attend", cache, stream, cache.addr, ctypes.addressof(a), _addr(q),
              _addr(q_positions), _addr(out), _addr(lse), _addr(ws), ws.numel())
 
 
@@ -789,5 +785,5 @@ def q4_evict(cache: Q4Cache, budget, ws, sinks: int = 0, recent: int = 0, stream
         budgets, budget = budget, 0
         _q4_i32(cache, budgets, (cache.batch, cache.num_kv_heads), "budget")
     _q4_on_device(cache, "budget and workspace", budgets, ws)
-    _q4_call("compresskv_q4_evict", cache, stream, int(budget), _addr(budgets), int(sinks),
+    _q4_call("compresskv_q4_evict", cache, stream, cache.addr, int(budget), _addr(budgets), int(sinks),
              int(recent), _addr(ws), ws.numel())

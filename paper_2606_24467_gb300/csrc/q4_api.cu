@@ -83,7 +83,7 @@ AttendArea attend_area(const ckv_q4_cache* c, int num_q_heads, int num_queries, 
   a.cta_o = a.cta_ml + align256(ctas * sizeof(float2));
   a.lse = a.cta_o + align256(ctas * kHeadDim * sizeof(float));
   a.z = a.lse + align256(units_of(c) * rows * sizeof(float));
-  a.bytes = a.z + (accumulate ? align256(units_of(c) * rows * c->capacity * sizeof(float)) : 0);
+  a.bytes = a.z + (accumulate ? align256(units_of(c) * (rows + rows % 2) * c->capacity * sizeof(float)) : 0);
   return a;
 }
 size_t evict_bytes(const ckv_q4_cache* c) {
@@ -313,6 +313,7 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.cta_o = reinterpret_cast<float*>(ws + area.cta_o);
   P.lse_ws = reinterpret_cast<float*>(ws + area.lse);
   P.z = reinterpret_cast<float*>(ws + area.z);
+  P.z_stride = P.rows + P.rows % 2;
   Tracer tr{c->trace, st};
   rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_attend(P, sms, st); });
   if (rc != CKV_OK || !P.accumulate) return rc;

@@ -49,8 +49,8 @@ namespace ckv {
 namespace {
 
 #ifndef Q4W1
-#define Q4T1 48
-#define Q4W1 12
+#define Q4T1 64
+#define Q4W1 8
 #define Q4S1 2
 #define Q4T2 64
 #define Q4W2 8
@@ -86,7 +86,8 @@ struct Shape {
   static constexpr int kSide = kWarps * kStages * kSideBytes;
   static constexpr int kScales = kWarps * kScaleTile;
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
-  static_assert(kTile % 16 == 0 && kTile > 32 && kTile <= 64, "two slots a lane");
+  static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
+  static_assert(kTile % 16 == 0, "steps");
   static_assert(kCodeTile % 512 == 0, "swizzle");
   static_assert(kStages * 2 * kCodeTile >= 8 * NB * kHeadDim * 4, "a warp's outputs fit its stages");
 };
@@ -168,18 +169,26 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
 }
-__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row) {
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row,
+                                         uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
-      "[%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(row)
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], "
+      "[%1, {%3, %4}], [%2], %5;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(row), "l"(policy)
       : "memory");
 }
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar,
+                                          uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(bar)
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
+          dst),
+      "l"(src), "r"(bytes), "r"(bar), "l"(policy)
       : "memory");
+}
+__device__ __forceinline__ uint64_t l2_policy_normal() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
 
 __device__ __forceinline__ int length_of(const Q4Cache& c, int unit) {
@@ -259,35 +268,32 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = block * (8 * NB) + nb * 8 + g;
-    float x[4][8];
-    uint32_t top = 0;
+    uint4 raw[4];
     int limit = 0x7fffffff;
+    uint32_t abs2 = 0;  // largest magnitudes of the low and of the high halves
     if (r < p.rows) {
       const int h = kv * p.group + r / p.num_queries, qi = r % p.num_queries;
       const uint16_t* src = p.q + b * p.q_bs + h * p.q_hs + qi * p.q_qs + 8 * t;
       if (p.q_positions) limit = __ldg(p.q_positions + b * p.num_queries + qi);
 #pragma unroll
-      for (int J = 0; J < 4; ++J) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + 32 * J));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[J][i] = to_float(i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xffffu, bf16);
-          top = max(top, __float_as_uint(x[J][i]) & 0x7fffffffu);
-        }
-      }
+      for (int J = 0; J < 4; ++J) raw[J] = __ldg(reinterpret_cast<const uint4*>(src + 32 * J));
     } else {
 #pragma unroll
-      for (int J = 0; J < 4; ++J)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[J][i] = 0.f;
+      for (int J = 0; J < 4; ++J) raw[J] = make_uint4(0u, 0u, 0u, 0u);
     }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+#pragma unroll
+    for (int J = 0; J < 4; ++J) {
+      // (magnitudes compare like their bits, NaN above all)
+      abs2 = __vmaxu2(abs2, __vmaxu2(raw[J].x & 0x7fff7fffu, raw[J].y & 0x7fff7fffu));
+      abs2 = __vmaxu2(abs2, __vmaxu2(raw[J].z & 0x7fff7fffu, raw[J].w & 0x7fff7fffu));
+    }
+    abs2 = __vmaxu2(abs2, __shfl_xor_sync(0xffffffffu, abs2, 1));
+    abs2 = __vmaxu2(abs2, __shfl_xor_sync(0xffffffffu, abs2, 2));
+    const uint32_t top = __float_as_uint(to_float(max(abs2 & 0xffffu, abs2 >> 16), bf16));
     // exponent of the largest element; a row of zeros, NaN or infinities as it is
     int e = top >= 0x7f800000u || top == 0 ? 14 : static_cast<int>(top >> 23) - 127;
     e = max(e, -110);  // smaller rows (bf16) scale by no more than 2^124
-    const float up = pow2(14 - e);
+    const float up = pow2(14 - e), up16 = up * 0.0625f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       Q.f2[nb][j] = __shfl_sync(0xffffffffu, pow2(e), 8 * t + 4 * j);
@@ -296,21 +302,22 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
     float part[4];
 #pragma unroll
     for (int J = 0; J < 4; ++J) {
-      part[J] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[J][i] *= up;
-        part[J] += x[J][i];
-      }
-      part[J] += __shfl_xor_sync(0xffffffffu, part[J], 1);
-      part[J] += __shfl_xor_sync(0xffffffffu, part[J], 2);
-      part[J] *= 5.9604644775390625e-8f * f1;  // 2^-24
+      const uint32_t w[4] = {raw[J].x, raw[J].y, raw[J].z, raw[J].w};
+      float even = 0.f, odd = 0.f;
       // nibbles (0, 4), (1, 5), (2, 6), (3, 7) of a word; the odd ones count 16-fold
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        Q.b[nb][2 * J + st][0] = pack_half2(x[J][2 * st], x[J][2 * st + 4]);
-        Q.b[nb][2 * J + st][1] = pack_half2(x[J][2 * st + 1] * 0.0625f, x[J][2 * st + 5] * 0.0625f);
+        const float a0 = to_float(w[st] & 0xffffu, bf16) * up, a1 = to_float(w[st + 2] & 0xffffu, bf16) * up;
+        const float b0 = to_float(w[st] >> 16, bf16) * up16, b1 = to_float(w[st + 2] >> 16, bf16) * up16;
+        Q.b[nb][2 * J + st][0] = pack_half2(a0, a1);
+        Q.b[nb][2 * J + st][1] = pack_half2(b0, b1);
+        even += a0 + a1;
+        odd += b0 + b1;
       }
+      part[J] = fmaf(odd, 16.0f, even);
+      part[J] += __shfl_xor_sync(0xffffffffu, part[J], 1);
+      part[J] += __shfl_xor_sync(0xffffffffu, part[J], 2);
+      part[J] *= 5.9604644775390625e-8f * f1;  // 2^-24
     }
     // k index J + 4 * part: this lane's pairs are groups 2 (t & 1), 2 (t & 1) + 1
     const float s0 = t & 1 ? part[2] : part[0], s1 = t & 1 ? part[3] : part[1];
@@ -330,7 +337,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   constexpr int kRows = 8 * NB;
   constexpr int kTile = S::kTile, kSteps = S::kSteps;
   constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
-  constexpr int kScaleTile = S::kScaleTile;
+  constexpr int kScaleTile = S::kScaleTile, kLane = S::kLane;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_sums[S::kWarps], s_most[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
   __shared__ float2 s_ml[S::kWarps][kRows];
@@ -479,6 +486,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     c.valid = len - slot;
   }
 
+  // logits that are read again stay in L2 in preference to the cache's rows
+  const uint64_t policy = p.accumulate ? l2_policy_evict_first() : l2_policy_normal();
   Place ahead = c;
   int to_issue = left;
   auto issue = [&](int stage) {
@@ -488,12 +497,12 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       // (or zeros, behind the last one) then come along and count nothing
       const int slots = min(kTile, (ahead.unit + 1) * p.c.capacity - ahead.row);
       mbar_arrive_expect_tx(bar, 2 * kCodeTile + slots * (2 * kQ4ParamBytes + (kPos ? 4 : 0)));
-      tma_rows(cd, &p.map_k, bar, ahead.row);
-      tma_rows(cd + kCodeTile, &p.map_v, bar, ahead.row);
+      tma_rows(cd, &p.map_k, bar, ahead.row, policy);
+      tma_rows(cd + kCodeTile, &p.map_v, bar, ahead.row, policy);
       const size_t row = static_cast<size_t>(ahead.row);
-      bulk_copy(sd, p.c.params[0] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar);
-      bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar);
-      if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, slots * 4, bar);
+      bulk_copy(sd, p.c.params[0] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar, policy);
+      bulk_copy(sd + kParamTile, p.c.params[1] + row * kQ4ParamBytes, slots * kQ4ParamBytes, bar, policy);
+      if (kPos) bulk_copy(sd + 2 * kParamTile, p.c.positions + row, slots * 4, bar, policy);
     }
     if (--to_issue > 0) ahead.template next<S::kTile>(p);
   };
@@ -545,14 +554,14 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     const uint32_t cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
     const int valid = c.valid;
 
-    // ---- scales: two slots a lane.  Slots behind the length and groups that
+    // ---- scales: one or two slots a lane.  Slots behind the length and groups that
     // hold a NaN count nothing in V's products
-    uint32_t nan_groups[2] = {0u, 0u};  // of this lane's slots
+    uint32_t nan_groups[kLane] = {};  // of this lane's slots
     bool special;
     {
-      uint4 w[2];
+      uint4 w[kLane];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kLane; ++i) {
         const int slot = lane + 32 * i;
         w[i] = make_uint4(0u, 0u, 0u, 0u);
         if (slot >= kTile) continue;
@@ -562,11 +571,15 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
                make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
                           __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
       }
-      uint32_t all = __reduce_max_sync(0xffffffffu, max(top_of(w[0]), top_of(w[1])));
+      uint32_t all = 0;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) all = max(all, top_of(w[i]));
+      all = __reduce_max_sync(0xffffffffu, all);
       special = all >= 0x7f800000u;
       if (special) {
+        all = 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kLane; ++i) {
           uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
           for (int J = 0; J < 4; ++J) {
@@ -578,8 +591,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             }
           }
           w[i] = make_uint4(x[0], x[1], x[2], x[3]);
+          all = max(all, top_of(w[i]));
         }
-        all = min(__reduce_max_sync(0xffffffffu, max(top_of(w[0]), top_of(w[1]))), 0x7f000000u);
+        all = min(__reduce_max_sync(0xffffffffu, all), 0x7f000000u);
       }
       const int k = max(static_cast<int>(all >> 23) - 127, kMinScaleExp);
       if (k > vexp) {  // the sums go to the new power of two
@@ -599,7 +613,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
       const float f = pow2(kTopExp - vexp);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kLane; ++i) {
         const uint32_t s01 = pack_half2(bf_lo(w[i].x) * f, bf_hi(w[i].x) * f);
         const uint32_t s23 = pack_half2(bf_lo(w[i].y) * f, bf_hi(w[i].y) * f);
         // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
@@ -671,21 +685,20 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             for (int nb = 0; nb < NB; ++nb) z[nb][h][i] = -INFINITY;
     }
     if (p.accumulate) {
+      // [slot][rows]: a lane's two rows are neighbours.  (Behind the length
+      // there may be the next unit.)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb) {
+        const int r = c.block * kRows + nb * 8 + 2 * t;
+        float* zp = p.z + static_cast<size_t>(c.row + g) * p.z_stride + r;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = c.block * (8 * NB) + nb * 8 + 2 * t + j;
-          if (r < p.rows) {
-            float* zp = p.z + (static_cast<long long>(c.unit) * (p.rows - 1) + r) * p.c.capacity + c.row + g;
+        for (int h = 0; h < kSteps; ++h)
 #pragma unroll
-            for (int h = 0; h < kSteps; ++h) {
-              // (behind the length there may be the next row)
-              if (h * 16 + g < valid) zp[h * 16] = z[nb][h][j] * Q.f2[nb][j];
-              if (h * 16 + 8 + g < valid) zp[h * 16 + 8] = z[nb][h][2 + j] * Q.f2[nb][j];
-            }
-          }
-        }
+          for (int i = 0; i < 2; ++i)
+            if (r < p.rows && h * 16 + 8 * i + g < valid)
+              *reinterpret_cast<float2*>(zp + (h * 16 + 8 * i) * p.z_stride) =
+                  make_float2(z[nb][h][2 * i] * Q.f2[nb][0], z[nb][h][2 * i + 1] * Q.f2[nb][1]);
+      }
     }
 
     // ---- references, probabilities (in place of z)
@@ -980,56 +993,69 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     s_last[threadIdx.x] = last;
   }
   __syncthreads();
+  // The parts of a row are summed by several warps where there are fewer rows,
+  // of both row blocks at once.
+  const int both = s_last[0] + s_last[1];
+  if (both == 0) return;
   float4* s_acc = reinterpret_cast<float4*>(smem_raw + (base - smem_u32(smem_raw)));
+  const int which = both == 2 ? warp & 1 : s_last[1];
+  const int warps = S::kWarps / both, mine = warp / both;
+  const Part part = shared[which] < 0 ? s_head[0] : s_tail[shared[which]];
+  const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
+  const int unit = part.block / p.blocks, row0 = (part.block - unit * p.blocks) * kRows;
+  const int rows = min(kRows, p.rows - row0);
+  // (rounds as many as the row block with more rows takes: every warp is at
+  // every barrier)
+  const int rounds = (min(kRows, p.rows) + warps - 1) / warps;
+  for (int round = 0; round < rounds; ++round) {
+    const int r0 = round * warps, rn = max(1, min(rows - r0, warps)), split = warps / rn;
+    const int r = r0 + mine % rn, k = mine / rn;
+    float top = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows && k < split) {
+      constexpr int kBatch = 8;
+      for (int c = c0 + k; c <= c1; c += kBatch * split) {
+        float2 ml[kBatch];
+        float4 v[kBatch];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    if (!s_last[which]) continue;
-    const Part part = shared[which] < 0 ? s_head[0] : s_tail[shared[which]];
-    const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
-    const int unit = part.block / p.blocks, row0 = (part.block - unit * p.blocks) * kRows;
-    const int rows = min(kRows, p.rows - row0);
-    for (int r0 = 0; r0 < rows; r0 += S::kWarps) {
-      // several warps a row where there are fewer rows
-      const int rn = min(rows - r0, S::kWarps), split = S::kWarps / rn;
-      const int r = r0 + warp % rn, k = warp / rn;
-      float top = -INFINITY, sum = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (k < split) {
-        // 32 parts at a time
-        for (int c = c0 + k; c <= c1; c += 32 * split) {
-          auto slot = [&](int i) {  // of the warp's i-th part
-            const int x = c + i * split;
-            return static_cast<size_t>(x * 2 + (x == c0)) * kRows + r;
-          };
-          const int n = min(32, (c1 - c) / split + 1);
-          float2 ml = make_float2(-INFINITY, 0.f);
-          if (lane < n) ml = __ldcg(&p.cta_ml[slot(lane)]);
-          float f, s;
-          const float t = weigh(ml, &f, &s);
-          const float both = fmaxf(top, t), ref0 = both == -INFINITY ? 0.f : both;
-          const float old = ex2_approx(top - ref0), now = ex2_approx(t - ref0);
-          sum = fmaf(sum, old, s * now);
-          acc = make_float4(acc.x * old, acc.y * old, acc.z * old, acc.w * old);
-          top = both;
-#pragma unroll 8
-          for (int i = 0; i < n; ++i)
-            add(acc, __ldcg(reinterpret_cast<const float4*>(p.cta_o + slot(i) * kHeadDim) + lane),
-                __shfl_sync(0xffffffffu, f, i) * now);
+        for (int i = 0; i < kBatch; ++i) {
+          const int x = c + i * split;
+          ml[i] = make_float2(-INFINITY, 0.f);
+          v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (x <= c1) {
+            const size_t from = static_cast<size_t>(x * 2 + (x == c0)) * kRows + r;
+            ml[i] = __ldcg(&p.cta_ml[from]);
+            v[i] = __ldcg(reinterpret_cast<const float4*>(p.cta_o + from * kHeadDim) + lane);
+          }
+        }
+        float t = top;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) t = fmaxf(t, ml[i].x);
+        const float ref0 = t == -INFINITY ? 0.f : t, old = ex2_approx(top - ref0);
+        sum *= old;
+        acc = make_float4(acc.x * old, acc.y * old, acc.z * old, acc.w * old);
+        top = t;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float f = ex2_approx(ml[i].x - ref0);
+          sum = fmaf(ml[i].y, f, sum);
+          add(acc, v[i], f);
         }
       }
-      __syncthreads();
-      s_acc[warp * 32 + lane] = acc;
-      if (lane == 0) s_ml[warp][0] = make_float2(top, sum);
-      __syncthreads();
-      if (k == 0) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (lane < split) ml = s_ml[warp + lane * rn][0];
-        float f;
-        top = weigh(ml, &f, &sum);
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = 0; i < split; ++i) add(acc, s_acc[(warp + i * rn) * 32 + lane], __shfl_sync(0xffffffffu, f, i));
-        write_row(p, unit, row0 + r, lane, acc, top, sum);
-      }
+    }
+    __syncthreads();
+    s_acc[warp * 32 + lane] = acc;
+    if (lane == 0) s_ml[warp][0] = make_float2(top, sum);
+    __syncthreads();
+    if (r < rows && k == 0) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < split) ml = s_ml[warp + lane * rn * both][0];
+      float f;
+      top = weigh(ml, &f, &sum);
+      acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < split; ++i)
+        add(acc, s_acc[(warp + i * rn * both) * 32 + lane], __shfl_sync(0xffffffffu, f, i));
+      write_row(p, unit, row0 + r, lane, acc, top, sum);
     }
   }
 }
@@ -1059,21 +1085,31 @@ __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int
 }
 
 // ---------------------------------------------------------------- weights
+// A thread takes a slot: its logits lie side by side.
 constexpr int kWeightThreads = 256;
 
 __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ Q4AttendParams p) {
+  __shared__ float s_lse[kMaxQRows];
   pdl_wait();
   pdl_launch_dependents();
-  const int unit = blockIdx.y;
+  const int unit = blockIdx.y, len = length_of(p.c, unit);
+  if (static_cast<int>(blockIdx.x) * kWeightThreads >= len) return;
+  for (int r = threadIdx.x; r < p.rows; r += kWeightThreads)
+    s_lse[r] = p.lse_ws[static_cast<long long>(unit) * p.rows + r];
+  __syncthreads();
   const int j = blockIdx.x * kWeightThreads + threadIdx.x;
-  if (j >= length_of(p.c, unit)) return;
+  if (j >= len) return;
+  const size_t slot = static_cast<size_t>(unit) * p.c.capacity + j;
+  const float2* z = reinterpret_cast<const float2*>(p.z + slot * p.z_stride);
+  // (a slot that a row does not see has -inf, and such a row may have no sum)
+  auto of = [&](float x, int r) { return r < p.rows && x != -INFINITY ? ex2_approx(x - s_lse[r]) : 0.f; };
   float add = 0.f;
-  for (int r = 0; r < p.rows; ++r) {
-    const long long row = static_cast<long long>(unit) * p.rows + r;
-    const float z = p.z[row * p.c.capacity + j];
-    if (z != -INFINITY) add += ex2_approx(z - p.lse_ws[row]);
+#pragma unroll 4
+  for (int r = 0; r < p.rows; r += 2) {
+    const float2 x = z[r >> 1];
+    add += of(x.x, r) + of(x.y, r + 1);
   }
-  p.c.weights[static_cast<long long>(unit) * p.c.capacity + j] += add;
+  p.c.weights[slot] += add;
 }
 
 template <int NB, bool kPos>

@@ -79,7 +79,8 @@ struct Q4AttendParams {
   float* cta_o;                // [CTAs][2]: likewise of row blocks from before, and going on
   float2* cta_ml;
   float* lse_ws;               // [units][rows]: base-2 log-sum-exp
-  float* z;                    // accumulate: [units][rows][capacity] base-2 logits
+  float* z;                    // accumulate: [units][capacity][z_stride] base-2 logits of the rows
+  int z_stride;                // rows, made even
 };
 
 struct Q4EvictParams {

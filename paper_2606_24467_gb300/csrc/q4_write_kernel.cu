@@ -319,7 +319,8 @@ __global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __g
 }
 
 // A CTA a sequence: the first of its rows with a negative position.
-__global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __grid_constant__ Q4AppendParams p) {
+constexpr int kLengthThreads = 1024;
+__global__ void __launch_bounds__(kLengthThreads) append_lengths_kernel(const __grid_constant__ Q4AppendParams p) {
   pdl_wait();  // the rows' kernel has read the lengths
   pdl_launch_dependents();
   __shared__ int s_used;
@@ -328,12 +329,12 @@ __global__ void __launch_bounds__(kWriteThreads) append_lengths_kernel(const __g
   if (threadIdx.x == 0) s_used = r.y;
   __syncthreads();
   int used = r.y;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < r.y; i += kWriteThreads)
-    if (p.positions[r.x + i] < 0) used = min(used, i);
+#pragma unroll 8
+  for (int i = threadIdx.x; i < r.y; i += kLengthThreads)
+    used = p.positions[r.x + i] < 0 ? min(used, i) : used;
   if (used < r.y) atomicMin(&s_used, used);
   __syncthreads();
-  for (int g = threadIdx.x; g < H; g += kWriteThreads)
+  for (int g = threadIdx.x; g < H; g += kLengthThreads)
     set_length(p, s * H + g, first_slot(p, s * H + g), s_used);
 }
 
@@ -432,7 +433,7 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t
   else
     e = p.is_bf16 ? launch_append_rows<true, kMostTasks>(p, tasks, stream) : launch_append_rows<false, kMostTasks>(p, tasks, stream);
   if (e != cudaSuccess) return e;
-  return launch_dependent(append_lengths_kernel, dim3(p.c.batch), kWriteThreads, 0, stream, p);
+  return launch_dependent(append_lengths_kernel, dim3(p.c.batch), kLengthThreads, 0, stream, p);
 }
 
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t stream) {
