@@ -6,8 +6,8 @@
 //
 // Bound by memory: 160 bytes a slot against at most a few thousand operations,
 // so the kernel is built around a steady stream of slots and few instructions
-// a code.  Every warp takes a run of tiles of 48 or 64 slots (see Q4AttendParams) and
-// keeps two to four in flight with TMA into its own part of shared memory.  A
+// a code.  Every warp takes a run of tiles of 64 slots (see Q4AttendParams) and
+// keeps two in flight with TMA into its own part of shared memory.  A
 // row block that lies in its run it finishes itself; of others it leaves the
 // softmax reference, sum and outputs, which its CTA joins, and for row blocks
 // that several CTAs share the last of them to come, always in slot order.
@@ -48,18 +48,6 @@ namespace ckv {
 
 namespace {
 
-#ifndef Q4W1
-#define Q4T1 64
-#define Q4W1 8
-#define Q4S1 2
-#define Q4T2 64
-#define Q4W2 8
-#define Q4S2 2
-#endif
-#ifndef Q4MIN
-#define Q4MIN 8
-#define Q4SOLO 4
-#endif
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
@@ -68,14 +56,18 @@ constexpr int kMinScaleExp = -110;     // smaller scales and minima share this r
 
 // Shared memory of a worker's stage: codes of K and V (swizzled), then params
 // and positions.
-constexpr int kMinTiles = Q4MIN;    // least tiles of a CTA that shares row blocks
-constexpr int kSoloTiles = Q4SOLO;  // most tiles a warp of a row block in one CTA
+constexpr int kMinTiles = 8;   // least tiles of a CTA that shares row blocks: one a warp
+constexpr int kSoloTiles = 4;  // most tiles a warp of a row block in one CTA
 
+// Eight warps of 64 slots a step with the next 64 on their way: 160 KB a CTA.
+// More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot
+// and come to the same time at long lengths (117 us against 120 and 124 for four
+// units of 128K slots), where reading alone takes 108.
 template <int NB>
 struct Shape {
-  static constexpr int kTile = NB == 1 ? Q4T1 : Q4T2;  // slots
-  static constexpr int kWarps = NB == 1 ? Q4W1 : Q4W2;
-  static constexpr int kStages = NB == 1 ? Q4S1 : Q4S2;
+  static constexpr int kTile = 64;  // slots
+  static constexpr int kWarps = 8;
+  static constexpr int kStages = 2;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kSteps = kTile / 16;
   static constexpr int kCodeTile = kTile * kQ4CodeBytes;

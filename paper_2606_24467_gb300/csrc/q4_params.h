@@ -56,7 +56,7 @@ using Q4AppendParams = Q4WriteParams<0>;
 using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
 using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
-// Attention.  The tiles (48 or 64 slots) of all row blocks -- up to 16 query rows of
+// Attention.  The tiles (64 slots) of all row blocks -- up to 16 query rows of
 // a unit -- form one sequence, of which every CTA takes an equal run, and every
 // warp of it a run of that.  Where there are few short row blocks, a CTA takes
 // one each instead.

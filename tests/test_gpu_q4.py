@@ -485,6 +485,77 @@ def test_attend_is_the_same_on_every_call(cuda_device):
         assert torch.equal(w.view(torch.int32), got[0][1].view(torch.int32))
 
 
+@pytest.mark.parametrize("b,h,most", [(140, 1, 300), (70, 4, 200), (129, 1, 2000), (500, 5, 90), (3, 1, 9000)])
+def test_attend_many_units(cuda_device, b, h, most):
+    """Units by the hundred, some empty: whole in a warp, in a CTA, or shared."""
+    gen = torch.Generator().manual_seed(b)
+    le = torch.randint(0, most, (b, h), generator=gen).numpy()
+    le[::7] = 0
+    le[-1, -1] = most
+    c = random_cache(b, h, most, le, cuda_device, gen)
+    run_attend(c, torch.randn((b, 2 * h, 1, 128), generator=gen).bfloat16().to(cuda_device))
+    run_attend(c, torch.randn((b, 9 * h, 1, 128), generator=gen).half().to(cuda_device))
+
+
+def test_attend_all_empty(cuda_device):
+    c = blank(3, 2, 64, cuda_device)
+    q = torch.randn((3, 8, 2, 128), device=cuda_device).half()
+    out, lse = run_attend(c, q)
+    assert not out.any() and (lse == float("-inf")).all()
+
+
+def test_attend_with_one_workspace_for_calls_of_many_shapes(cuda_device):
+    """Calls in turn, and captured graphs in turn, share a workspace."""
+    gen = torch.Generator().manual_seed(19)
+    calls = []
+    for b, h, n, group, le in ((1, 2, 1, 4, 9000), (2, 4, 3, 3, 700), (4, 1, 1, 16, 40), (1, 1, 1, 1, 20000)):
+        c = random_cache(b, h, le, le, cuda_device, gen)
+        q = torch.randn((b, h * group, n, 128), generator=gen).bfloat16().to(cuda_device)
+        want = torch.empty_like(q)
+        ckv.q4_attend(c, q, want, ckv.q4_workspace(c, h * group, n), accumulate=False)
+        calls.append((c, q, want, torch.empty_like(q)))
+    most = max(ckv.q4_workspace_size(c, q.shape[1], q.shape[2]) for c, q, _, _ in calls)
+    ws = torch.zeros(most, dtype=torch.uint8, device=cuda_device)
+    for c, q, want, got in calls * 2:
+        got.zero_()
+        ckv.q4_attend(c, q, got, ws)
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+    graphs = []
+    for c, q, want, got in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ckv.q4_attend(c, q, got, ws)
+        graphs.append(g)
+    for _ in range(2):
+        for g, (c, q, want, got) in zip(graphs, calls):
+            got.zero_()
+            g.replay()
+            assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
+def test_steps_on_a_share_of_the_sms(cuda_device):
+    """The stream of a green context: fewer CTAs, the same values."""
+    from test_gpu_shared_sms import GreenStream
+    try:
+        green = GreenStream(16)
+    except (OSError, AttributeError, RuntimeError) as e:
+        pytest.skip(f"no green contexts here: {e}")
+    gen = torch.Generator().manual_seed(23)
+    c = random_cache(2, 2, 5000, [[5000, 3000], [100, 0]], cuda_device, gen)
+    q = torch.randn((2, 8, 1, 128), generator=gen).bfloat16().to(cuda_device)
+    ws, out = ckv.q4_workspace(c, 8, 1), torch.empty_like(q)
+    lse = torch.empty((2, 8, 1), device=cuda_device)
+    before = host(c)
+    torch.cuda.synchronize()
+    ckv.q4_attend(c, q, out, ws, lse=lse, accumulate=True, stream=green.stream)
+    torch.cuda.synchronize()
+    after = host(c)
+    check_attend(before, q, out, lse, before["weights"], after["weights"], 128 ** -0.5)
+    ckv.q4_evict(c, 1000, ws, sinks=2, recent=5, stream=green.stream)
+    torch.cuda.synchronize()
+    check_evict(after, host(c), np.full((2, 2), 1000), 2, 5)
+
+
 def test_attend_lengths_outside_the_cache(cuda_device):
     gen = torch.Generator().manual_seed(13)
     c = random_cache(1, 3, 64, [[64, 64, 64]], cuda_device, gen)
