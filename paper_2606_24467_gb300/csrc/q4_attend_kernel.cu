@@ -1077,31 +1077,44 @@ __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int
 }
 
 // ---------------------------------------------------------------- weights
-// A thread takes a slot: its logits lie side by side.
+// A thread takes a slot, whose logits lie side by side: kWide of them a read.
+// (Groups of lanes that share a slot, or several slots a thread, took half as
+// long again: more instructions, and more lines at once than L1 holds.)
 constexpr int kWeightThreads = 256;
 
+template <int kWide>
 __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ Q4AttendParams p) {
-  __shared__ float s_lse[kMaxQRows];
+  __shared__ float s_lse[kMaxQRows + 2];
   pdl_wait();
   pdl_launch_dependents();
   const int unit = blockIdx.y, len = length_of(p.c, unit);
-  if (static_cast<int>(blockIdx.x) * kWeightThreads >= len) return;
-  for (int r = threadIdx.x; r < p.rows; r += kWeightThreads)
-    s_lse[r] = p.lse_ws[static_cast<long long>(unit) * p.rows + r];
-  __syncthreads();
   const int j = blockIdx.x * kWeightThreads + threadIdx.x;
-  if (j >= len) return;
+  if (j - static_cast<int>(threadIdx.x) >= len) return;
   const size_t slot = static_cast<size_t>(unit) * p.c.capacity + j;
-  const float2* z = reinterpret_cast<const float2*>(p.z + slot * p.z_stride);
-  // (a slot that a row does not see has -inf, and such a row may have no sum)
-  auto of = [&](float x, int r) { return r < p.rows && x != -INFINITY ? ex2_approx(x - s_lse[r]) : 0.f; };
+  const float old = j < len ? p.c.weights[slot] : 0.f;
+  for (int r = threadIdx.x; r < p.rows; r += kWeightThreads)
+    s_lse[r] = p.lse_ws[static_cast<size_t>(unit) * p.rows + r];
+  __syncthreads();
+  if (j >= len) return;
+  const float* z = p.z + slot * p.z_stride;
   float add = 0.f;
-#pragma unroll 4
-  for (int r = 0; r < p.rows; r += 2) {
-    const float2 x = z[r >> 1];
-    add += of(x.x, r) + of(x.y, r + 1);
+  // (a row that does not see the slot has -inf there; of an odd number of rows
+  // the last read holds one more, which is none)
+#pragma unroll 2
+  for (int r = 0; r < p.rows; r += kWide) {
+    float x[kWide];
+    if (kWide == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(z + r);
+      x[0] = v.x, x[1] = v.y, x[kWide - 2] = v.z, x[kWide - 1] = v.w;
+    } else {
+      const float2 v = *reinterpret_cast<const float2*>(z + r);
+      x[0] = v.x, x[1] = v.y;
+    }
+#pragma unroll
+    for (int i = 0; i < kWide; ++i)
+      if (r + i < p.rows && x[i] != -INFINITY) add += ex2_approx(x[i] - s_lse[r + i]);
   }
-  p.c.weights[slot] += add;
+  p.c.weights[slot] = old + add;
 }
 
 template <int NB, bool kPos>
@@ -1133,7 +1146,7 @@ cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t stre
 
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t stream) {
   const dim3 grid((p.c.capacity + kWeightThreads - 1) / kWeightThreads, p.c.batch * p.c.num_kv_heads);
-  return launch_dependent(weights_kernel, grid, kWeightThreads, 0, stream, p);
+  return launch_dependent(p.z_stride % 4 ? weights_kernel<2> : weights_kernel<4>, grid, kWeightThreads, 0, stream, p);
 }
 
 }  // namespace ckv

@@ -452,6 +452,11 @@ def test_attend_non_finite_slots(cuda_device):
     nan = torch.isnan(out[0, :4, 1])
     assert nan[:, 32:64].all() and not nan[:, :32].any() and not nan[:, 64:].any()
     assert torch.isnan(out[0, 4:, 1]).all() and torch.isnan(lse[0, 4:, 1]).all()
+    # an odd number of rows, none of which sees the slot
+    c.weights.zero_()
+    q3 = torch.randn((1, 6, 1, 128), generator=gen).bfloat16().to(cuda_device)
+    run_attend(c, q3, q_positions=at[:, :1].contiguous())
+    assert torch.isfinite(c.weights[0, 1, :80]).all() and (c.weights[0, 1, 41:80] == 0).all()
     # a query that holds a NaN or an infinity stays alone
     c = random_cache(1, 2, 96, [[90, 80]], cuda_device, gen)
     for bad in (float("nan"), float("inf")):
