@@ -14,8 +14,8 @@
 //
 // Codes enter the tensor cores as they are.  A nibble n masked out of a word is
 // the fp16 subnormal n * 2^-24 (one in bits 4-7 is 16 n * 2^-24), exact in a
-// product with fp32 sums, so five instructions make eight operands (V: four, see
-// below) and neither scale, minimum nor an offset is applied to a code.  mma.sync takes operands
+// product with fp32 sums, so five instructions make eight operands and neither
+// scale, minimum nor an offset is applied to a code.  mma.sync takes operands
 // from registers: with 8 or 16 query rows a unit's products are far below the
 // tensor cores' rate, while tcgen05 would want the operands expanded to 16 bits
 // in shared memory, four times the bytes of the codes.
@@ -26,14 +26,16 @@
 //     scaled by their s in fp32.  The minima's term sum_J m_J (sum of q over J)
 //     is one more product: the group sums as three bf16 parts (24 bits), m in bf16.
 //   O^T = V^T P^T: A = codes of 16 channels, B = P^T, which movmatrix makes of
-//     the result layout of S^T.  With p in fp16 (relative error 2^-12) the weights
-//     of group J's codes are p s_J (rounded once more), those of its minimum p; the
-//     minima's term is a product of its own.  A byte holds two channels n and n':
-//     the operands are n + 16 n' and 16 n' (both exact), whose sums give the
-//     channels' by one subtraction at the end, an instruction less a word than
-//     n and 16 n'.  Scales and minima are fp16 too,
-//     exact against a power of two that follows the largest of both: 2^-21 of it
-//     and above for scales, 2^-22 for minima.
+//     the result layout of S^T.  With c = n - 7.5 and the group's middle
+//     m + 7.5 s, out = sum p s c + sum p (m + 7.5 s): both terms stay as small as
+//     the output does where many slots share the attention.  (With n and m they
+//     grow with sum p; the tensor cores truncate their sums, so that at 128K slots
+//     3 % of the output were lost.)  The 7.5 comes off once a tile, by 7.5 sum p s
+//     from a product of the same operands with ones.  With p in fp16 (relative
+//     error 2^-12) the weights of group J's codes are p s_J (rounded once more),
+//     those of its middle p; the middles' term is a product of its own.  Scales and
+//     middles are fp16 too (scales exactly, middles to 2^-12) against a power of
+//     two that follows the largest of both, for scales down to 2^-21 of it.
 // Eight lanes of a warp need the same slot's scales, so one lane a slot converts
 // them for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
 // leaves them in shared memory.
@@ -51,7 +53,8 @@ namespace {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
-constexpr int kTopExp = 7;             // scales become < 2^4, minima < 2^8: p s < 2^15
+constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p s < 2^15
+constexpr uint32_t kFifteen = 0x000f000fu;  // 15 * 2^-24 twice: twice a code's middle
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
 // Shared memory of a worker's stage: codes of K and V (swizzled), then params
@@ -60,9 +63,9 @@ constexpr int kMinTiles = 8;   // least tiles of a CTA that shares row blocks: o
 constexpr int kSoloTiles = 4;  // most tiles a warp of a row block in one CTA
 
 // Eight warps of 64 slots a step with the next 64 on their way: 160 KB a CTA.
-// More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot
-// and come to the same time at long lengths (117 us against 120 and 124 for four
-// units of 128K slots), where reading alone takes 108.
+// More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot:
+// 117 us against 120 and 124 for four sequences of 128K slots when that was
+// measured, where reading alone takes 108.
 template <int NB>
 struct Shape {
   static constexpr int kTile = 64;  // slots
@@ -504,11 +507,13 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   // ldmatrix row of this lane: slot lane & 7, piece lane >> 3 of its 64 bytes,
   // stored at piece ^ (slot / 2) by the 64-byte swizzle
   const uint32_t mat = (lane & 7) * kQ4CodeBytes + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
+  // ... and for one group of 32 slots: slot lane, piece 0 (others by exclusive or)
+  const uint32_t group_mat = lane * kQ4CodeBytes + (((lane >> 1) & 3) << 4);
 
   const float f1 = p.scale_log2 * 1024.0f;
   Queries<NB> Q;
   float o[NB][4][2][4];   // [8 rows][group][step][channel, row pair]
-  float om[NB][4];        // minima's term (lanes of g >= 4)
+  float om[NB][4];        // middles' term (lanes of g >= 4)
   float ref[NB][2], l[NB][2];  // rows 2t, 2t + 1
   int vexp = kMinScaleExp;
   bool fresh = true;
@@ -606,15 +611,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       const float f = pow2(kTopExp - vexp);
 #pragma unroll
       for (int i = 0; i < kLane; ++i) {
-        const uint32_t s01 = pack_half2(bf_lo(w[i].x) * f, bf_hi(w[i].x) * f);
-        const uint32_t s23 = pack_half2(bf_lo(w[i].y) * f, bf_hi(w[i].y) * f);
+        const float s0 = bf_lo(w[i].x) * f, s1 = bf_hi(w[i].x) * f, s2 = bf_lo(w[i].y) * f, s3 = bf_hi(w[i].y) * f;
+        const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
+        // middles: m + 7.5 s
+        const uint32_t m01 = pack_half2(fmaf(s0, 7.5f, bf_lo(w[i].z) * f), fmaf(s1, 7.5f, bf_hi(w[i].z) * f));
+        const uint32_t m23 = pack_half2(fmaf(s2, 7.5f, bf_lo(w[i].w) * f), fmaf(s3, 7.5f, bf_hi(w[i].w) * f));
         // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
         const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
         const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
         if (lane + 32 * i < kTile) sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
-               make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632),
-                          pack_half2(bf_lo(w[i].z) * f, bf_hi(w[i].z) * f),
-                          pack_half2(bf_lo(w[i].w) * f, bf_hi(w[i].w) * f)));
+               make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), m01, m23));
       }
       __syncwarp();
     }
@@ -757,42 +763,57 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
     }
 
-    // ---- outputs
+    // ---- outputs: the middles' term, then the codes group by group
+    uint32_t p0[NB][kSteps], p1[NB][kSteps];
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) {
-      const int s16 = h * 16;
-      uint32_t va[4], vb[4], pm[4];
-      ldmatrix4_t(va, cd + kCodeTile + s16 * kQ4CodeBytes + mat);
-      ldmatrix4_t(vb, cd + kCodeTile + (s16 + 8) * kQ4CodeBytes + mat);
-      // rows of [2 pairs of scales, 4 minima]: rows 4-7 of the transposed
-      // operand are the minima; rows 8-15 repeat rows 0-7
-      ldmatrix4_t(pm, sd + kParamTile + (s16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
-      const uint2 s0 = lds64(sd + kParamTile + (s16 + 2 * t) * kQ4ParamBytes);
-      const uint2 s1 = lds64(sd + kParamTile + (s16 + 2 * t + 1) * kQ4ParamBytes);
-      const uint2 s2 = lds64(sd + kParamTile + (s16 + 8 + 2 * t) * kQ4ParamBytes);
-      const uint2 s3 = lds64(sd + kParamTile + (s16 + 9 + 2 * t) * kQ4ParamBytes);
-      const uint32_t sa[4] = {s0.x, s0.y, s1.x, s1.y}, sb[4] = {s2.x, s2.y, s3.x, s3.y};
-      uint32_t p0[NB], p1[NB];
+      uint32_t pm[4];
+      // rows of [2 pairs of scales, 4 middles]: rows 4-7 of the transposed
+      // operand are the middles; rows 8-15 repeat rows 0-7
+      ldmatrix4_t(pm, sd + kParamTile + (h * 16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        p0[nb] = transpose8(pack_half2(z[nb][h][0], z[nb][h][1]));
-        p1[nb] = transpose8(pack_half2(z[nb][h][2], z[nb][h][3]));
-        mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], p0[nb], p1[nb]);
+        p0[nb][h] = transpose8(pack_half2(z[nb][h][0], z[nb][h][1]));
+        p1[nb][h] = transpose8(pack_half2(z[nb][h][2], z[nb][h][3]));
+        mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], p0[nb][h], p1[nb][h]);
       }
+    }
 #pragma unroll
-      for (int J = 0; J < 4; ++J) {
-        // bytes 1 and 3 of a word in the place of 0 and 2
-        const uint32_t ah = __byte_perm(va[J], 0u, 0x4341), bh = __byte_perm(vb[J], 0u, 0x4341);
-        const uint32_t a0 = va[J] & 0x00ff00ffu, a1 = va[J] & 0x00f000f0u;
-        const uint32_t a2 = vb[J] & 0x00ff00ffu, a3 = vb[J] & 0x00f000f0u;
-        const uint32_t b1 = ah & 0x00f000f0u, b3 = bh & 0x00f000f0u;
+    for (int J = 0; J < 4; ++J) {
+      uint32_t v[kTile / 8];  // group J of 8 slots each
+#pragma unroll
+      for (int i = 0; i < kTile / 32; ++i)
+        ldmatrix4_t(*reinterpret_cast<uint32_t (*)[4]>(v + 4 * i),
+                    cd + kCodeTile + i * 32 * kQ4CodeBytes + (group_mat ^ (J << 4)));
+      float mass[NB][4];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mass[nb][i] = 0.f;
+#pragma unroll
+      for (int h = 0; h < kSteps; ++h) {
+        const uint32_t pair = sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
+        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * kQ4ParamBytes);
+        const uint32_t x = v[2 * h], y = v[2 * h + 1], xh = x >> 8, yh = y >> 8;
+        const uint32_t a0 = x & 0x000f000fu, a1 = x & 0x00f000f0u, a2 = y & 0x000f000fu, a3 = y & 0x00f000f0u;
+        const uint32_t b0 = xh & 0x000f000fu, b1 = xh & 0x00f000f0u, b2 = yh & 0x000f000fu, b3 = yh & 0x00f000f0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const uint32_t q0 = mul_half2(p0[nb], sa[J]), q1 = mul_half2(p1[nb], sb[J]);
+          const uint32_t q0 = mul_half2(p0[nb][h], sa), q1 = mul_half2(p1[nb][h], sb);
           mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
-          mma_f16(o[nb][J][1], ah, b1, bh, b3, q0, q1);
+          mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
+          mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
         }
       }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            o[nb][J][st][i] = fmaf(mass[nb][i], -0.5f, o[nb][J][st][i]);
+            o[nb][J][st][2 + i] = fmaf(mass[nb][i], -8.0f, o[nb][J][st][2 + i]);
+          }
     }
     if (special) {
       const float bad = __uint_as_float(0x7fc00000u);
@@ -833,7 +854,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         part.starts = starts;
         part.ends = ends;
       }
-      // sums of the codes' products: * 2^24 for the pair's sum, 2^20 for its second channel
+      // sums of the codes' products: * 2^24, and 1/16 for a byte's second channel
       const float f = pow2(vexp - kTopExp);
       float* head = p.head_o + static_cast<size_t>(blockIdx.x * S::kWarps + warp) * kRows * kHeadDim;
 #pragma unroll
@@ -861,9 +882,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             const float m = i ? m1 : m0;
             const int r = nb * 8 + 2 * t + i, row = block * kRows + r;
             float4 v;
-            v.x = fmaf(o[nb][J][0][i] - o[nb][J][0][2 + i], 16777216.0f, m) * f;
+            v.x = fmaf(o[nb][J][0][i], 16777216.0f, m) * f;
             v.y = fmaf(o[nb][J][0][2 + i], 1048576.0f, m) * f;
-            v.z = fmaf(o[nb][J][1][i] - o[nb][J][1][2 + i], 16777216.0f, m) * f;
+            v.z = fmaf(o[nb][J][1][i], 16777216.0f, m) * f;
             v.w = fmaf(o[nb][J][1][2 + i], 1048576.0f, m) * f;
             if (row >= p.rows) continue;
             if (whole) write_row(p, unit, row, 8 * J + g, v, ref[nb][i] - kLift, sum[i]);

@@ -6,9 +6,13 @@ Tolerances of the attention, derived from what it rounds.  Logits: the codes
 and the queries enter the products exactly; at most 32 roundings of at most
 2^-23 (sums that the tensor core truncates) of S, the sum of the magnitudes of
 a row's products, so |dz| <= 2^-18 S.  Probabilities: relative 2 |dz| + 2^-20.
-Output: a 16-bit rounding (2^-8 or 2^-11 of the value), the code term's weights
-in fp16 (2^-11 of sum p s n), the minimum term's in two bf16 parts (2^-16 of
-sum p |m|), and the probabilities' error on both.
+Output, as sum p s c + sum p m' with c = n - 7.5 and m' = m + 7.5 s: a 16-bit
+rounding (2^-8 or 2^-11 of the value); p in fp16 and once more p s, or m', in
+fp16: two roundings of 2^-11 of each term, 2^-10 (sum p s |c| + sum p |m'|);
+truncated sums: a step of 16 slots cuts at most 2^-23 of what its sum holds, so
+350 steps at most 2^-14 of the terms' magnitudes, and the four steps of a tile,
+which hold up to 15 p s a slot before the middle comes off, 2^-19 of sum p s;
+and the probabilities' error on both terms.
 """
 import numpy as np
 import pytest
@@ -318,12 +322,13 @@ def check_attend(c, q, out, lse, before, after, scale, q_positions=None, weights
             used = int(np.clip(c["lengths"][i, g], 0, c["positions"].shape[2]))
             k, v = stored(c, "k", i, g, used), stored(c, "v", i, g, used)
             par = c["v_params"][i, g, :used].astype(np.float64)
-            m = np.abs(np.repeat(par[:, 4:], 32, -1))
-            code = q4.unpack(c["v_codes"][i, g, :used]) * np.repeat(par[:, :4], 32, -1)
+            sc = np.repeat(par[:, :4], 32, -1)
+            m = np.abs(np.repeat(par[:, 4:], 32, -1) + 7.5 * sc)
+            code = np.abs(q4.unpack(c["v_codes"][i, g, :used]) - 7.5) * sc
             kp = c["k_params"][i, g, :used].astype(np.float64)
             kmag = (q4.unpack(c["k_codes"][i, g, :used]) * np.repeat(kp[:, :4], 32, -1)
                     + np.abs(np.repeat(kp[:, 4:], 32, -1)))
-            for x in (m, code, kmag):
+            for x in (m, code, kmag, sc):
                 x[np.isnan(x)] = 0
             add, slack = np.zeros(used), np.zeros(used)
             for hh in range(g * group, (g + 1) * group):
@@ -335,8 +340,9 @@ def check_attend(c, q, out, lse, before, after, scale, q_positions=None, weights
                     S = scale * (kmag[vis[t]] @ np.abs(qd[i, hh, t])).max(initial=0.0)
                     dz = 2.0 ** -18 * S
                     dp = 2 * dz + 2.0 ** -20
-                    a, mm = p[t][vis[t]] @ code[vis[t]], p[t][vis[t]] @ m[vis[t]]
-                    tol = half * np.abs(ro[t]) + (2.0 ** -11 + dp) * a + (2.0 ** -16 + dp) * mm + floor
+                    terms = p[t][vis[t]] @ (code + m)[vis[t]]
+                    tol = (half * np.abs(ro[t]) + (2.0 ** -10 + 2.0 ** -14 + dp) * terms
+                           + 2.0 ** -19 * (p[t][vis[t]] @ sc[vis[t]]) + floor)
                     same_nan = np.isnan(ro[t]) & np.isnan(got[i, hh, t])
                     assert ((np.abs(got[i, hh, t] - ro[t]) <= tol) | same_nan).all(), (i, hh, t)
                     if gl is not None:
@@ -500,6 +506,42 @@ def test_attend_many_units(cuda_device, b, h, most):
     c = random_cache(b, h, most, le, cuda_device, gen)
     run_attend(c, torch.randn((b, 2 * h, 1, 128), generator=gen).bfloat16().to(cuda_device))
     run_attend(c, torch.randn((b, 9 * h, 1, 128), generator=gen).half().to(cuda_device))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attend_averages_many_slots(cuda_device, dtype):
+    """Attention spread over 64K slots, each warp summing thousands: the output
+    is small against its terms, and keeps its precision.  Bound: 2^-8 or 2^-11 of
+    the value; eight standard deviations of the independent roundings of p, p s
+    and m' (at most 2^-11 each, of p s c or p m'); 2^-19 of sum p s for the tiles'
+    sums and, for a bias along the 432 steps of a warp, 2^-14 of the value."""
+    units, cap = 128, 65536
+    gen = torch.Generator(device=cuda_device).manual_seed(61)
+    c = ckv.q4_cache(16, 8, cap, cuda_device, weights=False)
+    for part in ("k", "v"):
+        getattr(c, part + "_codes").random_(0, 256, generator=gen)
+        par = getattr(c, part + "_params")
+        par[..., :4] = 0.1 + 0.05 * torch.rand((16, 8, cap, 4), generator=gen, device=cuda_device)
+        par[..., 4:] = -7.5 * par[..., :4].float() + 0.05 * torch.randn((16, 8, cap, 4), generator=gen,
+                                                                        device=cuda_device)
+    c.lengths.fill_(cap)
+    q = (0.7 * torch.randn((16, 32, 1, 128), generator=gen, device=cuda_device)).to(dtype)
+    out = torch.empty_like(q)
+    ckv.q4_attend(c, q, out, ckv.q4_workspace(c, 32, 1))
+    for b, g in ((0, 0), (7, 3), (15, 7)):
+        def term(part):
+            raw = getattr(c, part + "_codes")[b, g].int()
+            n = torch.stack([raw & 15, raw >> 4], -1).flatten(-2).double()
+            par = getattr(c, part + "_params")[b, g].double().repeat_interleave(32, -1)
+            return par[:, :128] * (n - 7.5), par[:, 128:] + 7.5 * par[:, :128], par[:, :128]
+        kc, km, _ = term("k")
+        vc, vm, vs = term("v")
+        for h in range(4 * g, 4 * g + 4):
+            p = ((kc + km) @ q[b, h, 0].double() * 128 ** -0.5).softmax(0)
+            want = p @ (vc + vm)
+            sd = 2.0 ** -11 * (2 * (p.square() @ (vc.square() + vm.square()))).sqrt()
+            tol = (HALF_STEP[dtype] + 2.0 ** -14) * want.abs() + 8 * sd + 2.0 ** -19 * (p @ vs)
+            assert ((out[b, h, 0].double() - want).abs() <= tol).all(), (b, h)
 
 
 def test_attend_all_empty(cuda_device):
