@@ -646,6 +646,8 @@ def _q4_rows(cache: Q4Cache, k, v):
         _invalid("k and v must be [rows, H_kv, 128]")
     if v.dtype != k.dtype or strides[2] != 1 or v.stride() != strides:
         _invalid("k and v must share their dtype and strides, head_dim contiguous")
+    if v.is_cuda and v.device != cache.device:  # (else page-locked host memory)
+        _invalid("v must be on the cache's device")
     return _q4_dtype(k), shape, strides
 
 

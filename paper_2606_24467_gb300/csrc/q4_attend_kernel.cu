@@ -36,8 +36,8 @@
 //     those of its middle p; the middles' term is a product of its own.  Scales and
 //     middles are fp16 too (scales exactly, middles to 2^-12) against a power of
 //     two that follows the largest of both, for scales down to 2^-21 of it.
-// Eight lanes of a warp need the same slot's scales, so one lane a slot converts
-// them for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
+// Eight lanes of a warp need the same slot's scales, so one lane converts them
+// for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
 // leaves them in shared memory.
 // Softmax references are raised only when a logit passes them by 2^8, so the
 // outputs are hardly ever rescaled.
@@ -57,8 +57,6 @@ constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p 
 constexpr uint32_t kFifteen = 0x000f000fu;  // 15 * 2^-24 twice: twice a code's middle
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
-// Shared memory of a worker's stage: codes of K and V (swizzled), then params
-// and positions.
 constexpr int kMinTiles = 8;   // least tiles of a CTA that shares row blocks: one a warp
 constexpr int kSoloTiles = 4;  // most tiles a warp of a row block in one CTA
 
@@ -66,6 +64,8 @@ constexpr int kSoloTiles = 4;  // most tiles a warp of a row block in one CTA
 // More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot:
 // 117 us against 120 and 124 for four sequences of 128K slots when that was
 // measured, where reading alone takes 108.
+// A warp's stage holds the codes of K and V (swizzled); their params and the
+// positions lie in an area of their own.
 template <int NB>
 struct Shape {
   static constexpr int kTile = 64;  // slots
@@ -210,7 +210,10 @@ struct Place {
       block = 0;
       ++unit;
     }
-    while ((valid = length_of(p.c, unit)) == 0) ++unit;
+    // (never past the last unit, whatever the lengths become meanwhile)
+    const int last = p.c.batch * p.c.num_kv_heads - 1;
+    unit = min(unit, last);
+    while ((valid = length_of(p.c, unit)) == 0 && unit < last) ++unit;
     row = unit * p.c.capacity;
   }
 };
@@ -356,7 +359,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   fence_mbar_init();
   __syncthreads();  // (the others' parts and the abort flag)
   pdl_wait();  // everything before is of this launch alone
-  pdl_launch_dependents();
+  if (p.accumulate) pdl_launch_dependents();  // the weights' kernel, which waits for this one
 
   // ---- this CTA's tiles, and this warp's share of them.  (The host bounds the
   // tiles by 2^30.)
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       unit0 = s_unit[warp];
       at = s_at[warp];
       int n;
-      while (at + (n = tiles_of<kTile>(p.c, unit0)) * p.blocks <= tile) {
+      while (at + (n = tiles_of<kTile>(p.c, unit0)) * p.blocks <= tile && unit0 < units - 1) {
         at += n * p.blocks;
         ++unit0;
       }
@@ -473,10 +476,11 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   }
   Place c = {};
   if (left > 0) {
-    const int len = length_of(p.c, unit0), n = (len + kTile - 1) / kTile;
+    unit0 = min(unit0, units - 1);
+    const int len = length_of(p.c, unit0), n = max(1, (len + kTile - 1) / kTile);
     c.unit = unit0;
-    c.block = (tile - at) / n;
-    const int slot = (tile - at - c.block * n) * kTile;
+    c.block = min((tile - at) / n, p.blocks - 1);
+    const int slot = min(tile - at - c.block * n, n - 1) * kTile;
     c.row = unit0 * p.c.capacity + slot;
     c.valid = len - slot;
   }
@@ -1107,7 +1111,6 @@ template <int kWide>
 __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ Q4AttendParams p) {
   __shared__ float s_lse[kMaxQRows + 2];
   pdl_wait();
-  pdl_launch_dependents();
   const int unit = blockIdx.y, len = length_of(p.c, unit);
   const int j = blockIdx.x * kWeightThreads + threadIdx.x;
   if (j - static_cast<int>(threadIdx.x) >= len) return;

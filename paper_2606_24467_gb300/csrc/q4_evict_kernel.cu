@@ -89,7 +89,6 @@ __global__ void __launch_bounds__(kThreads, kHold == kShortItems ? 6 : 1) evict_
   const uint32_t ranks = kCluster ? p.cluster : 1, rank = kCluster ? cluster_rank() : 0;
   const int unit = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
-  pdl_launch_dependents();
   const long long base = static_cast<long long>(unit) * p.c.capacity;
   const int32_t* pos = p.c.positions + base;
   const float* wt = p.c.weights + base;

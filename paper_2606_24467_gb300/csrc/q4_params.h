@@ -94,7 +94,10 @@ struct Q4EvictParams {
 };
 
 // Launches a kernel that may be brought up while the one before it in the
-// stream ends (its first act is then to wait for that one's results).
+// stream ends (its first act is then to wait for that one's results).  Only a
+// kernel that another of the same call follows lets its successor start before
+// its own end: what comes after a call may read the call's outputs at once, as
+// the scoring kernel reads K.
 template <class... A>
 cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t stream,
                              const A&... args) {

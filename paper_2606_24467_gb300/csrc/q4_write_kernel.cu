@@ -220,7 +220,6 @@ __device__ __forceinline__ void set_length(const Q4AppendParams& p, int unit, in
 template <bool kBf16>
 __global__ void __launch_bounds__(kWriteThreads) append_unit_kernel(const __grid_constant__ Q4AppendParams p) {
   pdl_wait();
-  pdl_launch_dependents();
   const int unit = blockIdx.x;
   const int s = unit / p.c.num_kv_heads, g = unit - s * p.c.num_kv_heads;
   const int2 r = rows_of(p, s);
@@ -289,7 +288,7 @@ __device__ __forceinline__ void move_rows(const Q4WriteParams<kTable>& p, const 
 template <bool kBf16, int kTasks>
 __global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __grid_constant__ Q4AppendParams p) {
   pdl_wait();
-  pdl_launch_dependents();
+  pdl_launch_dependents();  // the lengths' kernel, which waits for this one
   const int H = p.c.num_kv_heads;
   // (the host bounds the tasks by 2^31 - 1, and the slots)
   const unsigned tasks = static_cast<unsigned>(p.rows) * H;
@@ -322,7 +321,6 @@ __global__ void __launch_bounds__(kWriteThreads, 4) append_rows_kernel(const __g
 constexpr int kLengthThreads = 1024;
 __global__ void __launch_bounds__(kLengthThreads) append_lengths_kernel(const __grid_constant__ Q4AppendParams p) {
   pdl_wait();  // the rows' kernel has read the lengths
-  pdl_launch_dependents();
   __shared__ int s_used;
   const int s = blockIdx.x, H = p.c.num_kv_heads;
   const int2 r = rows_of(p, s);
@@ -343,7 +341,6 @@ __global__ void __launch_bounds__(kLengthThreads) append_lengths_kernel(const __
 template <bool kBf16, int kTasks, class P>
 __global__ void __launch_bounds__(kWriteThreads, 4) gather_q4_kernel(const __grid_constant__ P p) {
   pdl_wait();
-  pdl_launch_dependents();
   const int H = p.c.num_kv_heads, B = p.c.batch, lane = threadIdx.x & 31;
   const unsigned tasks = p.group_major ? p.rows : static_cast<unsigned>(p.rows) * H;
   const unsigned warps = (tasks + kTasks - 1) / kTasks;

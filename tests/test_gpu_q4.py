@@ -944,6 +944,31 @@ def test_refuses_tensors_of_another_device(cuda_device):
         assert e.value.code == B.CKV_ERR_INVALID_ARG
 
 
+def test_scores_of_the_values_that_an_append_returns(cuda_device):
+    """A scoring call right behind an append reads the append's k_values."""
+    dev, cfg = cuda_device, wl.get("c1").scaled(dtype="bf16", seq_len=3001)
+    d = wl.make_layer(cfg, 0)
+    q, k, v = d["q_win"].to(dev), d["k"].to(dev), d["v"].to(dev)
+    pos = torch.arange(3001, dtype=torch.int32, device=dev)
+    c = ckv.q4_cache(1, 8, 3001, dev)
+    kv, vv = torch.zeros_like(k), torch.zeros_like(v)
+    p = ckv.Problem(q, kv, d["cu_seqlens"], cfg.window, cfg.pool_width)
+    ws = ckv.workspace(p, dev)
+    raw = torch.empty((8, 3001 - cfg.window), device=dev)
+
+    def step(wait):
+        kv.zero_()
+        ckv.q4_append(c, k, v, pos, start=torch.zeros_like(c.lengths), k_values=kv, v_values=vv)
+        if wait:
+            torch.cuda.synchronize()
+        ckv.score(p, q, kv, d["srh_mask"], raw, ws)
+        return raw.clone()
+
+    want = step(True)
+    for _ in range(5):
+        assert torch.equal(step(False), want)
+
+
 def test_values_in_page_locked_host_memory(cuda_device):
     """V rows that the device reads over the host link."""
     gen = torch.Generator().manual_seed(51)
