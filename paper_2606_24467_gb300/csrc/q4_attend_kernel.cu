@@ -58,7 +58,7 @@ constexpr uint32_t kFifteen = 0x000f000fu;  // 15 * 2^-24 twice: twice a code's 
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
 constexpr int kMinTiles = 8;   // least tiles of a CTA that shares row blocks: one a warp
-constexpr int kSoloTiles = 4;  // most tiles a warp of a row block in one CTA
+constexpr int kSoloTiles = 4;  // most tiles a warp of a row block that one CTA takes
 
 // Eight warps of 64 slots a step with the next 64 on their way: 160 KB a CTA.
 // More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot:
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
   constexpr int kScaleTile = S::kScaleTile, kLane = S::kLane;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int s_sums[S::kWarps], s_most[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
+  __shared__ int s_sums[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
   __shared__ float2 s_ml[S::kWarps][kRows];
   __shared__ Part s_tail[S::kWarps], s_head[S::kWarps];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -363,98 +363,110 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 
   // ---- this CTA's tiles, and this warp's share of them.  (The host bounds the
   // tiles by 2^30.)
-  // Few short row blocks: a CTA takes one whole, and nothing is joined across
-  // CTAs.  Else all CTAs take equal runs of tiles, at least kMinTiles.
   const int units = p.c.batch * p.c.num_kv_heads, ctas = gridDim.x;
   int chunk = 0, tile = 0, left = 0;  // tiles of a CTA; this warp's first tile, and how many
   int unit0 = 0, at = 0;              // the unit that holds it, and that unit's first tile
-  auto divide = [&](int total, int most, int solo_first, int solo_count) {
-    const bool solo = units * p.blocks <= ctas && most <= kSoloTiles * S::kWarps;
-    chunk = solo ? solo_count : max((total + ctas - 1) / ctas, kMinTiles);
+  int own0 = -1;                      // first of the CTAs that have a row block to themselves
+  auto share_out = [&](int from, int count) {
     const int share = (chunk + S::kWarps - 1) / S::kWarps;
-    const int from = solo ? solo_first : static_cast<int>(blockIdx.x) * chunk;
-    const int count = solo ? solo_count : min(chunk, total - from);
     tile = from + warp * share;
     left = max(0, min(share, count - warp * share));
   };
+  // CTAs take equal runs of the whole sequence of tiles, at least kMinTiles
+  auto even_chunk = [&](int total) { return max((total + ctas - 1) / ctas, kMinTiles); };
   constexpr int kPer = 4;
   if (units <= 32 * kPer) {
     // every warp for itself: kPer units a lane
-    int n[kPer], mine = 0, most = 0;
+    int n[kPer], mine = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int u = lane * kPer + k;
       n[k] = u < units ? tiles_of<kTile>(p.c, u) : 0;
       mine += n[k];
-      most = max(most, n[k]);
     }
-    const int incl = warp_prefix(mine, lane);
-    const int total = __shfl_sync(0xffffffffu, incl, 31);
-    most = __reduce_max_sync(0xffffffffu, most);
-    // (first tile and tiles of unit u)
-    auto unit_at = [&](int u, int* count) {
-      int before = incl - mine, c = 0;
+    const int incl = warp_prefix(mine, lane), total = __shfl_sync(0xffffffffu, incl, 31) * p.blocks;
+    chunk = even_chunk(total);
+    // Where the row blocks come out about even over whole CTAs, each has its
+    // own: one where it is short, else in proportion.  No CTA then joins the end
+    // of one row block and the start of another (20 us against 18 for 8 units of
+    // 32K slots).
+    // (Quotients in fp32: every warp takes the same ones, near enough.)
+    int own[kPer], own_mine = 0, own_chunk = 0;
+    const float rate = __fdividef(static_cast<float>(ctas), static_cast<float>(total));
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        if (k < u % kPer) before += n[k];
-        if (k == u % kPer) c = n[k];
-      }
-      *count = __shfl_sync(0xffffffffu, c, u / kPer);
-      return __shfl_sync(0xffffffffu, before, u / kPer);
-    };
-    const int solo_unit = min(static_cast<int>(blockIdx.x) / p.blocks, units);
-    int solo_count = 0, solo_first = 0;
-    if (solo_unit < units) {
-      solo_first = unit_at(solo_unit, &solo_count) * p.blocks +
-                   (static_cast<int>(blockIdx.x) - solo_unit * p.blocks) * solo_count;
+    for (int k = 0; k < kPer; ++k) {
+      const int share = min(static_cast<int>(fmaf(n[k], rate, 1e-3f)), (n[k] + kMinTiles - 1) / kMinTiles);
+      own[k] = n[k] <= kSoloTiles * S::kWarps ? min(n[k], 1) : max(1, share);
+      own_mine += own[k] * p.blocks;
+      if (own[k]) own_chunk = max(own_chunk, static_cast<int>(__fdividef(n[k], own[k])));
     }
-    divide(total * p.blocks, most, solo_first, solo_count);
-    // the lane that holds the first tile, then the unit of that lane
-    const unsigned holds = __ballot_sync(0xffffffffu, incl * p.blocks > tile);
-    int before = incl - mine, u = lane * kPer;
+    const int own_incl = warp_prefix(own_mine, lane);
+    own_chunk = __reduce_max_sync(0xffffffffu, own_chunk);
+    if (__shfl_sync(0xffffffffu, own_incl, 31) <= ctas &&
+        own_chunk <= max(kSoloTiles * S::kWarps, chunk + chunk / 8 + 1)) {
+      const unsigned holds = __ballot_sync(0xffffffffu, own_incl > static_cast<int>(blockIdx.x));
+      int u = 0, rest = static_cast<int>(blockIdx.x) - (own_incl - own_mine), before = incl - mine, c = 0, count = 0;
+      bool found = false;
 #pragma unroll
-    for (int k = 0; k < kPer - 1; ++k)
-      if (u == lane * kPer + k && (before + n[k]) * p.blocks <= tile) {
-        before += n[k];
-        ++u;
+      for (int k = 0; k < kPer; ++k)
+        if (!found) {
+          if (rest < own[k] * p.blocks) {
+            found = true;
+            u = lane * kPer + k;
+            c = own[k];
+            count = n[k];
+          } else {
+            rest -= own[k] * p.blocks;
+            before += n[k];
+          }
+        }
+      const int src = holds ? __ffs(holds) - 1 : 0;
+      unit0 = __shfl_sync(0xffffffffu, u, src);
+      rest = __shfl_sync(0xffffffffu, rest, src);
+      c = __shfl_sync(0xffffffffu, c, src);
+      count = __shfl_sync(0xffffffffu, count, src);
+      at = __shfl_sync(0xffffffffu, before, src) * p.blocks;
+      chunk = 1;
+      if (holds && c > 0) {
+        const int block = rest / c, index = rest - block * c;
+        chunk = (count + c - 1) / c;
+        own0 = static_cast<int>(blockIdx.x) - index;
+        share_out(at + block * count + index * chunk, min(chunk, count - index * chunk));
       }
-    const int src = holds ? __ffs(holds) - 1 : 0;
-    unit0 = __shfl_sync(0xffffffffu, u, src);
-    at = __shfl_sync(0xffffffffu, before, src) * p.blocks;
+    } else {
+      const int from = static_cast<int>(blockIdx.x) * chunk;
+      share_out(from, min(chunk, total - from));
+      // the lane that holds the first tile, then the unit of that lane
+      const unsigned holds = __ballot_sync(0xffffffffu, incl * p.blocks > tile);
+      int before = incl - mine, u = lane * kPer;
+#pragma unroll
+      for (int k = 0; k < kPer - 1; ++k)
+        if (u == lane * kPer + k && (before + n[k]) * p.blocks <= tile) {
+          before += n[k];
+          ++u;
+        }
+      const int src = holds ? __ffs(holds) - 1 : 0;
+      unit0 = __shfl_sync(0xffffffffu, u, src);
+      at = __shfl_sync(0xffffffffu, before, src) * p.blocks;
+    }
   } else {
     const int span = (units + S::kThreads - 1) / S::kThreads;  // units a thread adds up
     const int u0 = min(static_cast<int>(threadIdx.x) * span, units), u1 = min(u0 + span, units);
-    int mine = 0, most = 0;
-    for (int u = u0; u < u1; ++u) {
-      const int n = tiles_of<kTile>(p.c, u);
-      mine += n;
-      most = max(most, n);
-    }
-    most = __reduce_max_sync(0xffffffffu, most);
+    int mine = 0;
+    for (int u = u0; u < u1; ++u) mine += tiles_of<kTile>(p.c, u);
     int incl = warp_prefix(mine, lane);
-    if (lane == 31) {
-      s_sums[warp] = incl;
-      s_most[warp] = most;
-    }
-    if (threadIdx.x == 0) s_at[0] = 0;
+    if (lane == 31) s_sums[warp] = incl;
     __syncthreads();
     int total = 0;
     for (int w = 0; w < S::kWarps; ++w) {
       if (w < warp) incl += s_sums[w];
       total += s_sums[w];
-      most = max(most, s_most[w]);
     }
     const int before = (incl - mine) * p.blocks;
-    // (no more than one unit a thread where a CTA takes a row block)
-    const int u = static_cast<int>(blockIdx.x) / p.blocks;
-    const bool one = units * p.blocks <= ctas;
-    if (one && static_cast<int>(threadIdx.x) == u && u < units) {
-      s_unit[0] = before + (static_cast<int>(blockIdx.x) - u * p.blocks) * mine;
-      s_at[0] = mine;
-    }
-    __syncthreads();
-    divide(total * p.blocks, most, s_unit[0], one ? s_at[0] : 0);
-    __syncthreads();
+    total *= p.blocks;
+    chunk = even_chunk(total);
+    const int from = static_cast<int>(blockIdx.x) * chunk;
+    share_out(from, min(chunk, total - from));
     // the thread that holds a warp's first tile
     const int share = (chunk + S::kWarps - 1) / S::kWarps;
     const int first = tile - warp * share;
@@ -992,6 +1004,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   if (shared[0] < -1 && shared[1] < -1) return;
 
   // ---- row blocks that CTAs share: the last one to come joins them, in order
+  auto first_cta = [&](const Part& x) { return own0 >= 0 ? own0 : x.first / chunk; };
+  auto last_cta = [&](const Part& x) {
+    return own0 >= 0 ? own0 + (x.count - 1) / chunk : (x.first + x.count - 1) / chunk;
+  };
   fence_acq_rel_gpu();
   __syncthreads();
   __shared__ int s_last[2];
@@ -1000,7 +1016,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     int last = 0;
     if (w >= -1) {
       const Part& part = w < 0 ? s_head[0] : s_tail[w];
-      const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
+      const int c0 = first_cta(part), c1 = last_cta(part);
       if (atomicAdd(p.tickets + c0, 1) == c1 - c0) {
         p.tickets[c0] = 0;  // for the next call
         last = 1;
@@ -1018,7 +1034,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int which = both == 2 ? warp & 1 : s_last[1];
   const int warps = S::kWarps / both, mine = warp / both;
   const Part part = shared[which] < 0 ? s_head[0] : s_tail[shared[which]];
-  const int c0 = part.first / chunk, c1 = (part.first + part.count - 1) / chunk;
+  const int c0 = first_cta(part), c1 = last_cta(part);
   const int unit = part.block / p.blocks, row0 = (part.block - unit * p.blocks) * kRows;
   const int rows = min(kRows, p.rows - row0);
   // (rounds as many as the row block with more rows takes: every warp is at

@@ -58,8 +58,8 @@ using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
 // Attention.  The tiles (64 slots) of all row blocks -- up to 16 query rows of
 // a unit -- form one sequence, of which every CTA takes an equal run, and every
-// warp of it a run of that.  Where there are few short row blocks, a CTA takes
-// one each instead.
+// warp of it a run of that; or, where they come out about even that way, each row
+// block has CTAs of its own.
 struct Q4AttendParams {
   CUtensorMap map_k, map_v;    // codes: [units * capacity] rows of 64 bytes, boxes of 32 rows
   Q4Cache c;
