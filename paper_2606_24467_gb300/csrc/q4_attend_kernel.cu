@@ -31,9 +31,10 @@
 //     the output does where many slots share the attention.  (With n and m they
 //     grow with sum p; the tensor cores truncate their sums, so that at 128K slots
 //     3 % of the output were lost.)  The 7.5 comes off once a tile, by 7.5 sum p s
-//     from a product of the same operands with ones.  With p in fp16 (relative
-//     error 2^-12) the weights of group J's codes are p s_J (rounded once more),
-//     those of its middle p; the middles' term is a product of its own.  Scales and
+//     from a product of the same operands with ones.  p is fp16 (relative error
+//     2^-12); the weights of group J's codes are p s_J, rounded once more for bf16
+//     outputs and once in all for f16 (kFine), those of its middle p; the middles'
+//     term is a product of its own.  Scales and
 //     middles are fp16 too (scales exactly, middles to 2^-12) against a power of
 //     two that follows the largest of both, for scales down to 2^-21 of it.
 // Eight lanes of a warp need the same slot's scales, so one lane converts them
@@ -42,6 +43,8 @@
 // Softmax references are raised only when a logit passes them by 2^8, so the
 // outputs are hardly ever rescaled.
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "ckv_device.cuh"
 #include "q4_params.h"
@@ -79,7 +82,7 @@ struct Shape {
   static constexpr int kScaleTile = kTile * 16;  // K's scales of the tile at hand, fp32
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
-  static constexpr int kScales = kWarps * kScaleTile;
+  static constexpr int kScales = 2 * kWarps * kScaleTile;  // (V's too where they are kept in fp32)
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
   static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
   static_assert(kTile % 16 == 0, "steps");
@@ -328,7 +331,9 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
   }
 }
 
-template <int NB, bool kPos>
+// kPos: slots are seen by position.  kFine: f16 outputs, whose rounding is as
+// small as that of the weights: these are then rounded once.
+template <int NB, bool kPos, bool kFine>
 __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     attend_kernel(const __grid_constant__ Q4AttendParams p) {
   using S = Shape<NB>;
@@ -345,7 +350,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   const uint32_t codes = base + warp * S::kStages * 2 * kCodeTile;
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
-  const uint32_t scales = base + S::kCodes + S::kSide + warp * kScaleTile;
+  const uint32_t scales = base + S::kCodes + S::kSide + warp * 2 * kScaleTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
   if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
@@ -628,15 +633,23 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 #pragma unroll
       for (int i = 0; i < kLane; ++i) {
         const float s0 = bf_lo(w[i].x) * f, s1 = bf_hi(w[i].x) * f, s2 = bf_lo(w[i].y) * f, s3 = bf_hi(w[i].y) * f;
-        const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
         // middles: m + 7.5 s
         const uint32_t m01 = pack_half2(fmaf(s0, 7.5f, bf_lo(w[i].z) * f), fmaf(s1, 7.5f, bf_hi(w[i].z) * f));
         const uint32_t m23 = pack_half2(fmaf(s2, 7.5f, bf_lo(w[i].w) * f), fmaf(s3, 7.5f, bf_hi(w[i].w) * f));
-        // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
-        const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
-        if (lane + 32 * i < kTile) sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
-               make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), m01, m23));
+        uint32_t a = 0u, b = 0u;
+        if (kFine) {
+          if (lane + 32 * i < kTile)
+            sts128(scales + kScaleTile + (lane + 32 * i) * 16,
+                   make_uint4(__float_as_uint(s0), __float_as_uint(s1), __float_as_uint(s2), __float_as_uint(s3)));
+        } else {
+          // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
+          const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
+          a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
+        }
+        if (lane + 32 * i < kTile)
+          sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
+                 make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), m01, m23));
       }
       __syncwarp();
     }
@@ -808,14 +821,24 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         for (int i = 0; i < 4; ++i) mass[nb][i] = 0.f;
 #pragma unroll
       for (int h = 0; h < kSteps; ++h) {
-        const uint32_t pair = sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
-        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * kQ4ParamBytes);
+        // scales: of slots g and g + 8, or of two pairs of slots
+        const uint32_t pair = kFine ? scales + kScaleTile + (h * 16 + g) * 16 + J * 4
+                                    : sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
+        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * 16);
         const uint32_t x = v[2 * h], y = v[2 * h + 1], xh = x >> 8, yh = y >> 8;
         const uint32_t a0 = x & 0x000f000fu, a1 = x & 0x00f000f0u, a2 = y & 0x000f000fu, a3 = y & 0x00f000f0u;
         const uint32_t b0 = xh & 0x000f000fu, b1 = xh & 0x00f000f0u, b2 = yh & 0x000f000fu, b3 = yh & 0x00f000f0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const uint32_t q0 = mul_half2(p0[nb][h], sa), q1 = mul_half2(p1[nb][h], sb);
+          uint32_t q0, q1;
+          if (kFine) {
+            const float fa = __uint_as_float(sa), fb = __uint_as_float(sb);
+            q0 = transpose8(pack_half2(z[nb][h][0] * fa, z[nb][h][1] * fa));
+            q1 = transpose8(pack_half2(z[nb][h][2] * fb, z[nb][h][3] * fb));
+          } else {
+            q0 = mul_half2(p0[nb][h], sa);
+            q1 = mul_half2(p1[nb][h], sb);
+          }
           mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
           mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
           mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
@@ -1157,9 +1180,9 @@ __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_co
   p.c.weights[slot] = old + add;
 }
 
-template <int NB, bool kPos>
+template <int NB, bool kPos, bool kFine>
 cudaError_t launch(const Q4AttendParams& p, int sms, cudaStream_t stream) {
-  return launch_dependent(attend_kernel<NB, kPos>, dim3(sms), Shape<NB>::kThreads, Shape<NB>::kSmem, stream, p);
+  return launch_dependent(attend_kernel<NB, kPos, kFine>, dim3(sms), Shape<NB>::kThreads, Shape<NB>::kSmem, stream, p);
 }
 
 }  // namespace
@@ -1172,16 +1195,26 @@ cudaError_t q4_attend_set_smem_limit() {
   auto set = [&](auto* f, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  set(attend_kernel<1, false>, Shape<1>::kSmem);
-  set(attend_kernel<1, true>, Shape<1>::kSmem);
-  set(attend_kernel<2, false>, Shape<2>::kSmem);
-  set(attend_kernel<2, true>, Shape<2>::kSmem);
+  set(attend_kernel<1, false, false>, Shape<1>::kSmem);
+  set(attend_kernel<1, false, true>, Shape<1>::kSmem);
+  set(attend_kernel<1, true, false>, Shape<1>::kSmem);
+  set(attend_kernel<1, true, true>, Shape<1>::kSmem);
+  set(attend_kernel<2, false, false>, Shape<2>::kSmem);
+  set(attend_kernel<2, false, true>, Shape<2>::kSmem);
+  set(attend_kernel<2, true, false>, Shape<2>::kSmem);
+  set(attend_kernel<2, true, true>, Shape<2>::kSmem);
   return e;
 }
 
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t stream) {
-  if (p.rows <= 8) return p.q_positions ? launch<1, true>(p, sms, stream) : launch<1, false>(p, sms, stream);
-  return p.q_positions ? launch<2, true>(p, sms, stream) : launch<2, false>(p, sms, stream);
+  auto choose = [&](auto positions, auto fine) {
+    return p.rows <= 8 ? launch<1, decltype(positions)::value, decltype(fine)::value>(p, sms, stream)
+                       : launch<2, decltype(positions)::value, decltype(fine)::value>(p, sms, stream);
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (p.is_bf16) return p.q_positions ? choose(Yes{}, No{}) : choose(No{}, No{});
+  return p.q_positions ? choose(Yes{}, Yes{}) : choose(No{}, Yes{});
 }
 
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t stream) {
