@@ -438,7 +438,8 @@ typedef struct ckv_q4_queries {
 } ckv_q4_queries;
 
 /* Bytes of workspace that compresskv_q4_attend (with these heads and query
- * tokens, or fewer of either) and compresskv_q4_evict need for the cache;
+ * tokens, or fewer of either) and compresskv_q4_evict need for the cache
+ * (where weights are kept, 4 bytes a slot and query row for the logits);
  * num_q_heads = num_queries = 0: for the eviction alone.  0 if invalid. */
 size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, int32_t num_queries);
 
@@ -495,8 +496,10 @@ int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t gr
  * lse: optional device float [batch][num_q_heads][num_queries].
  * accumulate: p, summed over the queries and the group's heads, is added to
  *   each visible slot's weight.
- * Logits, softmax sums and outputs are held in fp32; the results do not
- * depend on what else runs, and are the same bits on every call. */
+ * Logits, softmax sums and outputs are held in fp32; inside the sum over the
+ * slots p is rounded to fp16 (and p times a slot's scale, and the middle of a
+ * group's range), each by at most 2^-12 of itself.  The results are the same
+ * bits on every call with the same shapes, lengths and SMs. */
 int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const void* q,
                          const int32_t* q_positions, void* out, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);

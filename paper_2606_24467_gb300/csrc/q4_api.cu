@@ -40,6 +40,7 @@ int check_cache(const ckv_q4_cache* c, bool pointers = true) {
 }
 
 int units_of(const ckv_q4_cache* c) { return c->batch * c->num_kv_heads; }
+long long slots_of(const ckv_q4_cache* c) { return static_cast<long long>(units_of(c)) * c->capacity; }
 
 Q4Cache device_cache(const ckv_q4_cache* c) {
   Q4Cache d;
@@ -73,8 +74,8 @@ struct AttendArea {
 };
 AttendArea attend_area(const ckv_q4_cache* c, int num_q_heads, int num_queries, bool accumulate) {
   const size_t rows = static_cast<size_t>(num_q_heads / c->num_kv_heads) * num_queries;
-  const size_t brows = q4_block_rows(static_cast<int>(rows));
-  const size_t heads = kQ4MaxCtas * static_cast<size_t>(q4_attend_warps(static_cast<int>(rows))) * brows;
+  const size_t brows = q4_block_rows(static_cast<int>(rows), slots_of(c));
+  const size_t heads = kQ4MaxCtas * kQ4Warps * brows;
   const size_t ctas = kQ4MaxCtas * 2 * brows;
   AttendArea a;
   a.head_ml = kQ4HeaderBytes;
@@ -162,8 +163,6 @@ size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, 
     if (check_heads(c, num_q_heads, num_queries) != CKV_OK) return 0;
     const bool weights = c->weights != nullptr;
     n = std::max(n, attend_area(c, num_q_heads, num_queries, weights).bytes);
-    // (fewer rows may take smaller row blocks and then more warps)
-    n = std::max(n, attend_area(c, c->num_kv_heads, 1, weights).bytes);
   }
   return n;
 }
@@ -281,11 +280,10 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.group = a->num_q_heads / c->num_kv_heads;
   P.num_queries = a->num_queries;
   P.rows = P.group * P.num_queries;
-  P.blocks = (P.rows + q4_block_rows(P.rows) - 1) / q4_block_rows(P.rows);
-  const int tile = q4_attend_tile(P.rows);
-  const unsigned long long slots = static_cast<unsigned long long>(units_of(c)) * c->capacity;
-  if ((rc = make_row64_map(c->k_codes, slots, tile, &P.map_k)) != CKV_OK) return rc;
-  if ((rc = make_row64_map(c->v_codes, slots, tile, &P.map_v)) != CKV_OK) return rc;
+  P.block_rows = q4_block_rows(P.rows, slots_of(c));
+  P.blocks = (P.rows + P.block_rows - 1) / P.block_rows;
+  if ((rc = make_row64_map(c->k_codes, slots_of(c), kQ4Tile, &P.map_k)) != CKV_OK) return rc;
+  if ((rc = make_row64_map(c->v_codes, slots_of(c), kQ4Tile, &P.map_v)) != CKV_OK) return rc;
   P.c = device_cache(c);
   P.q = static_cast<const uint16_t*>(q);
   P.out = static_cast<uint16_t*>(out);
@@ -304,7 +302,7 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.accumulate = a->accumulate != 0;
   P.status = static_cast<int*>(workspace);
   // no more CTAs than there can be tiles
-  const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + tile - 1) / tile) * P.blocks;
+  const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + kQ4Tile - 1) / kQ4Tile) * P.blocks;
   sms = static_cast<int>(std::min<long long>({sms, kQ4MaxCtas, tiles}));
   P.tickets = reinterpret_cast<int*>(ws + kTicketBytes);
   P.head_ml = reinterpret_cast<float2*>(ws + area.head_ml);

@@ -60,8 +60,13 @@ constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p 
 constexpr uint32_t kFifteen = 0x000f000fu;  // 15 * 2^-24 twice: twice a code's middle
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
-constexpr int kMinTiles = 8;   // least tiles of a CTA that shares row blocks: one a warp
-constexpr int kSoloTiles = 4;  // most tiles a warp of a row block that one CTA takes
+// A row block of up to two tiles a warp is one CTA's; longer ones are shared,
+// by CTAs of at least four tiles.  Joining over CTAs costs about 3 us, a warp's
+// further tile 2.5.  Eight units of 777 slots (two tiles a warp): 10.0 us, and
+// 10.8 shared; of 2048 slots (four): 15.4 on one CTA each, 10.8 shared; of 4096
+// slots by CTAs of 2, 4, 8 and 16 tiles: 10.8, 11.0, 11.4 and 13.6 us.
+constexpr int kMinTiles = 4;
+constexpr int kSoloTiles = 2;
 
 // Eight warps of 64 slots a step with the next 64 on their way: 160 KB a CTA.
 // More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot:
@@ -71,8 +76,8 @@ constexpr int kSoloTiles = 4;  // most tiles a warp of a row block that one CTA 
 // positions lie in an area of their own.
 template <int NB>
 struct Shape {
-  static constexpr int kTile = 64;  // slots
-  static constexpr int kWarps = 8;
+  static constexpr int kTile = kQ4Tile;
+  static constexpr int kWarps = kQ4Warps;
   static constexpr int kStages = 2;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kSteps = kTile / 16;
@@ -1187,9 +1192,6 @@ cudaError_t launch(const Q4AttendParams& p, int sms, cudaStream_t stream) {
 
 }  // namespace
 
-int q4_attend_tile(int rows) { return rows <= 8 ? Shape<1>::kTile : Shape<2>::kTile; }
-int q4_attend_warps(int rows) { return rows <= 8 ? Shape<1>::kWarps : Shape<2>::kWarps; }
-
 cudaError_t q4_attend_set_smem_limit() {
   cudaError_t e = cudaSuccess;
   auto set = [&](auto* f, int bytes) {
@@ -1208,8 +1210,8 @@ cudaError_t q4_attend_set_smem_limit() {
 
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t stream) {
   auto choose = [&](auto positions, auto fine) {
-    return p.rows <= 8 ? launch<1, decltype(positions)::value, decltype(fine)::value>(p, sms, stream)
-                       : launch<2, decltype(positions)::value, decltype(fine)::value>(p, sms, stream);
+    return p.block_rows == 8 ? launch<1, decltype(positions)::value, decltype(fine)::value>(p, sms, stream)
+                             : launch<2, decltype(positions)::value, decltype(fine)::value>(p, sms, stream);
   };
   using Yes = std::true_type;
   using No = std::false_type;

@@ -30,7 +30,7 @@ namespace {
 constexpr int kBins = 256;
 constexpr int kRanked = 64;  // slots that are ranked directly
 constexpr int kItems = 16;   // keys a lane holds at most
-constexpr int kShortItems = 5;  // ... in a CTA of 256 threads for short units
+constexpr int kShortItems = 5;  // ... in CTAs for short units
 
 // Order-preserving key of a weight: larger weight, larger key; -0 and +0 are
 // one, NaN lies below everything.
@@ -77,7 +77,7 @@ __device__ __forceinline__ int4 remote_words(uint32_t addr, uint32_t rank) {
 
 // kHold: keys a lane holds (0: none, they are read again).
 template <int kThreads, int kHold, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kHold == kShortItems ? 6 : 1) evict_kernel(const __grid_constant__ Q4EvictParams p) {
+__global__ void __launch_bounds__(kThreads, kHold && kHold <= 8 ? 1536 / kThreads : 1) evict_kernel(const __grid_constant__ Q4EvictParams p) {
   constexpr int kWarps = kThreads / 32;
   constexpr int kHists = kCluster ? 4 : 1;  // one a pass where other CTAs read it
   extern __shared__ int32_t s_lists[];      // a single CTA's holes and rows
@@ -418,7 +418,9 @@ cudaError_t launch_q4_evict(const Q4EvictParams& params, int sms, cudaStream_t s
   if (p.cluster > 1)
     return cap <= 8192 * p.cluster ? launch<1024, 8, true>(p, stream) : launch<1024, kItems, true>(p, stream);
   if (cap <= 256 * kShortItems) return launch<256, kShortItems, false>(p, stream);
-  if (cap <= 256 * kItems) return launch<256, kItems, false>(p, stream);
+  if (cap <= 512 * kShortItems) return launch<512, kShortItems, false>(p, stream);
+  if (cap <= 512 * 8) return launch<512, 8, false>(p, stream);
+  if (cap <= 1024 * 8) return launch<1024, 8, false>(p, stream);
   return launch<1024, kItems, false>(p, stream);
 }
 

@@ -56,8 +56,17 @@ using Q4AppendParams = Q4WriteParams<0>;
 using Q4GatherParams = Q4WriteParams<kQ4SeqTable>;
 using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 
-// Attention.  The tiles (64 slots) of all row blocks -- up to 16 query rows of
-// a unit -- form one sequence, of which every CTA takes an equal run, and every
+constexpr int kQ4Tile = 64;  // attention: slots of a tile,
+constexpr int kQ4Warps = 8;  // warps of a CTA (there is one an SM),
+// query rows of a row block.  16 rows share the work on their codes, but leave
+// fewer tiles to a warp and take every register: 16 rows a unit (two heads of
+// eight query heads, bf16) take 39 us in blocks of 16 and 35 in blocks of 8 at
+// 64 units of 1000 to 8000 slots, four of 777 tokens 14 and 10, but 16 rows of
+// 32 units of 128K slots 201 and 241, 20 of 512 units of 1000 to 8000 (with
+// weights) 332 and 386.  `slots`: of all units.
+constexpr int q4_block_rows(int rows, long long slots) { return rows <= 8 || slots <= 1 << 20 ? 8 : 16; }
+
+// Attention.  The tiles of all row blocks -- some query rows of a unit -- form one sequence, of which every CTA takes an equal run, and every
 // warp of it a run of that; or, where they come out about even that way, each row
 // block has CTAs of its own.
 struct Q4AttendParams {
@@ -70,7 +79,7 @@ struct Q4AttendParams {
   long long q_bs, q_hs, q_qs, o_bs, o_hs, o_qs;  // elements
   float scale_log2;            // softmax scale * log2(e)
   int num_q_heads, group, num_queries, is_bf16, accumulate;
-  int rows, blocks;            // query rows of a unit, and row blocks of them
+  int rows, block_rows, blocks;  // query rows of a unit, of a row block, and row blocks of a unit
   int* status;
   // workspace
   int* tickets;                // [CTAs]: CTAs done with the row block that starts in one and goes on
@@ -117,9 +126,6 @@ cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads, size_
 cudaError_t launch_q4_append(const Q4AppendParams& p, int max_rows, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherParams& p, cudaStream_t s);
 cudaError_t launch_q4_gather(const Q4GatherUnitParams& p, cudaStream_t s);
-constexpr int q4_block_rows(int rows) { return rows <= 8 ? 8 : 16; }
-int q4_attend_tile(int rows);   // slots of a tile, for so many query rows a unit
-int q4_attend_warps(int rows);  // warps of a CTA; there is one an SM
 cudaError_t q4_attend_set_smem_limit();
 cudaError_t launch_q4_attend(const Q4AttendParams& p, int sms, cudaStream_t s);
 cudaError_t launch_q4_weights(const Q4AttendParams& p, cudaStream_t s);

@@ -33,7 +33,7 @@ namespace ckv {
 namespace {
 
 constexpr int kWriteThreads = 256;
-constexpr int kSmallRows = 64;  // appends of up to this many rows a sequence: one CTA a unit
+constexpr int kSmallRows = 32;  // appends of up to this many rows a sequence: one CTA a unit
 
 // The two numbers of a word.
 template <bool kBf16>

@@ -544,6 +544,39 @@ def test_attend_averages_many_slots(cuda_device, dtype):
             assert ((out[b, h, 0].double() - want).abs() <= tol).all(), (b, h)
 
 
+def test_attend_with_256_rows_a_unit(cuda_device):
+    gen = torch.Generator().manual_seed(71)
+    c = random_cache(1, 1, 500, [[490]], cuda_device, gen)
+    q = torch.randn((1, 16, 16, 128), generator=gen).bfloat16().to(cuda_device)
+    run_attend(c, q, q_positions=torch.randint(0, 1000, (1, 16), generator=gen).int().to(cuda_device))
+
+
+@pytest.mark.parametrize("lens", ["empty", "tile", "ragged", "long"])
+@pytest.mark.parametrize("group,n,causal", [(12, 1, False), (7, 4, True), (3, 5, False), (16, 16, True)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attend_of_a_large_cache(cuda_device, lens, group, n, causal, dtype):
+    """More than 2^20 slots, where row blocks have 16 rows, few of them in use."""
+    le = np.array(LENS[lens])
+    gen = torch.Generator().manual_seed(group + n)
+    small = random_cache(*le.shape, int(le.max()) + 40, le, cuda_device, gen)
+    c = blank(*le.shape, 2 ** 20 // le.size + 32, cuda_device)
+    used = small.capacity
+    for name in BYTES[:-1]:
+        getattr(c, name)[:, :, :used] = getattr(small, name)
+    c.lengths.copy_(small.lengths)
+    q = torch.randn((le.shape[0], le.shape[1] * group, n, 128), generator=gen).to(dtype).to(cuda_device)
+    at = None
+    if causal:
+        at = torch.randint(-1, 2 * used, (le.shape[0], n), generator=gen).int().to(cuda_device)
+    ws = ckv.q4_workspace(c, q.shape[1], n)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device=cuda_device)
+    ckv.q4_attend(c, q, out, ws, q_positions=at, lse=lse, accumulate=True)
+    assert ckv.read_device_status(ws) == 0
+    assert torch.isnan(c.weights[:, :, used:]).all() and (c.positions[:, :, used:] == -7).all()
+    after = c.weights[:, :, :used].cpu().numpy()
+    check_attend(host(small), q, out, lse, host(small)["weights"], after, 128 ** -0.5, at)
+
+
 def test_attend_all_empty(cuda_device):
     c = blank(3, 2, 64, cuda_device)
     q = torch.randn((3, 8, 2, 128), device=cuda_device).half()
@@ -709,7 +742,7 @@ def test_evict_weights(cuda_device, kind, n):
 
 
 @pytest.mark.parametrize("units,n", [(80, 5000), (2, 210001), (80, 26001), (20, 9000), (1, 26000),
-                                     (80, 1250), (3, 70000)])
+                                     (80, 1250), (3, 70000), (80, 9000)])
 def test_evict_of_long_units(cuda_device, units, n):
     """Units that a CTA or a cluster of them holds in shared memory, or does not
     (the first and the last unit are compared)."""

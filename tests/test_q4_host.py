@@ -252,6 +252,7 @@ def test_attend_refusals():
     assert call(num_q_heads=6) == bad and call(num_queries=0) == bad and call(dtype=7) == bad
     assert call(num_queries=17) == B.CKV_ERR_UNSUPPORTED
     assert call(num_q_heads=260) == B.CKV_ERR_UNSUPPORTED
+    assert call(num_q_heads=256, num_queries=5) == B.CKV_ERR_UNSUPPORTED  # 320 rows a unit
     assert call(scale=-1.0) == bad and call(scale=float("inf")) == bad and call(scale=float("nan")) == bad
     assert call(q=None) == bad and call(q=(1 << 30) + 8) == bad
     assert call(q_head_stride=100) == bad and call(out_query_stride=0) == bad
