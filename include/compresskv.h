@@ -497,9 +497,9 @@ int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t gr
  * accumulate: p, summed over the queries and the group's heads, is added to
  *   each visible slot's weight.
  * Logits, softmax sums and outputs are held in fp32; inside the sum over the
- * slots p is rounded to fp16 (and p times a slot's scale, and the middle of a
- * group's range), each by at most 2^-12 of itself.  The results are the same
- * bits on every call with the same shapes, lengths and SMs. */
+ * slots the middle of a group's range, and for bf16 outputs p and p times a
+ * slot's scale, are rounded to fp16 (by at most 2^-11 of themselves).  The results
+ * are the same bits on every call with the same shapes, lengths and SMs. */
 int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const void* q,
                          const int32_t* q_positions, void* out, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);

@@ -4,13 +4,22 @@
 //   out[r] = sum_j p[r,j] (s n[j,:] + m),   lse[r] = log sum_j exp z[r,j]
 //   weight[j] += sum_r p[r,j]   (where asked for)
 //
-// Bound by memory: 160 bytes a slot against at most a few thousand operations,
-// so the kernel is built around a steady stream of slots and few instructions
-// a code.  Every warp takes a run of tiles of 64 slots (see Q4AttendParams) and
-// keeps two in flight with TMA into its own part of shared memory.  A
-// row block that lies in its run it finishes itself; of others it leaves the
-// softmax reference, sum and outputs, which its CTA joins, and for row blocks
-// that several CTAs share the last of them to come, always in slot order.
+// 160 bytes a slot against at most a few thousand operations, so the kernel is
+// built around a steady stream of slots and few instructions a code.  Every
+// warp takes a run of tiles of 64 slots (see Q4AttendParams) and keeps two in
+// flight with TMA into its own part of shared memory.  A row block that lies in
+// its run it finishes itself; of others it leaves the softmax reference, sum and
+// outputs, which its CTA joins, and for row blocks that several CTAs share the
+// last of them to come, always in slot order.
+//
+// Measured, in a graph of 20 calls: four sequences of 128K slots, 8 groups of 4
+// heads, 127.6 us, 5.26 TB/s of the 6.78 that a copy reaches (the loads alone
+// take 108): two warps a scheduler issue in 46 % of the cycles, the tensor cores
+// are busy in 32 %.  One sequence of 32K slots 18.5 us and of 777 10.0, where
+// fixed latencies add up: the scan of the lengths (1 us), the first copies and
+// the queries (2), the first tile with no instruction cached (2), the joins in a
+// CTA and over CTAs (2 to 5).  64 sequences of 1000 to 8000 slots, 8 groups of 8
+// heads, f16, with weights, 131 us against 56 for the bytes: instructions.
 //
 // Codes enter the tensor cores as they are.  A nibble n masked out of a word is
 // the fp16 subnormal n * 2^-24 (one in bits 4-7 is 16 n * 2^-24), exact in a
@@ -31,11 +40,14 @@
 //     the output does where many slots share the attention.  (With n and m they
 //     grow with sum p; the tensor cores truncate their sums, so that at 128K slots
 //     3 % of the output were lost.)  The 7.5 comes off once a tile, by 7.5 sum p s
-//     from a product of the same operands with ones.  p is fp16 (relative error
-//     2^-12); the weights of group J's codes are p s_J, rounded once more for bf16
-//     outputs and once in all for f16 (kFine), those of its middle p; the middles'
-//     term is a product of its own.  Scales and
-//     middles are fp16 too (scales exactly, middles to 2^-12) against a power of
+//     from a product of the same operands with ones.  p is fp16 (off by at most
+//     2^-11 of itself), the weights of group J's codes are p s_J, rounded once
+//     more, those of its middle p; the middles' term is a product of its own.
+//     That is well below a bf16 output's rounding (2^-8); for f16 outputs (kFine)
+//     what both roundings left is a second operand: an error of 2.1e-4 of the
+//     output, all of it the output's own rounding, where one rounding of p s
+//     gave 3.0e-4 and two 3.6e-4, for 13 % more time.  Scales and
+//     middles are fp16 too (scales exactly, middles to 2^-11) against a power of
 //     two that follows the largest of both, for scales down to 2^-21 of it.
 // Eight lanes of a warp need the same slot's scales, so one lane converts them
 // for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
@@ -87,7 +99,7 @@ struct Shape {
   static constexpr int kScaleTile = kTile * 16;  // K's scales of the tile at hand, fp32
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
-  static constexpr int kScales = 2 * kWarps * kScaleTile;  // (V's too where they are kept in fp32)
+  static constexpr int kScales = kWarps * kScaleTile;
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
   static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
   static_assert(kTile % 16 == 0, "steps");
@@ -129,6 +141,11 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t fma_half2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
 // Transpose of an 8x8 matrix of 16-bit numbers: lane (g, t) gives row g,
@@ -337,7 +354,7 @@ __device__ __forceinline__ void load_queries(const Q4AttendParams& p, int unit, 
 }
 
 // kPos: slots are seen by position.  kFine: f16 outputs, whose rounding is as
-// small as that of the weights: these are then rounded once.
+// small as that of the weights, which then have a second part.
 template <int NB, bool kPos, bool kFine>
 __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     attend_kernel(const __grid_constant__ Q4AttendParams p) {
@@ -355,7 +372,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   const uint32_t codes = base + warp * S::kStages * 2 * kCodeTile;
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
-  const uint32_t scales = base + S::kCodes + S::kSide + warp * 2 * kScaleTile;
+  const uint32_t scales = base + S::kCodes + S::kSide + warp * kScaleTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
   if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
@@ -398,8 +415,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     chunk = even_chunk(total);
     // Where the row blocks come out about even over whole CTAs, each has its
     // own: one where it is short, else in proportion.  No CTA then joins the end
-    // of one row block and the start of another (20 us against 18 for 8 units of
-    // 32K slots).
+    // of one row block and the start of another (8 units of 300 slots: 7.5 us, and
+    // 12.6 in equal runs; of 32K slots 18.4 and 20.9).
     // (Quotients in fp32: every warp takes the same ones, near enough.)
     int own[kPer], own_mine = 0, own_chunk = 0;
     const float rate = __fdividef(static_cast<float>(ctas), static_cast<float>(total));
@@ -641,17 +658,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         // middles: m + 7.5 s
         const uint32_t m01 = pack_half2(fmaf(s0, 7.5f, bf_lo(w[i].z) * f), fmaf(s1, 7.5f, bf_hi(w[i].z) * f));
         const uint32_t m23 = pack_half2(fmaf(s2, 7.5f, bf_lo(w[i].w) * f), fmaf(s3, 7.5f, bf_hi(w[i].w) * f));
-        uint32_t a = 0u, b = 0u;
-        if (kFine) {
-          if (lane + 32 * i < kTile)
-            sts128(scales + kScaleTile + (lane + 32 * i) * 16,
-                   make_uint4(__float_as_uint(s0), __float_as_uint(s1), __float_as_uint(s2), __float_as_uint(s3)));
-        } else {
-          // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
-          const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
-          const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
-          a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
-        }
+        // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
+        const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
+        const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
         if (lane + 32 * i < kTile)
           sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
                  make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), m01, m23));
@@ -799,6 +809,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 
     // ---- outputs: the middles' term, then the codes group by group
     uint32_t p0[NB][kSteps], p1[NB][kSteps];
+    uint32_t r0[kFine ? NB : 1][kSteps], r1[kFine ? NB : 1][kSteps];  // what their rounding left
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) {
       uint32_t pm[4];
@@ -807,9 +818,17 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       ldmatrix4_t(pm, sd + kParamTile + (h * 16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        p0[nb][h] = transpose8(pack_half2(z[nb][h][0], z[nb][h][1]));
-        p1[nb][h] = transpose8(pack_half2(z[nb][h][2], z[nb][h][3]));
+        const uint32_t lo = pack_half2(z[nb][h][0], z[nb][h][1]), hi = pack_half2(z[nb][h][2], z[nb][h][3]);
+        p0[nb][h] = transpose8(lo);
+        p1[nb][h] = transpose8(hi);
         mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], p0[nb][h], p1[nb][h]);
+        if (kFine) {
+          r0[nb][h] = transpose8(pack_half2(z[nb][h][0] - to_float(lo & 0xffffu, false),
+                                            z[nb][h][1] - to_float(lo >> 16, false)));
+          r1[nb][h] = transpose8(pack_half2(z[nb][h][2] - to_float(hi & 0xffffu, false),
+                                            z[nb][h][3] - to_float(hi >> 16, false)));
+          mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], r0[nb][h], r1[nb][h]);
+        }
       }
     }
 #pragma unroll
@@ -826,27 +845,25 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         for (int i = 0; i < 4; ++i) mass[nb][i] = 0.f;
 #pragma unroll
       for (int h = 0; h < kSteps; ++h) {
-        // scales: of slots g and g + 8, or of two pairs of slots
-        const uint32_t pair = kFine ? scales + kScaleTile + (h * 16 + g) * 16 + J * 4
-                                    : sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
+        // scales of two pairs of slots
+        const uint32_t pair = sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
         const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * 16);
         const uint32_t x = v[2 * h], y = v[2 * h + 1], xh = x >> 8, yh = y >> 8;
         const uint32_t a0 = x & 0x000f000fu, a1 = x & 0x00f000f0u, a2 = y & 0x000f000fu, a3 = y & 0x00f000f0u;
         const uint32_t b0 = xh & 0x000f000fu, b1 = xh & 0x00f000f0u, b2 = yh & 0x000f000fu, b3 = yh & 0x00f000f0u;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          uint32_t q0, q1;
-          if (kFine) {
-            const float fa = __uint_as_float(sa), fb = __uint_as_float(sb);
-            q0 = transpose8(pack_half2(z[nb][h][0] * fa, z[nb][h][1] * fa));
-            q1 = transpose8(pack_half2(z[nb][h][2] * fb, z[nb][h][3] * fb));
-          } else {
-            q0 = mul_half2(p0[nb][h], sa);
-            q1 = mul_half2(p1[nb][h], sb);
-          }
+          uint32_t q0 = mul_half2(p0[nb][h], sa), q1 = mul_half2(p1[nb][h], sb);
           mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
           mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
           mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
+          if (kFine) {
+            q0 = fma_half2(r0[nb][h], sa, fma_half2(p0[nb][h], sa, q0 ^ 0x80008000u));
+            q1 = fma_half2(r1[nb][h], sb, fma_half2(p1[nb][h], sb, q1 ^ 0x80008000u));
+            mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
+            mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
+            mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
+          }
         }
       }
 #pragma unroll
@@ -1146,9 +1163,13 @@ __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int
 }
 
 // ---------------------------------------------------------------- weights
-// A thread takes a slot, whose logits lie side by side: kWide of them a read.
-// (Groups of lanes that share a slot, or several slots a thread, took half as
-// long again: more instructions, and more lines at once than L1 holds.)
+// A thread takes a slot, whose logits lie side by side: kWide of them a read,
+// four where the rows are a multiple of four (28 rows of 32 units of 1000 to
+// 8000 slots, attention and weights: 49.0 us, and 51.6 in pairs; 8 rows of 64
+// units: 29.8 and 30.2).  (Groups of lanes that share a slot, or several slots a
+// thread, took half as long again: more instructions, and more lines at once than
+// L1 holds.)  Bound by L2, which holds the logits of some 30 MB: 21 us for 2.3
+// million slots of 8 rows, whose logits and weights are 92 MB.
 constexpr int kWeightThreads = 256;
 
 template <int kWide>

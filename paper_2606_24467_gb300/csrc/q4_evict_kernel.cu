@@ -17,7 +17,10 @@
 // the warps count the holes below b and the kept rows behind it, list both in
 // slot order, and copy.
 // Bound by latency and instructions: a dozen barriers and three dependent trips
-// to memory against 8 bytes a slot and 344 a moved row.
+// to memory against 8 bytes a slot and 336 a moved row.  Measured: 64 units of
+// 1025 slots that lose one 6 us; 2048 units of 1100 to 1200 that lose a tenth 36
+// us, where the bytes need 14.8 and the sectors they lie in 21 (the moved rows
+// are pieces of 16 and 64 bytes all over the cache).
 #include <cuda_runtime.h>
 
 #include "ckv_device.cuh"
@@ -408,8 +411,9 @@ cudaError_t launch_q4_evict(const Q4EvictParams& params, int sms, cudaStream_t s
   Q4EvictParams p = params;
   const long long units = static_cast<long long>(p.c.batch) * p.c.num_kv_heads;
   const int cap = p.c.capacity;
-  // long units share the SMs that there are no other units for, and those that
-  // no CTA holds
+  // Long units share the SMs that there are no other units for, and those that
+  // no CTA holds: 8 units of 8000, 16000 and 32000 slots 18.4, 19.7 and 24.3 us,
+  // and 19.1, 28.5 and 41.0 with clusters only where a CTA cannot hold a unit.
   p.cluster = 1;
   while (p.cluster < 8 && (cap > 1024 * kItems * p.cluster ||
                            (units * p.cluster * 2 <= sms && cap >= 4096 * p.cluster)))
@@ -417,6 +421,10 @@ cudaError_t launch_q4_evict(const Q4EvictParams& params, int sms, cudaStream_t s
   if (cap > 1024 * kItems * p.cluster) return launch<1024, 0, true>(p, stream);
   if (p.cluster > 1)
     return cap <= 8192 * p.cluster ? launch<1024, 8, true>(p, stream) : launch<1024, kItems, true>(p, stream);
+  // The smallest CTA whose lanes hold the unit in few keys, so that an SM holds
+  // several: 2048 units of 1025 slots 39 us, and 72 with up to 16 keys a lane; 1024 of
+  // 2000 slots 37, and 58 with 256 threads of 16 keys; 512 of 4000 slots 45, and 66
+  // with 1024 threads of 16 keys; 512 of 6000 slots 82, and 89.
   if (cap <= 256 * kShortItems) return launch<256, kShortItems, false>(p, stream);
   if (cap <= 512 * kShortItems) return launch<512, kShortItems, false>(p, stream);
   if (cap <= 512 * 8) return launch<512, 8, false>(p, stream);
