@@ -80,10 +80,10 @@ constexpr int kMinScaleExp = -110;     // smaller scales and minima share this r
 constexpr int kMinTiles = 4;
 constexpr int kSoloTiles = 2;
 
-// Eight warps of 64 slots a step with the next 64 on their way: 160 KB a CTA.
-// More warps of fewer slots (12 of 48, 16 of 32) issue more instructions a slot:
-// 117 us against 120 and 124 for four sequences of 128K slots when that was
-// measured, where reading alone takes 108.
+// Eight warps of 64 slots a step with the next 64 on their way: 173 KB a CTA.
+// More warps of fewer slots issue more instructions a slot: for four sequences of
+// 128K slots 127.5 us, and 147 with 12 warps of 32, 140 with 16 and 175 with 8; for
+// one of 777 slots 9.8, and 10.1, 10.8 and 11.4.
 // A warp's stage holds the codes of K and V (swizzled); their params and the
 // positions lie in an area of their own.
 template <int NB>
