@@ -584,6 +584,7 @@ class Q4Cache:
         self.trace = trace
         self.batch, self.num_kv_heads, self.capacity = lead
         self.device = k_codes.device
+        self.index = k_codes.get_device()  # (-1: host memory)
         s = CkvQ4Cache(self.batch, self.num_kv_heads, 128, self.capacity, _addr(k_codes),
                        _addr(v_codes), _addr(k_params), _addr(v_params), _addr(positions),
                        _addr(weights), _addr(lengths),
@@ -622,20 +623,27 @@ def q4_cache(batch: int, num_kv_heads: int, capacity: int, device=None, weights:
 
 def _q4_call(name: str, cache: Q4Cache, stream, *args):
     """Enqueues on `stream` (default: the current stream of the cache's device)."""
-    dev = cache.device
-    if dev.type != "cuda":
+    index = cache.index
+    if index < 0:
         _invalid("the cache must be in device memory")
     fn = _fast(name)
-    if dev.index == torch.cuda.current_device():
-        _check(fn(*args, _raw_stream(stream)), name)
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
     else:
-        with torch.cuda.device(dev):
-            _check(fn(*args, _raw_stream(stream)), name)
+        stream = _raw_stream(stream)
+    if index == torch.cuda.current_device():
+        code = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args, stream)
+    if code != CKV_OK:
+        raise CompressKVError(code, name)
 
 
 def _q4_on_device(cache: Q4Cache, what: str, *tensors):
+    index = cache.index
     for t in tensors:
-        if t is not None and t.device != cache.device:
+        if t is not None and t.get_device() != index:
             _invalid(f"{what} must be on the cache's device")
 
 
@@ -646,7 +654,7 @@ def _q4_rows(cache: Q4Cache, k, v):
         _invalid("k and v must be [rows, H_kv, 128]")
     if v.dtype != k.dtype or strides[2] != 1 or v.stride() != strides:
         _invalid("k and v must share their dtype and strides, head_dim contiguous")
-    if v.is_cuda and v.device != cache.device:  # (else page-locked host memory)
+    if v.get_device() not in (cache.index, -1):  # (-1: page-locked host memory)
         _invalid("v must be on the cache's device")
     return _q4_dtype(k), shape, strides
 
