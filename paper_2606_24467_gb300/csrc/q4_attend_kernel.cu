@@ -19,7 +19,7 @@
 // fixed latencies add up: the scan of the lengths (1 us), the first copies and
 // the queries (2), the first tile with no instruction cached (2), the joins in a
 // CTA and over CTAs (2 to 5).  64 sequences of 1000 to 8000 slots, 8 groups of 8
-// heads, f16, with weights, 131 us against 56 for the bytes: instructions.
+// heads, f16, with weights, 122 us against 56 for the bytes: instructions.
 //
 // Codes enter the tensor cores as they are.  A nibble n masked out of a word is
 // the fp16 subnormal n * 2^-24 (one in bits 4-7 is 16 n * 2^-24), exact in a
@@ -39,14 +39,16 @@
 //     m + 7.5 s, out = sum p s c + sum p (m + 7.5 s): both terms stay as small as
 //     the output does where many slots share the attention.  (With n and m they
 //     grow with sum p; the tensor cores truncate their sums, so that at 128K slots
-//     3 % of the output were lost.)  The 7.5 comes off once a tile, by 7.5 sum p s
-//     from a product of the same operands with ones.  p is fp16 (off by at most
-//     2^-11 of itself), the weights of group J's codes are p s_J, rounded once
-//     more, those of its middle p; the middles' term is a product of its own.
-//     That is well below a bf16 output's rounding (2^-8); for f16 outputs (kFine)
-//     what both roundings left is a second operand: an error of 2.1e-4 of the
-//     output, all of it the output's own rounding, where one rounding of p s
-//     gave 3.0e-4 and two 3.6e-4, for 13 % more time.  Scales and
+//     3 % of the output were lost.)  The 7.5 comes off once a tile, as 7.5 sum p s.
+//     p is fp16 (off by at most 2^-11 of itself), the weights of group J's codes are
+//     p s_J, rounded once more, whose sum is a product with ones; the middles' term
+//     is a product of its own, with p.  That is well below a bf16 output's rounding
+//     (2^-8).  For f16 outputs (kFine) what both roundings left is a second operand;
+//     sum p s is then exact and comes with the middles' product, whose matrix has
+//     rows to spare, before the codes', so that it comes off half way, where the
+//     truncation before and after it cancels.  Error 2.1e-4 of the output, all of it
+//     the output's own rounding (2.7e-4 at 128K slots), where one rounding of p s
+//     gave 3.0e-4 and two 3.6e-4, for 6 % more time than the latter.  Scales and
 //     middles are fp16 too (scales exactly, middles to 2^-11) against a power of
 //     two that follows the largest of both, for scales down to 2^-21 of it.
 // Eight lanes of a warp need the same slot's scales, so one lane converts them
@@ -69,7 +71,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
 constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p s < 2^15
-constexpr uint32_t kFifteen = 0x000f000fu;  // 15 * 2^-24 twice: twice a code's middle
+constexpr uint32_t kOnes = 0x3c003c00u;        // 1 twice
+constexpr float kMiddle = 7.5f / 16777216.0f;  // of the codes, as they are held
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
 // A row block of up to two tiles a warp is one CTA's; longer ones are shared,
@@ -99,7 +102,8 @@ struct Shape {
   static constexpr int kScaleTile = kTile * 16;  // K's scales of the tile at hand, fp32
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
-  static constexpr int kScales = kWarps * kScaleTile;
+  static constexpr int kPairTile = kTile * 8;    // V's scales by pairs of slots, fp16
+  static constexpr int kScales = kWarps * (kScaleTile + kPairTile);
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
   static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
   static_assert(kTile % 16 == 0, "steps");
@@ -188,6 +192,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
+}
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) {
+  asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory");
 }
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row,
                                          uint64_t policy) {
@@ -362,7 +369,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   constexpr int kRows = 8 * NB;
   constexpr int kTile = S::kTile, kSteps = S::kSteps;
   constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
-  constexpr int kScaleTile = S::kScaleTile, kLane = S::kLane;
+  constexpr int kScaleTile = S::kScaleTile, kPairTile = S::kPairTile, kLane = S::kLane;
+  constexpr int kPairBytes = kFine ? 8 : kQ4ParamBytes;  // of V's scales, a slot
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_sums[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
   __shared__ float2 s_ml[S::kWarps][kRows];
@@ -372,7 +380,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   const uint32_t codes = base + warp * S::kStages * 2 * kCodeTile;
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
-  const uint32_t scales = base + S::kCodes + S::kSide + warp * kScaleTile;
+  const uint32_t scales = base + S::kCodes + S::kSide + warp * (kScaleTile + kPairTile);
+  const uint32_t pairs = scales + kScaleTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
   if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
@@ -556,7 +565,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const float f1 = p.scale_log2 * 1024.0f;
   Queries<NB> Q;
   float o[NB][4][2][4];   // [8 rows][group][step][channel, row pair]
-  float om[NB][4];        // middles' term (lanes of g >= 4)
+  float om[NB][2];        // middles' term (lanes of g >= 4)
   float ref[NB][2], l[NB][2];  // rows 2t, 2t + 1
   int vexp = kMinScaleExp;
   bool fresh = true;
@@ -574,7 +583,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         ref[nb][0] = ref[nb][1] = -INFINITY;
         l[nb][0] = l[nb][1] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) om[nb][i] = 0.f;
+        for (int i = 0; i < 2; ++i) om[nb][i] = 0.f;
 #pragma unroll
         for (int J = 0; J < 4; ++J)
 #pragma unroll
@@ -662,9 +671,12 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
         const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
         const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
-        if (lane + 32 * i < kTile)
+        if (lane + 32 * i < kTile) {
+          const uint32_t even = __byte_perm(a, b, 0x5410), odd = __byte_perm(a, b, 0x7632);
           sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
-                 make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), m01, m23));
+                 make_uint4(kFine ? s01 : even, kFine ? s23 : odd, m01, m23));
+          if (kFine) sts64(pairs + (lane + 32 * i) * 8, even, odd);
+        }
       }
       __syncwarp();
     }
@@ -807,29 +819,37 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       }
     }
 
-    // ---- outputs: the middles' term, then the codes group by group
+    // ---- outputs: the sums of p s and p m', then the codes group by group
+    // (lanes of g >= 4: p m' of group g - 4; of g < 4, with kFine: p s of group g)
+    float sums[NB][4];
     uint32_t p0[NB][kSteps], p1[NB][kSteps];
     uint32_t r0[kFine ? NB : 1][kSteps], r1[kFine ? NB : 1][kSteps];  // what their rounding left
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) {
       uint32_t pm[4];
-      // rows of [2 pairs of scales, 4 middles]: rows 4-7 of the transposed
-      // operand are the middles; rows 8-15 repeat rows 0-7
+      // rows of [4 scales (or 2 pairs of them), 4 middles], transposed; rows 8-15 of
+      // the operand repeat rows 0-7
       ldmatrix4_t(pm, sd + kParamTile + (h * 16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const uint32_t lo = pack_half2(z[nb][h][0], z[nb][h][1]), hi = pack_half2(z[nb][h][2], z[nb][h][3]);
         p0[nb][h] = transpose8(lo);
         p1[nb][h] = transpose8(hi);
-        mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], p0[nb][h], p1[nb][h]);
+        if (h == 0) sums[nb][0] = sums[nb][1] = sums[nb][2] = sums[nb][3] = 0.f;
+        mma_f16(sums[nb], pm[0], pm[1], pm[2], pm[3], p0[nb][h], p1[nb][h]);
         if (kFine) {
           r0[nb][h] = transpose8(pack_half2(z[nb][h][0] - to_float(lo & 0xffffu, false),
                                             z[nb][h][1] - to_float(lo >> 16, false)));
           r1[nb][h] = transpose8(pack_half2(z[nb][h][2] - to_float(hi & 0xffffu, false),
                                             z[nb][h][3] - to_float(hi >> 16, false)));
-          mma_f16(om[nb], pm[0], pm[1], pm[2], pm[3], r0[nb][h], r1[nb][h]);
+          mma_f16(sums[nb], pm[0], pm[1], pm[2], pm[3], r0[nb][h], r1[nb][h]);
         }
       }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      om[nb][0] += sums[nb][0];
+      om[nb][1] += sums[nb][1];
     }
 #pragma unroll
     for (int J = 0; J < 4; ++J) {
@@ -838,16 +858,32 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       for (int i = 0; i < kTile / 32; ++i)
         ldmatrix4_t(*reinterpret_cast<uint32_t (*)[4]>(v + 4 * i),
                     cd + kCodeTile + i * 32 * kQ4CodeBytes + (group_mat ^ (J << 4)));
+      // sum of p s; where p s is rounded, of the rounded ones
       float mass[NB][4];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mass[nb][i] = 0.f;
+        for (int i = 0; i < 4; ++i)
+          mass[nb][i] = kFine ? __shfl_sync(0xffffffffu, sums[nb][i & 1], 4 * J + t) : 0.f;
+      auto take_off = [&] {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              o[nb][J][st][i] = fmaf(mass[nb][i], -kMiddle, o[nb][J][st][i]);
+              o[nb][J][st][2 + i] = fmaf(mass[nb][i], -16.0f * kMiddle, o[nb][J][st][2 + i]);
+            }
+      };
 #pragma unroll
       for (int h = 0; h < kSteps; ++h) {
+        // (half way, where it is known: what the sums' truncation takes before, it
+        // gives after)
+        if (kFine && h == kSteps / 2) take_off();
         // scales of two pairs of slots
-        const uint32_t pair = sd + kParamTile + (h * 16 + 2 * t + (J >> 1)) * kQ4ParamBytes + (J & 1) * 4;
-        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * 16);
+        const uint32_t pair = (kFine ? pairs : sd + kParamTile) + (h * 16 + 2 * t + (J >> 1)) * kPairBytes + (J & 1) * 4;
+        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * kPairBytes);
         const uint32_t x = v[2 * h], y = v[2 * h + 1], xh = x >> 8, yh = y >> 8;
         const uint32_t a0 = x & 0x000f000fu, a1 = x & 0x00f000f0u, a2 = y & 0x000f000fu, a3 = y & 0x00f000f0u;
         const uint32_t b0 = xh & 0x000f000fu, b1 = xh & 0x00f000f0u, b2 = yh & 0x000f000fu, b3 = yh & 0x00f000f0u;
@@ -856,25 +892,17 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           uint32_t q0 = mul_half2(p0[nb][h], sa), q1 = mul_half2(p1[nb][h], sb);
           mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
           mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
-          mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
-          if (kFine) {
+          if (!kFine) {
+            mma_f16(mass[nb], kOnes, kOnes, kOnes, kOnes, q0, q1);
+          } else {
             q0 = fma_half2(r0[nb][h], sa, fma_half2(p0[nb][h], sa, q0 ^ 0x80008000u));
             q1 = fma_half2(r1[nb][h], sb, fma_half2(p1[nb][h], sb, q1 ^ 0x80008000u));
             mma_f16(o[nb][J][0], a0, a1, a2, a3, q0, q1);
             mma_f16(o[nb][J][1], b0, b1, b2, b3, q0, q1);
-            mma_f16(mass[nb], kFifteen, kFifteen, kFifteen, kFifteen, q0, q1);
           }
         }
       }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            o[nb][J][st][i] = fmaf(mass[nb][i], -0.5f, o[nb][J][st][i]);
-            o[nb][J][st][2 + i] = fmaf(mass[nb][i], -8.0f, o[nb][J][st][2 + i]);
-          }
+      if (!kFine) take_off();
     }
     if (special) {
       const float bad = __uint_as_float(0x7fc00000u);
