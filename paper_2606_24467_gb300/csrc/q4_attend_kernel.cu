@@ -13,9 +13,9 @@
 // last of them to come, always in slot order.
 //
 // Measured, in a graph of 20 calls: four sequences of 128K slots, 8 groups of 4
-// heads, 127.6 us, 5.26 TB/s of the 6.78 that a copy reaches (the loads alone
+// heads, 128.1 us, 5.24 TB/s of the 6.78 that a copy reaches (the loads alone
 // take 108): two warps a scheduler issue in 46 % of the cycles, the tensor cores
-// are busy in 32 %.  One sequence of 32K slots 18.5 us and of 777 10.0, where
+// are busy in 32 %.  One sequence of 32K slots 18.4 us and of 777 9.9, where
 // fixed latencies add up: the scan of the lengths (1 us), the first copies and
 // the queries (2), the first tile with no instruction cached (2), the joins in a
 // CTA and over CTAs (2 to 5).  64 sequences of 1000 to 8000 slots, 8 groups of 8
@@ -48,7 +48,7 @@
 //     rows to spare, before the codes', so that it comes off half way, where the
 //     truncation before and after it cancels.  Error 2.1e-4 of the output, all of it
 //     the output's own rounding (2.7e-4 at 128K slots), where one rounding of p s
-//     gave 3.0e-4 and two 3.6e-4, for 6 % more time than the latter.  Scales and
+//     gave 3.0e-4 (6 % faster) and two 3.6e-4 (8 %).  Scales and
 //     middles are fp16 too (scales exactly, middles to 2^-11) against a power of
 //     two that follows the largest of both, for scales down to 2^-21 of it.
 // Eight lanes of a warp need the same slot's scales, so one lane converts them
@@ -71,7 +71,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
 constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p s < 2^15
-constexpr uint32_t kOnes = 0x3c003c00u;        // 1 twice
+constexpr uint32_t kOnes = 0x3c003c00u;  // fp16, twice
 constexpr float kMiddle = 7.5f / 16777216.0f;  // of the codes, as they are held
 constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
 
