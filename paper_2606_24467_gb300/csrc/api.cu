@@ -655,6 +655,7 @@ int run_score(const ckv_problem* p, const Info& I, const void* q_win, const void
       if (raw && cudaMemsetAsync(raw + off, 0, bytes, stream) != cudaSuccess) return CKV_ERR_CUDA;
     }
   }
+  int first_launch = 1;
   for (const UnitSet& set : sets) {
     const int u0 = set.u0;
     const int nu = set.u1 - set.u0;
@@ -760,6 +761,8 @@ int run_score(const ckv_problem* p, const Info& I, const void* q_win, const void
     while (P.stages > 2 && score_smem_bytes(P.q_half_bytes, P.stages, P.epi_warps) > smem_cap)
       --P.stages;
     const size_t smem = score_smem_bytes(P.q_half_bytes, P.stages, P.epi_warps);
+    P.wait_inputs = first_launch;
+    first_launch = 0;
     if (given_lse) {  // raw scores come straight out of the scoring kernel
       rc = traced(tr, CKV_KERNEL_SCORE, [&] { return launch_score_lse(P, n_items, smem, stream); });
       if (rc != CKV_OK) return rc;
@@ -770,6 +773,7 @@ int run_score(const ckv_problem* p, const Info& I, const void* q_win, const void
       rc = traced(tr, CKV_KERNEL_SCORE, [&] { return launch_score(P, n_items, smem, stream); });
       if (rc != CKV_OK) return rc;
       P.lse_bias = ws.bias;
+      P.wait_inputs = 0;
       rc = traced(tr, CKV_KERNEL_SCORE, [&] { return launch_score_lse(P, n_items, smem, stream); });
       P.lse_bias = nullptr;
       if (rc != CKV_OK) return rc;

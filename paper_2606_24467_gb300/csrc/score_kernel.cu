@@ -126,6 +126,11 @@ __global__ void __launch_bounds__(Shape<kEpi>::kThreads, Shape<kEpi>::kCtasPerSm
   const int t0 = it.t0;
   const int ntiles = it.t1 - t0;  // >= 1 by construction
 
+  // What a kernel that lets its successor start early (compresskv_gather) has
+  // written may be this call's K.  A call's later launches read what its first
+  // one has waited for.
+  if (p.wait_inputs) pdl_wait();
+
   // ------------------------------------------------------------ set-up
   // Window-query rows of the SRH heads -> shared memory in the UMMA K-major
   // 128-byte-swizzle layout (row r, 16-byte chunk ch of each 64-column half
