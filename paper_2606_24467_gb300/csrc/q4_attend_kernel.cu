@@ -62,6 +62,7 @@
 
 #include "ckv_device.cuh"
 #include "q4_params.h"
+#include "q4_ring.h"
 
 namespace ckv {
 
@@ -570,8 +571,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   int vexp = kMinScaleExp;
   bool fresh = true;
   int seg_tiles = 0;  // tiles of the row block so far
-  uint32_t phase = 0;
-  int stage = 0;
+  TileRing<S::kStages> ring;
   bool failed = false;
 
   for (; left > 0; --left) {
@@ -594,13 +594,13 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       vexp = kMinScaleExp;
       fresh = false;
     }
-    if (!mbar_wait_bounded(bars + 8 * stage, phase, &s_abort, p.status)) {
+    if (!mbar_wait_bounded(bars + 8 * ring.stage, ring.phase, &s_abort, p.status)) {
       failed = true;
       break;
     }
     __syncwarp();
     ++seg_tiles;
-    const uint32_t cd = codes + stage * 2 * kCodeTile, sd = side + stage * kSideBytes;
+    const uint32_t cd = codes + ring.stage * 2 * kCodeTile, sd = side + ring.stage * kSideBytes;
     const int valid = c.valid;
 
     // ---- scales: one or two slots a lane.  Slots behind the length and groups that
@@ -919,11 +919,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     }
     fence_proxy_async_smem();  // (the scales were written into the stage)
     __syncwarp();  // every lane is done with the stage
-    if (to_issue > 0) issue(stage);
-    if (++stage == S::kStages) {
-      stage = 0;
-      phase ^= 1u;
-    }
+    if (to_issue > 0) issue(ring.stage);
+    ring.advance();
 
     // ---- the row block ends here, or this warp's share of it
     const int unit = c.unit, block = c.block, done = c.row - c.unit * p.c.capacity;
@@ -989,9 +986,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   }
   if (failed) {
     // copies in flight end before the shared memory does (or their wait runs out)
-    for (int i = 0; i < S::kStages; ++i) {
+    for (int k = 0; k < ring.in_flight(left); ++k) {
       const uint64_t t0 = globaltimer_ns();
-      while (!mbar_test_wait(bars + 8 * i, phase) && globaltimer_ns() - t0 < 100000000ull) {
+      while (!mbar_test_wait(bars + 8 * ring.stage_of(k), ring.phase_of(k)) && globaltimer_ns() - t0 < 100000000ull) {
       }
     }
   }
