@@ -594,11 +594,12 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       vexp = kMinScaleExp;
       fresh = false;
     }
-    if (!mbar_wait_bounded(bars + 8 * ring.stage, ring.phase, &s_abort, p.status)) {
+    // (all lanes go on, or none: another warp's abort may reach some lanes only)
+    const bool landed = mbar_wait_bounded(bars + 8 * ring.stage, ring.phase, &s_abort, p.status);
+    if (!__all_sync(0xffffffffu, landed)) {
       failed = true;
       break;
     }
-    __syncwarp();
     ++seg_tiles;
     const uint32_t cd = codes + ring.stage * 2 * kCodeTile, sd = side + ring.stage * kSideBytes;
     const int valid = c.valid;
