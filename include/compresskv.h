@@ -533,6 +533,13 @@ int compresskv_read_device_status(const void* workspace, void* stream, int32_t* 
  * CKV_ERR_INVALID_ARG).  Process-wide, one-shot; not for production use. */
 int compresskv_debug_stall_next_fused_call(long long wait_ns);
 
+/* The same for compresskv_q4_attend: one warp of the next call that holds
+ * slots waits, its copies under way, for a barrier that nothing completes.  The
+ * wait runs out after wait_ns and its CTA stops; the status reads
+ * CKV_ERR_DEVICE_TIMEOUT, and compresskv_q4_workspace_init makes the workspace
+ * usable again. */
+int compresskv_debug_stall_next_q4_attend(long long wait_ns);
+
 /* Error-aware layer budgets (Sec. 3.4: the offline per-layer eviction
  * errors, normalised as in Eq. 4, share the total budget after every layer
  * gets a minimum m, no layer above a maximum M; Sec. 4 uses m = 32 and

@@ -52,6 +52,7 @@ EXPORTED = (
     "compresskv_compress_layer_head_budgets",
     "compresskv_read_device_status",
     "compresskv_debug_stall_next_fused_call",
+    "compresskv_debug_stall_next_q4_attend",
     "compresskv_allocate_layer_budgets",
     "compresskv_status_string",
     "compresskv_q4_workspace_size",
@@ -147,6 +148,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
                                                               vp, vp, vp, vp, vp, c_size_t, vp]),
         "compresskv_read_device_status": (c_int32, [vp, vp, i32p]),
         "compresskv_debug_stall_next_fused_call": (c_int32, [ctypes.c_longlong]),
+        "compresskv_debug_stall_next_q4_attend": (c_int32, [ctypes.c_longlong]),
         "compresskv_allocate_layer_budgets": (c_int32, [POINTER(ctypes.c_double), c_int32,
                                                         c_int64, c_int32, c_int32, i32p]),
         "compresskv_status_string": (ctypes.c_char_p, [c_int32]),
@@ -517,6 +519,13 @@ def debug_stall_next_fused_call(wait_ns: int) -> None:
     with CKV_ERR_DEVICE_TIMEOUT after `wait_ns` (see the header)."""
     _check(load().compresskv_debug_stall_next_fused_call(ctypes.c_longlong(int(wait_ns))),
            "compresskv_debug_stall_next_fused_call")
+
+
+def debug_stall_next_q4_attend(wait_ns: int) -> None:
+    """Test hook: one warp of the next q4_attend stalls on purpose and stops its
+    CTA after wait_ns (0 cancels)."""
+    _check(load().compresskv_debug_stall_next_q4_attend(ctypes.c_longlong(int(wait_ns))),
+           "compresskv_debug_stall_next_q4_attend")
 
 
 def read_device_status(ws, stream=None) -> int:

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -17,6 +18,9 @@ using namespace ckv;
 namespace {
 
 constexpr int kMaxCapacity = 1 << 24;
+
+// Test hook: how long the next attention stalls on purpose (0: not).
+std::atomic<long long> g_stall_attend_ns{0};
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
@@ -155,6 +159,13 @@ int gather(P& P_, const ckv_problem* p, int group_major, const ckv_q4_cache* c, 
 }  // namespace
 
 extern "C" {
+
+int compresskv_debug_stall_next_q4_attend(long long wait_ns) {
+  if (wait_ns < 0 || (wait_ns > 0 && (wait_ns < 100000 || wait_ns > 2000000000ll)))
+    return CKV_ERR_INVALID_ARG;
+  g_stall_attend_ns.store(wait_ns);
+  return CKV_OK;
+}
 
 size_t compresskv_q4_workspace_size(const ckv_q4_cache* c, int32_t num_q_heads, int32_t num_queries) {
   if (check_cache(c, false) != CKV_OK) return 0;
@@ -312,6 +323,7 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   P.lse_ws = reinterpret_cast<float*>(ws + area.lse);
   P.z = reinterpret_cast<float*>(ws + area.z);
   P.z_stride = P.rows + P.rows % 2;
+  P.stall_ns = static_cast<unsigned long long>(g_stall_attend_ns.exchange(0));
   Tracer tr{c->trace, st};
   rc = traced(tr, CKV_KERNEL_Q4_ATTEND, [&] { return launch_q4_attend(P, sms, st); });
   if (rc != CKV_OK || !P.accumulate) return rc;

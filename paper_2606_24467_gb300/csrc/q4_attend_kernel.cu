@@ -105,7 +105,7 @@ struct Shape {
   static constexpr int kSide = kWarps * kStages * kSideBytes;
   static constexpr int kPairTile = kTile * 8;    // V's scales by pairs of slots, fp16
   static constexpr int kScales = kWarps * (kScaleTile + kPairTile);
-  static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8;
+  static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8 + 8;
   static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
   static_assert(kTile % 16 == 0, "steps");
   static_assert(kCodeTile % 512 == 0, "swizzle");
@@ -384,12 +384,14 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const uint32_t scales = base + S::kCodes + S::kSide + warp * (kScaleTile + kPairTile);
   const uint32_t pairs = scales + kScaleTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
+  const uint32_t never = base + S::kSmem - 1024 - 8;  // the test hook's stall waits for it
   if (lane == 0) {
     for (int i = 0; i < S::kStages; ++i) mbar_init(bars + 8 * i, 1);
     s_tail[warp].block = s_head[warp].block = -1;
   }
   if (threadIdx.x == 0) {
     s_abort = 0;
+    mbar_init(never, 1);
     tma_prefetch_map(&p.map_k);
     tma_prefetch_map(&p.map_v);
   }
@@ -572,9 +574,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   bool fresh = true;
   int seg_tiles = 0;  // tiles of the row block so far
   TileRing<S::kStages> ring;
-  bool failed = false;
+  bool failed = p.stall_ns && blockIdx.x == 0 && warp == 0 && left > 0 &&
+                !mbar_wait_bounded(never, 0, &s_abort, p.status, p.stall_ns);
 
-  for (; left > 0; --left) {
+  for (; left > 0 && !failed; --left) {
     if (fresh) {
       seg_tiles = 0;
       load_queries<NB>(p, c.unit, c.block, Q);

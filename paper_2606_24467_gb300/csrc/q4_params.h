@@ -90,6 +90,7 @@ struct Q4AttendParams {
   float* lse_ws;               // [units][rows]: base-2 log-sum-exp
   float* z;                    // accumulate: [units][capacity][z_stride] base-2 logits of the rows
   int z_stride;                // rows, made even
+  unsigned long long stall_ns; // test hook: CTA 0's first warp waits this long for what nothing sets; 0: not
 };
 
 struct Q4EvictParams {
