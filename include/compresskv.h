@@ -496,6 +496,10 @@ int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t gr
  * lse: optional device float [batch][num_q_heads][num_queries].
  * accumulate: p, summed over the queries and the group's heads, is added to
  *   each visible slot's weight.
+ * A wait that runs out (2 s) sets the workspace's status to
+ *   CKV_ERR_DEVICE_TIMEOUT if it is 0.  out and lse are then undefined; the
+ *   weights stay as they were, in this call and the ones after it, until
+ *   compresskv_q4_workspace_init.
  * Logits, softmax sums and outputs are held in fp32; inside the sum over the
  * slots the middle of a group's range, and for bf16 outputs p and p times a
  * slot's scale, are rounded to fp16 (by at most 2^-11 of themselves).  The results

@@ -70,7 +70,8 @@ int check_values(const void* k, const void* v) {
 }
 
 // The attention's area behind the workspace header (status word at its start,
-// the tickets from kTicketBytes on).
+// the word that says that a call has stopped behind it, the tickets from
+// kTicketBytes on).
 constexpr size_t kTicketBytes = 256;
 static_assert(kTicketBytes + kQ4MaxCtas * sizeof(int) <= kQ4HeaderBytes, "tickets");
 struct AttendArea {
@@ -315,6 +316,7 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   // no more CTAs than there can be tiles
   const long long tiles = static_cast<long long>(units_of(c)) * ((c->capacity + kQ4Tile - 1) / kQ4Tile) * P.blocks;
   sms = static_cast<int>(std::min<long long>({sms, kQ4MaxCtas, tiles}));
+  P.stopped = P.status + 1;
   P.tickets = reinterpret_cast<int*>(ws + kTicketBytes);
   P.head_ml = reinterpret_cast<float2*>(ws + area.head_ml);
   P.head_o = reinterpret_cast<float*>(ws + area.head_o);

@@ -989,6 +989,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     }
   }
   if (failed) {
+    if (lane == 0) *reinterpret_cast<volatile int*>(p.stopped) = 1;
     // copies in flight end before the shared memory does (or their wait runs out)
     for (int k = 0; k < ring.in_flight(left); ++k) {
       const uint64_t t0 = globaltimer_ns();
@@ -1205,6 +1206,8 @@ template <int kWide>
 __global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ Q4AttendParams p) {
   __shared__ float s_lse[kMaxQRows + 2];
   pdl_wait();
+  // an attention that stopped early leaves logits and sums of earlier calls
+  if (*reinterpret_cast<volatile const int*>(p.stopped)) return;
   const int unit = blockIdx.y, len = length_of(p.c, unit);
   const int j = blockIdx.x * kWeightThreads + threadIdx.x;
   if (j - static_cast<int>(threadIdx.x) >= len) return;

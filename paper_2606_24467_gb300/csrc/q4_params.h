@@ -82,6 +82,7 @@ struct Q4AttendParams {
   int rows, block_rows, blocks;  // query rows of a unit, of a row block, and row blocks of a unit
   int* status;
   // workspace
+  int* stopped;                // 1 once a wait has run out, until the workspace is set up again
   int* tickets;                // [CTAs]: CTAs done with the row block that starts in one and goes on
   float* head_o;               // [warps]: the end of a row block that another warp began,
   float2* head_ml;             //   [block rows][128], and its softmax reference and sum

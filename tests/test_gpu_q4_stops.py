@@ -43,6 +43,10 @@ def test_attend_wait_runs_out(cuda_device, lens, group, n, dtype):
     ckv.debug_stall_next_q4_attend(2_000_000)
     call(c, q, ws)
     assert ckv.read_device_status(ws) == B.CKV_ERR_DEVICE_TIMEOUT
+    # no weight of logits and sums that were not made, by this call or the next
+    assert torch.equal(w0.view(torch.int32), c.weights.view(torch.int32))
+    call(c, q, ws)
+    assert torch.equal(w0.view(torch.int32), c.weights.view(torch.int32))
     init(ws)
     assert ckv.read_device_status(ws) == 0
     for _ in range(2):  # (tickets of the row blocks that were left half done start again)
@@ -83,3 +87,22 @@ def test_a_call_without_slots_does_not_stall(cuda_device):
     ckv.debug_stall_next_q4_attend(2_000_000)
     out, lse = call(c, q, ws)
     assert ckv.read_device_status(ws) == 0 and not out.any() and (lse == float("-inf")).all()
+
+
+def test_weights_stay_whatever_the_status_said_before(cuda_device):
+    """The status keeps its first error, here an index that a gather skipped; a
+    call that does not stop adds its weights all the same, one that does does not."""
+    gen = torch.Generator().manual_seed(84)
+    c = random_cache(1, 2, 96, [[90, 70]], cuda_device, gen)
+    q = torch.randn((1, 8, 1, 128), generator=gen).half().to(cuda_device)
+    ws = ckv.q4_workspace(c, 8, 1)
+    ws[:4].view(torch.int32).fill_(B.CKV_ERR_DEVICE_INDEX)
+    w0 = c.weights.clone()
+    call(c, q, ws)
+    torch.cuda.synchronize()
+    assert (c.weights[0, 0, :90] > w0[0, 0, :90]).all()
+    w1 = c.weights.clone()
+    ckv.debug_stall_next_q4_attend(1_000_000)
+    call(c, q, ws)
+    assert ckv.read_device_status(ws) == B.CKV_ERR_DEVICE_INDEX
+    assert torch.equal(w1.view(torch.int32), c.weights.view(torch.int32))
