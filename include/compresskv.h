@@ -426,7 +426,7 @@ typedef struct ckv_q4_rows {
 
 /* Query tokens: [batch][num_q_heads][num_queries][head_dim], head_dim
  * contiguous, bases 16-byte aligned, strides multiples of 8 elements (`out`
- * the same shape; its rows must not overlap). */
+ * the same shape; rows that overlap are refused). */
 typedef struct ckv_q4_queries {
   int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads; head h uses group h / (its share) */
   int32_t num_queries;      /* query tokens of a sequence: 1..16; at most 256 with all heads of a group */

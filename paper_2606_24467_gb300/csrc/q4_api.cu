@@ -108,6 +108,37 @@ int check_heads(const ckv_q4_cache* c, int num_q_heads, int num_queries) {
   return CKV_OK;
 }
 
+// Whether two rows of kHeadDim elements share one, in a layout of n[i] rows at
+// strides[i] (0 .. kMaxStride) in each of three dimensions.  They do not where
+// every stride holds what the smaller ones span; otherwise they do exactly
+// where the indices' differences, not all zero, come to less than a row.
+constexpr int64_t kMaxStride = 1LL << 44;  // (32 TB: products of strides and indices stay in 64 bits)
+bool rows_overlap(const int64_t (&strides)[3], const int (&n)[3]) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return strides[a] < strides[b]; });
+  int64_t span = kHeadDim;
+  bool nested = true;
+  for (int d : order) {
+    if (n[d] == 1) continue;
+    nested = nested && strides[d] >= span;
+    span += strides[d] * (n[d] - 1);  // (a dimension of one row has no stride)
+  }
+  if (nested) return false;
+  // the dimension of most rows is solved for
+  const int a = static_cast<int>(std::max_element(n, n + 3) - n), b = (a + 1) % 3, c = (a + 2) % 3;
+  const int64_t s = strides[a], most = n[a] - 1;
+  if (most > 0 && s < kHeadDim) return true;
+  for (int64_t j = 0; j < n[b]; ++j)
+    for (int64_t k = j ? 1 - n[c] : 1; k < n[c]; ++k) {
+      const int64_t rest = j * strides[b] + k * strides[c], near = most ? -rest / s : 0;
+      for (int64_t i = near - 1; i <= near + 1; ++i) {
+        const int64_t at = rest + std::min(std::max(i, -most), most) * s;
+        if (at < kHeadDim && at > -kHeadDim) return true;
+      }
+    }
+  return false;
+}
+
 template <class P>
 int gather(P& P_, const ckv_problem* p, int group_major, const ckv_q4_cache* c, const int32_t* indices,
            const int32_t* cu_out, const void* k, const void* v, const float* raw, void* k_values,
@@ -277,10 +308,10 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   const int64_t in[3] = {a->q_batch_stride, a->q_head_stride, a->q_query_stride};
   const int64_t to[3] = {a->out_batch_stride, a->out_head_stride, a->out_query_stride};
   const int dims[3] = {c->batch, a->num_q_heads, a->num_queries};
-  for (int i = 0; i < 3; ++i) {
-    if (in[i] < 0 || in[i] % 8 || to[i] < 0 || to[i] % 8) return CKV_ERR_INVALID_ARG;
-    if (dims[i] > 1 && to[i] < kHeadDim) return CKV_ERR_INVALID_ARG;  // rows would overlap
-  }
+  for (int i = 0; i < 3; ++i)
+    if (in[i] < 0 || in[i] % 8 || to[i] < 0 || to[i] % 8 || (dims[i] > 1 && std::max(in[i], to[i]) > kMaxStride))
+      return CKV_ERR_INVALID_ARG;
+  if (rows_overlap(to, dims)) return CKV_ERR_INVALID_ARG;
   const AttendArea area = attend_area(c, a->num_q_heads, a->num_queries, a->accumulate != 0);
   if ((rc = check_workspace(workspace, workspace_bytes, area.bytes)) != CKV_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
