@@ -459,8 +459,8 @@ int compresskv_q4_workspace_init(void* workspace, size_t workspace_bytes, void* 
  * k_values, v_values: optional, [rows][num_kv_heads][head_dim] contiguous in
  *   the rows' dtype: the values that the codes stand for (what later steps
  *   will read), for instance for the attention of a prompt's own chunk.
- * Rows beyond the capacity are not written, and a unit whose start is outside
- *   0..capacity keeps what it has; either sets *device_status (optional
+ * Rows beyond the capacity are not written, and a unit whose given start is
+ *   outside 0..capacity keeps what it has; either sets *device_status (optional
  *   device int32) to CKV_ERR_DEVICE_INDEX if it is 0. */
 int compresskv_q4_append(const ckv_q4_cache* c, const ckv_q4_rows* r, const void* k, const void* v,
                          const int32_t* positions, const int32_t* start, void* k_values, void* v_values,

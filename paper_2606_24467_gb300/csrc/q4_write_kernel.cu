@@ -206,9 +206,11 @@ __device__ __forceinline__ void store_row(const Q4WriteParams<kTable>& p, uint4 
   if (lane == 16 && p.c.weights) p.c.weights[dst] = weight;
 }
 
-// The slot from which a unit's rows go, or -1 where it is outside the unit.
+// The slot from which a unit's rows go, or -1 where a given one is outside the
+// unit.  (A length outside it counts as the nearer end.)
 __device__ __forceinline__ int first_slot(const Q4AppendParams& p, int unit) {
-  const int at = p.start ? p.start[unit] : p.c.lengths[unit];
+  if (!p.start) return min(max(p.c.lengths[unit], 0), p.c.capacity);
+  const int at = p.start[unit];
   return at >= 0 && at <= p.c.capacity ? at : -1;
 }
 
