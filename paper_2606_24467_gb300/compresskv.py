@@ -661,7 +661,9 @@ def _q4_rows(cache: Q4Cache, k, v):
     shape, strides = k.shape, k.stride()
     if len(shape) != 3 or shape[1] != cache.num_kv_heads or shape[2] != 128 or v.shape != shape:
         _invalid("k and v must be [rows, H_kv, 128]")
-    if v.dtype != k.dtype or strides[2] != 1 or v.stride() != strides:
+    if v.dtype != k.dtype or strides[2] != 1 or (
+            v.stride() != strides  # (a dimension of one element has a stride that means nothing)
+            and any(n > 1 and a != b for n, a, b in zip(shape, strides, v.stride()))):
         _invalid("k and v must share their dtype and strides, head_dim contiguous")
     if v.get_device() not in (cache.index, -1):  # (-1: page-locked host memory)
         _invalid("v must be on the cache's device")

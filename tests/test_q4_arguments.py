@@ -5,6 +5,7 @@ import itertools
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2606_24467_gb300 as ckv
 from paper_2606_24467_gb300 import compresskv as B
@@ -57,3 +58,18 @@ def test_output_strides_that_interleave_or_are_far_apart():
     assert attend_code((2, 4, 5), (1 << 44, 1 << 40, 1 << 36)) == free
     assert attend_code((2, 4, 5), ((1 << 44) + 8, 640, 128)) == bad
     assert attend_code((60000, 1, 1), (120, 8, 8)) == bad and attend_code((60000, 1, 1), (128, 8, 8)) == free
+
+
+def test_rows_whose_strides_differ_where_they_mean_nothing():
+    """One row, or one KV head: K and V cut out of different tensors."""
+    c = ckv.q4_cache(1, 4, 32, device="cpu")
+    k = torch.zeros((1, 4, 128)).bfloat16()
+    v = torch.zeros((9, 4, 256)).bfloat16()[::3, :, :128]
+    assert B._q4_rows(c, k, v[:1].as_strided((1, 4, 128), (999, 128, 1)))[1] == (1, 4, 128)
+    with pytest.raises(ckv.CompressKVError):
+        B._q4_rows(c, k, v[:1])  # the heads' strides differ
+    one = ckv.q4_cache(1, 1, 32, device="cpu")
+    a, b = torch.zeros((5, 1, 128)).half(), torch.zeros((5, 2, 128)).half()[:, :1]
+    with pytest.raises(ckv.CompressKVError):
+        B._q4_rows(one, a, b)    # the rows' strides differ
+    assert B._q4_rows(one, a, a.as_strided((5, 1, 128), (128, 999, 1)))[2] == (128, 128, 1)
