@@ -125,6 +125,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// 1 / x of a sum of probabilities; 0 where there are none.
+__device__ __forceinline__ float inverse(float x) { return x == 0.f ? 0.f : 1.0f / x; }
 __device__ __forceinline__ float pow2(int e) {  // -126 <= e <= 127
   return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
@@ -949,13 +951,14 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       float* head = p.head_o + static_cast<size_t>(blockIdx.x * S::kWarps + warp) * kRows * kHeadDim;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float sum[2];
+        float sum[2], norm[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           sum[j] = l[nb][j];
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 4);
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+          norm[j] = f * inverse(sum[j]);
           if (!whole && g == 0) {
             const float2 ml = make_float2(ref[nb][j] - kLift, sum[j]);
             const int r = nb * 8 + 2 * t + j;
@@ -972,10 +975,10 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             const float m = i ? m1 : m0;
             const int r = nb * 8 + 2 * t + i, row = block * kRows + r;
             float4 v;
-            v.x = fmaf(o[nb][J][0][i], 16777216.0f, m) * f;
-            v.y = fmaf(o[nb][J][0][2 + i], 1048576.0f, m) * f;
-            v.z = fmaf(o[nb][J][1][i], 16777216.0f, m) * f;
-            v.w = fmaf(o[nb][J][1][2 + i], 1048576.0f, m) * f;
+            v.x = fmaf(o[nb][J][0][i], 16777216.0f, m) * norm[i];
+            v.y = fmaf(o[nb][J][0][2 + i], 1048576.0f, m) * norm[i];
+            v.z = fmaf(o[nb][J][1][i], 16777216.0f, m) * norm[i];
+            v.w = fmaf(o[nb][J][1][2 + i], 1048576.0f, m) * norm[i];
             if (row >= p.rows) continue;
             if (whole) write_row(p, unit, row, 8 * J + g, v, ref[nb][i] - kLift, sum[i]);
             else if (tail) sts128(codes + r * (kHeadDim * 4) + (8 * J + g) * 16,
@@ -1006,17 +1009,21 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   // ---- row blocks that this CTA's warps share: joined in slot order
   __syncthreads();
   if (s_abort) return;
-  // Sums weights f of parts 0 .. n - 1 (lane i has the reference and sum of part
-  // i) and returns their common reference.
+  // A part is a softmax reference, a sum and the outputs over that part alone:
+  // averages of averages stay within V's range.  Gives the weight f of each
+  // part (lane i has the reference and sum of part i) and the sum over all, and
+  // returns their common reference.
   auto weigh = [&](float2 ml, float* f, float* sum) {
     float top = ml.x;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     *f = ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
-    float x = ml.y * *f;
+    const float mine = ml.y * *f;
+    float x = mine;
 #pragma unroll
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     *sum = x;
+    *f = mine * inverse(x);
     return top;
   };
   auto add = [](float4& acc, float4 v, float f) {
@@ -1139,16 +1146,18 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         float t = top;
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) t = fmaxf(t, ml[i].x);
-        const float ref0 = t == -INFINITY ? 0.f : t, old = ex2_approx(top - ref0);
-        sum *= old;
-        acc = make_float4(acc.x * old, acc.y * old, acc.z * old, acc.w * old);
+        const float ref0 = t == -INFINITY ? 0.f : t, old = sum * ex2_approx(top - ref0);
+        sum = old;
         top = t;
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          const float f = ex2_approx(ml[i].x - ref0);
-          sum = fmaf(ml[i].y, f, sum);
-          add(acc, v[i], f);
+          ml[i].y *= ex2_approx(ml[i].x - ref0);
+          sum += ml[i].y;
         }
+        const float inv = inverse(sum), keep = old * inv;
+        acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) add(acc, v[i], ml[i].y * inv);
       }
     }
     __syncthreads();
@@ -1168,21 +1177,20 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   }
 }
 
-// Four channels (4 * lane ..) of a query row's output: v / sum, where `sum` is
-// that of 2^(logit - ref); the first lane writes the log-sum-exp.
+// Four channels (4 * lane ..) of a query row's output v, whose `sum` is that of
+// 2^(logit - ref); the first lane writes the log-sum-exp.
 __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int row, int lane, float4 v,
                                           float ref, float sum) {
   const int b = unit / p.c.num_kv_heads;
   const int hg = row / p.num_queries, qi = row - hg * p.num_queries;
   const int h = (unit - b * p.c.num_kv_heads) * p.group + hg;
-  const float f = sum == 0.f ? 0.f : 1.0f / sum;
   uint2 y;
   if (p.is_bf16) {
-    y.x = pack_bf16(v.x * f, v.y * f);
-    y.y = pack_bf16(v.z * f, v.w * f);
+    y.x = pack_bf16(v.x, v.y);
+    y.y = pack_bf16(v.z, v.w);
   } else {
-    y.x = pack_half2(v.x * f, v.y * f);
-    y.y = pack_half2(v.z * f, v.w * f);
+    y.x = pack_half2(v.x, v.y);
+    y.y = pack_half2(v.z, v.w);
   }
   *reinterpret_cast<uint2*>(p.out + b * p.o_bs + h * p.o_hs + qi * p.o_qs + 4 * lane) = y;
   if (lane == 0) {

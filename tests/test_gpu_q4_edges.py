@@ -6,7 +6,7 @@ import torch
 
 import paper_2606_24467_gb300 as ckv
 from paper_2606_24467_gb300 import compresskv as B
-from test_gpu_q4 import blank, check_rows, host
+from test_gpu_q4 import blank, check_rows, host, random_cache, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,16 @@ def test_append_behind_lengths_outside_the_cache(cuda_device, rows):
         assert np.array_equal(new["positions"][0, g, at:at + rows], np.arange(rows))
     assert np.array_equal(old["k_codes"][0, 1], new["k_codes"][0, 1])
     assert np.array_equal(old["positions"][0, 1], new["positions"][0, 1])
+
+
+@pytest.mark.parametrize("lens", [[[1, 20]], [[300, 700]], [[20000, 1500]]])
+def test_attend_values_near_the_largest_number(cuda_device, lens):
+    """V up to 2^127: by a warp alone, joined in a CTA, and joined by CTAs, no
+    sum on the way may pass what fp32 holds."""
+    gen = torch.Generator().manual_seed(91)
+    c = random_cache(1, 2, max(lens[0]), lens, cuda_device, gen)
+    for g in range(2):  # (behind the length there are NaN)
+        n = lens[0][g]
+        c.v_params[0, g, :n] = (c.v_params[0, g, :n].double() * 2.0 ** 124).bfloat16()
+    out, _ = run_attend(c, torch.randn((1, 8, 2, 128), generator=gen).bfloat16().to(cuda_device))
+    assert torch.isfinite(out).all()
