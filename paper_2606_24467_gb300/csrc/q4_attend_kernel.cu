@@ -50,7 +50,11 @@
 //     the output's own rounding (2.7e-4 at 128K slots), where one rounding of p s
 //     gave 3.0e-4 (6 % faster) and two 3.6e-4 (8 %).  Scales and
 //     middles are fp16 too (scales exactly, middles to 2^-11) against a power of
-//     two that follows the largest of both, for scales down to 2^-21 of it.
+//     two 2^e of the slot's own, which goes to the weights: p 2^e, times a power of
+//     two of the row's (its gain) that follows the largest of them.  What a row does
+//     not see, or hardly attends to, then costs the rest no bits, however large
+//     it is.  A weight below 2^-16 of the row's largest is off by 2^-27 of that one,
+//     and a scale below 2^-20 of the largest magnitude in its row of V loses bits.
 // Eight lanes of a warp need the same slot's scales, so one lane converts them
 // for all (K: times the softmax scale in fp32; V: fp16 pairs of slots) and
 // leaves them in shared memory.
@@ -71,10 +75,13 @@ namespace {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 8.0f;         // references lag behind the largest logit by at most this
 constexpr float kLift = 3.0f;          // probabilities are held times 2^3: at most 2^11
-constexpr int kTopExp = 7;             // scales become < 2^4, middles < 2^9: p s < 2^15
+constexpr int kTopExp = 3;             // a slot's scales become < 1, its middles < 2^5
 constexpr uint32_t kOnes = 0x3c003c00u;  // fp16, twice
 constexpr float kMiddle = 7.5f / 16777216.0f;  // of the codes, as they are held
-constexpr int kMinScaleExp = -110;     // smaller scales and minima share this reference
+constexpr int kMinScaleExp = -110;     // rows of smaller scales and minima share this exponent
+constexpr float kTopWeight = 32768.0f; // of weights p 2^e: w s < 2^15
+constexpr int kExpOff = 12;            // a slot's 2^e is held as 2^(e - 12): p 2^(e - 12) < 2^127
+constexpr int kMaxGain = 122;          // weights are p 2^(e - 12) times 2^gain
 
 // A row block of up to two tiles a warp is one CTA's; longer ones are shared,
 // by CTAs of at least four tiles.  Joining over CTAs costs about 3 us, a warp's
@@ -104,7 +111,8 @@ struct Shape {
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
   static constexpr int kPairTile = kTile * 8;    // V's scales by pairs of slots, fp16
-  static constexpr int kScales = kWarps * (kScaleTile + kPairTile);
+  static constexpr int kExpTile = kTile * 4;     // 2^(e - 12) of its slots, fp32
+  static constexpr int kScales = kWarps * (kScaleTile + kPairTile + kExpTile);
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8 + 8;
   static constexpr int kLane = (kTile + 31) / 32;  // slots a lane prepares
   static_assert(kTile % 16 == 0, "steps");
@@ -155,6 +163,13 @@ __device__ __forceinline__ uint32_t fma_half2(uint32_t a, uint32_t b, uint32_t c
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
+// a *= x, b *= y in one instruction.
+__device__ __forceinline__ void mul_pair(float& a, float& b, float x, float y) {
+  asm("{\n\t.reg .b64 s, t;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\t"
+      "mul.rn.f32x2 s, s, t;\n\tmov.b64 {%0, %1}, s;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(x), "f"(y));
+}
 // Transpose of an 8x8 matrix of 16-bit numbers: lane (g, t) gives row g,
 // columns 2t and 2t + 1, and receives those of column g.
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
@@ -195,6 +210,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t x) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
 }
 __device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) {
   asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory");
@@ -372,7 +390,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   constexpr int kRows = 8 * NB;
   constexpr int kTile = S::kTile, kSteps = S::kSteps;
   constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
-  constexpr int kScaleTile = S::kScaleTile, kPairTile = S::kPairTile, kLane = S::kLane;
+  constexpr int kScaleTile = S::kScaleTile, kPairTile = S::kPairTile, kExpTile = S::kExpTile, kLane = S::kLane;
   constexpr int kPairBytes = kFine ? 8 : kQ4ParamBytes;  // of V's scales, a slot
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_sums[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
@@ -383,8 +401,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   const uint32_t codes = base + warp * S::kStages * 2 * kCodeTile;
   const uint32_t side = base + S::kCodes + warp * S::kStages * kSideBytes;
-  const uint32_t scales = base + S::kCodes + S::kSide + warp * (kScaleTile + kPairTile);
-  const uint32_t pairs = scales + kScaleTile;
+  const uint32_t scales = base + S::kCodes + S::kSide + warp * (kScaleTile + kPairTile + kExpTile);
+  const uint32_t pairs = scales + kScaleTile, exps = pairs + kPairTile;
   const uint32_t bars = base + S::kCodes + S::kSide + S::kScales + warp * S::kStages * 8;
   const uint32_t never = base + S::kSmem - 1024 - 8;  // the test hook's stall waits for it
   if (lane == 0) {
@@ -572,10 +590,23 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   float o[NB][4][2][4];   // [8 rows][group][step][channel, row pair]
   float om[NB][2];        // middles' term (lanes of g >= 4)
   float ref[NB][2], l[NB][2];  // rows 2t, 2t + 1
-  int vexp = kMinScaleExp;
+  int gain[NB][2];
   bool fresh = true;
   int seg_tiles = 0;  // tiles of the row block so far
   TileRing<S::kStages> ring;
+  // the sums of row j of eight go from one gain to another, at most as large
+  auto scale_outputs = [&](int nb, int j, int& from, int to) {
+    const float f = pow2(max(to - from, -126));
+    from = to;
+    om[nb][j] *= f;
+#pragma unroll
+    for (int J = 0; J < 4; ++J)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        o[nb][J][st][j] *= f;
+        o[nb][J][st][2 + j] *= f;
+      }
+  };
   bool failed = p.stall_ns && blockIdx.x == 0 && warp == 0 && left > 0 &&
                 !mbar_wait_bounded(never, 0, &s_abort, p.status, p.stall_ns);
 
@@ -587,6 +618,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
       for (int nb = 0; nb < NB; ++nb) {
         ref[nb][0] = ref[nb][1] = -INFINITY;
         l[nb][0] = l[nb][1] = 0.f;
+        gain[nb][0] = gain[nb][1] = kMaxGain;
 #pragma unroll
         for (int i = 0; i < 2; ++i) om[nb][i] = 0.f;
 #pragma unroll
@@ -596,7 +628,6 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[nb][J][st][i] = 0.f;
       }
-      vexp = kMinScaleExp;
       fresh = false;
     }
     // (all lanes go on, or none: another warp's abort may reach some lanes only)
@@ -613,6 +644,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     // hold a NaN count nothing in V's products
     uint32_t nan_groups[kLane] = {};  // of this lane's slots
     bool special;
+    float largest;  // of the slots' 2^(e - 12)
     {
       uint4 w[kLane];
 #pragma unroll
@@ -626,9 +658,12 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
                make_uint4(__float_as_uint(bf_lo(kw.x) * f1), __float_as_uint(bf_hi(kw.x) * f1),
                           __float_as_uint(bf_lo(kw.y) * f1), __float_as_uint(bf_hi(kw.y) * f1)));
       }
-      uint32_t all = 0;
+      uint32_t top[kLane], all = 0;
 #pragma unroll
-      for (int i = 0; i < kLane; ++i) all = max(all, top_of(w[i]));
+      for (int i = 0; i < kLane; ++i) {
+        top[i] = top_of(w[i]);
+        all = max(all, top[i]);
+      }
       all = __reduce_max_sync(0xffffffffu, all);
       special = all >= 0x7f800000u;
       if (special) {
@@ -646,29 +681,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             }
           }
           w[i] = make_uint4(x[0], x[1], x[2], x[3]);
-          all = max(all, top_of(w[i]));
+          top[i] = min(top_of(w[i]), 0x7f000000u);
+          all = max(all, top[i]);
         }
-        all = min(__reduce_max_sync(0xffffffffu, all), 0x7f000000u);
+        all = __reduce_max_sync(0xffffffffu, all);
       }
-      const int k = max(static_cast<int>(all >> 23) - 127, kMinScaleExp);
-      if (k > vexp) {  // the sums go to the new power of two
-        const float f = pow2(max(vexp - k, -126));
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          om[nb][0] *= f;
-          om[nb][1] *= f;
-#pragma unroll
-          for (int J = 0; J < 4; ++J)
-#pragma unroll
-            for (int st = 0; st < 2; ++st)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[nb][J][st][i] *= f;
-        }
-        vexp = k;
-      }
-      const float f = pow2(kTopExp - vexp);
+      largest = pow2(max(static_cast<int>(all >> 23) - 127, kMinScaleExp) - kExpOff);
 #pragma unroll
       for (int i = 0; i < kLane; ++i) {
+        const int e = max(static_cast<int>(top[i] >> 23) - 127, kMinScaleExp);
+        const float f = pow2(kTopExp - e);
         const float s0 = bf_lo(w[i].x) * f, s1 = bf_hi(w[i].x) * f, s2 = bf_lo(w[i].y) * f, s3 = bf_hi(w[i].y) * f;
         // middles: m + 7.5 s
         const uint32_t m01 = pack_half2(fmaf(s0, 7.5f, bf_lo(w[i].z) * f), fmaf(s1, 7.5f, bf_hi(w[i].z) * f));
@@ -682,6 +704,7 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
                  make_uint4(kFine ? s01 : even, kFine ? s23 : odd, m01, m23));
           if (kFine) sts64(pairs + (lane + 32 * i) * 8, even, odd);
+          sts32(exps + (lane + 32 * i) * 4, __float_as_uint(pow2(e - kExpOff)));
         }
       }
       __syncwarp();
@@ -772,26 +795,24 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         top[j] = fmaxf(z[nb][0][j], z[nb][0][2 + j]);
 #pragma unroll
         for (int h = 1; h < kSteps; ++h) top[j] = fmaxf(top[j], fmaxf(z[nb][h][j], z[nb][h][2 + j]));
-        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 4));
-        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8));
-        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16)) * Q.f2[nb][j];
+        top[j] *= Q.f2[nb][j];
         raise |= top[j] > ref[nb][j] + kRaise;
       }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 4));
+          top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8));
+          top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
           if (!(top[j] > ref[nb][j] + kRaise)) continue;
-          const float f = ref[nb][j] == -INFINITY ? 0.f : ex2_approx(ref[nb][j] - top[j]);
-          ref[nb][j] = top[j];
-          l[nb][j] *= f;
-          om[nb][j] *= f;
-#pragma unroll
-          for (int J = 0; J < 4; ++J)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              o[nb][J][st][j] *= f;
-              o[nb][J][st][2 + j] *= f;
-            }
+          // (references are whole numbers; while there is none, nothing is summed yet)
+          const float up = ceilf(top[j]);
+          const int more = ref[nb][j] == -INFINITY ? 0 : static_cast<int>(fminf(up - ref[nb][j], 1000.f));
+          ref[nb][j] = up;
+          l[nb][j] *= pow2(max(-more, -126));
+          // probabilities shrink by 2^more, so the gain of the outputs' weights grows
+          gain[nb][j] += more;
+          if (gain[nb][j] > kMaxGain) scale_outputs(nb, j, gain[nb][j], kMaxGain);
         }
       }
       if (special) {
@@ -823,6 +844,35 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             l[nb][j] += z[nb][h][i];
           }
       }
+      // weights of the slots' rows of V: times 2^e, and the row's gain
+#pragma unroll
+      for (int h = 0; h < kSteps; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float x = __uint_as_float(lds32(exps + (h * 16 + 8 * i + g) * 4));
+          mul_pair(z[nb][h][2 * i], z[nb][h][2 * i + 1], x, x);
+        }
+      // (probabilities are at most 2^11: no need to look where no slot of the tile
+      // is beyond 2^4 in the row's terms)
+      if (__any_sync(0xffffffffu, largest * pow2(max(gain[nb][0], gain[nb][1])) > kTopWeight / 2048.0f)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float most = 0.f;
+#pragma unroll
+          for (int h = 0; h < kSteps; ++h) most = fmaxf(most, fmaxf(z[nb][h][j], z[nb][h][2 + j]));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 4));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 8));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 16));
+          // the largest of the tile becomes 2^2 .. 2^3
+          if (most * pow2(gain[nb][j]) > kTopWeight)
+            scale_outputs(nb, j, gain[nb][j], max(129 - static_cast<int>(__float_as_uint(most) >> 23), -122));
+        }
+      }
+      const float x0 = pow2(gain[nb][0]), x1 = pow2(gain[nb][1]);
+#pragma unroll
+      for (int h = 0; h < kSteps; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) mul_pair(z[nb][h][i], z[nb][h][i + 1], x0, x1);
     }
 
     // ---- outputs: the sums of p s and p m', then the codes group by group
@@ -947,7 +997,6 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         part.ends = ends;
       }
       // sums of the codes' products: * 2^24, and 1/16 for a byte's second channel
-      const float f = pow2(vexp - kTopExp);
       float* head = p.head_o + static_cast<size_t>(blockIdx.x * S::kWarps + warp) * kRows * kHeadDim;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -958,7 +1007,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 4);
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
           sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
-          norm[j] = f * inverse(sum[j]);
+          // 2^(kExpOff - kTopExp - gain) / sum
+          norm[j] = pow2(1 - gain[nb][j]) * (256.0f * inverse(sum[j]));
           if (!whole && g == 0) {
             const float2 ml = make_float2(ref[nb][j] - kLift, sum[j]);
             const int r = nb * 8 + 2 * t + j;
