@@ -500,9 +500,15 @@ int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t gr
  *   CKV_ERR_DEVICE_TIMEOUT if it is 0.  out and lse are then undefined; the
  *   weights stay as they were, in this call and the ones after it, until
  *   compresskv_q4_workspace_init.
- * Logits, softmax sums and outputs are held in fp32; inside the sum over the
- * slots the middle of a group's range, and for bf16 outputs p and p times a
- * slot's scale, are rounded to fp16 (by at most 2^-11 of themselves).  The results
+ * Logits, softmax sums and outputs are held in fp32, but added up by the tensor
+ * cores, 16 numbers to a sum at a time, which cut each of them off at 2^-25 and
+ * the result at 2^-23 of the largest: a logit is off by at most 2^-18 of the sum
+ * of its terms' magnitudes.  Inside the sum over the slots, p, p times a slot's
+ * scale, and the middle of a group's range enter as two fp16 parts each; for
+ * bf16 outputs the first two as one (off by at most 2^-11 of themselves).  What
+ * is below fp16's range is lost: a slot's weight p |V| is off by up to 2^-27 of
+ * the row's largest, and a group of a slot whose scale is below 2^-20 of the
+ * largest magnitude in its row of V by more than 2^-11 of itself.  The results
  * are the same bits on every call with the same shapes, lengths and SMs. */
 int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const void* q,
                          const int32_t* q_positions, void* out, float* lse, void* workspace,

@@ -42,14 +42,19 @@
 //     3 % of the output were lost.)  The 7.5 comes off once a tile, as 7.5 sum p s.
 //     p is fp16 (off by at most 2^-11 of itself), the weights of group J's codes are
 //     p s_J, rounded once more, whose sum is a product with ones; the middles' term
-//     is a product of its own, with p.  That is well below a bf16 output's rounding
-//     (2^-8).  For f16 outputs (kFine) what both roundings left is a second operand;
-//     sum p s is then exact and comes with the middles' product, whose matrix has
-//     rows to spare, before the codes', so that it comes off half way, where the
-//     truncation before and after it cancels.  Error 2.1e-4 of the output, all of it
-//     the output's own rounding (2.7e-4 at 128K slots), where one rounding of p s
-//     gave 3.0e-4 (6 % faster) and two 3.6e-4 (8 %).  Scales and
-//     middles are fp16 too (scales exactly, middles to 2^-11) against a power of
+//     is a product of its own, with p, whose operand has rows to spare: what rounding
+//     a middle to fp16 left is in the second eight.  (Where one channel is 30 or 100
+//     times wider than the others, the middles are large against the output: rounded
+//     once they cost f16 outputs 2 to 9 times their own rounding, bf16 1.3 to 2.4.)
+//     For f16 outputs (kFine) what rounding p and p s left is a second operand; sum
+//     p s is then exact and comes with the middles' product before the codes', so
+//     that it comes off half way, where the truncation before and after it cancels.
+//     Error 2.1e-4 of the output, all of it the output's own rounding (2.7e-4 at
+//     128K slots), where one rounding of p s gave 3.0e-4 and two 3.6e-4.  bf16
+//     outputs, whose rounding is eight times that, keep single roundings: second
+//     operands took 153 us for 133 at 128K x 4 slots, and the error is within 2 % of
+//     the output's own rounding (15 % where a channel is 100 times wider).
+//     Scales (exactly) and middles enter fp16 against a power of
 //     two 2^e of the slot's own, which goes to the weights: p 2^e, times a power of
 //     two of the row's (its gain) that follows the largest of them.  What a row does
 //     not see, or hardly attends to, then costs the rest no bits, however large
@@ -110,7 +115,7 @@ struct Shape {
   static constexpr int kScaleTile = kTile * 16;  // K's scales of the tile at hand, fp32
   static constexpr int kCodes = kWarps * kStages * 2 * kCodeTile;
   static constexpr int kSide = kWarps * kStages * kSideBytes;
-  static constexpr int kPairTile = kTile * 8;    // V's scales by pairs of slots, fp16
+  static constexpr int kPairTile = kTile * 16;   // V's scales by pairs of slots, rests of its middles, fp16
   static constexpr int kExpTile = kTile * 4;     // 2^(e - 12) of its slots, fp32
   static constexpr int kScales = kWarps * (kScaleTile + kPairTile + kExpTile);
   static constexpr int kSmem = 1024 + kCodes + kSide + kScales + kWarps * kStages * 8 + 8;
@@ -152,6 +157,10 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       "{%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// What rounding a and b to the pair h of fp16 numbers left, as another pair.
+__device__ __forceinline__ uint32_t half_rest(float a, float b, uint32_t h) {
+  return pack_half2(a - to_float(h & 0xffffu, false), b - to_float(h >> 16, false));
 }
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -213,9 +222,6 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
 }
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) {
   asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
-}
-__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) {
-  asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory");
 }
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row,
                                          uint64_t policy) {
@@ -391,7 +397,6 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
   constexpr int kTile = S::kTile, kSteps = S::kSteps;
   constexpr int kCodeTile = S::kCodeTile, kParamTile = S::kParamTile, kSideBytes = S::kSideBytes;
   constexpr int kScaleTile = S::kScaleTile, kPairTile = S::kPairTile, kExpTile = S::kExpTile, kLane = S::kLane;
-  constexpr int kPairBytes = kFine ? 8 : kQ4ParamBytes;  // of V's scales, a slot
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_sums[S::kWarps], s_unit[S::kWarps], s_at[S::kWarps], s_abort;
   __shared__ float2 s_ml[S::kWarps][kRows];
@@ -693,17 +698,17 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         const float f = pow2(kTopExp - e);
         const float s0 = bf_lo(w[i].x) * f, s1 = bf_hi(w[i].x) * f, s2 = bf_lo(w[i].y) * f, s3 = bf_hi(w[i].y) * f;
         // middles: m + 7.5 s
-        const uint32_t m01 = pack_half2(fmaf(s0, 7.5f, bf_lo(w[i].z) * f), fmaf(s1, 7.5f, bf_hi(w[i].z) * f));
-        const uint32_t m23 = pack_half2(fmaf(s2, 7.5f, bf_lo(w[i].w) * f), fmaf(s3, 7.5f, bf_hi(w[i].w) * f));
+        const float m0 = fmaf(s0, 7.5f, bf_lo(w[i].z) * f), m1 = fmaf(s1, 7.5f, bf_hi(w[i].z) * f);
+        const float m2 = fmaf(s2, 7.5f, bf_lo(w[i].w) * f), m3 = fmaf(s3, 7.5f, bf_hi(w[i].w) * f);
+        const uint32_t m01 = pack_half2(m0, m1), m23 = pack_half2(m2, m3);
         // an even lane keeps groups 0 and 1 of its pair of slots, an odd one 2 and 3
         const uint32_t s01 = pack_half2(s0, s1), s23 = pack_half2(s2, s3);
         const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & 1 ? s01 : s23, 1);
         const uint32_t a = lane & 1 ? got : s01, b = lane & 1 ? s23 : got;
         if (lane + 32 * i < kTile) {
           const uint32_t even = __byte_perm(a, b, 0x5410), odd = __byte_perm(a, b, 0x7632);
-          sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes,
-                 make_uint4(kFine ? s01 : even, kFine ? s23 : odd, m01, m23));
-          if (kFine) sts64(pairs + (lane + 32 * i) * 8, even, odd);
+          sts128(sd + kParamTile + (lane + 32 * i) * kQ4ParamBytes, make_uint4(s01, s23, m01, m23));
+          sts128(pairs + (lane + 32 * i) * 16, make_uint4(even, odd, half_rest(m0, m1, m01), half_rest(m2, m3, m23)));
           sts32(exps + (lane + 32 * i) * 4, __float_as_uint(pow2(e - kExpOff)));
         }
       }
@@ -876,16 +881,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     }
 
     // ---- outputs: the sums of p s and p m', then the codes group by group
-    // (lanes of g >= 4: p m' of group g - 4; of g < 4, with kFine: p s of group g)
+    // (lanes of g >= 4: p m' of group g - 4, of both parts; of g < 4: p s of group g)
     float sums[NB][4];
     uint32_t p0[NB][kSteps], p1[NB][kSteps];
     uint32_t r0[kFine ? NB : 1][kSteps], r1[kFine ? NB : 1][kSteps];  // what their rounding left
 #pragma unroll
     for (int h = 0; h < kSteps; ++h) {
       uint32_t pm[4];
-      // rows of [4 scales (or 2 pairs of them), 4 middles], transposed; rows 8-15 of
-      // the operand repeat rows 0-7
-      ldmatrix4_t(pm, sd + kParamTile + (h * 16 + (lane & 7) + ((lane & 16) >> 1)) * kQ4ParamBytes);
+      // rows of [4 scales, 4 middles], transposed, and as rows 8-15 of the operand
+      // of [2 pairs of scales, 4 rests of middles]
+      ldmatrix4_t(pm, (lane & 8 ? pairs : sd + kParamTile) + (h * 16 + (lane & 7) + ((lane & 16) >> 1)) * 16);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const uint32_t lo = pack_half2(z[nb][h][0], z[nb][h][1]), hi = pack_half2(z[nb][h][2], z[nb][h][3]);
@@ -894,18 +899,16 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         if (h == 0) sums[nb][0] = sums[nb][1] = sums[nb][2] = sums[nb][3] = 0.f;
         mma_f16(sums[nb], pm[0], pm[1], pm[2], pm[3], p0[nb][h], p1[nb][h]);
         if (kFine) {
-          r0[nb][h] = transpose8(pack_half2(z[nb][h][0] - to_float(lo & 0xffffu, false),
-                                            z[nb][h][1] - to_float(lo >> 16, false)));
-          r1[nb][h] = transpose8(pack_half2(z[nb][h][2] - to_float(hi & 0xffffu, false),
-                                            z[nb][h][3] - to_float(hi >> 16, false)));
+          r0[nb][h] = transpose8(half_rest(z[nb][h][0], z[nb][h][1], lo));
+          r1[nb][h] = transpose8(half_rest(z[nb][h][2], z[nb][h][3], hi));
           mma_f16(sums[nb], pm[0], pm[1], pm[2], pm[3], r0[nb][h], r1[nb][h]);
         }
       }
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      om[nb][0] += sums[nb][0];
-      om[nb][1] += sums[nb][1];
+      om[nb][0] += sums[nb][0] + sums[nb][2];
+      om[nb][1] += sums[nb][1] + sums[nb][3];
     }
 #pragma unroll
     for (int J = 0; J < 4; ++J) {
@@ -938,8 +941,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
         // gives after)
         if (kFine && h == kSteps / 2) take_off();
         // scales of two pairs of slots
-        const uint32_t pair = (kFine ? pairs : sd + kParamTile) + (h * 16 + 2 * t + (J >> 1)) * kPairBytes + (J & 1) * 4;
-        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * kPairBytes);
+        const uint32_t pair = pairs + (h * 16 + 2 * t + (J >> 1)) * 16 + (J & 1) * 4;
+        const uint32_t sa = lds32(pair), sb = lds32(pair + 8 * 16);
         const uint32_t x = v[2 * h], y = v[2 * h + 1], xh = x >> 8, yh = y >> 8;
         const uint32_t a0 = x & 0x000f000fu, a1 = x & 0x00f000f0u, a2 = y & 0x000f000fu, a3 = y & 0x00f000f0u;
         const uint32_t b0 = xh & 0x000f000fu, b1 = xh & 0x00f000f0u, b2 = yh & 0x000f000fu, b3 = yh & 0x00f000f0u;
