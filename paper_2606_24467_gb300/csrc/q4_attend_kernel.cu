@@ -849,17 +849,24 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
             l[nb][j] += z[nb][h][i];
           }
       }
-      // weights of the slots' rows of V: times 2^e, and the row's gain
+    }
+    // ---- weights of the slots' rows of V: probabilities times 2^e, and the row's gain
+    int high = gain[0][0];
 #pragma unroll
-      for (int h = 0; h < kSteps; ++h)
+    for (int nb = 0; nb < NB; ++nb) high = max(high, max(gain[nb][0], gain[nb][1]));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float x = __uint_as_float(lds32(exps + (h * 16 + 8 * i + g) * 4));
-          mul_pair(z[nb][h][2 * i], z[nb][h][2 * i + 1], x, x);
-        }
-      // (probabilities are at most 2^11: no need to look where no slot of the tile
-      // is beyond 2^4 in the row's terms)
-      if (__any_sync(0xffffffffu, largest * pow2(max(gain[nb][0], gain[nb][1])) > kTopWeight / 2048.0f)) {
+    for (int h = 0; h < kSteps; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x = __uint_as_float(lds32(exps + (h * 16 + 8 * i + g) * 4));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) mul_pair(z[nb][h][2 * i], z[nb][h][2 * i + 1], x, x);
+      }
+    // (probabilities are at most 2^11: no need to look where no slot of the tile is
+    // beyond 2^4 in any row's terms)
+    if (__any_sync(0xffffffffu, largest * pow2(high) > kTopWeight / 2048.0f)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           float most = 0.f;
@@ -872,7 +879,9 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
           if (most * pow2(gain[nb][j]) > kTopWeight)
             scale_outputs(nb, j, gain[nb][j], max(129 - static_cast<int>(__float_as_uint(most) >> 23), -122));
         }
-      }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
       const float x0 = pow2(gain[nb][0]), x1 = pow2(gain[nb][1]);
 #pragma unroll
       for (int h = 0; h < kSteps; ++h)
