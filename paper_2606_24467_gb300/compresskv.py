@@ -554,6 +554,14 @@ def _invalid(what: str):
     raise CompressKVError(CKV_ERR_INVALID_ARG, what)
 
 
+def _q4_int(x, what: str) -> int:
+    """A number that a call takes as int32 (ctypes would drop its upper bits)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        _invalid(f"{what} does not fit 32 bits")
+    return x
+
+
 def _q4_dtype(t: torch.Tensor) -> int:
     if t.dtype not in (torch.float16, torch.bfloat16):
         _invalid("rows and queries must be f16 or bf16")
@@ -681,7 +689,8 @@ def _q4_i32(cache, t, shape, what):
 
 
 def q4_workspace_size(cache: Q4Cache, num_q_heads: int = 0, num_queries: int = 0) -> int:
-    n = _fast("compresskv_q4_workspace_size")(cache.addr, int(num_q_heads), int(num_queries))
+    n = _fast("compresskv_q4_workspace_size")(cache.addr, _q4_int(num_q_heads, "num_q_heads"),
+                                              _q4_int(num_queries, "num_queries"))
     if n == 0:
         raise CompressKVError(CKV_ERR_INVALID_ARG, "compresskv_q4_workspace_size")
     return int(n)
@@ -806,5 +815,5 @@ def q4_evict(cache: Q4Cache, budget, ws, sinks: int = 0, recent: int = 0, stream
         budgets, budget = budget, 0
         _q4_i32(cache, budgets, (cache.batch, cache.num_kv_heads), "budget")
     _q4_on_device(cache, "budget and workspace", budgets, ws)
-    _q4_call("compresskv_q4_evict", cache, stream, cache.addr, int(budget), _addr(budgets), int(sinks),
-             int(recent), _addr(ws), ws.numel())
+    _q4_call("compresskv_q4_evict", cache, stream, cache.addr, _q4_int(budget, "budget"), _addr(budgets),
+             _q4_int(sinks, "sinks"), _q4_int(recent, "recent"), _addr(ws), ws.numel())

@@ -73,3 +73,14 @@ def test_rows_whose_strides_differ_where_they_mean_nothing():
     with pytest.raises(ckv.CompressKVError):
         B._q4_rows(one, a, b)    # the rows' strides differ
     assert B._q4_rows(one, a, a.as_strided((5, 1, 128), (128, 999, 1)))[2] == (128, 128, 1)
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """(a budget of 2^40 slots would otherwise have been one of 0)"""
+    c = ckv.q4_cache(2, 4, 64, device="cpu")
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    for kw in ({"budget": 2 ** 40}, {"budget": 10, "sinks": 2 ** 32}, {"budget": 10, "recent": -2 ** 33}):
+        with pytest.raises(ckv.CompressKVError, match="32 bits"):
+            ckv.q4_evict(c, ws=ws, **kw)
+    with pytest.raises(ckv.CompressKVError, match="32 bits"):
+        ckv.q4_workspace_size(c, 2 ** 32 + 8, 1)
