@@ -432,7 +432,7 @@ typedef struct ckv_q4_queries {
   int32_t num_queries;      /* query tokens of a sequence: 1..16; at most 256 with all heads of a group */
   int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16, of q and out */
   int32_t accumulate;       /* non-zero: add the attention to the cache's weights */
-  float scale;              /* softmax scale; 0 selects 1/sqrt(head_dim) */
+  float scale;              /* softmax scale, at most 2^96; 0 selects 1/sqrt(head_dim) */
   int64_t q_batch_stride, q_head_stride, q_query_stride;
   int64_t out_batch_stride, out_head_stride, out_query_stride;
 } ckv_q4_queries;

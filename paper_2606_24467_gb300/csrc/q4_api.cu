@@ -18,6 +18,7 @@ using namespace ckv;
 namespace {
 
 constexpr int kMaxCapacity = 1 << 24;
+constexpr float kMaxScale = 0x1p96f;
 
 // Test hook: how long the next attention stalls on purpose (0: not).
 std::atomic<long long> g_stall_attend_ns{0};
@@ -302,7 +303,8 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
   if (rc != CKV_OK) return rc;
   if (!a || (a->dtype != CKV_DTYPE_F16 && a->dtype != CKV_DTYPE_BF16)) return CKV_ERR_INVALID_ARG;
   if ((rc = check_heads(c, a->num_q_heads, a->num_queries)) != CKV_OK) return rc;
-  if (!(a->scale >= 0.f) || std::isinf(a->scale)) return CKV_ERR_INVALID_ARG;
+  // (NaN too; the kernel holds it times 2^10 log2 e)
+  if (!(a->scale >= 0.f && a->scale <= kMaxScale)) return CKV_ERR_INVALID_ARG;
   if (a->accumulate && !c->weights) return CKV_ERR_INVALID_ARG;
   if (!q || !out || !aligned16(q) || !aligned16(out)) return CKV_ERR_INVALID_ARG;
   const int64_t in[3] = {a->q_batch_stride, a->q_head_stride, a->q_query_stride};

@@ -84,3 +84,13 @@ def test_numbers_beyond_32_bits_are_refused():
             ckv.q4_evict(c, ws=ws, **kw)
     with pytest.raises(ckv.CompressKVError, match="32 bits"):
         ckv.q4_workspace_size(c, 2 ** 32 + 8, 1)
+
+
+def test_softmax_scales_that_overflow_are_refused():
+    c = ckv.q4_cache(1, 1, 32, device="cpu")
+    a = B.CkvQ4Queries(1, 1, B.CKV_DTYPE_BF16, 0, 0.0, 128, 128, 128, 128, 128, 128)
+    for scale, code in ((2.0 ** 96, B.CKV_ERR_WORKSPACE), (2.0 ** 97, B.CKV_ERR_INVALID_ARG),
+                        (3e38, B.CKV_ERR_INVALID_ARG)):
+        a.scale = scale
+        assert ckv.load().compresskv_q4_attend(c.addr, ctypes.addressof(a), 1 << 30, None, 1 << 30, None,
+                                               1 << 30, 0, None) == code
