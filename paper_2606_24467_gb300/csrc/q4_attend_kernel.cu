@@ -245,8 +245,10 @@ __device__ __forceinline__ uint64_t l2_policy_normal() {
   return p;
 }
 
+// (An ordinary load: the read-only path is for what nobody writes while the
+// kernel is there, and this one may be brought up while the append still runs.)
 __device__ __forceinline__ int length_of(const Q4Cache& c, int unit) {
-  return min(max(__ldg(c.lengths + unit), 0), c.capacity);
+  return min(max(c.lengths[unit], 0), c.capacity);
 }
 template <int kTile>
 __device__ __forceinline__ int tiles_of(const Q4Cache& c, int unit) {

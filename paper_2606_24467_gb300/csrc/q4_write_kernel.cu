@@ -191,11 +191,12 @@ __device__ __forceinline__ int2 rows_of(const Q4AppendParams& p, int s) {
   return make_int2(p.cu_rows[s], p.cu_rows[s + 1] - p.cu_rows[s]);
 }
 
-// This lane's 16 bytes of a source row, and the row into the cache.
+// This lane's 16 bytes of a source row, and the row into the cache.  (An
+// ordinary load: a gather that lets its successor start early may write the row.)
 template <int kTable>
 __device__ __forceinline__ uint4 load_row(const Q4WriteParams<kTable>& p, int row, int g) {
   const uint16_t* src = p.src[(threadIdx.x >> 4) & 1] + row * p.tok_stride + g * p.head_stride;
-  return __ldg(reinterpret_cast<const uint4*>(src) + (threadIdx.x & 15));
+  return reinterpret_cast<const uint4*>(src)[threadIdx.x & 15];
 }
 template <bool kBf16, int kTable>
 __device__ __forceinline__ void store_row(const Q4WriteParams<kTable>& p, uint4 raw, int dst, int value_row,
