@@ -392,7 +392,11 @@ int compresskv_compress_layer_noalloc(const ckv_problem* p, const void* q_win, c
  * down to bf16, scale s = the smallest bf16 with 15 s >= fl32(max x - m),
  * n_c = fl32(x_c - m) / s rounded to the nearest integer, ties to even (s = 0
  * and n = 0 where all are equal).  A group that holds a NaN or an infinity, or
- * whose spread is beyond fp32, has scale and minimum NaN.
+ * whose spread is beyond fp32, has scale and minimum NaN.  (Params of another
+ * origin: scales finite and not negative, minima finite, or both NaN.)  As m is
+ * rounded down and s up, a value can lie beyond its group's ends by up to 2^-6 of
+ * the largest magnitude in it; where that passes the 16-bit type's largest number,
+ * outputs in that type are infinite.
  *
  * What is behind a unit's length is free: the calls may write there, and what
  * it holds is never read as data.  A length outside 0..capacity counts as the
@@ -506,7 +510,7 @@ int compresskv_q4_gather(const ckv_problem* p, const ckv_q4_cache* c, int32_t gr
  * of its terms' magnitudes.  Inside the sum over the slots, p, p times a slot's
  * scale, and the middle of a group's range enter as two fp16 parts each; for
  * bf16 outputs the first two as one (off by at most 2^-11 of themselves).  What
- * is below fp16's range is lost: a slot's weight p |V| is off by up to 2^-27 of
+ * is below fp16's range is lost: a slot's weight p |V| is off by up to 2^-26 of
  * the row's largest, and a group of a slot whose scale is below 2^-20 of the
  * largest magnitude in its row of V by more than 2^-11 of itself.  The results
  * are the same bits on every call with the same shapes, lengths and SMs. */

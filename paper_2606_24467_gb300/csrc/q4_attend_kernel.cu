@@ -13,13 +13,13 @@
 // last of them to come, always in slot order.
 //
 // Measured, in a graph of 20 calls: four sequences of 128K slots, 8 groups of 4
-// heads, 128.1 us, 5.24 TB/s of the 6.78 that a copy reaches (the loads alone
+// heads, 134 us, 5.0 TB/s of the 6.78 that a copy reaches (the loads alone
 // take 108): two warps a scheduler issue in 46 % of the cycles, the tensor cores
-// are busy in 32 %.  One sequence of 32K slots 18.4 us and of 777 9.9, where
+// are busy in 30 %.  One sequence of 32K slots 18.9 us and of 777 10.3, where
 // fixed latencies add up: the scan of the lengths (1 us), the first copies and
 // the queries (2), the first tile with no instruction cached (2), the joins in a
 // CTA and over CTAs (2 to 5).  64 sequences of 1000 to 8000 slots, 8 groups of 8
-// heads, f16, with weights, 122 us against 56 for the bytes: instructions.
+// heads, f16, with weights, 125 us against 56 for the bytes: instructions.
 //
 // Codes enter the tensor cores as they are.  A nibble n masked out of a word is
 // the fp16 subnormal n * 2^-24 (one in bits 4-7 is 16 n * 2^-24), exact in a
@@ -30,8 +30,10 @@
 // in shared memory, four times the bytes of the codes.
 //
 //   S^T = K Q^T: A = codes of 16 slots, B = 8 query rows (as fp16, scaled by a
-//     power of two a row so that the largest element is in [2^14, 2^15): exact
-//     but for elements below 2^-34 of it); the four groups are summed apart and
+//     power of two a row so that the largest element is in [2^14, 2^15), odd
+//     channels by 1/16 of it: bf16 elements are exact down to 2^-31 of the largest
+//     (even channels) and 2^-27 (odd ones), f16 ones to 2^-28 and 2^-24, and smaller
+//     ones off by at most 2^-39 and 2^-35 of it); the four groups are summed apart and
 //     scaled by their s in fp32.  The minima's term sum_J m_J (sum of q over J)
 //     is one more product: the group sums as three bf16 parts (24 bits), m in bf16.
 //   O^T = V^T P^T: A = codes of 16 channels, B = P^T, which movmatrix makes of
@@ -90,16 +92,18 @@ constexpr int kMaxGain = 122;          // weights are p 2^(e - 12) times 2^gain
 
 // A row block of up to two tiles a warp is one CTA's; longer ones are shared,
 // by CTAs of at least four tiles.  Joining over CTAs costs about 3 us, a warp's
-// further tile 2.5.  Eight units of 777 slots (two tiles a warp): 10.0 us, and
-// 10.8 shared; of 2048 slots (four): 15.4 on one CTA each, 10.8 shared; of 4096
-// slots by CTAs of 2, 4, 8 and 16 tiles: 10.8, 11.0, 11.4 and 13.6 us.
+// further tile 2.5.  Eight units of 777 slots (two tiles a warp): 10.4 us, and
+// 11.2 shared; of 2048 slots (four): 16.0 on one CTA each, 11.2 shared; of 4096
+// slots by CTAs of 2, 4, 8 and 16 tiles: 11.4, 11.3, 12.0 and 14.5 us.  64 units of
+// 2048 slots: 14.7 us shared, 16.7 on one CTA each.
 constexpr int kMinTiles = 4;
 constexpr int kSoloTiles = 2;
 
-// Eight warps of 64 slots a step with the next 64 on their way: 173 KB a CTA.
-// More warps of fewer slots issue more instructions a slot: for four sequences of
-// 128K slots 127.5 us, and 147 with 12 warps of 32, 140 with 16 and 175 with 8; for
-// one of 777 slots 9.8, and 10.1, 10.8 and 11.4.
+// Eight warps of 64 slots a step with the next 64 on their way: 183 KB a CTA.
+// More warps of fewer slots issue more instructions a slot: measured when V's
+// exponents were not yet a slot's own, for four sequences of 128K slots 127.5 us,
+// and 147 with 12 warps of 32, 140 with 16 and 175 with 8; for one of 777 slots
+// 9.8, and 10.1, 10.8 and 11.4.
 // A warp's stage holds the codes of K and V (swizzled); their params and the
 // positions lie in an area of their own.
 template <int NB>
@@ -454,8 +458,8 @@ __global__ void __launch_bounds__(Shape<NB>::kThreads, 1)
     chunk = even_chunk(total);
     // Where the row blocks come out about even over whole CTAs, each has its
     // own: one where it is short, else in proportion.  No CTA then joins the end
-    // of one row block and the start of another (8 units of 300 slots: 7.5 us, and
-    // 12.6 in equal runs; of 32K slots 18.4 and 20.9).
+    // of one row block and the start of another (8 units of 300 slots: 7.7 us, and
+    // 10.4 in equal runs; of 32K slots 19.1 and 22.7).
     // (Quotients in fp32: every warp takes the same ones, near enough.)
     int own[kPer], own_mine = 0, own_chunk = 0;
     const float rate = __fdividef(static_cast<float>(ctas), static_cast<float>(total));
@@ -1267,8 +1271,8 @@ __device__ __forceinline__ void write_row(const Q4AttendParams& p, int unit, int
 // ---------------------------------------------------------------- weights
 // A thread takes a slot, whose logits lie side by side: kWide of them a read,
 // four where the rows are a multiple of four (28 rows of 32 units of 1000 to
-// 8000 slots, attention and weights: 49.0 us, and 51.6 in pairs; 8 rows of 64
-// units: 29.8 and 30.2).  (Groups of lanes that share a slot, or several slots a
+// 8000 slots, attention and weights: 47.7 us, and 52.2 in pairs; 8 rows of 64
+// units: 28.4 and 28.8).  (Groups of lanes that share a slot, or several slots a
 // thread, took half as long again: more instructions, and more lines at once than
 // L1 holds.)  Bound by L2, which holds the logits of some 30 MB: 21 us for 2.3
 // million slots of 8 rows, whose logits and weights are 92 MB.

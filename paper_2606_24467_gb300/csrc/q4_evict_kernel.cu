@@ -410,6 +410,9 @@ cudaError_t q4_evict_set_smem_limit() {
 cudaError_t launch_q4_evict(const Q4EvictParams& params, int sms, cudaStream_t stream) {
   Q4EvictParams p = params;
   const long long units = static_cast<long long>(p.c.batch) * p.c.num_kv_heads;
+  // (All by the capacity: the host does not know the lengths.  256 units of 1100
+  // slots that lose 76 take 7.7 us in a cache of 1152 slots each, 23 in one of 16K
+  // and 124 in one of 64K.)
   const int cap = p.c.capacity;
   // Long units share the SMs that there are no other units for, and those that
   // no CTA holds: 8 units of 8000, 16000 and 32000 slots 18.4, 19.7 and 24.3 us,

@@ -59,18 +59,18 @@ using Q4GatherUnitParams = Q4WriteParams<kQ4UnitTable>;
 constexpr int kQ4Tile = 64;  // attention: slots of a tile,
 constexpr int kQ4Warps = 8;  // warps of a CTA (there is one an SM),
 // query rows of a row block.  16 rows share the work on their codes, but leave
-// fewer tiles to a warp and take every register: 16 rows a unit (two heads of
-// eight query heads, bf16) take 39 us in blocks of 16 and 35 in blocks of 8 at
-// 64 units of 1000 to 8000 slots, four of 777 tokens 14 and 10, but 16 rows of
-// 32 units of 128K slots 201 and 241, 20 of 512 units of 1000 to 8000 (with
-// weights) 332 and 386.  `slots`: of all units.
+// fewer tiles to a warp and take every register: 16 rows a unit (bf16) take 37.5
+// us in blocks of 16 and 32.6 in blocks of 8 at 64 units of 1000 to 8000 slots,
+// at four of 777 14.7 and 10.4, but 16 rows of 32 units of 128K slots 205 and 254,
+// 20 of 512 units of 1000 to 8000 (with weights) 327 and 374.  `slots`: the
+// capacity of all units, as the host does not know the lengths.
 constexpr int q4_block_rows(int rows, long long slots) { return rows <= 8 || slots <= 1 << 20 ? 8 : 16; }
 
 // Attention.  The tiles of all row blocks -- some query rows of a unit -- form one sequence, of which every CTA takes an equal run, and every
 // warp of it a run of that; or, where they come out about even that way, each row
 // block has CTAs of its own.
 struct Q4AttendParams {
-  CUtensorMap map_k, map_v;    // codes: [units * capacity] rows of 64 bytes, boxes of 32 rows
+  CUtensorMap map_k, map_v;    // codes: [units * capacity] rows of 64 bytes, boxes of kQ4Tile rows
   Q4Cache c;
   const uint16_t* q;           // f16 / bf16 bits
   uint16_t* out;
@@ -100,15 +100,14 @@ struct Q4EvictParams {
   int budget;                  // where `budgets` is null
   int sinks, recent;
   int cluster;                 // CTAs a unit (set at the launch)
-  int32_t* lists;              // workspace: [units][capacity] pairs of slots
+  int32_t* lists;              // workspace: [units][capacity]: the holes, from capacity / 2 on the rows
   int* status;
 };
 
 // Launches a kernel that may be brought up while the one before it in the
 // stream ends (its first act is then to wait for that one's results).  Only a
 // kernel that another of the same call follows lets its successor start before
-// its own end: what comes after a call may read the call's outputs at once, as
-// the scoring kernel reads K.
+// its own end: whatever comes after a call finds its outputs complete.
 template <class... A>
 cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t stream,
                              const A&... args) {

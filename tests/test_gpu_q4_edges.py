@@ -126,3 +126,21 @@ def test_attend_when_a_later_slot_outweighs_large_values(cuda_device):
         spread(c, 0, 0, torch.arange(100, 192, device=cuda_device), later)
         q = (0.2 + 0.05 * torch.randn((1, 4, 1, 128), generator=gen)).bfloat16().to(cuda_device)
         run_attend(c, q)
+
+
+def test_values_beyond_the_largest_f16_number(cuda_device):
+    """A group from -65504 to 65504: its top code stands for more than f16 holds."""
+    k = torch.zeros((1, 1, 128)).half()
+    k[0, 0, 0], k[0, 0, 1], k[0, 0, 2] = 65504.0, -65504.0, 60000.0
+    c = blank(1, 1, 32, cuda_device)
+    kd = k.to(cuda_device)
+    kv, vv = torch.empty_like(kd), torch.empty_like(kd)
+    c.lengths.zero_()
+    ckv.q4_append(c, kd, kd, torch.zeros(1, dtype=torch.int32, device=cuda_device), k_values=kv, v_values=vv)
+    codes, s, m = q4.quantise(k[0].float().numpy())
+    want = q4.values(codes, s, m)
+    assert 65520 < want[0, 0] < 65504 * (1 + 2.0 ** -6)
+    assert torch.equal(kv.cpu()[0], torch.from_numpy(want).half()) and torch.isinf(kv[0, 0, 0])
+    q = torch.zeros((1, 1, 1, 128), device=cuda_device).bfloat16()
+    out, _ = run_attend(c, q, accumulate=False)
+    assert torch.isfinite(out).all()
