@@ -547,8 +547,8 @@ int compresskv_read_device_status(const void* workspace, void* stream, int32_t* 
  * CKV_ERR_INVALID_ARG).  Process-wide, one-shot; not for production use. */
 int compresskv_debug_stall_next_fused_call(long long wait_ns);
 
-/* The same for compresskv_q4_attend: one warp of the next call that holds
- * slots waits, its copies under way, for a barrier that nothing completes.  The
+/* The same for compresskv_q4_attend: one warp of the next call (if that holds
+ * slots) waits, its copies under way, for a barrier that nothing completes.  The
  * wait runs out after wait_ns and its CTA stops; the status reads
  * CKV_ERR_DEVICE_TIMEOUT, and compresskv_q4_workspace_init makes the workspace
  * usable again. */
