@@ -82,7 +82,8 @@ enum {
   CKV_ERR_DEVICE_TIMEOUT = -7,  /* a kernel's bounded wait ran out (device status only) */
   CKV_ERR_DEVICE_INDEX = -8,    /* an index outside its sequence: given to compresskv_gather, or
                                    produced by a selection (a device self-check); a row without
-                                   room in its unit of a 4-bit cache */
+                                   room in its unit of a 4-bit cache; a row outside its sequence,
+                                   or a page outside the pool, of a paged cache */
   CKV_ERR_STATIC_SCRATCH = -9   /* problem needs more than CKV_STATIC_SCRATCH_BYTES of scratch */
 };
 
@@ -123,7 +124,11 @@ enum {
   CKV_KERNEL_FUSED = 5,         /* all four steps for every unit of a call (persistent kernels) */
   CKV_KERNEL_Q4_WRITE = 6,      /* rows into a 4-bit cache (append, gather) */
   CKV_KERNEL_Q4_ATTEND = 7,     /* attention over a 4-bit cache */
-  CKV_KERNEL_Q4_EVICT = 8       /* eviction from a 4-bit cache */
+  CKV_KERNEL_Q4_EVICT = 8,      /* eviction from a 4-bit cache */
+  CKV_KERNEL_ROPE = 9,          /* rotary positions of rows */
+  CKV_KERNEL_PAGED_WRITE = 10,  /* rows into a paged cache */
+  CKV_KERNEL_PAGED_GATHER = 11, /* rows out of a paged cache */
+  CKV_KERNEL_PAGED_ATTEND = 12  /* attention over a paged cache */
 };
 
 /* Optional launch trace.  When ckv_problem.trace is non-null every kernel
@@ -531,6 +536,190 @@ int compresskv_q4_attend(const ckv_q4_cache* c, const ckv_q4_queries* a, const v
  *   the protected slots.  A `budget` below sinks + recent is CKV_ERR_BUDGET. */
 int compresskv_q4_evict(const ckv_q4_cache* c, int32_t budget, const int32_t* budgets, int32_t sinks,
                         int32_t recent, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------- rotary positions
+ * The rotation of Q and K by the token's position, which the compression takes
+ * for granted ("post-RoPE").  Of each head's row the first rot_dim channels
+ * form rot_dim / 2 pairs (a_i, b_i): channels (i, i + rot_dim / 2), or
+ * (2i, 2i + 1) where interleaved; at position m
+ *   a' = scale (a cos(m f_i) - b sin(m f_i)),
+ *   b' = scale (a sin(m f_i) + b cos(m f_i)).
+ * The other channels are copied.  Angles are exact: a frequency is held as
+ * turns a position in units of 2^-64, so that m f_i is right to 2^-32 of a turn
+ * at every 32-bit position; cosine, sine and products are fp32, rounded once. */
+typedef struct ckv_rope {
+  int32_t rot_dim;          /* even, 2..128 */
+  int32_t interleaved;      /* non-zero: pairs (2i, 2i + 1) */
+  float scale;              /* of the rotated channels (finite) */
+  int32_t reserved;
+  uint64_t turns[64];       /* filled by compresskv_rope_init */
+} ckv_rope;
+
+/* How frequencies f_i = base^(-2i / rot_dim) are scaled for contexts `factor`
+ * times as long as those they were made for. */
+enum {
+  CKV_ROPE_PLAIN = 0,       /* f_i */
+  CKV_ROPE_LINEAR = 1,      /* f_i / factor (positions interpolated) */
+  CKV_ROPE_BASE = 2,        /* of base * factor^(rot_dim / (rot_dim - 2)): the longest wave is
+                               stretched by factor, the shortest stays (rot_dim > 2) */
+  CKV_ROPE_WAVES = 3,       /* by the turns t_i = original_length f_i / 2 pi of a wave: keep_i =
+                               (t_i - low) / (high - low) within 0..1, f_i (keep_i + (1 - keep_i) / factor) */
+  CKV_ROPE_RAMP = 4         /* likewise, but keep_i falls linearly in i between the channels (rounded
+                               outwards to whole ones) whose waves make `high` and `low` turns */
+};
+
+/* Host only: frequencies (double [rot_dim / 2], radians a position).  factor >= 1
+ * and finite, base > 0 (RAMP: > 1); WAVES and RAMP also take original_length > 0
+ * and 0 < low < high; else CKV_ERR_INVALID_ARG. */
+int compresskv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                double original_length, double low, double high, double* frequencies);
+
+/* Host only: fills *r.  frequencies: double [rot_dim / 2], finite, at most 2^20
+ * in magnitude. */
+int compresskv_rope_init(ckv_rope* r, int32_t rot_dim, int32_t interleaved, const double* frequencies,
+                         double scale);
+
+/* Rows to rotate: q [rows][num_q_heads][128] and k [rows][num_k_heads][128],
+ * head_dim contiguous, bases 16-byte aligned, strides (elements) multiples of 8
+ * and not negative; outputs the same shapes.  Outputs whose rows overlap are
+ * refused, and so is an output that shares memory with its input otherwise
+ * than by being it (same address and strides: in place). */
+typedef struct ckv_rope_rows {
+  int32_t rows;
+  int32_t num_q_heads;      /* 0..256 */
+  int32_t num_k_heads;      /* 0..256 */
+  int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16 */
+  int32_t backward;         /* non-zero: by minus the angles -- the gradient of the rotation, and its
+                               inverse where scale is 1 */
+  int32_t reserved;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+  ckv_trace* trace;         /* optional launch trace, NULL for none */
+} ckv_rope_rows;
+
+/* Rotate rows; positions: device int32 [rows] (any 32-bit value).  q or k is
+ * NULL exactly where it has no heads. */
+int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32_t* positions,
+                          const void* q, const void* k, void* q_out, void* k_out, void* stream);
+
+/* ------------------------------------------------------------ paged cache
+ * The 16-bit cache that a prompt is prefilled into, chunk by chunk, before it is
+ * compressed: compresskv_paged_append writes rows (rotating K, and Q with it),
+ * compresskv_paged_attend attends over them and gives the log-sum-exp that
+ * compresskv_compress_layer(s)_lse takes, and compresskv_paged_gather packs a
+ * prompt's rows as the compression takes them.
+ *
+ * A pool of num_pages pages holds page_size slots each; sequence s has the pages
+ * table[s][0..], and its token (slot) j is row j % page_size of page
+ * table[s][j / page_size].  Element (page, slot, head, c) of K is at k_pages +
+ * page*page_stride + slot*slot_stride + head*head_stride + c, and V's likewise.
+ * lengths[s] slots are in use.  Table entries behind them are not read.  A
+ * length or first row beyond what the table holds (table_width * page_size)
+ * counts as that, and a negative one marks a sequence that is not there: nothing
+ * is written for it, and its attention sees nothing.  Slots behind the length may
+ * hold anything, NaN among it.
+ * Calls that use one workspace must not overlap on the GPU, and neither must two
+ * calls of which one writes what the other uses. */
+typedef struct ckv_paged_cache {
+  int32_t batch;            /* sequences, 1..512 */
+  int32_t num_kv_heads;     /* 1..64 */
+  int32_t head_dim;         /* 128 */
+  int32_t dtype;            /* CKV_DTYPE_F16 | CKV_DTYPE_BF16 */
+  int32_t page_size;        /* 16, 32, 64, 128 or 256 */
+  int32_t num_pages;
+  int32_t table_width;      /* pages of a sequence; table_width * page_size is at most 2^24 */
+  int32_t reserved;
+  void* k_pages;            /* 16-byte aligned */
+  void* v_pages;
+  int64_t page_stride;      /* elements, multiples of 8; rows that overlap are refused */
+  int64_t slot_stride;
+  int64_t head_stride;
+  const int32_t* table;     /* device [batch][table_stride] */
+  int64_t table_stride;     /* elements, at least table_width */
+  int32_t* lengths;         /* device [batch] */
+  ckv_trace* trace;         /* optional launch trace, NULL for none */
+} ckv_paged_cache;
+
+/* Rows of sequences, packed: k and v [rows][num_kv_heads][128], q and q_out
+ * [rows][num_q_heads][128]; as in ckv_rope_rows. */
+typedef struct ckv_paged_rows {
+  int32_t rows_per_seq;     /* rows of every sequence, where cu_rows is NULL */
+  int32_t num_q_heads;      /* 0: no q */
+  const int32_t* cu_rows;   /* host [batch+1]: sequence s has rows cu_rows[s] .. */
+  int64_t kv_token_stride, kv_head_stride;   /* V shares K's strides */
+  int64_t q_token_stride, q_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride;
+} ckv_paged_rows;
+
+/* Write rows of new tokens: row i of sequence s goes to its slot start[s] + i,
+ * and lengths[s] becomes start[s] + its rows (at most what the table holds).
+ * start: optional device int32 [batch]; NULL, or the cache's lengths: the
+ *   lengths.  (Otherwise it must not share memory with them.)
+ * rope: NULL writes K as it is; else K is rotated, and so are the q rows (which
+ *   need a rope) into q_out, by the rows' positions.
+ * positions: optional device int32 [rows]; NULL: the slots.
+ * A row without a slot in the table, or whose page is outside the pool, is not
+ * written; it sets *device_status (optional device int32) to
+ * CKV_ERR_DEVICE_INDEX if that is 0.  Rows of sequences that are not there are
+ * skipped, q_out among them. */
+int compresskv_paged_append(const ckv_paged_cache* c, const ckv_paged_rows* r, const void* k,
+                            const void* v, const int32_t* start, const ckv_rope* rope,
+                            const int32_t* positions, const void* q, void* q_out,
+                            int32_t* device_status, void* stream);
+
+/* Read rows back: row i of sequence s is its slot start[s] + i.
+ * k_out, v_out: [rows][num_kv_heads][128] contiguous, 16-byte aligned; either
+ *   may be NULL.  cu_rows / rows_per_seq as in ckv_paged_rows.
+ * start: optional device int32 [batch]; NULL: 0.
+ * A row at or behind the length, or of a page outside the pool, is left as it
+ * was in the outputs and reported like compresskv_paged_append's; rows of
+ * sequences that are not there (start or length negative) are left without a
+ * report. */
+int compresskv_paged_gather(const ckv_paged_cache* c, const int32_t* cu_rows, int32_t rows_per_seq,
+                            const int32_t* start, void* k_out, void* v_out, int32_t* device_status,
+                            void* stream);
+
+/* Query tokens: q and out [rows][num_q_heads][128], packed by sequence. */
+typedef struct ckv_paged_queries {
+  int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads, at most 128 a KV head */
+  int32_t rows_per_seq;     /* query tokens of every sequence, where cu_rows is NULL */
+  const int32_t* cu_rows;   /* host [batch+1] */
+  int32_t causal;           /* non-zero: a token sees the slots up to its own */
+  float scale;              /* softmax scale, at most 2^96; 0 selects 1/sqrt(head_dim) */
+  int64_t q_token_stride, q_head_stride;     /* elements, multiples of 8; q's positive */
+  int64_t out_token_stride, out_head_stride;
+} ckv_paged_queries;
+
+/* Bytes of workspace for compresskv_paged_attend with these heads and at most
+ * num_queries query tokens of a sequence; 0 if invalid. */
+size_t compresskv_paged_workspace_size(const ckv_paged_cache* c, int32_t num_q_heads, int32_t num_queries);
+
+/* Zero the workspace's header (on `stream`): once after allocating it and after
+ * reading a non-zero status; every call that completes leaves it ready. */
+int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of chunks of query tokens over the pages:
+ *   z_j = scale * q . K_j,  p = softmax of z over the visible slots,
+ *   out = sum_j p_j V_j (rounded to the dtype),  lse = log sum_j exp(z_j).
+ * Query token i of sequence s stands at slot start[s] + i; start: optional
+ *   device int32 [batch]; NULL: the sequence's newest slots, lengths[s] - rows.
+ *   It sees the slots in use up to its own (causal) or all in use.  A token that
+ *   sees none gives out = 0 and lse = -infinity.
+ * lse: optional device float [num_q_heads][rows]: with equal rows a sequence,
+ *   the last W of them are lse_win of compresskv_compress_layer_lse with
+ *   lse_batch_stride = rows a sequence and lse_head_stride = rows.
+ * What a token does not see leaves no trace in its results, infinities and NaN
+ * among it; what it sees propagates.  A page outside the pool counts as zeros,
+ * and sets the workspace's status to CKV_ERR_DEVICE_INDEX if it is 0.
+ * A wait that runs out (2 s) sets it to CKV_ERR_DEVICE_TIMEOUT if it is 0; out
+ * and lse are then undefined, in this call and the ones after it, until
+ * compresskv_paged_workspace_init.
+ * Logits, softmax sums and outputs are held in fp32; the probabilities enter the
+ * product with V rounded once to the dtype.  The results are the same bits on
+ * every call with the same shapes, lengths and SMs. */
+int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a, const void* q,
+                            const int32_t* start, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* Synchronise `stream`, copy the workspace status word to *status and return
  * CKV_OK (or CKV_ERR_CUDA if the copy fails). */

@@ -9,8 +9,10 @@ from . import compresskv  # noqa: F401
 from .compresskv import (  # noqa: F401
     CompressKVError,
     LayerOutputs,
+    PagedCache,
     Problem,
     Q4Cache,
+    Rope,
     Trace,
     allocate_layer_budgets,
     compress_layer,
@@ -25,6 +27,12 @@ from .compresskv import (  # noqa: F401
     head_budget_layout,
     load,
     output_layout,
+    paged_append,
+    paged_attend,
+    paged_cache,
+    paged_gather,
+    paged_workspace,
+    paged_workspace_size,
     q4_append,
     q4_attend,
     q4_cache,
@@ -33,6 +41,8 @@ from .compresskv import (  # noqa: F401
     q4_workspace,
     q4_workspace_size,
     read_device_status,
+    rope_apply,
+    rope_frequencies,
     score,
     select,
     status_string,

@@ -20,7 +20,8 @@ LIB_PATH = os.path.join(OUT_DIR, "libcompresskv.so")
 SOURCES = ["api.cu", "fused_kernel.cu", "resident_kernel.cu", "score_kernel.cu", "combine_kernel.cu", "select_kernel.cu",
            "pool_kernel.cu",
            "gather_kernel.cu", "q4_api.cu", "q4_write_kernel.cu", "q4_attend_kernel.cu",
-           "q4_evict_kernel.cu", "budget_alloc.cpp"]
+           "q4_evict_kernel.cu", "paged_api.cu", "rope_kernel.cu", "paged_gather_kernel.cu",
+           "paged_attend_kernel.cu", "budget_alloc.cpp", "rope_table.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -34,7 +34,9 @@ CKV_POOL_MAX = 1
 CKV_SELECT_PER_GROUP = 0
 CKV_SELECT_PER_LAYER = 1
 KERNEL_KINDS = {1: "score", 2: "combine", 3: "select", 4: "gather", 5: "fused", 6: "q4_write",
-                7: "q4_attend", 8: "q4_evict"}
+                7: "q4_attend", 8: "q4_evict", 9: "rope", 10: "paged_write", 11: "paged_gather",
+                12: "paged_attend"}
+ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "waves": 3, "ramp": 4}
 Q4_TILE = 32  # a 4-bit cache's capacity is a multiple of this
 
 EXPORTED = (
@@ -61,6 +63,14 @@ EXPORTED = (
     "compresskv_q4_gather",
     "compresskv_q4_attend",
     "compresskv_q4_evict",
+    "compresskv_rope_frequencies",
+    "compresskv_rope_init",
+    "compresskv_rope_apply",
+    "compresskv_paged_append",
+    "compresskv_paged_gather",
+    "compresskv_paged_workspace_size",
+    "compresskv_paged_workspace_init",
+    "compresskv_paged_attend",
 )
 
 
@@ -97,6 +107,44 @@ class CkvQ4Queries(ctypes.Structure):
                 ("q_batch_stride", c_int64), ("q_head_stride", c_int64),
                 ("q_query_stride", c_int64), ("out_batch_stride", c_int64),
                 ("out_head_stride", c_int64), ("out_query_stride", c_int64)]
+
+
+class CkvRope(ctypes.Structure):
+    _fields_ = [("rot_dim", c_int32), ("interleaved", c_int32), ("scale", c_float),
+                ("reserved", c_int32), ("turns", ctypes.c_uint64 * 64)]
+
+
+class CkvRopeRows(ctypes.Structure):
+    _fields_ = [("rows", c_int32), ("num_q_heads", c_int32), ("num_k_heads", c_int32),
+                ("dtype", c_int32), ("backward", c_int32), ("reserved", c_int32),
+                ("q_token_stride", c_int64), ("q_head_stride", c_int64),
+                ("k_token_stride", c_int64), ("k_head_stride", c_int64),
+                ("q_out_token_stride", c_int64), ("q_out_head_stride", c_int64),
+                ("k_out_token_stride", c_int64), ("k_out_head_stride", c_int64),
+                ("trace", POINTER(CkvTrace))]
+
+
+class CkvPagedCache(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32),
+                ("dtype", c_int32), ("page_size", c_int32), ("num_pages", c_int32),
+                ("table_width", c_int32), ("reserved", c_int32), ("k_pages", c_void_p),
+                ("v_pages", c_void_p), ("page_stride", c_int64), ("slot_stride", c_int64),
+                ("head_stride", c_int64), ("table", c_void_p), ("table_stride", c_int64),
+                ("lengths", c_void_p), ("trace", POINTER(CkvTrace))]
+
+
+class CkvPagedRows(ctypes.Structure):
+    _fields_ = [("rows_per_seq", c_int32), ("num_q_heads", c_int32), ("cu_rows", c_void_p),
+                ("kv_token_stride", c_int64), ("kv_head_stride", c_int64),
+                ("q_token_stride", c_int64), ("q_head_stride", c_int64),
+                ("q_out_token_stride", c_int64), ("q_out_head_stride", c_int64)]
+
+
+class CkvPagedQueries(ctypes.Structure):
+    _fields_ = [("num_q_heads", c_int32), ("rows_per_seq", c_int32), ("cu_rows", c_void_p),
+                ("causal", c_int32), ("scale", c_float), ("q_token_stride", c_int64),
+                ("q_head_stride", c_int64), ("out_token_stride", c_int64),
+                ("out_head_stride", c_int64)]
 
 
 class CompressKVError(RuntimeError):
@@ -158,6 +206,16 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "compresskv_q4_gather": (c_int32, [pp, vp, c_int32, vp, i32p, vp, vp, vp, vp, vp, vp, vp]),
         "compresskv_q4_attend": (c_int32, [vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
         "compresskv_q4_evict": (c_int32, [vp, c_int32, vp, c_int32, c_int32, vp, c_size_t, vp]),
+        "compresskv_rope_frequencies": (c_int32, [c_int32, ctypes.c_double, c_int32,
+                                                  ctypes.c_double, ctypes.c_double,
+                                                  ctypes.c_double, ctypes.c_double, vp]),
+        "compresskv_rope_init": (c_int32, [vp, c_int32, c_int32, vp, ctypes.c_double]),
+        "compresskv_rope_apply": (c_int32, [vp, vp, vp, vp, vp, vp, vp, vp]),
+        "compresskv_paged_append": (c_int32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "compresskv_paged_gather": (c_int32, [vp, vp, c_int32, vp, vp, vp, vp, vp]),
+        "compresskv_paged_workspace_size": (c_size_t, [vp, c_int32, c_int32]),
+        "compresskv_paged_workspace_init": (c_int32, [vp, c_size_t, vp]),
+        "compresskv_paged_attend": (c_int32, [vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -638,11 +696,16 @@ def q4_cache(batch: int, num_kv_heads: int, capacity: int, device=None, weights:
                    empty(lead, torch.float32) if weights else None, trace)
 
 
-def _q4_call(name: str, cache: Q4Cache, stream, *args):
+def _q4_call(name: str, cache, stream, *args):
     """Enqueues on `stream` (default: the current stream of the cache's device)."""
-    index = cache.index
-    if index < 0:
+    if cache.index < 0:
         _invalid("the cache must be in device memory")
+    _device_call(name, cache.index, stream, *args)
+
+
+def _device_call(name: str, index: int, stream, *args):
+    if index < 0:
+        _invalid("tensors must be in device memory")
     fn = _fast(name)
     if stream is None:
         stream = torch._C._cuda_getCurrentRawStream(index)
@@ -817,3 +880,279 @@ def q4_evict(cache: Q4Cache, budget, ws, sinks: int = 0, recent: int = 0, stream
     _q4_on_device(cache, "budget and workspace", budgets, ws)
     _q4_call("compresskv_q4_evict", cache, stream, cache.addr, _q4_int(budget, "budget"), _addr(budgets),
              _q4_int(sinks, "sinks"), _q4_int(recent, "recent"), _addr(ws), ws.numel())
+
+
+# ------------------------------------------------------------ rotary positions
+def rope_frequencies(rot_dim: int = 128, base: float = 10000.0, scaling: "str | None" = None,
+                     factor: float = 1.0, original_length: float = 0.0, low: float = 1.0,
+                     high: float = 4.0) -> np.ndarray:
+    """Rotary frequencies (float64 ``[rot_dim / 2]``, radians a position), plain or
+    scaled for contexts ``factor`` times as long: "linear" (positions
+    interpolated), "base" (a larger base), "waves" / "ramp" (only the waves that
+    make few turns over ``original_length``; see the header)."""
+    if scaling not in ROPE_SCALINGS:
+        _invalid(f"scaling must be one of {list(ROPE_SCALINGS)}")
+    f = np.zeros(64, np.float64)
+    rot_dim = _q4_int(rot_dim, "rot_dim")
+    _check(_fast("compresskv_rope_frequencies")(rot_dim, float(base), ROPE_SCALINGS[scaling],
+                                                float(factor), float(original_length), float(low),
+                                                float(high), f.ctypes.data),
+           "compresskv_rope_frequencies")
+    return f[:rot_dim // 2]
+
+
+class Rope:
+    """A rotary table (wraps ``ckv_rope``): pairs (i, i + rot_dim / 2) of a head's
+    first ``rot_dim`` channels, or (2i, 2i + 1) where ``interleaved``, turn by
+    position times frequency and are multiplied by ``scale``.  ``frequencies``
+    (float64 ``[rot_dim / 2]``) replaces those of rope_frequencies."""
+
+    def __init__(self, rot_dim: int = 128, base: float = 10000.0, interleaved: bool = False,
+                 scaling: "str | None" = None, factor: float = 1.0, original_length: float = 0.0,
+                 low: float = 1.0, high: float = 4.0, scale: float = 1.0, frequencies=None):
+        rot_dim = _q4_int(rot_dim, "rot_dim")
+        if frequencies is None:
+            f = rope_frequencies(rot_dim, base, scaling, factor, original_length, low, high)
+        else:
+            f = np.ascontiguousarray(frequencies, np.float64)
+            if f.shape != (rot_dim // 2,):
+                _invalid("frequencies must be [rot_dim / 2]")
+        self.rot_dim, self.interleaved, self.frequencies = rot_dim, bool(interleaved), f.copy()
+        self.struct = CkvRope()
+        self.addr = ctypes.addressof(self.struct)
+        _check(_fast("compresskv_rope_init")(self.addr, rot_dim, int(self.interleaved), f.ctypes.data,
+                                             float(scale)), "compresskv_rope_init")
+
+
+def _head_rows(t, rows, what, dtype=None):
+    """(heads, token stride, head stride) of rows [rows, heads, 128]."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != rows or shape[2] != 128 or strides[2] != 1:
+        _invalid(f"{what} must be [rows, heads, 128], head_dim contiguous")
+    if dtype is not None and t.dtype != dtype:
+        _invalid(f"{what} must be {dtype}")
+    # a dimension of one element has a stride that means nothing
+    heads = shape[1]
+    head = strides[1] if heads > 1 else 128
+    return heads, strides[0] if rows > 1 else max(heads, 1) * 128, head
+
+
+def _rows_i32(t, rows, what):
+    if t is not None and (t.dtype != torch.int32 or t.shape != (rows,) or not t.is_contiguous()):
+        _invalid(f"{what} must be a contiguous int32 tensor {(rows,)}")
+
+
+def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, backward: bool = False,
+               trace: "Trace | None" = None, stream=None) -> None:
+    """Rotates ``q`` ``[rows, H_q, 128]`` (and ``k`` ``[rows, H_k, 128]``) by
+    ``positions`` (int32 ``[rows]``), in place or into ``q_out`` / ``k_out``;
+    ``backward``: by minus the angles (the gradient)."""
+    rows = q.shape[0]
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    if (k is None) != (k_out is None):
+        _invalid("k_out without k")
+    dtype = _q4_dtype(q)
+    hq, qt, qh = _head_rows(q, rows, "q")
+    ho, qot, qoh = _head_rows(q_out, rows, "q_out", q.dtype)
+    hk, kt, kh, kot, koh = 0, 0, 0, 0, 0
+    if k is not None:
+        hk, kt, kh = _head_rows(k, rows, "k", q.dtype)
+        h, kot, koh = _head_rows(k_out, rows, "k_out", q.dtype)
+        if h != hk:
+            _invalid("k_out must have k's shape")
+    if ho != hq:
+        _invalid("q_out must have q's shape")
+    _rows_i32(positions, rows, "positions")
+    index = q.get_device()
+    for t in (positions, k, q_out, k_out):
+        if t is not None and t.get_device() != index:
+            _invalid("q, k, positions and outputs must be on one device")
+    x = CkvRopeRows(rows, hq, hk, dtype, int(bool(backward)), 0, qt, qh, kt, kh, qot, qoh, kot, koh,
+                    ctypes.pointer(trace.struct) if trace is not None else None)
+    _device_call("compresskv_rope_apply", index, stream, rope.addr, ctypes.addressof(x), _addr(positions),
+                 _addr(q) if hq else None, _addr(k) if hk else None, _addr(q_out) if hq else None,
+                 _addr(k_out) if hk else None)
+
+
+# ----------------------------------------------------------------- paged cache
+class PagedCache:
+    """A paged 16-bit KV cache over the caller's tensors (wraps
+    ``ckv_paged_cache``).
+
+    ``k_pages`` / ``v_pages`` are f16 or bf16 ``[pages, page_size, H_kv, 128]``
+    (any strides, 128 contiguous: a pool kept as ``[pages, H_kv, page_size, 128]``
+    is passed as its transpose(1, 2)), ``table`` int32 ``[B, width]`` (the pages
+    of each sequence in order), ``lengths`` int32 ``[B]`` (slots in use; negative:
+    the sequence is not there); all on one device.  The tensors stay the caller's
+    and are kept alive by this object."""
+
+    def __init__(self, k_pages, v_pages, table, lengths, trace: "Trace | None" = None):
+        if k_pages.dim() != 4 or k_pages.shape[3] != 128 or k_pages.stride(3) != 1:
+            _invalid("k_pages must be [pages, page_size, H_kv, 128], head_dim contiguous")
+        dtype = _q4_dtype(k_pages)
+        shape, strides = k_pages.shape, k_pages.stride()
+        if v_pages.dtype != k_pages.dtype or v_pages.shape != shape or any(
+                n > 1 and a != b for n, a, b in zip(shape, strides, v_pages.stride())):
+            _invalid("v_pages must share k_pages' dtype, shape and strides")
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            _invalid("table must be int32 [B, width], its rows contiguous")
+        if lengths.dtype != torch.int32 or lengths.shape != table.shape[:1] or not lengths.is_contiguous():
+            _invalid("lengths must be a contiguous int32 [B]")
+        if any(t.device != k_pages.device for t in (v_pages, table, lengths)):
+            _invalid("pages, table and lengths must be on one device")
+        self.k_pages, self.v_pages, self.table, self.lengths = k_pages, v_pages, table, lengths
+        self.trace, self.dtype = trace, k_pages.dtype
+        self.num_pages, self.page_size, self.num_kv_heads = shape[:3]
+        self.batch, self.table_width = table.shape
+        self.capacity = self.table_width * self.page_size
+        self.device = k_pages.device
+        self.index = k_pages.get_device()
+        # a dimension of one element has a stride that means nothing
+        head = strides[2] if shape[2] > 1 else 128
+        slot = strides[1] if shape[1] > 1 else 128
+        page = strides[0] if shape[0] > 1 else max(head * shape[2], slot * shape[1])
+        self.struct = CkvPagedCache(self.batch, self.num_kv_heads, 128, dtype, self.page_size,
+                                    self.num_pages, self.table_width, 0, _addr(k_pages),
+                                    _addr(v_pages), page, slot, head, _addr(table),
+                                    table.stride(0) if self.batch > 1 else self.table_width,
+                                    _addr(lengths),
+                                    ctypes.pointer(trace.struct) if trace is not None else None)
+        self.addr = ctypes.addressof(self.struct)
+
+    def sequences(self, first: int, count: int) -> "PagedCache":
+        """Sequences ``first .. first + count - 1`` as a cache of their own over
+        the same pool."""
+        first, count = int(first), int(count)
+        if first < 0 or count < 1 or first + count > self.batch:
+            _invalid("sequences outside the cache")
+        cut = slice(first, first + count)
+        return PagedCache(self.k_pages, self.v_pages, self.table[cut], self.lengths[cut], self.trace)
+
+
+def paged_cache(batch: int, num_kv_heads: int, capacity: int, page_size: int = 64,
+                dtype=torch.bfloat16, device=None, trace: "Trace | None" = None) -> PagedCache:
+    """An empty paged cache with a pool of its own, in which every sequence has
+    pages for ``capacity`` slots."""
+    batch, heads, page = int(batch), int(num_kv_heads), int(page_size)
+    width = -(-int(capacity) // page)
+    device = device or "cuda"
+    pools = [torch.empty((batch * width, heads, page, 128), dtype=dtype, device=device).transpose(1, 2)
+             for _ in range(2)]
+    table = torch.arange(batch * width, dtype=torch.int32, device=device).view(batch, width)
+    return PagedCache(*pools, table, torch.zeros(batch, dtype=torch.int32, device=device), trace)
+
+
+def _paged_rows(cache: PagedCache, rows: int, cu_rows):
+    """(rows a sequence, cu_rows to keep alive, its address)."""
+    if cu_rows is None:
+        if rows % cache.batch:
+            _invalid("the rows do not divide by the sequences: give cu_rows")
+        return rows // cache.batch, None, None
+    cu = _host_i32(cu_rows)
+    if cu.shape != (cache.batch + 1,) or int(cu[-1]) != rows:
+        _invalid("cu_rows must be [B+1] and end at the rows")
+    return 0, cu, _data(cu)
+
+
+def paged_append(cache: PagedCache, k, v, cu_rows=None, start=None, rope: "Rope | None" = None,
+                 positions=None, q=None, q_out=None, device_status=None, stream=None) -> None:
+    """Writes rows of new tokens, ``k`` / ``v`` ``[rows, H_kv, 128]`` packed by
+    sequence (``cu_rows``: host ``[B+1]``; None: the same number for each), to
+    the slots from ``start`` (int32 ``[B]``; default: the lengths) on, and sets
+    the lengths.  With a ``rope`` K is rotated on the way, and ``q`` ``[rows, H_q,
+    128]`` into ``q_out`` (default: in place), by ``positions`` (int32 ``[rows]``;
+    default: the slots)."""
+    rows = k.shape[0]
+    heads, kt, kh = _head_rows(k, rows, "k", cache.dtype)
+    vh = _head_rows(v, rows, "v", cache.dtype)
+    if heads != cache.num_kv_heads or vh != (heads, kt, kh):
+        _invalid("k and v must be [rows, H_kv, 128] of the same strides")
+    hq, qt, qh, qot, qoh = 0, 0, 0, 0, 0
+    if q is not None:
+        if rope is None:
+            _invalid("q needs a rope")
+        q_out = q if q_out is None else q_out
+        hq, qt, qh = _head_rows(q, rows, "q", cache.dtype)
+        ho, qot, qoh = _head_rows(q_out, rows, "q_out", cache.dtype)
+        if ho != hq:
+            _invalid("q_out must have q's shape")
+    elif q_out is not None:
+        _invalid("q_out without q")
+    _rows_i32(start, cache.batch, "start")
+    _rows_i32(positions, rows, "positions")
+    _rows_i32(device_status, 1, "device_status")
+    _q4_on_device(cache, "rows, start, positions and status", k, v, start, positions, q, q_out,
+                  device_status)
+    each, cu, at = _paged_rows(cache, rows, cu_rows)
+    r = CkvPagedRows(each, hq, at, kt, kh, qt, qh, qot, qoh)
+    _q4_call("compresskv_paged_append", cache, stream, cache.addr, ctypes.addressof(r), _addr(k),
+             _addr(v), _addr(start), None if rope is None else rope.addr, _addr(positions),
+             _addr(q) if hq else None, _addr(q_out) if hq else None, _addr(device_status))
+
+
+def paged_gather(cache: PagedCache, k_out, v_out=None, cu_rows=None, start=None, device_status=None,
+                 stream=None) -> None:
+    """Reads rows back: sequence s's slots from ``start`` (int32 ``[B]``; default
+    0) on, into ``k_out`` / ``v_out`` ``[rows, H_kv, 128]`` (contiguous; either
+    may be None), packed by sequence as ``cu_rows`` says (host ``[B+1]``; None:
+    the same number for each)."""
+    like = k_out if k_out is not None else v_out
+    if like is None:
+        _invalid("k_out or v_out is needed")
+    rows = like.shape[0]
+    for t in (k_out, v_out):
+        if t is not None and (t.dtype != cache.dtype or t.shape != (rows, cache.num_kv_heads, 128)
+                              or not t.is_contiguous()):
+            _invalid("k_out and v_out must be contiguous [rows, H_kv, 128] in the cache's dtype")
+    _rows_i32(start, cache.batch, "start")
+    _rows_i32(device_status, 1, "device_status")
+    _q4_on_device(cache, "outputs, start and status", k_out, v_out, start, device_status)
+    each, cu, at = _paged_rows(cache, rows, cu_rows)
+    _q4_call("compresskv_paged_gather", cache, stream, cache.addr, at, each, _addr(start), _addr(k_out),
+             _addr(v_out), _addr(device_status))
+
+
+def paged_workspace_size(cache: PagedCache, num_q_heads: int, num_queries: int) -> int:
+    n = _fast("compresskv_paged_workspace_size")(cache.addr, _q4_int(num_q_heads, "num_q_heads"),
+                                                 _q4_int(num_queries, "num_queries"))
+    if n == 0:
+        raise CompressKVError(CKV_ERR_INVALID_ARG, "compresskv_paged_workspace_size")
+    return int(n)
+
+
+def paged_workspace(cache: PagedCache, num_q_heads: int, num_queries: int, stream=None) -> torch.Tensor:
+    """A zero-status workspace for paged_attend with these heads and at most
+    ``num_queries`` query tokens of a sequence."""
+    if cache.device.type != "cuda":
+        _invalid("the cache must be in device memory")
+    n = paged_workspace_size(cache, num_q_heads, num_queries)
+    ws = torch.empty(n, dtype=torch.uint8, device=cache.device)
+    assert ws.data_ptr() % 256 == 0
+    with torch.cuda.device(cache.device):
+        _check(_fast("compresskv_paged_workspace_init")(ws.data_ptr(), n, _raw_stream(stream)),
+               "compresskv_paged_workspace_init")
+    return ws
+
+
+def paged_attend(cache: PagedCache, q, out, ws, cu_rows=None, start=None, scale: float = 0.0, lse=None,
+                 causal: bool = True, stream=None) -> None:
+    """Attention of ``q`` ``[rows, H_q, 128]``, packed by sequence (``cu_rows``:
+    host ``[B+1]``; None: the same number for each), over the cache into ``out``
+    (same shape and dtype).  Token i of a sequence stands at slot ``start`` + i
+    (int32 ``[B]``; default: the sequence's newest slots) and sees the slots up
+    to its own, or all in use where not ``causal``.  ``lse`` float32 ``[H_q,
+    rows]``."""
+    rows = q.shape[0]
+    hq, qt, qh = _head_rows(q, rows, "q", cache.dtype)
+    ho, ot, oh = _head_rows(out, rows, "out", cache.dtype)
+    if ho != hq:
+        _invalid("out must have q's shape")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (hq, rows)
+                            or not lse.is_contiguous()):
+        _invalid("lse must be a contiguous float32 [H_q, rows]")
+    _rows_i32(start, cache.batch, "start")
+    _q4_on_device(cache, "q, out, start, lse and workspace", q, out, start, lse, ws)
+    each, cu, at = _paged_rows(cache, rows, cu_rows)
+    a = CkvPagedQueries(hq, each, at, int(bool(causal)), float(scale), qt, qh, ot, oh)
+    _q4_call("compresskv_paged_attend", cache, stream, cache.addr, ctypes.addressof(a), _addr(q),
+             _addr(start), _addr(out), _addr(lse), _addr(ws), ws.numel())

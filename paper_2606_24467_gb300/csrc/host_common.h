@@ -5,8 +5,10 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <algorithm>
 #include <cstdint>
 
+#include "ckv_params.h"
 #include "compresskv.h"
 
 namespace ckv {
@@ -32,6 +34,37 @@ struct NvtxRange {
 };
 
 inline bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
+
+// Whether two rows of kHeadDim elements share one, in a layout of n[i] rows at
+// strides[i] (0 .. kMaxStride) in each of three dimensions.  They do not where
+// every stride holds what the smaller ones span; otherwise they do exactly
+// where the indices' differences, not all zero, come to less than a row.
+constexpr int64_t kMaxStride = 1LL << 44;  // (32 TB: products of strides and indices stay in 64 bits)
+inline bool rows_overlap(const int64_t (&strides)[3], const int (&n)[3]) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return strides[a] < strides[b]; });
+  int64_t span = ckv::kHeadDim;
+  bool nested = true;
+  for (int d : order) {
+    if (n[d] == 1) continue;
+    nested = nested && strides[d] >= span;
+    span += strides[d] * (n[d] - 1);  // (a dimension of one row has no stride)
+  }
+  if (nested) return false;
+  // the dimension of most rows is solved for
+  const int a = static_cast<int>(std::max_element(n, n + 3) - n), b = (a + 1) % 3, c = (a + 2) % 3;
+  const int64_t s = strides[a], most = n[a] - 1;
+  if (most > 0 && s < ckv::kHeadDim) return true;
+  for (int64_t j = 0; j < n[b]; ++j)
+    for (int64_t k = j ? 1 - n[c] : 1; k < n[c]; ++k) {
+      const int64_t rest = j * strides[b] + k * strides[c], near = most ? -rest / s : 0;
+      for (int64_t i = near - 1; i <= near + 1; ++i) {
+        const int64_t at = rest + std::min(std::max(i, -most), most) * s;
+        if (at < ckv::kHeadDim && at > -ckv::kHeadDim) return true;
+      }
+    }
+  return false;
+}
 
 // ------------------------------------------------------------------ tracing
 // Records the caller's trace events around each launch.  A failed record

@@ -1,0 +1,319 @@
+// Host side of the rotary and paged-cache entry points (include/compresskv.h):
+// argument checks, workspace and launches.  Nothing here allocates device
+// memory or waits for a stream.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "compresskv.h"
+#include "host_common.h"
+#include "paged_params.h"
+
+using namespace ckv;
+
+namespace {
+
+constexpr int kMaxPagedCapacity = 1 << 24;
+constexpr float kMaxScale = 0x1p96f;
+
+bool dtype_ok(int dtype) { return dtype == CKV_DTYPE_F16 || dtype == CKV_DTYPE_BF16; }
+
+bool strides_ok(int64_t token, int64_t head) {
+  return token >= 0 && head >= 0 && token % 8 == 0 && head % 8 == 0 && std::max(token, head) <= kMaxStride;
+}
+
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool share(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uint64_t x = reinterpret_cast<uint64_t>(a), y = reinterpret_cast<uint64_t>(b);
+  return na && nb && x < y + nb && y < x + na;
+}
+
+// Elements from the first row's start to the last row's end.
+uint64_t span_of(int rows, int heads, int64_t token, int64_t head) {
+  return static_cast<uint64_t>(rows - 1) * token + static_cast<uint64_t>(heads - 1) * head + kHeadDim;
+}
+
+// Rows [rows][heads][128] from `in` to `out`, at least one of each.
+int check_rows(int rows, int heads, const void* in, int64_t in_token, int64_t in_head, const void* out,
+               int64_t out_token, int64_t out_head) {
+  if (!in || !out || !aligned16(in) || !aligned16(out)) return CKV_ERR_INVALID_ARG;
+  if (!strides_ok(in_token, in_head) || !strides_ok(out_token, out_head)) return CKV_ERR_INVALID_ARG;
+  const int64_t strides[3] = {out_token, out_head, 0};
+  const int dims[3] = {rows, heads, 1};
+  if (rows_overlap(strides, dims)) return CKV_ERR_INVALID_ARG;
+  const bool in_place = in == out && (rows == 1 || in_token == out_token) && (heads == 1 || in_head == out_head);
+  if (!in_place && share(in, 2 * span_of(rows, heads, in_token, in_head), out,
+                         2 * span_of(rows, heads, out_token, out_head)))
+    return CKV_ERR_INVALID_ARG;
+  return CKV_OK;
+}
+
+RowSet row_set(const void* in, int64_t in_token, int64_t in_head, void* out, int64_t out_token, int64_t out_head) {
+  return {static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), in_token, in_head, out_token, out_head};
+}
+
+int check_rope(const ckv_rope* r) {
+  if (!r || r->rot_dim < 2 || r->rot_dim > kHeadDim || r->rot_dim % 2 || !std::isfinite(r->scale))
+    return CKV_ERR_INVALID_ARG;
+  return CKV_OK;
+}
+
+RopeTable rope_table(const ckv_rope* r) {
+  RopeTable t;
+  std::memcpy(t.turns, r->turns, sizeof(t.turns));
+  t.scale = r->scale;
+  t.pairs = r->rot_dim / 2;
+  t.interleaved = r->interleaved != 0;
+  return t;
+}
+
+int check_cache(const ckv_paged_cache* c, bool pointers = true) {
+  if (!c || c->batch < 1 || c->num_kv_heads < 1 || c->num_pages < 1 || c->table_width < 1 || !dtype_ok(c->dtype))
+    return CKV_ERR_INVALID_ARG;
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return CKV_ERR_INVALID_ARG;
+  if (c->batch > kMaxBatch || c->head_dim != kHeadDim || c->num_kv_heads > kMaxKvHeads ||
+      static_cast<int64_t>(c->table_width) * c->page_size > kMaxPagedCapacity)
+    return CKV_ERR_UNSUPPORTED;
+  if (!pointers) return CKV_OK;
+  if (!c->k_pages || !c->v_pages || !c->table || !c->lengths || !aligned16(c->k_pages) || !aligned16(c->v_pages))
+    return CKV_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(c->table) & 3u) || (reinterpret_cast<uintptr_t>(c->lengths) & 3u) ||
+      c->table_stride < c->table_width)
+    return CKV_ERR_INVALID_ARG;
+  if (!strides_ok(c->page_stride, c->slot_stride) || !strides_ok(0, c->head_stride)) return CKV_ERR_INVALID_ARG;
+  const int64_t strides[3] = {c->page_stride, c->slot_stride, c->head_stride};
+  const int dims[3] = {c->num_pages, c->page_size, c->num_kv_heads};
+  return rows_overlap(strides, dims) ? CKV_ERR_INVALID_ARG : CKV_OK;
+}
+
+PagedCache device_cache(const ckv_paged_cache* c) {
+  PagedCache d;
+  d.pages[0] = static_cast<uint16_t*>(c->k_pages);
+  d.pages[1] = static_cast<uint16_t*>(c->v_pages);
+  d.table = c->table;
+  d.lengths = c->lengths;
+  d.page_stride = c->page_stride;
+  d.slot_stride = c->slot_stride;
+  d.head_stride = c->head_stride;
+  d.table_stride = c->table_stride;
+  d.batch = c->batch;
+  d.num_kv_heads = c->num_kv_heads;
+  d.num_pages = c->num_pages;
+  d.table_width = c->table_width;
+  d.page_shift = 0;
+  while ((1 << d.page_shift) < c->page_size) ++d.page_shift;
+  d.capacity = c->table_width * c->page_size;
+  return d;
+}
+
+// The rows of each sequence, into a parameter block.
+int take_rows(const ckv_paged_cache* c, const int32_t* cu, int32_t rows_per_seq, int* to, int* per_seq, int* rows,
+              int* most) {
+  long long all = 0;
+  *most = 0;
+  if (cu) {
+    if (cu[0] != 0) return CKV_ERR_INVALID_ARG;
+    for (int s = 0; s < c->batch; ++s) {
+      if (cu[s + 1] < cu[s]) return CKV_ERR_INVALID_ARG;
+      *most = std::max(*most, cu[s + 1] - cu[s]);
+    }
+    std::copy(cu, cu + c->batch + 1, to);
+    all = cu[c->batch];
+    *per_seq = -1;
+  } else {
+    if (rows_per_seq < 0) return CKV_ERR_INVALID_ARG;
+    *per_seq = *most = rows_per_seq;
+    all = static_cast<long long>(rows_per_seq) * c->batch;
+  }
+  if (all > (1LL << 31) - 1) return CKV_ERR_UNSUPPORTED;
+  *rows = static_cast<int>(all);
+  return CKV_OK;
+}
+
+int check_index(const int32_t* ptr) { return reinterpret_cast<uintptr_t>(ptr) & 3u ? CKV_ERR_INVALID_ARG : CKV_OK; }
+
+int check_workspace(const void* ws, size_t have, size_t need) {
+  if (!ws || have < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) return CKV_ERR_WORKSPACE;
+  return CKV_OK;
+}
+
+int check_heads(const ckv_paged_cache* c, int num_q_heads) {
+  if (num_q_heads < 1 || num_q_heads % c->num_kv_heads) return CKV_ERR_INVALID_ARG;
+  if (num_q_heads > kMaxQHeads || num_q_heads / c->num_kv_heads > kPagedTile) return CKV_ERR_UNSUPPORTED;
+  return CKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32_t* positions, const void* q,
+                          const void* k, void* q_out, void* k_out, void* stream) {
+  NvtxRange nvtx_range(__func__);
+  int rc = check_rope(r);
+  if (rc != CKV_OK) return rc;
+  if (!x || x->rows < 0 || x->num_q_heads < 0 || x->num_k_heads < 0 || !dtype_ok(x->dtype))
+    return CKV_ERR_INVALID_ARG;
+  if (x->num_q_heads > kMaxQHeads || x->num_k_heads > kMaxQHeads) return CKV_ERR_UNSUPPORTED;
+  if (x->num_q_heads == 0 ? (q || q_out) : x->num_k_heads == 0 && (k || k_out)) return CKV_ERR_INVALID_ARG;
+  if (x->num_k_heads == 0 && (k || k_out)) return CKV_ERR_INVALID_ARG;
+  if (x->rows == 0 || x->num_q_heads + x->num_k_heads == 0) return CKV_OK;
+  if (!positions || (rc = check_index(positions)) != CKV_OK) return CKV_ERR_INVALID_ARG;
+  if (x->num_q_heads && (rc = check_rows(x->rows, x->num_q_heads, q, x->q_token_stride, x->q_head_stride, q_out,
+                                         x->q_out_token_stride, x->q_out_head_stride)) != CKV_OK)
+    return rc;
+  if (x->num_k_heads && (rc = check_rows(x->rows, x->num_k_heads, k, x->k_token_stride, x->k_head_stride, k_out,
+                                         x->k_out_token_stride, x->k_out_head_stride)) != CKV_OK)
+    return rc;
+  static thread_local RopeParams P;
+  std::memset(&P, 0, sizeof(P));
+  P.rope = rope_table(r);
+  P.q = row_set(q, x->q_token_stride, x->q_head_stride, q_out, x->q_out_token_stride, x->q_out_head_stride);
+  P.k = row_set(k, x->k_token_stride, x->k_head_stride, k_out, x->k_out_token_stride, x->k_out_head_stride);
+  P.positions = positions;
+  P.rows = x->rows;
+  P.num_q = x->num_q_heads;
+  P.num_k = x->num_k_heads;
+  P.is_bf16 = x->dtype == CKV_DTYPE_BF16;
+  P.backward = x->backward != 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Tracer tr{x->trace, st};
+  return traced(tr, CKV_KERNEL_ROPE, [&] { return launch_rope(P, st); });
+}
+
+int compresskv_paged_append(const ckv_paged_cache* c, const ckv_paged_rows* r, const void* k, const void* v,
+                            const int32_t* start, const ckv_rope* rope, const int32_t* positions, const void* q,
+                            void* q_out, int32_t* device_status, void* stream) {
+  NvtxRange nvtx_range(__func__);
+  int rc = check_cache(c);
+  if (rc != CKV_OK) return rc;
+  if (!r || r->num_q_heads < 0) return CKV_ERR_INVALID_ARG;
+  if (r->num_q_heads > kMaxQHeads) return CKV_ERR_UNSUPPORTED;
+  if (rope ? (rc = check_rope(rope)) != CKV_OK : r->num_q_heads > 0) return CKV_ERR_INVALID_ARG;
+  if (r->num_q_heads == 0 && (q || q_out)) return CKV_ERR_INVALID_ARG;
+  if (check_index(start) != CKV_OK || check_index(positions) != CKV_OK || check_index(device_status) != CKV_OK)
+    return CKV_ERR_INVALID_ARG;
+  if (start == c->lengths) start = nullptr;
+  const uint64_t word = sizeof(int32_t) * static_cast<uint64_t>(c->batch);
+  if (start && share(start, word, c->lengths, word)) return CKV_ERR_INVALID_ARG;
+  static thread_local RopeParams P;
+  std::memset(&P, 0, sizeof(P));
+  int most = 0;
+  if ((rc = take_rows(c, r->cu_rows, r->rows_per_seq, P.cu_rows, &P.rows_per_seq, &P.rows, &most)) != CKV_OK)
+    return rc;
+  if (P.rows == 0 && !start) return CKV_OK;  // no row, and every length stays
+  if (P.rows > 0) {
+    if (!k || !v || !aligned16(k) || !aligned16(v) || !strides_ok(r->kv_token_stride, r->kv_head_stride))
+      return CKV_ERR_INVALID_ARG;
+    if (r->num_q_heads && (rc = check_rows(P.rows, r->num_q_heads, q, r->q_token_stride, r->q_head_stride, q_out,
+                                           r->q_out_token_stride, r->q_out_head_stride)) != CKV_OK)
+      return rc;
+  }
+  P.c = device_cache(c);
+  if (rope)
+    P.rope = rope_table(rope);
+  P.q = row_set(q, r->q_token_stride, r->q_head_stride, q_out, r->q_out_token_stride, r->q_out_head_stride);
+  P.k = row_set(k, r->kv_token_stride, r->kv_head_stride, nullptr, 0, 0);
+  P.v = row_set(v, r->kv_token_stride, r->kv_head_stride, nullptr, 0, 0);
+  P.positions = positions;
+  P.start = start;
+  P.status = device_status;
+  P.num_q = r->num_q_heads;
+  P.num_k = c->num_kv_heads;
+  P.is_bf16 = c->dtype == CKV_DTYPE_BF16;
+  P.paged = 1;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Tracer tr{c->trace, st};
+  return traced(tr, CKV_KERNEL_PAGED_WRITE, [&] { return launch_paged_append(P, most, st); });
+}
+
+int compresskv_paged_gather(const ckv_paged_cache* c, const int32_t* cu_rows, int32_t rows_per_seq,
+                            const int32_t* start, void* k_out, void* v_out, int32_t* device_status, void* stream) {
+  NvtxRange nvtx_range(__func__);
+  int rc = check_cache(c);
+  if (rc != CKV_OK) return rc;
+  if (check_index(start) != CKV_OK || check_index(device_status) != CKV_OK || !aligned16(k_out) || !aligned16(v_out))
+    return CKV_ERR_INVALID_ARG;
+  static thread_local PagedGatherParams P;
+  std::memset(&P, 0, sizeof(P));
+  int most = 0;
+  if ((rc = take_rows(c, cu_rows, rows_per_seq, P.cu_rows, &P.rows_per_seq, &P.rows, &most)) != CKV_OK) return rc;
+  if (P.rows == 0 || (!k_out && !v_out)) return CKV_OK;
+  P.c = device_cache(c);
+  P.out[0] = static_cast<uint16_t*>(k_out);
+  P.out[1] = static_cast<uint16_t*>(v_out);
+  P.start = start;
+  P.status = device_status;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Tracer tr{c->trace, st};
+  return traced(tr, CKV_KERNEL_PAGED_GATHER, [&] { return launch_paged_gather(P, st); });
+}
+
+size_t compresskv_paged_workspace_size(const ckv_paged_cache* c, int32_t num_q_heads, int32_t num_queries) {
+  if (check_cache(c, false) != CKV_OK || num_queries < 0 || check_heads(c, num_q_heads) != CKV_OK) return 0;
+  return kPagedHeaderBytes;
+}
+
+int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange nvtx_range(__func__);
+  const int rc = check_workspace(workspace, workspace_bytes, kPagedHeaderBytes);
+  if (rc != CKV_OK) return rc;
+  return cudaMemsetAsync(workspace, 0, kPagedHeaderBytes, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? CKV_OK
+             : CKV_ERR_CUDA;
+}
+
+int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a, const void* q,
+                            const int32_t* start, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  NvtxRange nvtx_range(__func__);
+  int rc = check_cache(c);
+  if (rc != CKV_OK) return rc;
+  if (!a) return CKV_ERR_INVALID_ARG;
+  if ((rc = check_heads(c, a->num_q_heads)) != CKV_OK) return rc;
+  if (!(a->scale >= 0.f && a->scale <= kMaxScale)) return CKV_ERR_INVALID_ARG;  // (NaN too)
+  if (check_index(start) != CKV_OK || (reinterpret_cast<uintptr_t>(lse) & 3u)) return CKV_ERR_INVALID_ARG;
+  static thread_local PagedAttendParams P;
+  std::memset(&P, 0, sizeof(P));
+  int most = 0;
+  if ((rc = take_rows(c, a->cu_rows, a->rows_per_seq, P.cu_rows, &P.rows_per_seq, &P.rows, &most)) != CKV_OK)
+    return rc;
+  if (P.rows > 0) {
+    if ((rc = check_rows(P.rows, a->num_q_heads, q, a->q_token_stride, a->q_head_stride, out, a->out_token_stride,
+                         a->out_head_stride)) != CKV_OK)
+      return rc;
+    if (a->q_token_stride == 0 || a->q_head_stride == 0) return CKV_ERR_INVALID_ARG;
+    if (share(q, 2 * span_of(P.rows, a->num_q_heads, a->q_token_stride, a->q_head_stride), out,
+              2 * span_of(P.rows, a->num_q_heads, a->out_token_stride, a->out_head_stride)))
+      return CKV_ERR_INVALID_ARG;  // (a row of q is read after another's output is written)
+    if (static_cast<int64_t>(P.rows) * a->num_q_heads > (1LL << 31) - 1) return CKV_ERR_UNSUPPORTED;
+  }
+  if ((rc = check_workspace(workspace, workspace_bytes,
+                            compresskv_paged_workspace_size(c, a->num_q_heads, most))) != CKV_OK)
+    return rc;
+  if (P.rows == 0) return CKV_OK;
+  P.c = device_cache(c);
+  P.q = static_cast<const uint16_t*>(q);
+  P.out = static_cast<uint16_t*>(out);
+  P.lse = lse;
+  P.start = start;
+  P.q_token = a->q_token_stride;
+  P.q_head = a->q_head_stride;
+  P.o_token = a->out_token_stride;
+  P.o_head = a->out_head_stride;
+  const double scale = a->scale > 0.f ? a->scale : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
+  P.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
+  P.num_q_heads = a->num_q_heads;
+  P.group = a->num_q_heads / c->num_kv_heads;
+  P.causal = a->causal != 0;
+  P.is_bf16 = c->dtype == CKV_DTYPE_BF16;
+  P.status = static_cast<int*>(workspace);
+  P.stopped = P.status + 1;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Tracer tr{c->trace, st};
+  return traced(tr, CKV_KERNEL_PAGED_ATTEND, [&] { return launch_paged_attend(P, st); });
+}
+
+}  // extern "C"
