@@ -681,7 +681,8 @@ int compresskv_paged_gather(const ckv_paged_cache* c, const int32_t* cu_rows, in
 
 /* Query tokens: q and out [rows][num_q_heads][128], packed by sequence. */
 typedef struct ckv_paged_queries {
-  int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads, at most 128 a KV head */
+  int32_t num_q_heads;      /* 1..256, a multiple of num_kv_heads, at most 128 a KV head; times
+                               the query tokens of all sequences at most 2^26 */
   int32_t rows_per_seq;     /* query tokens of every sequence, where cu_rows is NULL */
   const int32_t* cu_rows;   /* host [batch+1] */
   int32_t causal;           /* non-zero: a token sees the slots up to its own */
@@ -691,7 +692,8 @@ typedef struct ckv_paged_queries {
 } ckv_paged_queries;
 
 /* Bytes of workspace for compresskv_paged_attend with these heads and at most
- * num_queries query tokens of a sequence; 0 if invalid. */
+ * num_queries query tokens of a sequence (some 80 MB where these, times the
+ * query heads of a KV head, are more than 128); 0 if invalid. */
 size_t compresskv_paged_workspace_size(const ckv_paged_cache* c, int32_t num_q_heads, int32_t num_queries);
 
 /* Zero the workspace's header (on `stream`): once after allocating it and after
@@ -742,6 +744,11 @@ int compresskv_debug_stall_next_fused_call(long long wait_ns);
  * CKV_ERR_DEVICE_TIMEOUT, and compresskv_q4_workspace_init makes the workspace
  * usable again. */
 int compresskv_debug_stall_next_q4_attend(long long wait_ns);
+
+/* The same for compresskv_paged_attend: its first CTA waits, copies and products
+ * under way, for what nothing completes, and stops;
+ * compresskv_paged_workspace_init makes the workspace usable again. */
+int compresskv_debug_stall_next_paged_attend(long long wait_ns);
 
 /* Error-aware layer budgets (Sec. 3.4: the offline per-layer eviction
  * errors, normalised as in Eq. 4, share the total budget after every layer

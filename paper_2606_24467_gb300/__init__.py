@@ -22,6 +22,7 @@ from .compresskv import (  # noqa: F401
     compress_layers,
     compress_layers_lse,
     debug_stall_next_fused_call,
+    debug_stall_next_paged_attend,
     debug_stall_next_q4_attend,
     gather,
     head_budget_layout,

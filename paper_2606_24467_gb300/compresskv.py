@@ -55,6 +55,7 @@ EXPORTED = (
     "compresskv_read_device_status",
     "compresskv_debug_stall_next_fused_call",
     "compresskv_debug_stall_next_q4_attend",
+    "compresskv_debug_stall_next_paged_attend",
     "compresskv_allocate_layer_budgets",
     "compresskv_status_string",
     "compresskv_q4_workspace_size",
@@ -197,6 +198,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "compresskv_read_device_status": (c_int32, [vp, vp, i32p]),
         "compresskv_debug_stall_next_fused_call": (c_int32, [ctypes.c_longlong]),
         "compresskv_debug_stall_next_q4_attend": (c_int32, [ctypes.c_longlong]),
+        "compresskv_debug_stall_next_paged_attend": (c_int32, [ctypes.c_longlong]),
         "compresskv_allocate_layer_budgets": (c_int32, [POINTER(ctypes.c_double), c_int32,
                                                         c_int64, c_int32, c_int32, i32p]),
         "compresskv_status_string": (ctypes.c_char_p, [c_int32]),
@@ -584,6 +586,13 @@ def debug_stall_next_q4_attend(wait_ns: int) -> None:
     CTA after wait_ns (0 cancels)."""
     _check(load().compresskv_debug_stall_next_q4_attend(ctypes.c_longlong(int(wait_ns))),
            "compresskv_debug_stall_next_q4_attend")
+
+
+def debug_stall_next_paged_attend(wait_ns: int) -> None:
+    """Test hook: the first CTA of the next paged_attend stalls on purpose and
+    stops after wait_ns (0 cancels)."""
+    _check(load().compresskv_debug_stall_next_paged_attend(ctypes.c_longlong(int(wait_ns))),
+           "compresskv_debug_stall_next_paged_attend")
 
 
 def read_device_status(ws, stream=None) -> int:

@@ -16,6 +16,7 @@
 #include "ckv_params.h"
 #include "compresskv.h"
 #include "host_common.h"
+#include "paged_params.h"
 #include "q4_params.h"
 
 using namespace ckv;
@@ -113,6 +114,7 @@ int device_facts(DeviceFacts** out) {
     if (resident_set_smem_limit(static_cast<size_t>(optin)) != cudaSuccess) return CKV_ERR_CUDA;
     if (q4_attend_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
     if (q4_evict_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
+    if (paged_attend_set_smem_limit() != cudaSuccess) return CKV_ERR_CUDA;
     if (combine_set_smem_limit(static_cast<size_t>(optin), &f.combine_smem_max) != cudaSuccess)
       return CKV_ERR_CUDA;
     if (select_set_smem_limit(static_cast<size_t>(select_max_smem_floats()) * 4) != cudaSuccess)
@@ -260,6 +262,22 @@ int ckv::make_row64_map(const void* base, unsigned long long rows, unsigned box_
       g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box,
                estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? CKV_OK : CKV_ERR_INVALID_ARG;
+}
+
+int ckv::make_rows_map(const void* base, bool bf16, int rank, const unsigned long long* dims,
+                       const long long* strides, const unsigned* box, CUtensorMap* map) {
+  cuuint64_t d[5] = {static_cast<cuuint64_t>(kHeadDim)}, st[4];
+  cuuint32_t b[5] = {64u}, estr[5] = {1u, 1u, 1u, 1u, 1u};
+  for (int i = 1; i < rank; ++i) {
+    d[i] = dims[i - 1];
+    st[i - 1] = static_cast<cuuint64_t>(strides[i - 1]) * 2;
+    b[i] = box[i - 1];
+  }
+  const CUresult r = g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              static_cast<cuuint32_t>(rank), const_cast<void*>(base), d, st, b, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? CKV_OK : CKV_ERR_INVALID_ARG;
 }
 

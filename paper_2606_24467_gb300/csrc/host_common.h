@@ -20,6 +20,10 @@ int check_problem(const ckv_problem* p);
 int device_readable(const void* ptr, const void** dev);
 int usable_sms(cudaStream_t stream, int* sms);
 int make_row64_map(const void* base, unsigned long long rows, unsigned box_rows, CUtensorMap* map);
+// A map over f16 / bf16 rows of 128 channels in `rank` - 1 dimensions (strides in
+// elements), for boxes of 64 channels, 128-byte swizzle.
+int make_rows_map(const void* base, bool bf16, int rank, const unsigned long long* dims, const long long* strides,
+                  const unsigned* box, CUtensorMap* map);
 }  // namespace ckv
 
 namespace {

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -17,6 +18,27 @@ namespace {
 
 constexpr int kMaxPagedCapacity = 1 << 24;
 constexpr float kMaxScale = 0x1p96f;
+constexpr int64_t kMaxQueryRows = 1 << 26;  // query tokens times heads (items and pieces count in 32 bits)
+
+// Test hook: how long the next attention stalls on purpose (0: not).
+std::atomic<long long> g_stall_attend_ns{0};
+
+// The attention's area behind the workspace header: results of pieces.  Where a
+// tile holds all rows of a unit, each CTA has at most two units in part.
+struct AttendArea {
+  size_t ml = 0, o = 0, bytes = 0;
+  int rows = 0;
+};
+AttendArea attend_area(long long rows) {
+  AttendArea a;
+  const bool pair = rows > kPagedTile;
+  a.rows = pair ? 2 * kPagedTile : static_cast<int>(rows);
+  const size_t all = static_cast<size_t>(pair ? kPagedSlots : 2 * kPagedMaxCtas) * a.rows;
+  a.ml = kPagedHeaderBytes;
+  a.o = a.ml + (all * sizeof(float2) + 255) / 256 * 256;
+  a.bytes = a.o + all * kHeadDim * sizeof(float);
+  return a;
+}
 
 bool dtype_ok(int dtype) { return dtype == CKV_DTYPE_F16 || dtype == CKV_DTYPE_BF16; }
 
@@ -251,9 +273,19 @@ int compresskv_paged_gather(const ckv_paged_cache* c, const int32_t* cu_rows, in
   return traced(tr, CKV_KERNEL_PAGED_GATHER, [&] { return launch_paged_gather(P, st); });
 }
 
+int compresskv_debug_stall_next_paged_attend(long long wait_ns) {
+  if (wait_ns < 0 || (wait_ns > 0 && (wait_ns < 100000 || wait_ns > 2000000000ll)))
+    return CKV_ERR_INVALID_ARG;
+  g_stall_attend_ns.store(wait_ns);
+  return CKV_OK;
+}
+
 size_t compresskv_paged_workspace_size(const ckv_paged_cache* c, int32_t num_q_heads, int32_t num_queries) {
   if (check_cache(c, false) != CKV_OK || num_queries < 0 || check_heads(c, num_q_heads) != CKV_OK) return 0;
-  return kPagedHeaderBytes;
+  const long long rows = static_cast<long long>(num_queries) * (num_q_heads / c->num_kv_heads);
+  size_t n = attend_area(std::min<long long>(rows, kPagedTile)).bytes;
+  if (rows > kPagedTile) n = std::max(n, attend_area(rows).bytes);
+  return n;
 }
 
 int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
@@ -288,32 +320,66 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
     if (share(q, 2 * span_of(P.rows, a->num_q_heads, a->q_token_stride, a->q_head_stride), out,
               2 * span_of(P.rows, a->num_q_heads, a->out_token_stride, a->out_head_stride)))
       return CKV_ERR_INVALID_ARG;  // (a row of q is read after another's output is written)
-    if (static_cast<int64_t>(P.rows) * a->num_q_heads > (1LL << 31) - 1) return CKV_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(P.rows) * a->num_q_heads > kMaxQueryRows) return CKV_ERR_UNSUPPORTED;
   }
   if ((rc = check_workspace(workspace, workspace_bytes,
                             compresskv_paged_workspace_size(c, a->num_q_heads, most))) != CKV_OK)
     return rc;
   if (P.rows == 0) return CKV_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int sms = 0;
+  if ((rc = usable_sms(st, &sms)) != CKV_OK) return rc;
+  const bool bf16 = c->dtype == CKV_DTYPE_BF16;
+  P.group = a->num_q_heads / c->num_kv_heads;
+  const long long unit_rows = static_cast<long long>(most) * P.group;
+  P.pair = unit_rows > kPagedTile;
+  P.tile_tokens = kPagedTile / P.group;
+  P.item_tokens = P.pair ? 2 * P.tile_tokens : P.tile_tokens;
+  const int box_tokens = std::min(P.tile_tokens, most);
+  P.q_box_bytes = box_tokens * P.group * 64 * 2;
+  {
+    const unsigned long long dims[2] = {static_cast<unsigned long long>(a->num_q_heads),
+                                        static_cast<unsigned long long>(P.rows)};
+    const long long strides[2] = {a->q_head_stride, a->q_token_stride};
+    const unsigned box[2] = {static_cast<unsigned>(P.group), static_cast<unsigned>(box_tokens)};
+    if ((rc = make_rows_map(q, bf16, 3, dims, strides, box, &P.map_q)) != CKV_OK) return rc;
+  }
+  {
+    const unsigned long long dims[3] = {static_cast<unsigned long long>(c->num_kv_heads),
+                                        static_cast<unsigned long long>(c->page_size),
+                                        static_cast<unsigned long long>(c->num_pages)};
+    const long long strides[3] = {c->head_stride, c->slot_stride, c->page_stride};
+    const unsigned box[3] = {1u, static_cast<unsigned>(std::min(c->page_size, kPagedTile)), 1u};
+    if ((rc = make_rows_map(c->k_pages, bf16, 4, dims, strides, box, &P.map_k)) != CKV_OK) return rc;
+    if ((rc = make_rows_map(c->v_pages, bf16, 4, dims, strides, box, &P.map_v)) != CKV_OK) return rc;
+  }
   P.c = device_cache(c);
-  P.q = static_cast<const uint16_t*>(q);
   P.out = static_cast<uint16_t*>(out);
   P.lse = lse;
   P.start = start;
-  P.q_token = a->q_token_stride;
-  P.q_head = a->q_head_stride;
   P.o_token = a->out_token_stride;
   P.o_head = a->out_head_stride;
   const double scale = a->scale > 0.f ? a->scale : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
   P.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
-  P.num_q_heads = a->num_q_heads;
-  P.group = a->num_q_heads / c->num_kv_heads;
   P.causal = a->causal != 0;
-  P.is_bf16 = c->dtype == CKV_DTYPE_BF16;
+  P.is_bf16 = bf16;
   P.status = static_cast<int*>(workspace);
   P.stopped = P.status + 1;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  P.next = P.status + 2;
+  P.done = P.status + 3;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  P.tickets = reinterpret_cast<int*>(ws + kPagedTickets);
+  const AttendArea area = attend_area(unit_rows);
+  P.part_ml = reinterpret_cast<float2*>(ws + area.ml);
+  P.part_o = reinterpret_cast<float*>(ws + area.o);
+  P.part_rows = area.rows;
+  P.stall_ns = static_cast<unsigned long long>(g_stall_attend_ns.exchange(0));
+  // no more CTAs than there can be tiles
+  const long long items = std::max<long long>((P.rows + P.item_tokens - 1) / P.item_tokens, 1) + c->batch;
+  const long long tiles = items * c->num_kv_heads * ((c->table_width * static_cast<long long>(c->page_size) + kPagedTile - 1) / kPagedTile);
+  const int ctas = static_cast<int>(std::min<long long>({sms, kPagedMaxCtas, tiles}));
   Tracer tr{c->trace, st};
-  return traced(tr, CKV_KERNEL_PAGED_ATTEND, [&] { return launch_paged_attend(P, st); });
+  return traced(tr, CKV_KERNEL_PAGED_ATTEND, [&] { return launch_paged_attend(P, ctas, st); });
 }
 
 }  // extern "C"

@@ -1,9 +1,32 @@
 // Attention of chunks of query tokens over a paged cache.
 //
-// One pass over the slots with each row's running maximum m and sum l: a tile's
-// logits z raise m to m', and l and the output are scaled by 2^(m - m') before
-// 2^(z - m') is added.  A row is one head of one query token; 16 rows of a KV
-// group share the tiles of 32 slots.
+// A row is one head of one query token.  For the rows of a KV group, over the
+// slots j that a row sees,
+//   z_j = q . K_j,  p_j = 2^(c z_j - c m),  l = sum p_j,  out = sum p_j V_j / l,
+// in one pass: m is the largest logit so far, and when it has grown by more than
+// 2^8 in p, l and the output so far are scaled by 2^(c (m_old - m)).  (Until then
+// m stays: p is at most 2^8, which fp32 sums and the 16-bit types hold as well as
+// 1.)  Logits and output are products on the tensor cores (tcgen05), 128 rows by
+// 128 slots at a time, with fp32 accumulators in tensor memory; p enters the
+// second product rounded to the 16-bit type, from tensor memory, while l sums it
+// unrounded.
+//
+// One CTA per SM, in roles: four warps a 128-row tile for the softmax, one lane of
+// them a row; a warp that finds the work and moves Q, K and V by TMA; one that
+// issues the products; and two that make V fit for tiles of which some rows see
+// only a part.  Two forms:
+//  * kPair, for chunks: two 128-row tiles of the same KV group and sequence share
+//    each tile of K and V, and while the tensor cores work for one, the other's
+//    softmax runs.  An item is two tiles of rows; where there are few items for
+//    the SMs, the slots are cut into blocks, and CTAs take (item, block) pieces by
+//    ticket, block by block, so that CTAs that run together read the same K and V.
+//  * single, where 128 rows hold all query tokens of a sequence (decode): the
+//    bytes of K and V bound it.  The tiles of all units form one sequence, of which
+//    each CTA takes an equal run; logits of the next tile are made while the
+//    softmax of this one runs.
+// What the pieces of an item leave in the workspace (output, reference and sum in
+// fp32) is joined by whichever CTA finishes the last of them, in the order of the
+// slots.
 #include "ckv_device.cuh"
 #include "paged_params.h"
 #include "q4_params.h"
@@ -11,119 +34,1102 @@
 namespace ckv {
 namespace {
 
-constexpr int kRows = 16, kSlots = 32, kThreads = 128;
+constexpr int kTile = kPagedTile;
+constexpr int kThreads = 384;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kFixWarp = 10;  // (0-3, 4-7: softmax)
+constexpr int kHalf = kTile * 128;                          // 64 channels of a tile, bytes
+constexpr int kTileBytes2 = 2 * kHalf;                      // K, V or Q: 32 KB
+constexpr int kRing = 4;                                    // piece descriptors
+constexpr int kDiagTiles = 3;                               // tiles that an item's rows see in part, at most
+constexpr float kGrowth = 8.f;                              // log2 of how far p may pass 1
 
+// A part of an item's slots, as the roles get it.
+struct Piece {
+  int go;                 // 0: no more pieces
+  int seq, head;
+  int row0;               // packed row of the item's first token
+  int tokens;             // of the item
+  int pos0;               // slot of its first token
+  int length;             // slots in use
+  int tile0;              // first tile
+  int tiles[2];           // of each 128-row tile (its rows see none behind); 0: not there
+  int pieces[2];          // of the item, for each 128-row tile; 1: the piece is all of it
+  int slot, ticket;       // where the piece's results go, and who counts them
+  // to find the slots of the item's pieces: single: the CTA that has its first
+  // tile; kPair: the sequence's first slot, t, tiles of a block
+  int base, item, size, rows, start;
+};
+
+template <bool kPair>
+struct Shape {
+  static constexpr int kQTiles = kPair ? 2 : 1;
+  static constexpr int kStages = kPair ? 5 : 6;
+  static constexpr int kConsumers = kPair ? 11 : 7;  // warps that read a piece
+};
+
+struct Misc {
+  uint64_t full[6], empty[6], vready[6];
+  uint64_t qfull[2], qempty[2], sfull[2], pready[2], odone[2], oempty[2];
+  uint64_t pfull[kRing], pempty[kRing], drain;
+  Piece ring[kRing];
+  uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite
+  uint32_t tmem;
+  int abort;
+};
+constexpr int kOperandBytes = 7 * kTileBytes2;  // (2 + 5 or 1 + 6)
+constexpr int kSmemBytes = kOperandBytes + static_cast<int>(sizeof(Misc));
+static_assert(kSmemBytes <= 232448, "shared memory");
+
+// ------------------------------------------------------------------- numbers
 template <bool kBf16>
-__device__ __forceinline__ float value(uint16_t w) {
-  if (kBf16) return __uint_as_float(static_cast<uint32_t>(w) << 16);
-  float r;
-  asm("{\n\t.reg .f16 h;\n\tmov.b16 h, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(r) : "h"(w));
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  if (!kBf16) return pack_half2(lo, hi);
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
 template <bool kBf16>
-__device__ __forceinline__ uint16_t rounded(float x) {
-  uint32_t r;
-  if (kBf16)
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(0.f), "f"(x));
-  else
-    r = pack_half2(x, 0.f);
-  return static_cast<uint16_t>(r);
+__device__ __forceinline__ float value(uint32_t w) {  // of the low half
+  if (kBf16) return __uint_as_float(w << 16);
+  float r;
+  asm("{\n\t.reg .f16 h, g;\n\tmov.b32 {h, g}, %1;\n\tcvt.f32.f16 %0, h;\n\t}" : "=f"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 split_of(uint64_t p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
-template <bool kBf16>
-__global__ void __launch_bounds__(kThreads) paged_attend_kernel(const __grid_constant__ PagedAttendParams p) {
-  pdl_wait();
-  __shared__ float q[kRows][kHeadDim], kv[kSlots][kHeadDim + 1], z[kRows][kSlots + 1];
-  __shared__ float m[kRows], l[kRows], rescale[kRows];
-  const int seq = blockIdx.z, head = blockIdx.y, tid = threadIdx.x;
-  const int row0 = p.rows_per_seq >= 0 ? seq * p.rows_per_seq : p.cu_rows[seq];
-  const int n = p.rows_per_seq >= 0 ? p.rows_per_seq : p.cu_rows[seq + 1] - row0;
-  const int r0 = blockIdx.x * kRows;
-  if (r0 >= n * p.group) return;
-  const int length = max(min(p.c.lengths[seq], p.c.capacity), 0);
-  const long long start = p.start ? p.start[seq] : static_cast<long long>(length) - n;
-  auto token = [&](int r) { return (r0 + r) / p.group; };
-  auto q_head = [&](int r) { return head * p.group + (r0 + r) % p.group; };
-  for (int r = 0; r < kRows; ++r)
-    q[r][tid] = token(r) < n ? value<kBf16>(p.q[(row0 + token(r)) * p.q_token + q_head(r) * p.q_head + tid]) : 0.f;
-  if (tid < kRows) {
-    m[tid] = -INFINITY;
-    l[tid] = 0.f;
+// ------------------------------------------------------------- tensor memory
+__device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+// The product of an operand in tensor memory (rows in lanes, two numbers of K to
+// a column) and one in shared memory.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// V as the right operand: rows of slots, 64 channels (128 bytes, swizzled) to a
+// row; groups of 8 rows 1024 bytes apart, the other 64 channels kHalf further.
+__device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
+  d |= static_cast<uint64_t>(kHalf >> 4) << 16;  // between the two groups of 64 channels
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;   // between groups of 8 slots
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;           // 128-byte swizzle
+  return d;
+}
+
+// ------------------------------------------------------------------- the call
+struct Cta {
+  const PagedAttendParams& p;
+  Misc* m;
+  uint32_t smem;  // of the operands: Q tiles, then the stages
+  // Bounded wait on a phase; false: this CTA stops.
+  __device__ __forceinline__ bool wait(uint64_t& bar, uint32_t parity) const {
+    return wait_for(bar, parity, kWaitTimeoutNs);
   }
-  float o[kRows] = {};
-  long long end = length;
-  if (p.causal) end = min(end, start + min(token(kRows - 1), n - 1) + 1);
-  for (int s0 = 0; s0 < end; s0 += kSlots) {
-    long long at[2];
-    __syncthreads();
-    for (int j = 0; j < kSlots; ++j) {
-      const int slot = s0 + j;
-      int page = -1;
-      if (slot < length) {
-        page = p.c.table[seq * p.c.table_stride + (slot >> p.c.page_shift)];
-        if (page < 0 || page >= p.c.num_pages) {
-          page = -1;
-          if (tid == 0) atomicCAS(p.status, 0, CKV_DEV_ERR_INDEX);
+  __device__ bool wait_for(uint64_t& bar, uint32_t parity, uint64_t ns) const {
+    const bool ok = mbar_wait_bounded(smem_u32(&bar), parity, &m->abort, p.status, ns);
+    if (!ok) atomicExch(p.stopped, 1);
+    return ok;
+  }
+  __device__ __forceinline__ bool wait_warp(uint64_t& bar, uint32_t parity) const {
+    return __all_sync(0xffffffffu, wait(bar, parity));
+  }
+  __device__ __forceinline__ bool stopped() const { return *reinterpret_cast<volatile int*>(&m->abort) != 0; }
+};
+
+// A piece from the ring, for a whole warp; the last use of it is followed by done().
+struct Reader {
+  const Cta& c;
+  int at = 0;
+  __device__ __forceinline__ const Piece* next() {
+    if (!c.wait_warp(c.m->pfull[at % kRing], (at / kRing) & 1)) return nullptr;
+    const Piece* x = &c.m->ring[at % kRing];
+    return x->go ? x : nullptr;
+  }
+  __device__ __forceinline__ void done() {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c.m->pempty[at % kRing]));
+    ++at;
+  }
+};
+
+__device__ __forceinline__ int clamp_to(long long x, int lo, int hi) {
+  return static_cast<int>(x < lo ? lo : x > hi ? hi : x);
+}
+// Slots that the token at slot `pos` sees.
+__device__ __forceinline__ int limit_of(const PagedAttendParams& p, int pos, int length) {
+  return p.causal ? min(max(pos + 1, 0), length) : length;
+}
+__device__ __forceinline__ int tiles_of(int limit) { return max((limit + kTile - 1) / kTile, 1); }
+
+// A sequence, as a lane of the work-finding warp sees it.
+struct Sequence {
+  int rows, row0, length, start;
+  __device__ void load(const PagedAttendParams& p, int s) {
+    rows = row0 = length = start = 0;
+    if (s >= p.c.batch) return;
+    row0 = p.rows_per_seq >= 0 ? s * p.rows_per_seq : p.cu_rows[s];
+    rows = p.rows_per_seq >= 0 ? p.rows_per_seq : p.cu_rows[s + 1] - row0;
+    length = max(min(p.c.lengths[s], p.c.capacity), 0);
+    // (far beyond any slot or token all positions are alike)
+    start = p.start ? clamp_to(p.start[s], -(1 << 28), 1 << 28) : length - rows;
+  }
+  // Tiles that tokens first .. last - 1 see together.
+  __device__ int tiles(const PagedAttendParams& p, int last) const {
+    return tiles_of(limit_of(p, start + last - 1, length));
+  }
+};
+
+__device__ __forceinline__ int warp_prefix(int x, int lane) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// kPair: the blocks of a sequence.  Item t covers tokens t per .. ; block b the
+// tiles b size .. of those items that see that far: items first(b) .. items - 1.
+struct Blocks {
+  int items, per, size;
+  // first(b), or `items` where no item sees block b
+  __device__ int first(const PagedAttendParams& p, const Sequence& s, int b) const {
+    if (b == 0) return 0;
+    const int slots = b * size * kTile;  // an item takes part if it sees more than these
+    if (s.length <= slots) return items;
+    if (!p.causal) return 0;
+    if (s.start + s.rows <= slots) return items;
+    const int tokens = slots - s.start + 1;  // that it must reach
+    return min(max((tokens + per - 1) / per - 1, 0), items - 1);
+  }
+  __device__ int pieces(const PagedAttendParams& p, const Sequence& s) const {  // of a head
+    int n = 0;
+    for (int b = 0, f; (f = first(p, s, b)) < items; ++b) n += items - f;
+    return n;
+  }
+  // of items with more than one block
+  __device__ int shared_pieces(const PagedAttendParams& p, const Sequence& s) const {
+    int n = items - first(p, s, 1);
+    for (int b = 1, f; (f = first(p, s, b)) < items; ++b) n += items - f;
+    return n;
+  }
+};
+
+__device__ __forceinline__ Blocks blocks_of(const PagedAttendParams& p, const Sequence& s, int size) {
+  return {(s.rows + p.item_tokens - 1) / p.item_tokens, p.item_tokens, size};
+}
+
+// Finds the pieces of this CTA, a warp together.
+template <bool kPair>
+struct Finder {
+  const PagedAttendParams& p;
+  int lane;
+  // the 32 sequences that the lanes hold, and what came before them
+  int group = -1;
+  Sequence s;
+  int mine = 0, upto = 0;      // single: tiles of a head; kPair: pieces of a head; and prefix, inclusive
+  int shared = 0, shared_upto = 0;
+  int before = 0, shared_before = 0;
+  // kPair
+  int size = 0;                // tiles of a block
+  int ticket = 0;
+  // single
+  long long all = 0, at = 0, end = 0;
+  int ctas = 0;
+  uint64_t policy = l2_policy_evict_last();
+
+  __device__ void hold(int g) {
+    group = g;
+    s.load(p, g * 32 + lane);
+    mine = shared = 0;
+    if (s.rows > 0) {
+      if (kPair) {
+        const Blocks b = blocks_of(p, s, size);
+        mine = b.pieces(p, s);
+        shared = b.shared_pieces(p, s);
+      } else {
+        mine = s.tiles(p, s.rows);
+      }
+    }
+    upto = warp_prefix(mine, lane);
+    if (kPair) shared_upto = warp_prefix(shared, lane);
+  }
+  __device__ bool advance() {  // to the next 32
+    if ((group + 1) * 32 >= p.c.batch) return false;
+    before += __shfl_sync(0xffffffffu, upto, 31);
+    if (kPair) shared_before += __shfl_sync(0xffffffffu, shared_upto, 31);
+    hold(group + 1);
+    return true;
+  }
+  __device__ int groups() const { return (p.c.batch + 31) / 32; }
+
+  __device__ void start() {
+    if (kPair) {
+      // work, roughly, and the longest item
+      long long work = 0;
+      int longest = 0;
+      for (int g = 0; g < groups(); ++g) {
+        Sequence x;
+        x.load(p, g * 32 + lane);
+        if (x.rows <= 0) continue;
+        const int items = (x.rows + p.item_tokens - 1) / p.item_tokens;
+        const int far = x.tiles(p, x.rows);
+        work += static_cast<long long>(items) * (x.tiles(p, min(p.item_tokens, x.rows)) + far);
+        longest = max(longest, far);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) {
+        work += __shfl_xor_sync(0xffffffffu, work, o);
+        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+      }
+      const long long share = max(work * p.c.num_kv_heads / (2 * static_cast<long long>(gridDim.x)), 1LL);
+      // Blocks of a share's kPagedCuts-th part where an item is more than that
+      // twice over, and no fewer than kPagedBlock tiles; as many as the results
+      // of shared items have room for.
+      size = longest;
+      if (2LL * longest * kPagedCuts > 4 * share) size = clamp_to(share / kPagedCuts, kPagedBlock, longest > kPagedBlock ? longest : kPagedBlock);
+      const int cuts = (longest + size - 1) / size;
+      size = max((longest + cuts - 1) / cuts, 1);
+      for (; size < longest; size *= 2) {
+        long long n = 0;
+        for (int g = 0; g < groups(); ++g) {
+          Sequence x;
+          x.load(p, g * 32 + lane);
+          if (x.rows > 0) n += blocks_of(p, x, size).shared_pieces(p, x);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        if (n * p.c.num_kv_heads <= kPagedSlots) break;
+      }
+      if (lane == 0) ticket = atomicAdd(p.next, 1);
+      ticket = __shfl_sync(0xffffffffu, ticket, 0);
+      hold(0);
+    } else {
+      hold(0);
+      int n = __shfl_sync(0xffffffffu, upto, 31);
+      while (advance()) n += __shfl_sync(0xffffffffu, upto, 31);
+      all = static_cast<long long>(n) * p.c.num_kv_heads;
+      ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), all));
+      if (blockIdx.x < ctas) {
+        at = all * blockIdx.x / ctas;
+        end = all * (blockIdx.x + 1) / ctas;
+      }
+      if (group > 0) {
+        before = 0;
+        hold(0);
+      }
+    }
+  }
+
+  // Into *x by lane 0; false: there is none.
+  __device__ bool find(Piece* x) {
+    const int heads = p.c.num_kv_heads;
+    const long long want = kPair ? ticket : at;
+    if (!kPair && at >= end) return false;
+    while (want >= static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, 31)) * heads)
+      if (!advance()) return false;
+    const unsigned over = __ballot_sync(0xffffffffu, static_cast<long long>(before + upto) * heads > want);
+    const int src = __ffs(over) - 1;
+    Sequence q;
+    q.rows = __shfl_sync(0xffffffffu, s.rows, src);
+    q.row0 = __shfl_sync(0xffffffffu, s.row0, src);
+    q.length = __shfl_sync(0xffffffffu, s.length, src);
+    q.start = __shfl_sync(0xffffffffu, s.start, src);
+    const int count = __shfl_sync(0xffffffffu, mine, src);
+    const long long first = static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, src) - count) * heads;
+    const int in_seq = static_cast<int>(want - first), head = in_seq / count;
+    int rest = in_seq - head * count;
+    Piece y;
+    y.go = 1;
+    y.seq = group * 32 + src;
+    y.head = head;
+    y.length = q.length;
+    y.rows = q.rows;
+    y.start = q.start;
+    if (kPair) {
+      const Blocks b = blocks_of(p, q, size);
+      int block = 0, f = 0, slots = 0;  // slots: of shared items' pieces before the block
+      const int f1 = b.first(p, q, 1);
+      for (;; ++block) {
+        f = b.first(p, q, block);
+        if (rest < b.items - f) break;
+        rest -= b.items - f;
+        slots += b.items - (block == 0 ? f1 : f);
+      }
+      const int t = b.items - 1 - rest;  // those that see most first
+      const int token = t * p.item_tokens;
+      y.item = t;
+      y.row0 = q.row0 + token;
+      y.tokens = min(p.item_tokens, q.rows - token);
+      y.pos0 = q.start + token;
+      const int tokens_a = min(p.item_tokens / 2, y.tokens);
+      const int most[2] = {q.tiles(p, token + tokens_a), q.tiles(p, token + y.tokens)};
+      y.tile0 = block * size;
+      const int to = min(most[1], y.tile0 + size);
+      y.tiles[0] = max(min(most[0], to) - y.tile0, 0);
+      y.tiles[1] = y.tokens > tokens_a ? to - y.tile0 : 0;
+      for (int i = 0; i < 2; ++i) y.pieces[i] = (most[i] + size - 1) / size;
+      y.size = size;
+      const int shared0 = shared_before + __shfl_sync(0xffffffffu, shared_upto - shared, src);
+      const int shared_n = __shfl_sync(0xffffffffu, shared, src);
+      y.base = shared0 * heads + head * shared_n;
+      y.slot = y.base + slots + t - (block == 0 ? f1 : f);
+      y.ticket = y.base + t - f1;
+    } else {
+      y.item = 0;
+      y.row0 = q.row0;
+      y.tokens = q.rows;
+      y.pos0 = q.start;
+      y.tile0 = rest;
+      const int n = static_cast<int>(min(static_cast<long long>(count - rest), end - at));
+      y.tiles[0] = n;
+      y.tiles[1] = 0;
+      const long long u0 = first + static_cast<long long>(head) * count;  // the unit's first tile
+      auto owner = [&](long long tile) { return static_cast<int>(((tile + 1) * ctas - 1) / all); };
+      y.base = owner(u0);
+      y.pieces[0] = y.pieces[1] = owner(u0 + count - 1) - y.base + 1;
+      y.size = 0;
+      y.ticket = y.base;
+      y.slot = 2 * static_cast<int>(blockIdx.x) + (rest == 0);
+      at += n;
+    }
+    if (lane == 0) *x = y;
+    if (kPair) {
+      if (lane == 0) ticket = atomicAdd(p.next, 1);
+      ticket = __shfl_sync(0xffffffffu, ticket, 0);
+    }
+    return true;
+  }
+};
+
+// The slots of an item's pieces, in order.
+template <bool kPair>
+struct Slots {
+  const PagedAttendParams& p;
+  const Piece& x;
+  int k = 0, at = 0, f1 = 0;
+  Sequence s;
+  __device__ Slots(const PagedAttendParams& p_, const Piece& x_) : p(p_), x(x_) {
+    s.rows = x.rows;
+    s.length = x.length;
+    s.start = x.start;
+    if (kPair) f1 = blocks_of(p, s, x.size).first(p, s, 1);
+  }
+  __device__ int next() {
+    int r;
+    if (kPair) {
+      const Blocks b = blocks_of(p, s, x.size);
+      const int f = k == 0 ? f1 : b.first(p, s, k);
+      r = x.base + at + x.item - f;
+      at += b.items - f;
+    } else {
+      r = k == 0 ? 2 * x.base + 1 : 2 * (x.base + k);
+    }
+    ++k;
+    return r;
+  }
+};
+
+// ---------------------------------------------------------------- TMA warp
+// Waits for a phase whether the CTA stops or not.
+__device__ void settle(uint64_t& bar, uint32_t parity, uint64_t ns) {
+  const uint64_t t0 = globaltimer_ns();
+  while (!mbar_try_wait(smem_u32(&bar), parity) && globaltimer_ns() - t0 < ns) {
+  }
+}
+
+template <bool kPair>
+__device__ void load_role(const Cta& c) {
+  using S = Shape<kPair>;
+  const PagedAttendParams& p = c.p;
+  const int lane = threadIdx.x & 31;
+  const int page = 1 << p.c.page_shift, box = min(page, kTile), copies = 2 * (kTile / box);
+  Finder<kPair> f{p, lane};
+  f.start();
+  int pos = 0, loaded = 0;  // stages filled (pos: the one waited for included)
+  int q_count[2] = {0, 0};
+  // this lane's page of a tile (not yet checked)
+  auto look_up = [&](const Piece& x, int tile) {
+    const int slot = tile * kTile + (lane >> 1) * box;
+    if (lane >= copies || slot >= x.length) return p.c.num_pages;
+    const int e = p.c.table[x.seq * p.c.table_stride + (slot >> p.c.page_shift)];
+    return e;
+  };
+  auto load_tile = [&](const Piece& x, const CUtensorMap& map, int tile, int entry) {
+    const int st = pos % S::kStages;
+    if (!c.wait_warp(c.m->empty[st], ((pos / S::kStages) & 1) ^ 1)) return false;
+    const uint32_t bar = smem_u32(&c.m->full[st]);
+    if (lane == 0) mbar_arrive_expect_tx(bar, kTileBytes2);
+    __syncwarp();
+    loaded = ++pos;
+    if (lane < copies) {
+      const int half = lane & 1, part = lane >> 1;
+      if (entry < 0 || entry > p.c.num_pages ||
+          (entry == p.c.num_pages && tile * kTile + part * box < x.length)) {
+        atomicCAS(p.status, 0, CKV_DEV_ERR_INDEX);
+        entry = p.c.num_pages;
+      }
+      // (a page behind the pool, as behind the length, is read as zeros)
+      tma_load_4d(c.smem + (S::kQTiles + st) * kTileBytes2 + half * kHalf + part * box * 128, &map, bar, half * 64,
+                  x.head, (tile * kTile) & (page - 1), entry, f.policy);
+    }
+    return true;
+  };
+  auto load_q = [&](const Piece& x, int t) {
+    if (!c.wait_warp(c.m->qempty[t], (q_count[t] & 1) ^ 1)) return false;
+    if (lane == 0) {
+      const uint32_t bar = smem_u32(&c.m->qfull[t]);
+      mbar_arrive_expect_tx(bar, p.q_box_bytes * 2);
+      for (int half = 0; half < 2; ++half)
+        tma_load_3d(c.smem + t * kTileBytes2 + half * kHalf, &p.map_q, bar, half * 64, x.head * p.group,
+                    x.row0 + t * p.tile_tokens, f.policy);
+    }
+    __syncwarp();
+    ++q_count[t];
+    return true;
+  };
+  bool ok = true;
+  for (int n = 0; ok; ++n) {
+    if (!c.wait_warp(c.m->pempty[n % kRing], ((n / kRing) & 1) ^ 1)) break;
+    Piece& x = c.m->ring[n % kRing];
+    const bool found = f.find(&x);
+    if (!found && lane == 0) x.go = 0;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&c.m->pfull[n % kRing]));
+    if (!found) break;
+    const int tiles = max(x.tiles[0], x.tiles[1]), first = x.tile0;
+    int now = look_up(x, first), next = tiles > 1 ? look_up(x, first + 1) : 0;
+    ok = load_tile(x, p.map_k, first, now);
+    for (int t = 0; ok && t < S::kQTiles; ++t)
+      if (x.tiles[t]) ok = load_q(x, t);
+    for (int j = 0; ok && j < tiles; ++j) {
+      const int after = j + 2 < tiles ? look_up(x, first + j + 2) : 0;
+      if (j + 1 < tiles) ok = load_tile(x, p.map_k, first + j + 1, next);
+      if (ok) ok = load_tile(x, p.map_v, first + j, now);
+      now = next;
+      next = after;
+    }
+  }
+  // No copy, and no arrival that a stage or Q tile is free again, may come after
+  // this CTA has ended.  (A stopped CTA has only its copies to wait for.)
+  const bool all = !c.stopped();
+  for (int i = max(loaded - S::kStages, 0); i < loaded; ++i) {
+    if (all)
+      c.wait_warp(c.m->empty[i % S::kStages], (i / S::kStages) & 1);
+    else
+      settle(c.m->full[i % S::kStages], (i / S::kStages) & 1, 100000000ull);
+  }
+  for (int t = 0; t < S::kQTiles; ++t)
+    if (q_count[t]) {
+      if (all)
+        c.wait_warp(c.m->qempty[t], (q_count[t] - 1) & 1);
+      else
+        settle(c.m->qfull[t], (q_count[t] - 1) & 1, 100000000ull);
+    }
+}
+
+// ---------------------------------------------------------------- products
+template <bool kBf16, bool kPair>
+__device__ void product_role(const Cta& c, uint32_t tmem) {
+  using S = Shape<kPair>;
+  const bool lead = (threadIdx.x & 31) == 0;
+  constexpr uint32_t kQk = umma_idesc_f16(kTile, kTile, kBf16);
+  constexpr uint32_t kPv = kQk | 1u << 16;  // V: channels, not slots, are contiguous
+  const uint32_t stages = c.smem + S::kQTiles * kTileBytes2;
+  auto bar = [&](uint64_t& b) { return smem_u32(&b); };
+  auto stage = [&](int pos) { return pos % S::kStages; };
+  auto logits = [&](int q, int buffer, int pos) {
+    const uint64_t a = smem_desc_sw128(c.smem + q * kTileBytes2);
+    const uint64_t b = smem_desc_sw128(stages + stage(pos) * kTileBytes2);
+#pragma unroll
+    for (int i = 0; i < kHeadDim / 16; ++i) {
+      const uint64_t step = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+      umma_f16(tmem + buffer * kTile, a + step, b + step, kQk, i > 0);
+    }
+  };
+  auto output = [&](int o, int buffer, int pos, bool more) {
+    const uint64_t b = v_desc(stages + stage(pos) * kTileBytes2);
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i)
+      umma_f16_ts(tmem + (2 + o) * kTile, tmem + buffer * kTile + i * 8, b + i * (2048 >> 4), kPv, more || i > 0);
+  };
+  Reader reader{c};
+  int pos = 0;
+  uint32_t v_phase = 0;   // by stage
+  int q_count[2] = {0, 0}, p_count[2] = {0, 0}, o_count[2] = {0, 0};
+  auto wait_k = [&](int at) { return c.wait_warp(c.m->full[stage(at)], (at / S::kStages) & 1); };
+  auto wait_v = [&](int at) {
+    const int st = stage(at);
+    const bool ok = wait_k(at) && c.wait_warp(c.m->vready[st], (v_phase >> st) & 1);
+    v_phase ^= 1u << st;
+    return ok;
+  };
+  while (const Piece* x = reader.next()) {
+    const int n[2] = {x->tiles[0], kPair ? x->tiles[1] : 0};
+    const int tiles = max(n[0], n[1]);
+    if (!wait_k(pos)) break;
+    bool ok = true;
+    for (int t = 0; ok && t < S::kQTiles; ++t)
+      if (n[t]) {
+        ok = c.wait_warp(c.m->qfull[t], q_count[t]++ & 1);
+        const int buffer = kPair ? t : p_count[0] & 1;
+        if (ok && lead) {
+          tc_fence_after();
+          logits(t, buffer, pos);
+          umma_commit(bar(c.m->sfull[buffer]));
+          if (n[t] == 1) umma_commit(bar(c.m->qempty[t]));
         }
       }
-      at[0] = page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + head * p.c.head_stride;
-      kv[j][tid] = page >= 0 ? value<kBf16>(p.c.pages[0][at[0] + tid]) : 0.f;
+    if (!ok) break;
+    if (lead) umma_commit(bar(c.m->empty[stage(pos)]));
+    ++pos;
+    if (c.p.stall_ns && blockIdx.x == 0) {  // test hook: a wait for what nothing completes
+      c.wait_for(c.m->drain, 0, c.p.stall_ns);
+      break;
     }
-    __syncthreads();
-    for (int i = tid; i < kRows * kSlots; i += kThreads) {
-      const int r = i / kSlots, j = i % kSlots;
-      float x = 0.f;
-      for (int c = 0; c < kHeadDim; ++c) x = fmaf(q[r][c], kv[j][c], x);
-      const bool seen = s0 + j < length && (!p.causal || s0 + j <= start + token(r));
-      z[r][j] = seen ? x * p.scale_log2 : -INFINITY;
-    }
-    __syncthreads();
-    if (tid < kRows) {
-      float top = m[tid];
-      for (int j = 0; j < kSlots; ++j) top = fmaxf(top, z[tid][j]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-      for (int j = 0; j < kSlots; ++j) {
-        z[tid][j] = exp2f(z[tid][j] - ref);
-        sum += z[tid][j];
+    for (int j = 0; ok && j < tiles; ++j) {
+      const bool more = j + 1 < tiles;
+      const int kpos = pos, vpos = pos + more;
+      pos = vpos + 1;
+      if (kPair) {
+        ok = wait_v(vpos) && (!more || wait_k(kpos));
+        for (int t = 0; ok && t < 2; ++t)
+          if (j < n[t]) {
+            ok = c.wait_warp(c.m->pready[t], p_count[t]++ & 1);
+            if (ok && j == 0) ok = c.wait_warp(c.m->oempty[t], (o_count[t]++ & 1) ^ 1);
+            if (ok && lead) {
+              tc_fence_after();
+              output(t, t, vpos, j > 0);
+              if (j + 1 < n[t]) {
+                logits(t, t, kpos);
+                umma_commit(bar(c.m->sfull[t]));
+                if (j + 2 == n[t]) umma_commit(bar(c.m->qempty[t]));
+              } else {
+                umma_commit(bar(c.m->odone[t]));
+              }
+            }
+          }
+        if (ok && lead) {
+          umma_commit(bar(c.m->empty[stage(vpos)]));
+          if (more) umma_commit(bar(c.m->empty[stage(kpos)]));
+        }
+      } else {
+        if (more) {
+          ok = wait_k(kpos);
+          const int buffer = (p_count[0] + 1) & 1;
+          if (ok && lead) {
+            tc_fence_after();
+            logits(0, buffer, kpos);
+            umma_commit(bar(c.m->sfull[buffer]));
+            umma_commit(bar(c.m->empty[stage(kpos)]));
+            if (j + 2 == tiles) umma_commit(bar(c.m->qempty[0]));
+          }
+        }
+        const int buffer = p_count[0] & 1, phase = (p_count[0] >> 1) & 1;
+        ++p_count[0];
+        ok = ok && wait_v(vpos) && c.wait_warp(c.m->pready[buffer], phase);
+        if (ok && j == 0) ok = c.wait_warp(c.m->oempty[0], (o_count[0]++ & 1) ^ 1);
+        if (ok && lead) {
+          tc_fence_after();
+          output(0, buffer, vpos, j > 0);
+          umma_commit(bar(c.m->odone[0]));
+          umma_commit(bar(c.m->empty[stage(vpos)]));
+        }
       }
-      rescale[tid] = exp2f(m[tid] - ref);
-      l[tid] = l[tid] * rescale[tid] + sum;
-      m[tid] = top;
+      __syncwarp();
     }
-    __syncthreads();
-    for (int r = 0; r < kRows; ++r) o[r] *= rescale[r];
-    for (int j = 0; j < kSlots; ++j) {
-      const int slot = s0 + j;
-      if (slot >= length) break;
-      const int page = p.c.table[seq * p.c.table_stride + (slot >> p.c.page_shift)];
-      if (page < 0 || page >= p.c.num_pages) continue;
-      at[1] = page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + head * p.c.head_stride;
-      const float v = value<kBf16>(p.c.pages[1][at[1] + tid]);
-      for (int r = 0; r < kRows; ++r)
-        if (!p.causal || slot <= start + token(r)) o[r] = fmaf(z[r][j], v, o[r]);
+    if (!ok) break;
+    reader.done();
+  }
+  // every product, and every arrival that waits for one, is over before the
+  // tensor memory is given back
+  if (lead) umma_commit(bar(c.m->drain));
+  settle(c.m->drain, 0, 1000000000ull);
+}
+
+// ---------------------------------------------------------------- V of tiles that rows see in part
+// A hidden slot has p = 0, but 0 times what is not finite is not 0.  In tiles that
+// the item's first token does not see whole, rows of slots behind the length
+// become zero, and what is not finite in slots that other tokens see: those slots
+// are noted, and the rows that do see them get it added to their output.
+template <bool kBf16, bool kPair>
+__device__ void fix_role(const Cta& c, int part) {
+  using S = Shape<kPair>;
+  const PagedAttendParams& p = c.p;
+  const int lane = threadIdx.x & 31;
+  constexpr uint32_t kTop = kBf16 ? 0x7f807f80u : 0x7c007c00u;  // exponents of all ones
+  Reader reader{c};
+  int pos = 0;
+  while (const Piece* x = reader.next()) {
+    uint32_t(*poison)[4] = c.m->poison[reader.at % kRing];
+    if (lane < 2 * kDiagTiles) poison[lane >> 1][2 * part + (lane & 1)] = 0;
+    __syncwarp();
+    const int tiles = max(x->tiles[0], x->tiles[1]), tile0 = x->tile0, length = x->length;
+    const int whole = limit_of(p, x->pos0, length);  // slots that all rows see
+    bool ok = true;
+    ++pos;  // (the first K)
+    for (int j = 0; j < tiles; ++j) {
+      if (j + 1 < tiles) ++pos;
+      const int st = pos % S::kStages;
+      if (!(ok = c.wait_warp(c.m->full[st], (pos / S::kStages) & 1))) break;
+      ++pos;
+      const int base = (tile0 + j) * kTile;
+      if (base + kTile > whole) {
+        char* v = reinterpret_cast<char*>(c.m) - kOperandBytes + (S::kQTiles + st) * kTileBytes2;
+        const int diag = tile0 + j - whole / kTile;
+        // two slots at a time, 16 pieces of 16 bytes each
+        for (int i = max(whole - base, 64 * part) & ~1; i < 64 * part + 64; i += 2) {
+          const int slot = i + (lane >> 4);
+          uint4* at = reinterpret_cast<uint4*>(v + ((lane >> 3) & 1) * kHalf + slot * 128) + (lane & 7);
+          if (base + slot >= length) {
+            *at = make_uint4(0, 0, 0, 0);
+          } else if (base + slot >= whole) {
+            uint4 w = *at;
+            uint32_t* word = &w.x;
+            bool found = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t e = word[k] & kTop;
+              if ((e & 0xffffu) == (kTop & 0xffffu)) word[k] &= 0xffff0000u, found = true;
+              if ((e & 0xffff0000u) == (kTop & 0xffff0000u)) word[k] &= 0xffffu, found = true;
+            }
+            if (found) {
+              *at = w;
+              if (diag < kDiagTiles) atomicOr(&poison[diag][slot >> 5], 1u << (slot & 31));
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->vready[st]));
+    }
+    if (!ok) return;
+    reader.done();
+  }
+}
+
+// ---------------------------------------------------------------- softmax
+// The results of an item's pieces for this warp's rows, joined: the weights of the
+// pieces are 2^(their reference - the largest), over the sum.
+template <bool kBf16, bool kPair>
+__device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int tile, int row0, unsigned valid) {
+  const int lane = threadIdx.x & 31, pieces = x.pieces[tile];
+  while (valid) {
+    int row[4];
+    bool have[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      have[i] = valid != 0;
+      row[i] = valid ? __ffs(valid) - 1 : row[0];
+      valid &= valid - 1;
+    }
+    float top[4], sum[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top[i] = -INFINITY;
+    {
+      Slots<kPair> slots(p, x);
+      for (int k0 = 0; k0 < pieces; k0 += 32) {
+        int mine = -1;
+        for (int k = 0; k < min(32, pieces - k0); ++k) {
+          const int s = slots.next();
+          if (k == lane) mine = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float2 ml = make_float2(-INFINITY, 0.f);
+          if (mine >= 0) ml = __ldcg(p.part_ml + static_cast<long long>(mine) * p.part_rows + row0 + row[i]);
+          float t = ml.y == 0.f ? -INFINITY : ml.x;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+          top[i] = fmaxf(top[i], t);
+        }
+      }
+    }
+    float4 acc[4] = {};
+    {
+      Slots<kPair> slots(p, x);
+      for (int k0 = 0; k0 < pieces; k0 += 32) {
+        const int count = min(32, pieces - k0);
+        int mine = -1;
+        for (int k = 0; k < count; ++k) {
+          const int s = slots.next();
+          if (k == lane) mine = s;
+        }
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float2 ml = make_float2(-INFINITY, 0.f);
+          if (mine >= 0) ml = __ldcg(p.part_ml + static_cast<long long>(mine) * p.part_rows + row0 + row[i]);
+          // (equal infinities: 1, so that they and NaN go on into the sum)
+          w[i] = ml.y == 0.f ? 0.f : ml.x == top[i] ? 1.f : exp2f(ml.x - top[i]);
+          float l = ml.y == 0.f ? 0.f : ml.y * w[i];
+#pragma unroll
+          for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+          sum[i] += l;
+        }
+        for (int k = 0; k < count; k += 4) {
+          float4 v[4][4];
+          float f[4][4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int from = min(k + u, 31);
+            const int s = __shfl_sync(0xffffffffu, mine, from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f[u][i] = __shfl_sync(0xffffffffu, w[i], from);
+              if (k + u >= count) f[u][i] = 0.f;
+              v[u][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (f[u][i] != 0.f)
+                v[u][i] = __ldcg(reinterpret_cast<const float4*>(
+                                     p.part_o + (static_cast<long long>(s) * p.part_rows + row0 + row[i]) * kHeadDim) +
+                                 lane);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[i].x = fmaf(f[u][i], v[u][i].x, acc[i].x);
+              acc[i].y = fmaf(f[u][i], v[u][i].y, acc[i].y);
+              acc[i].z = fmaf(f[u][i], v[u][i].z, acc[i].z);
+              acc[i].w = fmaf(f[u][i], v[u][i].w, acc[i].w);
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!have[i]) continue;
+      const int r = (row0 + row[i]) % kTile, token = tile * p.tile_tokens + r / p.group;
+      const int head = x.head * p.group + r % p.group;
+      const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+      const bool none = sum[i] == 0.f;
+      uint2 o;
+      o.x = none ? 0u : pack<kBf16>(acc[i].x * inv, acc[i].y * inv);
+      o.y = none ? 0u : pack<kBf16>(acc[i].z * inv, acc[i].w * inv);
+      const long long row_at = x.row0 + token;
+      reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] = o;
+      if (p.lse && lane == 0)
+        p.lse[static_cast<long long>(head) * p.rows + row_at] =
+            none ? -INFINITY : (top[i] + log2f(sum[i])) * 0.6931471805599453f;
     }
   }
-  __syncthreads();
-  for (int r = 0; r < kRows; ++r)
-    if (token(r) < n) {
-      const float x = l[r] == 0.f ? 0.f : o[r] / l[r];  // (a NaN row has a sum, NaN)
-      p.out[(row0 + token(r)) * p.o_token + q_head(r) * p.o_head + tid] = rounded<kBf16>(x);
-      if (p.lse && tid == 0)
-        p.lse[static_cast<long long>(q_head(r)) * p.rows + row0 + token(r)] =
-            l[r] == 0.f ? -INFINITY : (m[r] + log2f(l[r])) * 0.6931471805599453f;
+}
+
+template <bool kBf16, bool kPair>
+__device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
+  const PagedAttendParams& p = c.p;
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, r = warp * 32 + lane;
+  const int in_tile = r / p.group;
+  const uint32_t lanes = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+  const uint32_t o_addr = lanes + (2 + tile) * kTile;
+  const float scale = p.scale_log2;
+  Reader reader{c};
+  int count = 0, o_count = 0;  // tiles done; (waits for) products with V
+  while (const Piece* x = reader.next()) {
+    const int n = x->tiles[tile];
+    if (n == 0) {
+      reader.done();
+      continue;
     }
+    const int token = tile * p.tile_tokens + in_tile, tile0 = x->tile0, length = x->length, pos0 = x->pos0;
+    const bool valid = in_tile < p.tile_tokens && token < x->tokens;
+    const unsigned rows = __ballot_sync(0xffffffffu, valid);
+    const int limit = valid ? limit_of(p, pos0 + token, length) : 0x7fffffff;
+    const int least = __reduce_min_sync(0xffffffffu, limit);
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < n; ++j, ++count) {
+      const int buffer = kPair ? tile : count & 1;
+      if (!c.wait_warp(c.m->sfull[buffer], (kPair ? count : count >> 1) & 1)) return;
+      const uint32_t s_addr = lanes + buffer * kTile;
+      if (rows) {
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_load32_async(s_addr + 32 * k, s[k]);
+        tmem_wait_ld(s[0]);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) tmem_order_after_wait(s[k]);
+        const int base = (tile0 + j) * kTile;
+        if (base + kTile > least) {
+          const int see = limit - base;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * k + i >= see) s[k][i] = 0xff800000u;
+        }
+        float top[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          top[k] = __uint_as_float(s[k][0]);
+#pragma unroll
+          for (int i = 1; i < 32; ++i) top[k] = fmaxf(top[k], __uint_as_float(s[k][i]));
+        }
+        const float now = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), m);
+        if (!kPair && j > 0 && !c.wait_warp(c.m->odone[0], o_count++ & 1)) return;
+        const bool grown = now > m && (m == -INFINITY || (now - m) * scale > kGrowth);
+        if (__any_sync(0xffffffffu, grown)) {
+          const float f = grown ? ex2_approx((m - now) * scale) : 1.f;
+          if (grown) m = now;
+          l *= f;
+          if (j > 0) {
+            tc_fence_after();
+            const uint64_t f2 = pair_of(f, f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t o[32];
+              tmem_load32_async(o_addr + 32 * k, o);
+              tmem_wait_ld(o);
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                const float2 y = split_of(mul2(pair_of(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), f2));
+                o[i] = __float_as_uint(y.x);
+                o[i + 1] = __float_as_uint(y.y);
+              }
+              tmem_store32(o_addr + 32 * k, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m * scale;
+        const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
+        uint64_t sum[4] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 e = split_of(
+                fma2(pair_of(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), scale2, ref2));
+            const float a = ex2_approx(e.x), b = ex2_approx(e.y);
+            sum[i & 3] = add2(sum[i & 3], pair_of(a, b));
+            w[i] = pack<kBf16>(a, b);
+          }
+          tmem_store16(s_addr + 16 * k, w);
+        }
+        const float2 total = split_of(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+        l += total.x + total.y;
+        tmem_wait_st();
+        tc_fence_before();
+      } else if (!kPair && j > 0 && !c.wait_warp(c.m->odone[0], o_count++ & 1)) {
+        return;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer]));
+    }
+    // the piece's output
+    if (!c.wait_warp(c.m->odone[tile], o_count++ & 1)) return;
+    uint32_t o[4][32];
+    tc_fence_after();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tmem_load32_async(o_addr + 32 * k, o[k]);
+    tmem_wait_ld(o[0]);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) tmem_order_after_wait(o[k]);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&c.m->oempty[tile]));
+    const Piece y = *x;
+    const int whole = limit_of(p, pos0, length);
+    for (int d = 0; d < kDiagTiles; ++d)
+      for (int k = 0; k < 4; ++k) {
+        uint32_t bits = c.m->poison[reader.at % kRing][d][k];
+        for (; bits; bits &= bits - 1) {
+          const int slot = (whole / kTile + d) * kTile + 32 * k + __ffs(bits) - 1;
+          if (slot >= limit || !valid) continue;
+          const int page = p.c.table[y.seq * p.c.table_stride + (slot >> p.c.page_shift)];
+          if (page < 0 || page >= p.c.num_pages) continue;
+          const uint16_t* v = p.c.pages[1] + page * p.c.page_stride +
+                              (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + y.head * p.c.head_stride;
+#pragma unroll
+          for (int i = 0; i < 128; ++i) {
+            const float f = value<kBf16>(v[i]);
+            if (!(fabsf(f) < INFINITY)) o[i / 32][i % 32] = __float_as_uint(__uint_as_float(o[i / 32][i % 32]) + f);
+          }
+        }
+      }
+    reader.done();
+    const float ref = m == -INFINITY ? 0.f : m * scale;
+    const int row0 = tile * kTile + warp * 32;
+    if (y.pieces[tile] == 1) {
+      if (valid) {
+        const float inv = 1.f / l;
+        const bool none = l == 0.f;
+        const long long row_at = y.row0 + token;
+        const int head = y.head * p.group + r - in_tile * p.group;
+        uint16_t* to = p.out + row_at * p.o_token + head * p.o_head;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int at = 8 * i + 2 * k;
+            w[k] = none ? 0u
+                        : pack<kBf16>(__uint_as_float(o[at / 32][at % 32]) * inv,
+                                      __uint_as_float(o[at / 32][at % 32 + 1]) * inv);
+          }
+          reinterpret_cast<uint4*>(to)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (p.lse)
+          p.lse[static_cast<long long>(head) * p.rows + row_at] =
+              none ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+      }
+    } else if (rows) {
+      if (valid) {
+        const long long at = static_cast<long long>(y.slot) * p.part_rows + row0 + lane;
+        p.part_ml[at] = make_float2(ref, l);
+        float4* to = reinterpret_cast<float4*>(p.part_o + at * kHeadDim);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          to[i] = make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
+                              __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
+      }
+      __threadfence();
+      __syncwarp();
+      int* ticket = p.tickets + (y.ticket * 2 + tile) * 4 + warp;
+      int before = 0;
+      if (lane == 0) before = atomicAdd(ticket, 1);
+      before = __shfl_sync(0xffffffffu, before, 0);
+      if (before == y.pieces[tile] - 1) {
+        __threadfence();
+        if (lane == 0) *ticket = 0;
+        join<kBf16, kPair>(p, y, tile, row0, rows);
+      }
+    }
+  }
+}
+
+template <bool kBf16, bool kPair>
+__global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_constant__ PagedAttendParams p) {
+  using S = Shape<kPair>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Misc* m = reinterpret_cast<Misc*>(smem + kOperandBytes);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(smem_u32(&m->full[i]), 1);
+      mbar_init(smem_u32(&m->empty[i]), 1);
+      mbar_init(smem_u32(&m->vready[i]), 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&m->qfull[i]), 1);
+      mbar_init(smem_u32(&m->qempty[i]), 1);
+      mbar_init(smem_u32(&m->sfull[i]), 1);
+      mbar_init(smem_u32(&m->pready[i]), 4);
+      mbar_init(smem_u32(&m->odone[i]), 1);
+      mbar_init(smem_u32(&m->oempty[i]), 4);
+    }
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&m->pfull[i]), 1);
+      mbar_init(smem_u32(&m->pempty[i]), S::kConsumers);
+    }
+    mbar_init(smem_u32(&m->drain), 1);
+    m->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(&m->tmem), 512);
+    tmem_relinquish();
+  }
+  if (warp == kLoadWarp && lane == 0) {
+    tma_prefetch_map(&p.map_q);
+    tma_prefetch_map(&p.map_k);
+    tma_prefetch_map(&p.map_v);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = m->tmem;
+  const Cta c{p, m, smem_u32(smem)};
+  // a call that stopped may have left tickets behind: nothing runs until the
+  // workspace is set up again
+  if (*reinterpret_cast<volatile int*>(p.stopped) == 0) {
+    if (warp < 4)
+      softmax_role<kBf16, kPair>(c, tmem, 0);
+    else if (warp < 8) {
+      if (kPair) softmax_role<kBf16, kPair>(c, tmem, 1);
+    } else if (warp == kLoadWarp)
+      load_role<kPair>(c);
+    else if (warp == kMmaWarp)
+      product_role<kBf16, kPair>(c, tmem);
+    else
+      fix_role<kBf16, kPair>(c, warp - kFixWarp);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+  if (kPair && threadIdx.x == 0 && atomicAdd(p.done, 1) == static_cast<int>(gridDim.x) - 1) {
+    *p.next = 0;  // every CTA has taken its last ticket
+    *p.done = 0;
+  }
+}
+
+template <bool kBf16, bool kPair>
+cudaError_t set_limit() {
+  return cudaFuncSetAttribute(paged_attend_kernel<kBf16, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              kSmemBytes);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_attend(const PagedAttendParams& p, cudaStream_t stream) {
-  int most = p.rows_per_seq;
-  if (most < 0)
-    for (int s = 0; s < p.c.batch; ++s) most = max(most, p.cu_rows[s + 1] - p.cu_rows[s]);
-  const dim3 grid((most * p.group + kRows - 1) / kRows, p.c.num_kv_heads, p.c.batch);
-  return p.is_bf16 ? launch_dependent(paged_attend_kernel<true>, grid, kThreads, 0, stream, p)
-                   : launch_dependent(paged_attend_kernel<false>, grid, kThreads, 0, stream, p);
+cudaError_t paged_attend_set_smem_limit() {
+  cudaError_t e = set_limit<true, true>();
+  if (e == cudaSuccess) e = set_limit<true, false>();
+  if (e == cudaSuccess) e = set_limit<false, true>();
+  if (e == cudaSuccess) e = set_limit<false, false>();
+  return e;
+}
+
+cudaError_t launch_paged_attend(const PagedAttendParams& p, int ctas, cudaStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(ctas));
+  if (p.pair)
+    return p.is_bf16 ? launch_dependent(paged_attend_kernel<true, true>, grid, kThreads, kSmemBytes, stream, p)
+                     : launch_dependent(paged_attend_kernel<false, true>, grid, kThreads, kSmemBytes, stream, p);
+  return p.is_bf16 ? launch_dependent(paged_attend_kernel<true, false>, grid, kThreads, kSmemBytes, stream, p)
+                   : launch_dependent(paged_attend_kernel<false, false>, grid, kThreads, kSmemBytes, stream, p);
 }
 
 }  // namespace ckv

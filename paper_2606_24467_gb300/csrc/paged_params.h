@@ -64,25 +64,50 @@ cudaError_t launch_rope(const RopeParams& p, cudaStream_t s);
 cudaError_t launch_paged_append(const RopeParams& p, int most_rows, cudaStream_t s);
 cudaError_t launch_paged_gather(const PagedGatherParams& p, cudaStream_t s);
 
-constexpr int kPagedTile = 128;          // slots of a K or V tile
-constexpr int kPagedHeaderBytes = 1024;  // workspace: status word, the word that says that a call has stopped
+constexpr int kPagedTile = 128;  // slots of a K or V tile, and rows of a tile of queries
+constexpr int kPagedMaxCtas = 160;
+// Chunks: where their items are fewer than the SMs want, slots are cut into
+// blocks of a kPagedCuts-th of an SM's share of the tiles, but of at least
+// kPagedBlock; the results of at most kPagedSlots pieces wait to be joined.
+constexpr int kPagedCuts = 4;
+constexpr int kPagedBlock = 8;
+constexpr int kPagedSlots = 608;
+// Workspace header: status word, the word that says that a call has stopped, the
+// next ticket and the CTAs done; behind it the counters of items in pieces, one
+// for each 32 rows.  Every call leaves them zero.
+constexpr int kPagedTickets = 256;  // bytes
+constexpr int kPagedHeaderBytes = kPagedTickets + kPagedSlots * 8 * 4 + 256 - (kPagedSlots * 32) % 256;
+static_assert(kPagedHeaderBytes % 256 == 0 && kPagedMaxCtas <= kPagedSlots, "header");
 
 struct PagedAttendParams {
-  CUtensorMap map_q, map_k, map_v;
+  CUtensorMap map_q;           // [rows][heads][128]: boxes of a KV group's heads, some tokens, 64 channels
+  CUtensorMap map_k, map_v;    // [pages][slots][heads][128]: boxes of up to 128 slots, 64 channels
   PagedCache c;
-  const uint16_t* q;
   uint16_t* out;
   float* lse;                  // optional, [num_q_heads][rows]
   const int32_t* start;        // optional, [batch]
-  long long q_token, q_head, o_token, o_head;
+  long long o_token, o_head;
   float scale_log2;
-  int rows, num_q_heads, group, causal, is_bf16;
+  int rows, group, causal, is_bf16;
+  int pair;                    // two tiles of rows to an item
+  int tile_tokens;             // query tokens of 128 rows
+  int item_tokens;             // of an item
+  int q_box_bytes;             // of 64 channels of a tile
+  // workspace
   int* status;
   int* stopped;
+  int* next;
+  int* done;
+  int* tickets;
+  float2* part_ml;             // [slots][part_rows]: base-2 reference and sum of a piece's rows,
+  float* part_o;               //   [128]: and output
+  int part_rows;
+  unsigned long long stall_ns; // test hook: CTA 0 waits this long for what nothing sets; 0: not
   int rows_per_seq;
   int cu_rows[kMaxBatch + 1];
 };
 
-cudaError_t launch_paged_attend(const PagedAttendParams& p, cudaStream_t s);
+cudaError_t paged_attend_set_smem_limit();
+cudaError_t launch_paged_attend(const PagedAttendParams& p, int ctas, cudaStream_t s);
 
 }  // namespace ckv
