@@ -1082,17 +1082,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   const Cta c{p, m, smem_u32(smem)};
   // a call that stopped may have left tickets behind: nothing runs until the
   // workspace is set up again
-  if (*reinterpret_cast<volatile int*>(p.stopped) == 0) {
-    if (warp < 4)
-      softmax_role<kBf16, kPair>(c, tmem, 0);
-    else if (warp < 8) {
-      if (kPair) softmax_role<kBf16, kPair>(c, tmem, 1);
-    } else if (warp == kLoadWarp)
-      load_role<kPair>(c);
-    else if (warp == kMmaWarp)
-      product_role<kBf16, kPair>(c, tmem);
-    else
-      fix_role<kBf16, kPair>(c, warp - kFixWarp);
+  const bool go = *reinterpret_cast<volatile int*>(p.stopped) == 0;
+  if (warp < 8) {
+    // registers for the softmax, which holds a row of logits (256 x 208 + 128 x 88
+    // of the launch's 384 x 168)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if (go && (kPair || warp < 4)) softmax_role<kBf16, kPair>(c, tmem, warp / 4);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (go) {
+      if (warp == kLoadWarp)
+        load_role<kPair>(c);
+      else if (warp == kMmaWarp)
+        product_role<kBf16, kPair>(c, tmem);
+      else
+        fix_role<kBf16, kPair>(c, warp - kFixWarp);
+    }
   }
   __syncwarp();
   tc_fence_before();
