@@ -12,9 +12,9 @@
 // unrounded.
 //
 // One CTA per SM, in roles: four warps a 128-row tile for the softmax, one lane of
-// them a row; a warp that finds the work and moves Q, K and V by TMA; one that
-// issues the products; and two that make V fit for tiles of which some rows see
-// only a part.  Two forms:
+// them a row; a warp that finds the work and moves Q, K and V by TMA; one that issues
+// the products; and two that make V fit for tiles of which some rows
+// see only a part.  Two forms:
 //  * kPair, for chunks: two 128-row tiles of the same KV group and sequence share
 //    each tile of K and V, and while the tensor cores work for one, the other's
 //    softmax runs.  An item is two tiles of rows; where there are few items for
@@ -36,7 +36,8 @@ namespace {
 
 constexpr int kTile = kPagedTile;
 constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kFixWarp = 10;  // (0-3, 4-7: softmax)
+constexpr int kMmaWarp = 0, kLoadWarp = 1, kFixWarp = 2;    // 2 and 3: V of tiles seen in part
+constexpr int kSoftWarp = 4;                                // 4 .. 7 and 8 .. 11: softmax of a tile of rows
 constexpr int kHalf = kTile * 128;                          // 64 channels of a tile, bytes
 constexpr int kTileBytes2 = 2 * kHalf;                      // K, V or Q: 32 KB
 constexpr int kRing = 4;                                    // piece descriptors
@@ -68,11 +69,13 @@ struct Shape {
 };
 
 struct Misc {
-  uint64_t full[6], empty[6], vready[6];
-  uint64_t qfull[2], qempty[2], sfull[2], pready[2], odone[2], oempty[2];
+  // a piece's first K; V of a tile with K of the next; stages free again; V fixed
+  uint64_t kfull[kRing], full[kRing], empty[6], vready[kRing];
+  uint64_t qfull[2], qempty[2], sfull[2], pready[2][2], odone[2], oempty[2];
   uint64_t pfull[kRing], pempty[kRing], drain;
   Piece ring[kRing];
-  uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite
+  uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite,
+  uint32_t found[kRing][2];               // and whether there are any, by fixing warp
   uint32_t tmem;
   int abort;
 };
@@ -121,6 +124,12 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // ------------------------------------------------------------- tensor memory
 __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -153,6 +162,23 @@ __device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
   return d;
 }
 
+// One lane of a converged warp; the compiler then knows that no other runs what
+// follows.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
+// The rest of a wait, out of line: the roles' loops run from the instruction
+// caches, and code that hardly ever runs between them costs every pass over it.
+__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort, int* status, int* stopped,
+                                     uint64_t ns) {
+  const bool ok = mbar_wait_bounded(bar, parity, abort, status, ns);
+  if (!ok) atomicExch(stopped, 1);
+  return ok;
+}
+
 // ------------------------------------------------------------------- the call
 struct Cta {
   const PagedAttendParams& p;
@@ -160,15 +186,17 @@ struct Cta {
   uint32_t smem;  // of the operands: Q tiles, then the stages
   // Bounded wait on a phase; false: this CTA stops.
   __device__ __forceinline__ bool wait(uint64_t& bar, uint32_t parity) const {
-    return wait_for(bar, parity, kWaitTimeoutNs);
-  }
-  __device__ bool wait_for(uint64_t& bar, uint32_t parity, uint64_t ns) const {
-    const bool ok = mbar_wait_bounded(smem_u32(&bar), parity, &m->abort, p.status, ns);
-    if (!ok) atomicExch(p.stopped, 1);
-    return ok;
+    const uint32_t at = smem_u32(&bar);
+    return mbar_try_wait(at, parity) || wait_on(at, parity, &m->abort, p.status, p.stopped, kWaitTimeoutNs);
   }
   __device__ __forceinline__ bool wait_warp(uint64_t& bar, uint32_t parity) const {
     return __all_sync(0xffffffffu, wait(bar, parity));
+  }
+  // (without a call: the softmax's registers are full)
+  __device__ __forceinline__ bool wait_here(uint64_t& bar, uint32_t parity) const {
+    const bool ok = mbar_wait_bounded(smem_u32(&bar), parity, &m->abort, p.status);
+    if (!ok) atomicExch(p.stopped, 1);
+    return __all_sync(0xffffffffu, ok);
   }
   __device__ __forceinline__ bool stopped() const { return *reinterpret_cast<volatile int*>(&m->abort) != 0; }
 };
@@ -178,7 +206,7 @@ struct Reader {
   const Cta& c;
   int at = 0;
   __device__ __forceinline__ const Piece* next() {
-    if (!c.wait_warp(c.m->pfull[at % kRing], (at / kRing) & 1)) return nullptr;
+    if (!c.wait_here(c.m->pfull[at % kRing], (at / kRing) & 1)) return nullptr;
     const Piece* x = &c.m->ring[at % kRing];
     return x->go ? x : nullptr;
   }
@@ -256,6 +284,28 @@ __device__ __forceinline__ Blocks blocks_of(const PagedAttendParams& p, const Se
   return {(s.rows + p.item_tokens - 1) / p.item_tokens, p.item_tokens, size};
 }
 
+__device__ __forceinline__ long long warp_prefix(long long x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ long long warp_sum(long long x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// kPair: a sequence's heads 0 .. whole - 1 have `pieces[0]` pieces each, the others
+// pieces[1] (`shared` of them of items with more than one).
+struct Heads {
+  int whole, pieces[2], shared[2];
+  __device__ int all(int heads) const { return whole * pieces[0] + (heads - whole) * pieces[1]; }
+  __device__ int all_shared(int heads) const { return whole * shared[0] + (heads - whole) * shared[1]; }
+};
+
 // Finds the pieces of this CTA, a warp together.
 template <bool kPair>
 struct Finder {
@@ -264,80 +314,112 @@ struct Finder {
   // the 32 sequences that the lanes hold, and what came before them
   int group = -1;
   Sequence s;
-  int mine = 0, upto = 0;      // single: tiles of a head; kPair: pieces of a head; and prefix, inclusive
-  int shared = 0, shared_upto = 0;
-  int before = 0, shared_before = 0;
+  int mine = 0, upto = 0;      // single: tiles of a head; kPair: pieces; and prefix, inclusive
+  int before = 0;
   // kPair
-  int size = 0;                // tiles of a block
+  Heads h;
+  int shared_upto = 0, shared_before = 0;
+  long long work_upto = 0, work_before = 0;
+  int size[2];                 // tiles of a block
+  long long body = 0;          // work of the heads whose blocks are of size[0]
   int ticket = 0;
   // single
   long long all = 0, at = 0, end = 0;
   int ctas = 0;
   uint64_t policy = l2_policy_evict_last();
 
+  // Work of a head, in tiles for two tiles of rows: as if items grew evenly.
+  __device__ long long work_of(const Sequence& x) const {
+    if (x.rows <= 0) return 0;
+    const int items = (x.rows + p.item_tokens - 1) / p.item_tokens;
+    return (static_cast<long long>(items) * (x.tiles(p, min(p.item_tokens, x.rows)) + x.tiles(p, x.rows)) + 1) / 2;
+  }
+  // (work_before and work_upto known)
+  __device__ Heads heads_of(const Sequence& x, long long work, long long ahead) const {
+    Heads r{};
+    if (x.rows <= 0) return r;
+    r.whole = clamp_to((body - ahead) / work, 0, p.c.num_kv_heads);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Blocks b = blocks_of(p, x, size[i]);
+      r.pieces[i] = b.pieces(p, x);
+      r.shared[i] = b.shared_pieces(p, x);
+    }
+    return r;
+  }
   __device__ void hold(int g) {
     group = g;
     s.load(p, g * 32 + lane);
-    mine = shared = 0;
-    if (s.rows > 0) {
-      if (kPair) {
-        const Blocks b = blocks_of(p, s, size);
-        mine = b.pieces(p, s);
-        shared = b.shared_pieces(p, s);
-      } else {
-        mine = s.tiles(p, s.rows);
-      }
+    if (kPair) {
+      const int heads = p.c.num_kv_heads;
+      const long long work = work_of(s);
+      work_upto = warp_prefix(work * heads, lane);
+      h = heads_of(s, work, work_before + work_upto - work * heads);
+      mine = h.all(heads);
+      shared_upto = warp_prefix(h.all_shared(heads), lane);
+    } else {
+      mine = s.rows > 0 ? s.tiles(p, s.rows) : 0;
     }
     upto = warp_prefix(mine, lane);
-    if (kPair) shared_upto = warp_prefix(shared, lane);
   }
   __device__ bool advance() {  // to the next 32
     if ((group + 1) * 32 >= p.c.batch) return false;
     before += __shfl_sync(0xffffffffu, upto, 31);
-    if (kPair) shared_before += __shfl_sync(0xffffffffu, shared_upto, 31);
+    if (kPair) {
+      shared_before += __shfl_sync(0xffffffffu, shared_upto, 31);
+      work_before += __shfl_sync(0xffffffffu, work_upto, 31);
+    }
     hold(group + 1);
     return true;
   }
   __device__ int groups() const { return (p.c.batch + 31) / 32; }
 
-  __device__ void start() {
-    if (kPair) {
-      // work, roughly, and the longest item
-      long long work = 0;
-      int longest = 0;
+  // kPair: the sizes of blocks.  Where items are many, each is a piece; but those
+  // of the last heads, about what the CTAs need to end together, are cut.  Where
+  // they are few, all are.
+  __device__ void plan() {
+    const int heads = p.c.num_kv_heads;
+    long long work = 0;
+    int longest = 0;
+    for (int g = 0; g < groups(); ++g) {
+      Sequence x;
+      x.load(p, g * 32 + lane);
+      work += work_of(x);
+      if (x.rows > 0) longest = max(longest, x.tiles(p, x.rows));
+    }
+    __syncwarp();
+    work = warp_sum(work) * heads;
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    const long long ctas = gridDim.x, share = max(work / ctas, 1LL);
+    size[0] = longest;
+    if (kPagedFew * static_cast<long long>(longest) <= share) {
+      size[1] = min(max(longest / kPagedTailCuts, kPagedBlock), longest);
+      body = max(work - ctas * longest / 2, 0LL);
+    } else {
+      body = 0;
+      size[1] = clamp_to(share / kPagedCuts, min(kPagedBlock, longest), longest);
+      const int cuts = (longest + size[1] - 1) / size[1];
+      size[1] = (longest + cuts - 1) / cuts;
+    }
+    // as many pieces as there is room for their results
+    for (; size[1] < longest; size[1] += max(size[1] / 4, 1)) {
+      long long n = 0, ahead = 0;
       for (int g = 0; g < groups(); ++g) {
         Sequence x;
         x.load(p, g * 32 + lane);
-        if (x.rows <= 0) continue;
-        const int items = (x.rows + p.item_tokens - 1) / p.item_tokens;
-        const int far = x.tiles(p, x.rows);
-        work += static_cast<long long>(items) * (x.tiles(p, min(p.item_tokens, x.rows)) + far);
-        longest = max(longest, far);
+        const long long w = work_of(x), up = warp_prefix(w * heads, lane);
+        n += heads_of(x, w, ahead + up - w * heads).all_shared(heads);
+        ahead += __shfl_sync(0xffffffffu, up, 31);
       }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        work += __shfl_xor_sync(0xffffffffu, work, o);
-        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
-      }
-      const long long share = max(work * p.c.num_kv_heads / (2 * static_cast<long long>(gridDim.x)), 1LL);
-      // Blocks of a share's kPagedCuts-th part where an item is more than that
-      // twice over, and no fewer than kPagedBlock tiles; as many as the results
-      // of shared items have room for.
-      size = longest;
-      if (2LL * longest * kPagedCuts > 4 * share) size = clamp_to(share / kPagedCuts, kPagedBlock, longest > kPagedBlock ? longest : kPagedBlock);
-      const int cuts = (longest + size - 1) / size;
-      size = max((longest + cuts - 1) / cuts, 1);
-      for (; size < longest; size *= 2) {
-        long long n = 0;
-        for (int g = 0; g < groups(); ++g) {
-          Sequence x;
-          x.load(p, g * 32 + lane);
-          if (x.rows > 0) n += blocks_of(p, x, size).shared_pieces(p, x);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        if (n * p.c.num_kv_heads <= kPagedSlots) break;
-      }
+      __syncwarp();
+      if (warp_sum(n) <= kPagedSlots) break;
+    }
+    size[1] = min(size[1], longest);
+  }
+
+  __device__ void start() {
+    if (kPair) {
+      plan();
       if (lane == 0) ticket = atomicAdd(p.next, 1);
       ticket = __shfl_sync(0xffffffffu, ticket, 0);
       hold(0);
@@ -360,7 +442,7 @@ struct Finder {
 
   // Into *x by lane 0; false: there is none.
   __device__ bool find(Piece* x) {
-    const int heads = p.c.num_kv_heads;
+    const int heads = kPair ? 1 : p.c.num_kv_heads;  // that `mine` counts one of
     const long long want = kPair ? ticket : at;
     if (!kPair && at >= end) return false;
     while (want >= static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, 31)) * heads)
@@ -374,17 +456,30 @@ struct Finder {
     q.start = __shfl_sync(0xffffffffu, s.start, src);
     const int count = __shfl_sync(0xffffffffu, mine, src);
     const long long first = static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, src) - count) * heads;
-    const int in_seq = static_cast<int>(want - first), head = in_seq / count;
-    int rest = in_seq - head * count;
+    const int in_seq = static_cast<int>(want - first);
     Piece y;
     y.go = 1;
     y.seq = group * 32 + src;
-    y.head = head;
     y.length = q.length;
     y.rows = q.rows;
     y.start = q.start;
     if (kPair) {
-      const Blocks b = blocks_of(p, q, size);
+      Heads r;
+      r.whole = __shfl_sync(0xffffffffu, h.whole, src);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        r.pieces[i] = __shfl_sync(0xffffffffu, h.pieces[i], src);
+        r.shared[i] = __shfl_sync(0xffffffffu, h.shared[i], src);
+      }
+      const int in_body = r.whole * r.pieces[0];
+      const bool cut = in_seq >= in_body;
+      const int per = cut ? r.pieces[1] : r.pieces[0], at_head = (cut ? in_seq - in_body : in_seq) / per;
+      int rest = (cut ? in_seq - in_body : in_seq) - at_head * per;
+      y.head = at_head + (cut ? r.whole : 0);
+      y.size = cut ? size[1] : size[0];
+      y.base = shared_before + __shfl_sync(0xffffffffu, shared_upto - h.all_shared(p.c.num_kv_heads), src) +
+               (cut ? r.whole * r.shared[0] + at_head * r.shared[1] : at_head * r.shared[0]);
+      const Blocks b = blocks_of(p, q, y.size);
       int block = 0, f = 0, slots = 0;  // slots: of shared items' pieces before the block
       const int f1 = b.first(p, q, 1);
       for (;; ++block) {
@@ -401,18 +496,16 @@ struct Finder {
       y.pos0 = q.start + token;
       const int tokens_a = min(p.item_tokens / 2, y.tokens);
       const int most[2] = {q.tiles(p, token + tokens_a), q.tiles(p, token + y.tokens)};
-      y.tile0 = block * size;
-      const int to = min(most[1], y.tile0 + size);
+      y.tile0 = block * y.size;
+      const int to = min(most[1], y.tile0 + y.size);
       y.tiles[0] = max(min(most[0], to) - y.tile0, 0);
       y.tiles[1] = y.tokens > tokens_a ? to - y.tile0 : 0;
-      for (int i = 0; i < 2; ++i) y.pieces[i] = (most[i] + size - 1) / size;
-      y.size = size;
-      const int shared0 = shared_before + __shfl_sync(0xffffffffu, shared_upto - shared, src);
-      const int shared_n = __shfl_sync(0xffffffffu, shared, src);
-      y.base = shared0 * heads + head * shared_n;
+      for (int i = 0; i < 2; ++i) y.pieces[i] = (most[i] + y.size - 1) / y.size;
       y.slot = y.base + slots + t - (block == 0 ? f1 : f);
       y.ticket = y.base + t - f1;
     } else {
+      const int head = in_seq / count, rest = in_seq - head * count;
+      y.head = head;
       y.item = 0;
       y.row0 = q.row0;
       y.tokens = q.rows;
@@ -483,7 +576,7 @@ __device__ void load_role(const Cta& c) {
   const int page = 1 << p.c.page_shift, box = min(page, kTile), copies = 2 * (kTile / box);
   Finder<kPair> f{p, lane};
   f.start();
-  int pos = 0, loaded = 0;  // stages filled (pos: the one waited for included)
+  int pos = 0, pieces = 0, count = 0;  // stages filled; pieces and tiles begun
   int q_count[2] = {0, 0};
   // this lane's page of a tile (not yet checked)
   auto look_up = [&](const Piece& x, int tile) {
@@ -492,13 +585,14 @@ __device__ void load_role(const Cta& c) {
     const int e = p.c.table[x.seq * p.c.table_stride + (slot >> p.c.page_shift)];
     return e;
   };
-  auto load_tile = [&](const Piece& x, const CUtensorMap& map, int tile, int entry) {
+  // `arm`: bytes that the barrier is to wait for from here on
+  auto load_tile = [&](const Piece& x, const CUtensorMap& map, int tile, int entry, uint64_t& full, uint32_t arm) {
     const int st = pos % S::kStages;
     if (!c.wait_warp(c.m->empty[st], ((pos / S::kStages) & 1) ^ 1)) return false;
-    const uint32_t bar = smem_u32(&c.m->full[st]);
-    if (lane == 0) mbar_arrive_expect_tx(bar, kTileBytes2);
+    const uint32_t bar = smem_u32(&full);
+    if (lane == 0 && arm) mbar_arrive_expect_tx(bar, arm);
     __syncwarp();
-    loaded = ++pos;
+    ++pos;
     if (lane < copies) {
       const int half = lane & 1, part = lane >> 1;
       if (entry < 0 || entry > p.c.num_pages ||
@@ -536,13 +630,20 @@ __device__ void load_role(const Cta& c) {
     if (!found) break;
     const int tiles = max(x.tiles[0], x.tiles[1]), first = x.tile0;
     int now = look_up(x, first), next = tiles > 1 ? look_up(x, first + 1) : 0;
-    ok = load_tile(x, p.map_k, first, now);
+    ok = load_tile(x, p.map_k, first, now, c.m->kfull[n % kRing], kTileBytes2);
+    pieces += ok;
     for (int t = 0; ok && t < S::kQTiles; ++t)
       if (x.tiles[t]) ok = load_q(x, t);
     for (int j = 0; ok && j < tiles; ++j) {
       const int after = j + 2 < tiles ? look_up(x, first + j + 2) : 0;
-      if (j + 1 < tiles) ok = load_tile(x, p.map_k, first + j + 1, next);
-      if (ok) ok = load_tile(x, p.map_v, first + j, now);
+      const bool more = j + 1 < tiles;
+      uint64_t& full = c.m->full[count % kRing];
+      if (more) {
+        ok = load_tile(x, p.map_k, first + j + 1, next, full, 2 * kTileBytes2);
+        count += ok;
+      }
+      if (ok) ok = load_tile(x, p.map_v, first + j, now, full, more ? 0 : kTileBytes2);
+      count += ok && !more;
       now = next;
       next = after;
     }
@@ -550,11 +651,14 @@ __device__ void load_role(const Cta& c) {
   // No copy, and no arrival that a stage or Q tile is free again, may come after
   // this CTA has ended.  (A stopped CTA has only its copies to wait for.)
   const bool all = !c.stopped();
-  for (int i = max(loaded - S::kStages, 0); i < loaded; ++i) {
-    if (all)
+  if (all) {
+    for (int i = max(pos - S::kStages, 0); i < pos; ++i)
       c.wait_warp(c.m->empty[i % S::kStages], (i / S::kStages) & 1);
-    else
-      settle(c.m->full[i % S::kStages], (i / S::kStages) & 1, 100000000ull);
+  } else {
+    for (int i = max(pieces - kRing, 0); i < pieces; ++i)
+      settle(c.m->kfull[i % kRing], (i / kRing) & 1, 100000000ull);
+    for (int i = max(count - kRing, 0); i < count; ++i)
+      settle(c.m->full[i % kRing], (i / kRing) & 1, 100000000ull);
   }
   for (int t = 0; t < S::kQTiles; ++t)
     if (q_count[t]) {
@@ -566,121 +670,134 @@ __device__ void load_role(const Cta& c) {
 }
 
 // ---------------------------------------------------------------- products
+// One lane does all of it: what it spends between two issues (a wait of a whole
+// warp costs 110 to 150 cycles even where there is nothing to wait for) the tensor
+// cores idle.  With kPair it takes the two tiles of rows in turn, so that one's
+// softmax runs beside the other's products: a lane for each tile let them fall
+// into step, both softmaxes at a time and then both products (7550 us instead of
+// 6300 for a chunk of 4096 tokens after 128K).
 template <bool kBf16, bool kPair>
 __device__ void product_role(const Cta& c, uint32_t tmem) {
   using S = Shape<kPair>;
-  const bool lead = (threadIdx.x & 31) == 0;
   constexpr uint32_t kQk = umma_idesc_f16(kTile, kTile, kBf16);
   constexpr uint32_t kPv = kQk | 1u << 16;  // V: channels, not slots, are contiguous
   const uint32_t stages = c.smem + S::kQTiles * kTileBytes2;
   auto bar = [&](uint64_t& b) { return smem_u32(&b); };
-  auto stage = [&](int pos) { return pos % S::kStages; };
-  auto logits = [&](int q, int buffer, int pos) {
+  auto logits = [&](int q, int buffer, int st) {
     const uint64_t a = smem_desc_sw128(c.smem + q * kTileBytes2);
-    const uint64_t b = smem_desc_sw128(stages + stage(pos) * kTileBytes2);
+    const uint64_t b = smem_desc_sw128(stages + st * kTileBytes2);
 #pragma unroll
     for (int i = 0; i < kHeadDim / 16; ++i) {
       const uint64_t step = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
       umma_f16(tmem + buffer * kTile, a + step, b + step, kQk, i > 0);
     }
   };
-  auto output = [&](int o, int buffer, int pos, bool more) {
-    const uint64_t b = v_desc(stages + stage(pos) * kTileBytes2);
+  auto output = [&](int o, int buffer, int st, bool more, int i0, int i1) {
+    const uint64_t b = v_desc(stages + st * kTileBytes2);
 #pragma unroll
-    for (int i = 0; i < kTile / 16; ++i)
+    for (int i = i0; i < i1; ++i)
       umma_f16_ts(tmem + (2 + o) * kTile, tmem + buffer * kTile + i * 8, b + i * (2048 >> 4), kPv, more || i > 0);
   };
-  Reader reader{c};
-  int pos = 0;
-  uint32_t v_phase = 0;   // by stage
-  int q_count[2] = {0, 0}, p_count[2] = {0, 0}, o_count[2] = {0, 0};
-  auto wait_k = [&](int at) { return c.wait_warp(c.m->full[stage(at)], (at / S::kStages) & 1); };
-  auto wait_v = [&](int at) {
-    const int st = stage(at);
-    const bool ok = wait_k(at) && c.wait_warp(c.m->vready[st], (v_phase >> st) & 1);
-    v_phase ^= 1u << st;
-    return ok;
+  int at = 0, count = 0;  // the next stage; tiles
+  auto step = [&] {
+    const int st = at;
+    at = at + 1 == S::kStages ? 0 : at + 1;
+    return st;
   };
-  while (const Piece* x = reader.next()) {
-    const int n[2] = {x->tiles[0], kPair ? x->tiles[1] : 0};
-    const int tiles = max(n[0], n[1]);
-    if (!wait_k(pos)) break;
-    bool ok = true;
-    for (int t = 0; ok && t < S::kQTiles; ++t)
-      if (n[t]) {
-        ok = c.wait_warp(c.m->qfull[t], q_count[t]++ & 1);
-        const int buffer = kPair ? t : p_count[0] & 1;
-        if (ok && lead) {
-          tc_fence_after();
-          logits(t, buffer, pos);
-          umma_commit(bar(c.m->sfull[buffer]));
-          if (n[t] == 1) umma_commit(bar(c.m->qempty[t]));
-        }
+  // phases, a bit for each stage, tile of rows or buffer
+  uint32_t v_phase = 0, q_phase = 0, o_phase = 3, p_phase = 0;
+  auto turn = [](uint32_t& phases, int i) {
+    const uint32_t phase = (phases >> i) & 1;
+    phases ^= 1u << i;
+    return phase;
+  };
+  // the product with V of buffer b's probabilities into output t
+  auto add = [&](int t, int b, int v, int j) {
+    if (j == 0 && !c.wait(c.m->oempty[t], turn(o_phase, t))) return false;
+    const uint32_t phase = turn(p_phase, b);
+    if (!c.wait(c.m->pready[b][0], phase)) return false;
+    tc_fence_after();
+    output(t, b, v, j > 0, 0, kTile / 32);
+    if (!c.wait(c.m->pready[b][1], phase)) return false;
+    tc_fence_after();
+    output(t, b, v, j > 0, kTile / 32, kTile / 16);
+    return true;
+  };
+  bool ok = true;
+  int next = 0;  // single: buffer of the next logits
+  for (int piece = 0; ok; ++piece) {
+    if (!(ok = c.wait(c.m->pfull[piece % kRing], (piece / kRing) & 1))) break;
+    const Piece& x = c.m->ring[piece % kRing];
+    if (!x.go) break;
+    const int n0 = x.tiles[0], n1 = kPair ? x.tiles[1] : 0;
+    const int in_part = limit_of(c.p, x.pos0, x.length) / kTile - x.tile0;  // first tile that not all rows see whole
+    mbar_arrive(bar(c.m->pempty[piece % kRing]));
+    const int tiles = max(n0, n1);
+    if (!(ok = c.wait(c.m->kfull[piece % kRing], (piece / kRing) & 1))) break;
+    const int k0 = step();
+#pragma unroll
+    for (int t = 0; t < S::kQTiles; ++t) {
+      const int n = t ? n1 : n0;
+      if (!ok || !n) continue;
+      ok = c.wait(c.m->qfull[t], turn(q_phase, t));
+      const int buffer = kPair ? t : next;
+      next ^= 1;
+      if (ok) {
+        tc_fence_after();
+        logits(t, buffer, k0);
+        umma_commit(bar(c.m->sfull[buffer]));
+        if (n == 1) umma_commit(bar(c.m->qempty[t]));
       }
+    }
     if (!ok) break;
-    if (lead) umma_commit(bar(c.m->empty[stage(pos)]));
-    ++pos;
+    umma_commit(bar(c.m->empty[k0]));
     if (c.p.stall_ns && blockIdx.x == 0) {  // test hook: a wait for what nothing completes
-      c.wait_for(c.m->drain, 0, c.p.stall_ns);
+      wait_on(bar(c.m->drain), 0, &c.m->abort, c.p.status, c.p.stopped, c.p.stall_ns);
       break;
     }
+#pragma unroll 1
     for (int j = 0; ok && j < tiles; ++j) {
       const bool more = j + 1 < tiles;
-      const int kpos = pos, vpos = pos + more;
-      pos = vpos + 1;
+      const int k = more ? step() : 0, v = step(), slot = count % kRing;
+      ok = c.wait(c.m->full[slot], (count / kRing) & 1) &&
+           (j < in_part || c.wait(c.m->vready[slot], turn(v_phase, slot)));
+      if (!ok) break;
+      ++count;
       if (kPair) {
-        ok = wait_v(vpos) && (!more || wait_k(kpos));
-        for (int t = 0; ok && t < 2; ++t)
-          if (j < n[t]) {
-            ok = c.wait_warp(c.m->pready[t], p_count[t]++ & 1);
-            if (ok && j == 0) ok = c.wait_warp(c.m->oempty[t], (o_count[t]++ & 1) ^ 1);
-            if (ok && lead) {
-              tc_fence_after();
-              output(t, t, vpos, j > 0);
-              if (j + 1 < n[t]) {
-                logits(t, t, kpos);
-                umma_commit(bar(c.m->sfull[t]));
-                if (j + 2 == n[t]) umma_commit(bar(c.m->qempty[t]));
-              } else {
-                umma_commit(bar(c.m->odone[t]));
-              }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int n = t ? n1 : n0;
+          if (ok && j < n && (ok = add(t, t, v, j))) {
+            if (t == 1 || j >= n1) umma_commit(bar(c.m->empty[v]));
+            if (j + 1 < n) {
+              logits(t, t, k);
+              umma_commit(bar(c.m->sfull[t]));
+              if (j + 2 == n) umma_commit(bar(c.m->qempty[t]));
+            } else {
+              umma_commit(bar(c.m->odone[t]));
             }
           }
-        if (ok && lead) {
-          umma_commit(bar(c.m->empty[stage(vpos)]));
-          if (more) umma_commit(bar(c.m->empty[stage(kpos)]));
         }
+        if (ok && more) umma_commit(bar(c.m->empty[k]));
       } else {
         if (more) {
-          ok = wait_k(kpos);
-          const int buffer = (p_count[0] + 1) & 1;
-          if (ok && lead) {
-            tc_fence_after();
-            logits(0, buffer, kpos);
-            umma_commit(bar(c.m->sfull[buffer]));
-            umma_commit(bar(c.m->empty[stage(kpos)]));
-            if (j + 2 == tiles) umma_commit(bar(c.m->qempty[0]));
-          }
-        }
-        const int buffer = p_count[0] & 1, phase = (p_count[0] >> 1) & 1;
-        ++p_count[0];
-        ok = ok && wait_v(vpos) && c.wait_warp(c.m->pready[buffer], phase);
-        if (ok && j == 0) ok = c.wait_warp(c.m->oempty[0], (o_count[0]++ & 1) ^ 1);
-        if (ok && lead) {
           tc_fence_after();
-          output(0, buffer, vpos, j > 0);
-          umma_commit(bar(c.m->odone[0]));
-          umma_commit(bar(c.m->empty[stage(vpos)]));
+          logits(0, next, k);
+          umma_commit(bar(c.m->sfull[next]));
+          umma_commit(bar(c.m->empty[k]));
+          if (j + 2 == tiles) umma_commit(bar(c.m->qempty[0]));
+          next ^= 1;
         }
+        // (the buffer that holds this tile's: next, if the other one's logits are under way)
+        if (!(ok = add(0, more ? next : next ^ 1, v, j))) break;
+        umma_commit(bar(c.m->odone[0]));
+        umma_commit(bar(c.m->empty[v]));
       }
-      __syncwarp();
     }
-    if (!ok) break;
-    reader.done();
   }
   // every product, and every arrival that waits for one, is over before the
   // tensor memory is given back
-  if (lead) umma_commit(bar(c.m->drain));
+  umma_commit(bar(c.m->drain));
   settle(c.m->drain, 0, 1000000000ull);
 }
 
@@ -689,6 +806,18 @@ __device__ void product_role(const Cta& c, uint32_t tmem) {
 // the item's first token does not see whole, rows of slots behind the length
 // become zero, and what is not finite in slots that other tokens see: those slots
 // are noted, and the rows that do see them get it added to their output.
+// (Two warps, eight slots at a time each.  x times 0 is 0, or NaN where x is not
+// finite: a multiply-add a pair of channels finds the few that need a closer look.
+// One warp that looked at each exponent took up to 8700 cycles a tile.)
+template <bool kBf16>
+__device__ __forceinline__ uint32_t add_zeros(uint32_t x, uint32_t sum) {
+  if (kBf16)
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+  else
+    asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+  return sum;
+}
+
 template <bool kBf16, bool kPair>
 __device__ void fix_role(const Cta& c, int part) {
   using S = Shape<kPair>;
@@ -696,50 +825,73 @@ __device__ void fix_role(const Cta& c, int part) {
   const int lane = threadIdx.x & 31;
   constexpr uint32_t kTop = kBf16 ? 0x7f807f80u : 0x7c007c00u;  // exponents of all ones
   Reader reader{c};
-  int pos = 0;
+  int pos = 0, count = 0;
   while (const Piece* x = reader.next()) {
+    uint32_t* found = c.m->found[reader.at % kRing];
     uint32_t(*poison)[4] = c.m->poison[reader.at % kRing];
-    if (lane < 2 * kDiagTiles) poison[lane >> 1][2 * part + (lane & 1)] = 0;
+    // (this warp's bits: those of slots 8 part .. 8 part + 7 of each 16)
+    const uint32_t mine = part ? 0xff00ff00u : 0x00ff00ffu;
+    if (lane < 4 * kDiagTiles) atomicAnd(&poison[lane >> 2][lane & 3], ~mine);
+    if (lane == 0) found[part] = 0;
     __syncwarp();
     const int tiles = max(x->tiles[0], x->tiles[1]), tile0 = x->tile0, length = x->length;
     const int whole = limit_of(p, x->pos0, length);  // slots that all rows see
     bool ok = true;
-    ++pos;  // (the first K)
-    for (int j = 0; j < tiles; ++j) {
-      if (j + 1 < tiles) ++pos;
-      const int st = pos % S::kStages;
-      if (!(ok = c.wait_warp(c.m->full[st], (pos / S::kStages) & 1))) break;
-      ++pos;
+    auto pass = [&](int at) {  // a stage is not free before these warps are past it
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->empty[at % S::kStages]));
+    };
+    for (int j = 0; j < tiles; ++j, ++count) {
+      // (of every tile, or the phase of a later one could be taken for it)
+      if (!(ok = c.wait_warp(c.m->full[count % kRing], (count / kRing) & 1))) break;
+      if (j == 0) pass(pos++);             // the first K
+      if (j + 1 < tiles) pass(pos++);      // the next K
+      const int st = pos++ % S::kStages;
       const int base = (tile0 + j) * kTile;
       if (base + kTile > whole) {
         char* v = reinterpret_cast<char*>(c.m) - kOperandBytes + (S::kQTiles + st) * kTileBytes2;
         const int diag = tile0 + j - whole / kTile;
-        // two slots at a time, 16 pieces of 16 bytes each
-        for (int i = max(whole - base, 64 * part) & ~1; i < 64 * part + 64; i += 2) {
-          const int slot = i + (lane >> 4);
-          uint4* at = reinterpret_cast<uint4*>(v + ((lane >> 3) & 1) * kHalf + slot * 128) + (lane & 7);
-          if (base + slot >= length) {
-            *at = make_uint4(0, 0, 0, 0);
-          } else if (base + slot >= whole) {
-            uint4 w = *at;
-            uint32_t* word = &w.x;
-            bool found = false;
+        // 16 pieces of 16 bytes a slot
+        for (int i = (max(whole - base, 0) & ~15) + 8 * part; i < kTile; i += 16) {
+          uint4* at = reinterpret_cast<uint4*>(v + ((lane >> 3) & 1) * kHalf + (i + (lane >> 4)) * 128) + (lane & 7);
+          const int slot = base + i + (lane >> 4);
+          uint32_t sum = 0;
+          if (base + i < length) {
+            uint4 w[4];
 #pragma unroll
+            for (int u = 0; u < 4; ++u) w[u] = at[16 * u];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (slot + 2 * u < length)
+                sum = add_zeros<kBf16>(w[u].x, add_zeros<kBf16>(w[u].y, add_zeros<kBf16>(w[u].z, add_zeros<kBf16>(w[u].w, sum))));
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (slot + 2 * u >= length) at[16 * u] = make_uint4(0, 0, 0, 0);
+          if ((sum & 0x7fff7fffu) == 0) continue;
+#pragma unroll 1
+          for (int u = 0; u < 4; ++u) {
+            const int s = slot + 2 * u;
+            if (s >= length || s < whole) continue;
+            bool any = false;
+            uint32_t* word = reinterpret_cast<uint32_t*>(at + 16 * u);
+#pragma unroll 1
             for (int k = 0; k < 4; ++k) {
-              const uint32_t e = word[k] & kTop;
-              if ((e & 0xffffu) == (kTop & 0xffffu)) word[k] &= 0xffff0000u, found = true;
-              if ((e & 0xffff0000u) == (kTop & 0xffff0000u)) word[k] &= 0xffffu, found = true;
+              uint32_t y = word[k];
+              if ((y & kTop & 0xffffu) == (kTop & 0xffffu)) y &= 0xffff0000u, any = true;
+              if ((y & kTop & 0xffff0000u) == (kTop & 0xffff0000u)) y &= 0xffffu, any = true;
+              word[k] = y;
             }
-            if (found) {
-              *at = w;
-              if (diag < kDiagTiles) atomicOr(&poison[diag][slot >> 5], 1u << (slot & 31));
+            if (any && diag < kDiagTiles) {
+              atomicOr(&poison[diag][(s - base) >> 5], 1u << ((s - base) & 31));
+              found[part] = 1;
             }
           }
         }
         fence_proxy_async_smem();
         __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c.m->vready[count % kRing]));
       }
-      if (lane == 0) mbar_arrive(smem_u32(&c.m->vready[st]));
+      pass(st);
     }
     if (!ok) return;
     reader.done();
@@ -747,9 +899,77 @@ __device__ void fix_role(const Cta& c, int part) {
 }
 
 // ---------------------------------------------------------------- softmax
+// A row's output and log-sum-exp, of base-2 reference `ref` and sum `l`.
+template <bool kBf16>
+__device__ __forceinline__ void write_row(const PagedAttendParams& p, long long row, int head, float ref, float l,
+                                          const uint32_t (&o)[4][32]) {
+  const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
+  const float inv = 1.f / l;
+  uint4* to = reinterpret_cast<uint4*>(p.out + row * p.o_token + head * p.o_head);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = 8 * i + 2 * k;
+      w[k] = none ? 0u
+                  : pack<kBf16>(__uint_as_float(o[at / 32][at % 32]) * inv,
+                                __uint_as_float(o[at / 32][at % 32 + 1]) * inv);
+    }
+    to[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  if (p.lse)
+    p.lse[static_cast<long long>(head) * p.rows + row] = none ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+}
+
 // The results of an item's pieces for this warp's rows, joined: the weights of the
-// pieces are 2^(their reference - the largest), over the sum.
-template <bool kBf16, bool kPair>
+// pieces are 2^(their reference - the largest), over the sum.  kPair: rows by
+// lanes, as they were computed; four channels of consecutive rows are side by side
+// (rows by the warp, in order, as below: a split item of 256 rows took 35 us more).
+template <bool kBf16>
+__device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piece& x, int tile, int row, int token,
+                                          int head, bool valid, uint32_t (&o)[4][32]) {
+  const int pieces = x.pieces[tile];
+  float top = -INFINITY, sum = 0.f;
+  {
+    Slots<true> slots(p, x);
+    for (int k = 0; k < pieces; ++k) {
+      const float2 ml = __ldcg(p.part_ml + static_cast<long long>(slots.next()) * p.part_rows + row);
+      if (ml.y != 0.f) top = fmaxf(top, ml.x);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 128; ++i) o[i / 32][i % 32] = 0;
+  Slots<true> slots(p, x);
+  for (int k = 0; k < pieces; ++k) {
+    const long long slot = slots.next();
+    const float2 ml = __ldcg(p.part_ml + slot * p.part_rows + row);
+    // (equal infinities: 1, so that they and NaN go on into the sum)
+    const float w = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : exp2f(ml.x - top);
+    sum += ml.y == 0.f ? 0.f : ml.y * w;
+    const float4* from = reinterpret_cast<const float4*>(p.part_o) + slot * p.part_rows * 32 + row;
+    if (w != 0.f) {
+#pragma unroll
+      for (int i0 = 0; i0 < 32; i0 += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __ldcg(from + (i0 + i) * p.part_rows);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = 4 * (i0 + i);
+          uint32_t* to = &o[at / 32][at % 32];
+          to[0] = __float_as_uint(fmaf(w, v[i].x, __uint_as_float(to[0])));
+          to[1] = __float_as_uint(fmaf(w, v[i].y, __uint_as_float(to[1])));
+          to[2] = __float_as_uint(fmaf(w, v[i].z, __uint_as_float(to[2])));
+          to[3] = __float_as_uint(fmaf(w, v[i].w, __uint_as_float(to[3])));
+        }
+      }
+    }
+  }
+  if (valid) write_row<kBf16>(p, x.row0 + token, head, top, sum, o);
+}
+
+template <bool kBf16>
 __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int tile, int row0, unsigned valid) {
   const int lane = threadIdx.x & 31, pieces = x.pieces[tile];
   while (valid) {
@@ -765,7 +985,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
 #pragma unroll
     for (int i = 0; i < 4; ++i) top[i] = -INFINITY;
     {
-      Slots<kPair> slots(p, x);
+      Slots<false> slots(p, x);
       for (int k0 = 0; k0 < pieces; k0 += 32) {
         int mine = -1;
         for (int k = 0; k < min(32, pieces - k0); ++k) {
@@ -785,7 +1005,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
     }
     float4 acc[4] = {};
     {
-      Slots<kPair> slots(p, x);
+      Slots<false> slots(p, x);
       for (int k0 = 0; k0 < pieces; k0 += 32) {
         const int count = min(32, pieces - k0);
         int mine = -1;
@@ -878,7 +1098,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     float m = -INFINITY, l = 0.f;
     for (int j = 0; j < n; ++j, ++count) {
       const int buffer = kPair ? tile : count & 1;
-      if (!c.wait_warp(c.m->sfull[buffer], (kPair ? count : count >> 1) & 1)) return;
+      if (!c.wait_here(c.m->sfull[buffer], (kPair ? count : count >> 1) & 1)) return;
       const uint32_t s_addr = lanes + buffer * kTile;
       if (rows) {
         tc_fence_after();
@@ -897,15 +1117,13 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
             for (int i = 0; i < 32; ++i)
               if (32 * k + i >= see) s[k][i] = 0xff800000u;
         }
-        float top[4];
+        float top[4] = {m, m, m, m};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          top[k] = __uint_as_float(s[k][0]);
+        for (int i = 0; i < 32; i += 2)
 #pragma unroll
-          for (int i = 1; i < 32; ++i) top[k] = fmaxf(top[k], __uint_as_float(s[k][i]));
-        }
-        const float now = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), m);
-        if (!kPair && j > 0 && !c.wait_warp(c.m->odone[0], o_count++ & 1)) return;
+          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(s[k][i]), __uint_as_float(s[k][i + 1]));
+        const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], o_count++ & 1)) return;
         const bool grown = now > m && (m == -INFINITY || (now - m) * scale > kGrowth);
         if (__any_sync(0xffffffffu, grown)) {
           const float f = grown ? ex2_approx((m - now) * scale) : 1.f;
@@ -944,19 +1162,26 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
             w[i] = pack<kBf16>(a, b);
           }
           tmem_store16(s_addr + 16 * k, w);
+          if (k == 1) {  // the product with the first half of the slots can begin
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][0]));
+          }
         }
         const float2 total = split_of(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
         l += total.x + total.y;
         tmem_wait_st();
         tc_fence_before();
-      } else if (!kPair && j > 0 && !c.wait_warp(c.m->odone[0], o_count++ & 1)) {
-        return;
+      } else {
+        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], o_count++ & 1)) return;
+        if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][0]));
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer]));
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][1]));
     }
     // the piece's output
-    if (!c.wait_warp(c.m->odone[tile], o_count++ & 1)) return;
+    if (!c.wait_here(c.m->odone[tile], o_count++ & 1)) return;
     uint32_t o[4][32];
     tc_fence_after();
 #pragma unroll
@@ -969,6 +1194,8 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     if (lane == 0) mbar_arrive(smem_u32(&c.m->oempty[tile]));
     const Piece y = *x;
     const int whole = limit_of(p, pos0, length);
+    const uint32_t* found = c.m->found[reader.at % kRing];
+    if (found[0] | found[1])
     for (int d = 0; d < kDiagTiles; ++d)
       for (int k = 0; k < 4; ++k) {
         uint32_t bits = c.m->poison[reader.at % kRing][d][k];
@@ -989,38 +1216,21 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     reader.done();
     const float ref = m == -INFINITY ? 0.f : m * scale;
     const int row0 = tile * kTile + warp * 32;
+    const int head = y.head * p.group + r - in_tile * p.group;
     if (y.pieces[tile] == 1) {
-      if (valid) {
-        const float inv = 1.f / l;
-        const bool none = l == 0.f;
-        const long long row_at = y.row0 + token;
-        const int head = y.head * p.group + r - in_tile * p.group;
-        uint16_t* to = p.out + row_at * p.o_token + head * p.o_head;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int at = 8 * i + 2 * k;
-            w[k] = none ? 0u
-                        : pack<kBf16>(__uint_as_float(o[at / 32][at % 32]) * inv,
-                                      __uint_as_float(o[at / 32][at % 32 + 1]) * inv);
-          }
-          reinterpret_cast<uint4*>(to)[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        if (p.lse)
-          p.lse[static_cast<long long>(head) * p.rows + row_at] =
-              none ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
-      }
+      if (valid) write_row<kBf16>(p, y.row0 + token, head, ref, l, o);
     } else if (rows) {
+      const int row = row0 + lane;
       if (valid) {
-        const long long at = static_cast<long long>(y.slot) * p.part_rows + row0 + lane;
-        p.part_ml[at] = make_float2(ref, l);
-        float4* to = reinterpret_cast<float4*>(p.part_o + at * kHeadDim);
+        const long long at = static_cast<long long>(y.slot) * p.part_rows;
+        p.part_ml[at + row] = make_float2(ref, l);
+        float4* to = reinterpret_cast<float4*>(p.part_o) + at * 32 + (kPair ? row : row * 32);
+        const int step = kPair ? p.part_rows : 1;
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          to[i] = make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
-                              __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
+          to[i * step] =
+              make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
+                          __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
       }
       __threadfence();
       __syncwarp();
@@ -1031,7 +1241,10 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
       if (before == y.pieces[tile] - 1) {
         __threadfence();
         if (lane == 0) *ticket = 0;
-        join<kBf16, kPair>(p, y, tile, row0, rows);
+        if (kPair)
+          join_rows<kBf16>(p, y, tile, row, token, head, valid, o);
+        else
+          join<kBf16>(p, y, tile, row0, rows);
       }
     }
   }
@@ -1045,19 +1258,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(smem_u32(&m->full[i]), 1);
-      mbar_init(smem_u32(&m->empty[i]), 1);
-      mbar_init(smem_u32(&m->vready[i]), 2);
+      mbar_init(smem_u32(&m->empty[i]), 3);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&m->qfull[i]), 1);
       mbar_init(smem_u32(&m->qempty[i]), 1);
       mbar_init(smem_u32(&m->sfull[i]), 1);
-      mbar_init(smem_u32(&m->pready[i]), 4);
+      mbar_init(smem_u32(&m->pready[i][0]), 4);
+      mbar_init(smem_u32(&m->pready[i][1]), 4);
       mbar_init(smem_u32(&m->odone[i]), 1);
       mbar_init(smem_u32(&m->oempty[i]), 4);
     }
     for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&m->kfull[i]), 1);
+      mbar_init(smem_u32(&m->full[i]), 1);
+      mbar_init(smem_u32(&m->vready[i]), 2);
       mbar_init(smem_u32(&m->pfull[i]), 1);
       mbar_init(smem_u32(&m->pempty[i]), S::kConsumers);
     }
@@ -1083,20 +1298,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   // a call that stopped may have left tickets behind: nothing runs until the
   // workspace is set up again
   const bool go = *reinterpret_cast<volatile int*>(p.stopped) == 0;
-  if (warp < 8) {
+  if (warp >= kSoftWarp && warp < kSoftWarp + 8) {
     // registers for the softmax, which holds a row of logits (256 x 208 + 128 x 88
     // of the launch's 384 x 168)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    if (go && (kPair || warp < 4)) softmax_role<kBf16, kPair>(c, tmem, warp / 4);
+    if (go && (kPair || warp < kSoftWarp + 4)) softmax_role<kBf16, kPair>(c, tmem, (warp - kSoftWarp) / 4);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (go) {
       if (warp == kLoadWarp)
         load_role<kPair>(c);
-      else if (warp == kMmaWarp)
-        product_role<kBf16, kPair>(c, tmem);
-      else
+      else if (warp != kMmaWarp)
         fix_role<kBf16, kPair>(c, warp - kFixWarp);
+      else if (elect_one())
+        product_role<kBf16, kPair>(c, tmem);
     }
   }
   __syncwarp();

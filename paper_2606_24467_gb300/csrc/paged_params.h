@@ -66,10 +66,13 @@ cudaError_t launch_paged_gather(const PagedGatherParams& p, cudaStream_t s);
 
 constexpr int kPagedTile = 128;  // slots of a K or V tile, and rows of a tile of queries
 constexpr int kPagedMaxCtas = 160;
-// Chunks: where their items are fewer than the SMs want, slots are cut into
-// blocks of a kPagedCuts-th of an SM's share of the tiles, but of at least
-// kPagedBlock; the results of at most kPagedSlots pieces wait to be joined.
-constexpr int kPagedCuts = 4;
+// Chunks.  An item (two tiles of rows) of more than a kPagedFew-th of an SM's share
+// of the tiles is cut into blocks of slots of about a kPagedCuts-th of it, but of
+// at least kPagedBlock tiles; else only those at the end are, in kPagedTailCuts.
+// The results of at most kPagedSlots pieces wait to be joined.
+constexpr int kPagedFew = 2;
+constexpr int kPagedCuts = 2;
+constexpr int kPagedTailCuts = 5;
 constexpr int kPagedBlock = 8;
 constexpr int kPagedSlots = 608;
 // Workspace header: status word, the word that says that a call has stopped, the
