@@ -12,9 +12,9 @@
 // unrounded.
 //
 // One CTA per SM, in roles: four warps a 128-row tile for the softmax, one lane of
-// them a row; a warp that finds the work and moves Q, K and V by TMA; one that issues
-// the products; and two that make V fit for tiles of which some rows
-// see only a part.  Two forms:
+// them a row; a warp that finds the work and moves Q, K and V by TMA; one a
+// tile that issues the products; and one that makes V fit for tiles of which some
+// rows see only a part.  Two forms:
 //  * kPair, for chunks: two 128-row tiles of the same KV group and sequence share
 //    each tile of K and V, and while the tensor cores work for one, the other's
 //    softmax runs.  An item is two tiles of rows; where there are few items for
@@ -36,7 +36,7 @@ namespace {
 
 constexpr int kTile = kPagedTile;
 constexpr int kThreads = 384;
-constexpr int kMmaWarp = 0, kLoadWarp = 1, kFixWarp = 2;    // 2 and 3: V of tiles seen in part
+constexpr int kMmaWarp = 0, kLoadWarp = 1, kFixWarp = 2;    // (kPair: 3 issues for the second tile)
 constexpr int kSoftWarp = 4;                                // 4 .. 7 and 8 .. 11: softmax of a tile of rows
 constexpr int kHalf = kTile * 128;                          // 64 channels of a tile, bytes
 constexpr int kTileBytes2 = 2 * kHalf;                      // K, V or Q: 32 KB
@@ -65,17 +65,17 @@ template <bool kPair>
 struct Shape {
   static constexpr int kQTiles = kPair ? 2 : 1;
   static constexpr int kStages = kPair ? 5 : 6;
-  static constexpr int kConsumers = kPair ? 11 : 7;  // warps that read a piece
+  static constexpr int kConsumers = kPair ? 11 : 6;  // warps that read a piece
 };
 
 struct Misc {
   // a piece's first K; V of a tile with K of the next; stages free again; V fixed
   uint64_t kfull[kRing], full[kRing], empty[6], vready[kRing];
   uint64_t qfull[2], qempty[2], sfull[2], pready[2][2], odone[2], oempty[2];
-  uint64_t pfull[kRing], pempty[kRing], drain;
+  uint64_t pfull[kRing], pempty[kRing], drain[2], turn[2];
   Piece ring[kRing];
   uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite,
-  uint32_t found[kRing][2];               // and whether there are any, by fixing warp
+  uint32_t found[kRing];                  // and whether there are any
   uint32_t tmem;
   int abort;
 };
@@ -670,14 +670,14 @@ __device__ void load_role(const Cta& c) {
 }
 
 // ---------------------------------------------------------------- products
-// One lane does all of it: what it spends between two issues (a wait of a whole
-// warp costs 110 to 150 cycles even where there is nothing to wait for) the tensor
-// cores idle.  With kPair it takes the two tiles of rows in turn, so that one's
-// softmax runs beside the other's products: a lane for each tile let them fall
-// into step, both softmaxes at a time and then both products (7550 us instead of
-// 6300 for a chunk of 4096 tokens after 128K).
+// One lane does a tile's products (a wait of a whole warp costs 110 to 150 cycles
+// even where there is nothing to wait for).  With kPair two lanes of two warps take
+// turns, so that one tile's softmax runs beside the other's products, and each
+// waits for its operands while the other issues: one lane for both spent 2600 of a
+// tile's 2048 cycles of products, and two without turns fell into step, both
+// softmaxes at a time and then all products.
 template <bool kBf16, bool kPair>
-__device__ void product_role(const Cta& c, uint32_t tmem) {
+__device__ void product_role(const Cta& c, uint32_t tmem, int t) {
   using S = Shape<kPair>;
   constexpr uint32_t kQk = umma_idesc_f16(kTile, kTile, kBf16);
   constexpr uint32_t kPv = kQk | 1u << 16;  // V: channels, not slots, are contiguous
@@ -704,101 +704,105 @@ __device__ void product_role(const Cta& c, uint32_t tmem) {
     at = at + 1 == S::kStages ? 0 : at + 1;
     return st;
   };
-  // phases, a bit for each stage, tile of rows or buffer
-  uint32_t v_phase = 0, q_phase = 0, o_phase = 3, p_phase = 0;
-  auto turn = [](uint32_t& phases, int i) {
-    const uint32_t phase = (phases >> i) & 1;
-    phases ^= 1u << i;
-    return phase;
+  uint32_t v_phase = 0, q_phase = 0, o_phase = 1;  // (v_phase: a bit for each of the ring)
+  int done = 0;                                    // tiles with products
+  uint32_t turn = t ^ 1;
+  // A lane's turn to issue.
+  auto begin = [&] {
+    const bool ok = !kPair || c.wait(c.m->turn[t], turn);
+    turn ^= 1;
+    return ok;
   };
-  // the product with V of buffer b's probabilities into output t
-  auto add = [&](int t, int b, int v, int j) {
-    if (j == 0 && !c.wait(c.m->oempty[t], turn(o_phase, t))) return false;
-    const uint32_t phase = turn(p_phase, b);
-    if (!c.wait(c.m->pready[b][0], phase)) return false;
-    tc_fence_after();
-    output(t, b, v, j > 0, 0, kTile / 32);
-    if (!c.wait(c.m->pready[b][1], phase)) return false;
-    tc_fence_after();
-    output(t, b, v, j > 0, kTile / 32, kTile / 16);
-    return true;
+  auto end = [&] {
+    if (kPair) mbar_arrive(bar(c.m->turn[t ^ 1]));
   };
+  auto drop = [&](int st) { mbar_arrive(bar(c.m->empty[st])); };  // a stage that this tile's rows do not need
   bool ok = true;
-  int next = 0;  // single: buffer of the next logits
   for (int piece = 0; ok; ++piece) {
     if (!(ok = c.wait(c.m->pfull[piece % kRing], (piece / kRing) & 1))) break;
     const Piece& x = c.m->ring[piece % kRing];
     if (!x.go) break;
-    const int n0 = x.tiles[0], n1 = kPair ? x.tiles[1] : 0;
+    const int n = x.tiles[t], tiles = kPair ? max(n, x.tiles[t ^ 1]) : n;
     const int in_part = limit_of(c.p, x.pos0, x.length) / kTile - x.tile0;  // first tile that not all rows see whole
     mbar_arrive(bar(c.m->pempty[piece % kRing]));
-    const int tiles = max(n0, n1);
     if (!(ok = c.wait(c.m->kfull[piece % kRing], (piece / kRing) & 1))) break;
     const int k0 = step();
-#pragma unroll
-    for (int t = 0; t < S::kQTiles; ++t) {
-      const int n = t ? n1 : n0;
-      if (!ok || !n) continue;
-      ok = c.wait(c.m->qfull[t], turn(q_phase, t));
-      const int buffer = kPair ? t : next;
-      next ^= 1;
-      if (ok) {
-        tc_fence_after();
-        logits(t, buffer, k0);
-        umma_commit(bar(c.m->sfull[buffer]));
-        if (n == 1) umma_commit(bar(c.m->qempty[t]));
-      }
+    if (n) {
+      ok = c.wait(c.m->qfull[t], q_phase) && begin();
+      q_phase ^= 1;
+      if (!ok) break;
+      const int buffer = kPair ? t : done & 1;
+      tc_fence_after();
+      logits(t, buffer, k0);
+      end();
+      umma_commit(bar(c.m->sfull[buffer]));
+      umma_commit(bar(c.m->empty[k0]));
+      if (n == 1) umma_commit(bar(c.m->qempty[t]));
+    } else {
+      if (!(ok = begin())) break;
+      end();
+      drop(k0);
     }
-    if (!ok) break;
-    umma_commit(bar(c.m->empty[k0]));
     if (c.p.stall_ns && blockIdx.x == 0) {  // test hook: a wait for what nothing completes
-      wait_on(bar(c.m->drain), 0, &c.m->abort, c.p.status, c.p.stopped, c.p.stall_ns);
+      wait_on(bar(c.m->drain[t]), 0, &c.m->abort, c.p.status, c.p.stopped, c.p.stall_ns);
       break;
     }
 #pragma unroll 1
     for (int j = 0; ok && j < tiles; ++j) {
       const bool more = j + 1 < tiles;
       const int k = more ? step() : 0, v = step(), slot = count % kRing;
-      ok = c.wait(c.m->full[slot], (count / kRing) & 1) &&
-           (j < in_part || c.wait(c.m->vready[slot], turn(v_phase, slot)));
-      if (!ok) break;
+      ok = c.wait(c.m->full[slot], (count / kRing) & 1);
       ++count;
-      if (kPair) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int n = t ? n1 : n0;
-          if (ok && j < n && (ok = add(t, t, v, j))) {
-            if (t == 1 || j >= n1) umma_commit(bar(c.m->empty[v]));
-            if (j + 1 < n) {
-              logits(t, t, k);
-              umma_commit(bar(c.m->sfull[t]));
-              if (j + 2 == n) umma_commit(bar(c.m->qempty[t]));
-            } else {
-              umma_commit(bar(c.m->odone[t]));
-            }
-          }
-        }
-        if (ok && more) umma_commit(bar(c.m->empty[k]));
-      } else {
-        if (more) {
-          tc_fence_after();
-          logits(0, next, k);
-          umma_commit(bar(c.m->sfull[next]));
-          umma_commit(bar(c.m->empty[k]));
-          if (j + 2 == tiles) umma_commit(bar(c.m->qempty[0]));
-          next ^= 1;
-        }
-        // (the buffer that holds this tile's: next, if the other one's logits are under way)
-        if (!(ok = add(0, more ? next : next ^ 1, v, j))) break;
-        umma_commit(bar(c.m->odone[0]));
+      if (ok && j >= in_part) {
+        ok = c.wait(c.m->vready[slot], (v_phase >> slot) & 1);
+        v_phase ^= 1u << slot;
+      }
+      if (!ok) break;
+      if (j >= n) {
+        if (!(ok = begin())) break;
+        end();
+        drop(v);
+        if (more) drop(k);
+        continue;
+      }
+      const int buffer = kPair ? t : done & 1, phase = (kPair ? done : done >> 1) & 1;
+      ++done;
+      if (!kPair && more) {  // the next tile's logits beside this one's softmax
+        tc_fence_after();
+        logits(0, buffer ^ 1, k);
+        umma_commit(bar(c.m->sfull[buffer ^ 1]));
+        umma_commit(bar(c.m->empty[k]));
+        if (j + 2 == n) umma_commit(bar(c.m->qempty[0]));
+      }
+      if (j == 0) {
+        ok = c.wait(c.m->oempty[t], o_phase);
+        o_phase ^= 1;
+      }
+      if (!(ok = ok && c.wait(c.m->pready[buffer][0], phase) && begin())) break;
+      tc_fence_after();
+      output(t, buffer, v, j > 0, 0, kTile / 32);
+      if (!(ok = c.wait(c.m->pready[buffer][1], phase))) break;
+      tc_fence_after();
+      output(t, buffer, v, true, kTile / 32, kTile / 16);
+      if (kPair && j + 1 < n) {
+        logits(t, t, k);
+        end();
+        umma_commit(bar(c.m->sfull[t]));
         umma_commit(bar(c.m->empty[v]));
+        umma_commit(bar(c.m->empty[k]));
+        if (j + 2 == n) umma_commit(bar(c.m->qempty[t]));
+      } else {
+        end();
+        umma_commit(bar(c.m->odone[t]));
+        umma_commit(bar(c.m->empty[v]));
+        if (kPair && more) drop(k);
       }
     }
   }
   // every product, and every arrival that waits for one, is over before the
   // tensor memory is given back
-  umma_commit(bar(c.m->drain));
-  settle(c.m->drain, 0, 1000000000ull);
+  umma_commit(bar(c.m->drain[t]));
+  settle(c.m->drain[t], 0, 1000000000ull);
 }
 
 // ---------------------------------------------------------------- V of tiles that rows see in part
@@ -806,9 +810,9 @@ __device__ void product_role(const Cta& c, uint32_t tmem) {
 // the item's first token does not see whole, rows of slots behind the length
 // become zero, and what is not finite in slots that other tokens see: those slots
 // are noted, and the rows that do see them get it added to their output.
-// (Two warps, eight slots at a time each.  x times 0 is 0, or NaN where x is not
+// (Eight slots at a time.  x times 0 is 0, or NaN where x is not
 // finite: a multiply-add a pair of channels finds the few that need a closer look.
-// One warp that looked at each exponent took up to 8700 cycles a tile.)
+// Looking at each exponent took up to 8700 cycles a tile.)
 template <bool kBf16>
 __device__ __forceinline__ uint32_t add_zeros(uint32_t x, uint32_t sum) {
   if (kBf16)
@@ -819,7 +823,7 @@ __device__ __forceinline__ uint32_t add_zeros(uint32_t x, uint32_t sum) {
 }
 
 template <bool kBf16, bool kPair>
-__device__ void fix_role(const Cta& c, int part) {
+__device__ void fix_role(const Cta& c) {
   using S = Shape<kPair>;
   const PagedAttendParams& p = c.p;
   const int lane = threadIdx.x & 31;
@@ -827,17 +831,15 @@ __device__ void fix_role(const Cta& c, int part) {
   Reader reader{c};
   int pos = 0, count = 0;
   while (const Piece* x = reader.next()) {
-    uint32_t* found = c.m->found[reader.at % kRing];
+    uint32_t& found = c.m->found[reader.at % kRing];
     uint32_t(*poison)[4] = c.m->poison[reader.at % kRing];
-    // (this warp's bits: those of slots 8 part .. 8 part + 7 of each 16)
-    const uint32_t mine = part ? 0xff00ff00u : 0x00ff00ffu;
-    if (lane < 4 * kDiagTiles) atomicAnd(&poison[lane >> 2][lane & 3], ~mine);
-    if (lane == 0) found[part] = 0;
+    if (lane < 4 * kDiagTiles) poison[lane >> 2][lane & 3] = 0;
+    if (lane == 0) found = 0;
     __syncwarp();
     const int tiles = max(x->tiles[0], x->tiles[1]), tile0 = x->tile0, length = x->length;
     const int whole = limit_of(p, x->pos0, length);  // slots that all rows see
     bool ok = true;
-    auto pass = [&](int at) {  // a stage is not free before these warps are past it
+    auto pass = [&](int at) {  // a stage is not free before this warp is past it
       if (lane == 0) mbar_arrive(smem_u32(&c.m->empty[at % S::kStages]));
     };
     for (int j = 0; j < tiles; ++j, ++count) {
@@ -851,7 +853,7 @@ __device__ void fix_role(const Cta& c, int part) {
         char* v = reinterpret_cast<char*>(c.m) - kOperandBytes + (S::kQTiles + st) * kTileBytes2;
         const int diag = tile0 + j - whole / kTile;
         // 16 pieces of 16 bytes a slot
-        for (int i = (max(whole - base, 0) & ~15) + 8 * part; i < kTile; i += 16) {
+        for (int i = max(whole - base, 0) & ~7; i < kTile; i += 8) {
           uint4* at = reinterpret_cast<uint4*>(v + ((lane >> 3) & 1) * kHalf + (i + (lane >> 4)) * 128) + (lane & 7);
           const int slot = base + i + (lane >> 4);
           uint32_t sum = 0;
@@ -883,7 +885,7 @@ __device__ void fix_role(const Cta& c, int part) {
             }
             if (any && diag < kDiagTiles) {
               atomicOr(&poison[diag][(s - base) >> 5], 1u << ((s - base) & 31));
-              found[part] = 1;
+              found = 1;
             }
           }
         }
@@ -1194,8 +1196,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     if (lane == 0) mbar_arrive(smem_u32(&c.m->oempty[tile]));
     const Piece y = *x;
     const int whole = limit_of(p, pos0, length);
-    const uint32_t* found = c.m->found[reader.at % kRing];
-    if (found[0] | found[1])
+    if (c.m->found[reader.at % kRing])
     for (int d = 0; d < kDiagTiles; ++d)
       for (int k = 0; k < 4; ++k) {
         uint32_t bits = c.m->poison[reader.at % kRing][d][k];
@@ -1258,7 +1259,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(smem_u32(&m->empty[i]), 3);
+      mbar_init(smem_u32(&m->empty[i]), 1 + S::kQTiles);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&m->qfull[i]), 1);
@@ -1272,11 +1273,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&m->kfull[i]), 1);
       mbar_init(smem_u32(&m->full[i]), 1);
-      mbar_init(smem_u32(&m->vready[i]), 2);
+      mbar_init(smem_u32(&m->vready[i]), 1);
       mbar_init(smem_u32(&m->pfull[i]), 1);
       mbar_init(smem_u32(&m->pempty[i]), S::kConsumers);
     }
-    mbar_init(smem_u32(&m->drain), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&m->drain[i]), 1);
+      mbar_init(smem_u32(&m->turn[i]), 1);
+    }
     m->abort = 0;
     fence_mbar_init();
   }
@@ -1308,10 +1312,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
     if (go) {
       if (warp == kLoadWarp)
         load_role<kPair>(c);
-      else if (warp != kMmaWarp)
-        fix_role<kBf16, kPair>(c, warp - kFixWarp);
-      else if (elect_one())
-        product_role<kBf16, kPair>(c, tmem);
+      else if (warp == kFixWarp)
+        fix_role<kBf16, kPair>(c);
+      else if ((kPair || warp == kMmaWarp) && elect_one())
+        product_role<kBf16, kPair>(c, tmem, warp != kMmaWarp);
     }
   }
   __syncwarp();
