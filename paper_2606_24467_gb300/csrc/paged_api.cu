@@ -337,6 +337,7 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
   P.item_tokens = P.pair ? 2 * P.tile_tokens : P.tile_tokens;
   const int box_tokens = std::min(P.tile_tokens, most);
   P.q_box_bytes = box_tokens * P.group * 64 * 2;
+  P.q_buffers = box_tokens * P.group <= 32 ? 4 : box_tokens * P.group <= 64 ? 2 : 1;
   {
     const unsigned long long dims[2] = {static_cast<unsigned long long>(a->num_q_heads),
                                         static_cast<unsigned long long>(P.rows)};

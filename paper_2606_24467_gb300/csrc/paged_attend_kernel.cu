@@ -71,7 +71,7 @@ struct Shape {
 struct Misc {
   // a piece's first K; V of a tile with K of the next; stages free again; V fixed
   uint64_t kfull[kRing], full[kRing], empty[6], vready[kRing];
-  uint64_t qfull[2], qempty[2], sfull[2], pready[2][2], odone[2], oempty[2];
+  uint64_t qfull[4], qempty[4], sfull[2], pready[2][2], odone[2], oempty[2];
   uint64_t pfull[kRing], pempty[kRing], drain[2], turn[2];
   Piece ring[kRing];
   uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite,
@@ -577,7 +577,10 @@ __device__ void load_role(const Cta& c) {
   Finder<kPair> f{p, lane};
   f.start();
   int pos = 0, pieces = 0, count = 0;  // stages filled; pieces and tiles begun
-  int q_count[2] = {0, 0};
+  // kPair: a Q buffer for each tile of rows; single: as many, for pieces to come, as
+  // their rows leave room for (a tile's rows behind them are whatever lies there)
+  const int q_step = kPair ? kTileBytes2 : kHalf / p.q_buffers;
+  uint32_t q_used = 0, q_phase = 0;  // a bit for each buffer
   // this lane's page of a tile (not yet checked)
   auto look_up = [&](const Piece& x, int tile) {
     const int slot = tile * kTile + (lane >> 1) * box;
@@ -606,17 +609,18 @@ __device__ void load_role(const Cta& c) {
     }
     return true;
   };
-  auto load_q = [&](const Piece& x, int t) {
-    if (!c.wait_warp(c.m->qempty[t], (q_count[t] & 1) ^ 1)) return false;
+  auto load_q = [&](const Piece& x, int t, int buffer) {
+    if (!c.wait_warp(c.m->qempty[buffer], ((q_phase >> buffer) & 1) ^ 1)) return false;
     if (lane == 0) {
-      const uint32_t bar = smem_u32(&c.m->qfull[t]);
+      const uint32_t bar = smem_u32(&c.m->qfull[buffer]);
       mbar_arrive_expect_tx(bar, p.q_box_bytes * 2);
       for (int half = 0; half < 2; ++half)
-        tma_load_3d(c.smem + t * kTileBytes2 + half * kHalf, &p.map_q, bar, half * 64, x.head * p.group,
+        tma_load_3d(c.smem + buffer * q_step + half * kHalf, &p.map_q, bar, half * 64, x.head * p.group,
                     x.row0 + t * p.tile_tokens, f.policy);
     }
     __syncwarp();
-    ++q_count[t];
+    q_used |= 1u << buffer;
+    q_phase ^= 1u << buffer;
     return true;
   };
   bool ok = true;
@@ -633,7 +637,7 @@ __device__ void load_role(const Cta& c) {
     ok = load_tile(x, p.map_k, first, now, c.m->kfull[n % kRing], kTileBytes2);
     pieces += ok;
     for (int t = 0; ok && t < S::kQTiles; ++t)
-      if (x.tiles[t]) ok = load_q(x, t);
+      if (x.tiles[t]) ok = load_q(x, t, kPair ? t : n % p.q_buffers);
     for (int j = 0; ok && j < tiles; ++j) {
       const int after = j + 2 < tiles ? look_up(x, first + j + 2) : 0;
       const bool more = j + 1 < tiles;
@@ -660,12 +664,12 @@ __device__ void load_role(const Cta& c) {
     for (int i = max(count - kRing, 0); i < count; ++i)
       settle(c.m->full[i % kRing], (i / kRing) & 1, 100000000ull);
   }
-  for (int t = 0; t < S::kQTiles; ++t)
-    if (q_count[t]) {
+  for (int i = 0; i < kRing; ++i)
+    if ((q_used >> i) & 1) {
       if (all)
-        c.wait_warp(c.m->qempty[t], (q_count[t] - 1) & 1);
+        c.wait_warp(c.m->qempty[i], ((q_phase >> i) & 1) ^ 1);
       else
-        settle(c.m->qfull[t], (q_count[t] - 1) & 1, 100000000ull);
+        settle(c.m->qfull[i], ((q_phase >> i) & 1) ^ 1, 100000000ull);
     }
 }
 
@@ -683,8 +687,9 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
   constexpr uint32_t kPv = kQk | 1u << 16;  // V: channels, not slots, are contiguous
   const uint32_t stages = c.smem + S::kQTiles * kTileBytes2;
   auto bar = [&](uint64_t& b) { return smem_u32(&b); };
+  const int q_step = kPair ? kTileBytes2 : kHalf / c.p.q_buffers;
   auto logits = [&](int q, int buffer, int st) {
-    const uint64_t a = smem_desc_sw128(c.smem + q * kTileBytes2);
+    const uint64_t a = smem_desc_sw128(c.smem + q * q_step);
     const uint64_t b = smem_desc_sw128(stages + st * kTileBytes2);
 #pragma unroll
     for (int i = 0; i < kHeadDim / 16; ++i) {
@@ -704,7 +709,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
     at = at + 1 == S::kStages ? 0 : at + 1;
     return st;
   };
-  uint32_t v_phase = 0, q_phase = 0, o_phase = 1;  // (v_phase: a bit for each of the ring)
+  uint32_t v_phase = 0, q_phase = 0, o_phase = 1;  // (v_phase, q_phase: a bit for each of the ring)
   int done = 0;                                    // tiles with products
   uint32_t turn = t ^ 1;
   // A lane's turn to issue.
@@ -726,18 +731,18 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
     const int in_part = limit_of(c.p, x.pos0, x.length) / kTile - x.tile0;  // first tile that not all rows see whole
     mbar_arrive(bar(c.m->pempty[piece % kRing]));
     if (!(ok = c.wait(c.m->kfull[piece % kRing], (piece / kRing) & 1))) break;
-    const int k0 = step();
+    const int k0 = step(), q = kPair ? t : piece % c.p.q_buffers;
     if (n) {
-      ok = c.wait(c.m->qfull[t], q_phase) && begin();
-      q_phase ^= 1;
+      ok = c.wait(c.m->qfull[q], (q_phase >> q) & 1) && begin();
+      q_phase ^= 1u << q;
       if (!ok) break;
       const int buffer = kPair ? t : done & 1;
       tc_fence_after();
-      logits(t, buffer, k0);
+      logits(q, buffer, k0);
       end();
       umma_commit(bar(c.m->sfull[buffer]));
       umma_commit(bar(c.m->empty[k0]));
-      if (n == 1) umma_commit(bar(c.m->qempty[t]));
+      if (n == 1) umma_commit(bar(c.m->qempty[q]));
     } else {
       if (!(ok = begin())) break;
       end();
@@ -769,10 +774,10 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
       ++done;
       if (!kPair && more) {  // the next tile's logits beside this one's softmax
         tc_fence_after();
-        logits(0, buffer ^ 1, k);
+        logits(q, buffer ^ 1, k);
         umma_commit(bar(c.m->sfull[buffer ^ 1]));
         umma_commit(bar(c.m->empty[k]));
-        if (j + 2 == n) umma_commit(bar(c.m->qempty[0]));
+        if (j + 2 == n) umma_commit(bar(c.m->qempty[q]));
       }
       if (j == 0) {
         ok = c.wait(c.m->oempty[t], o_phase);
@@ -1262,8 +1267,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
       mbar_init(smem_u32(&m->empty[i]), 1 + S::kQTiles);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&m->qfull[i]), 1);
-      mbar_init(smem_u32(&m->qempty[i]), 1);
       mbar_init(smem_u32(&m->sfull[i]), 1);
       mbar_init(smem_u32(&m->pready[i][0]), 4);
       mbar_init(smem_u32(&m->pready[i][1]), 4);
@@ -1271,6 +1274,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
       mbar_init(smem_u32(&m->oempty[i]), 4);
     }
     for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&m->qfull[i]), 1);
+      mbar_init(smem_u32(&m->qempty[i]), 1);
       mbar_init(smem_u32(&m->kfull[i]), 1);
       mbar_init(smem_u32(&m->full[i]), 1);
       mbar_init(smem_u32(&m->vready[i]), 1);

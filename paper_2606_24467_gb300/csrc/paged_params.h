@@ -96,6 +96,7 @@ struct PagedAttendParams {
   int tile_tokens;             // query tokens of 128 rows
   int item_tokens;             // of an item
   int q_box_bytes;             // of 64 channels of a tile
+  int q_buffers;               // single: Q of 1, 2 or 4 pieces at a time
   // workspace
   int* status;
   int* stopped;
