@@ -65,17 +65,19 @@ template <bool kPair>
 struct Shape {
   static constexpr int kQTiles = kPair ? 2 : 1;
   static constexpr int kStages = kPair ? 5 : 6;
-  static constexpr int kConsumers = kPair ? 11 : 6;  // warps that read a piece
+  static constexpr int kConsumers = kPair ? 11 : 10;  // warps that read a piece
 };
 
 struct Misc {
   // a piece's first K; V of a tile with K of the next; stages free again; V fixed
   uint64_t kfull[kRing], full[kRing], empty[6], vready[kRing];
   uint64_t qfull[4], qempty[4], sfull[2], pready[2][2], odone[2], oempty[2];
+  uint64_t sready[2], oready[2];          // single: a piece's references and sums, and output
   uint64_t pfull[kRing], pempty[kRing], drain[2], turn[2];
   Piece ring[kRing];
   uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite,
   uint32_t found[kRing];                  // and whether there are any
+  float2 sums[2][kTile];
   uint32_t tmem;
   int abort;
 };
@@ -298,6 +300,11 @@ __device__ __forceinline__ long long warp_sum(long long x) {
   return x;
 }
 
+// (64-bit divisions take some hundred instructions, 32-bit ones far fewer)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return (a | b) >> 32 ? a / b : static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
+}
+
 // kPair: a sequence's heads 0 .. whole - 1 have `pieces[0]` pieces each, the others
 // pieces[1] (`shared` of them of items with more than one).
 struct Heads {
@@ -430,8 +437,8 @@ struct Finder {
       all = static_cast<long long>(n) * p.c.num_kv_heads;
       ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), all));
       if (blockIdx.x < ctas) {
-        at = all * blockIdx.x / ctas;
-        end = all * (blockIdx.x + 1) / ctas;
+        at = quotient(all * blockIdx.x, ctas);
+        end = quotient(all * (blockIdx.x + 1), ctas);
       }
       if (group > 0) {
         before = 0;
@@ -515,7 +522,7 @@ struct Finder {
       y.tiles[0] = n;
       y.tiles[1] = 0;
       const long long u0 = first + static_cast<long long>(head) * count;  // the unit's first tile
-      auto owner = [&](long long tile) { return static_cast<int>(((tile + 1) * ctas - 1) / all); };
+      auto owner = [&](long long tile) { return static_cast<int>(quotient((tile + 1) * ctas - 1, all)); };
       y.base = owner(u0);
       y.pieces[0] = y.pieces[1] = owner(u0 + count - 1) - y.base + 1;
       y.size = 0;
@@ -532,29 +539,23 @@ struct Finder {
   }
 };
 
-// The slots of an item's pieces, in order.
-template <bool kPair>
+// kPair: the slots of an item's pieces, in order.
 struct Slots {
   const PagedAttendParams& p;
   const Piece& x;
-  int k = 0, at = 0, f1 = 0;
+  int k = 0, at = 0, f1;
   Sequence s;
   __device__ Slots(const PagedAttendParams& p_, const Piece& x_) : p(p_), x(x_) {
     s.rows = x.rows;
     s.length = x.length;
     s.start = x.start;
-    if (kPair) f1 = blocks_of(p, s, x.size).first(p, s, 1);
+    f1 = blocks_of(p, s, x.size).first(p, s, 1);
   }
-  __device__ int next() {
-    int r;
-    if (kPair) {
-      const Blocks b = blocks_of(p, s, x.size);
-      const int f = k == 0 ? f1 : b.first(p, s, k);
-      r = x.base + at + x.item - f;
-      at += b.items - f;
-    } else {
-      r = k == 0 ? 2 * x.base + 1 : 2 * (x.base + k);
-    }
+  __device__ long long next() {
+    const Blocks b = blocks_of(p, s, x.size);
+    const int f = k == 0 ? f1 : b.first(p, s, k);
+    const int r = x.base + at + x.item - f;
+    at += b.items - f;
     ++k;
     return r;
   }
@@ -574,6 +575,9 @@ __device__ void load_role(const Cta& c) {
   const PagedAttendParams& p = c.p;
   const int lane = threadIdx.x & 31;
   const int page = 1 << p.c.page_shift, box = min(page, kTile), copies = 2 * (kTile / box);
+  // a call that stopped may have left tickets behind: nothing runs until the
+  // workspace is set up again
+  const bool go = *reinterpret_cast<volatile int*>(p.stopped) == 0;
   Finder<kPair> f{p, lane};
   f.start();
   int pos = 0, pieces = 0, count = 0;  // stages filled; pieces and tiles begun
@@ -627,7 +631,7 @@ __device__ void load_role(const Cta& c) {
   for (int n = 0; ok; ++n) {
     if (!c.wait_warp(c.m->pempty[n % kRing], ((n / kRing) & 1) ^ 1)) break;
     Piece& x = c.m->ring[n % kRing];
-    const bool found = f.find(&x);
+    const bool found = go && f.find(&x);
     if (!found && lane == 0) x.go = 0;
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&c.m->pfull[n % kRing]));
@@ -709,7 +713,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
     at = at + 1 == S::kStages ? 0 : at + 1;
     return st;
   };
-  uint32_t v_phase = 0, q_phase = 0, o_phase = 1;  // (v_phase, q_phase: a bit for each of the ring)
+  uint32_t v_phase = 0, q_phase = 0, o_phase = 3;  // bits: of the ring, of Q buffers, of outputs
   int done = 0;                                    // tiles with products
   uint32_t turn = t ^ 1;
   // A lane's turn to issue.
@@ -731,7 +735,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
     const int in_part = limit_of(c.p, x.pos0, x.length) / kTile - x.tile0;  // first tile that not all rows see whole
     mbar_arrive(bar(c.m->pempty[piece % kRing]));
     if (!(ok = c.wait(c.m->kfull[piece % kRing], (piece / kRing) & 1))) break;
-    const int k0 = step(), q = kPair ? t : piece % c.p.q_buffers;
+    const int k0 = step(), q = kPair ? t : piece % c.p.q_buffers, o = kPair ? t : piece & 1;
     if (n) {
       ok = c.wait(c.m->qfull[q], (q_phase >> q) & 1) && begin();
       q_phase ^= 1u << q;
@@ -780,15 +784,15 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
         if (j + 2 == n) umma_commit(bar(c.m->qempty[q]));
       }
       if (j == 0) {
-        ok = c.wait(c.m->oempty[t], o_phase);
-        o_phase ^= 1;
+        ok = c.wait(c.m->oempty[o], (o_phase >> o) & 1);
+        o_phase ^= 1u << o;
       }
       if (!(ok = ok && c.wait(c.m->pready[buffer][0], phase) && begin())) break;
       tc_fence_after();
-      output(t, buffer, v, j > 0, 0, kTile / 32);
+      output(o, buffer, v, j > 0, 0, kTile / 32);
       if (!(ok = c.wait(c.m->pready[buffer][1], phase))) break;
       tc_fence_after();
-      output(t, buffer, v, true, kTile / 32, kTile / 16);
+      output(o, buffer, v, true, kTile / 32, kTile / 16);
       if (kPair && j + 1 < n) {
         logits(t, t, k);
         end();
@@ -799,6 +803,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
       } else {
         end();
         umma_commit(bar(c.m->odone[t]));
+        if (!kPair && !more) umma_commit(bar(c.m->oready[o]));
         umma_commit(bar(c.m->empty[v]));
         if (kPair && more) drop(k);
       }
@@ -939,7 +944,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
   const int pieces = x.pieces[tile];
   float top = -INFINITY, sum = 0.f;
   {
-    Slots<true> slots(p, x);
+    Slots slots(p, x);
     for (int k = 0; k < pieces; ++k) {
       const float2 ml = __ldcg(p.part_ml + static_cast<long long>(slots.next()) * p.part_rows + row);
       if (ml.y != 0.f) top = fmaxf(top, ml.x);
@@ -947,7 +952,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
   }
 #pragma unroll
   for (int i = 0; i < 128; ++i) o[i / 32][i % 32] = 0;
-  Slots<true> slots(p, x);
+  Slots slots(p, x);
   for (int k = 0; k < pieces; ++k) {
     const long long slot = slots.next();
     const float2 ml = __ldcg(p.part_ml + slot * p.part_rows + row);
@@ -957,12 +962,12 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
     const float4* from = reinterpret_cast<const float4*>(p.part_o) + slot * p.part_rows * 32 + row;
     if (w != 0.f) {
 #pragma unroll
-      for (int i0 = 0; i0 < 32; i0 += 8) {
-        float4 v[8];
+      for (int i0 = 0; i0 < 32; i0 += 16) {
+        float4 v[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __ldcg(from + (i0 + i) * p.part_rows);
+        for (int i = 0; i < 16; ++i) v[i] = __ldcg(from + (i0 + i) * p.part_rows);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 16; ++i) {
           const int at = 4 * (i0 + i);
           uint32_t* to = &o[at / 32][at % 32];
           to[0] = __float_as_uint(fmaf(w, v[i].x, __uint_as_float(to[0])));
@@ -976,104 +981,90 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
   if (valid) write_row<kBf16>(p, x.row0 + token, head, top, sum, o);
 }
 
+// Single: few rows and many pieces: a row by the warp.  Memory answers slowly here,
+// at the end and beside everyone's loads: four rows and four pieces at a time are
+// under way, and references and sums are read once where a lane holds them.
 template <bool kBf16>
-__device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int tile, int row0, unsigned valid) {
-  const int lane = threadIdx.x & 31, pieces = x.pieces[tile];
+__device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int row0, unsigned valid) {
+  const int lane = threadIdx.x & 31, pieces = x.pieces[0];
+  auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * x.base + 1 : 2 * (x.base + k)); };
   while (valid) {
     int row[4];
     bool have[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       have[i] = valid != 0;
-      row[i] = valid ? __ffs(valid) - 1 : row[0];
+      row[i] = row0 + (valid ? __ffs(valid) - 1 : row[0] - row0);
       valid &= valid - 1;
     }
+    float2 ml[4];  // of piece k0 + lane
+    auto read = [&](int k0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        ml[i] = k0 + lane < pieces ? __ldcg(p.part_ml + slot(k0 + lane) * p.part_rows + row[i]) : make_float2(0.f, 0.f);
+    };
     float top[4], sum[4] = {};
 #pragma unroll
     for (int i = 0; i < 4; ++i) top[i] = -INFINITY;
-    {
-      Slots<false> slots(p, x);
-      for (int k0 = 0; k0 < pieces; k0 += 32) {
-        int mine = -1;
-        for (int k = 0; k < min(32, pieces - k0); ++k) {
-          const int s = slots.next();
-          if (k == lane) mine = s;
-        }
+    for (int k0 = 0; k0 < pieces; k0 += 32) {
+      read(k0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float2 ml = make_float2(-INFINITY, 0.f);
-          if (mine >= 0) ml = __ldcg(p.part_ml + static_cast<long long>(mine) * p.part_rows + row0 + row[i]);
-          float t = ml.y == 0.f ? -INFINITY : ml.x;
+      for (int i = 0; i < 4; ++i) {
+        float t = ml[i].y == 0.f ? -INFINITY : ml[i].x;
 #pragma unroll
-          for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-          top[i] = fmaxf(top[i], t);
-        }
+        for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+        top[i] = fmaxf(top[i], t);
       }
     }
     float4 acc[4] = {};
-    {
-      Slots<false> slots(p, x);
-      for (int k0 = 0; k0 < pieces; k0 += 32) {
-        const int count = min(32, pieces - k0);
-        int mine = -1;
-        for (int k = 0; k < count; ++k) {
-          const int s = slots.next();
-          if (k == lane) mine = s;
-        }
-        float w[4];
+    for (int k0 = 0; k0 < pieces; k0 += 32) {
+      const int count = min(32, pieces - k0);
+      if (pieces > 32) read(k0);
+      float w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float2 ml = make_float2(-INFINITY, 0.f);
-          if (mine >= 0) ml = __ldcg(p.part_ml + static_cast<long long>(mine) * p.part_rows + row0 + row[i]);
-          // (equal infinities: 1, so that they and NaN go on into the sum)
-          w[i] = ml.y == 0.f ? 0.f : ml.x == top[i] ? 1.f : exp2f(ml.x - top[i]);
-          float l = ml.y == 0.f ? 0.f : ml.y * w[i];
+      for (int i = 0; i < 4; ++i) {
+        w[i] = ml[i].y == 0.f ? 0.f : ml[i].x == top[i] ? 1.f : exp2f(ml[i].x - top[i]);  // (as in join_rows)
+        float l = ml[i].y == 0.f ? 0.f : ml[i].y * w[i];
 #pragma unroll
-          for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-          sum[i] += l;
-        }
-        for (int k = 0; k < count; k += 4) {
-          float4 v[4][4];
-          float f[4][4];
+        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        sum[i] += l;
+      }
+      for (int k = 0; k < count; k += 4) {
+        float4 v[4][4];
+        float f[4][4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int from = min(k + u, 31);
-            const int s = __shfl_sync(0xffffffffu, mine, from);
+        for (int u = 0; u < 4; ++u) {
+          const int from = min(k + u, 31);
+          const float4* o = reinterpret_cast<const float4*>(p.part_o) + slot(k0 + from) * p.part_rows * 32 + lane;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              f[u][i] = __shfl_sync(0xffffffffu, w[i], from);
-              if (k + u >= count) f[u][i] = 0.f;
-              v[u][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (f[u][i] != 0.f)
-                v[u][i] = __ldcg(reinterpret_cast<const float4*>(
-                                     p.part_o + (static_cast<long long>(s) * p.part_rows + row0 + row[i]) * kHeadDim) +
-                                 lane);
-            }
+          for (int i = 0; i < 4; ++i) {
+            f[u][i] = __shfl_sync(0xffffffffu, w[i], from);
+            if (k + u >= count) f[u][i] = 0.f;
+            v[u][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (f[u][i] != 0.f) v[u][i] = __ldcg(o + row[i] * 32);
           }
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[i].x = fmaf(f[u][i], v[u][i].x, acc[i].x);
-              acc[i].y = fmaf(f[u][i], v[u][i].y, acc[i].y);
-              acc[i].z = fmaf(f[u][i], v[u][i].z, acc[i].z);
-              acc[i].w = fmaf(f[u][i], v[u][i].w, acc[i].w);
-            }
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[i].x = fmaf(f[u][i], v[u][i].x, acc[i].x);
+            acc[i].y = fmaf(f[u][i], v[u][i].y, acc[i].y);
+            acc[i].z = fmaf(f[u][i], v[u][i].z, acc[i].z);
+            acc[i].w = fmaf(f[u][i], v[u][i].w, acc[i].w);
+          }
       }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (!have[i]) continue;
-      const int r = (row0 + row[i]) % kTile, token = tile * p.tile_tokens + r / p.group;
-      const int head = x.head * p.group + r % p.group;
-      const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+      const int token = row[i] / p.group, head = x.head * p.group + row[i] - token * p.group;
       const bool none = sum[i] == 0.f;
-      uint2 o;
-      o.x = none ? 0u : pack<kBf16>(acc[i].x * inv, acc[i].y * inv);
-      o.y = none ? 0u : pack<kBf16>(acc[i].z * inv, acc[i].w * inv);
+      const float inv = 1.f / sum[i];
       const long long row_at = x.row0 + token;
-      reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] = o;
+      reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] =
+          none ? make_uint2(0u, 0u)
+               : make_uint2(pack<kBf16>(acc[i].x * inv, acc[i].y * inv), pack<kBf16>(acc[i].z * inv, acc[i].w * inv));
       if (p.lse && lane == 0)
         p.lse[static_cast<long long>(head) * p.rows + row_at] =
             none ? -INFINITY : (top[i] + log2f(sum[i])) * 0.6931471805599453f;
@@ -1081,33 +1072,116 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
   }
 }
 
+// A lane's row of a piece.
+struct Row {
+  int in_tile, token, head, limit;  // row of the tile; token of the item; query head; slots that it sees
+  bool valid;
+  unsigned rows;                    // of the warp that are
+  __device__ __forceinline__ Row(const PagedAttendParams& p, const Piece& x, int tile, int warp, int lane) {
+    in_tile = warp * 32 + lane;
+    const int at = in_tile / p.group;
+    token = tile * p.tile_tokens + at;
+    head = x.head * p.group + in_tile - at * p.group;
+    valid = at < p.tile_tokens && token < x.tokens;
+    limit = valid ? limit_of(p, x.pos0 + token, x.length) : 0x7fffffff;
+    rows = __ballot_sync(0xffffffffu, valid);
+  }
+};
+
+// The output of a piece's rows (of reference `ref` and sum `l`), from tensor memory
+// to where it goes.
+template <bool kBf16, bool kPair>
+__device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece& x, int tile, uint32_t o_addr,
+                                       uint64_t& oempty, const Row& row, float ref, float l) {
+  const PagedAttendParams& p = c.p;
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  uint32_t o[4][32];
+  tc_fence_after();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) tmem_load32_async(o_addr + 32 * k, o[k]);
+  tmem_wait_ld(o[0]);
+#pragma unroll
+  for (int k = 1; k < 4; ++k) tmem_order_after_wait(o[k]);
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(smem_u32(&oempty));
+  if (c.m->found[reader.at % kRing]) {
+    const int whole = limit_of(p, x.pos0, x.length);
+#pragma unroll 1
+    for (int d = 0; d < 4 * kDiagTiles; ++d)
+      for (uint32_t bits = c.m->poison[reader.at % kRing][d / 4][d % 4]; bits; bits &= bits - 1) {
+        const int slot = whole / kTile * kTile + 32 * d + __ffs(bits) - 1;
+        if (slot >= row.limit || !row.valid) continue;
+        const int page = p.c.table[x.seq * p.c.table_stride + (slot >> p.c.page_shift)];
+        if (page < 0 || page >= p.c.num_pages) continue;
+        const uint16_t* v = p.c.pages[1] + page * p.c.page_stride +
+                            (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + x.head * p.c.head_stride;
+#pragma unroll
+        for (int i = 0; i < 128; ++i) {
+          const float f = value<kBf16>(v[i]);
+          if (!(fabsf(f) < INFINITY)) o[i / 32][i % 32] = __float_as_uint(__uint_as_float(o[i / 32][i % 32]) + f);
+        }
+      }
+  }
+  const Piece y = x;
+  reader.done();
+  if (!row.rows) return;
+  if (y.pieces[tile] == 1) {
+    if (row.valid) write_row<kBf16>(p, y.row0 + row.token, row.head, ref, l, o);
+    return;
+  }
+  const int at = tile * kTile + row.in_tile;
+  if (row.valid) {
+    const long long slot = static_cast<long long>(y.slot) * p.part_rows;
+    p.part_ml[slot + at] = make_float2(ref, l);
+    float4* to = reinterpret_cast<float4*>(p.part_o) + slot * 32 + (kPair ? at : at * 32);
+    const int step = kPair ? p.part_rows : 1;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      to[i * step] =
+          make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
+                      __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
+  }
+  __threadfence();
+  __syncwarp();
+  int* ticket = p.tickets + (y.ticket * 2 + tile) * 4 + warp;
+  int before = 0;
+  if (lane == 0) before = atomicAdd(ticket, 1);
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (before == y.pieces[tile] - 1) {
+    __threadfence();
+    if (lane == 0) *ticket = 0;
+    if (kPair)
+      join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid, o);
+    else
+      join<kBf16>(p, y, warp * 32, row.rows);
+  }
+}
+
 template <bool kBf16, bool kPair>
 __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
   const PagedAttendParams& p = c.p;
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, r = warp * 32 + lane;
-  const int in_tile = r / p.group;
   const uint32_t lanes = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-  const uint32_t o_addr = lanes + (2 + tile) * kTile;
   const float scale = p.scale_log2;
   Reader reader{c};
-  int count = 0, o_count = 0;  // tiles done; (waits for) products with V
+  int count = 0, o_count = 0;  // tiles and pieces done
   while (const Piece* x = reader.next()) {
     const int n = x->tiles[tile];
     if (n == 0) {
       reader.done();
       continue;
     }
-    const int token = tile * p.tile_tokens + in_tile, tile0 = x->tile0, length = x->length, pos0 = x->pos0;
-    const bool valid = in_tile < p.tile_tokens && token < x->tokens;
-    const unsigned rows = __ballot_sync(0xffffffffu, valid);
-    const int limit = valid ? limit_of(p, pos0 + token, length) : 0x7fffffff;
-    const int least = __reduce_min_sync(0xffffffffu, limit);
+    const Row row(p, *x, tile, warp, lane);
+    const int tile0 = x->tile0, limit = row.limit, least = __reduce_min_sync(0xffffffffu, limit);
+    // (single: two outputs in turns)
+    const uint32_t o_addr = lanes + (2 + (kPair ? tile : reader.at & 1)) * kTile;
     float m = -INFINITY, l = 0.f;
     for (int j = 0; j < n; ++j, ++count) {
       const int buffer = kPair ? tile : count & 1;
       if (!c.wait_here(c.m->sfull[buffer], (kPair ? count : count >> 1) & 1)) return;
       const uint32_t s_addr = lanes + buffer * kTile;
-      if (rows) {
+      if (row.rows) {
         tc_fence_after();
         uint32_t s[4][32];
 #pragma unroll
@@ -1130,7 +1204,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(s[k][i]), __uint_as_float(s[k][i + 1]));
         const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]);
-        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], o_count++ & 1)) return;
+        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], (count - 1) & 1)) return;
         const bool grown = now > m && (m == -INFINITY || (now - m) * scale > kGrowth);
         if (__any_sync(0xffffffffu, grown)) {
           const float f = grown ? ex2_approx((m - now) * scale) : 1.f;
@@ -1181,78 +1255,38 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
         tmem_wait_st();
         tc_fence_before();
       } else {
-        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], o_count++ & 1)) return;
+        if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], (count - 1) & 1)) return;
         if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][0]));
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][1]));
     }
-    // the piece's output
-    if (!c.wait_here(c.m->odone[tile], o_count++ & 1)) return;
-    uint32_t o[4][32];
-    tc_fence_after();
-#pragma unroll
-    for (int k = 0; k < 4; ++k) tmem_load32_async(o_addr + 32 * k, o[k]);
-    tmem_wait_ld(o[0]);
-#pragma unroll
-    for (int k = 1; k < 4; ++k) tmem_order_after_wait(o[k]);
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&c.m->oempty[tile]));
-    const Piece y = *x;
-    const int whole = limit_of(p, pos0, length);
-    if (c.m->found[reader.at % kRing])
-    for (int d = 0; d < kDiagTiles; ++d)
-      for (int k = 0; k < 4; ++k) {
-        uint32_t bits = c.m->poison[reader.at % kRing][d][k];
-        for (; bits; bits &= bits - 1) {
-          const int slot = (whole / kTile + d) * kTile + 32 * k + __ffs(bits) - 1;
-          if (slot >= limit || !valid) continue;
-          const int page = p.c.table[y.seq * p.c.table_stride + (slot >> p.c.page_shift)];
-          if (page < 0 || page >= p.c.num_pages) continue;
-          const uint16_t* v = p.c.pages[1] + page * p.c.page_stride +
-                              (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + y.head * p.c.head_stride;
-#pragma unroll
-          for (int i = 0; i < 128; ++i) {
-            const float f = value<kBf16>(v[i]);
-            if (!(fabsf(f) < INFINITY)) o[i / 32][i % 32] = __float_as_uint(__uint_as_float(o[i / 32][i % 32]) + f);
-          }
-        }
-      }
-    reader.done();
-    const float ref = m == -INFINITY ? 0.f : m * scale;
-    const int row0 = tile * kTile + warp * 32;
-    const int head = y.head * p.group + r - in_tile * p.group;
-    if (y.pieces[tile] == 1) {
-      if (valid) write_row<kBf16>(p, y.row0 + token, head, ref, l, o);
-    } else if (rows) {
-      const int row = row0 + lane;
-      if (valid) {
-        const long long at = static_cast<long long>(y.slot) * p.part_rows;
-        p.part_ml[at + row] = make_float2(ref, l);
-        float4* to = reinterpret_cast<float4*>(p.part_o) + at * 32 + (kPair ? row : row * 32);
-        const int step = kPair ? p.part_rows : 1;
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          to[i * step] =
-              make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
-                          __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
-      }
-      __threadfence();
+    if (kPair) {
+      if (!c.wait_here(c.m->odone[tile], o_count++ & 1)) return;
+      finish<kBf16, true>(c, reader, *x, tile, o_addr, c.m->oempty[tile], row, m == -INFINITY ? 0.f : m * scale, l);
+    } else {  // the other warps take it from here
+      const int o = reader.at & 1;
+      if (!c.wait_here(c.m->oempty[o], ((reader.at >> 1) & 1) ^ 1)) return;  // (they have read the one before)
+      c.m->sums[o][r] = make_float2(m == -INFINITY ? 0.f : m * scale, l);
       __syncwarp();
-      int* ticket = p.tickets + (y.ticket * 2 + tile) * 4 + warp;
-      int before = 0;
-      if (lane == 0) before = atomicAdd(ticket, 1);
-      before = __shfl_sync(0xffffffffu, before, 0);
-      if (before == y.pieces[tile] - 1) {
-        __threadfence();
-        if (lane == 0) *ticket = 0;
-        if (kPair)
-          join_rows<kBf16>(p, y, tile, row, token, head, valid, o);
-        else
-          join<kBf16>(p, y, tile, row0, rows);
-      }
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->sready[o]));
+      reader.done();
     }
+  }
+}
+
+// Single: the pieces' outputs, while the softmax goes on with the next piece.
+template <bool kBf16>
+__device__ void output_role(const Cta& c, uint32_t tmem) {
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  Reader reader{c};
+  while (const Piece* x = reader.next()) {
+    const int o = reader.at & 1, phase = (reader.at >> 1) & 1;
+    const Row row(c.p, *x, 0, warp, lane);
+    if (!c.wait_here(c.m->sready[o], phase) || !c.wait_here(c.m->oready[o], phase)) return;
+    const float2 sums = c.m->sums[o][warp * 32 + lane];
+    finish<kBf16, false>(c, reader, *x, 0, tmem + (static_cast<uint32_t>(warp * 32) << 16) + (2 + o) * kTile,
+                         c.m->oempty[o], row, sums.x, sums.y);
   }
 }
 
@@ -1272,6 +1306,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
       mbar_init(smem_u32(&m->pready[i][1]), 4);
       mbar_init(smem_u32(&m->odone[i]), 1);
       mbar_init(smem_u32(&m->oempty[i]), 4);
+      mbar_init(smem_u32(&m->sready[i]), 4);
+      mbar_init(smem_u32(&m->oready[i]), 1);
     }
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&m->qfull[i]), 1);
@@ -1304,24 +1340,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   pdl_wait();
   const uint32_t tmem = m->tmem;
   const Cta c{p, m, smem_u32(smem)};
-  // a call that stopped may have left tickets behind: nothing runs until the
-  // workspace is set up again
-  const bool go = *reinterpret_cast<volatile int*>(p.stopped) == 0;
   if (warp >= kSoftWarp && warp < kSoftWarp + 8) {
     // registers for the softmax, which holds a row of logits (256 x 208 + 128 x 88
     // of the launch's 384 x 168)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    if (go && (kPair || warp < kSoftWarp + 4)) softmax_role<kBf16, kPair>(c, tmem, (warp - kSoftWarp) / 4);
+    if (kPair || warp < kSoftWarp + 4)
+      softmax_role<kBf16, kPair>(c, tmem, (warp - kSoftWarp) / 4);
+    else
+      output_role<kBf16>(c, tmem);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    if (go) {
-      if (warp == kLoadWarp)
-        load_role<kPair>(c);
-      else if (warp == kFixWarp)
-        fix_role<kBf16, kPair>(c);
-      else if ((kPair || warp == kMmaWarp) && elect_one())
-        product_role<kBf16, kPair>(c, tmem, warp != kMmaWarp);
-    }
+    if (warp == kLoadWarp)
+      load_role<kPair>(c);
+    else if (warp == kFixWarp)
+      fix_role<kBf16, kPair>(c);
+    else if ((kPair || warp == kMmaWarp) && elect_one())
+      product_role<kBf16, kPair>(c, tmem, warp != kMmaWarp);
   }
   __syncwarp();
   tc_fence_before();
