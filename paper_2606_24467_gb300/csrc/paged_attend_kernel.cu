@@ -72,7 +72,7 @@ struct Misc {
   // a piece's first K; V of a tile with K of the next; stages free again; V fixed
   uint64_t kfull[kRing], full[kRing], empty[6], vready[kRing];
   uint64_t qfull[4], qempty[4], sfull[2], pready[2][2], odone[2], oempty[2];
-  uint64_t sready[2], oready[2];          // single: a piece's references and sums, and output
+  uint64_t sready[2], oready[2], stored;  // single: a piece's references and sums, output, and output in memory
   uint64_t pfull[kRing], pempty[kRing], drain[2], turn[2];
   Piece ring[kRing];
   uint32_t poison[kRing][kDiagTiles][4];  // slots whose V holds what is not finite,
@@ -981,94 +981,80 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
   if (valid) write_row<kBf16>(p, x.row0 + token, head, top, sum, o);
 }
 
-// Single: few rows and many pieces: a row by the warp.  Memory answers slowly here,
-// at the end and beside everyone's loads: four rows and four pieces at a time are
-// under way, and references and sums are read once where a lane holds them.
+// Counts a piece of an item (whose results this warp has written, or seen written);
+// true for the last one, which finds the others' in memory.
+__device__ __forceinline__ bool take_ticket(int* ticket, int pieces) {
+  int before = 0;
+  if ((threadIdx.x & 31) == 0) before = atomicAdd(ticket, 1);
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (before != pieces - 1) return false;
+  __threadfence();
+  if ((threadIdx.x & 31) == 0) *ticket = 0;
+  return true;
+}
+
+// Single: rows first, first + 4, .. of few, of many pieces: a row by the warp.  (This
+// runs once, from instructions that no cache holds: unrolled over four rows it
+// took 15500 cycles, of which memory's answers are some 3000.)
 template <bool kBf16>
-__device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int row0, unsigned valid) {
+__device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int first, int rows) {
   const int lane = threadIdx.x & 31, pieces = x.pieces[0];
   auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * x.base + 1 : 2 * (x.base + k)); };
-  while (valid) {
-    int row[4];
-    bool have[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      have[i] = valid != 0;
-      row[i] = row0 + (valid ? __ffs(valid) - 1 : row[0] - row0);
-      valid &= valid - 1;
-    }
-    float2 ml[4];  // of piece k0 + lane
-    auto read = [&](int k0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        ml[i] = k0 + lane < pieces ? __ldcg(p.part_ml + slot(k0 + lane) * p.part_rows + row[i]) : make_float2(0.f, 0.f);
+#pragma unroll 1
+  for (int row = first; row < rows; row += 4) {
+    auto read = [&](int k) {
+      return k < pieces ? __ldcg(p.part_ml + slot(k) * p.part_rows + row) : make_float2(0.f, 0.f);
     };
-    float top[4], sum[4] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top[i] = -INFINITY;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 1
     for (int k0 = 0; k0 < pieces; k0 += 32) {
-      read(k0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float t = ml[i].y == 0.f ? -INFINITY : ml[i].x;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-        top[i] = fmaxf(top[i], t);
-      }
+      const float2 ml = read(k0 + lane);
+      if (ml.y != 0.f) top = fmaxf(top, ml.x);
     }
-    float4 acc[4] = {};
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
     for (int k0 = 0; k0 < pieces; k0 += 32) {
+      const float2 ml = read(k0 + lane);
+      const float w = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : exp2f(ml.x - top);  // (as in join_rows)
+      float l = ml.y == 0.f ? 0.f : ml.y * w;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      sum += l;
       const int count = min(32, pieces - k0);
-      if (pieces > 32) read(k0);
-      float w[4];
+#pragma unroll 1
+      for (int k = 0; k < count; k += 8) {
+        float4 v[8];
+        float f[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = ml[i].y == 0.f ? 0.f : ml[i].x == top[i] ? 1.f : exp2f(ml[i].x - top[i]);  // (as in join_rows)
-        float l = ml[i].y == 0.f ? 0.f : ml[i].y * w[i];
-#pragma unroll
-        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        sum[i] += l;
-      }
-      for (int k = 0; k < count; k += 4) {
-        float4 v[4][4];
-        float f[4][4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int from = min(k + u, 31);
-          const float4* o = reinterpret_cast<const float4*>(p.part_o) + slot(k0 + from) * p.part_rows * 32 + lane;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            f[u][i] = __shfl_sync(0xffffffffu, w[i], from);
-            if (k + u >= count) f[u][i] = 0.f;
-            v[u][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (f[u][i] != 0.f) v[u][i] = __ldcg(o + row[i] * 32);
-          }
+        for (int u = 0; u < 8; ++u) {
+          f[u] = __shfl_sync(0xffffffffu, w, (k + u) & 31);
+          v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k + u < count && f[u] != 0.f)
+            v[u] = __ldcg(reinterpret_cast<const float4*>(p.part_o) + (slot(k0 + k + u) * p.part_rows + row) * 32 + lane);
+          else
+            f[u] = 0.f;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[i].x = fmaf(f[u][i], v[u][i].x, acc[i].x);
-            acc[i].y = fmaf(f[u][i], v[u][i].y, acc[i].y);
-            acc[i].z = fmaf(f[u][i], v[u][i].z, acc[i].z);
-            acc[i].w = fmaf(f[u][i], v[u][i].w, acc[i].w);
-          }
+        for (int u = 0; u < 8; ++u) {
+          acc.x = fmaf(f[u], v[u].x, acc.x);
+          acc.y = fmaf(f[u], v[u].y, acc.y);
+          acc.z = fmaf(f[u], v[u].z, acc.z);
+          acc.w = fmaf(f[u], v[u].w, acc.w);
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (!have[i]) continue;
-      const int token = row[i] / p.group, head = x.head * p.group + row[i] - token * p.group;
-      const bool none = sum[i] == 0.f;
-      const float inv = 1.f / sum[i];
-      const long long row_at = x.row0 + token;
-      reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] =
-          none ? make_uint2(0u, 0u)
-               : make_uint2(pack<kBf16>(acc[i].x * inv, acc[i].y * inv), pack<kBf16>(acc[i].z * inv, acc[i].w * inv));
-      if (p.lse && lane == 0)
-        p.lse[static_cast<long long>(head) * p.rows + row_at] =
-            none ? -INFINITY : (top[i] + log2f(sum[i])) * 0.6931471805599453f;
-    }
+    const int token = row / p.group, head = x.head * p.group + row - token * p.group;
+    const bool none = sum == 0.f;
+    const float inv = 1.f / sum;
+    const long long row_at = x.row0 + token;
+    reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] =
+        none ? make_uint2(0u, 0u)
+             : make_uint2(pack<kBf16>(acc.x * inv, acc.y * inv), pack<kBf16>(acc.z * inv, acc.w * inv));
+    if (p.lse && lane == 0)
+      p.lse[static_cast<long long>(head) * p.rows + row_at] =
+          none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
   }
 }
 
@@ -1125,11 +1111,11 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
   }
   const Piece y = x;
   reader.done();
-  if (!row.rows) return;
   if (y.pieces[tile] == 1) {
     if (row.valid) write_row<kBf16>(p, y.row0 + row.token, row.head, ref, l, o);
     return;
   }
+  if (kPair && !row.rows) return;
   const int at = tile * kTile + row.in_tile;
   if (row.valid) {
     const long long slot = static_cast<long long>(y.slot) * p.part_rows;
@@ -1145,16 +1131,8 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
   __threadfence();
   __syncwarp();
   int* ticket = p.tickets + (y.ticket * 2 + tile) * 4 + warp;
-  int before = 0;
-  if (lane == 0) before = atomicAdd(ticket, 1);
-  before = __shfl_sync(0xffffffffu, before, 0);
-  if (before == y.pieces[tile] - 1) {
-    __threadfence();
-    if (lane == 0) *ticket = 0;
-    if (kPair)
-      join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid, o);
-    else
-      join<kBf16>(p, y, warp * 32, row.rows);
+  if (kPair) {
+    if (take_ticket(ticket, y.pieces[tile])) join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid, o);
   }
 }
 
@@ -1279,14 +1257,23 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
 template <bool kBf16>
 __device__ void output_role(const Cta& c, uint32_t tmem) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  uint32_t stored = 0;
   Reader reader{c};
   while (const Piece* x = reader.next()) {
     const int o = reader.at & 1, phase = (reader.at >> 1) & 1;
     const Row row(c.p, *x, 0, warp, lane);
     if (!c.wait_here(c.m->sready[o], phase) || !c.wait_here(c.m->oready[o], phase)) return;
     const float2 sums = c.m->sums[o][warp * 32 + lane];
+    const Piece y = *x;
     finish<kBf16, false>(c, reader, *x, 0, tmem + (static_cast<uint32_t>(warp * 32) << 16) + (2 + o) * kTile,
                          c.m->oempty[o], row, sums.x, sums.y);
+    if (y.pieces[0] > 1) {  // each warp counts the CTA's rows, and joins some of them
+      if (lane == 0) mbar_arrive(smem_u32(&c.m->stored));
+      if (!c.wait_here(c.m->stored, stored)) return;
+      stored ^= 1;
+      __threadfence();
+      if (take_ticket(c.p.tickets + y.ticket * 8 + warp, y.pieces[0])) join<kBf16>(c.p, y, warp, y.tokens * c.p.group);
+    }
   }
 }
 
@@ -1296,50 +1283,52 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   extern __shared__ __align__(1024) unsigned char smem[];
   Misc* m = reinterpret_cast<Misc*>(smem + kOperandBytes);
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(smem_u32(&m->empty[i]), 1 + S::kQTiles);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&m->sfull[i]), 1);
-      mbar_init(smem_u32(&m->pready[i][0]), 4);
-      mbar_init(smem_u32(&m->pready[i][1]), 4);
-      mbar_init(smem_u32(&m->odone[i]), 1);
-      mbar_init(smem_u32(&m->oempty[i]), 4);
-      mbar_init(smem_u32(&m->sready[i]), 4);
-      mbar_init(smem_u32(&m->oready[i]), 1);
-    }
-    for (int i = 0; i < kRing; ++i) {
-      mbar_init(smem_u32(&m->qfull[i]), 1);
-      mbar_init(smem_u32(&m->qempty[i]), 1);
-      mbar_init(smem_u32(&m->kfull[i]), 1);
-      mbar_init(smem_u32(&m->full[i]), 1);
-      mbar_init(smem_u32(&m->vready[i]), 1);
-      mbar_init(smem_u32(&m->pfull[i]), 1);
-      mbar_init(smem_u32(&m->pempty[i]), S::kConsumers);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&m->drain[i]), 1);
-      mbar_init(smem_u32(&m->turn[i]), 1);
-    }
-    m->abort = 0;
-    fence_mbar_init();
-  }
-  if (warp == kMmaWarp) {
-    tmem_alloc(smem_u32(&m->tmem), 512);
-    tmem_relinquish();
-  }
-  if (warp == kLoadWarp && lane == 0) {
-    tma_prefetch_map(&p.map_q);
-    tma_prefetch_map(&p.map_k);
-    tma_prefetch_map(&p.map_v);
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  pdl_wait();
-  const uint32_t tmem = m->tmem;
   const Cta c{p, m, smem_u32(smem)};
+  // The warp that moves tiles sets the barriers up and goes on; the others wait for
+  // them, and for tensor memory.
+  constexpr int kReady = 1;  // named barrier
+  if (warp == kLoadWarp) {
+    if (lane == 0) {
+      for (int i = 0; i < S::kStages; ++i) mbar_init(smem_u32(&m->empty[i]), 1 + S::kQTiles);
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&m->sfull[i]), 1);
+        mbar_init(smem_u32(&m->pready[i][0]), 4);
+        mbar_init(smem_u32(&m->pready[i][1]), 4);
+        mbar_init(smem_u32(&m->odone[i]), 1);
+        mbar_init(smem_u32(&m->oempty[i]), 4);
+        mbar_init(smem_u32(&m->sready[i]), 4);
+        mbar_init(smem_u32(&m->oready[i]), 1);
+        mbar_init(smem_u32(&m->drain[i]), 1);
+        mbar_init(smem_u32(&m->turn[i]), 1);
+      }
+#pragma unroll 1
+      for (int i = 0; i < kRing; ++i) {
+        mbar_init(smem_u32(&m->qfull[i]), 1);
+        mbar_init(smem_u32(&m->qempty[i]), 1);
+        mbar_init(smem_u32(&m->kfull[i]), 1);
+        mbar_init(smem_u32(&m->full[i]), 1);
+        mbar_init(smem_u32(&m->vready[i]), 1);
+        mbar_init(smem_u32(&m->pfull[i]), 1);
+        mbar_init(smem_u32(&m->pempty[i]), S::kConsumers);
+      }
+      mbar_init(smem_u32(&m->stored), 4);
+      m->abort = 0;
+      fence_mbar_init();
+    }
+    __syncwarp();
+    asm volatile("bar.arrive %0, %1;" ::"n"(kReady), "n"(kThreads) : "memory");
+  } else {
+    if (warp == kMmaWarp) {
+      tmem_alloc(smem_u32(&m->tmem), 512);
+      tmem_relinquish();
+      tc_fence_before();
+    }
+    named_bar_sync(kReady, kThreads);
+    tc_fence_after();
+  }
+  pdl_wait();
+  const uint32_t tmem = warp == kLoadWarp ? 0 : m->tmem;
   if (warp >= kSoftWarp && warp < kSoftWarp + 8) {
     // registers for the softmax, which holds a row of logits (256 x 208 + 128 x 88
     // of the launch's 384 x 168)
