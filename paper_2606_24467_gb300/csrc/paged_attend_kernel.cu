@@ -141,6 +141,16 @@ __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&r)
       "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&r)[16]) {  // and waits
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
 // The product of an operand in tensor memory (rows in lanes, two numbers of K to
 // a column) and one in shared memory.
 __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
@@ -1142,6 +1152,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, r = warp * 32 + lane;
   const uint32_t lanes = tmem + (static_cast<uint32_t>(warp * 32) << 16);
   const float scale = p.scale_log2;
+  const uint64_t scale2 = pair_of(scale, scale);
   Reader reader{c};
   int count = 0, o_count = 0;  // tiles and pieces done
   while (const Piece* x = reader.next()) {
@@ -1176,6 +1187,23 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
             for (int i = 0; i < 32; ++i)
               if (32 * k + i >= see) s[k][i] = 0xff800000u;
         }
+        // The first 32 probabilities are made with the old reference while the
+        // largest logit is found, and again in the few cases where that has grown.
+        uint64_t sum[4] = {};
+        auto exponentials = [&](int k, uint32_t (&w)[16], float ref) {
+          const uint64_t ref2 = pair_of(ref, ref);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 e = split_of(
+                fma2(pair_of(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), scale2, ref2));
+            const float a = ex2_approx(e.x), b = ex2_approx(e.y);
+            sum[i & 3] = add2(sum[i & 3], pair_of(a, b));
+            w[i] = pack<kBf16>(a, b);
+          }
+        };
+        uint32_t w[16];
+        float ref = m == -INFINITY ? 0.f : -m * scale;
+        exponentials(0, w, ref);
         float top[4] = {m, m, m, m};
 #pragma unroll
         for (int i = 0; i < 32; i += 2)
@@ -1191,35 +1219,28 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
           if (j > 0) {
             tc_fence_after();
             const uint64_t f2 = pair_of(f, f);
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              uint32_t o[16];
+              tmem_load16(o_addr + 16 * k, o);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t o[32];
-              tmem_load32_async(o_addr + 32 * k, o);
-              tmem_wait_ld(o);
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) {
+              for (int i = 0; i < 16; i += 2) {
                 const float2 y = split_of(mul2(pair_of(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), f2));
                 o[i] = __float_as_uint(y.x);
                 o[i + 1] = __float_as_uint(y.y);
               }
-              tmem_store32(o_addr + 32 * k, o);
+              tmem_store16(o_addr + 16 * k, o);
             }
           }
+          ref = m == -INFINITY ? 0.f : -m * scale;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] = 0;
+          exponentials(0, w, ref);
         }
-        const float ref = m == -INFINITY ? 0.f : m * scale;
-        const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
-        uint64_t sum[4] = {};
+        tmem_store16(s_addr, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float2 e = split_of(
-                fma2(pair_of(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), scale2, ref2));
-            const float a = ex2_approx(e.x), b = ex2_approx(e.y);
-            sum[i & 3] = add2(sum[i & 3], pair_of(a, b));
-            w[i] = pack<kBf16>(a, b);
-          }
+        for (int k = 1; k < 4; ++k) {
+          exponentials(k, w, ref);
           tmem_store16(s_addr + 16 * k, w);
           if (k == 1) {  // the product with the first half of the slots can begin
             tmem_wait_st();
