@@ -363,6 +363,7 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
   const double scale = a->scale > 0.f ? a->scale : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
   P.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
   P.causal = a->causal != 0;
+  P.wide_rows = (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && a->out_token_stride % 16 == 0 && a->out_head_stride % 16 == 0;
   P.is_bf16 = bf16;
   P.status = static_cast<int*>(workspace);
   P.stopped = P.status + 1;

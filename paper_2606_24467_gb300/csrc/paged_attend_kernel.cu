@@ -413,10 +413,34 @@ struct Finder {
       size[1] = min(max(longest / kPagedTailCuts, kPagedBlock), longest);
       body = max(work - ctas * longest / 2, 0LL);
     } else {
+      // as many pieces as make the shortest time, if they were all alike
       body = 0;
-      size[1] = clamp_to(share / kPagedCuts, min(kPagedBlock, longest), longest);
-      const int cuts = (longest + size[1] - 1) / size[1];
-      size[1] = (longest + cuts - 1) / cuts;
+      size[1] = longest;
+      float least = INFINITY;
+#pragma unroll 1
+      for (int k = 1; k <= kPagedCuts; ++k) {
+        const int tiles = (longest + k - 1) / k;
+        if (k > 1 && tiles < kPagedBlock) break;
+        long long n = 0, shared = 0;
+#pragma unroll 1
+        for (int g = 0; g < groups(); ++g) {
+          Sequence x;
+          x.load(p, g * 32 + lane);
+          if (x.rows <= 0) continue;
+          const Blocks b = blocks_of(p, x, tiles);
+          n += b.pieces(p, x);
+          shared += b.shared_pieces(p, x);
+        }
+        __syncwarp();
+        n = warp_sum(n) * heads;
+        if (warp_sum(shared) * heads > kPagedSlots) break;
+        const float rounds = ceilf(static_cast<float>(n) / static_cast<float>(ctas));
+        const float time = rounds * (static_cast<float>(work) / static_cast<float>(n) + kPagedPiece);
+        if (time < least) {
+          least = time;
+          size[1] = tiles;
+        }
+      }
     }
     // as many pieces as there is room for their results
     for (; size[1] < longest; size[1] += max(size[1] / 4, 1)) {
@@ -927,18 +951,27 @@ __device__ __forceinline__ void write_row(const PagedAttendParams& p, long long 
                                           const uint32_t (&o)[4][32]) {
   const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
   const float inv = 1.f / l;
-  uint4* to = reinterpret_cast<uint4*>(p.out + row * p.o_token + head * p.o_head);
+  uint16_t* to = p.out + row * p.o_token + head * p.o_head;
+  // 32 bytes at a time where rows are aligned to that: a warp's rows are far apart,
+  // and each of its stores takes as many steps as it has rows
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    uint32_t w[4];
+  for (int i = 0; i < 8; ++i) {
+    uint32_t w[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int at = 8 * i + 2 * k;
+    for (int k = 0; k < 8; ++k) {
+      const int at = 16 * i + 2 * k;
       w[k] = none ? 0u
                   : pack<kBf16>(__uint_as_float(o[at / 32][at % 32]) * inv,
                                 __uint_as_float(o[at / 32][at % 32 + 1]) * inv);
     }
-    to[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (p.wide_rows) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * i), "r"(w[0]), "r"(w[1]),
+                   "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else {
+      reinterpret_cast<uint4*>(to)[2 * i] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(to)[2 * i + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
   }
   if (p.lse)
     p.lse[static_cast<long long>(head) * p.rows + row] = none ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;

@@ -66,13 +66,15 @@ cudaError_t launch_paged_gather(const PagedGatherParams& p, cudaStream_t s);
 
 constexpr int kPagedTile = 128;  // slots of a K or V tile, and rows of a tile of queries
 constexpr int kPagedMaxCtas = 160;
-// Chunks.  An item (two tiles of rows) of more than a kPagedFew-th of an SM's share
-// of the tiles is cut into blocks of slots of about a kPagedCuts-th of it, but of
-// at least kPagedBlock tiles; else only those at the end are, in kPagedTailCuts.
-// The results of at most kPagedSlots pieces wait to be joined.
+// Chunks.  Where an item (two tiles of rows) is more than a kPagedFew-th of an SM's
+// share of the tiles, all are cut into blocks of slots: into 1 .. kPagedCuts, of at
+// least kPagedBlock tiles, as makes the shortest time if a piece costs as much as
+// kPagedPiece tiles beside its own.  Else only the items at the end are, into
+// kPagedTailCuts.  The results of at most kPagedSlots pieces wait to be joined.
 constexpr int kPagedFew = 2;
-constexpr int kPagedCuts = 2;
-constexpr int kPagedTailCuts = 5;
+constexpr int kPagedCuts = 24;
+constexpr int kPagedPiece = 6;
+constexpr int kPagedTailCuts = 4;
 constexpr int kPagedBlock = 8;
 constexpr int kPagedSlots = 608;
 // Workspace header: status word, the word that says that a call has stopped, the
@@ -93,6 +95,7 @@ struct PagedAttendParams {
   float scale_log2;
   int rows, group, causal, is_bf16;
   int pair;                    // two tiles of rows to an item
+  int wide_rows;               // rows of `out` are aligned to 32 bytes
   int tile_tokens;             // query tokens of 128 rows
   int item_tokens;             // of an item
   int q_box_bytes;             // of 64 channels of a tile
