@@ -933,17 +933,16 @@ class Rope:
                                              float(scale)), "compresskv_rope_init")
 
 
-def _head_rows(t, rows, what, dtype=None):
+def _head_rows(t, rows, what, dtype):
     """(heads, token stride, head stride) of rows [rows, heads, 128]."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != rows or shape[2] != 128 or strides[2] != 1:
-        _invalid(f"{what} must be [rows, heads, 128], head_dim contiguous")
-    if dtype is not None and t.dtype != dtype:
-        _invalid(f"{what} must be {dtype}")
+    if t.dim() != 3:
+        _invalid(f"{what} must be [rows, heads, 128]")
+    n, heads, d = t.shape
+    token, head, one = t.stride()
+    if n != rows or d != 128 or one != 1 or t.dtype != dtype:
+        _invalid(f"{what} must be {dtype} [{rows}, heads, 128], head_dim contiguous")
     # a dimension of one element has a stride that means nothing
-    heads = shape[1]
-    head = strides[1] if heads > 1 else 128
-    return heads, strides[0] if rows > 1 else max(heads, 1) * 128, head
+    return (heads, token if rows > 1 else (heads or 1) * 128, head if heads > 1 else 128)
 
 
 def _rows_i32(t, rows, what):
@@ -956,31 +955,34 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, backwar
     """Rotates ``q`` ``[rows, H_q, 128]`` (and ``k`` ``[rows, H_k, 128]``) by
     ``positions`` (int32 ``[rows]``), in place or into ``q_out`` / ``k_out``;
     ``backward``: by minus the angles (the gradient)."""
-    rows = q.shape[0]
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    if (k is None) != (k_out is None):
-        _invalid("k_out without k")
-    dtype = _q4_dtype(q)
-    hq, qt, qh = _head_rows(q, rows, "q")
-    ho, qot, qoh = _head_rows(q_out, rows, "q_out", q.dtype)
-    hk, kt, kh, kot, koh = 0, 0, 0, 0, 0
-    if k is not None:
-        hk, kt, kh = _head_rows(k, rows, "k", q.dtype)
-        h, kot, koh = _head_rows(k_out, rows, "k_out", q.dtype)
-        if h != hk:
-            _invalid("k_out must have k's shape")
+    rows, dtype = q.shape[0], q.dtype
+    if q_out is None:
+        q_out = q
+    index = q.get_device()
+    hq, qt, qh = _head_rows(q, rows, "q", dtype)
+    ho, qot, qoh = (hq, qt, qh) if q_out is q else _head_rows(q_out, rows, "q_out", dtype)
     if ho != hq:
         _invalid("q_out must have q's shape")
-    _rows_i32(positions, rows, "positions")
-    index = q.get_device()
-    for t in (positions, k, q_out, k_out):
-        if t is not None and t.get_device() != index:
+    hk, kt, kh, kot, koh = 0, 0, 0, 0, 0
+    if k is not None:
+        if k_out is None:
+            k_out = k
+        hk, kt, kh = _head_rows(k, rows, "k", dtype)
+        ho, kot, koh = (hk, kt, kh) if k_out is k else _head_rows(k_out, rows, "k_out", dtype)
+        if ho != hk:
+            _invalid("k_out must have k's shape")
+        if k.get_device() != index or k_out.get_device() != index:
             _invalid("q, k, positions and outputs must be on one device")
-    x = CkvRopeRows(rows, hq, hk, dtype, int(bool(backward)), 0, qt, qh, kt, kh, qot, qoh, kot, koh,
-                    ctypes.pointer(trace.struct) if trace is not None else None)
-    _device_call("compresskv_rope_apply", index, stream, rope.addr, ctypes.addressof(x), _addr(positions),
-                 _addr(q) if hq else None, _addr(k) if hk else None, _addr(q_out) if hq else None,
-                 _addr(k_out) if hk else None)
+    elif k_out is not None:
+        _invalid("k_out without k")
+    _rows_i32(positions, rows, "positions")
+    if q_out.get_device() != index or positions.get_device() != index:
+        _invalid("q, k, positions and outputs must be on one device")
+    x = CkvRopeRows(rows, hq, hk, _q4_dtype(q), 1 if backward else 0, 0, qt, qh, kt, kh, qot, qoh, kot, koh,
+                    None if trace is None else ctypes.pointer(trace.struct))
+    _device_call("compresskv_rope_apply", index, stream, rope.addr, ctypes.addressof(x), positions.data_ptr(),
+                 q.data_ptr() if hq else None, k.data_ptr() if hk else None,
+                 q_out.data_ptr() if hq else None, k_out.data_ptr() if hk else None)
 
 
 # ----------------------------------------------------------------- paged cache
@@ -1073,16 +1075,16 @@ def paged_append(cache: PagedCache, k, v, cu_rows=None, start=None, rope: "Rope 
     default: the slots)."""
     rows = k.shape[0]
     heads, kt, kh = _head_rows(k, rows, "k", cache.dtype)
-    vh = _head_rows(v, rows, "v", cache.dtype)
-    if heads != cache.num_kv_heads or vh != (heads, kt, kh):
+    if heads != cache.num_kv_heads or _head_rows(v, rows, "v", cache.dtype) != (heads, kt, kh):
         _invalid("k and v must be [rows, H_kv, 128] of the same strides")
     hq, qt, qh, qot, qoh = 0, 0, 0, 0, 0
     if q is not None:
         if rope is None:
             _invalid("q needs a rope")
-        q_out = q if q_out is None else q_out
         hq, qt, qh = _head_rows(q, rows, "q", cache.dtype)
-        ho, qot, qoh = _head_rows(q_out, rows, "q_out", cache.dtype)
+        if q_out is None:
+            q_out = q
+        ho, qot, qoh = (hq, qt, qh) if q_out is q else _head_rows(q_out, rows, "q_out", cache.dtype)
         if ho != hq:
             _invalid("q_out must have q's shape")
     elif q_out is not None:

@@ -18,10 +18,12 @@ namespace ckv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBlocks = 4;                      // CTAs of an SM, at least
 constexpr int kWarps = kThreads / 32;
 constexpr int kLanes = 8;                       // lanes of a head
 constexpr int kPairsLane = kRopePairs / kLanes; // 8
-constexpr int kUnroll = 4;                      // heads of a lane in flight
+constexpr int kUnroll = 2;                      // heads of a lane in flight
+constexpr int kFill = 2432;                     // warps that the GPU is to have where there is enough for them
 constexpr int kFewRows = 16;                    // rows of a sequence that one CTA appends
 
 // Where a lane's eight pairs are.
@@ -57,21 +59,32 @@ __device__ __forceinline__ int pair_of(int l, int i) {
   return kLayout == kOddHalves ? l + kLanes * i : kPairsLane * l + i;
 }
 
+// The four lanes that hold the same pairs, of four heads, compute two of their
+// angles each and hand them on (all of them: 31 instead of 24 us for 8191 tokens of
+// 28 and 4 heads).
 template <int kLayout>
-__device__ __forceinline__ void angles_at(const RopeTable& r, int position, bool backward, int l, Angles& a) {
+__device__ __forceinline__ void angles_at(const RopeTable& r, int position, bool backward, int lane, Angles& a) {
+  constexpr int kEach = kPairsLane * kLanes / 32;  // 2
+  const int l = lane % kLanes;
+  float c[kEach], s[kEach];
 #pragma unroll
-  for (int i = 0; i < kPairsLane; ++i) {
-    a.c[i] = 1.f;
-    a.s[i] = 0.f;
-    const int pair = pair_of<kLayout>(l, i);
+  for (int e = 0; e < kEach; ++e) {
+    c[e] = 1.f;
+    s[e] = 0.f;
+    const int pair = pair_of<kLayout>(l, lane / kLanes * kEach + e);
     if (pair < r.pairs) {
       const unsigned long long t = r.turns[pair] * static_cast<unsigned long long>(static_cast<long long>(position));
       const float half_turns = static_cast<float>(static_cast<int>(t >> 32)) * 0x1p-31f;
-      float s, c;
-      sincospif(half_turns, &s, &c);
-      a.c[i] = c * r.scale;
-      a.s[i] = (backward ? -s : s) * r.scale;
+      sincospif(half_turns, &s[e], &c[e]);
+      c[e] *= r.scale;
+      s[e] *= backward ? -r.scale : r.scale;
     }
+  }
+#pragma unroll
+  for (int i = 0; i < kPairsLane; ++i) {
+    const int from = l + kLanes * (i / kEach);
+    a.c[i] = __shfl_sync(0xffffffffu, c[i % kEach], from);
+    a.s[i] = __shfl_sync(0xffffffffu, s[i % kEach], from);
   }
 }
 
@@ -187,13 +200,12 @@ __device__ __forceinline__ void row_heads(const RopeParams& p, int row, int posi
     else if (w == 0 && lane == 0 && p.status)
       atomicCAS(p.status, 0, CKV_DEV_ERR_INDEX);
   }
-  Angles t;
-  angles_at<kLayout>(p.rope, position, p.backward != 0, l, t);
   const int fours = (heads + 3) / 4;
-  for (int f0 = w; f0 < fours; f0 += of * kUnroll) {
-    Piece x[kUnroll];
-    uint16_t* to[kUnroll];
-    bool turned[kUnroll];
+  // (the first rows are on their way while the angles are computed)
+  Piece x[kUnroll];
+  uint16_t* to[kUnroll];
+  bool turned[kUnroll];
+  auto fetch = [&](int f0) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       int h = (f0 + u * of) * 4 + lane / kLanes;
@@ -220,12 +232,20 @@ __device__ __forceinline__ void row_heads(const RopeParams& p, int row, int posi
         if (to[u]) load<kLayout>(from, l, pairs, x[u]);
       }
     }
+  };
+  fetch(w);
+  Angles t;
+  angles_at<kLayout>(p.rope, position, p.backward != 0, lane, t);
+  for (int f0 = w;;) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
       if (to[u]) {
         if (turned[u]) turn<kBf16, kLayout>(t, l, pairs, x[u]);
         store<kLayout>(to[u], l, pairs, x[u]);
       }
+    f0 += of * kUnroll;
+    if (f0 >= fours) break;
+    fetch(f0);
   }
 }
 
@@ -248,7 +268,7 @@ __device__ __forceinline__ void set_length(const RopeParams& p, int seq, int fir
 
 // Warp w of a row's `of` warps.
 template <bool kBf16, int kLayout>
-__global__ void __launch_bounds__(kThreads) rope_rows_kernel(const __grid_constant__ RopeParams p, int of) {
+__global__ void __launch_bounds__(kThreads, kBlocks) rope_rows_kernel(const __grid_constant__ RopeParams p, int of) {
   if (p.paged && !p.start) pdl_launch_dependents();  // the kernel that sets the lengths follows
   pdl_wait();
   const long long task = static_cast<long long>(blockIdx.x) * kWarps + threadIdx.x / 32;
@@ -268,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) rope_rows_kernel(const __grid_consta
 
 // A sequence to a CTA, which reads its length before it writes it.
 template <bool kBf16, int kLayout>
-__global__ void __launch_bounds__(kThreads) append_sequence_kernel(const __grid_constant__ RopeParams p, int of) {
+__global__ void __launch_bounds__(kThreads, kBlocks) append_sequence_kernel(const __grid_constant__ RopeParams p, int of) {
   pdl_wait();
   const int seq = blockIdx.x, first = first_slot(p, seq), rows = rows_of(p, seq);
   const int row0 = p.rows_per_seq >= 0 ? seq * p.rows_per_seq : p.cu_rows[seq];
@@ -294,7 +314,7 @@ cudaError_t launch(const RopeParams& p, int most_rows, cudaStream_t stream) {
     return launch_dependent(append_sequence_kernel<kBf16, kLayout>, dim3(p.c.batch), kThreads, 0, stream, p, of);
   }
   // a warp a row fills the GPU from some thousands of rows on
-  int of = p.rows > 0 ? (4864 + p.rows - 1) / p.rows : 1;
+  int of = p.rows > 0 ? (kFill + p.rows - 1) / p.rows : 1;
   of = of < 1 ? 1 : of > fours ? fours : of;
   const long long ctas = (static_cast<long long>(p.rows) * of + kWarps - 1) / kWarps;
   const cudaError_t e = launch_dependent(rope_rows_kernel<kBf16, kLayout>, dim3(static_cast<unsigned>(ctas > 0 ? ctas : 1)),
