@@ -618,8 +618,9 @@ int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32
  * counts as that, and a negative one marks a sequence that is not there: nothing
  * is written for it, and its attention sees nothing.  Slots behind the length may
  * hold anything, NaN among it.
- * Calls that use one workspace must not overlap on the GPU, and neither must two
- * calls of which one writes what the other uses. */
+ * Sequences may share pages to read; where two rows of an append go to one slot,
+ * it holds either.  Calls that use one workspace must not overlap on the GPU, and
+ * neither must two calls of which one writes what the other uses. */
 typedef struct ckv_paged_cache {
   int32_t batch;            /* sequences, 1..512 */
   int32_t num_kv_heads;     /* 1..64 */
@@ -687,7 +688,7 @@ typedef struct ckv_paged_queries {
   const int32_t* cu_rows;   /* host [batch+1] */
   int32_t causal;           /* non-zero: a token sees the slots up to its own */
   float scale;              /* softmax scale, at most 2^96; 0 selects 1/sqrt(head_dim) */
-  int64_t q_token_stride, q_head_stride;     /* elements, multiples of 8; q's positive */
+  int64_t q_token_stride, q_head_stride;     /* elements, multiples of 8, below 2^39; q's positive */
   int64_t out_token_stride, out_head_stride;
 } ckv_paged_queries;
 
@@ -745,7 +746,7 @@ int compresskv_debug_stall_next_fused_call(long long wait_ns);
  * usable again. */
 int compresskv_debug_stall_next_q4_attend(long long wait_ns);
 
-/* The same for compresskv_paged_attend: its first CTA waits, copies and products
+/* The same for compresskv_paged_attend: one of its CTAs waits, copies and products
  * under way, for what nothing completes, and stops;
  * compresskv_paged_workspace_init makes the workspace usable again. */
 int compresskv_debug_stall_next_paged_attend(long long wait_ns);

@@ -589,8 +589,8 @@ def debug_stall_next_q4_attend(wait_ns: int) -> None:
 
 
 def debug_stall_next_paged_attend(wait_ns: int) -> None:
-    """Test hook: the first CTA of the next paged_attend stalls on purpose and
-    stops after wait_ns (0 cancels)."""
+    """Test hook: a CTA of the next paged_attend stalls on purpose and stops
+    after wait_ns (0 cancels)."""
     _check(load().compresskv_debug_stall_next_paged_attend(ctypes.c_longlong(int(wait_ns))),
            "compresskv_debug_stall_next_paged_attend")
 

@@ -316,7 +316,8 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
     if ((rc = check_rows(P.rows, a->num_q_heads, q, a->q_token_stride, a->q_head_stride, out, a->out_token_stride,
                          a->out_head_stride)) != CKV_OK)
       return rc;
-    if (a->q_token_stride == 0 || a->q_head_stride == 0) return CKV_ERR_INVALID_ARG;
+    if ((P.rows > 1 && a->q_token_stride == 0) || (a->num_q_heads > 1 && a->q_head_stride == 0))
+      return CKV_ERR_INVALID_ARG;
     if (share(q, 2 * span_of(P.rows, a->num_q_heads, a->q_token_stride, a->q_head_stride), out,
               2 * span_of(P.rows, a->num_q_heads, a->out_token_stride, a->out_head_stride)))
       return CKV_ERR_INVALID_ARG;  // (a row of q is read after another's output is written)
@@ -341,7 +342,9 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
   {
     const unsigned long long dims[2] = {static_cast<unsigned long long>(a->num_q_heads),
                                         static_cast<unsigned long long>(P.rows)};
-    const long long strides[2] = {a->q_head_stride, a->q_token_stride};
+    // (a dimension of one element has a stride that means nothing)
+    const long long strides[2] = {a->num_q_heads > 1 ? a->q_head_stride : kHeadDim,
+                                  P.rows > 1 ? a->q_token_stride : kHeadDim};
     const unsigned box[2] = {static_cast<unsigned>(P.group), static_cast<unsigned>(box_tokens)};
     if ((rc = make_rows_map(q, bf16, 3, dims, strides, box, &P.map_q)) != CKV_OK) return rc;
   }
@@ -349,7 +352,8 @@ int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a
     const unsigned long long dims[3] = {static_cast<unsigned long long>(c->num_kv_heads),
                                         static_cast<unsigned long long>(c->page_size),
                                         static_cast<unsigned long long>(c->num_pages)};
-    const long long strides[3] = {c->head_stride, c->slot_stride, c->page_stride};
+    const long long strides[3] = {c->num_kv_heads > 1 ? c->head_stride : kHeadDim, c->slot_stride,
+                                  c->num_pages > 1 ? c->page_stride : kHeadDim};
     const unsigned box[3] = {1u, static_cast<unsigned>(std::min(c->page_size, kPagedTile)), 1u};
     if ((rc = make_rows_map(c->k_pages, bf16, 4, dims, strides, box, &P.map_k)) != CKV_OK) return rc;
     if ((rc = make_rows_map(c->v_pages, bf16, 4, dims, strides, box, &P.map_v)) != CKV_OK) return rc;

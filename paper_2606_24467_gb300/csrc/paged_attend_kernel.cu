@@ -47,6 +47,7 @@ constexpr float kGrowth = 8.f;                              // log2 of how far p
 // A part of an item's slots, as the roles get it.
 struct Piece {
   int go;                 // 0: no more pieces
+  int first;              // of the call
   int seq, head;
   int row0;               // packed row of the item's first token
   int tokens;             // of the item
@@ -84,6 +85,12 @@ struct Misc {
 constexpr int kOperandBytes = 7 * kTileBytes2;  // (2 + 5 or 1 + 6)
 constexpr int kSmemBytes = kOperandBytes + static_cast<int>(sizeof(Misc));
 static_assert(kSmemBytes <= 232448, "shared memory");
+
+__device__ __forceinline__ uint64_t l2_policy_evict_normal() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
 
 // ------------------------------------------------------------------- numbers
 template <bool kBf16>
@@ -343,7 +350,8 @@ struct Finder {
   // single
   long long all = 0, at = 0, end = 0;
   int ctas = 0;
-  uint64_t policy = l2_policy_evict_last();
+  // (K and V of chunks are read by many CTAs; single's once)
+  uint64_t policy = kPair ? l2_policy_evict_last() : l2_policy_evict_normal();
 
   // Work of a head, in tiles for two tiles of rows: as if items grew evenly.
   __device__ long long work_of(const Sequence& x) const {
@@ -500,6 +508,7 @@ struct Finder {
     const int in_seq = static_cast<int>(want - first);
     Piece y;
     y.go = 1;
+    y.first = want == 0;
     y.seq = group * 32 + src;
     y.length = q.length;
     y.rows = q.rows;
@@ -766,6 +775,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
     const Piece& x = c.m->ring[piece % kRing];
     if (!x.go) break;
     const int n = x.tiles[t], tiles = kPair ? max(n, x.tiles[t ^ 1]) : n;
+    const bool stall = c.p.stall_ns != 0 && x.first;
     const int in_part = limit_of(c.p, x.pos0, x.length) / kTile - x.tile0;  // first tile that not all rows see whole
     mbar_arrive(bar(c.m->pempty[piece % kRing]));
     if (!(ok = c.wait(c.m->kfull[piece % kRing], (piece / kRing) & 1))) break;
@@ -786,7 +796,7 @@ __device__ void product_role(const Cta& c, uint32_t tmem, int t) {
       end();
       drop(k0);
     }
-    if (c.p.stall_ns && blockIdx.x == 0) {  // test hook: a wait for what nothing completes
+    if (stall) {  // test hook: a wait for what nothing completes
       wait_on(bar(c.m->drain[t]), 0, &c.m->abort, c.p.status, c.p.stopped, c.p.stall_ns);
       break;
     }

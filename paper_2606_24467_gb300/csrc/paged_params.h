@@ -109,7 +109,7 @@ struct PagedAttendParams {
   float2* part_ml;             // [slots][part_rows]: base-2 reference and sum of a piece's rows,
   float* part_o;               //   [128]: and output
   int part_rows;
-  unsigned long long stall_ns; // test hook: CTA 0 waits this long for what nothing sets; 0: not
+  unsigned long long stall_ns; // test hook: the CTA of the first piece waits this long for what nothing sets; 0: not
   int rows_per_seq;
   int cu_rows[kMaxBatch + 1];
 };

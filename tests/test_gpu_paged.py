@@ -252,12 +252,12 @@ def test_tokens_that_see_nothing():
     check(cache, q, out, lse, [0, 3, 6], sequences=[1])
 
 
-@pytest.mark.parametrize("rows", [1, 6, 90])
-def test_what_is_not_seen_leaves_no_trace(rows):
+@pytest.mark.parametrize("rows, length", [(1, 300), (6, 300), (90, 300), (90, 9000), (300, 9000), (130, 131)])
+def test_what_is_not_seen_leaves_no_trace(rows, length):
     """Infinities and NaN in slots that a token does not see: of the chunk's later
     tokens, and behind the length (where make() puts NaN); in those that it sees
     they reach every channel that they are in."""
-    length, h, hq, page = 300, 2, 8, 32
+    h, hq, page = 2, 8, 32
     cache = make([length], h, page)
     q = queries(rows, hq, BF)
     clean, clean_lse, _ = attend(cache, q)
@@ -331,6 +331,18 @@ def test_long_contexts_and_many_pieces():
         check(cache, q, out, lse, cu)
 
 
+def test_chunks_in_pieces_whose_tiles_see_different_blocks():
+    """One head a group: the second 128 rows see a block of slots more; starts that
+    are not the newest slots; many short sequences beside a long one."""
+    run([20000], [260], 1, 1, 128, BF)
+    run([20000, 9000], [260, 200], 2, 2, 64, HF)
+    run([30000], [300], 4, 1, start=[-200])
+    run([30000], [300], 4, 1, start=[20000])
+    run([30000, 40], [300, 0], 4, 1, causal=False)
+    cache, q, out, lse = run([9000] + [150] * 20, [200] + [100] * 20, 8, 2)
+    run([9000] + [150] * 20, [1] + [100] * 20, 8, 2)
+
+
 def test_a_whole_prompt():
     run([3000], [3000], 4, 1, 128, BF)
 
@@ -375,6 +387,70 @@ def test_pages_outside_the_pool_count_as_zeros():
         out, lse, status = attend(cache, q)
         assert status == -8
         check(cache, q, out, lse, [0, rows])
+
+
+def test_shared_pages_and_parts_of_a_cache():
+    """Sequences with a prefix in common; some sequences of a cache; a table that is
+    wider than it is used; a pool of one page."""
+    page, h = 32, 2
+    cache = make([200, 180, 90], h, page, slack=4)
+    cache.table[1, :2] = cache.table[0, :2]
+    for rows in (1, 60):
+        q = queries(3 * rows, 8, BF)
+        out, lse, _ = attend(cache, q)
+        check(cache, q, out, lse, packed([rows] * 3))
+        part = cache.sequences(1, 2)
+        out2, lse2, _ = attend(part, q[rows:])
+        assert torch.equal(out2, out[rows:]) and torch.equal(lse2, lse[:, rows:])
+    narrow = ckv.PagedCache(cache.k_pages, cache.v_pages, cache.table[:, :7], cache.lengths)
+    out3, _, _ = attend(narrow, q)
+    assert torch.equal(out3, out)
+    one = make([17], 1, 64, extra=0, slack=0)
+    assert one.num_pages == 1
+    for rows in (1, 17):
+        q = queries(rows, 3, BF)
+        out, lse, _ = attend(one, q)
+        check(one, q, out, lse, [0, rows])
+
+
+@pytest.mark.parametrize("n", [8, 64])
+def test_on_a_share_of_the_sms(n):
+    from test_gpu_shared_sms import GreenStream
+
+    try:
+        green = GreenStream(n)
+    except (OSError, AttributeError, RuntimeError) as e:
+        pytest.skip(f"no green contexts here: {e}")
+    for lengths, rows in (([9000, 300], [1, 1]), ([6000, 300], [150, 40])):
+        cache = make(lengths, 2, 64, fill=0.0)
+        cu = packed(rows)
+        q = queries(int(cu[-1]), 8, BF)
+        ws = ckv.paged_workspace(cache, 8, max(rows))
+        torch.cuda.synchronize()
+        out, lse, status = attend(cache, q, cu, ws=ws, stream=green.stream)
+        assert status == 0
+        check(cache, q, out, lse, cu)
+
+
+@pytest.mark.parametrize("lengths, rows", [([777], [1]), ([30000, 5000], [1, 1]), ([300, 200], [300, 130]),
+                                           ([9000], [200])])
+def test_a_wait_that_runs_out(lengths, rows):
+    """A hook makes a CTA wait for what nothing completes: the call ends, the context
+    stays usable, later calls do nothing until the workspace is set up again."""
+    cache = make(lengths, 2, 64, fill=0.0)
+    cu = packed(rows)
+    q = queries(int(cu[-1]), 8, BF)
+    ws = ckv.paged_workspace(cache, 8, max(rows))
+    want, want_lse, _ = attend(cache, q, cu, ws=ws)
+    ckv.debug_stall_next_paged_attend(2_000_000)
+    _, _, status = attend(cache, q, cu, ws=ws)
+    assert status == -7
+    out, _, status = attend(cache, q, cu, ws=ws)
+    assert status == -7 and (out == 7).all()
+    assert ckv.load().compresskv_paged_workspace_init(ws.data_ptr(), ws.numel(), None) == 0
+    for _ in range(2):
+        out, lse, status = attend(cache, q, cu, ws=ws)
+        assert status == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
 def test_two_calls_give_the_same_bits():

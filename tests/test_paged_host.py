@@ -198,10 +198,17 @@ def test_attend_refusals():
                dict(start=AT + 2), dict(q_token_stride=0), dict(q_token_stride=100), dict(out_head_stride=64),
                dict(out_token_stride=0), dict(rows_per_seq=-1), dict(out=AT * 8), dict(out=AT * 8 + 1024)):
         assert attend_code(c, **kw) == BAD, kw
-    assert attend_code(c, num_q_heads=258) == NOT
+    assert attend_code(c, num_q_heads=258) == NOT and attend_code(c, rows_per_seq=1 << 24, out=AT * 1000) == NOT
     assert attend_code(cache_struct(num_kv_heads=1), num_q_heads=129) == NOT
     assert attend_code(c) == WS and attend_code(c, ws=AT, size=16) == WS
     assert attend_code(c, ws=AT + 128, size=1 << 40) == WS
+
+
+def test_stall_hook_limits():
+    for bad in (-1, 99_999, 2_000_000_001):
+        refused(BAD, ckv.debug_stall_next_paged_attend, bad)
+    ckv.debug_stall_next_paged_attend(1_000_000)
+    ckv.debug_stall_next_paged_attend(0)  # cancelled: no later call stalls
 
 
 def test_workspace_size():
