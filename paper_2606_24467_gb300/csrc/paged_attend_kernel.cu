@@ -291,12 +291,6 @@ struct Blocks {
     for (int b = 0, f; (f = first(p, s, b)) < items; ++b) n += items - f;
     return n;
   }
-  // of items with more than one block
-  __device__ int shared_pieces(const PagedAttendParams& p, const Sequence& s) const {
-    int n = items - first(p, s, 1);
-    for (int b = 1, f; (f = first(p, s, b)) < items; ++b) n += items - f;
-    return n;
-  }
 };
 
 __device__ __forceinline__ Blocks blocks_of(const PagedAttendParams& p, const Sequence& s, int size) {
@@ -368,7 +362,7 @@ struct Finder {
     for (int i = 0; i < 2; ++i) {
       const Blocks b = blocks_of(p, x, size[i]);
       r.pieces[i] = b.pieces(p, x);
-      r.shared[i] = b.shared_pieces(p, x);
+      r.shared[i] = r.pieces[i] - b.first(p, x, 1);  // but items of one block
     }
     return r;
   }
@@ -401,7 +395,9 @@ struct Finder {
 
   // kPair: the sizes of blocks.  Where items are many, each is a piece; but those
   // of the last heads, about what the CTAs need to end together, are cut.  Where
-  // they are few, all are.
+  // they are few, all are, into as many as make the shortest time if they were all
+  // alike: a lane weighs a number, by the tiles of each sequence's first and last
+  // item.  (Exact counts took 28000 cycles.)
   __device__ void plan() {
     const int heads = p.c.num_kv_heads;
     long long work = 0;
@@ -415,63 +411,63 @@ struct Finder {
     __syncwarp();
     work = warp_sum(work) * heads;
     longest = __reduce_max_sync(0xffffffffu, longest);
-    const long long ctas = gridDim.x, share = max(work / ctas, 1LL);
+    const int ctas = static_cast<int>(gridDim.x);
     size[0] = longest;
-    if (kPagedFew * static_cast<long long>(longest) <= share) {
+    if (static_cast<long long>(kPagedFew) * longest * ctas <= work) {
       size[1] = min(max(longest / kPagedTailCuts, kPagedBlock), longest);
-      body = max(work - ctas * longest / 2, 0LL);
+      body = max(work - static_cast<long long>(ctas) * longest / 2, 0LL);
     } else {
-      // as many pieces as make the shortest time, if they were all alike
       body = 0;
-      size[1] = longest;
-      float least = INFINITY;
+      const int cuts = lane + 1;
+      int tiles = (longest + cuts - 1) / cuts;
+      const float per = 1.f / static_cast<float>(tiles);
+      float n = 0.f;
 #pragma unroll 1
-      for (int k = 1; k <= kPagedCuts; ++k) {
-        const int tiles = (longest + k - 1) / k;
-        if (k > 1 && tiles < kPagedBlock) break;
-        long long n = 0, shared = 0;
-#pragma unroll 1
-        for (int g = 0; g < groups(); ++g) {
-          Sequence x;
-          x.load(p, g * 32 + lane);
-          if (x.rows <= 0) continue;
-          const Blocks b = blocks_of(p, x, tiles);
-          n += b.pieces(p, x);
-          shared += b.shared_pieces(p, x);
-        }
-        __syncwarp();
-        n = warp_sum(n) * heads;
-        if (warp_sum(shared) * heads > kPagedSlots) break;
-        const float rounds = ceilf(static_cast<float>(n) / static_cast<float>(ctas));
-        const float time = rounds * (static_cast<float>(work) / static_cast<float>(n) + kPagedPiece);
-        if (time < least) {
-          least = time;
-          size[1] = tiles;
-        }
-      }
-    }
-    // as many pieces as there is room for their results
-    for (; size[1] < longest; size[1] += max(size[1] / 4, 1)) {
-      long long n = 0, ahead = 0;
       for (int g = 0; g < groups(); ++g) {
         Sequence x;
         x.load(p, g * 32 + lane);
-        const long long w = work_of(x), up = warp_prefix(w * heads, lane);
-        n += heads_of(x, w, ahead + up - w * heads).all_shared(heads);
-        ahead += __shfl_sync(0xffffffffu, up, 31);
+        const int items = x.rows > 0 ? (x.rows + p.item_tokens - 1) / p.item_tokens : 0;
+        const int low = items ? x.tiles(p, min(p.item_tokens, x.rows)) : 0, high = items ? x.tiles(p, x.rows) : 0;
+#pragma unroll 1
+        for (unsigned left = __ballot_sync(0xffffffffu, items > 0); left; left &= left - 1) {
+          const int from = __ffs(left) - 1;
+          const float k = static_cast<float>(__shfl_sync(0xffffffffu, items, from));
+          const float c0 = static_cast<float>(__shfl_sync(0xffffffffu, low, from)) * per;
+          const float c1 = static_cast<float>(__shfl_sync(0xffffffffu, high, from)) * per;
+          n += k * 0.5f * (ceilf(c0 - 1e-3f) + ceilf(c1 - 1e-3f));
+        }
       }
-      __syncwarp();
-      if (warp_sum(n) <= kPagedSlots) break;
+      n *= static_cast<float>(heads);
+      float time = ceilf(n / static_cast<float>(ctas)) * (static_cast<float>(work) / n + kPagedPiece);
+      if (cuts > kPagedCuts || (cuts > 1 && (tiles < kPagedBlock || n > kPagedSlots))) time = INFINITY;
+      // the shortest; of equals the fewest pieces
+      float least = time;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+      size[1] = __shfl_sync(0xffffffffu, tiles, __ffs(__ballot_sync(0xffffffffu, time == least)) - 1);
     }
-    size[1] = min(size[1], longest);
+    // no more pieces than there is room for their results
+    for (;; size[1] += max(size[1] / 4, 1)) {
+      size[1] = min(size[1], longest);
+      before = shared_before = 0;
+      work_before = 0;
+      hold(0);
+      while (advance()) {
+      }
+      if (shared_before + __shfl_sync(0xffffffffu, shared_upto, 31) <= kPagedSlots || size[1] == longest) break;
+    }
+    if (group > 0) {
+      before = shared_before = 0;
+      work_before = 0;
+      hold(0);
+    }
   }
 
   __device__ void start() {
     if (kPair) {
-      plan();
       if (lane == 0) ticket = atomicAdd(p.next, 1);
+      plan();
       ticket = __shfl_sync(0xffffffffu, ticket, 0);
-      hold(0);
     } else {
       hold(0);
       int n = __shfl_sync(0xffffffffu, upto, 31);
@@ -955,25 +951,20 @@ __device__ void fix_role(const Cta& c) {
 }
 
 // ---------------------------------------------------------------- softmax
-// A row's output and log-sum-exp, of base-2 reference `ref` and sum `l`.
+// 32 channels of a row's output, over the sum of its exponentials.
 template <bool kBf16>
-__device__ __forceinline__ void write_row(const PagedAttendParams& p, long long row, int head, float ref, float l,
-                                          const uint32_t (&o)[4][32]) {
+__device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, float l, const uint32_t (&o)[32]) {
   const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
   const float inv = 1.f / l;
-  uint16_t* to = p.out + row * p.o_token + head * p.o_head;
-  // 32 bytes at a time where rows are aligned to that: a warp's rows are far apart,
-  // and each of its stores takes as many steps as it has rows
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 2; ++i) {
     uint32_t w[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int at = 16 * i + 2 * k;
+    for (int k = 0; k < 8; ++k)
       w[k] = none ? 0u
-                  : pack<kBf16>(__uint_as_float(o[at / 32][at % 32]) * inv,
-                                __uint_as_float(o[at / 32][at % 32 + 1]) * inv);
-    }
+                  : pack<kBf16>(__uint_as_float(o[16 * i + 2 * k]) * inv, __uint_as_float(o[16 * i + 2 * k + 1]) * inv);
+    // (32 bytes at a time where rows are aligned to that: a warp's rows are far
+    // apart, and each of its stores takes as many steps as it has rows)
     if (p.wide_rows) {
       asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * i), "r"(w[0]), "r"(w[1]),
                    "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
@@ -983,55 +974,83 @@ __device__ __forceinline__ void write_row(const PagedAttendParams& p, long long 
       reinterpret_cast<uint4*>(to)[2 * i + 1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
   }
+}
+// A row's log-sum-exp, of base-2 reference `ref` and sum `l`.
+__device__ __forceinline__ void write_lse(const PagedAttendParams& p, long long row, int head, float ref, float l) {
   if (p.lse)
-    p.lse[static_cast<long long>(head) * p.rows + row] = none ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+    p.lse[static_cast<long long>(head) * p.rows + row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
 }
 
 // The results of an item's pieces for this warp's rows, joined: the weights of the
 // pieces are 2^(their reference - the largest), over the sum.  kPair: rows by
 // lanes, as they were computed; four channels of consecutive rows are side by side
 // (rows by the warp, in order, as below: a split item of 256 rows took 35 us more).
+// 32 channels of four pieces at a time are under way.
 template <bool kBf16>
 __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piece& x, int tile, int row, int token,
-                                          int head, bool valid, uint32_t (&o)[4][32]) {
+                                          int head, bool valid) {
   const int pieces = x.pieces[tile];
+  float weight[kPagedCuts];
+  int slot[kPagedCuts];
   float top = -INFINITY, sum = 0.f;
-  {
-    Slots slots(p, x);
-    for (int k = 0; k < pieces; ++k) {
-      const float2 ml = __ldcg(p.part_ml + static_cast<long long>(slots.next()) * p.part_rows + row);
-      if (ml.y != 0.f) top = fmaxf(top, ml.x);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 128; ++i) o[i / 32][i % 32] = 0;
   Slots slots(p, x);
-  for (int k = 0; k < pieces; ++k) {
-    const long long slot = slots.next();
-    const float2 ml = __ldcg(p.part_ml + slot * p.part_rows + row);
-    // (equal infinities: 1, so that they and NaN go on into the sum)
-    const float w = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : exp2f(ml.x - top);
-    sum += ml.y == 0.f ? 0.f : ml.y * w;
-    const float4* from = reinterpret_cast<const float4*>(p.part_o) + slot * p.part_rows * 32 + row;
-    if (w != 0.f) {
+#pragma unroll 1
+  for (int k = 0; k < pieces; ++k) slot[k] = slots.next();
+#pragma unroll 1
+  for (int k0 = 0; k0 < pieces; k0 += 4) {
+    float2 ml[4];
 #pragma unroll
-      for (int i0 = 0; i0 < 32; i0 += 16) {
-        float4 v[16];
+    for (int u = 0; u < 4; ++u)
+      ml[u] = k0 + u < pieces ? __ldcg(p.part_ml + static_cast<long long>(slot[k0 + u]) * p.part_rows + row)
+                              : make_float2(0.f, 0.f);
+    // (the largest so far may grow: weights and sum follow)
+    float now = top;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __ldcg(from + (i0 + i) * p.part_rows);
+    for (int u = 0; u < 4; ++u)
+      if (ml[u].y != 0.f) now = fmaxf(now, ml[u].x);
+    const float f = now == top ? 1.f : exp2f(top - now);
+    sum *= f;
+#pragma unroll 1
+    for (int k = 0; k < k0; ++k) weight[k] *= f;
+    top = now;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 4 * (i0 + i);
-          uint32_t* to = &o[at / 32][at % 32];
-          to[0] = __float_as_uint(fmaf(w, v[i].x, __uint_as_float(to[0])));
-          to[1] = __float_as_uint(fmaf(w, v[i].y, __uint_as_float(to[1])));
-          to[2] = __float_as_uint(fmaf(w, v[i].z, __uint_as_float(to[2])));
-          to[3] = __float_as_uint(fmaf(w, v[i].w, __uint_as_float(to[3])));
-        }
+    for (int u = 0; u < 4; ++u)
+      if (k0 + u < pieces) {
+        // (equal infinities: 1, so that they and NaN go on into the sum)
+        const float w = ml[u].y == 0.f ? 0.f : ml[u].x == top ? 1.f : exp2f(ml[u].x - top);
+        weight[k0 + u] = w;
+        sum += ml[u].y == 0.f ? 0.f : ml[u].y * w;
       }
-    }
   }
-  if (valid) write_row<kBf16>(p, x.row0 + token, head, top, sum, o);
+  uint16_t* to = p.out + (x.row0 + token) * p.o_token + head * p.o_head;
+#pragma unroll 1
+  for (int part = 0; part < 4; ++part) {
+    uint32_t o[32] = {};
+#pragma unroll 1
+    for (int k0 = 0; k0 < pieces; k0 += 4) {
+      float4 v[4][8];
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        w[u] = k0 + u < pieces ? weight[k0 + u] : 0.f;
+        const float4* from = reinterpret_cast<const float4*>(p.part_o) + row +
+                             (static_cast<long long>(slot[min(k0 + u, pieces - 1)]) * 32 + part * 8) * p.part_rows;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = w[u] != 0.f ? __ldcg(from + i * p.part_rows) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[4 * i] = __float_as_uint(fmaf(w[u], v[u][i].x, __uint_as_float(o[4 * i])));
+          o[4 * i + 1] = __float_as_uint(fmaf(w[u], v[u][i].y, __uint_as_float(o[4 * i + 1])));
+          o[4 * i + 2] = __float_as_uint(fmaf(w[u], v[u][i].z, __uint_as_float(o[4 * i + 2])));
+          o[4 * i + 3] = __float_as_uint(fmaf(w[u], v[u][i].w, __uint_as_float(o[4 * i + 3])));
+        }
+    }
+    if (valid) write_channels<kBf16>(p, to + 32 * part, sum, o);
+  }
+  if (valid) write_lse(p, x.row0 + token, head, top, sum);
 }
 
 // Counts a piece of an item (whose results this warp has written, or seen written);
@@ -1134,59 +1153,66 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
                                        uint64_t& oempty, const Row& row, float ref, float l) {
   const PagedAttendParams& p = c.p;
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
-  uint32_t o[4][32];
+  const Piece y = x;
+  const bool all = y.pieces[tile] == 1;
+  const int at = tile * kTile + row.in_tile;
+  uint16_t* to = p.out + (y.row0 + row.token) * p.o_token + row.head * p.o_head;
+  float4* part_o = reinterpret_cast<float4*>(p.part_o) + static_cast<long long>(y.slot) * p.part_rows * 32 +
+                   (kPair ? at : at * 32);
+  const int step = kPair ? p.part_rows : 1;
+  const bool found = c.m->found[reader.at % kRing] != 0;
   tc_fence_after();
+  // (32 channels at a time: this runs once a piece, from instructions that no cache
+  // holds; all at once took 5000 cycles)
+#pragma unroll 1
+  for (int part = 0; part < 4; ++part) {
+    uint32_t o[32];
+    tmem_load32_async(o_addr + 32 * part, o);
+    tmem_wait_ld(o);
+    if (found) {
+      const int whole = limit_of(p, y.pos0, y.length);
+#pragma unroll 1
+      for (int d = 0; d < 4 * kDiagTiles; ++d)
+        for (uint32_t bits = c.m->poison[reader.at % kRing][d / 4][d % 4]; bits; bits &= bits - 1) {
+          const int slot = whole / kTile * kTile + 32 * d + __ffs(bits) - 1;
+          if (slot >= row.limit || !row.valid) continue;
+          const int page = p.c.table[y.seq * p.c.table_stride + (slot >> p.c.page_shift)];
+          if (page < 0 || page >= p.c.num_pages) continue;
+          const uint16_t* v = p.c.pages[1] + page * p.c.page_stride +
+                              (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + y.head * p.c.head_stride +
+                              32 * part;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) tmem_load32_async(o_addr + 32 * k, o[k]);
-  tmem_wait_ld(o[0]);
+          for (int i = 0; i < 32; ++i) {
+            const float f = value<kBf16>(v[i]);
+            if (!(fabsf(f) < INFINITY)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f);
+          }
+        }
+    }
+    if (row.valid) {
+      if (all) {
+        write_channels<kBf16>(p, to + 32 * part, l, o);
+      } else {
 #pragma unroll
-  for (int k = 1; k < 4; ++k) tmem_order_after_wait(o[k]);
+        for (int i = 0; i < 8; ++i)
+          part_o[(8 * part + i) * step] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                      __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+      }
+    }
+  }
   tc_fence_before();
   __syncwarp();
   if (lane == 0) mbar_arrive(smem_u32(&oempty));
-  if (c.m->found[reader.at % kRing]) {
-    const int whole = limit_of(p, x.pos0, x.length);
-#pragma unroll 1
-    for (int d = 0; d < 4 * kDiagTiles; ++d)
-      for (uint32_t bits = c.m->poison[reader.at % kRing][d / 4][d % 4]; bits; bits &= bits - 1) {
-        const int slot = whole / kTile * kTile + 32 * d + __ffs(bits) - 1;
-        if (slot >= row.limit || !row.valid) continue;
-        const int page = p.c.table[x.seq * p.c.table_stride + (slot >> p.c.page_shift)];
-        if (page < 0 || page >= p.c.num_pages) continue;
-        const uint16_t* v = p.c.pages[1] + page * p.c.page_stride +
-                            (slot & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride + x.head * p.c.head_stride;
-#pragma unroll
-        for (int i = 0; i < 128; ++i) {
-          const float f = value<kBf16>(v[i]);
-          if (!(fabsf(f) < INFINITY)) o[i / 32][i % 32] = __float_as_uint(__uint_as_float(o[i / 32][i % 32]) + f);
-        }
-      }
-  }
-  const Piece y = x;
   reader.done();
-  if (y.pieces[tile] == 1) {
-    if (row.valid) write_row<kBf16>(p, y.row0 + row.token, row.head, ref, l, o);
+  if (all) {
+    if (row.valid) write_lse(p, y.row0 + row.token, row.head, ref, l);
     return;
   }
   if (kPair && !row.rows) return;
-  const int at = tile * kTile + row.in_tile;
-  if (row.valid) {
-    const long long slot = static_cast<long long>(y.slot) * p.part_rows;
-    p.part_ml[slot + at] = make_float2(ref, l);
-    float4* to = reinterpret_cast<float4*>(p.part_o) + slot * 32 + (kPair ? at : at * 32);
-    const int step = kPair ? p.part_rows : 1;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      to[i * step] =
-          make_float4(__uint_as_float(o[i / 8][4 * (i % 8)]), __uint_as_float(o[i / 8][4 * (i % 8) + 1]),
-                      __uint_as_float(o[i / 8][4 * (i % 8) + 2]), __uint_as_float(o[i / 8][4 * (i % 8) + 3]));
-  }
+  if (row.valid) p.part_ml[static_cast<long long>(y.slot) * p.part_rows + at] = make_float2(ref, l);
   __threadfence();
   __syncwarp();
-  int* ticket = p.tickets + (y.ticket * 2 + tile) * 4 + warp;
-  if (kPair) {
-    if (take_ticket(ticket, y.pieces[tile])) join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid, o);
-  }
+  if (kPair && take_ticket(p.tickets + (y.ticket * 2 + tile) * 4 + warp, y.pieces[tile]))
+    join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid);
 }
 
 template <bool kBf16, bool kPair>
