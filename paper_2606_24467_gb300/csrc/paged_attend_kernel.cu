@@ -414,8 +414,8 @@ struct Finder {
     const int ctas = static_cast<int>(gridDim.x);
     size[0] = longest;
     if (static_cast<long long>(kPagedFew) * longest * ctas <= work) {
-      size[1] = min(max(longest / kPagedTailCuts, kPagedBlock), longest);
-      body = max(work - static_cast<long long>(ctas) * longest / 2, 0LL);
+      size[1] = min(max(longest / kPagedTailCuts, kPagedTailBlock), longest);
+      body = max(work - static_cast<long long>(ctas) * longest * kPagedTail / 8, 0LL);
     } else {
       body = 0;
       const int cuts = lane + 1;

@@ -69,13 +69,19 @@ constexpr int kPagedMaxCtas = 160;
 // Chunks.  Where an item (two tiles of rows) is more than a kPagedFew-th of an SM's
 // share of the tiles, all are cut into blocks of slots: into 1 .. kPagedCuts, of at
 // least kPagedBlock tiles, as makes the shortest time if a piece costs as much as
-// kPagedPiece tiles beside its own.  Else only the items at the end are, into
-// kPagedTailCuts.  The results of at most kPagedSlots pieces wait to be joined.
+// kPagedPiece tiles beside its own (501 tokens after 9000 to 16000: 171 us, 193 cut
+// in quarters of a share).  Else items are whole but for the last ones, kPagedTail
+// eighths of an item a CTA, in kPagedTailCuts or into blocks of kPagedTailBlock
+// tiles: 4096 tokens after 128K take 5000 us so and 5950 with all items whole, 8191
+// from the first on 380 and 393 (of 16 tiles each: 388).  The results of at most
+// kPagedSlots pieces wait to be joined.
 constexpr int kPagedFew = 2;
 constexpr int kPagedCuts = 24;
 constexpr int kPagedPiece = 6;
-constexpr int kPagedTailCuts = 4;
 constexpr int kPagedBlock = 8;
+constexpr int kPagedTail = 4;
+constexpr int kPagedTailCuts = 5;
+constexpr int kPagedTailBlock = 40;
 constexpr int kPagedSlots = 608;
 // Workspace header: status word, the word that says that a call has stopped, the
 // next ticket and the CTAs done; behind it the counters of items in pieces, one
