@@ -245,6 +245,18 @@ __device__ __forceinline__ int limit_of(const PagedAttendParams& p, int pos, int
 }
 __device__ __forceinline__ int tiles_of(int limit) { return max((limit + kTile - 1) / kTile, 1); }
 
+// bf16: p enters times 2^-down, or a sum of p V (2^8 in each of `length` slots, at
+// most) would pass fp32's range where V is large and the output is not; V below
+// 2^(down - 126) may be lost for it.  fp16's V is small enough, and its p has no room.
+template <bool kBf16>
+__device__ __forceinline__ float down_of(int length) {
+  return kBf16 ? static_cast<float>(static_cast<int>(kGrowth) + 32 - __clz(length)) : 0.f;
+}
+template <bool kBf16>
+__device__ __forceinline__ float up_of(int length) {  // 2^down
+  return kBf16 ? __int_as_float((127 + static_cast<int>(kGrowth) + 32 - __clz(length)) << 23) : 1.f;
+}
+
 // A sequence, as a lane of the work-finding warp sees it.
 struct Sequence {
   int rows, row0, length, start;
@@ -951,11 +963,12 @@ __device__ void fix_role(const Cta& c) {
 }
 
 // ---------------------------------------------------------------- softmax
-// 32 channels of a row's output, over the sum of its exponentials.
+// 32 channels of a row's output, over the sum of its exponentials (`up`: up_of()).
 template <bool kBf16>
-__device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, float l, const uint32_t (&o)[32]) {
+__device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, float l, float up,
+                                               const uint32_t (&o)[32]) {
   const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
-  const float inv = 1.f / l;
+  const float inv = up / l;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     uint32_t w[8];
@@ -1048,7 +1061,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
           o[4 * i + 3] = __float_as_uint(fmaf(w[u], v[u][i].w, __uint_as_float(o[4 * i + 3])));
         }
     }
-    if (valid) write_channels<kBf16>(p, to + 32 * part, sum, o);
+    if (valid) write_channels<kBf16>(p, to + 32 * part, sum, up_of<kBf16>(x.length), o);
   }
   if (valid) write_lse(p, x.row0 + token, head, top, sum);
 }
@@ -1119,7 +1132,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
     }
     const int token = row / p.group, head = x.head * p.group + row - token * p.group;
     const bool none = sum == 0.f;
-    const float inv = 1.f / sum;
+    const float inv = up_of<kBf16>(x.length) / sum;
     const long long row_at = x.row0 + token;
     reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] =
         none ? make_uint2(0u, 0u)
@@ -1190,7 +1203,7 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
     }
     if (row.valid) {
       if (all) {
-        write_channels<kBf16>(p, to + 32 * part, l, o);
+        write_channels<kBf16>(p, to + 32 * part, l, up_of<kBf16>(y.length), o);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -1234,6 +1247,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     const int tile0 = x->tile0, limit = row.limit, least = __reduce_min_sync(0xffffffffu, limit);
     // (single: two outputs in turns)
     const uint32_t o_addr = lanes + (2 + (kPair ? tile : reader.at & 1)) * kTile;
+    const float down = down_of<kBf16>(x->length), up = up_of<kBf16>(x->length);
     float m = -INFINITY, l = 0.f;
     for (int j = 0; j < n; ++j, ++count) {
       const int buffer = kPair ? tile : count & 1;
@@ -1271,7 +1285,8 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
           }
         };
         uint32_t w[16];
-        float ref = m == -INFINITY ? 0.f : -m * scale;
+        auto reference = [&] { return -((m == -INFINITY ? 0.f : m * scale) + down); };
+        float ref = reference();
         exponentials(0, w, ref);
         float top[4] = {m, m, m, m};
 #pragma unroll
@@ -1301,7 +1316,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
               tmem_store16(o_addr + 16 * k, o);
             }
           }
-          ref = m == -INFINITY ? 0.f : -m * scale;
+          ref = reference();
 #pragma unroll
           for (int i = 0; i < 4; ++i) sum[i] = 0;
           exponentials(0, w, ref);
@@ -1319,7 +1334,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
           }
         }
         const float2 total = split_of(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
-        l += total.x + total.y;
+        l += (total.x + total.y) * up;
         tmem_wait_st();
         tc_fence_before();
       } else {
@@ -1329,13 +1344,15 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][1]));
     }
+    // (the reference as it entered, rounded beside `down`: the difference is exact)
+    const float ref = ((m == -INFINITY ? 0.f : m * scale) + down) - down;
     if (kPair) {
       if (!c.wait_here(c.m->odone[tile], o_count++ & 1)) return;
-      finish<kBf16, true>(c, reader, *x, tile, o_addr, c.m->oempty[tile], row, m == -INFINITY ? 0.f : m * scale, l);
+      finish<kBf16, true>(c, reader, *x, tile, o_addr, c.m->oempty[tile], row, ref, l);
     } else {  // the other warps take it from here
       const int o = reader.at & 1;
       if (!c.wait_here(c.m->oempty[o], ((reader.at >> 1) & 1) ^ 1)) return;  // (they have read the one before)
-      c.m->sums[o][r] = make_float2(m == -INFINITY ? 0.f : m * scale, l);
+      c.m->sums[o][r] = make_float2(ref, l);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.m->sready[o]));
       reader.done();

@@ -319,6 +319,25 @@ def test_growing_and_extreme_logits(dtype):
         check(cache, q, out, lse, [0, 70])
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("length, rows", [(700, 1), (40000, 1), (9000, 200)])
+def test_values_near_the_largest_number(dtype, length, rows):
+    """Averages of values near the type's largest number are finite, whatever the sum
+    of their weights; small ones are kept (bf16: down to 2^(8 - 126) times the length,
+    rounded up to a power of two)."""
+    cache = make([length], 1, 64, dtype)
+    slot = torch.arange(length, device="cuda")
+    pages = cache.table[0].long()[slot // 64]
+    v = cache.v_pages[pages, slot % 64]
+    q = queries(rows, 4, dtype)
+    least = 2.0 ** -90 if dtype == BF else torch.finfo(dtype).smallest_normal * 64
+    for size in (torch.finfo(dtype).max / 4, least):
+        cache.v_pages[pages, slot % 64] = (v.double().clamp(-1, 1).abs() * size).to(dtype)
+        out, lse, _ = attend(cache, q)
+        assert torch.isfinite(out).all()
+        check(cache, q, out, lse, [0, rows])
+
+
 def test_long_contexts_and_many_pieces():
     """Slots beyond 64K, shared by many CTAs; a chunk over a long context."""
     for lengths, rows, hq, h in (([70000], [1], 4, 1), ([70001, 300], [3, 1], 8, 2), ([40000], [40], 8, 1),
