@@ -81,7 +81,10 @@ def attend(cache, q, cu=None, start=None, causal=True, ws=None, **kw):
     lse = torch.full((q.shape[1], q.shape[0]), 7.0, device="cuda")
     ckv.paged_attend(cache, q, out, ws, cu_rows=cu, start=start, lse=lse, causal=causal, **kw)
     torch.cuda.synchronize()
-    return out, lse, ckv.read_device_status(ws)
+    status = ckv.read_device_status(ws)
+    if status == 0:  # every row is written
+        assert not (out == 7).all(-1).any() and not (lse == 7).any()
+    return out, lse, status
 
 
 def run(lengths, rows, hq, h, page=64, dtype=BF, layout="head", start=None, causal=True, seed=0):
@@ -378,6 +381,26 @@ def test_many_sequences():
     q = queries(int(cu[-1]), 8, BF)
     out, lse, _ = attend(cache, q, cu)
     check(cache, q, out, lse, cu, sequences=range(0, 512, 37))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_batches_of_chunks(seed):
+    """Batches of up to a hundred sequences, some of them long, some with one token:
+    what CTAs share, and how the last items are cut, differ from case to case."""
+    gen = np.random.default_rng(seed)
+    b = int(gen.integers(1, 100))
+    most = int(4000 / b) + 10
+    rows = gen.integers(0, most, b)
+    rows[gen.random(b) < 0.3] = 1
+    rows[0] += 200
+    lengths = rows + (gen.random(b) ** 6 * 20000).astype(int)
+    hq, h = [(8, 2), (6, 1), (4, 4), (14, 2), (16, 2), (3, 1)][seed]
+    cache = make(lengths.tolist(), h, [16, 32, 64, 128, 256, 64][seed], [BF, HF][seed % 2], seed=seed)
+    cu = packed(rows)
+    q = queries(int(cu[-1]), hq, [BF, HF][seed % 2], seed)
+    out, lse, status = attend(cache, q, cu)
+    assert status == 0
+    check(cache, q, out, lse, cu, sequences=sorted({0, b - 1, *gen.integers(0, b, 6).tolist()}))
 
 
 def test_strided_queries_and_outputs():
