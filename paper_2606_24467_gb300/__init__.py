@@ -1,8 +1,9 @@
 """CompressKV prefill-end KV-cache compression on one GB300 (sm_103a).
 
 The compression path (window scoring with the SRH heads, pooling, budgeted
-top-k, K/V gather) runs in the CUDA kernels of ``libcompresskv``; this
-package holds the kernels' sources (``csrc/``), their nvcc build and a thin
+top-k, K/V gather), what stands in front of it (rotary positions, a paged cache
+and attention over it) and behind it (a 4-bit cache) run in the CUDA kernels of
+``libcompresskv``; this package holds the kernels' sources (``csrc/``), their nvcc build and a thin
 ctypes binding of the C ABI in ``include/compresskv.h``.
 """
 from . import compresskv  # noqa: F401
