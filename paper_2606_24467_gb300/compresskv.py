@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
@@ -146,6 +147,15 @@ class CkvPagedQueries(ctypes.Structure):
                 ("causal", c_int32), ("scale", c_float), ("q_token_stride", c_int64),
                 ("q_head_stride", c_int64), ("out_token_stride", c_int64),
                 ("out_head_stride", c_int64)]
+
+
+# What a call describes of its rows, packed as the structures above (native alignment;
+# filling a ctypes structure takes twice as long).
+_ROPE_ROWS = struct.Struct("6i8qP")
+_PAGED_ROWS = struct.Struct("2iP6q")
+_PAGED_QUERIES = struct.Struct("2iPif4q")
+assert (_ROPE_ROWS.size, _PAGED_ROWS.size, _PAGED_QUERIES.size) == tuple(
+    ctypes.sizeof(t) for t in (CkvRopeRows, CkvPagedRows, CkvPagedQueries))
 
 
 class CompressKVError(RuntimeError):
@@ -715,12 +725,12 @@ def _q4_call(name: str, cache, stream, *args):
 def _device_call(name: str, index: int, stream, *args):
     if index < 0:
         _invalid("tensors must be in device memory")
-    fn = _fast(name)
+    fn = _FAST.get(name) or _fast(name)
     if stream is None:
         stream = torch._C._cuda_getCurrentRawStream(index)
     else:
         stream = _raw_stream(stream)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         code = fn(*args, stream)
     else:
         with torch.cuda.device(index):
@@ -939,7 +949,7 @@ def _head_rows(t, rows, what, dtype):
         _invalid(f"{what} must be [rows, heads, 128]")
     n, heads, d = t.shape
     token, head, one = t.stride()
-    if n != rows or d != 128 or one != 1 or t.dtype != dtype:
+    if n != rows or d != 128 or one != 1 or t.dtype != dtype or rows >= 1 << 31:
         _invalid(f"{what} must be {dtype} [{rows}, heads, 128], head_dim contiguous")
     # a dimension of one element has a stride that means nothing
     return (heads, token if rows > 1 else (heads or 1) * 128, head if heads > 1 else 128)
@@ -978,9 +988,9 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, backwar
     _rows_i32(positions, rows, "positions")
     if q_out.get_device() != index or positions.get_device() != index:
         _invalid("q, k, positions and outputs must be on one device")
-    x = CkvRopeRows(rows, hq, hk, _q4_dtype(q), 1 if backward else 0, 0, qt, qh, kt, kh, qot, qoh, kot, koh,
-                    None if trace is None else ctypes.pointer(trace.struct))
-    _device_call("compresskv_rope_apply", index, stream, rope.addr, ctypes.addressof(x), positions.data_ptr(),
+    x = _ROPE_ROWS.pack(rows, hq, hk, _q4_dtype(q), 1 if backward else 0, 0, qt, qh, kt, kh, qot, qoh, kot,
+                        koh, 0 if trace is None else ctypes.addressof(trace.struct))
+    _device_call("compresskv_rope_apply", index, stream, rope.addr, x, positions.data_ptr(),
                  q.data_ptr() if hq else None, k.data_ptr() if hk else None,
                  q_out.data_ptr() if hq else None, k_out.data_ptr() if hk else None)
 
@@ -1095,8 +1105,8 @@ def paged_append(cache: PagedCache, k, v, cu_rows=None, start=None, rope: "Rope 
     _q4_on_device(cache, "rows, start, positions and status", k, v, start, positions, q, q_out,
                   device_status)
     each, cu, at = _paged_rows(cache, rows, cu_rows)
-    r = CkvPagedRows(each, hq, at, kt, kh, qt, qh, qot, qoh)
-    _q4_call("compresskv_paged_append", cache, stream, cache.addr, ctypes.addressof(r), _addr(k),
+    r = _PAGED_ROWS.pack(each, hq, at or 0, kt, kh, qt, qh, qot, qoh)
+    _q4_call("compresskv_paged_append", cache, stream, cache.addr, r, _addr(k),
              _addr(v), _addr(start), None if rope is None else rope.addr, _addr(positions),
              _addr(q) if hq else None, _addr(q_out) if hq else None, _addr(device_status))
 
@@ -1163,7 +1173,9 @@ def paged_attend(cache: PagedCache, q, out, ws, cu_rows=None, start=None, scale:
         _invalid("lse must be a contiguous float32 [H_q, rows]")
     _rows_i32(start, cache.batch, "start")
     _q4_on_device(cache, "q, out, start, lse and workspace", q, out, start, lse, ws)
+    if not -3e38 < scale < 3e38:
+        _invalid("scale must be a finite number")
     each, cu, at = _paged_rows(cache, rows, cu_rows)
-    a = CkvPagedQueries(hq, each, at, int(bool(causal)), float(scale), qt, qh, ot, oh)
-    _q4_call("compresskv_paged_attend", cache, stream, cache.addr, ctypes.addressof(a), _addr(q),
+    a = _PAGED_QUERIES.pack(hq, each, at or 0, 1 if causal else 0, scale, qt, qh, ot, oh)
+    _q4_call("compresskv_paged_attend", cache, stream, cache.addr, a, _addr(q),
              _addr(start), _addr(out), _addr(lse), _addr(ws), ws.numel())

@@ -247,6 +247,10 @@ def test_binding_refusals():
     refused(BAD, ckv.paged_gather, c, k.transpose(0, 1))
     refused(BAD, ckv.paged_gather, c, k, k[:5])
     refused(BAD, ckv.paged_attend, c, q, q[:, :2], None)
+    for scale in (float("nan"), float("inf"), 1e39, -1e39):
+        refused(BAD, ckv.paged_attend, c, q, q.clone(), torch.empty(16, dtype=torch.uint8), scale=scale)
+    long = torch.zeros(1, 4, 128, dtype=torch.bfloat16).expand(1 << 32, 4, 128)
+    refused(BAD, ckv.paged_attend, c, long, long, torch.empty(16, dtype=torch.uint8))
     refused(BAD, ckv.paged_workspace, c, 4, 1)
     refused(BAD, ckv.paged_workspace_size, c, 3, 1)
 
