@@ -18,8 +18,9 @@
 //  * kPair, for chunks: two 128-row tiles of the same KV group and sequence share
 //    each tile of K and V, and while the tensor cores work for one, the other's
 //    softmax runs.  An item is two tiles of rows; where there are few items for
-//    the SMs, the slots are cut into blocks, and CTAs take (item, block) pieces by
-//    ticket, block by block, so that CTAs that run together read the same K and V.
+//    the SMs, all their tiles are shared in equal runs, else items are taken by
+//    ticket, so that CTAs that run together read the same K and V, and only the
+//    last ones are shared in runs.
 //  * single, where 128 rows hold all query tokens of a sequence (decode): the
 //    bytes of K and V bound it.  The tiles of all units form one sequence, of which
 //    each CTA takes an equal run; logits of the next tile are made while the
@@ -41,6 +42,8 @@ constexpr int kSoftWarp = 4;                                // 4 .. 7 and 8 .. 1
 constexpr int kHalf = kTile * 128;                          // 64 channels of a tile, bytes
 constexpr int kTileBytes2 = 2 * kHalf;                      // K, V or Q: 32 KB
 constexpr int kRing = 4;                                    // piece descriptors
+constexpr int kAhead = 4;                                   // tiles to load when the next piece is found,
+constexpr int kTicketAhead = 2;                             // and more when its ticket is taken
 constexpr int kDiagTiles = 3;                               // tiles that an item's rows see in part, at most
 constexpr float kGrowth = 8.f;                              // log2 of how far p may pass 1
 
@@ -56,10 +59,11 @@ struct Piece {
   int tile0;              // first tile
   int tiles[2];           // of each 128-row tile (its rows see none behind); 0: not there
   int pieces[2];          // of the item, for each 128-row tile; 1: the piece is all of it
-  int slot, ticket;       // where the piece's results go, and who counts them
-  // to find the slots of the item's pieces: single: the CTA that has its first
-  // tile; kPair: the sequence's first slot, t, tiles of a block
-  int base, item, size, rows, start;
+  int slot;               // where the piece's results go
+  // CTA (kPair: run) that has the item's first tile.  The others' are those behind
+  // it; its own piece begins the item, so its slot is 2 base + 1, theirs 2 (base + k).
+  int base;
+  __device__ long long slot_of(int k) const { return k == 0 ? 2 * base + 1 : 2 * (base + k); }
 };
 
 template <bool kPair>
@@ -284,31 +288,6 @@ __device__ __forceinline__ int warp_prefix(int x, int lane) {  // inclusive
   return x;
 }
 
-// kPair: the blocks of a sequence.  Item t covers tokens t per .. ; block b the
-// tiles b size .. of those items that see that far: items first(b) .. items - 1.
-struct Blocks {
-  int items, per, size;
-  // first(b), or `items` where no item sees block b
-  __device__ int first(const PagedAttendParams& p, const Sequence& s, int b) const {
-    if (b == 0) return 0;
-    const int slots = b * size * kTile;  // an item takes part if it sees more than these
-    if (s.length <= slots) return items;
-    if (!p.causal) return 0;
-    if (s.start + s.rows <= slots) return items;
-    const int tokens = slots - s.start + 1;  // that it must reach
-    return min(max((tokens + per - 1) / per - 1, 0), items - 1);
-  }
-  __device__ int pieces(const PagedAttendParams& p, const Sequence& s) const {  // of a head
-    int n = 0;
-    for (int b = 0, f; (f = first(p, s, b)) < items; ++b) n += items - f;
-    return n;
-  }
-};
-
-__device__ __forceinline__ Blocks blocks_of(const PagedAttendParams& p, const Sequence& s, int size) {
-  return {(s.rows + p.item_tokens - 1) / p.item_tokens, p.item_tokens, size};
-}
-
 __device__ __forceinline__ long long warp_prefix(long long x, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -317,23 +296,29 @@ __device__ __forceinline__ long long warp_prefix(long long x, int lane) {
   }
   return x;
 }
-__device__ __forceinline__ long long warp_sum(long long x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
-}
-
 // (64-bit divisions take some hundred instructions, 32-bit ones far fewer)
 __device__ __forceinline__ long long quotient(long long a, long long b) {
   return (a | b) >> 32 ? a / b : static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
 }
 
-// kPair: a sequence's heads 0 .. whole - 1 have `pieces[0]` pieces each, the others
-// pieces[1] (`shared` of them of items with more than one).
-struct Heads {
-  int whole, pieces[2], shared[2];
-  __device__ int all(int heads) const { return whole * pieces[0] + (heads - whole) * pieces[1]; }
-  __device__ int all_shared(int heads) const { return whole * shared[0] + (heads - whole) * shared[1]; }
+// kPair: the items of a sequence and head, those that see most first, on the line of
+// all work: an item takes its tiles and kPagedPiece.  (As if they grew evenly, so
+// that a position is found by arithmetic; what an item has beyond or short of that
+// makes a piece a tile longer or shorter.)
+struct Items {
+  int count, low, high;  // tiles of the item that sees least, and most
+  __device__ void load(const PagedAttendParams& p, const Sequence& x) {
+    count = low = high = 0;
+    if (x.rows <= 0) return;
+    count = (x.rows + p.item_tokens - 1) / p.item_tokens;
+    low = x.tiles(p, min(p.item_tokens, x.rows));
+    high = x.tiles(p, x.rows);
+  }
+  __device__ long long before(int n) const {  // of the first n
+    if (n == 0) return 0;
+    const long long steps = static_cast<long long>(n) * (n - 1) * (high - low);
+    return static_cast<long long>(n) * (high + kPagedPiece) - quotient(steps, 2 * max(count - 1, 1));
+  }
 };
 
 // Finds the pieces of this CTA, a warp together.
@@ -344,142 +329,149 @@ struct Finder {
   // the 32 sequences that the lanes hold, and what came before them
   int group = -1;
   Sequence s;
-  int mine = 0, upto = 0;      // single: tiles of a head; kPair: pieces; and prefix, inclusive
-  int before = 0;
-  // kPair
-  Heads h;
-  int shared_upto = 0, shared_before = 0;
+  // kPair: items, and work, before what the lane holds and with it
+  Items it;
+  int items_upto = 0, items_before = 0;
   long long work_upto = 0, work_before = 0;
-  int size[2];                 // tiles of a block
-  long long body = 0;          // work of the heads whose blocks are of size[0]
-  int ticket = 0;
+  int whole = 0, runs = 0;     // items that are a piece, and runs of the work behind them
+  long long body = 0;          // work of the former
+  bool taken = false;          // a ticket that is still to be used:
+  int ticket = 0, run = 0;     // of lane 0, and run at hand (negative: an item)
+  long long all = 0, at = 0, end = 0;  // work, and this CTA's next
   // single
-  long long all = 0, at = 0, end = 0;
   int ctas = 0;
+  int mine = 0, upto = 0;      // tiles of a head; and prefix, inclusive
+  int before = 0;
   // (K and V of chunks are read by many CTAs; single's once)
   uint64_t policy = kPair ? l2_policy_evict_last() : l2_policy_evict_normal();
 
-  // Work of a head, in tiles for two tiles of rows: as if items grew evenly.
-  __device__ long long work_of(const Sequence& x) const {
-    if (x.rows <= 0) return 0;
-    const int items = (x.rows + p.item_tokens - 1) / p.item_tokens;
-    return (static_cast<long long>(items) * (x.tiles(p, min(p.item_tokens, x.rows)) + x.tiles(p, x.rows)) + 1) / 2;
-  }
-  // (work_before and work_upto known)
-  __device__ Heads heads_of(const Sequence& x, long long work, long long ahead) const {
-    Heads r{};
-    if (x.rows <= 0) return r;
-    r.whole = clamp_to((body - ahead) / work, 0, p.c.num_kv_heads);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const Blocks b = blocks_of(p, x, size[i]);
-      r.pieces[i] = b.pieces(p, x);
-      r.shared[i] = r.pieces[i] - b.first(p, x, 1);  // but items of one block
-    }
-    return r;
-  }
   __device__ void hold(int g) {
     group = g;
     s.load(p, g * 32 + lane);
     if (kPair) {
       const int heads = p.c.num_kv_heads;
-      const long long work = work_of(s);
-      work_upto = warp_prefix(work * heads, lane);
-      h = heads_of(s, work, work_before + work_upto - work * heads);
-      mine = h.all(heads);
-      shared_upto = warp_prefix(h.all_shared(heads), lane);
+      it.load(p, s);
+      work_upto = warp_prefix(it.before(it.count) * heads, lane);
+      items_upto = warp_prefix(it.count * heads, lane);
     } else {
       mine = s.rows > 0 ? s.tiles(p, s.rows) : 0;
+      upto = warp_prefix(mine, lane);
     }
-    upto = warp_prefix(mine, lane);
   }
   __device__ bool advance() {  // to the next 32
     if ((group + 1) * 32 >= p.c.batch) return false;
-    before += __shfl_sync(0xffffffffu, upto, 31);
     if (kPair) {
-      shared_before += __shfl_sync(0xffffffffu, shared_upto, 31);
+      items_before += __shfl_sync(0xffffffffu, items_upto, 31);
       work_before += __shfl_sync(0xffffffffu, work_upto, 31);
+    } else {
+      before += __shfl_sync(0xffffffffu, upto, 31);
     }
     hold(group + 1);
     return true;
   }
+  __device__ void rewind() {
+    if (group == 0) return;
+    before = items_before = 0;
+    work_before = 0;
+    hold(0);
+  }
   __device__ int groups() const { return (p.c.batch + 31) / 32; }
 
-  // kPair: the sizes of blocks.  Where items are many, each is a piece; but those
-  // of the last heads, about what the CTAs need to end together, are cut.  Where
-  // they are few, all are, into as many as make the shortest time if they were all
-  // alike: a lane weighs a number, by the tiles of each sequence's first and last
-  // item.  (Exact counts took 28000 cycles.)
-  __device__ void plan() {
-    const int heads = p.c.num_kv_heads;
-    long long work = 0;
-    int longest = 0;
-    for (int g = 0; g < groups(); ++g) {
-      Sequence x;
-      x.load(p, g * 32 + lane);
-      work += work_of(x);
-      if (x.rows > 0) longest = max(longest, x.tiles(p, x.rows));
-    }
-    __syncwarp();
-    work = warp_sum(work) * heads;
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    const int ctas = static_cast<int>(gridDim.x);
-    size[0] = longest;
-    if (static_cast<long long>(kPagedFew) * longest * ctas <= work) {
-      size[1] = min(max(longest / kPagedTailCuts, kPagedTailBlock), longest);
-      body = max(work - static_cast<long long>(ctas) * longest * kPagedTail / 8, 0LL);
+  // kPair: an item of the line: its sequence, head and number, and where it begins.
+  struct Place {
+    int src, head, number;
+    Sequence q;
+    Items it;
+    long long from;  // (found by position)
+  };
+  // By its number on the line, or by a position in it (neither goes back).
+  template <bool kNumber>
+  __device__ Place locate(long long want) {
+    while (want >= (kNumber ? items_before + __shfl_sync(0xffffffffu, items_upto, 31)
+                            : work_before + __shfl_sync(0xffffffffu, work_upto, 31)))
+      if (!advance()) break;
+    const long long to = kNumber ? items_before + items_upto : work_before + work_upto;
+    const int src = max(__ffs(__ballot_sync(0xffffffffu, to > want)) - 1, 0);
+    Place y;
+    y.src = src;
+    y.q.rows = __shfl_sync(0xffffffffu, s.rows, src);
+    y.q.row0 = __shfl_sync(0xffffffffu, s.row0, src);
+    y.q.length = __shfl_sync(0xffffffffu, s.length, src);
+    y.q.start = __shfl_sync(0xffffffffu, s.start, src);
+    y.it.count = __shfl_sync(0xffffffffu, it.count, src);
+    y.it.low = __shfl_sync(0xffffffffu, it.low, src);
+    y.it.high = __shfl_sync(0xffffffffu, it.high, src);
+    if (kNumber) {
+      const int in = static_cast<int>(want) - (items_before + __shfl_sync(0xffffffffu, items_upto, src) -
+                                               y.it.count * p.c.num_kv_heads);
+      y.head = in / y.it.count;
+      y.number = in - y.head * y.it.count;
+      y.from = 0;
     } else {
-      body = 0;
-      const int cuts = lane + 1;
-      int tiles = (longest + cuts - 1) / cuts;
-      const float per = 1.f / static_cast<float>(tiles);
-      float n = 0.f;
-#pragma unroll 1
-      for (int g = 0; g < groups(); ++g) {
-        Sequence x;
-        x.load(p, g * 32 + lane);
-        const int items = x.rows > 0 ? (x.rows + p.item_tokens - 1) / p.item_tokens : 0;
-        const int low = items ? x.tiles(p, min(p.item_tokens, x.rows)) : 0, high = items ? x.tiles(p, x.rows) : 0;
-#pragma unroll 1
-        for (unsigned left = __ballot_sync(0xffffffffu, items > 0); left; left &= left - 1) {
-          const int from = __ffs(left) - 1;
-          const float k = static_cast<float>(__shfl_sync(0xffffffffu, items, from));
-          const float c0 = static_cast<float>(__shfl_sync(0xffffffffu, low, from)) * per;
-          const float c1 = static_cast<float>(__shfl_sync(0xffffffffu, high, from)) * per;
-          n += k * 0.5f * (ceilf(c0 - 1e-3f) + ceilf(c1 - 1e-3f));
-        }
+      const long long work = y.it.before(y.it.count);
+      const long long first = work_before + __shfl_sync(0xffffffffu, work_upto, src) - work * p.c.num_kv_heads;
+      y.head = static_cast<int>(quotient(want - first, work));
+      const long long in = want - first - y.head * work;
+      int at = 0, n = y.it.count;  // it is one of these
+      while (n > 1) {
+        const int step = (n + 31) / 32, mine = at + step * lane;
+        const unsigned ok = __ballot_sync(0xffffffffu, step * lane < n && y.it.before(mine) <= in);
+        const int k = 31 - __clz(ok);
+        at += step * k;
+        n = min(step, n - step * k);
       }
-      n *= static_cast<float>(heads);
-      float time = ceilf(n / static_cast<float>(ctas)) * (static_cast<float>(work) / n + kPagedPiece);
-      if (cuts > kPagedCuts || (cuts > 1 && (tiles < kPagedBlock || n > kPagedSlots))) time = INFINITY;
-      // the shortest; of equals the fewest pieces
-      float least = time;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
-      size[1] = __shfl_sync(0xffffffffu, tiles, __ffs(__ballot_sync(0xffffffffu, time == least)) - 1);
+      y.number = at;
+      y.from = first + y.head * work + y.it.before(at);
     }
-    // no more pieces than there is room for their results
-    for (;; size[1] += max(size[1] / 4, 1)) {
-      size[1] = min(size[1], longest);
-      before = shared_before = 0;
-      work_before = 0;
-      hold(0);
-      while (advance()) {
-      }
-      if (shared_before + __shfl_sync(0xffffffffu, shared_upto, 31) <= kPagedSlots || size[1] == longest) break;
-    }
-    if (group > 0) {
-      before = shared_before = 0;
-      work_before = 0;
-      hold(0);
-    }
+    return y;
+  }
+  // The tile of an item of n at which a run that ends `in` behind the item's
+  // beginning ends.  (No pieces of a few tiles.)
+  static __device__ int tile_at(long long in, int n) {
+    const long long k = in - kPagedPiece;
+    return k < kPagedLeast ? 0 : n - k < kPagedLeast ? n : static_cast<int>(k);
   }
 
+  // kPair: where items are many, each is a piece, taken in turn, but for the last ones:
+  // that work, or where items are few all, is shared in equal runs.
+  __device__ void plan() {
+    const int grid = static_cast<int>(gridDim.x);
+    hold(0);
+    int longest = it.high;
+    while (advance()) longest = max(longest, it.high);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    all = work_before + __shfl_sync(0xffffffffu, work_upto, 31);
+    const int items = items_before + __shfl_sync(0xffffffffu, items_upto, 31);
+    rewind();
+    if (all == 0) return;
+    runs = grid;
+    if (static_cast<long long>(kPagedFew) * longest * grid <= all) {
+      // An eighth of the longest item a CTA; of items that are nearly alike all behind
+      // the last full round, if that leaves many CTAs without one.
+      const long long most = longest + kPagedPiece;
+      long long tail = (grid * most + 7) / 8;
+      const int left = items % grid;
+      if (8 * all >= 7 * most * items && 4 * left < 3 * grid) tail = max(tail, left * most);
+      const Place y = locate<false>(max(all - tail, 0LL));
+      whole = items_before + __shfl_sync(0xffffffffu, items_upto, y.src) - (p.c.num_kv_heads - y.head) * y.it.count +
+              y.number;
+      body = y.from;
+      runs = kPagedRuns * grid;
+      rewind();
+    }
+    runs = clamp_to((all - body) / kPagedShare, 1, min(runs, kPagedSlots / 2));
+  }
+
+  // kPair: a ticket for find(), which need not wait for it then.
+  __device__ void take() {
+    if (!kPair || taken || at < end) return;
+    if (lane == 0) ticket = atomicAdd(p.next, 1);
+    taken = true;
+  }
   __device__ void start() {
     if (kPair) {
-      if (lane == 0) ticket = atomicAdd(p.next, 1);
+      take();
       plan();
-      ticket = __shfl_sync(0xffffffffu, ticket, 0);
     } else {
       hold(0);
       int n = __shfl_sync(0xffffffffu, upto, 31);
@@ -490,125 +482,108 @@ struct Finder {
         at = quotient(all * blockIdx.x, ctas);
         end = quotient(all * (blockIdx.x + 1), ctas);
       }
-      if (group > 0) {
-        before = 0;
-        hold(0);
-      }
+      rewind();
     }
   }
 
   // Into *x by lane 0; false: there is none.
-  __device__ bool find(Piece* x) {
-    const int heads = kPair ? 1 : p.c.num_kv_heads;  // that `mine` counts one of
-    const long long want = kPair ? ticket : at;
-    if (!kPair && at >= end) return false;
-    while (want >= static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, 31)) * heads)
-      if (!advance()) return false;
-    const unsigned over = __ballot_sync(0xffffffffu, static_cast<long long>(before + upto) * heads > want);
-    const int src = __ffs(over) - 1;
-    Sequence q;
-    q.rows = __shfl_sync(0xffffffffu, s.rows, src);
-    q.row0 = __shfl_sync(0xffffffffu, s.row0, src);
-    q.length = __shfl_sync(0xffffffffu, s.length, src);
-    q.start = __shfl_sync(0xffffffffu, s.start, src);
-    const int count = __shfl_sync(0xffffffffu, mine, src);
-    const long long first = static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, src) - count) * heads;
-    const int in_seq = static_cast<int>(want - first);
+  __device__ bool find(Piece* x) { return kPair ? find_chunk(x) : find_single(x); }
+
+  __device__ bool find_chunk(Piece* x) {
     Piece y;
-    y.go = 1;
-    y.first = want == 0;
-    y.seq = group * 32 + src;
-    y.length = q.length;
-    y.rows = q.rows;
-    y.start = q.start;
-    if (kPair) {
-      Heads r;
-      r.whole = __shfl_sync(0xffffffffu, h.whole, src);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        r.pieces[i] = __shfl_sync(0xffffffffu, h.pieces[i], src);
-        r.shared[i] = __shfl_sync(0xffffffffu, h.shared[i], src);
+    Place i;
+    int from, to, most[2];  // tiles of the item
+    long long next = 0;  // where on the line the item after it begins
+    for (;;) {
+      y.first = 0;
+      if (at >= end) {
+        take();
+        const int n = __shfl_sync(0xffffffffu, ticket, 0);
+        taken = false;
+        if (n >= whole + runs) return false;
+        y.first = n == 0;
+        run = n - whole;
+        if (run >= 0) {
+          at = body + quotient((all - body) * run, runs);
+          end = body + quotient((all - body) * (run + 1), runs);
+        }
       }
-      const int in_body = r.whole * r.pieces[0];
-      const bool cut = in_seq >= in_body;
-      const int per = cut ? r.pieces[1] : r.pieces[0], at_head = (cut ? in_seq - in_body : in_seq) / per;
-      int rest = (cut ? in_seq - in_body : in_seq) - at_head * per;
-      y.head = at_head + (cut ? r.whole : 0);
-      y.size = cut ? size[1] : size[0];
-      y.base = shared_before + __shfl_sync(0xffffffffu, shared_upto - h.all_shared(p.c.num_kv_heads), src) +
-               (cut ? r.whole * r.shared[0] + at_head * r.shared[1] : at_head * r.shared[0]);
-      const Blocks b = blocks_of(p, q, y.size);
-      int block = 0, f = 0, slots = 0;  // slots: of shared items' pieces before the block
-      const int f1 = b.first(p, q, 1);
-      for (;; ++block) {
-        f = b.first(p, q, block);
-        if (rest < b.items - f) break;
-        rest -= b.items - f;
-        slots += b.items - (block == 0 ? f1 : f);
-      }
-      const int t = b.items - 1 - rest;  // those that see most first
-      const int token = t * p.item_tokens;
-      y.item = t;
-      y.row0 = q.row0 + token;
-      y.tokens = min(p.item_tokens, q.rows - token);
-      y.pos0 = q.start + token;
+      i = run < 0 ? locate<true>(whole + run) : locate<false>(at);
+      const int token = (i.it.count - 1 - i.number) * p.item_tokens;
+      y.row0 = i.q.row0 + token;
+      y.tokens = min(p.item_tokens, i.q.rows - token);
+      y.pos0 = i.q.start + token;
       const int tokens_a = min(p.item_tokens / 2, y.tokens);
-      const int most[2] = {q.tiles(p, token + tokens_a), q.tiles(p, token + y.tokens)};
-      y.tile0 = block * y.size;
-      const int to = min(most[1], y.tile0 + y.size);
-      y.tiles[0] = max(min(most[0], to) - y.tile0, 0);
-      y.tiles[1] = y.tokens > tokens_a ? to - y.tile0 : 0;
-      for (int i = 0; i < 2; ++i) y.pieces[i] = (most[i] + y.size - 1) / y.size;
-      y.slot = y.base + slots + t - (block == 0 ? f1 : f);
-      y.ticket = y.base + t - f1;
-    } else {
-      const int head = in_seq / count, rest = in_seq - head * count;
-      y.head = head;
-      y.item = 0;
-      y.row0 = q.row0;
-      y.tokens = q.rows;
-      y.pos0 = q.start;
-      y.tile0 = rest;
-      const int n = static_cast<int>(min(static_cast<long long>(count - rest), end - at));
-      y.tiles[0] = n;
-      y.tiles[1] = 0;
-      const long long u0 = first + static_cast<long long>(head) * count;  // the unit's first tile
-      auto owner = [&](long long tile) { return static_cast<int>(quotient((tile + 1) * ctas - 1, all)); };
-      y.base = owner(u0);
-      y.pieces[0] = y.pieces[1] = owner(u0 + count - 1) - y.base + 1;
-      y.size = 0;
-      y.ticket = y.base;
-      y.slot = 2 * static_cast<int>(blockIdx.x) + (rest == 0);
-      at += n;
+      most[0] = i.q.tiles(p, token + tokens_a);
+      most[1] = i.q.tiles(p, token + y.tokens);
+      from = 0;
+      to = most[1];
+      if (run >= 0) {
+        next = i.from + i.it.before(i.number + 1) - i.it.before(i.number);
+        from = tile_at(at - i.from, most[1]);
+        if (end < next) to = tile_at(end - i.from, most[1]);
+        at = min(end, next);
+      }
+      if (from < to) break;
+    }
+    y.go = 1;
+    y.seq = group * 32 + i.src;
+    y.head = i.head;
+    y.length = i.q.length;
+    y.tile0 = from;
+    y.tiles[0] = max(min(most[0], to) - from, 0);
+    y.tiles[1] = y.tokens > p.item_tokens / 2 ? to - from : 0;
+    y.pieces[0] = y.pieces[1] = 1;
+    y.base = y.slot = 0;
+    if (run >= 0) {
+      // the runs that begin inside the item are consecutive: from tile kPagedLeast on,
+      // before the last kPagedLeast (and before the last that the first 128 rows see)
+      auto begun = [&](long long x) { return quotient((x - body) * runs + all - body - 1, all - body); };
+      const long long tile = i.from + kPagedPiece;
+      const long long past = min(tile + most[1] - kPagedLeast + 1, next);
+      const long long first = begun(tile + kPagedLeast);
+      const int inside = static_cast<int>(max(begun(past) - first, 0LL));
+      y.pieces[1] = inside + 1;
+      y.pieces[0] = min(static_cast<int>(max(begun(min(past, tile + most[0])) - first, 0LL)), inside) + 1;
+      y.base = inside ? static_cast<int>(first) - 1 : run;
+      y.slot = 2 * run + (from == 0);
     }
     if (lane == 0) *x = y;
-    if (kPair) {
-      if (lane == 0) ticket = atomicAdd(p.next, 1);
-      ticket = __shfl_sync(0xffffffffu, ticket, 0);
-    }
     return true;
   }
-};
 
-// kPair: the slots of an item's pieces, in order.
-struct Slots {
-  const PagedAttendParams& p;
-  const Piece& x;
-  int k = 0, at = 0, f1;
-  Sequence s;
-  __device__ Slots(const PagedAttendParams& p_, const Piece& x_) : p(p_), x(x_) {
-    s.rows = x.rows;
-    s.length = x.length;
-    s.start = x.start;
-    f1 = blocks_of(p, s, x.size).first(p, s, 1);
-  }
-  __device__ long long next() {
-    const Blocks b = blocks_of(p, s, x.size);
-    const int f = k == 0 ? f1 : b.first(p, s, k);
-    const int r = x.base + at + x.item - f;
-    at += b.items - f;
-    ++k;
-    return r;
+  __device__ bool find_single(Piece* x) {
+    const int heads = p.c.num_kv_heads;  // that `mine` counts one of
+    if (at >= end) return false;
+    while (at >= static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, 31)) * heads)
+      if (!advance()) return false;
+    const unsigned over = __ballot_sync(0xffffffffu, static_cast<long long>(before + upto) * heads > at);
+    const int src = __ffs(over) - 1;
+    const int count = __shfl_sync(0xffffffffu, mine, src);
+    const long long first = static_cast<long long>(before + __shfl_sync(0xffffffffu, upto, src) - count) * heads;
+    const int in_seq = static_cast<int>(at - first);
+    const int head = in_seq / count, rest = in_seq - head * count;
+    Piece y;
+    y.go = 1;
+    y.first = at == 0;
+    y.seq = group * 32 + src;
+    y.length = __shfl_sync(0xffffffffu, s.length, src);
+    y.head = head;
+    y.row0 = __shfl_sync(0xffffffffu, s.row0, src);
+    y.tokens = __shfl_sync(0xffffffffu, s.rows, src);
+    y.pos0 = __shfl_sync(0xffffffffu, s.start, src);
+    y.tile0 = rest;
+    const int n = static_cast<int>(min(static_cast<long long>(count - rest), end - at));
+    y.tiles[0] = n;
+    y.tiles[1] = 0;
+    const long long u0 = first + static_cast<long long>(head) * count;  // the unit's first tile
+    auto owner = [&](long long tile) { return static_cast<int>(quotient((tile + 1) * ctas - 1, all)); };
+    y.base = owner(u0);
+    y.pieces[0] = y.pieces[1] = owner(u0 + count - 1) - y.base + 1;
+    y.slot = 2 * static_cast<int>(blockIdx.x) + (rest == 0);
+    at += n;
+    if (lane == 0) *x = y;
+    return true;
   }
 };
 
@@ -678,15 +653,19 @@ __device__ void load_role(const Cta& c) {
     q_phase ^= 1u << buffer;
     return true;
   };
-  bool ok = true;
-  for (int n = 0; ok; ++n) {
-    if (!c.wait_warp(c.m->pempty[n % kRing], ((n / kRing) & 1) ^ 1)) break;
+  bool found = false;
+  auto find = [&](int n) {
+    if (!c.wait_warp(c.m->pempty[n % kRing], ((n / kRing) & 1) ^ 1)) return false;
     Piece& x = c.m->ring[n % kRing];
-    const bool found = go && f.find(&x);
+    found = go && f.find(&x);
     if (!found && lane == 0) x.go = 0;
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&c.m->pfull[n % kRing]));
-    if (!found) break;
+    return true;
+  };
+  bool ok = find(0);
+  for (int n = 0; ok && found; ++n) {
+    const Piece& x = c.m->ring[n % kRing];
     const int tiles = max(x.tiles[0], x.tiles[1]), first = x.tile0;
     int now = look_up(x, first), next = tiles > 1 ? look_up(x, first + 1) : 0;
     ok = load_tile(x, p.map_k, first, now, c.m->kfull[n % kRing], kTileBytes2);
@@ -694,6 +673,7 @@ __device__ void load_role(const Cta& c) {
     for (int t = 0; ok && t < S::kQTiles; ++t)
       if (x.tiles[t]) ok = load_q(x, t, kPair ? t : n % p.q_buffers);
     for (int j = 0; ok && j < tiles; ++j) {
+      if (j == max(tiles - kAhead - kTicketAhead, 0)) f.take();
       const int after = j + 2 < tiles ? look_up(x, first + j + 2) : 0;
       const bool more = j + 1 < tiles;
       uint64_t& full = c.m->full[count % kRing];
@@ -705,7 +685,11 @@ __device__ void load_role(const Cta& c) {
       count += ok && !more;
       now = next;
       next = after;
+      // (kPair: so early that the piece's first tiles are not late, so late that the
+      // CTA that is through first takes it)
+      if (kPair && ok && j == max(tiles - 1 - kAhead, 0)) ok = find(n + 1);
     }
+    if (!kPair && ok) ok = find(n + 1);
   }
   // No copy, and no arrival that a stage or Q tile is free again, may come after
   // this CTA has ended.  (A stopped CTA has only its copies to wait for.)
@@ -964,13 +948,13 @@ __device__ void fix_role(const Cta& c) {
 
 // ---------------------------------------------------------------- softmax
 // 32 channels of a row's output, over the sum of its exponentials (`up`: up_of()).
-template <bool kBf16>
+template <bool kBf16, int kN>
 __device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, float l, float up,
-                                               const uint32_t (&o)[32]) {
+                                               const uint32_t (&o)[kN]) {
   const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
   const float inv = up / l;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < kN / 16; ++i) {
     uint32_t w[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -1003,63 +987,57 @@ template <bool kBf16>
 __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piece& x, int tile, int row, int token,
                                           int head, bool valid) {
   const int pieces = x.pieces[tile];
-  float weight[kPagedCuts];
-  int slot[kPagedCuts];
+  auto read = [&](int k) {
+    return k < pieces ? __ldcg(p.part_ml + x.slot_of(k) * p.part_rows + row) : make_float2(0.f, 0.f);
+  };
+  // (equal infinities: 1, so that they and NaN go on into the sum)
+  auto weight = [](float2 ml, float top) { return ml.y == 0.f ? 0.f : ml.x == top ? 1.f : exp2f(ml.x - top); };
   float top = -INFINITY, sum = 0.f;
-  Slots slots(p, x);
-#pragma unroll 1
-  for (int k = 0; k < pieces; ++k) slot[k] = slots.next();
 #pragma unroll 1
   for (int k0 = 0; k0 < pieces; k0 += 4) {
     float2 ml[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      ml[u] = k0 + u < pieces ? __ldcg(p.part_ml + static_cast<long long>(slot[k0 + u]) * p.part_rows + row)
-                              : make_float2(0.f, 0.f);
-    // (the largest so far may grow: weights and sum follow)
+    for (int u = 0; u < 4; ++u) ml[u] = read(k0 + u);
+    // (the largest so far may grow: the sum follows)
     float now = top;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (ml[u].y != 0.f) now = fmaxf(now, ml[u].x);
-    const float f = now == top ? 1.f : exp2f(top - now);
-    sum *= f;
-#pragma unroll 1
-    for (int k = 0; k < k0; ++k) weight[k] *= f;
+    sum *= now == top ? 1.f : exp2f(top - now);
     top = now;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (k0 + u < pieces) {
-        // (equal infinities: 1, so that they and NaN go on into the sum)
-        const float w = ml[u].y == 0.f ? 0.f : ml[u].x == top ? 1.f : exp2f(ml[u].x - top);
-        weight[k0 + u] = w;
-        sum += ml[u].y == 0.f ? 0.f : ml[u].y * w;
-      }
+    for (int u = 0; u < 4; ++u) sum += ml[u].y == 0.f ? 0.f : ml[u].y * weight(ml[u], top);
   }
   uint16_t* to = p.out + (x.row0 + token) * p.o_token + head * p.o_head;
+  // 32 channels, two pieces at a time (four, or the next on their way meanwhile: registers
+  // spill, or code that runs once is longer; both slower)
+  const float4* rows = reinterpret_cast<const float4*>(p.part_o) + row;
 #pragma unroll 1
   for (int part = 0; part < 4; ++part) {
     uint32_t o[32] = {};
 #pragma unroll 1
-    for (int k0 = 0; k0 < pieces; k0 += 4) {
-      float4 v[4][8];
-      float w[4];
+    for (int k0 = 0; k0 < pieces; k0 += 2) {
+      float2 ml[2];
+      float4 v[2][8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        w[u] = k0 + u < pieces ? weight[k0 + u] : 0.f;
-        const float4* from = reinterpret_cast<const float4*>(p.part_o) + row +
-                             (static_cast<long long>(slot[min(k0 + u, pieces - 1)]) * 32 + part * 8) * p.part_rows;
+      for (int u = 0; u < 2; ++u) {
+        ml[u] = read(k0 + u);
+        const float4* from = rows + (x.slot_of(min(k0 + u, pieces - 1)) * 32 + 8 * part) * p.part_rows;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = w[u] != 0.f ? __ldcg(from + i * p.part_rows) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = 0; c < 8; ++c) v[u][c] = __ldcg(from + c * p.part_rows);
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const float w = weight(ml[u], top);
+        if (w != 0.f)  // (0 times what is not finite)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[4 * i] = __float_as_uint(fmaf(w[u], v[u][i].x, __uint_as_float(o[4 * i])));
-          o[4 * i + 1] = __float_as_uint(fmaf(w[u], v[u][i].y, __uint_as_float(o[4 * i + 1])));
-          o[4 * i + 2] = __float_as_uint(fmaf(w[u], v[u][i].z, __uint_as_float(o[4 * i + 2])));
-          o[4 * i + 3] = __float_as_uint(fmaf(w[u], v[u][i].w, __uint_as_float(o[4 * i + 3])));
-        }
+          for (int c = 0; c < 8; ++c) {
+            o[4 * c] = __float_as_uint(fmaf(w, v[u][c].x, __uint_as_float(o[4 * c])));
+            o[4 * c + 1] = __float_as_uint(fmaf(w, v[u][c].y, __uint_as_float(o[4 * c + 1])));
+            o[4 * c + 2] = __float_as_uint(fmaf(w, v[u][c].z, __uint_as_float(o[4 * c + 2])));
+            o[4 * c + 3] = __float_as_uint(fmaf(w, v[u][c].w, __uint_as_float(o[4 * c + 3])));
+          }
+      }
     }
     if (valid) write_channels<kBf16>(p, to + 32 * part, sum, up_of<kBf16>(x.length), o);
   }
@@ -1084,11 +1062,10 @@ __device__ __forceinline__ bool take_ticket(int* ticket, int pieces) {
 template <bool kBf16>
 __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x, int first, int rows) {
   const int lane = threadIdx.x & 31, pieces = x.pieces[0];
-  auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * x.base + 1 : 2 * (x.base + k)); };
 #pragma unroll 1
   for (int row = first; row < rows; row += 4) {
     auto read = [&](int k) {
-      return k < pieces ? __ldcg(p.part_ml + slot(k) * p.part_rows + row) : make_float2(0.f, 0.f);
+      return k < pieces ? __ldcg(p.part_ml + x.slot_of(k) * p.part_rows + row) : make_float2(0.f, 0.f);
     };
     float top = -INFINITY, sum = 0.f;
 #pragma unroll 1
@@ -1117,7 +1094,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
           f[u] = __shfl_sync(0xffffffffu, w, (k + u) & 31);
           v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (k + u < count && f[u] != 0.f)
-            v[u] = __ldcg(reinterpret_cast<const float4*>(p.part_o) + (slot(k0 + k + u) * p.part_rows + row) * 32 + lane);
+            v[u] = __ldcg(reinterpret_cast<const float4*>(p.part_o) + (x.slot_of(k0 + k + u) * p.part_rows + row) * 32 + lane);
           else
             f[u] = 0.f;
         }
@@ -1224,7 +1201,7 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
   if (row.valid) p.part_ml[static_cast<long long>(y.slot) * p.part_rows + at] = make_float2(ref, l);
   __threadfence();
   __syncwarp();
-  if (kPair && take_ticket(p.tickets + (y.ticket * 2 + tile) * 4 + warp, y.pieces[tile]))
+  if (kPair && take_ticket(p.tickets + (y.base * 2 + tile) * 4 + warp, y.pieces[tile]))
     join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid);
 }
 
@@ -1379,7 +1356,7 @@ __device__ void output_role(const Cta& c, uint32_t tmem) {
       if (!c.wait_here(c.m->stored, stored)) return;
       stored ^= 1;
       __threadfence();
-      if (take_ticket(c.p.tickets + y.ticket * 8 + warp, y.pieces[0])) join<kBf16>(c.p, y, warp, y.tokens * c.p.group);
+      if (take_ticket(c.p.tickets + y.base * 8 + warp, y.pieces[0])) join<kBf16>(c.p, y, warp, y.tokens * c.p.group);
     }
   }
 }
@@ -1437,15 +1414,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attend_kernel(const __grid_
   pdl_wait();
   const uint32_t tmem = warp == kLoadWarp ? 0 : m->tmem;
   if (warp >= kSoftWarp && warp < kSoftWarp + 8) {
-    // registers for the softmax, which holds a row of logits (256 x 208 + 128 x 88
-    // of the launch's 384 x 168)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // registers for the softmax, which holds a row of logits: of the launch's 384 x
+    // 168 kPair 256 x 200 and 128 x 104 (finding pieces spills with 88: 3 % of a
+    // prompt), single 256 x 208 and 128 x 88
+    if constexpr (kPair)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     if (kPair || warp < kSoftWarp + 4)
       softmax_role<kBf16, kPair>(c, tmem, (warp - kSoftWarp) / 4);
     else
       output_role<kBf16>(c, tmem);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if constexpr (kPair)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == kLoadWarp)
       load_role<kPair>(c);
     else if (warp == kFixWarp)

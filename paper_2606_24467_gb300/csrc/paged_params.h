@@ -66,23 +66,24 @@ cudaError_t launch_paged_gather(const PagedGatherParams& p, cudaStream_t s);
 
 constexpr int kPagedTile = 128;  // slots of a K or V tile, and rows of a tile of queries
 constexpr int kPagedMaxCtas = 160;
-// Chunks.  Where an item (two tiles of rows) is more than a kPagedFew-th of an SM's
-// share of the tiles, all are cut into blocks of slots: into 1 .. kPagedCuts, of at
-// least kPagedBlock tiles, as makes the shortest time if a piece costs as much as
-// kPagedPiece tiles beside its own (501 tokens after 9000 to 16000: 171 us, 193 cut
-// in quarters of a share).  Else items are whole but for the last ones, kPagedTail
-// eighths of an item a CTA, in kPagedTailCuts or into blocks of kPagedTailBlock
-// tiles: 4096 tokens after 128K take 5000 us so and 5950 with all items whole, 8191
-// from the first on 380 and 393 (of 16 tiles each: 388).  The results of at most
-// kPagedSlots pieces wait to be joined.
+// Chunks.  All work is a line, an item (two tiles of rows of a KV head) after another;
+// each takes its tiles and kPagedPiece, what its beginning and end cost.  Where that is
+// less than kPagedFew of the longest items an SM, the line is cut into equal runs, one an
+// SM: 501 tokens after 9000 to 16000 take 148 us so, 172 with items cut into blocks of
+// slots that SMs take in turn; 777 after 3000 to 20000, four times, 537 and 605.
+// Else items are whole and taken in turn, as CTAs that run together then read the same
+// tiles (4096 tokens after 128K: 5000 us, in runs 6100), but for the last ones, in
+// kPagedRuns runs an SM: 8191 tokens from the first on 368 us so, 380 all in runs.
+// No piece has fewer than kPagedLeast tiles of an item that has more (16: 160 us for the
+// first), no run less than kPagedShare of the line.  The results of at most kPagedSlots
+// pieces, two a run, wait to be joined.
 constexpr int kPagedFew = 2;
-constexpr int kPagedCuts = 24;
-constexpr int kPagedPiece = 6;
-constexpr int kPagedBlock = 8;
-constexpr int kPagedTail = 4;
-constexpr int kPagedTailCuts = 5;
-constexpr int kPagedTailBlock = 40;
+constexpr int kPagedPiece = 4;
+constexpr int kPagedLeast = 4;
+constexpr int kPagedShare = 12;
+constexpr int kPagedRuns = 2;
 constexpr int kPagedSlots = 608;
+static_assert(kPagedShare > kPagedPiece + kPagedLeast, "a run has a piece");
 // Workspace header: status word, the word that says that a call has stopped, the
 // next ticket and the CTAs done; behind it the counters of items in pieces, one
 // for each 32 rows.  Every call leaves them zero.

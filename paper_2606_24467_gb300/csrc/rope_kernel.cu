@@ -60,8 +60,8 @@ __device__ __forceinline__ int pair_of(int l, int i) {
 }
 
 // The four lanes that hold the same pairs, of four heads, compute two of their
-// angles each and hand them on (all of them: 31 instead of 24 us for 8191 tokens of
-// 28 and 4 heads).
+// angles each and hand them on.  (8191 tokens of 28 and 4 heads: 23.7 us, with loads
+// that start before the angles; 29.6 before both.)
 template <int kLayout>
 __device__ __forceinline__ void angles_at(const RopeTable& r, int position, bool backward, int lane, Angles& a) {
   constexpr int kEach = kPairsLane * kLanes / 32;  // 2

@@ -365,6 +365,31 @@ def test_chunks_in_pieces_whose_tiles_see_different_blocks():
     run([9000] + [150] * 20, [1] + [100] * 20, 8, 2)
 
 
+@pytest.mark.parametrize("lengths, rows, hq, h, start, causal", [
+    ([60000], [140], 4, 1, None, True),                        # three items, each in some fifty pieces
+    ([20000, 300, 40, 5000], [200, 150, 0, 129], 7, 1, None, True),
+    ([9000, 9000, 9000], [300, 300, 300], 4, 2, [-200, 9000, 100], True),
+    ([9000, 1000], [300, 200], 4, 4, None, False),
+    ([700] * 40, [300] * 40, 8, 4, None, True),                # items that are whole, and few tiles
+    ([3000] * 10, [256] * 10, 32, 8, None, True),              # alike: two rounds, and 16 items in runs
+    ([2000] * 9 + [1, 300] * 20, [400] * 9 + [1, 130] * 20, 16, 4, None, True),
+    ([130] * 70, [129] * 70, 2, 2, None, True),                # three lanes' worth of sequences, a tile or two each
+])
+def test_chunks_in_runs_and_in_whole_items(lengths, rows, hq, h, start, causal):
+    """What is cut into runs, where runs end, and how many share an item."""
+    dtype = BF if len(lengths) % 2 else HF
+    cache = make(lengths, h, 64, dtype)
+    cu = packed(rows)
+    q = queries(int(cu[-1]), hq, dtype)
+    first = None if start is None else ints(start)
+    ws = ckv.paged_workspace(cache, hq, max(rows))
+    out, lse, status = attend(cache, q, cu, first, causal, ws=ws)
+    assert status == 0
+    check(cache, q, out, lse, cu, first, causal, sequences=range(0, len(lengths), 1 + len(lengths) // 12))
+    again, lse2, status = attend(cache, q, cu, first, causal, ws=ws)
+    assert status == 0 and torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 def test_a_whole_prompt():
     run([3000], [3000], 4, 1, 128, BF)
 
