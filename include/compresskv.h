@@ -564,8 +564,9 @@ enum {
                                stretched by factor, the shortest stays (rot_dim > 2) */
   CKV_ROPE_WAVES = 3,       /* by the turns t_i = original_length f_i / 2 pi of a wave: keep_i =
                                (t_i - low) / (high - low) within 0..1, f_i (keep_i + (1 - keep_i) / factor) */
-  CKV_ROPE_RAMP = 4         /* likewise, but keep_i falls linearly in i between the channels (rounded
-                               outwards to whole ones) whose waves make `high` and `low` turns */
+  CKV_ROPE_RAMP = 4         /* likewise, but keep_i falls linearly in i between the i (rounded outwards to
+                               whole numbers, the one at least 0, the other at most rot_dim - 1, which
+                               may lie past the last pair) whose waves make `high` and `low` turns */
 };
 
 /* Host only: frequencies (double [rot_dim / 2], radians a position).  factor >= 1

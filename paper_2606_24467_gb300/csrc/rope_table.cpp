@@ -46,7 +46,9 @@ int compresskv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, d
     if (!(base > 1.0)) return CKV_ERR_INVALID_ARG;
     const double per = rot_dim / (2.0 * std::log(base));
     first = std::fmax(std::floor(per * std::log(original_length / (kTwoPi * high))), 0.0);
-    last = std::fmin(std::ceil(per * std::log(original_length / (kTwoPi * low))), pairs - 1.0);
+    // (at most the last channel's number, not the last pair's: a pair of fewer turns
+    // than `low` need not exist)
+    last = std::fmin(std::ceil(per * std::log(original_length / (kTwoPi * low))), rot_dim - 1.0);
     if (!(last > first)) last = first + 1e-3;  // one step
   }
   for (int i = 0; i < pairs; ++i) {
