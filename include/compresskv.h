@@ -544,9 +544,11 @@ int compresskv_q4_evict(const ckv_q4_cache* c, int32_t budget, const int32_t* bu
  * (2i, 2i + 1) where interleaved; at position m
  *   a' = scale (a cos(m f_i) - b sin(m f_i)),
  *   b' = scale (a sin(m f_i) + b cos(m f_i)).
- * The other channels are copied.  Angles are exact: a frequency is held as
- * turns a position in units of 2^-64, so that m f_i is right to 2^-32 of a turn
- * at every 32-bit position; cosine, sine and products are fp32, rounded once. */
+ * The other channels are copied.  A frequency is held as turns a position in
+ * units of 2^-64, made in double: m f_i is right to 2^-31 + |m f_i| 2^-55 of a turn
+ * (2^-30 at positions up to 2^24 where f_i is at most 1), and is then rounded to fp32,
+ * as half turns in -1 .. 1, by at most 2^-26 of a turn.  Cosine, sine and products are
+ * fp32, and the result is rounded once. */
 typedef struct ckv_rope {
   int32_t rot_dim;          /* even, 2..128 */
   int32_t interleaved;      /* non-zero: pairs (2i, 2i + 1) */

@@ -2,8 +2,8 @@
 //
 // A frequency f (radians a position) is held as f / 2 pi turns modulo one, in
 // units of 2^-64: the product with a 32-bit position, modulo 2^64, is then the
-// angle with no rounding but that of the table, 2^-65 of a turn (and of f's own
-// 53 bits) a position.
+// angle with no rounding but that of the table, 2^-64 of a turn and |f| 2^-55 (the
+// quotient is a double) a position.
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -77,10 +77,10 @@ int compresskv_rope_init(ckv_rope* r, int32_t rot_dim, int32_t interleaved, cons
   r->interleaved = interleaved != 0;
   r->scale = s;
   for (int i = 0; i < rot_dim / 2; ++i) {
-    const double t = frequencies[i] / kTwoPi;
-    double part = t - std::floor(t);            // 0 .. 1 (1: a tiny negative t, rounded)
-    part = std::ldexp(part, 64);
-    r->turns[i] = part >= 18446744073709551616.0 ? 0 : static_cast<uint64_t>(part);
+    // (negated as an integer: one minus a small part keeps fewer of its bits)
+    const double t = std::fabs(frequencies[i]) / kTwoPi;
+    const uint64_t part = static_cast<uint64_t>(std::ldexp(t - std::floor(t), 64));
+    r->turns[i] = frequencies[i] < 0.0 ? 0 - part : part;
   }
   return CKV_OK;
 }

@@ -1,5 +1,6 @@
 """Rotary frequencies and tables against their formulas, written out (no GPU)."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -37,3 +38,33 @@ def test_ramp_by_its_formula(rot_dim, base, factor, length, low, high):
     got = ckv.rope_frequencies(rot_dim, base, "ramp", factor, length, low, high)
     # (logarithms and powers of two libraries: some units in the last place of exponents up to 14)
     np.testing.assert_allclose(got, ramp(rot_dim, base, factor, length, low, high), rtol=1e-13)
+
+
+def turns_exactly(f):
+    """f / 2 pi modulo 1 in units of 2^-64, as a rational (pi by Machin's formula)."""
+    bits = 400
+
+    def atan_of_inverse(x):
+        term = total = (1 << bits) // x
+        for n in range(3, bits, 2):
+            term //= -x * x
+            total += term // n
+        return total
+
+    two_pi = 8 * (4 * atan_of_inverse(5) - atan_of_inverse(239))
+    return Fraction(f) * (1 << bits) * (1 << 64) / two_pi % (1 << 64)
+
+
+@pytest.mark.parametrize("frequencies", [
+    [1.0, -1.0, 100.0, -100.0, 1048575.7, -1048575.7, 2.0 ** 20, 0.0],
+    [1e-6, -1e-6, 1e-17, -1e-17, 2 * math.pi, -2 * math.pi, 1e-300, -5e-324],
+    [3.0 ** -i for i in range(16, 24)],
+    list(500000.0 ** (-np.arange(64) / 64.0)),
+])
+def test_tables_hold_turns(frequencies):
+    rope = ckv.Rope(2 * len(frequencies), frequencies=np.array(frequencies))
+    for f, t in zip(frequencies, rope.struct.turns):
+        gap = abs(int(t) - turns_exactly(f))
+        # a quotient of doubles, 2 pi rounded: 1.5 * 2^-53 of it, at most |f| 2^-55 (1.5 < 2 pi / 4); and cut to units
+        bound = abs(Fraction(f)) / 4 * Fraction(1, 1 << 53) * (1 << 64) + 1
+        assert min(gap, (1 << 64) - gap) <= bound, (f, float(gap), float(bound))
