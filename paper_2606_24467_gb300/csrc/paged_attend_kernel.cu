@@ -1029,7 +1029,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const float w = weight(ml[u], top);
-        if (w != 0.f)  // (0 times what is not finite)
+        if (k0 + u < pieces)  // (a weight of 0 too: times what is not finite it is not 0)
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
             o[4 * c] = __float_as_uint(fmaf(w, v[u][c].x, __uint_as_float(o[4 * c])));
@@ -1093,10 +1093,8 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
         for (int u = 0; u < 8; ++u) {
           f[u] = __shfl_sync(0xffffffffu, w, (k + u) & 31);
           v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (k + u < count && f[u] != 0.f)
+          if (k + u < count)  // (whatever its weight, as in join_rows)
             v[u] = __ldcg(reinterpret_cast<const float4*>(p.part_o) + (x.slot_of(k0 + k + u) * p.part_rows + row) * 32 + lane);
-          else
-            f[u] = 0.f;
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) {

@@ -1,0 +1,37 @@
+"""Attention over the paged cache where numbers are extreme: against float64
+(oracle/paged_oracle.py), or against what the formula gives exactly."""
+import pytest
+import torch
+
+import paper_2606_24467_gb300 as ckv  # noqa: F401  (the tests' helpers use it)
+from test_gpu_paged import BF, HF, NAN, attend, check, make, queries
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_at(cache, length, s=0):
+    """Page and row of a sequence's first slots, to index the pools by."""
+    slot = torch.arange(length, device="cuda")
+    page = cache.page_size
+    return cache.table[s].long()[slot // page], slot % page
+
+
+@pytest.mark.parametrize("rows, length", [(1, 100), (1, 40000), (90, 40000), (200, 300), (200, 40000)])
+def test_weights_that_vanish_carry_what_is_not_finite(rows, length):
+    """Half of the slots 181 nats below the others, one of them with a NaN or an infinity
+    in V: it reaches the output (0 times it is NaN), whether a unit is one piece or several that are joined."""
+    cache = make([length], 2, 64)
+    at = rows_at(cache, length)
+    sign = torch.where(torch.arange(length, device="cuda") < length // 2, -1.0, 1.0)
+    cache.k_pages[at] = sign[:, None, None].to(BF).expand(length, 2, 128)
+    q = torch.full((rows, 8, 128), 8.0, dtype=BF, device="cuda")
+    clean, clean_lse, _ = attend(cache, q)
+    assert torch.isfinite(clean).all()
+    slot = min(20, length - rows)  # seen by every token
+    page, row = at[0][slot], at[1][slot]
+    for value in (NAN, float("inf")):
+        cache.v_pages[page, row, 1, 77] = value
+        out, lse, _ = attend(cache, q)
+        assert not torch.isfinite(out[:, 4:, 77]).any()  # (an infinity where a token sees no other slots)
+        out[:, 4:, 77] = clean[:, 4:, 77]
+        assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
