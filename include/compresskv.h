@@ -710,7 +710,8 @@ int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, voi
  * Query token i of sequence s stands at slot start[s] + i; start: optional
  *   device int32 [batch]; NULL: the sequence's newest slots, lengths[s] - rows.
  *   It sees the slots in use up to its own (causal) or all in use.  A token that
- *   sees none gives out = 0 and lse = -infinity.
+ *   sees none gives out = 0 and lse = -infinity; one that sees slots, all with a
+ *   logit of -infinity, gives NaN (0 / 0) and lse = -infinity.
  * lse: optional device float [num_q_heads][rows]: with equal rows a sequence,
  *   the last W of them are lse_win of compresskv_compress_layer_lse with
  *   lse_batch_stride = rows a sequence and lse_head_stride = rows.

@@ -948,10 +948,11 @@ __device__ void fix_role(const Cta& c) {
 
 // ---------------------------------------------------------------- softmax
 // 32 channels of a row's output, over the sum of its exponentials (`up`: up_of()).
+// `none`: the row sees no slot.  (One that does may have a sum of 0 or NaN, and gives
+// NaN.)
 template <bool kBf16, int kN>
-__device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, float l, float up,
+__device__ __forceinline__ void write_channels(const PagedAttendParams& p, uint16_t* to, bool none, float l, float up,
                                                const uint32_t (&o)[kN]) {
-  const bool none = l == 0.f;  // (a row with NaN has a sum, NaN)
   const float inv = up / l;
 #pragma unroll
   for (int i = 0; i < kN / 16; ++i) {
@@ -1009,6 +1010,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
     for (int u = 0; u < 4; ++u) sum += ml[u].y == 0.f ? 0.f : ml[u].y * weight(ml[u], top);
   }
   uint16_t* to = p.out + (x.row0 + token) * p.o_token + head * p.o_head;
+  const bool none = limit_of(p, x.pos0 + token, x.length) == 0;
   // 32 channels, two pieces at a time (four, or the next on their way meanwhile: registers
   // spill, or code that runs once is longer; both slower)
   const float4* rows = reinterpret_cast<const float4*>(p.part_o) + row;
@@ -1039,7 +1041,7 @@ __device__ __forceinline__ void join_rows(const PagedAttendParams& p, const Piec
           }
       }
     }
-    if (valid) write_channels<kBf16>(p, to + 32 * part, sum, up_of<kBf16>(x.length), o);
+    if (valid) write_channels<kBf16>(p, to + 32 * part, none, sum, up_of<kBf16>(x.length), o);
   }
   if (valid) write_lse(p, x.row0 + token, head, top, sum);
 }
@@ -1106,7 +1108,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
       }
     }
     const int token = row / p.group, head = x.head * p.group + row - token * p.group;
-    const bool none = sum == 0.f;
+    const bool none = limit_of(p, x.pos0 + token, x.length) == 0;
     const float inv = up_of<kBf16>(x.length) / sum;
     const long long row_at = x.row0 + token;
     reinterpret_cast<uint2*>(p.out + row_at * p.o_token + head * p.o_head)[lane] =
@@ -1114,7 +1116,7 @@ __device__ __forceinline__ void join(const PagedAttendParams& p, const Piece& x,
              : make_uint2(pack<kBf16>(acc.x * inv, acc.y * inv), pack<kBf16>(acc.z * inv, acc.w * inv));
     if (p.lse && lane == 0)
       p.lse[static_cast<long long>(head) * p.rows + row_at] =
-          none ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+          sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
   }
 }
 
@@ -1178,7 +1180,7 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
     }
     if (row.valid) {
       if (all) {
-        write_channels<kBf16>(p, to + 32 * part, l, up_of<kBf16>(y.length), o);
+        write_channels<kBf16>(p, to + 32 * part, row.limit == 0, l, up_of<kBf16>(y.length), o);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

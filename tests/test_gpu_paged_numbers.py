@@ -35,3 +35,22 @@ def test_weights_that_vanish_carry_what_is_not_finite(rows, length):
         assert not torch.isfinite(out[:, 4:, 77]).any()  # (an infinity where a token sees no other slots)
         out[:, 4:, 77] = clean[:, 4:, 77]
         assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+@pytest.mark.parametrize("rows, length", [(1, 5), (1, 40000), (90, 200), (200, 300), (200, 40000)])
+def test_logits_of_minus_infinity(rows, length):
+    """A token all of whose slots have a logit of -infinity has a sum of 0: its output is
+    NaN (0 / 0) and its log-sum-exp -infinity; tokens with another slot are not touched."""
+    cache = make([length], 2, 64)
+    at = rows_at(cache, length)
+    cache.k_pages[at[0], at[1], 1, 3] = -float("inf")
+    q = queries(rows, 8, BF).abs() + 0.25  # (no 0 times infinity)
+    out, lse, _ = attend(cache, q)
+    assert torch.isfinite(out[:, :4]).all() and torch.isfinite(lse[:4]).all()
+    assert torch.isnan(out[:, 4:]).all() and (lse[4:] == -float("inf")).all()
+    # the last slot, which the last token alone sees, as any other
+    cache.k_pages[at[0][-1], at[1][-1], 1, 3] = 1.0
+    out, lse, _ = attend(cache, q)
+    last = cache.v_pages[at[0][-1], at[1][-1], 1]
+    assert torch.equal(out[-1, 4:], last.expand(4, 128)) and torch.isfinite(lse[4:, -1]).all()
+    assert torch.isnan(out[:-1, 4:]).all() and (lse[4:, :-1] == -float("inf")).all()
