@@ -690,7 +690,8 @@ typedef struct ckv_paged_queries {
   int32_t rows_per_seq;     /* query tokens of every sequence, where cu_rows is NULL */
   const int32_t* cu_rows;   /* host [batch+1] */
   int32_t causal;           /* non-zero: a token sees the slots up to its own */
-  float scale;              /* softmax scale, at most 2^96; 0 selects 1/sqrt(head_dim) */
+  float scale;              /* softmax scale, at most 2^96 (logits with it are to stay below 2^127);
+                               0 selects 1/sqrt(head_dim) */
   int64_t q_token_stride, q_head_stride;     /* elements, multiples of 8, below 2^39; q's positive */
   int64_t out_token_stride, out_head_stride;
 } ckv_paged_queries;

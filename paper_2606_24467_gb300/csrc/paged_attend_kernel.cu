@@ -46,6 +46,7 @@ constexpr int kAhead = 4;                                   // tiles to load whe
 constexpr int kTicketAhead = 2;                             // and more when its ticket is taken
 constexpr int kDiagTiles = 3;                               // tiles that an item's rows see in part, at most
 constexpr float kGrowth = 8.f;                              // log2 of how far p may pass 1
+constexpr float kFar = 0x1p18f;                             // references from where fp32's steps in them count
 
 // A part of an item's slots, as the roles get it.
 struct Piece {
@@ -1205,6 +1206,11 @@ __device__ __forceinline__ void finish(const Cta& c, Reader& reader, const Piece
     join_rows<kBf16>(p, y, tile, at, row.token, row.head, row.valid);
 }
 
+// Whether a row's reference is so far from zero that logits are taken relative to it.
+__device__ __forceinline__ bool far_off(float m, float scale) {
+  return m > -INFINITY && fabsf(m * scale) > kFar;
+}
+
 template <bool kBf16, bool kPair>
 __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
   const PagedAttendParams& p = c.p;
@@ -1226,6 +1232,7 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
     const uint32_t o_addr = lanes + (2 + (kPair ? tile : reader.at & 1)) * kTile;
     const float down = down_of<kBf16>(x->length), up = up_of<kBf16>(x->length);
     float m = -INFINITY, l = 0.f;
+    bool far = false;  // (not for rows that are none, which may hold anything)
     for (int j = 0; j < n; ++j, ++count) {
       const int buffer = kPair ? tile : count & 1;
       if (!c.wait_here(c.m->sfull[buffer], (kPair ? count : count >> 1) & 1)) return;
@@ -1273,9 +1280,10 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
         const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]);
         if (!kPair && j > 0 && !c.wait_here(c.m->odone[0], (count - 1) & 1)) return;
         const bool grown = now > m && (m == -INFINITY || (now - m) * scale > kGrowth);
-        if (__any_sync(0xffffffffu, grown)) {
+        if (__any_sync(0xffffffffu, grown || far)) {
           const float f = grown ? ex2_approx((m - now) * scale) : 1.f;
           if (grown) m = now;
+          far = row.valid && far_off(m, scale);
           l *= f;
           if (j > 0) {
             tc_fence_after();
@@ -1293,7 +1301,17 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
               tmem_store16(o_addr + 16 * k, o);
             }
           }
-          ref = reference();
+          ref = far ? -down : reference();
+          // c z - c m with c m rounded is off by half of fp32's step in c m, the same for all
+          // of a row: nothing, until it takes p out of its type's range.  Far from zero p
+          // is made from z - m.
+          if (__any_sync(0xffffffffu, far)) {
+            const float by = far ? m : 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) s[k][i] = __float_as_uint(__uint_as_float(s[k][i]) - by);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) sum[i] = 0;
           exponentials(0, w, ref);
@@ -1321,8 +1339,8 @@ __device__ void softmax_role(const Cta& c, uint32_t tmem, int tile) {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&c.m->pready[buffer][1]));
     }
-    // (the reference as it entered, rounded beside `down`: the difference is exact)
-    const float ref = ((m == -INFINITY ? 0.f : m * scale) + down) - down;
+    // (the reference as it entered, rounded beside `down`)
+    const float ref = far ? m * scale : ((m == -INFINITY ? 0.f : m * scale) + down) - down;
     if (kPair) {
       if (!c.wait_here(c.m->odone[tile], o_count++ & 1)) return;
       finish<kBf16, true>(c, reader, *x, tile, o_addr, c.m->oempty[tile], row, ref, l);

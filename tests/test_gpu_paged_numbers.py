@@ -54,3 +54,35 @@ def test_logits_of_minus_infinity(rows, length):
     last = cache.v_pages[at[0][-1], at[1][-1], 1]
     assert torch.equal(out[-1, 4:], last.expand(4, 128)) and torch.isfinite(lse[4:, -1]).all()
     assert torch.isnan(out[:-1, 4:]).all() and (lse[4:, :-1] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype, size, scale", [(BF, 1.0, 2.0 ** 40), (BF, 1.0, 2.0 ** 96), (BF, 60000.0, 128 ** -0.5),
+                                                (HF, 1.0, 2.0 ** 30), (HF, 1.0, 2.0 ** 96),
+                                                (HF, 3000.0, 128 ** -0.5), (HF, 60000.0, 128 ** -0.5)])
+@pytest.mark.parametrize("rows, length", [(1, 300), (1, 9000), (200, 300), (200, 9000)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_logits_far_from_zero(dtype, size, scale, rows, length, sign):
+    """Where fp32's steps of a logit are more than 1 the slots with the largest one have
+    all the weight: one slot's V, bit by bit, or the average of two equal ones."""
+    cache = make([length], 1, 64, dtype)
+    at = rows_at(cache, length)
+    best, other = length // 3 if length > 2 * rows else 20, 7
+    k = cache.k_pages[at]
+    k[:] = 0.5 * size if sign > 0 else size
+    k[best] = size if sign > 0 else 0.5 * size
+    cache.k_pages[at] = k
+    gen = torch.Generator().manual_seed(0)
+    q = ((torch.rand((rows, 4, 128), generator=gen) * 0.5 + 0.5) * size * sign).to(dtype).cuda()
+    v = cache.v_pages[at][:, 0]
+    out, lse, status = attend(cache, q, scale=scale)
+    assert status == 0 and torch.equal(out, v[best].expand(rows, 4, 128))
+    want = (q.double() @ k[best, 0].double() * scale).T
+    # (2^-20 of the terms' magnitudes for the logit, all of one sign here; 2^-22 for the rest)
+    assert ((lse.double() - want).abs() <= (2.0 ** -20 + 2.0 ** -22) * want.abs()).all()
+    k[other] = k[best]
+    cache.k_pages[at] = k
+    out, _, _ = attend(cache, q, scale=scale)
+    both = (v[best].double() + v[other].double()) / 2
+    half = torch.finfo(dtype).eps / 2
+    # a half each, exactly; sums of two in fp32, and the output's rounding
+    assert ((out.double() - both).abs() <= (half + 2.0 ** -22) * both.abs() + 2.0 ** -22 * v[best].double().abs()).all()
