@@ -723,11 +723,11 @@ int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, voi
  * and lse are then undefined, in this call and the ones after it, until
  * compresskv_paged_workspace_init.
  * Logits, softmax sums and outputs are held in fp32; the probabilities enter the
- * product with V rounded once to the dtype (f16: what is below 2^-24 of a row's
- * largest is lost; bf16: they are scaled so that averages of V near its largest
- * number stay finite, and V below 2^-118 times the length, rounded up to a power of
- * two, may be lost).  The results are the same bits on
- * every call with the same shapes, lengths and SMs. */
+ * product with V rounded once to the dtype.  (f16: times 2^7, so that below 2^-21 of a
+ * row's largest they have steps of 2^-31 of it, and below 2^-32 are lost.  bf16: scaled
+ * so that averages of V near its largest number stay finite, and V below 2^-118 times
+ * the length, rounded up to a power of two, may be lost.)  The results are the same
+ * bits on every call with the same shapes, lengths and SMs. */
 int compresskv_paged_attend(const ckv_paged_cache* c, const ckv_paged_queries* a, const void* q,
                             const int32_t* start, void* out, float* lse, void* workspace,
                             size_t workspace_bytes, void* stream);

@@ -63,15 +63,15 @@ def tolerance(dtype, slots, out, lse, parts):
     it rounds: a logit by 2^-20 of its terms' magnitudes (fp32 sums of the tensor
     cores, and the scale), so p by twice that and as much again for the sum of
     exponentials; an exponential and the sums of it by 2^-20; a probability to the
-    dtype, half a step (and for f16, below 2^-14 of the largest, 2^-25 of that);
-    the output's fp32 sums by 2^-23 for every 16 slots; and the output to the
-    dtype."""
+    dtype, half a step (and for f16, which it enters times 2^7, below 2^-21 of the
+    largest, 2^-32 of that); the output's fp32 sums by 2^-23 for every 16 slots; and
+    the output to the dtype."""
     half = torch.finfo(dtype).eps / 2
     logit = parts["mass"] * 2.0 ** -20
     per = (4 * logit + 2.0 ** -19).T[..., None] + half + (slots / 16 + 16) * 2.0 ** -23
     tol = parts["pv"] * per + half * out.abs() + torch.finfo(dtype).smallest_normal * half
     if dtype == torch.float16:
-        tol = tol + parts["sv"] * parts["top"].T[..., None] * 2.0 ** -25
+        tol = tol + parts["sv"] * parts["top"].T[..., None] * 2.0 ** -32
     seen = torch.isfinite(lse)
     ltol = 2 * logit + 2.0 ** -19 + torch.where(seen, lse, 0).abs() * 2.0 ** -22
     return tol, ltol

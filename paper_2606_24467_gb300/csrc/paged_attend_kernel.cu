@@ -250,16 +250,23 @@ __device__ __forceinline__ int limit_of(const PagedAttendParams& p, int pos, int
 }
 __device__ __forceinline__ int tiles_of(int limit) { return max((limit + kTile - 1) / kTile, 1); }
 
-// bf16: p enters times 2^-down, or a sum of p V (2^8 in each of `length` slots, at
-// most) would pass fp32's range where V is large and the output is not; V below
-// 2^(down - 126) may be lost for it.  fp16's V is small enough, and its p has no room.
+// p enters the product with V times 2^-down, and the output leaves it times 2^down.
+// bf16: a sum of p V (2^8 in each of `length` slots, at most) would pass fp32's range
+// where V is large and the output is not; V below 2^(down - 126) may be lost for it.
+// f16: its V is small enough for any sum, and its p has room above: 2^8 times 2^7 is
+// half of its largest number.  Without that, p below 2^-14 of the reference had fewer
+// bits and below 2^-25 none: what 32K slots, each 18 nats below a sink, add up to was
+// off by 42 % (2-norm; 0.4 % so), and slots 16 +- 1 below it by 4 % (0.1 %).
+constexpr float kDownF16 = -7.f;
+static_assert(kGrowth - kDownF16 < 16.f, "p is below 2^16 in f16");
 template <bool kBf16>
 __device__ __forceinline__ float down_of(int length) {
-  return kBf16 ? static_cast<float>(static_cast<int>(kGrowth) + 32 - __clz(length)) : 0.f;
+  return kBf16 ? static_cast<float>(static_cast<int>(kGrowth) + 32 - __clz(length)) : kDownF16;
 }
 template <bool kBf16>
 __device__ __forceinline__ float up_of(int length) {  // 2^down
-  return kBf16 ? __int_as_float((127 + static_cast<int>(kGrowth) + 32 - __clz(length)) << 23) : 1.f;
+  return kBf16 ? __int_as_float((127 + static_cast<int>(kGrowth) + 32 - __clz(length)) << 23)
+               : __int_as_float((127 + static_cast<int>(kDownF16)) << 23);
 }
 
 // A sequence, as a lane of the work-finding warp sees it.

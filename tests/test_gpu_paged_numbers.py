@@ -86,3 +86,26 @@ def test_logits_far_from_zero(dtype, size, scale, rows, length, sign):
     half = torch.finfo(dtype).eps / 2
     # a half each, exactly; sums of two in fp32, and the output's rounding
     assert ((out.double() - both).abs() <= (half + 2.0 ** -22) * both.abs() + 2.0 ** -22 * v[best].double().abs()).all()
+
+
+@pytest.mark.parametrize("rows, logit, sd", [(1, 18.0, 0.0), (1, 16.0, 1.0), (3, 17.0, 0.5), (130, 18.0, 0.0),
+                                             (130, 16.0, 1.0)])
+def test_f16_keeps_the_tail_behind_a_sink(rows, logit, sd):
+    """A sink with 99 % of the mass or more and V = 0: the output is what tens of thousands
+    of slots with probabilities about 2^-25 of the largest add up to.  (As many heads as a
+    cache has, so that pieces are long: each has a reference of its own.)"""
+    length, h = 32768, 64
+    cache = make([length], h, 256, HF)
+    at = rows_at(cache, length)
+    gen = torch.Generator().manual_seed(1)
+    u = torch.randn(128, generator=gen)
+    one = u * 128 ** 0.5 / u.dot(u)  # a logit of 1
+    k = torch.randn((length, 1), generator=gen) * sd * one
+    k[0] = one * logit
+    cache.k_pages[at] = k.to(HF).cuda()[:, None]
+    v = torch.rand((length, 128), generator=gen) + 0.5
+    v[0] = 0.0
+    cache.v_pages[at] = v.to(HF).cuda()[:, None]
+    q = u.to(HF).cuda().expand(rows, h, 128).contiguous()
+    out, lse, _ = attend(cache, q)
+    check(cache, q, out, lse, [0, rows])
