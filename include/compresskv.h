@@ -585,8 +585,10 @@ int compresskv_rope_init(ckv_rope* r, int32_t rot_dim, int32_t interleaved, cons
 /* Rows to rotate: q [rows][num_q_heads][128] and k [rows][num_k_heads][128],
  * head_dim contiguous, bases 16-byte aligned, strides (elements) multiples of 8
  * and not negative; outputs the same shapes.  Outputs whose rows overlap are
- * refused, and so is an output that shares memory with its input otherwise
- * than by being it (same address and strides: in place). */
+ * refused, and so is an output whose range of memory meets its input's otherwise
+ * than by being it (same address and strides: in place).  An output must not share
+ * memory with another tensor of the call; where q's rows and k's have one token
+ * stride and meet (q and k in a fused projection do not), the call is refused. */
 typedef struct ckv_rope_rows {
   int32_t rows;
   int32_t num_q_heads;      /* 0..256 */
@@ -622,8 +624,10 @@ int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32
  * is written for it, and its attention sees nothing.  Slots behind the length may
  * hold anything, NaN among it.
  * Sequences may share pages to read; where two rows of an append go to one slot,
- * it holds either.  Calls that use one workspace must not overlap on the GPU, and
- * neither must two calls of which one writes what the other uses. */
+ * it holds channels of both.  No output of a call, nor pages that it writes, may share
+ * memory with another tensor of that call (K's pool may be V's, for the same rows).
+ * Calls that use one workspace must not overlap on the GPU, and neither must two
+ * calls of which one writes what the other uses. */
 typedef struct ckv_paged_cache {
   int32_t batch;            /* sequences, 1..512 */
   int32_t num_kv_heads;     /* 1..64 */

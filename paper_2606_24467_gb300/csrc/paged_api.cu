@@ -72,6 +72,43 @@ int check_rows(int rows, int heads, const void* in, int64_t in_token, int64_t in
   return CKV_OK;
 }
 
+// Whether a row of one set of rows ([rows][heads][128]) shares an element with one of
+// another.  (With token strides that differ: not told.)
+bool rows_meet(int rows, const void* a, int heads_a, int64_t token_a, int64_t head_a, const void* b, int heads_b,
+               int64_t token_b, int64_t head_b) {
+  if (heads_a == 0 || heads_b == 0) return false;
+  const int64_t span_a = static_cast<int64_t>(span_of(1, heads_a, 0, head_a));
+  const int64_t span_b = static_cast<int64_t>(span_of(1, heads_b, 0, head_b));
+  if (!share(a, 2 * span_of(rows, heads_a, token_a, head_a), b, 2 * span_of(rows, heads_b, token_b, head_b)))
+    return false;
+  if (rows > 1 && token_a != token_b) return false;
+  const int64_t off = (static_cast<int64_t>(reinterpret_cast<uintptr_t>(b)) -
+                       static_cast<int64_t>(reinterpret_cast<uintptr_t>(a))) / 2;
+  const int64_t most = rows - 1, token = most ? token_a : 0;
+  if (token > 0) {  // side by side within a token, as in a fused projection
+    const int64_t at = (off % token + token) % token;
+    if (at >= span_a && at + span_b <= token) return false;
+  }
+  // of two heads x apart: whether some tokens' rows meet
+  auto near = [&](int64_t x) {
+    const int64_t at = token ? -x / token : 0;
+    for (int64_t d = at - 1; d <= at + 1; ++d) {
+      const int64_t gap = x + std::min(std::max(d, -most), most) * token;
+      if (gap < kHeadDim && gap > -kHeadDim) return true;
+    }
+    return false;
+  };
+  if (head_a == head_b) {
+    for (int i = 1 - heads_a; i < heads_b; ++i)
+      if (near(off + i * head_a)) return true;
+    return false;
+  }
+  for (int i = 0; i < heads_a; ++i)
+    for (int j = 0; j < heads_b; ++j)
+      if (near(off + j * head_b - i * head_a)) return true;
+  return false;
+}
+
 RowSet row_set(const void* in, int64_t in_token, int64_t in_head, void* out, int64_t out_token, int64_t out_head) {
   return {static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), in_token, in_head, out_token, out_head};
 }
@@ -189,6 +226,13 @@ int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32
   if (x->num_k_heads && (rc = check_rows(x->rows, x->num_k_heads, k, x->k_token_stride, x->k_head_stride, k_out,
                                          x->k_out_token_stride, x->k_out_head_stride)) != CKV_OK)
     return rc;
+  if (rows_meet(x->rows, q_out, x->num_q_heads, x->q_out_token_stride, x->q_out_head_stride, k, x->num_k_heads,
+                x->k_token_stride, x->k_head_stride) ||
+      rows_meet(x->rows, q_out, x->num_q_heads, x->q_out_token_stride, x->q_out_head_stride, k_out, x->num_k_heads,
+                x->k_out_token_stride, x->k_out_head_stride) ||
+      rows_meet(x->rows, k_out, x->num_k_heads, x->k_out_token_stride, x->k_out_head_stride, q, x->num_q_heads,
+                x->q_token_stride, x->q_head_stride))
+    return CKV_ERR_INVALID_ARG;
   static thread_local RopeParams P;
   std::memset(&P, 0, sizeof(P));
   P.rope = rope_table(r);
@@ -232,6 +276,10 @@ int compresskv_paged_append(const ckv_paged_cache* c, const ckv_paged_rows* r, c
     if (r->num_q_heads && (rc = check_rows(P.rows, r->num_q_heads, q, r->q_token_stride, r->q_head_stride, q_out,
                                            r->q_out_token_stride, r->q_out_head_stride)) != CKV_OK)
       return rc;
+    for (const void* from : {k, v})
+      if (rows_meet(P.rows, q_out, r->num_q_heads, r->q_out_token_stride, r->q_out_head_stride, from,
+                    c->num_kv_heads, r->kv_token_stride, r->kv_head_stride))
+        return CKV_ERR_INVALID_ARG;
   }
   P.c = device_cache(c);
   if (rope)
