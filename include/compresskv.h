@@ -618,11 +618,13 @@ int compresskv_rope_apply(const ckv_rope* r, const ckv_rope_rows* x, const int32
  * table[s][0..], and its token (slot) j is row j % page_size of page
  * table[s][j / page_size].  Element (page, slot, head, c) of K is at k_pages +
  * page*page_stride + slot*slot_stride + head*head_stride + c, and V's likewise.
- * lengths[s] slots are in use.  Table entries behind them are not read.  A
- * length or first row beyond what the table holds (table_width * page_size)
- * counts as that, and a negative one marks a sequence that is not there: nothing
- * is written for it, and its attention sees nothing.  Slots behind the length may
- * hold anything, NaN among it.
+ * lengths[s] slots are in use.  Table entries behind them (and behind the rows of
+ * an append) are not read.  A length, or the start of an append, beyond what the
+ * table holds (table_width * page_size) counts as that.  A negative length, or a
+ * negative start of an append or a gather, marks a sequence that is not there:
+ * nothing is written for it, and its attention sees nothing.  (The start of
+ * compresskv_paged_attend is a place, and may be negative.)  Slots behind the length
+ * may hold anything, NaN among it.
  * Sequences may share pages to read; where two rows of an append go to one slot,
  * it holds channels of both.  No output of a call, nor pages that it writes, may share
  * memory with another tensor of that call (K's pool may be V's, for the same rows).
@@ -713,8 +715,8 @@ int compresskv_paged_workspace_init(void* workspace, size_t workspace_bytes, voi
  *   z_j = scale * q . K_j,  p = softmax of z over the visible slots,
  *   out = sum_j p_j V_j (rounded to the dtype),  lse = log sum_j exp(z_j).
  * Query token i of sequence s stands at slot start[s] + i; start: optional
- *   device int32 [batch]; NULL: the sequence's newest slots, lengths[s] - rows.
- *   It sees the slots in use up to its own (causal) or all in use.  A token that
+ *   device int32 [batch], any value; NULL: the sequence's newest slots, lengths[s] -
+ *   rows.  It sees the slots in use up to its own (causal) or all in use.  A token that
  *   sees none gives out = 0 and lse = -infinity; one that sees slots, all with a
  *   logit of -infinity, gives NaN (0 / 0) and lse = -infinity.
  * lse: optional device float [num_q_heads][rows]: with equal rows a sequence,
