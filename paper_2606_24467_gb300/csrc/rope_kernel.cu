@@ -24,7 +24,11 @@ constexpr int kLanes = 8;                       // lanes of a head
 constexpr int kPairsLane = kRopePairs / kLanes; // 8
 constexpr int kUnroll = 2;                      // heads of a lane in flight
 constexpr int kFill = 2432;                     // warps that the GPU is to have where there is enough for them
-constexpr int kFewRows = 16;                    // rows of a sequence that one CTA appends
+// Rows of a sequence that one CTA appends where the start is the length itself; more take
+// a second launch for the lengths.  In a graph, 32 + 8 heads with Q, 1 / 8 / 64 sequences
+// of one row: 3.3 / 3.6 / 3.5 us so, 4.1 / 4.5 / 4.3 in two launches; of two rows: 5.0 / 5.1 /
+// 5.1 and 4.3 / 4.2 / 4.9; of 16 rows: 25 / 25 / 26 and 4.5 / 4.9 / 8.2.
+constexpr int kFewRows = 1;
 
 // Where a lane's eight pairs are.
 enum Layout {
