@@ -69,11 +69,12 @@ constexpr int kPagedMaxCtas = 160;
 // Chunks.  All work is a line, an item (two tiles of rows of a KV head) after another;
 // each takes its tiles and kPagedPiece, what its beginning and end cost.  Where that is
 // less than kPagedFew of the longest items an SM, the line is cut into equal runs, one an
-// SM: 501 tokens after 9000 to 16000 take 148 us so, 172 with items cut into blocks of
-// slots that SMs take in turn; 777 after 3000 to 20000, four times, 537 and 605.
-// Else items are whole and taken in turn, as CTAs that run together then read the same
-// tiles (4096 tokens after 128K: 5000 us, in runs 6100), but for the last ones, in
-// kPagedRuns runs an SM: 8191 tokens from the first on 368 us so, 380 all in runs.
+// SM: 501 tokens after 9000 to 16000 take 147 us so, 170 with items whole but for the
+// last; 777 after 3000 to 20000, four times, 480 and 580.  Else items are whole and taken
+// in turn, as CTAs that run together then read the same tiles, but for the last ones, in
+// kPagedRuns runs an SM: 4096 tokens after 128K take 4980 us so, 5840 all in runs; eight
+// times 2000 from the first on 270 and 350; 8191 once 365 and 373.  (Each side by side on
+// one GPU, L2 flushed; from one GPU to another these times differ by 5 %.)
 // No piece has fewer than kPagedLeast tiles of an item that has more (16: 160 us for the
 // first), no run less than kPagedShare of the line.  The results of at most kPagedSlots
 // pieces, two a run, wait to be joined.
