@@ -3,7 +3,6 @@
 import pytest
 import torch
 
-import paper_2606_24467_gb300 as ckv  # noqa: F401  (the tests' helpers use it)
 from test_gpu_paged import BF, HF, NAN, attend, check, make, queries
 
 pytestmark = pytest.mark.gpu
@@ -19,7 +18,8 @@ def rows_at(cache, length, s=0):
 @pytest.mark.parametrize("rows, length", [(1, 100), (1, 40000), (90, 40000), (200, 300), (200, 40000)])
 def test_weights_that_vanish_carry_what_is_not_finite(rows, length):
     """Half of the slots 181 nats below the others, one of them with a NaN or an infinity
-    in V: it reaches the output (0 times it is NaN), whether a unit is one piece or several that are joined."""
+    in V: it reaches the output (0 times it is NaN), whether a unit is one piece or several
+    that are joined."""
     cache = make([length], 2, 64)
     at = rows_at(cache, length)
     sign = torch.where(torch.arange(length, device="cuda") < length // 2, -1.0, 1.0)
